@@ -446,6 +446,121 @@ lazymar_status lazymar_head_sync(lazymar_head *hd, void *stream);
  * Returns INVALID_ARG unless 1 <= n_steps <= n_train. */
 lazymar_status lazymar_head_schedule(int n_train, int n_steps, int32_t *kept, float *consts);
 
+/* ------------------------------------------------------------------------
+ * Training a block with 8-bit activations. The paper trains nothing; these
+ * entry points are what tuning a block of the transformer needs next to the
+ * decoding step: LayerNorm's gradient, activations kept for the backward pass
+ * in 8 bits, and 8-bit matrix products with a scale for each block of 128.
+ * Device pointers only; no call allocates; a workspace is the caller's.
+ *
+ * The 8-bit format ("block8") of a [rows, cols] tensor: E4M3 bytes q with row
+ * stride ldq and one power-of-two scale for each row and block of 128 columns
+ * (the last one may be shorter), held as its exponent + 127 at
+ * scale[(col / 128) * lds + row]; value = q * 2^(scale - 127). A block's
+ * exponent is the smallest e >= -126 with max |x| <= 448 * 2^e over its finite
+ * values, q = E4M3(x * 2^-e), to nearest even; infinities and NaN become NaN.
+ * The values are exact in bf16 (numbers that round to 2^128 read back as
+ * infinity). A weight matrix [N, K] has one scale for each
+ * 128 x 128 block, at scale[(k / 128) * lds + n / 128].
+ * q is 16-byte aligned, ldq a multiple of 16 and >= cols (bytes between cols
+ * and ldq are neither read as values nor written); lds >= rows (weights:
+ * >= ceil(N / 128)).
+ *
+ * Strides (ld*) count elements; fp32 and bf16 tensors may have any stride >=
+ * their columns and any element alignment (rows on boundaries of four elements
+ * are faster). Sums, statistics and parameter gradients are fp32. Results are
+ * the same from call to call (no atomics). accumulate = 1 adds to the
+ * parameter gradients instead of overwriting them.
+ * ------------------------------------------------------------------------ */
+typedef struct lazymar_block8 {
+  void* q;
+  uint8_t* scale;
+  int ldq;
+  int lds;
+} lazymar_block8;
+
+/* LayerNorm over D of x [M, ldx] (fp32 or bf16) with its statistics:
+ *   mean[m], rstd[m] = 1 / sqrt(var + eps)   (fp32, each may be NULL)
+ *   y = (x - mean) rstd g + b                (g, b fp32 [D], each may be NULL)
+ * y goes to y [M, ldy] (fp32 or bf16; may be NULL) and / or y8 (may be NULL),
+ * the operand of lazymar_block8_linear; x8 (may be NULL) receives x itself, the
+ * checkpoint for lazymar_layernorm_backward. At least one of y, y8, x8 and the
+ * statistics is given. 1 <= D <= 8192. */
+lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, int ldx, const float* g, const float* b,
+                                         int y_dtype, void* y, int ldy, const lazymar_block8* y8,
+                                         const lazymar_block8* x8, float* mean, float* rstd, int M, int D, float eps,
+                                         void* stream);
+
+/* Its gradient. With xh = (x - mean) rstd and a = dy g:
+ *   dx = rstd (a - mean_D(a) - xh mean_D(a xh)) [+ dres]
+ *   dg = sum_m dy xh,  db = sum_m dy
+ * dy [M, lddy] fp32 or bf16; the input either as x [M, ldx] (fp32 or bf16) or as
+ * its checkpoint x8 (exactly one of the two); mean, rstd from the forward
+ * pass; g may be NULL. dres [M, lddres] fp32 (may be NULL; the residual
+ * stream's gradient) is added; dx [M, lddx] fp32 or bf16 may be dres itself.
+ * dg and db [D] fp32 are both given or both NULL. workspace:
+ * lazymar_layernorm_backward_workspace(M, D) bytes, 16-byte aligned, not needed
+ * without dg and db. */
+size_t lazymar_layernorm_backward_workspace(int M, int D);
+lazymar_status lazymar_layernorm_backward(int dy_dtype, const void* dy, int lddy, int x_dtype, const void* x, int ldx,
+                                          const lazymar_block8* x8, const float* mean, const float* rstd,
+                                          const float* g, const float* dres, int lddres, int dx_dtype, void* dx,
+                                          int lddx, float* dg, float* db, int accumulate, int M, int D,
+                                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* x [rows, ldx] (fp32 or bf16) to block8, and back. */
+lazymar_status lazymar_block8_pack(int dtype, const void* x, int ldx, const lazymar_block8* q, int rows, int cols,
+                                   void* stream);
+lazymar_status lazymar_block8_unpack(const lazymar_block8* q, int dtype, void* x, int ldx, int rows, int cols,
+                                     void* stream);
+
+/* A weight matrix w [N, ldw] (fp32 or bf16) to block8 with 128 x 128 blocks:
+ * q [N, K], the operand of the forward product, and / or its transpose qt
+ * [K, N] (the same bytes and scales), that of the input gradient. Either may be
+ * NULL. */
+lazymar_status lazymar_block8_pack_weight(int dtype, const void* w, int ldw, const lazymar_block8* q,
+                                          const lazymar_block8* qt, int N, int K, void* stream);
+
+/* Gradient through GELU (erf form) from the checkpoint u [rows, cols] of its
+ * input: du = da * GELU'(u), da [rows, ldda] fp32 or bf16. u NULL: du = da (the
+ * gradient of a linear layer's output). du goes to du [rows, lddu] (fp32 or
+ * bf16; may be NULL) and / or du8 (may be NULL; the operand of the input
+ * gradient's product); db [cols] fp32 (may be NULL) = sum over the rows of du,
+ * the bias gradient. workspace:
+ * lazymar_block8_gelu_backward_workspace(rows, cols) bytes, 16-byte aligned,
+ * not needed without db. */
+size_t lazymar_block8_gelu_backward_workspace(int rows, int cols);
+lazymar_status lazymar_block8_gelu_backward(int dtype, const void* da, int ldda, const lazymar_block8* u, int du_dtype,
+                                            void* du, int lddu, const lazymar_block8* du8, float* db, int accumulate,
+                                            int rows, int cols, void* workspace, size_t workspace_bytes,
+                                            void* stream);
+
+/* y = a w^T + bias with a [M, K] and w [N, K] in block8 (w with 128 x 128
+ * blocks), accumulated in fp32 on the 8-bit tensor cores with the scales
+ * applied there (kind::mxf8f6f4); bias fp32 [N] (may be NULL).
+ *   LAZYMAR_EPI_BIAS      out = y
+ *   LAZYMAR_EPI_GELU      out = GELU(y) (erf form)
+ *   LAZYMAR_EPI_RESIDUAL  out = residual + y, residual [M, ldr] and out fp32
+ *                         (out may be residual itself)
+ * out [M, ldo] fp32 or bf16 (may be NULL) and / or out8 [M, N] (may be NULL; not
+ * for RESIDUAL); u8 [M, N] (GELU only, may be NULL) receives y, the checkpoint
+ * for lazymar_block8_gelu_backward. Any M, N >= 0 and K >= 1. */
+lazymar_status lazymar_block8_linear(int epilogue, const lazymar_block8* a, const lazymar_block8* w,
+                                     const float* bias, const float* residual, int ldr, int out_dtype, void* out,
+                                     int ldo, const lazymar_block8* out8, const lazymar_block8* u8, int M, int N,
+                                     int K, void* stream);
+
+/* Weight gradient of a linear layer from its output's gradient and the 8-bit
+ * checkpoint of its input: dw[n, k] (+)= sum_m dy[m, n] x[m, k]; dy [M, lddy]
+ * bf16 (16-byte aligned, lddy a multiple of 8), x block8 [M, K], dw [N, lddw]
+ * fp32. Products of bf16 values (the checkpoint's are exact there), summed in
+ * fp32. workspace: lazymar_block8_wgrad_workspace(M, N, K) bytes, 16-byte
+ * aligned. */
+size_t lazymar_block8_wgrad_workspace(int M, int N, int K);
+lazymar_status lazymar_block8_wgrad(const void* dy, int lddy, const lazymar_block8* x, float* dw, int lddw,
+                                    int accumulate, int M, int N, int K, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
 /* Per kernel class: kernel launches, algorithmic flops and bytes, and (while
  * profiling is on) device time from CUDA events recorded around each call on
  * its stream (timed_launches counts those event pairs).

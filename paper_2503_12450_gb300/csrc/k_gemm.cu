@@ -883,6 +883,10 @@ bool make_tmap_bf16(CUtensorMap* m, const void* base, uint64_t inner, uint64_t o
                     uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swz) {
   return make_tmap_2d(CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, m, base, inner, outer, pitch_bytes, box_inner, box_outer, swz);
 }
+bool make_tmap_u8(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint64_t pitch_bytes,
+                  uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swz) {
+  return make_tmap_2d(CU_TENSOR_MAP_DATA_TYPE_UINT8, m, base, inner, outer, pitch_bytes, box_inner, box_outer, swz);
+}
 
 bool gemm_supported(int dtype, int M, int N, int K, const GemmEpi& epi, const char** why) {
   if (M < 0 || N <= 0 || K <= 0) { *why = "M >= 0, N > 0, K > 0 required"; return false; }

@@ -1,0 +1,547 @@
+// The block-scaled 8-bit product (lazymar_block8_linear):
+//   y[m, n] = sum_k a[m, k] 2^ea[m, k/128] w[n, k] 2^ew[n/128, k/128] + bias[n]
+// with E4M3 a and w, fp32 accumulation, and bias, GELU or an fp32 residual,
+// fp32, bf16 and / or 8-bit outputs in the epilogue.
+//
+// The scales are powers of two, so the tensor cores apply them themselves:
+// kind::mxf8f6f4 takes one exponent byte per row and 32 columns of K from tensor
+// memory, and a block of 128 is four equal ones. A 32-bit column of tensor
+// memory holds four bytes a row; here they are the scales of four K blocks of
+// 128, and the instruction descriptor names the byte. So the scales of 512
+// columns of K are four tensor-memory columns for the 128 rows of a (lane =
+// row % 32, column = row / 32, the same in each quarter of the lanes) and eight for
+// 256 rows of w, written by tcgen05.st straight from the scale bytes.
+#include <cuda.h>
+
+#include <cstring>
+
+#include "block8.cuh"
+
+namespace lm {
+
+// k_gemm.cu
+bool make_tmap_u8(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint64_t pitch_bytes,
+                  uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swz);
+
+namespace l8 {
+
+constexpr int BM = 128;               // rows of a CTA's tile
+constexpr int KB_BYTES = 128;         // K of a pipeline stage: one scale block, one swizzle atom
+constexpr int STAGES = 6;
+constexpr uint32_t A_BYTES = BM * KB_BYTES;
+constexpr uint32_t B_BYTES = 128 * KB_BYTES;  // rows of w in a CTA's shared memory: the tile's, or a pair's half
+constexpr uint32_t STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr int EPI_WARPS = 8;
+constexpr uint32_t STG_BYTES = 32 * 128;      // a warp's staging: 32 rows of 128 bytes
+constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STG_BYTES + 512;
+constexpr int THREADS = 512;  // warps 0 TMA, 1 MMA, 4-7 scales, 8-15 epilogue
+// Registers: 512 threads launch with 128; the epilogue holds a row's 128 values.
+constexpr int REGS_EPI = 200, REGS_REST = 48;
+static_assert((REGS_EPI + REGS_REST) * 256 <= 128 * THREADS, "the register split must fit what the launch holds");
+constexpr int SF_SLOTS = 4;           // scale slots of 16 tensor-memory columns: 4 of a, 8 of w
+constexpr uint32_t SF_BASE = 256;     // behind the accumulator's columns
+
+struct Params {
+  const uint8_t *a_scale, *w_scale;
+  int lds_a, lds_w;
+  int epilogue, M, N, K;
+  const float* bias;
+  const float* residual;
+  int ldr;
+  void* out;
+  int ldo, out_dtype;
+  uint8_t *out8, *u8;  // may be NULL
+  int ldout8, ldu8;
+  uint8_t *out8_scale, *u8_scale;
+  int lds_out8, lds_u8;
+  bool bias_vec, out_vec, res_vec;
+};
+
+// Instruction descriptor of kind::mxf8f6f4: E4M3 operands (format 0), K-major,
+// N / 8 at bit 17, UE8M0 scales (bit 23), M / 16 at bit 24; the byte of the scale
+// columns at bit 29 (a) and 4 (w).
+__device__ __forceinline__ constexpr uint32_t idesc(int m, int n, uint32_t sf) {
+  return (sf << 4) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24) | (sf << 29);
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t ad, uint64_t bd, uint32_t id, uint32_t sfa, uint32_t sfb,
+                                    uint32_t accumulate) {
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+            d),
+        "l"(ad), "l"(bd), "r"(id), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+            d),
+        "l"(ad), "l"(bd), "r"(id), "r"(sfa), "r"(sfb), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ uint64_t sw128_desc(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) |
+         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&r)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3])
+               : "memory");
+}
+
+// A row's 128 values to E4M3 words and the scale byte. The scale is that of the
+// finite values; infinities become NaN.
+__device__ __forceinline__ uint32_t quantize_row(const float (&v)[128], uint32_t (&w)[32]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 128; i += 2) m = fmax3(m, fabsf(v[i]), fabsf(v[i + 1]));
+  uint32_t amax = __float_as_uint(m);
+  const bool special = amax >= 0x7F800000u;
+  if (special) {
+    amax = 0;
+#pragma unroll
+    for (int i = 0; i < 128; ++i) {
+      const uint32_t b = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+      amax = max(amax, b < 0x7F800000u ? b : 0u);
+    }
+  }
+  const uint32_t byte = block8_exp(amax);
+  const float s = block8_inv(byte);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    w[i] = e4m3x4(v[4 * i] * s, v[4 * i + 1] * s, v[4 * i + 2] * s, v[4 * i + 3] * s);
+    if (special) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if ((__float_as_uint(v[4 * i + j]) & 0x7F800000u) == 0x7F800000u) w[i] |= 0x7Fu << (8 * j);
+    }
+  }
+  return byte;
+}
+
+}  // namespace l8
+
+// PAIR: two CTAs (a cluster of two) share a tile of 256 x 256, each its own 128
+// rows of a and half of the tile's rows of w; the even CTA issues the MMAs for
+// both. Otherwise tiles of 128 x 128 on single CTAs.
+// Accumulator: 256 columns, a pair's whole tile or two single tiles in turn. The
+// epilogue warps (two for each lane quarter, one for each 128 columns) take a
+// row's 128 columns into registers and hand the accumulator back at once.
+template <bool PAIR>
+__global__ void __launch_bounds__(l8::THREADS, 1)
+    linear8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                   const __grid_constant__ CUtensorMap tmO8, const __grid_constant__ CUtensorMap tmU8,
+                   const l8::Params p, unsigned* err) {
+  using namespace l8;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sA = smem;
+  uint8_t* sB = smem + STAGES * A_BYTES;
+  uint8_t* sStg = smem + STAGES * STAGE_BYTES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sStg + EPI_WARPS * STG_BYTES);
+  uint64_t* empty = full + STAGES;
+  uint64_t* sf_full = empty + STAGES;
+  uint64_t* sf_empty = sf_full + SF_SLOTS;
+  uint64_t* acc_full = sf_empty + SF_SLOTS;
+  uint64_t* acc_empty = acc_full + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int TM = PAIR ? 2 * BM : BM, TN = PAIR ? 256 : 128;
+  const int num_n = (p.N + TN - 1) / TN, tiles = ((p.M + TM - 1) / TM) * num_n;
+  const int KB = (p.K + KB_BYTES - 1) / KB_BYTES;
+  const int rank = PAIR ? (int)cluster_ctarank() : 0;
+  const int first = PAIR ? (int)blockIdx.x / 2 : (int)blockIdx.x, step = PAIR ? (int)gridDim.x / 2 : (int)gridDim.x;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < SF_SLOTS; ++s) {
+      mbar_init(&sf_full[s], PAIR ? 8 : 4);
+      mbar_init(&sf_empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&acc_full[b], 1);
+      mbar_init(&acc_empty[b], PAIR ? 2 * EPI_WARPS : EPI_WARPS / 2);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+    prefetch_tmap(&tmA);
+    prefetch_tmap(&tmB);
+  }
+  if (warp == 1) {
+    if (PAIR) {
+      tmem_alloc_pair(tmem_slot, 512);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(tmem_slot, 512);
+      tmem_relinquish();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_wait();
+  pdl_trigger();
+
+  if (warp < 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_REST));
+    if (warp == 0 && lane == 0) {
+      // ---------------- TMA producer ----------------
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        const int m0 = (tile / num_n) * TM + rank * BM, n0 = (tile % num_n) * TN + rank * 128;
+        for (int kb = 0; kb < KB; ++kb) {
+          if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, err)) { ok = false; break; }
+          uint8_t *da = sA + stage * A_BYTES, *db = sB + stage * B_BYTES;
+          if (PAIR) {
+            if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * STAGE_BYTES);
+            const uint32_t bar = cluster_map(smem_u32(&full[stage]), 0);
+            tma_load_2d_pair(&tmA, bar, da, kb * KB_BYTES, m0);
+            tma_load_2d_pair(&tmB, bar, db, kb * KB_BYTES, n0);
+          } else {
+            mbar_arrive_expect_tx(&full[stage], STAGE_BYTES);
+            tma_load_2d(&tmA, &full[stage], da, kb * KB_BYTES, m0);
+            tma_load_2d(&tmB, &full[stage], db, kb * KB_BYTES, n0);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+    } else if (warp == 1 && rank == 0) {
+      // ---------------- MMA issuer (of a pair: the even CTA's) ----------------
+      const bool lead = elect_one();
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        const bool done = mbar_wait(bar, parity, abort_flag, err);
+        return (bool)__all_sync(0xffffffffu, done);
+      };
+      int stage = 0, slot = 0, it = 0;
+      uint32_t phase = 0, sf_phase = 0;
+      bool ok = true;
+      for (int tile = first; tile < tiles && ok; tile += step, ++it) {
+        const int buf = PAIR ? 0 : it & 1;
+        const uint32_t use = PAIR ? (uint32_t)it & 1u : (uint32_t)(it >> 1) & 1u;
+        if (!wait(&acc_empty[buf], use ^ 1u)) break;
+        tc_fence_after();
+        const uint32_t d = tmem_base + (uint32_t)(buf * 128);
+        for (int kb = 0; kb < KB; ++kb) {
+          if ((kb & 3) == 0 && !(ok = wait(&sf_full[slot], sf_phase))) break;
+          if (!(ok = wait(&full[stage], phase))) break;
+          tc_fence_after();
+          const uint64_t a0 = sw128_desc(smem_u32(sA + stage * A_BYTES));
+          const uint64_t b0 = sw128_desc(smem_u32(sB + stage * B_BYTES));
+          const uint32_t sf = tmem_base + SF_BASE + (uint32_t)(slot * 16);
+          const uint32_t id = idesc(TM, TN, (uint32_t)(kb & 3));
+          if (lead) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma<PAIR>(d, a0 + 2 * k, b0 + 2 * k, id, sf, sf + 4, (kb | k) != 0 ? 1u : 0u);
+            if (PAIR) umma_commit_pair(&empty[stage]);
+            else umma_commit(&empty[stage]);
+            if ((kb & 3) == 3 || kb == KB - 1) {
+              if (PAIR) umma_commit_pair(&sf_empty[slot]);
+              else umma_commit(&sf_empty[slot]);
+            }
+          }
+          __syncwarp();
+          if ((kb & 3) == 3 || kb == KB - 1)
+            if (++slot == SF_SLOTS) { slot = 0; sf_phase ^= 1u; }
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        }
+        if (ok && lead) {
+          if (PAIR) umma_commit_pair(&acc_full[0]);
+          else umma_commit(&acc_full[buf]);
+        }
+        __syncwarp();
+      }
+    } else if (warp >= 4) {
+      // ---------------- scales: global memory to tensor memory ----------------
+      const uint32_t lane_quarter = (uint32_t)((warp & 3) * 32) << 16;
+      const int nblk = (p.N + kBlk - 1) / kBlk;
+      int slot = 0;
+      uint32_t sf_phase = 0;
+      bool ok = true;
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        const int m0 = (tile / num_n) * TM + rank * BM, b0 = (tile % num_n) * (TN / kBlk);
+        for (int kb0 = 0; kb0 < KB; kb0 += 4) {
+          uint32_t wa[4] = {0, 0, 0, 0}, wb[TN / kBlk];
+#pragma unroll
+          for (int h = 0; h < TN / kBlk; ++h) wb[h] = 0;
+          const int here = min(4, KB - kb0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (j < here) {
+              const uint8_t* sa = p.a_scale + (size_t)(kb0 + j) * p.lds_a;
+              const uint8_t* sw = p.w_scale + (size_t)(kb0 + j) * p.lds_w;
+#pragma unroll
+              for (int c = 0; c < 4; ++c) wa[c] |= (uint32_t)sa[min(m0 + 32 * c + lane, p.M - 1)] << (8 * j);
+#pragma unroll
+              for (int h = 0; h < TN / kBlk; ++h) wb[h] |= (uint32_t)sw[min(b0 + h, nblk - 1)] << (8 * j);
+            }
+          }
+          const bool done = mbar_wait(&sf_empty[slot], sf_phase ^ 1u, abort_flag, err);
+          if (!__all_sync(0xffffffffu, done)) { ok = false; break; }
+          const uint32_t t = tmem_base + lane_quarter + SF_BASE + (uint32_t)(slot * 16);
+          tc_fence_after();
+          tmem_st4(t, wa);
+#pragma unroll
+          for (int h = 0; h < TN / kBlk; ++h) {
+            const uint32_t w4[4] = {wb[h], wb[h], wb[h], wb[h]};
+            tmem_st4(t + 4 + 4 * h, w4);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (PAIR) mbar_arrive_cluster(cluster_map(smem_u32(&sf_full[slot]), 0));
+            else mbar_arrive(&sf_full[slot]);
+          }
+          if (++slot == SF_SLOTS) { slot = 0; sf_phase ^= 1u; }
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------- epilogue ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
+    const int quarter = warp & 3, unit = (warp - 8) >> 2;  // lane quarter, 128 columns of the accumulator
+    uint8_t* stg = sStg + (warp - 8) * STG_BYTES;
+    int it = 0;
+    for (int tile = first; tile < tiles; tile += step, ++it) {
+      // single CTAs: the tiles alternate between the two units
+      if (!PAIR && (it & 1) != unit) continue;
+      const uint32_t use = PAIR ? (uint32_t)it & 1u : (uint32_t)(it >> 1) & 1u;
+      const int rbase = (tile / num_n) * TM + rank * BM + quarter * 32;
+      const int n0 = (tile % num_n) * TN + (PAIR ? unit * 128 : 0);
+      const bool done = mbar_wait(&acc_full[PAIR ? 0 : unit], use, abort_flag, err);
+      if (!__all_sync(0xffffffffu, done)) break;
+      tc_fence_after();
+      float v[128];
+      {
+        const uint32_t t = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(unit * 128);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t r[32];
+          tmem_ld32(t + 32 * c, r);
+          tmem_wait_ld_regs(r);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[32 * c + i] = __uint_as_float(r[i]);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (PAIR) mbar_arrive_cluster(cluster_map(smem_u32(&acc_empty[0]), 0));
+        else mbar_arrive(&acc_empty[unit]);
+      }
+      if (n0 >= p.N || rbase >= p.M) continue;
+      const int row = rbase + lane;
+      if (p.bias) {
+        if (p.bias_vec && n0 + 128 <= p.N) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const float4 b = *reinterpret_cast<const float4*>(p.bias + n0 + 4 * i);
+            v[4 * i] += b.x; v[4 * i + 1] += b.y; v[4 * i + 2] += b.z; v[4 * i + 3] += b.w;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 128; ++i)
+            if (n0 + i < p.N) v[i] += p.bias[n0 + i];
+        }
+      }
+      // a row's 128 E4M3 bytes: staged with the TMA's 128-byte swizzle, one store
+      // of 32 rows. TMA writes whole 16-byte pieces, so a last piece that the
+      // tensor does not fill leaves by plain stores.
+      auto put8 = [&](const CUtensorMap* tm, uint8_t* q, int ldq, uint8_t* scale, int lds) {
+        uint32_t w[32];
+        const uint32_t byte = quantize_row(v, w);
+        if (row < p.M) scale[(size_t)(n0 / kBlk) * lds + row] = (uint8_t)byte;
+        if (lane == 0) bulk_wait_read();
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          *reinterpret_cast<uint4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+              make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+        if ((p.N & 15) == 0 || n0 + 128 <= p.N) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(tm, stg, n0, rbase);
+            bulk_commit();
+          }
+          return;
+        }
+        __syncwarp();
+        const int piece = lane & 7, here = min(16, p.N - n0 - 16 * piece);
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+          const int lr = 4 * i + (lane >> 3), r = rbase + lr;
+          if (r >= p.M || here <= 0) continue;
+          const uint8_t* src = stg + lr * 128 + ((piece ^ (lr & 7)) << 4);
+          uint8_t* dst = q + (size_t)r * ldq + n0 + 16 * piece;
+          if (here == 16) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
+          else
+            for (int j = 0; j < here; ++j) dst[j] = src[j];
+        }
+        __syncwarp();
+      };
+      if (p.u8) put8(&tmU8, p.u8, p.ldu8, p.u8_scale, p.lds_u8);
+      if (p.epilogue == LAZYMAR_EPI_GELU) {
+#pragma unroll
+        for (int i = 0; i < 64; ++i) gelu_erf_x2(v[2 * i], v[2 * i + 1]);
+      }
+      if (p.out8) put8(&tmO8, p.out8, p.ldout8, p.out8_scale, p.lds_out8);
+      if (p.out) {
+        // 32 columns at a time through the staging buffer, so that stores and
+        // residual loads cover whole rows of it
+        const int lr0 = lane >> 3, cq = lane & 7;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int col = n0 + 32 * c + 4 * cq;
+          if (n0 + 32 * c >= p.N) break;
+          if (lane == 0) bulk_wait_read();
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<float4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+                make_float4(v[32 * c + 4 * j], v[32 * c + 4 * j + 1], v[32 * c + 4 * j + 2], v[32 * c + 4 * j + 3]);
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int lr = 4 * q + lr0, r = rbase + lr;
+            float4 o = *reinterpret_cast<const float4*>(stg + lr * 128 + ((cq ^ (lr & 7)) << 4));
+            if (r >= p.M || col >= p.N) continue;
+            if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
+              const float* x = p.residual + (size_t)r * p.ldr + col;
+              if (p.res_vec && col + 4 <= p.N) {
+                const float4 z = *reinterpret_cast<const float4*>(x);
+                o = make_float4(o.x + z.x, o.y + z.y, o.z + z.z, o.w + z.w);
+              } else {
+                o.x += x[0];
+                if (col + 1 < p.N) o.y += x[1];
+                if (col + 2 < p.N) o.z += x[2];
+                if (col + 3 < p.N) o.w += x[3];
+              }
+            }
+            if (p.out_dtype == LAZYMAR_F32) {
+              float* y = static_cast<float*>(p.out) + (size_t)r * p.ldo + col;
+              if (p.out_vec && col + 4 <= p.N) {
+                *reinterpret_cast<float4*>(y) = o;
+              } else {
+                y[0] = o.x;
+                if (col + 1 < p.N) y[1] = o.y;
+                if (col + 2 < p.N) y[2] = o.z;
+                if (col + 3 < p.N) y[3] = o.w;
+              }
+            } else {
+              bf16* y = static_cast<bf16*>(p.out) + (size_t)r * p.ldo + col;
+              if (p.out_vec && col + 4 <= p.N) {
+                *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+              } else {
+                y[0] = from_f<bf16>(o.x);
+                if (col + 1 < p.N) y[1] = from_f<bf16>(o.y);
+                if (col + 2 < p.N) y[2] = from_f<bf16>(o.z);
+                if (col + 3 < p.N) y[3] = from_f<bf16>(o.w);
+              }
+            }
+          }
+          __syncwarp();
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_all();
+    __syncwarp();
+  }
+  __syncthreads();
+  if (PAIR) cluster_sync();
+  if (warp == 1) {
+    tc_fence_after();
+    if (PAIR) tmem_dealloc_pair(tmem_base, 512);
+    else tmem_dealloc(tmem_base, 512);
+  }
+}
+
+namespace {
+
+// Shared-memory size and, once for each device, the check that the launch holds
+// the registers that the kernel's warps share out.
+template <bool PAIR>
+cudaError_t prepare_linear8() {
+  static int ready[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 0 && dev < 64 && ready[dev]) return cudaSuccess;
+  cudaFuncAttributes a;
+  if ((e = cudaFuncGetAttributes(&a, linear8_kernel<PAIR>)) != cudaSuccess) return e;
+  if (a.numRegs * l8::THREADS < (l8::REGS_EPI + l8::REGS_REST) * 256) return cudaErrorInvalidConfiguration;
+  e = cudaFuncSetAttribute(linear8_kernel<PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l8::SMEM);
+  if (e == cudaSuccess && dev >= 0 && dev < 64) ready[dev] = 1;
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_linear8(const Ctx& c, const Linear8& x) {
+  using namespace l8;
+  CUtensorMap ta, tb, to, tu;
+  std::memset(&to, 0, sizeof to);
+  std::memset(&tu, 0, sizeof tu);
+  const auto sw = CU_TENSOR_MAP_SWIZZLE_128B;
+  if (!make_tmap_u8(&ta, x.a.q, x.K, x.M, x.a.ldq, KB_BYTES, BM, sw) ||
+      !make_tmap_u8(&tb, x.w.q, x.K, x.N, x.w.ldq, KB_BYTES, 128, sw) ||
+      (x.out8.q && !make_tmap_u8(&to, x.out8.q, x.N, x.M, x.out8.ldq, 128, 32, sw)) ||
+      (x.u8.q && !make_tmap_u8(&tu, x.u8.q, x.N, x.M, x.u8.ldq, 128, 32, sw)))
+    return cudaErrorInvalidValue;
+  Params p{};
+  p.a_scale = x.a.scale;
+  p.w_scale = x.w.scale;
+  p.lds_a = x.a.lds;
+  p.lds_w = x.w.lds;
+  p.epilogue = x.epilogue;
+  p.M = x.M;
+  p.N = x.N;
+  p.K = x.K;
+  p.bias = x.bias;
+  p.residual = static_cast<const float*>(x.residual.p);
+  p.ldr = x.residual.ld;
+  p.out = x.out.p;
+  p.ldo = x.out.ld;
+  p.out_dtype = x.out.dtype;
+  p.out8_scale = x.out8.scale;
+  p.u8_scale = x.u8.scale;
+  p.lds_out8 = x.out8.lds;
+  p.lds_u8 = x.u8.lds;
+  p.out8 = static_cast<uint8_t*>(x.out8.q);
+  p.u8 = static_cast<uint8_t*>(x.u8.q);
+  p.ldout8 = x.out8.ldq;
+  p.ldu8 = x.u8.ldq;
+  const auto at = [](const void* q, size_t n) { return reinterpret_cast<uintptr_t>(q) % n == 0; };
+  p.bias_vec = at(x.bias, 16);
+  p.out_vec = x.out.ld % 4 == 0 && at(x.out.p, x.out.dtype == LAZYMAR_F32 ? 16 : 8);
+  p.res_vec = x.residual.ld % 4 == 0 && at(x.residual.p, 16);
+  const long long pair_tiles = (long long)((x.M + 255) / 256) * ((x.N + 255) / 256);
+  const int pairs = c.num_sms / 2;
+  cudaError_t e;
+  if (pair_tiles >= pairs) {
+    if ((e = prepare_linear8<true>()) != cudaSuccess) return e;
+    return launch_pdl_cluster(linear8_kernel<true>, dim3((unsigned)(2 * pairs)), dim3(THREADS), SMEM, 2, c.stream, ta, tb,
+                              to, tu, p, c.err);
+  }
+  const long long tiles = (long long)((x.M + 127) / 128) * ((x.N + 127) / 128);
+  if ((e = prepare_linear8<false>()) != cudaSuccess) return e;
+  return launch_pdl(linear8_kernel<false>, dim3((unsigned)(tiles < c.num_sms ? tiles : c.num_sms)), dim3(THREADS), SMEM,
+                    c.stream, ta, tb, to, tu, p, c.err);
+}
+
+}  // namespace lm

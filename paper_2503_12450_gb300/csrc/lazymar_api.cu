@@ -33,6 +33,9 @@ lazymar_status report_error(lazymar_status s, const char* msg) { return fail(s, 
 static lazymar_status cuda_fail(cudaError_t e, const char* what) {
   return fail(LAZYMAR_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
 }
+namespace lm {
+lazymar_status report_cuda(cudaError_t e, const char* what) { return cuda_fail(e, what); }
+}  // namespace lm
 #define LM_CUDA(expr)                                  \
   do {                                                 \
     cudaError_t e_ = (expr);                           \
@@ -48,7 +51,8 @@ static lazymar_status cuda_fail(cudaError_t e, const char* what) {
 // module's static device memory; handles use their own word).
 static __device__ unsigned g_component_err;
 
-static lazymar_status component_ctx(void* stream, Ctx* c) {
+namespace lm {
+lazymar_status component_ctx(void* stream, Ctx* c) {
   int dev = 0;
   LM_CUDA(cudaGetDevice(&dev));
   int sms = 0;
@@ -61,7 +65,7 @@ static lazymar_status component_ctx(void* stream, Ctx* c) {
   return LAZYMAR_OK;
 }
 
-static bool is_device_ptr(const void* p) {
+bool is_device_ptr(const void* p) {
   if (!p) return false;
   cudaPointerAttributes a;
   if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
@@ -70,6 +74,7 @@ static bool is_device_ptr(const void* p) {
   }
   return a.type == cudaMemoryTypeDevice || a.type == cudaMemoryTypeManaged;
 }
+}  // namespace lm
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 static lazymar_status read_error_word(unsigned* word, cudaStream_t stream) {

@@ -693,5 +693,10 @@ struct NvtxRange {
 // Records `msg` as the calling thread's last error (lazymar_last_error) and
 // returns `s`.
 lazymar_status report_error(lazymar_status s, const char* msg);
+// The same for a failed CUDA call or launch.
+lazymar_status report_cuda(cudaError_t e, const char* what);
+// Stream, error word and SM count of a component entry point on the current device.
+lazymar_status component_ctx(void* stream, Ctx* c);
+bool is_device_ptr(const void* p);
 
 }  // namespace lm

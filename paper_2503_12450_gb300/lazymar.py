@@ -82,6 +82,11 @@ class lazymar_head_weights(ctypes.Structure):
         (n, _FP) for n in HEAD_FIELDS_B]
 
 
+class lazymar_block8_desc(ctypes.Structure):
+    """struct lazymar_block8; `addr` is its address, `keep` what it points to."""
+    _fields_ = [("q", _FP), ("scale", _FP), ("ldq", ctypes.c_int), ("lds", ctypes.c_int)]
+
+
 _lib = None
 
 
@@ -129,6 +134,18 @@ def lib():
         "lazymar_head_counters": (st, [vp, ctypes.POINTER(ctypes.c_longlong), ctypes.POINTER(ctypes.c_double)]),
         "lazymar_head_sync": (st, [vp, vp]),
         "lazymar_head_schedule": (st, [i, i, vp, vp]),
+        "lazymar_layernorm_forward": (st, [i, vp, i, vp, vp, i, vp, i, vp, vp, vp, vp, i, i, f, vp]),
+        "lazymar_layernorm_backward_workspace": (sz, [i, i]),
+        "lazymar_layernorm_backward": (st, [i, vp, i, i, vp, i, vp, vp, vp, vp, vp, i, i, vp, i, vp, vp, i, i, i, vp,
+                                            sz, vp]),
+        "lazymar_block8_pack": (st, [i, vp, i, vp, i, i, vp]),
+        "lazymar_block8_unpack": (st, [vp, i, vp, i, i, i, vp]),
+        "lazymar_block8_pack_weight": (st, [i, vp, i, vp, vp, i, i, vp]),
+        "lazymar_block8_gelu_backward_workspace": (sz, [i, i]),
+        "lazymar_block8_gelu_backward": (st, [i, vp, i, vp, i, vp, i, vp, vp, i, i, i, vp, sz, vp]),
+        "lazymar_block8_linear": (st, [i, vp, vp, vp, vp, i, i, vp, i, vp, vp, i, i, i, vp]),
+        "lazymar_block8_wgrad_workspace": (sz, [i, i, i]),
+        "lazymar_block8_wgrad": (st, [vp, i, vp, vp, i, i, i, i, i, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -409,6 +426,83 @@ def lazymar_head_schedule(n_train, n_steps):
 
 def lazymar_head_sync(hd, stream=None):
     _check(lib().lazymar_head_sync(hd.ptr, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# Training a block with 8-bit activations
+# ---------------------------------------------------------------------------
+
+def lazymar_block8(q, scale, ldq=None, lds=None):
+    """Describes an 8-bit tensor to the calls below: q [rows, ldq] bytes, scale
+    [blocks of 128 columns, lds] bytes (weights: [blocks of K, blocks of N]). The
+    strides are the tensors' own unless given. Keeps the tensors alive; make it
+    once and use it again."""
+    if ldq is None:
+        ldq = q.stride(0) if q.shape[0] > 1 else max(q.stride(0), q.shape[1])
+    if lds is None:
+        lds = scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), scale.shape[1])
+    d = lazymar_block8_desc(_ptr(q), _ptr(scale), int(ldq), int(lds))
+    d.keep = (q, scale)
+    d.addr = ctypes.addressof(d)
+    return d
+
+
+def _desc(d):
+    return None if d is None else d.addr
+
+
+def lazymar_layernorm_forward(x_dtype, x, ldx, g, b, y_dtype, y, ldy, y8, x8, mean, rstd, M, D, eps, stream=None):
+    _check(lib().lazymar_layernorm_forward(x_dtype, _ptr(x), ldx, _ptr(g), _ptr(b), y_dtype, _ptr(y), ldy, _desc(y8),
+                                           _desc(x8), _ptr(mean), _ptr(rstd), M, D, eps, _stream(stream)))
+
+
+def lazymar_layernorm_backward_workspace(M, D):
+    return lib().lazymar_layernorm_backward_workspace(M, D)
+
+
+def lazymar_layernorm_backward(dy_dtype, dy, lddy, x_dtype, x, ldx, x8, mean, rstd, g, dres, lddres, dx_dtype, dx,
+                               lddx, dg, db, accumulate, M, D, workspace, workspace_bytes, stream=None):
+    _check(lib().lazymar_layernorm_backward(dy_dtype, _ptr(dy), lddy, x_dtype, _ptr(x), ldx, _desc(x8), _ptr(mean),
+                                            _ptr(rstd), _ptr(g), _ptr(dres), lddres, dx_dtype, _ptr(dx), lddx,
+                                            _ptr(dg), _ptr(db), int(accumulate), M, D, _ptr(workspace),
+                                            workspace_bytes, _stream(stream)))
+
+
+def lazymar_block8_pack(dtype, x, ldx, q, rows, cols, stream=None):
+    _check(lib().lazymar_block8_pack(dtype, _ptr(x), ldx, _desc(q), rows, cols, _stream(stream)))
+
+
+def lazymar_block8_unpack(q, dtype, x, ldx, rows, cols, stream=None):
+    _check(lib().lazymar_block8_unpack(_desc(q), dtype, _ptr(x), ldx, rows, cols, _stream(stream)))
+
+
+def lazymar_block8_pack_weight(dtype, w, ldw, q, qt, N, K, stream=None):
+    _check(lib().lazymar_block8_pack_weight(dtype, _ptr(w), ldw, _desc(q), _desc(qt), N, K, _stream(stream)))
+
+
+def lazymar_block8_gelu_backward_workspace(rows, cols):
+    return lib().lazymar_block8_gelu_backward_workspace(rows, cols)
+
+
+def lazymar_block8_gelu_backward(dtype, da, ldda, u, du_dtype, du, lddu, du8, db, accumulate, rows, cols, workspace,
+                                 workspace_bytes, stream=None):
+    _check(lib().lazymar_block8_gelu_backward(dtype, _ptr(da), ldda, _desc(u), du_dtype, _ptr(du), lddu, _desc(du8),
+                                              _ptr(db), int(accumulate), rows, cols, _ptr(workspace),
+                                              workspace_bytes, _stream(stream)))
+
+
+def lazymar_block8_linear(epilogue, a, w, bias, residual, ldr, out_dtype, out, ldo, out8, u8, M, N, K, stream=None):
+    _check(lib().lazymar_block8_linear(epilogue, _desc(a), _desc(w), _ptr(bias), _ptr(residual), ldr, out_dtype,
+                                       _ptr(out), ldo, _desc(out8), _desc(u8), M, N, K, _stream(stream)))
+
+
+def lazymar_block8_wgrad_workspace(M, N, K):
+    return lib().lazymar_block8_wgrad_workspace(M, N, K)
+
+
+def lazymar_block8_wgrad(dy, lddy, x, dw, lddw, accumulate, M, N, K, workspace, workspace_bytes, stream=None):
+    _check(lib().lazymar_block8_wgrad(_ptr(dy), lddy, _desc(x), _ptr(dw), lddw, int(accumulate), M, N, K,
+                                      _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 class HeadHandle:

@@ -1,0 +1,170 @@
+"""The training operators without a GPU: the oracle's pins (format, gradients
+against differences), exports, and the argument checks that need no device."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+from oracle import training as T
+from paper_2503_12450_gb300 import build
+from paper_2503_12450_gb300 import lazymar as lm
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return lm.lib()
+
+
+# --------------------------------------------------------------------------
+# Oracle
+# --------------------------------------------------------------------------
+
+def test_e4m3_every_byte_decodes_and_encodes_to_itself():
+    q = np.arange(256, dtype=np.uint8)
+    v = T.e4m3_decode(q)
+    assert v[0x7E] == 448.0 and v[0x01] == 2.0 ** -9 and v[0x08] == 2.0 ** -6 and v[0x38] == 1.0
+    keep = ~np.isnan(v)
+    assert (T.e4m3_encode(v[keep]) == q[keep]).all()
+
+
+def test_e4m3_rounds_to_the_nearest_ties_to_even():
+    v = np.sort(T.e4m3_decode(np.arange(0, 0x7F, dtype=np.uint8)))
+    mid = (v[1:] + v[:-1]) / 2
+    q = T.e4m3_encode(mid)
+    assert (q % 2 == 0).all()  # the neighbour with the even mantissa
+    assert (T.e4m3_decode(T.e4m3_encode(mid * (1 + 1e-9))) == v[1:]).all()
+    assert (T.e4m3_decode(T.e4m3_encode(mid * (1 - 1e-9))) == v[:-1]).all()
+
+
+def test_exponent_is_the_smallest_that_holds_the_maximum():
+    for a in [448.0, 448.0000001, 1.0, 3.5, 1.75, 1.7500001, 3.4e38, 1e-30, 2.0 ** -118]:
+        e = int(T.exponent(a))
+        assert a <= 448.0 * 2.0 ** e and (e == -126 or a > 448.0 * 2.0 ** (e - 1))
+    assert int(T.exponent(0.0)) == -126 and int(T.exponent(1e-45)) == -126
+
+
+def test_pack_error_is_that_of_three_mantissa_bits():
+    x = np.random.default_rng(0).standard_normal((7, 300)) * np.exp2(np.arange(7) * 9.0 - 30)[:, None]
+    q, s = T.pack(x)
+    v = T.unpack(q, s)
+    big = np.abs(x) >= np.exp2(s.astype(float) - 127 - 6)[np.arange(300) // 128].T
+    assert (np.abs(v - x)[big] <= np.abs(x)[big] / 16).all()
+    assert (v.astype(np.float32).view(np.uint32) & 0xFFFF == 0).all()  # exact in bf16
+
+
+def _difference(f, x, h):
+    d = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        a, b = x.copy(), x.copy()
+        a[i] += h
+        b[i] -= h
+        d[i] = (f(a) - f(b)) / (2 * h)
+    return d
+
+
+def test_layernorm_gradient_against_differences():
+    r = np.random.default_rng(1)
+    x, dy, g, b = r.standard_normal((3, 9)), r.standard_normal((3, 9)), r.standard_normal(9), r.standard_normal(9)
+    f = lambda x, g, b: float((T.layernorm(x, g, b, 1e-6)[0] * dy).sum())  # noqa: E731
+    _, mean, rstd = T.layernorm(x, g, b, 1e-6)
+    dx, dg, db = T.layernorm_grad(dy, x, mean, rstd, g)
+    # central differences of step h: error O(h^2) + rounding 1e-16 / h
+    np.testing.assert_allclose(dx, _difference(lambda v: f(v, g, b), x, 1e-5), atol=1e-8)
+    np.testing.assert_allclose(dg, _difference(lambda v: f(x, v, b), g, 1e-5), atol=1e-8)
+    np.testing.assert_allclose(db, _difference(lambda v: f(x, g, v), b, 1e-5), atol=1e-8)
+
+
+def test_gelu_gradient_against_differences():
+    x = np.linspace(-8, 8, 161)
+    np.testing.assert_allclose(T.gelu_grad(x), (T.gelu(x + 1e-5) - T.gelu(x - 1e-5)) / 2e-5, atol=1e-9)
+
+
+# --------------------------------------------------------------------------
+# Library
+# --------------------------------------------------------------------------
+
+def test_exports_every_declared_training_symbol(lib):
+    text = open(os.path.join(ROOT, "include", "lazymar.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = [n for n in set(re.findall(r"\b(lazymar_[a-z0-9_]+)\s*\(", text)) if "block8" in n or "_forward" in n
+             or "_backward" in n]
+    assert len(names) == 11
+    raw = ctypes.CDLL(lm.LIB_PATH)
+    assert not [n for n in names if not hasattr(raw, n) or not hasattr(lm, n)]
+
+
+def _b8(q=0, scale=0, ldq=128, lds=4):
+    d = lm.lazymar_block8_desc(q or None, scale or None, ldq, lds)
+    d.addr = ctypes.addressof(d)
+    return d
+
+
+@pytest.mark.parametrize("call,status,word", [
+    (lambda L, q: L.lazymar_layernorm_forward(0, None, 8, None, None, 0, None, 8, None, None, None, None, 4, 8, 1e-6,
+                                              None), 1, "no output"),
+    (lambda L, q: L.lazymar_layernorm_forward(0, None, 8, None, None, 0, 16, 8, None, None, None, None, -1, 8, 1e-6,
+                                              None), 1, "M >= 0"),
+    (lambda L, q: L.lazymar_layernorm_forward(0, None, 8, None, None, 0, 16, 8, None, None, None, None, 4, 0, 1e-6,
+                                              None), 1, "D >= 1"),
+    (lambda L, q: L.lazymar_layernorm_forward(0, None, 8, None, None, 0, 16, 8, None, None, None, None, 4, 8, 0.0,
+                                              None), 1, "eps"),
+    (lambda L, q: L.lazymar_layernorm_forward(0, None, 9000, None, None, 0, 16, 9000, None, None, None, None, 4, 8193,
+                                              1e-6, None), 6, "8192"),
+    (lambda L, q: L.lazymar_layernorm_forward(2, 16, 8, None, None, 0, 16, 8, None, None, None, None, 4, 8, 1e-6,
+                                              None), 1, "x:"),
+    (lambda L, q: L.lazymar_layernorm_forward(0, 16, 7, None, None, 0, 16, 8, None, None, None, None, 4, 8, 1e-6,
+                                              None), 1, "ldx"),
+    (lambda L, q: L.lazymar_layernorm_backward(0, 16, 8, 0, None, 0, None, 16, 16, None, None, 0, 0, 16, 8, None, None,
+                                               0, 4, 8, None, 0, None), 1, "exactly one"),
+    (lambda L, q: L.lazymar_layernorm_backward(0, 16, 8, 0, 16, 8, q.addr, 16, 16, None, None, 0, 0, 16, 8, None, None,
+                                               0, 4, 8, None, 0, None), 1, "exactly one"),
+    (lambda L, q: L.lazymar_layernorm_backward(0, 16, 8, 0, 16, 8, None, 16, 16, None, None, 0, 0, 16, 8, 16, None, 0,
+                                               4, 8, None, 0, None), 1, "both or neither"),
+    (lambda L, q: L.lazymar_block8_pack(0, 16, 8, None, 4, 8, None), 1, "q required"),
+    (lambda L, q: L.lazymar_block8_pack(0, 16, 8, q.addr, 4, 0, None), 1, "cols >= 1"),
+    (lambda L, q: L.lazymar_block8_unpack(q.addr, 0, 16, 8, -1, 8, None), 1, "rows >= 0"),
+    (lambda L, q: L.lazymar_block8_unpack(q.addr, 0, 16, 8, 4, 8, None), 1, "q:"),
+    (lambda L, q: L.lazymar_block8_pack_weight(0, 16, 8, None, None, 4, 8, None), 1, "q or qt"),
+    (lambda L, q: L.lazymar_block8_gelu_backward(0, 16, 8, None, 0, None, 0, None, None, 0, 4, 8, None, 0, None), 1,
+     "no output"),
+    (lambda L, q: L.lazymar_block8_linear(3, q.addr, q.addr, None, None, 0, 0, 16, 8, None, None, 4, 8, 8, None), 1,
+     "epilogue"),
+    (lambda L, q: L.lazymar_block8_linear(0, q.addr, q.addr, None, None, 0, 0, None, 8, None, None, 4, 8, 8, None), 1,
+     "out or out8"),
+    (lambda L, q: L.lazymar_block8_linear(0, q.addr, q.addr, None, None, 0, 0, 16, 8, None, q.addr, 4, 8, 8, None), 1,
+     "u8 is for"),
+    (lambda L, q: L.lazymar_block8_linear(0, q.addr, q.addr, None, 16, 8, 0, 16, 8, None, None, 4, 8, 8, None), 1,
+     "residual is for"),
+    (lambda L, q: L.lazymar_block8_linear(2, q.addr, q.addr, None, 16, 8, 1, 16, 8, None, None, 4, 8, 8, None), 1,
+     "RESIDUAL"),
+    (lambda L, q: L.lazymar_block8_linear(0, q.addr, q.addr, None, None, 0, 0, 16, 8, None, None, 4, 8, 0, None), 1,
+     "K >= 1"),
+    (lambda L, q: L.lazymar_block8_wgrad(16, 8, q.addr, 16, 8, 0, 4, 8, 0, None, 0, None), 1, "K >= 1"),
+])
+def test_refusals_before_touching_the_device(lib, call, status, word):
+    q = _b8()
+    assert call(lib, q) == status
+    assert word in lib.lazymar_last_error().decode()
+
+
+def test_empty_calls_succeed_without_a_device(lib):
+    q = _b8()
+    assert lib.lazymar_layernorm_forward(0, None, 8, None, None, 0, 16, 8, None, None, None, None, 0, 8, 1e-6, None) == 0
+    assert lib.lazymar_block8_pack(0, None, 8, q.addr, 0, 8, None) == 0
+    assert lib.lazymar_block8_unpack(q.addr, 0, None, 8, 0, 8, None) == 0
+    assert lib.lazymar_block8_pack_weight(0, None, 8, q.addr, None, 0, 8, None) == 0
+    assert lib.lazymar_block8_linear(0, q.addr, q.addr, None, None, 0, 0, 16, 8, None, None, 0, 8, 8, None) == 0
+    assert lib.lazymar_block8_wgrad(None, 8, q.addr, None, 8, 0, 4, 0, 8, None, 0, None) == 0
+
+
+def test_workspaces_cover_small_and_large_sizes(lib):
+    assert lm.lazymar_layernorm_backward_workspace(0, 768) == 0
+    assert lm.lazymar_layernorm_backward_workspace(1, 768) == 2 * 768 * 4
+    assert lm.lazymar_layernorm_backward_workspace(40960, 1280) <= 8 << 20
+    assert lm.lazymar_block8_gelu_backward_workspace(0, 768) == 0
+    assert lm.lazymar_block8_gelu_backward_workspace(40960, 5120) <= 16 << 20
