@@ -505,6 +505,72 @@ def test_linear_ignores_padding_bytes_and_keeps_nan_in_its_row():
 
 
 # --------------------------------------------------------------------------
+# The weight gradient
+# --------------------------------------------------------------------------
+def _wgrad_bound(mag, M):
+    """Products of two bf16 values are exact in fp32. Within 512 tokens, 32 steps of 16 on an accumulator that may
+    truncate with its terms lined up: 4 u a step; then one rounding for each 512 tokens and each split."""
+    return (48 * 4 + M / 512 + 34) * U * mag + 1e-30
+
+
+@pytest.mark.parametrize("M,N,K,pad", [(1, 1, 1, 0), (1, 128, 128, 0), (63, 130, 77, 1), (64, 64, 64, 0),
+                                       (65, 256, 256, 4), (700, 300, 200, 0), (3211, 1000, 776, 0), (5000, 8, 300, 3),
+                                       (129, 2100, 1100, 0), (1600, 1280, 1024, 0), (4096, 129, 1, 0), (513, 4096, 1024, 0)])
+def test_wgrad(M, N, K, pad):
+    torch = torch_cuda()
+    r = rng(M, N, K, 21)
+    ldy = -(-(N + pad) // 8) * 8
+    dy, dyv = dev(r.standard_normal((M, N)) * np.exp(r.standard_normal((M, 1))), "bf16", ldy - N)
+    x, xv = held(r.standard_normal((M, K)) * np.exp2(r.integers(-20, 20, (M, 1)).astype(float)), lds=M + pad)
+    dw = out(N, K, "fp32", pad)
+    ws = torch.full((lm.lazymar_block8_wgrad_workspace(M, N, K) + 16,), 0xFF, dtype=torch.uint8, device="cuda")
+    args = (dy, ldy, x.d, dw, K + pad)
+    lm.lazymar_block8_wgrad(*args, False, M, N, K, ws, ws.numel())
+    sync()
+    want, bound = dyv.T @ xv, _wgrad_bound(np.abs(dyv).T @ np.abs(xv), M)
+    close(dw, want, bound)
+    first = dw.clone()
+    lm.lazymar_block8_wgrad(*args, True, M, N, K, ws, ws.numel())
+    sync()
+    assert torch.equal(dw, first + first)
+
+
+def test_wgrad_without_rows():
+    dw = vec(np.ones((300, 70)))
+    lm.lazymar_block8_wgrad(None, 300, None, dw, 70, True, 0, 300, 70, None, 0)
+    sync()
+    assert (dw == 1).all()
+    lm.lazymar_block8_wgrad(None, 300, None, dw, 70, False, 0, 300, 70, None, 0)
+    sync()
+    assert (dw == 0).all()
+
+
+def test_wgrad_keeps_nan_and_the_range_of_scales():
+    """A NaN byte reaches its column of dw and no other; scales at both ends of their range; bytes beyond K are not
+    read as values."""
+    r = rng(22)
+    v = r.standard_normal((200, 150)) * 1e-3
+    v[0], v[1] = 2.0 ** 100, 2.0 ** -120
+    x, xv = held(v.astype(np.float32), more=32)
+    x.q[9, 17] = 0xFF
+    dy, dyv = dev(r.standard_normal((200, 136)), "bf16")
+    dyv[0] = 0
+    dy[0] = 0
+    dw = out(136, 150)
+    lm.lazymar_block8_wgrad(dy, 136, x.d, dw, 150, False, 200, 136, 150, None if not
+                            lm.lazymar_block8_wgrad_workspace(200, 136, 150) else
+                            torch_cuda().empty(lm.lazymar_block8_wgrad_workspace(200, 136, 150), dtype=torch_cuda().uint8,
+                                               device="cuda"), lm.lazymar_block8_wgrad_workspace(200, 136, 150))
+    sync()
+    got = dw.double().cpu().numpy()
+    assert np.isnan(got[:, 17]).all() and np.isnan(got).sum() == 136
+    keep = np.arange(150) != 17
+    xv[0] = 0
+    want = dyv.T @ xv
+    assert (np.abs(got - want) <= _wgrad_bound(np.abs(dyv).T @ np.abs(xv), 200))[:, keep].all()
+
+
+# --------------------------------------------------------------------------
 # Streams, offsets, refusals
 # --------------------------------------------------------------------------
 def test_calls_follow_the_callers_stream():
