@@ -467,7 +467,7 @@ lazymar_status lazymar_head_schedule(int n_train, int n_steps, int32_t *kept, fl
  * >= ceil(N / 128)).
  *
  * Strides (ld*) count elements; fp32 and bf16 tensors may have any stride >=
- * their columns and any element alignment (rows on boundaries of four elements
+ * their columns and any element alignment (rows on boundaries of eight elements
  * are faster). Sums, statistics and parameter gradients are fp32. Results are
  * the same from call to call (no atomics). accumulate = 1 adds to the
  * parameter gradients instead of overwriting them.

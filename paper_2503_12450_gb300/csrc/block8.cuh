@@ -50,33 +50,68 @@ __device__ __forceinline__ float4 f4_nonfinite_to(float4 v, float to) {
   return make_float4(f(v.x), f(v.y), f(v.z), f(v.w));
 }
 
-// A warp's block of 128 columns, four consecutive ones a lane, to E4M3: the
-// scale byte (the same in every lane) and this lane's four bytes. The scale is
-// that of the finite values; infinities and NaN become NaN, so an overflow
-// stays visible and does not disturb its neighbours.
-__device__ __forceinline__ uint32_t block8_quantize(float4 v, uint32_t& q) {
-  const float m = fmax3(fmaxf(fabsf(v.x), fabsf(v.y)), fabsf(v.z), fabsf(v.w));
-  uint32_t amax = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
-  if (amax >= 0x7F800000u) {  // an infinity, or a lane of NaN alone
-    const float4 z = f4_nonfinite_to(v, 0.f);
-    const float mz = fmax3(fmaxf(fabsf(z.x), fabsf(z.y)), fabsf(z.z), fabsf(z.w));
-    amax = __reduce_max_sync(0xffffffffu, __float_as_uint(mz));
-    v = f4_nonfinite_to(v, __uint_as_float(0x7FC00000u));
+// Two blocks of 128 columns in a warp, one in each half, eight consecutive
+// columns a lane, to E4M3: the scale byte of the lane's block and the lane's
+// eight bytes. The scale is that of the finite values; infinities and NaN become
+// NaN, so an overflow stays visible and does not disturb its neighbours.
+__device__ __forceinline__ uint32_t block8_amax(const float (&v)[8]) {
+  const float m = fmax3(fmax3(fabsf(v[0]), fabsf(v[1]), fabsf(v[2])), fmax3(fabsf(v[3]), fabsf(v[4]), fabsf(v[5])),
+                        fmaxf(fabsf(v[6]), fabsf(v[7])));
+  return __float_as_uint(m);
+}
+__device__ __forceinline__ float nonfinite_to(float x, float to) {
+  return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u ? to : x;
+}
+__device__ __forceinline__ uint32_t half_warp_max(uint32_t m, bool upper, uint32_t& both) {
+  const uint32_t lo = __reduce_max_sync(0xffffffffu, upper ? 0u : m);
+  const uint32_t hi = __reduce_max_sync(0xffffffffu, upper ? m : 0u);
+  both = max(lo, hi);
+  return upper ? hi : lo;
+}
+__device__ __forceinline__ uint32_t block8_quantize(const float (&v)[8], uint2& q) {
+  const bool upper = threadIdx.x & 16;
+  uint32_t both, amax = half_warp_max(block8_amax(v), upper, both);
+  float w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = v[i];
+  if (both >= 0x7F800000u) {  // an infinity
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = nonfinite_to(v[i], 0.f);
+    amax = half_warp_max(block8_amax(z), upper, both);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = nonfinite_to(v[i], __uint_as_float(0x7FC00000u));
   }
   const uint32_t byte = block8_exp(amax);
   const float s = block8_inv(byte);
-  q = e4m3x4(v.x * s, v.y * s, v.z * s, v.w * s);
+  const unsigned long long ss = f32x2_pack(s, s);
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) f32x2_unpack(f32x2_mul(f32x2_pack(w[i], w[i + 1]), ss), w[i], w[i + 1]);
+  q = make_uint2(e4m3x4(w[0], w[1], w[2], w[3]), e4m3x4(w[4], w[5], w[6], w[7]));
   return byte;
 }
+// Eight E4M3 bytes times a scale.
+__device__ __forceinline__ void block8_values(uint2 q, float s, float (&v)[8]) {
+  const float2 a = e4m3x2_to_f2(q.x & 0xFFFFu), b = e4m3x2_to_f2(q.x >> 16);
+  const float2 c = e4m3x2_to_f2(q.y & 0xFFFFu), d = e4m3x2_to_f2(q.y >> 16);
+  const unsigned long long ss = f32x2_pack(s, s);
+  f32x2_unpack(f32x2_mul(f32x2_pack(a.x, a.y), ss), v[0], v[1]);
+  f32x2_unpack(f32x2_mul(f32x2_pack(b.x, b.y), ss), v[2], v[3]);
+  f32x2_unpack(f32x2_mul(f32x2_pack(c.x, c.y), ss), v[4], v[5]);
+  f32x2_unpack(f32x2_mul(f32x2_pack(d.x, d.y), ss), v[6], v[7]);
+}
 
-// Tensors as the kernels take them. dtype LAZYMAR_F32 or LAZYMAR_BF16.
+// Tensors as the kernels take them. dtype LAZYMAR_F32 or LAZYMAR_BF16; vec:
+// rows start on boundaries of eight elements.
 struct Mat {
   const void* p;
   int ld, dtype;
+  bool vec;
 };
 struct MatOut {
   void* p;
   int ld, dtype;
+  bool vec;
 };
 
 struct LnForward {
@@ -87,7 +122,6 @@ struct LnForward {
   float *mean, *rstd;      // may be NULL
   int M, D;
   float eps;
-  bool vec;  // rows of x and y start on 4-element boundaries
 };
 struct LnBackward {
   Mat dy, x;          // x.p NULL: x8
@@ -99,7 +133,6 @@ struct LnBackward {
   bool accumulate;
   int M, D;
   float* ws;
-  bool vec;
 };
 // The row-wise pass over [rows, cols] behind pack and the GELU gradient.
 struct Rows8 {
@@ -111,7 +144,6 @@ struct Rows8 {
   bool accumulate;
   int rows, cols;
   float* ws;
-  bool vec;
 };
 
 constexpr int kLnMaxWidth = 8192;

@@ -3,9 +3,12 @@
 // shift's gradients, and the passes between fp32/bf16 tensors and the 8-bit
 // block format (checkpoint, GELU's gradient from a checkpoint, weights).
 //
-// All of them are bound by HBM bandwidth. A warp covers a block of 128 columns
-// with four consecutive ones a lane: loads and stores are whole 128-byte lines
-// in every type, and a block's maximum is one warp reduction.
+// All of them are bound by HBM bandwidth, and next to it by instruction issue:
+// at 6 bytes an element the memory delivers four elements a cycle and SM, which
+// leaves some 30 instructions for each. So a lane takes eight consecutive columns
+// (one 16- or 32-byte access a tensor, 8 bytes of E4M3) and a half warp a block of
+// 128, whose maximum is a warp reduction; addresses, scales and reductions are
+// spread over eight elements.
 #include "block8.cuh"
 
 namespace lm {
@@ -13,69 +16,160 @@ namespace lm {
 namespace {
 
 constexpr int kSMs = 152;
+constexpr int kChunk = 256;  // columns of a warp: two blocks
 
 // ---------------------------------------------------------------------------
-// Four columns of a row
+// Eight columns of a row
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float4 ld4_bf16(const bf16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
-  const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
-  return make_float4(a.x, a.y, b.x, b.y);
+// At a boundary of eight elements. (Volatile: not to be moved above the wait for
+// the predecessor grid.)
+__device__ __forceinline__ void ld8a(const float* p, float (&v)[8]) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "l"(p));
 }
-// Columns col..col+3 of a row; those from D on read as zero. vec: the row
-// starts on a boundary of four elements.
-template <typename T>
-__device__ __forceinline__ float4 ld4(const T* row, int col, int D, bool vec) {
-  if (vec && col + 4 <= D) {
-    if constexpr (sizeof(T) == 2) return ld4_bf16(row + col);
-    else return *reinterpret_cast<const float4*>(row + col);
-  }
-  float v[4];
+__device__ __forceinline__ void bf16x8(uint4 u, float (&v)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = col + i < D ? to_f(row[col + i]) : 0.f;
-  return make_float4(v[0], v[1], v[2], v[3]);
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
 }
+__device__ __forceinline__ void ld8a(const bf16* p, float (&v)[8]) { bf16x8(*reinterpret_cast<const uint4*>(p), v); }
+__device__ __forceinline__ void st8a(float* p, const float (&v)[8]) {
+  asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+               "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void st8a(bf16* p, const float (&v)[8]) {
+  *reinterpret_cast<uint4*>(p) =
+      make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+// A warp's 256 columns from c0 on, eight a lane; columns from D on read as zero
+// and are not written. Rows off the boundary go through the warp's 256 floats of
+// shared memory, so that the accesses of a warp stay contiguous. Every lane of
+// the warp takes part.
 template <typename T>
-__device__ __forceinline__ void st4(T* row, int col, int D, bool vec, float4 v) {
-  if (vec && col + 4 <= D) {
-    if constexpr (sizeof(T) == 2)
-      *reinterpret_cast<uint2*>(row + col) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-    else
-      *reinterpret_cast<float4*>(row + col) = v;
+__device__ __forceinline__ void ld8(const T* row, int c0, int D, bool vec, float* sm, float (&v)[8]) {
+  const int lane = threadIdx.x & 31, col = c0 + 8 * lane;
+  if (vec) {
+    if (col + 8 <= D) {
+      ld8a(row + col, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = col + i < D ? to_f(row[col + i]) : 0.f;
+    }
     return;
   }
-  const float o[4] = {v.x, v.y, v.z, v.w};
+  __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (col + i < D) row[col + i] = from_f<T>(o[i]);
+  for (int i = 0; i < 8; ++i) {
+    const int c = c0 + 32 * i + lane;
+    sm[32 * i + lane] = c < D ? to_f(row[c]) : 0.f;
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = sm[8 * lane + i];
 }
-// The same without a boundary: every column exists and rows are aligned.
-template <typename T, bool FULL>
-__device__ __forceinline__ float4 ld4t(const T* row, int col, int D, bool vec) {
-  return FULL ? ld4<T>(row, col, col + 4, true) : ld4<T>(row, col, D, vec);
-}
-// Four E4M3 bytes of a block8 row. Rows are 16-byte aligned and padded to 16
-// bytes, so the word is readable where any of its columns exists; bytes of
-// columns that do not are cleared.
-__device__ __forceinline__ uint32_t ldq4(const uint8_t* row, int col, int D) {
-  if (col >= D) return 0u;
-  uint32_t w = *reinterpret_cast<const uint32_t*>(row + col);
-  if (col + 4 > D) w &= 0xFFFFFFFFu >> (8 * (col + 4 - D));
-  return w;
-}
-// Columns at and beyond D keep what the padding held.
-__device__ __forceinline__ void stq4(uint8_t* row, int col, int D, uint32_t w) {
-  if (col + 4 <= D) {
-    *reinterpret_cast<uint32_t*>(row + col) = w;
-  } else {
-    for (int i = 0; col + i < D; ++i) row[col + i] = (uint8_t)(w >> (8 * i));
+template <typename T>
+__device__ __forceinline__ void st8(T* row, int c0, int D, bool vec, float* sm, const float (&v)[8]) {
+  const int lane = threadIdx.x & 31, col = c0 + 8 * lane;
+  if (vec) {
+    if (col + 8 <= D) {
+      st8a(row + col, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i < D) row[col + i] = from_f<T>(v[i]);
+    }
+    return;
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sm[8 * lane + i] = v[i];
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int c = c0 + 32 * i + lane;
+    if (c < D) row[c] = from_f<T>(sm[32 * i + lane]);
   }
 }
-__device__ __forceinline__ float4 mask4(float4 v, int col, int D) {
-  return make_float4(col < D ? v.x : 0.f, col + 1 < D ? v.y : 0.f, col + 2 < D ? v.z : 0.f, col + 3 < D ? v.w : 0.f);
+// FULL: every column exists and the row is on the boundary.
+template <bool FULL>
+__device__ __forceinline__ void ld_mat(const Mat& m, size_t row, int c0, int D, float* sm, float (&v)[8]) {
+  if (m.dtype == LAZYMAR_F32) {
+    const float* r = static_cast<const float*>(m.p) + row * m.ld;
+    if (FULL) ld8a(r + c0 + 8 * (threadIdx.x & 31), v);
+    else ld8<float>(r, c0, D, m.vec, sm, v);
+  } else {
+    const bf16* r = static_cast<const bf16*>(m.p) + row * m.ld;
+    if (FULL) ld8a(r + c0 + 8 * (threadIdx.x & 31), v);
+    else ld8<bf16>(r, c0, D, m.vec, sm, v);
+  }
 }
-__device__ __forceinline__ float sum4(float4 v) { return (v.x + v.y) + (v.z + v.w); }
+template <bool FULL>
+__device__ __forceinline__ void st_mat(const MatOut& m, size_t row, int c0, int D, float* sm, const float (&v)[8]) {
+  if (m.dtype == LAZYMAR_F32) {
+    float* r = static_cast<float*>(m.p) + row * m.ld;
+    if (FULL) st8a(r + c0 + 8 * (threadIdx.x & 31), v);
+    else st8<float>(r, c0, D, m.vec, sm, v);
+  } else {
+    bf16* r = static_cast<bf16*>(m.p) + row * m.ld;
+    if (FULL) st8a(r + c0 + 8 * (threadIdx.x & 31), v);
+    else st8<bf16>(r, c0, D, m.vec, sm, v);
+  }
+}
+// fp32 parameters of eight columns.
+template <bool FULL>
+__device__ __forceinline__ void ld_param(const float* p, int col, int D, float (&v)[8]) {
+  if (FULL) {
+    ld8a(p + col, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = col + i < D ? p[col + i] : 0.f;
+  }
+}
+// Eight E4M3 bytes of a block8 row. Rows are 16-byte aligned and padded to 16
+// bytes, so the bytes are readable where the first of them exists; those of
+// columns that do not exist are cleared.
+__device__ __forceinline__ uint2 clear_beyond(uint2 w, int n) {  // keeps the first n bytes
+  if (n < 4) return make_uint2(n <= 0 ? 0u : w.x & (0xFFFFFFFFu >> (32 - 8 * n)), 0u);
+  return make_uint2(w.x, n == 4 ? 0u : n < 8 ? w.y & (0xFFFFFFFFu >> (64 - 8 * n)) : w.y);
+}
+__device__ __forceinline__ uint2 ldq8(const uint8_t* row, int col, int D) {
+  if (col >= D) return make_uint2(0u, 0u);
+  const uint2 w = *reinterpret_cast<const uint2*>(row + col);
+  return col + 8 <= D ? w : clear_beyond(w, D - col);
+}
+__device__ __forceinline__ void stq8(uint8_t* row, int col, int D, uint2 w) {
+  if (col + 8 <= D) {
+    *reinterpret_cast<uint2*>(row + col) = w;
+  } else {
+    for (int i = 0; col + i < D; ++i) row[col + i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+  }
+}
+// A warp's 256 columns (two blocks) of row `row` to block8.
+template <bool FULL>
+__device__ __forceinline__ void put8(const lazymar_block8& o, size_t row, int c0, int D, const float (&v)[8]) {
+  const int lane = threadIdx.x & 31, col = c0 + 8 * lane;
+  uint2 w;
+  const uint32_t byte = block8_quantize(v, w);
+  uint8_t* q = static_cast<uint8_t*>(o.q) + row * o.ldq;
+  if (FULL) *reinterpret_cast<uint2*>(q + col) = w;
+  else stq8(q, col, D, w);
+  if ((lane & 15) == 0 && (FULL || col < D)) o.scale[(size_t)(col / kBlk) * o.lds + row] = (uint8_t)byte;
+}
+template <bool FULL>
+__device__ __forceinline__ void mask8(float (&v)[8], int col, int D) {
+  if (FULL || col + 8 <= D) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (col + i >= D) v[i] = 0.f;
+}
+__device__ __forceinline__ float sum8(const float (&v)[8]) {
+  return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
 
 // Sum of v over the WPR warps of a row (`red`: this row's slots in shared
 // memory). Every warp of the CTA takes part.
@@ -96,43 +190,40 @@ __device__ __forceinline__ float row_sum(float v, float* red, int part) {
 // ---------------------------------------------------------------------------
 // LayerNorm forward
 // ---------------------------------------------------------------------------
-// WPR warps a row, NB blocks of 128 columns a warp, the row in registers: one
+// WPR warps a row, NC chunks of 256 columns a warp, the row in registers: one
 // read of x, mean and then the squared deviations from it (no cancellation).
-// FULL: D = 128 NB WPR and aligned rows, so that no column needs a check.
-template <int NB, int WPR, bool FULL>
-__global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256) ln_forward_kernel(const LnForward p) {
-  constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR;
+// FULL: D = 256 NC WPR and aligned rows, so that no column needs a check.
+template <int NC, int WPR, bool FULL>
+__global__ void __launch_bounds__(256) ln_forward_kernel(const LnForward p) {
+  constexpr int GROUPS = 8 / WPR;
   __shared__ float red[2][GROUPS][WPR];
+  __shared__ float stage[FULL ? 1 : 8][kChunk];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
-  const int D = p.D, row = blockIdx.x * GROUPS + grp, c0 = part * NB * kBlk + 4 * lane;
+  float* sm = stage[FULL ? 0 : warp];
+  const int D = p.D, row = blockIdx.x * GROUPS + grp, c0 = part * NC * kChunk;
   const bool live = row < p.M;
   pdl_wait();
   pdl_trigger();
-  float4 v[NB];
-  if (live) {
-    if (p.x.dtype == LAZYMAR_F32) {
-      const float* xr = static_cast<const float*>(p.x.p) + (size_t)row * p.x.ld;
-#pragma unroll
-      for (int j = 0; j < NB; ++j) v[j] = ld4t<float, FULL>(xr, c0 + j * kBlk, D, p.vec);
-    } else {
-      const bf16* xr = static_cast<const bf16*>(p.x.p) + (size_t)row * p.x.ld;
-#pragma unroll
-      for (int j = 0; j < NB; ++j) v[j] = ld4t<bf16, FULL>(xr, c0 + j * kBlk, D, p.vec);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < NB; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-  }
+  float v[NC][8];
   float s = 0.f;
+  if (live) {
 #pragma unroll
-  for (int j = 0; j < NB; ++j) s += sum4(v[j]);
+    for (int c = 0; c < NC; ++c) ld_mat<FULL>(p.x, row, c0 + c * kChunk, D, sm, v[c]);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) s += sum8(v[c]);
+  }
   const float mean = row_sum<WPR>(s, red[0][grp], part) / (float)D;
   float q = 0.f;
+  if (live) {
 #pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    float4 d = make_float4(v[j].x - mean, v[j].y - mean, v[j].z - mean, v[j].w - mean);
-    if (!FULL) d = mask4(d, c0 + j * kBlk, D);
-    q += (d.x * d.x + d.y * d.y) + (d.z * d.z + d.w * d.w);
+    for (int c = 0; c < NC; ++c) {
+      if (p.x8.q && (FULL || c0 + c * kChunk < D)) put8<FULL>(p.x8, row, c0 + c * kChunk, D, v[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] -= mean;
+      mask8<FULL>(v[c], c0 + c * kChunk + 8 * lane, D);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q = fmaf(v[c][i], v[c][i], q);
+    }
   }
   const float rstd = rsqrtf(row_sum<WPR>(q, red[1][grp], part) / (float)D + p.eps);
   if (!live) return;
@@ -140,54 +231,39 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256) ln_forward_kernel(co
     if (p.mean) p.mean[row] = mean;
     if (p.rstd) p.rstd[row] = rstd;
   }
+  if (!p.y.p && !p.y8.q) return;
 #pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int col = c0 + j * kBlk;
-    if (!FULL && col - 4 * lane >= D) break;  // (uniform over the warp)
-    if (p.x8.q) {
-      uint32_t w;
-      const uint32_t byte = block8_quantize(v[j], w);
-      uint8_t* qr = static_cast<uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq;
-      if (FULL) *reinterpret_cast<uint32_t*>(qr + col) = w;
-      else stq4(qr, col, D, w);
-      if (lane == 0) p.x8.scale[(size_t)(part * NB + j) * p.x8.lds + row] = (uint8_t)byte;
-    }
-    float4 y = make_float4((v[j].x - mean) * rstd, (v[j].y - mean) * rstd, (v[j].z - mean) * rstd,
-                           (v[j].w - mean) * rstd);
+  for (int c = 0; c < NC; ++c) {
+    const int cc = c0 + c * kChunk, col = cc + 8 * lane;
+    if (!FULL && cc >= D) break;  // (uniform over the warp)
+    float y[8], t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = v[c][i] * rstd;
     if (p.g) {
-      const float4 g = FULL ? *reinterpret_cast<const float4*>(p.g + col) : ld4<float>(p.g, col, D, false);
-      y = make_float4(y.x * g.x, y.y * g.y, y.z * g.z, y.w * g.w);
+      ld_param<FULL>(p.g, col, D, t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] *= t[i];
     }
     if (p.b) {
-      const float4 b = FULL ? *reinterpret_cast<const float4*>(p.b + col) : ld4<float>(p.b, col, D, false);
-      y = make_float4(y.x + b.x, y.y + b.y, y.z + b.z, y.w + b.w);
+      ld_param<FULL>(p.b, col, D, t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] += t[i];
     }
-    if (!FULL) y = mask4(y, col, D);
-    if (p.y8.q) {
-      uint32_t w;
-      const uint32_t byte = block8_quantize(y, w);
-      uint8_t* qr = static_cast<uint8_t*>(p.y8.q) + (size_t)row * p.y8.ldq;
-      if (FULL) *reinterpret_cast<uint32_t*>(qr + col) = w;
-      else stq4(qr, col, D, w);
-      if (lane == 0) p.y8.scale[(size_t)(part * NB + j) * p.y8.lds + row] = (uint8_t)byte;
-    }
-    if (p.y.p) {
-      if (p.y.dtype == LAZYMAR_F32)
-        st4<float>(static_cast<float*>(p.y.p) + (size_t)row * p.y.ld, col, FULL ? col + 4 : D, FULL || p.vec, y);
-      else
-        st4<bf16>(static_cast<bf16*>(p.y.p) + (size_t)row * p.y.ld, col, FULL ? col + 4 : D, FULL || p.vec, y);
-    }
+    mask8<FULL>(y, col, D);
+    if (p.y8.q) put8<FULL>(p.y8, row, cc, D, y);
+    if (p.y.p) st_mat<FULL>(p.y, row, cc, D, sm, y);
   }
 }
 
-template <int NB, int WPR>
+bool param_vec(const float* p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; }
+
+template <int NC, int WPR>
 cudaError_t ln_forward_run(const Ctx& c, const LnForward& p) {
-  constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR;
-  const dim3 grid((unsigned)((p.M + GROUPS - 1) / GROUPS)), block(WPR > 8 ? WPR * 32 : 256);
-  const bool aligned = ((reinterpret_cast<uintptr_t>(p.g) | reinterpret_cast<uintptr_t>(p.b)) & 15u) == 0;
-  if (p.vec && aligned && p.D == NB * WPR * kBlk)
-    return launch_pdl(ln_forward_kernel<NB, WPR, true>, grid, block, 0, c.stream, p);
-  return launch_pdl(ln_forward_kernel<NB, WPR, false>, grid, block, 0, c.stream, p);
+  constexpr int GROUPS = 8 / WPR;
+  const dim3 grid((unsigned)((p.M + GROUPS - 1) / GROUPS)), block(256);
+  if (p.x.vec && p.y.vec && param_vec(p.g) && param_vec(p.b) && p.D == NC * WPR * kChunk)
+    return launch_pdl(ln_forward_kernel<NC, WPR, true>, grid, block, 0, c.stream, p);
+  return launch_pdl(ln_forward_kernel<NC, WPR, false>, grid, block, 0, c.stream, p);
 }
 
 // ---------------------------------------------------------------------------
@@ -234,168 +310,328 @@ cudaError_t column_sums(const Ctx& c, const float* part, int P, int n, int n1, f
 // A CTA works through rows of a stride and keeps its share of dg and db in
 // registers (a lane owns its columns), so that the column sums cost one pass
 // over 2 D floats a CTA instead of one over the data.
-template <int NB, int WPR, bool FULL>
-__global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256) ln_backward_kernel(const LnBackward p) {
-  constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR;
-  extern __shared__ float cols[];  // [2][NB WPR 128]
-  __shared__ float red[2][2][GROUPS][WPR];
+
+// dg and db of the CTA's row groups added in turn, to its row of the workspace.
+template <int NC, int WPR>
+__device__ __forceinline__ void put_columns(const LnBackward& p, float* cols, const float (&dg)[NC][8],
+                                            const float (&db)[NC][8]) {
+  constexpr int W = NC * WPR * kChunk;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
-  const int D = p.D, c0 = part * NB * kBlk + 4 * lane;
-  pdl_wait();
-  pdl_trigger();
-  float4 dg[NB], db[NB];
+  const int groups = (int)(blockDim.x >> 5) / WPR;
+  for (int g = 0; g < groups; ++g) {
+    __syncthreads();
+    if (g == grp) {
 #pragma unroll
-  for (int j = 0; j < NB; ++j) dg[j] = db[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int stride = (int)gridDim.x * GROUPS;
-  int it = 0;
-  // (every warp makes the same number of rounds: row_sum is a CTA-wide step)
-  for (int base = (int)blockIdx.x * GROUPS; base < p.M; base += stride, it ^= 1) {
-    const int row = base + grp;
-    const bool live = row < p.M;
-    float4 xh[NB], a[NB];
-    if (live) {
-      if (p.dy.dtype == LAZYMAR_F32) {
-        const float* r = static_cast<const float*>(p.dy.p) + (size_t)row * p.dy.ld;
+      for (int c = 0; c < NC; ++c) {
+        float* s = cols + (part * NC + c) * kChunk + 8 * lane;
 #pragma unroll
-        for (int j = 0; j < NB; ++j) a[j] = ld4t<float, FULL>(r, c0 + j * kBlk, D, p.vec);
-      } else {
-        const bf16* r = static_cast<const bf16*>(p.dy.p) + (size_t)row * p.dy.ld;
-#pragma unroll
-        for (int j = 0; j < NB; ++j) a[j] = ld4t<bf16, FULL>(r, c0 + j * kBlk, D, p.vec);
-      }
-      const float mean = p.mean[row], rstd = p.rstd[row];
-      if (!p.x.p) {
-        const uint8_t* r = static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq;
-        const int nb = (D + kBlk - 1) / kBlk - part * NB;  // blocks from this warp's first on
-        const uint32_t sb = lane < NB && lane < nb ? p.x8.scale[(size_t)(part * NB + lane) * p.x8.lds + row] : 0u;
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-          const uint32_t w = FULL ? *reinterpret_cast<const uint32_t*>(r + c0 + j * kBlk) : ldq4(r, c0 + j * kBlk, D);
-          xh[j] = e4m3x4_to_f4(w, block8_scale(__shfl_sync(0xffffffffu, sb, j)));
+        for (int i = 0; i < 8; ++i) {
+          s[i] = g == 0 ? dg[c][i] : s[i] + dg[c][i];
+          s[W + i] = g == 0 ? db[c][i] : s[W + i] + db[c][i];
         }
-      } else if (p.x.dtype == LAZYMAR_F32) {
-        const float* r = static_cast<const float*>(p.x.p) + (size_t)row * p.x.ld;
-#pragma unroll
-        for (int j = 0; j < NB; ++j) xh[j] = ld4t<float, FULL>(r, c0 + j * kBlk, D, p.vec);
-      } else {
-        const bf16* r = static_cast<const bf16*>(p.x.p) + (size_t)row * p.x.ld;
-#pragma unroll
-        for (int j = 0; j < NB; ++j) xh[j] = ld4t<bf16, FULL>(r, c0 + j * kBlk, D, p.vec);
-      }
-      float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const int col = c0 + j * kBlk;
-        float4 h = make_float4((xh[j].x - mean) * rstd, (xh[j].y - mean) * rstd, (xh[j].z - mean) * rstd,
-                               (xh[j].w - mean) * rstd);
-        if (!FULL) h = mask4(h, col, D);
-        xh[j] = h;
-        const float4 y = a[j];
-        dg[j].x = fmaf(y.x, h.x, dg[j].x); dg[j].y = fmaf(y.y, h.y, dg[j].y);
-        dg[j].z = fmaf(y.z, h.z, dg[j].z); dg[j].w = fmaf(y.w, h.w, dg[j].w);
-        db[j].x += y.x; db[j].y += y.y; db[j].z += y.z; db[j].w += y.w;
-        if (p.g) {
-          const float4 g = FULL ? *reinterpret_cast<const float4*>(p.g + col) : ld4<float>(p.g, col, D, false);
-          a[j] = make_float4(y.x * g.x, y.y * g.y, y.z * g.z, y.w * g.w);
-        }
-        s1 += sum4(a[j]);
-        s2 += (a[j].x * h.x + a[j].y * h.y) + (a[j].z * h.z + a[j].w * h.w);
-      }
-      s1 = warp_sum(s1);
-      s2 = warp_sum(s2);
-      if constexpr (WPR > 1) {
-        if (lane == 0) {
-          red[it][0][grp][part] = s1;
-          red[it][1][grp][part] = s2;
-        }
-      } else {
-        red[it][0][grp][0] = s1;  // (its own warp's: read back below)
-        red[it][1][grp][0] = s2;
       }
     }
-    if constexpr (WPR > 1) __syncthreads();
-    else __syncwarp();
+  }
+  __syncthreads();
+  float* o = p.ws + (size_t)blockIdx.x * 2 * p.D;
+  for (int i = threadIdx.x; i < 2 * p.D; i += blockDim.x) o[i] = i < p.D ? cols[i] : cols[W + i - p.D];
+}
+
+// Widths that are a multiple of eight up to 1280 with rows on boundaries: a warp
+// a row. The rows of dy, x and dres come by bulk copies into the warp's ring in
+// shared memory, so that the next rows are on their way while this one is worked
+// on and nothing of them waits in registers; a row is read twice from there, for
+// the sums and for dx.
+template <int NC>
+__global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackward p, int depth, uint32_t row_bytes,
+                                                                  uint32_t x_at, uint32_t r_at, unsigned* err) {
+  extern __shared__ __align__(128) uint8_t ring_smem[];  // g [NC 256] fp32, then [warps][depth][row_bytes]
+  __shared__ uint64_t bars[8][4];
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5, D = p.D;
+  float* gs = reinterpret_cast<float*>(ring_smem);
+  uint8_t* ring = ring_smem + NC * kChunk * 4 + (size_t)warp * depth * row_bytes;
+  if (threadIdx.x == 0) abort_word = 0;
+  if (lane == 0)
+    for (int s = 0; s < depth; ++s) mbar_init(&bars[warp][s], 1);
+  fence_mbar_init();
+  pdl_wait();
+  pdl_trigger();
+  for (int i = threadIdx.x; i < NC * kChunk; i += blockDim.x) gs[i] = i < D ? (p.g ? p.g[i] : 1.f) : 0.f;
+  __syncthreads();
+  const int step = (int)gridDim.x * warps, first = (int)blockIdx.x * warps + warp;
+  const size_t dy_e = p.dy.dtype == LAZYMAR_F32 ? 4 : 2, x_e = p.x.dtype == LAZYMAR_F32 ? 4 : 2;
+  const uint32_t dy_b = (uint32_t)(D * dy_e), x_b = p.x.p ? (uint32_t)(D * x_e) : (uint32_t)((D + 15) & ~15);
+  const uint32_t r_b = p.dres.p ? (uint32_t)D * 4 : 0u;
+  auto fetch = [&](int row, int s) {
+    uint8_t* dst = ring + (size_t)s * row_bytes;
+    uint64_t* bar = &bars[warp][s];
+    mbar_arrive_expect_tx(bar, dy_b + x_b + r_b);
+    bulk_load(dst, static_cast<const uint8_t*>(p.dy.p) + (size_t)row * p.dy.ld * dy_e, dy_b, bar);
+    bulk_load(dst + x_at,
+              p.x.p ? static_cast<const uint8_t*>(p.x.p) + (size_t)row * p.x.ld * x_e
+                    : static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq,
+              x_b, bar);
+    if (r_b) bulk_load(dst + r_at, static_cast<const float*>(p.dres.p) + (size_t)row * p.dres.ld, r_b, bar);
+  };
+  if (lane == 0)
+    for (int s = 0; s < depth; ++s)
+      if ((long long)first + (long long)s * step < p.M) fetch(first + s * step, s);
+  // scales (lane: block), mean and rstd of the next row
+  float mean = 0.f, rstd = 0.f;
+  uint32_t sb = 0;
+  auto statistics = [&](long long row) {
+    if (row >= p.M) return;
+    mean = p.mean[row];
+    rstd = p.rstd[row];
+    if (!p.x.p && lane * kBlk < D && lane < 2 * NC) sb = p.x8.scale[(size_t)lane * p.x8.lds + row];
+  };
+  statistics(first);
+
+  float dg[NC][8], db[NC][8];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.f;
+  int slot = 0;
+  uint32_t phase = 0;
+  for (long long row = first; row < p.M; row += step) {
+    const float mu = mean, rs = rstd;
+    const uint32_t scales = sb;
+    statistics(row + step);
+    const bool ok = mbar_wait(&bars[warp][slot], phase, abort_flag, err);
+    if (!__all_sync(0xffffffffu, ok)) break;
+    const uint8_t* src = ring + (size_t)slot * row_bytes;
+    auto take = [&](int c, float (&y)[8], float (&h)[8]) {
+      const int at = c * kChunk + 8 * lane;
+      if (p.dy.dtype == LAZYMAR_F32) {
+        const float4* f = reinterpret_cast<const float4*>(src + 4 * at);
+        const float4 a = f[0], b = f[1];
+        y[0] = a.x; y[1] = a.y; y[2] = a.z; y[3] = a.w; y[4] = b.x; y[5] = b.y; y[6] = b.z; y[7] = b.w;
+      } else {
+        bf16x8(*reinterpret_cast<const uint4*>(src + 2 * at), y);
+      }
+      if (!p.x.p) {
+        const uint32_t byte = __shfl_sync(0xffffffffu, scales, 2 * c + (lane >> 4));
+        block8_values(*reinterpret_cast<const uint2*>(src + x_at + at), block8_scale(byte), h);
+      } else if (p.x.dtype == LAZYMAR_F32) {
+        const float4* f = reinterpret_cast<const float4*>(src + x_at + 4 * at);
+        const float4 a = f[0], b = f[1];
+        h[0] = a.x; h[1] = a.y; h[2] = a.z; h[3] = a.w; h[4] = b.x; h[5] = b.y; h[6] = b.z; h[7] = b.w;
+      } else {
+        bf16x8(*reinterpret_cast<const uint4*>(src + x_at + 2 * at), h);
+      }
+      if (at >= D) {  // what a shorter row leaves of the ring's last columns
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = h[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = (h[i] - mu) * rs;
+    };
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float y[8], h[8];
+      take(c, y, h);
+      const float4* gp = reinterpret_cast<const float4*>(gs + c * kChunk + 8 * lane);
+      const float4 g0 = gp[0], g1 = gp[1];
+      const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float a = y[i] * g[i];
+        dg[c][i] = fmaf(y[i], h[i], dg[c][i]);
+        db[c][i] += y[i];
+        s1 += a;
+        s2 = fmaf(a, h[i], s2);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    s1 /= (float)D;
+    s2 /= (float)D;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int at = c * kChunk + 8 * lane;
+      float y[8], h[8];
+      take(c, y, h);
+      if (at < D) {
+        const float4* gp = reinterpret_cast<const float4*>(gs + at);
+        const float4 g0 = gp[0], g1 = gp[1];
+        const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = rs * (fmaf(y[i], g[i], -s1) - h[i] * s2);
+        if (r_b) {
+          const float4* rp = reinterpret_cast<const float4*>(src + r_at + 4 * at);
+          const float4 r0 = rp[0], r1 = rp[1];
+          const float r[8] = {r0.x, r0.y, r0.z, r0.w, r1.x, r1.y, r1.z, r1.w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] += r[i];
+        }
+        if (p.dx.dtype == LAZYMAR_F32) st8a(static_cast<float*>(p.dx.p) + (size_t)row * p.dx.ld + at, y);
+        else st8a(static_cast<bf16*>(p.dx.p) + (size_t)row * p.dx.ld + at, y);
+      }
+    }
+    __syncwarp();  // every lane has read the row
+    if (lane == 0 && row + (long long)depth * step < p.M) {
+      fence_proxy_async_smem();
+      fetch((int)(row + (long long)depth * step), slot);
+    }
+    if (++slot == depth) { slot = 0; phase ^= 1u; }
+  }
+  if (!p.dg) return;
+  __syncthreads();  // the ring is free: the column sums take its place
+  put_columns<NC, 1>(p, gs, dg, db);
+}
+
+// Any width, stride and alignment: WPR warps a row, NC chunks of 256 columns a
+// warp, dy and x in registers.
+template <int NC, int WPR>
+__global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256) ln_backward_kernel(const LnBackward p) {
+  constexpr int WARPS = WPR > 8 ? WPR : 8, GROUPS = WARPS / WPR;
+  extern __shared__ float cols[];  // [2][NC WPR 256]
+  __shared__ float red[2][2][GROUPS][WPR];
+  __shared__ float stage[WARPS][kChunk];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
+  float* sm = stage[warp];
+  const int D = p.D, c0 = part * NC * kChunk;
+  pdl_wait();
+  pdl_trigger();
+  float dg[NC][8], db[NC][8];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.f;
+  const int stride = (int)gridDim.x * GROUPS;
+  int it = 0;
+  // (every warp makes the same number of rounds: the row sums are a CTA-wide step)
+  for (long long base = (long long)blockIdx.x * GROUPS; base < p.M; base += stride, it ^= 1) {
+    const long long row = base + grp;
+    const bool live = row < p.M;
+    float h[NC][8], a[NC][8], s1 = 0.f, s2 = 0.f, rstd = 0.f;
     if (live) {
-      float s1 = 0.f, s2 = 0.f;
+      const float mean = p.mean[row];
+      rstd = p.rstd[row];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int cc = c0 + c * kChunk, col = cc + 8 * lane;
+        ld_mat<false>(p.dy, row, cc, D, sm, a[c]);
+        if (!p.x.p) {
+          const uint2 w = ldq8(static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq, col, D);
+          const uint32_t byte = col < D ? p.x8.scale[(size_t)(col / kBlk) * p.x8.lds + row] : 127u;
+          block8_values(w, block8_scale(byte), h[c]);
+        } else {
+          ld_mat<false>(p.x, row, cc, D, sm, h[c]);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int col = c0 + c * kChunk + 8 * lane;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[c][i] = (h[c][i] - mean) * rstd;
+        mask8<false>(h[c], col, D);
+        float g[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = 1.f;
+        if (p.g) ld_param<false>(p.g, col, D, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          dg[c][i] = fmaf(a[c][i], h[c][i], dg[c][i]);
+          db[c][i] += a[c][i];
+          a[c][i] *= g[i];
+          s1 += a[c][i];
+          s2 = fmaf(a[c][i], h[c][i], s2);
+        }
+      }
+    }
+    s1 = warp_sum(s1);
+    s2 = warp_sum(s2);
+    if constexpr (WPR > 1) {
+      if (lane == 0) {
+        red[it][0][grp][part] = s1;
+        red[it][1][grp][part] = s2;
+      }
+      __syncthreads();
+      s1 = s2 = 0.f;
 #pragma unroll
       for (int i = 0; i < WPR; ++i) {
         s1 += red[it][0][grp][i];
         s2 += red[it][1][grp][i];
       }
+    }
+    if (live) {
       s1 /= (float)D;
       s2 /= (float)D;
-      const float rstd = p.rstd[row];
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const int col = c0 + j * kBlk;
-        float4 o = make_float4(rstd * (a[j].x - s1 - xh[j].x * s2), rstd * (a[j].y - s1 - xh[j].y * s2),
-                               rstd * (a[j].z - s1 - xh[j].z * s2), rstd * (a[j].w - s1 - xh[j].w * s2));
+      for (int c = 0; c < NC; ++c) {
+        const int cc = c0 + c * kChunk;
+        if (cc >= D) break;  // (uniform over the warp)
+        float o[8], r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = rstd * (a[c][i] - s1 - h[c][i] * s2);
         if (p.dres.p) {
-          const float4 r = ld4t<float, FULL>(static_cast<const float*>(p.dres.p) + (size_t)row * p.dres.ld, col, D,
-                                             p.vec);
-          o = make_float4(o.x + r.x, o.y + r.y, o.z + r.z, o.w + r.w);
-        }
-        if (p.dx.dtype == LAZYMAR_F32)
-          st4<float>(static_cast<float*>(p.dx.p) + (size_t)row * p.dx.ld, col, FULL ? col + 4 : D, FULL || p.vec, o);
-        else
-          st4<bf16>(static_cast<bf16*>(p.dx.p) + (size_t)row * p.dx.ld, col, FULL ? col + 4 : D, FULL || p.vec, o);
-      }
-    }
-  }
-  if (!p.dg) return;
-  // the CTA's rows' sums: its groups add in turn
-  constexpr int W = NB * WPR * kBlk;
-  for (int g = 0; g < GROUPS; ++g) {
-    if (g == grp) {
+          ld_mat<false>(p.dres, row, cc, D, sm, r);
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        float4* s = reinterpret_cast<float4*>(cols + c0 + j * kBlk);
-        float4* t = reinterpret_cast<float4*>(cols + W + c0 + j * kBlk);
-        if (g == 0) {
-          *s = dg[j];
-          *t = db[j];
-        } else {
-          const float4 u = *s, w = *t;
-          *s = make_float4(u.x + dg[j].x, u.y + dg[j].y, u.z + dg[j].z, u.w + dg[j].w);
-          *t = make_float4(w.x + db[j].x, w.y + db[j].y, w.z + db[j].z, w.w + db[j].w);
+          for (int i = 0; i < 8; ++i) o[i] += r[i];
         }
+        st_mat<false>(p.dx, row, cc, D, sm, o);
       }
     }
-    __syncthreads();
   }
-  float* o = p.ws + (size_t)blockIdx.x * 2 * D;
-  for (int i = threadIdx.x; i < 2 * D; i += blockDim.x) o[i] = i < D ? cols[i] : cols[W + i - D];
+  if (p.dg) put_columns<NC, WPR>(p, cols, dg, db);
 }
 
-// CTAs of a backward launch: two resident ones for every SM.
+// CTAs of a backward launch: at most two resident ones for every SM.
 int ln_backward_ctas(int M, int groups) {
   const int need = (M + groups - 1) / groups, most = 2 * kSMs;
   return need < most ? need : most;
 }
 
-template <int NB, int WPR>
-cudaError_t ln_backward_run(const Ctx& c, const LnBackward& p) {
-  constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR;
-  const int ctas = ln_backward_ctas(p.M, GROUPS);
-  const dim3 grid((unsigned)ctas), block(WPR > 8 ? WPR * 32 : 256);
-  constexpr size_t smem = (size_t)2 * NB * WPR * kBlk * sizeof(float);
-  const bool full = p.vec && (reinterpret_cast<uintptr_t>(p.g) & 15u) == 0 && p.D == NB * WPR * kBlk;
-  cudaError_t e;
-  if (full) {
-    if (smem > 48 * 1024)
-      if ((e = cudaFuncSetAttribute(ln_backward_kernel<NB, WPR, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    (int)smem)) != cudaSuccess)
-        return e;
-    e = launch_pdl(ln_backward_kernel<NB, WPR, true>, grid, block, smem, c.stream, p);
-  } else {
-    if (smem > 48 * 1024)
-      if ((e = cudaFuncSetAttribute(ln_backward_kernel<NB, WPR, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    (int)smem)) != cudaSuccess)
-        return e;
-    e = launch_pdl(ln_backward_kernel<NB, WPR, false>, grid, block, smem, c.stream, p);
+cudaError_t big_smem(const void* kernel, size_t smem) {
+  return smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)
+                          : cudaSuccess;
+}
+
+// Rows in shared memory: as many a warp, up to four, as let two CTAs of eight
+// warps live on an SM, or one CTA, or one of four warps.
+template <int NC>
+cudaError_t ln_backward_ring_run(const Ctx& c, const LnBackward& p, int* ctas) {
+  const uint32_t dy_b = (uint32_t)NC * kChunk * (p.dy.dtype == LAZYMAR_F32 ? 4 : 2);
+  const uint32_t x_b = (uint32_t)NC * kChunk * (p.x.p ? (p.x.dtype == LAZYMAR_F32 ? 4 : 2) : 1);
+  const uint32_t r_b = p.dres.p ? (uint32_t)NC * kChunk * 4 : 0u, row_b = dy_b + x_b + r_b;
+  const size_t fixed = (size_t)NC * kChunk * 4, sums = (size_t)2 * NC * kChunk * 4;
+  int warps = 8, per_sm = 2;
+  long long depth = ((long long)110 * 1024 - (long long)fixed) / ((long long)warps * row_b);
+  if (depth < 2) {
+    per_sm = 1;
+    depth = ((long long)220 * 1024 - (long long)fixed) / ((long long)warps * row_b);
   }
-  if (e != cudaSuccess || !p.dg) return e;
-  return column_sums(c, p.ws, ctas, 2 * p.D, p.D, p.dg, p.db, p.accumulate);
+  if (depth < 2) {
+    warps = 4;
+    depth = ((long long)220 * 1024 - (long long)fixed) / ((long long)warps * row_b);
+  }
+  if (depth > 4) depth = 4;
+  size_t smem = fixed + (size_t)warps * depth * row_b;
+  if (smem < sums) smem = sums;
+  const int need = (p.M + warps - 1) / warps, most = per_sm * kSMs;
+  *ctas = need < most ? need : most;
+  cudaError_t e = big_smem(reinterpret_cast<const void*>(ln_backward_ring_kernel<NC>), smem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(ln_backward_ring_kernel<NC>, dim3((unsigned)*ctas), dim3((unsigned)warps * 32), smem, c.stream, p,
+                    (int)depth, row_b, dy_b, dy_b + x_b, c.err);
+}
+
+template <int NC, int WPR>
+cudaError_t ln_backward_run(const Ctx& c, const LnBackward& p, int* ctas) {
+  constexpr int WARPS = WPR > 8 ? WPR : 8;
+  constexpr size_t smem = (size_t)2 * NC * WPR * kChunk * sizeof(float);
+  *ctas = ln_backward_ctas(p.M, WARPS / WPR);
+  cudaError_t e = big_smem(reinterpret_cast<const void*>(ln_backward_kernel<NC, WPR>), smem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(ln_backward_kernel<NC, WPR>, dim3((unsigned)*ctas), dim3(WARPS * 32), smem, c.stream, p);
 }
 
 // ---------------------------------------------------------------------------
@@ -407,33 +643,39 @@ cudaError_t ln_backward_run(const Ctx& c, const LnBackward& p) {
 // which leaves 241 entries a sign. A look-up takes half of the instructions of
 // an evaluation and has the error of erfcf and expf (1e-7) instead of a
 // polynomial's.
-constexpr int kGradLo = (127 - 26) << 3, kGradHi = (127 + 4) << 3, kGradN = kGradHi - kGradLo + 1;
+constexpr int kGradLo = (127 - 26) << 3, kGradN = ((127 + 4) << 3) - kGradLo + 1, kGradNeg = 256;
+constexpr int kGradSize = kGradNeg + kGradN;
 
 __device__ __forceinline__ void gelu_grad_table(float* tab) {
-  for (int i = threadIdx.x; i < 2 * kGradN; i += blockDim.x) {
-    const float a = __uint_as_float((uint32_t)(kGradLo + i % kGradN) << 20), x = i < kGradN ? a : -a;
+  for (int i = threadIdx.x; i < kGradSize; i += blockDim.x) {
+    const int j = i & (kGradNeg - 1);
+    if (j >= kGradN) continue;
+    const float a = __uint_as_float((uint32_t)(kGradLo + j) << 20), x = i < kGradNeg ? a : -a;
     tab[i] = fmaf(x * 0.39894228040143268f, expf(-0.5f * x * x), 0.5f * erfcf(-0.70710678118654752f * x));
   }
 }
 __device__ __forceinline__ float gelu_grad_at(const float* tab, float x) {
   const uint32_t b = __float_as_uint(x);
-  const int i = min(max((int)((b >> 20) & 0x7FFu), kGradLo), kGradHi) - kGradLo + (((int)b >> 31) & kGradN);
-  return fmaf(x, 0.f, tab[i]);  // NaN stays NaN
+  // byte offsets: entry (exponent and mantissa bits - kGradLo), clamped, 1024 up for negative x
+  const int i = min(max((int)((b >> 18) & 0x1FFCu) - 4 * kGradLo, 0), 4 * (kGradN - 1));
+  const uint32_t at = ((b >> 21) & (4u * kGradNeg)) | (uint32_t)i;
+  return fmaf(x, 0.f, *reinterpret_cast<const float*>(reinterpret_cast<const char*>(tab) + at));  // NaN stays NaN
 }
 
 // in [rows, cols] through an optional GELU' of the checkpoint u, to `out`
-// and / or block8, with optional column sums. A warp owns a block of 128
-// columns and a stride of rows, kRowsU at a time, so that the column sums stay
-// in its registers; neighbouring warps take neighbouring blocks of the same
-// rows.
+// and / or block8, with optional column sums. A warp owns 256 columns and a
+// stride of rows, kRowsU at a time, so that the column sums stay in its
+// registers; neighbouring warps take neighbouring columns of the same rows.
 constexpr int kRowsU = 4;
 
 template <typename T, bool HAS_U>
-__global__ void __launch_bounds__(256) rows8_kernel(const Rows8 p, int nblk, int groups) {
-  const int lane = threadIdx.x & 31;
-  const int task = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int grp = task / nblk, blk = task - grp * nblk, col = blk * kBlk + 4 * lane, cols = p.cols;
-  __shared__ float grad[HAS_U ? 2 * kGradN : 1];
+__global__ void __launch_bounds__(256, 3) rows8_kernel(const Rows8 p, int nchunk, int groups) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int task = (int)blockIdx.x * 8 + warp;
+  const int grp = task / nchunk, c0 = (task - grp * nchunk) * kChunk, col = c0 + 8 * lane, cols = p.cols;
+  __shared__ float grad[HAS_U ? kGradSize : 1];
+  __shared__ float stage[8][kChunk];
+  float* sm = stage[warp];
   if (HAS_U) {
     gelu_grad_table(grad);
     __syncthreads();
@@ -441,94 +683,143 @@ __global__ void __launch_bounds__(256) rows8_kernel(const Rows8 p, int nblk, int
   pdl_wait();
   pdl_trigger();
   if (grp >= groups) return;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  const T* in = static_cast<const T*>(p.in.p);
-  for (long long r0 = (long long)grp * kRowsU; r0 < p.rows; r0 += (long long)groups * kRowsU) {
-    float4 v[kRowsU];
-    uint32_t uq[kRowsU], us[kRowsU];
+  float acc[8];
 #pragma unroll
-    for (int i = 0; i < kRowsU; ++i) {
-      const size_t r = (size_t)(r0 + i);
-      const bool live = r0 + i < p.rows;
-      v[i] = live ? ld4<T>(in + r * p.in.ld, col, cols, p.vec) : make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+  const T* in = static_cast<const T*>(p.in.p);
+  const bool whole = p.in.vec && col + 8 <= cols;
+  const uint8_t* us = HAS_U ? p.u.scale + (size_t)(min(col, cols - 1) / kBlk) * p.u.lds : nullptr;
+  for (long long r0 = (long long)grp * kRowsU; r0 < p.rows; r0 += (long long)groups * kRowsU) {
+    constexpr int W = sizeof(T) / 2;
+    uint4 raw[kRowsU][W];
+    uint2 uq[kRowsU];
+    uint32_t ub[kRowsU];
+#pragma unroll
+    for (int j = 0; j < kRowsU; ++j) {
+      const size_t r = (size_t)min(r0 + j, (long long)p.rows - 1);
+      if (whole) {
+        const uint4* src = reinterpret_cast<const uint4*>(in + r * p.in.ld + col);
+#pragma unroll
+        for (int k = 0; k < W; ++k) raw[j][k] = src[k];
+      }
       if (HAS_U) {
-        uq[i] = live ? ldq4(static_cast<const uint8_t*>(p.u.q) + r * p.u.ldq, col, cols) : 0u;
-        us[i] = live ? p.u.scale[(size_t)blk * p.u.lds + r] : 0u;
+        uq[j] = ldq8(static_cast<const uint8_t*>(p.u.q) + r * p.u.ldq, col, cols);
+        ub[j] = us[r];
       }
     }
 #pragma unroll
-    for (int i = 0; i < kRowsU; ++i) {
-      if (r0 + i >= p.rows) break;
-      const size_t r = (size_t)(r0 + i);
+    for (int j = 0; j < kRowsU; ++j) {
+      if (r0 + j >= p.rows) break;
+      const size_t r = (size_t)(r0 + j);
+      float v[8];
+      if (whole) {
+        if constexpr (W == 1) {
+          bf16x8(raw[j][0], v);
+        } else {
+          const uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w,
+                                 raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+        }
+      }
+      if (!p.in.vec || c0 + kChunk > cols) {  // (uniform over the warp; whole lanes read again)
+        ld8<T>(in + r * p.in.ld, c0, cols, p.in.vec, sm, v);
+      }
       if (HAS_U) {
-        const float4 u = e4m3x4_to_f4(uq[i], block8_scale(us[i]));
-        v[i].x *= gelu_grad_at(grad, u.x);
-        v[i].y *= gelu_grad_at(grad, u.y);
-        v[i].z *= gelu_grad_at(grad, u.z);
-        v[i].w *= gelu_grad_at(grad, u.w);
+        float u[8];
+        block8_values(uq[j], block8_scale(ub[j]), u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= gelu_grad_at(grad, u[i]);
       }
       if (p.db) {
-        acc.x += v[i].x; acc.y += v[i].y; acc.z += v[i].z; acc.w += v[i].w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += v[i];
       }
-      if (p.out.p) {
-        if (p.out.dtype == LAZYMAR_F32)
-          st4<float>(static_cast<float*>(p.out.p) + r * p.out.ld, col, cols, p.vec, v[i]);
-        else
-          st4<bf16>(static_cast<bf16*>(p.out.p) + r * p.out.ld, col, cols, p.vec, v[i]);
-      }
-      if (p.out8.q) {
-        uint32_t w;
-        const uint32_t byte = block8_quantize(v[i], w);
-        stq4(static_cast<uint8_t*>(p.out8.q) + r * p.out8.ldq, col, cols, w);
-        if (lane == 0) p.out8.scale[(size_t)blk * p.out8.lds + r] = (uint8_t)byte;
-      }
+      if (p.out.p) st_mat<false>(p.out, r, c0, cols, sm, v);
+      if (p.out8.q) put8<false>(p.out8, r, c0, cols, v);
     }
   }
-  if (p.db) st4<float>(p.ws + (size_t)grp * cols, col, cols, false, acc);
+  if (p.db) {
+    float* o = p.ws + (size_t)grp * cols + col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col + i < cols) o[i] = acc[i];
+  }
 }
 
-// Row groups of a launch: about 48 warps for every SM in all.
-int rows8_groups(int rows, int nblk) {
-  const int want = (kSMs * 48 + nblk - 1) / nblk, most = (rows + kRowsU - 1) / kRowsU;
-  return want < most ? want : most;
+// Row groups of a launch: the 24 warps that fit on every SM, once.
+int rows8_groups(int rows, int nchunk) {
+  const int want = kSMs * 24 / nchunk, most = (rows + kRowsU - 1) / kRowsU;
+  return want < 1 ? 1 : want < most ? want : most;
 }
 
 // ---------------------------------------------------------------------------
 // Back to fp32 / bf16, and weights
 // ---------------------------------------------------------------------------
 template <typename T>
-__global__ void __launch_bounds__(256) unpack8_kernel(const lazymar_block8 q, T* __restrict__ x, int ld, int rows,
-                                                      int cols, int nblk, bool vec) {
-  const int lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(256, 4) unpack8_kernel(const lazymar_block8 q, T* __restrict__ x, int ld, int rows,
+                                                         int cols, int nchunk, bool vec) {
+  __shared__ float stage[8][kChunk];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
-  const long long tasks = (long long)rows * nblk, step = (long long)gridDim.x * 8 * 4;
-  for (long long t0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * 4; t0 < tasks; t0 += step) {
-    uint32_t w[4], s[4];
+  const long long tasks = (long long)rows * nchunk, step = (long long)gridDim.x * 8 * 4;
+  for (long long t0 = ((long long)blockIdx.x * 8 + warp) * 4; t0 < tasks; t0 += step) {
+    uint2 w[4];
+    uint32_t s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const long long t = t0 + i < tasks ? t0 + i : tasks - 1;
-      const size_t r = (size_t)(t / nblk);
-      const int blk = (int)(t - (long long)r * nblk);
-      w[i] = ldq4(static_cast<const uint8_t*>(q.q) + r * q.ldq, blk * kBlk + 4 * lane, cols);
-      s[i] = q.scale[(size_t)blk * q.lds + r];
+      const long long r = t / nchunk;
+      const int col = (int)(t - r * nchunk) * kChunk + 8 * lane;
+      w[i] = ldq8(static_cast<const uint8_t*>(q.q) + (size_t)r * q.ldq, col, cols);
+      s[i] = q.scale[(size_t)(min(col, cols - 1) / kBlk) * q.lds + r];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const long long t = t0 + i;
       if (t >= tasks) break;
-      const size_t r = (size_t)(t / nblk);
-      const int blk = (int)(t - (long long)r * nblk);
-      st4<T>(x + r * ld, blk * kBlk + 4 * lane, cols, vec, e4m3x4_to_f4(w[i], block8_scale(s[i])));
+      const long long r = t / nchunk;
+      float v[8];
+      block8_values(w[i], block8_scale(s[i]), v);
+      st8<T>(x + (size_t)r * ld, (int)(t - r * nchunk) * kChunk, cols, vec, stage[warp], v);
     }
   }
+}
+
+// Columns col..col+3 of a weight's row; those from K on read as zero.
+template <typename T>
+__device__ __forceinline__ float4 ld4(const T* row, int col, int K, bool vec) {
+  if (vec && col + 4 <= K) {
+    if constexpr (sizeof(T) == 2) {
+      const uint2 u = *reinterpret_cast<const uint2*>(row + col);
+      return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
+                         __uint_as_float(u.y & 0xFFFF0000u));
+    } else {
+      return *reinterpret_cast<const float4*>(row + col);
+    }
+  }
+  float v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = col + i < K ? to_f(row[col + i]) : 0.f;
+  return make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void stq4(uint8_t* row, int col, int K, uint32_t w) {
+  if (col + 4 <= K) {
+    *reinterpret_cast<uint32_t*>(row + col) = w;
+  } else {
+    for (int i = 0; col + i < K; ++i) row[col + i] = (uint8_t)(w >> (8 * i));
+  }
+}
+__device__ __forceinline__ float4 f4_nonfinite_to(float4 v, float to) {
+  return make_float4(nonfinite_to(v.x, to), nonfinite_to(v.y, to), nonfinite_to(v.z, to), nonfinite_to(v.w, to));
 }
 
 // One 128 x 128 block of a weight matrix to E4M3 with one scale, and the same
 // bytes transposed. Each warp holds 16 rows; the transpose goes through shared
 // memory, 132 bytes a row.
 __global__ void __launch_bounds__(256) pack_weight8_kernel(const Mat w, const lazymar_block8 q,
-                                                           const lazymar_block8 qt, int N, int K, bool vec) {
+                                                           const lazymar_block8 qt, int N, int K) {
   __shared__ uint32_t tile[128][33];
   __shared__ uint32_t mx[8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -542,10 +833,8 @@ __global__ void __launch_bounds__(256) pack_weight8_kernel(const Mat w, const la
     const int n = n0 + warp * 16 + i;
     v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (n < N) {
-      if (w.dtype == LAZYMAR_F32)
-        v[i] = ld4<float>(static_cast<const float*>(w.p) + (size_t)n * w.ld, col, K, vec);
-      else
-        v[i] = ld4<bf16>(static_cast<const bf16*>(w.p) + (size_t)n * w.ld, col, K, vec);
+      v[i] = w.dtype == LAZYMAR_F32 ? ld4<float>(static_cast<const float*>(w.p) + (size_t)n * w.ld, col, K, w.vec)
+                                    : ld4<bf16>(static_cast<const bf16*>(w.p) + (size_t)n * w.ld, col, K, w.vec);
     }
     const float4 z = f4_nonfinite_to(v[i], 0.f);
     m = fmaxf(m, fmax3(fmaxf(fabsf(z.x), fabsf(z.y)), fabsf(z.z), fabsf(z.w)));
@@ -587,18 +876,17 @@ __global__ void __launch_bounds__(256) pack_weight8_kernel(const Mat w, const la
 
 cudaError_t launch_ln_forward(const Ctx& c, const LnForward& p) {
   if (p.M == 0) return cudaSuccess;
-  const int nb = (p.D + kBlk - 1) / kBlk;
-  if (nb <= 1) return ln_forward_run<1, 1>(c, p);
-  if (nb <= 2) return ln_forward_run<2, 1>(c, p);
-  if (nb <= 4) return ln_forward_run<4, 1>(c, p);
-  if (nb <= 6) return ln_forward_run<6, 1>(c, p);
-  if (nb <= 8) return ln_forward_run<8, 1>(c, p);
-  if (nb <= 10) return ln_forward_run<10, 1>(c, p);
-  if (nb <= 16) return ln_forward_run<8, 2>(c, p);
-  if (nb <= 20) return ln_forward_run<10, 2>(c, p);
-  if (nb <= 32) return ln_forward_run<8, 4>(c, p);
-  if (nb <= 40) return ln_forward_run<10, 4>(c, p);
-  return ln_forward_run<8, 8>(c, p);
+  const int nc = (p.D + kChunk - 1) / kChunk;
+  if (nc <= 1) return ln_forward_run<1, 1>(c, p);
+  if (nc <= 2) return ln_forward_run<2, 1>(c, p);
+  if (nc <= 3) return ln_forward_run<3, 1>(c, p);
+  if (nc <= 4) return ln_forward_run<4, 1>(c, p);
+  if (nc <= 5) return ln_forward_run<5, 1>(c, p);
+  if (nc <= 8) return ln_forward_run<4, 2>(c, p);
+  if (nc <= 10) return ln_forward_run<5, 2>(c, p);
+  if (nc <= 16) return ln_forward_run<4, 4>(c, p);
+  if (nc <= 20) return ln_forward_run<5, 4>(c, p);
+  return ln_forward_run<4, 8>(c, p);
 }
 
 size_t ln_backward_workspace(int M, int D) {
@@ -610,23 +898,31 @@ cudaError_t launch_ln_backward(const Ctx& c, const LnBackward& p) {
     if (!p.dg || p.accumulate) return cudaSuccess;
     return column_sums(c, p.ws, 0, 2 * p.D, p.D, p.dg, p.db, false);
   }
-  const int nb = (p.D + kBlk - 1) / kBlk;
-  if (nb <= 1) return ln_backward_run<1, 1>(c, p);
-  if (nb <= 2) return ln_backward_run<2, 1>(c, p);
-  if (nb <= 4) return ln_backward_run<4, 1>(c, p);
-  if (nb <= 6) return ln_backward_run<3, 2>(c, p);
-  if (nb <= 8) return ln_backward_run<4, 2>(c, p);
-  if (nb <= 10) return ln_backward_run<5, 2>(c, p);
-  if (nb <= 16) return ln_backward_run<4, 4>(c, p);
-  if (nb <= 20) return ln_backward_run<5, 4>(c, p);
-  if (nb <= 32) return ln_backward_run<4, 8>(c, p);
-  if (nb <= 40) return ln_backward_run<5, 8>(c, p);
-  return ln_backward_run<4, 16>(c, p);
+  const int nc = (p.D + kChunk - 1) / kChunk;
+  int ctas = 0;
+  cudaError_t e;
+  if (nc <= 5 && p.D % 8 == 0 && p.dy.vec && p.x.vec && p.dres.vec && p.dx.vec) {
+    e = nc <= 1   ? ln_backward_ring_run<1>(c, p, &ctas)
+        : nc <= 2 ? ln_backward_ring_run<2>(c, p, &ctas)
+        : nc <= 3 ? ln_backward_ring_run<3>(c, p, &ctas)
+        : nc <= 4 ? ln_backward_ring_run<4>(c, p, &ctas)
+                  : ln_backward_ring_run<5>(c, p, &ctas);
+  } else {
+    e = nc <= 1    ? ln_backward_run<1, 1>(c, p, &ctas)
+        : nc <= 2  ? ln_backward_run<2, 1>(c, p, &ctas)
+        : nc <= 4  ? ln_backward_run<2, 2>(c, p, &ctas)
+        : nc <= 6  ? ln_backward_run<3, 2>(c, p, &ctas)
+        : nc <= 8  ? ln_backward_run<2, 4>(c, p, &ctas)
+        : nc <= 16 ? ln_backward_run<2, 8>(c, p, &ctas)
+                   : ln_backward_run<2, 16>(c, p, &ctas);
+  }
+  if (e != cudaSuccess || !p.dg) return e;
+  return column_sums(c, p.ws, ctas, 2 * p.D, p.D, p.dg, p.db, p.accumulate);
 }
 
 size_t rows8_workspace(int rows, int cols) {
   if (rows < 1 || cols < 1) return 0;
-  return (size_t)rows8_groups(rows, (cols + kBlk - 1) / kBlk) * cols * sizeof(float);
+  return (size_t)rows8_groups(rows, (cols + kChunk - 1) / kChunk) * cols * sizeof(float);
 }
 
 cudaError_t launch_rows8(const Ctx& c, const Rows8& p) {
@@ -634,37 +930,35 @@ cudaError_t launch_rows8(const Ctx& c, const Rows8& p) {
     if (!p.db || p.accumulate) return cudaSuccess;
     return column_sums(c, p.ws, 0, p.cols, p.cols, p.db, nullptr, false);
   }
-  const int nblk = (p.cols + kBlk - 1) / kBlk, groups = rows8_groups(p.rows, nblk);
-  const dim3 grid((unsigned)(((long long)nblk * groups + 7) / 8)), block(256);
+  const int nchunk = (p.cols + kChunk - 1) / kChunk, groups = rows8_groups(p.rows, nchunk);
+  const dim3 grid((unsigned)(((long long)nchunk * groups + 7) / 8)), block(256);
   cudaError_t e;
   if (p.in.dtype == LAZYMAR_F32)
-    e = p.u.q ? launch_pdl(rows8_kernel<float, true>, grid, block, 0, c.stream, p, nblk, groups)
-              : launch_pdl(rows8_kernel<float, false>, grid, block, 0, c.stream, p, nblk, groups);
+    e = p.u.q ? launch_pdl(rows8_kernel<float, true>, grid, block, 0, c.stream, p, nchunk, groups)
+              : launch_pdl(rows8_kernel<float, false>, grid, block, 0, c.stream, p, nchunk, groups);
   else
-    e = p.u.q ? launch_pdl(rows8_kernel<bf16, true>, grid, block, 0, c.stream, p, nblk, groups)
-              : launch_pdl(rows8_kernel<bf16, false>, grid, block, 0, c.stream, p, nblk, groups);
+    e = p.u.q ? launch_pdl(rows8_kernel<bf16, true>, grid, block, 0, c.stream, p, nchunk, groups)
+              : launch_pdl(rows8_kernel<bf16, false>, grid, block, 0, c.stream, p, nchunk, groups);
   if (e != cudaSuccess || !p.db) return e;
   return column_sums(c, p.ws, groups, p.cols, p.cols, p.db, nullptr, p.accumulate);
 }
 
 cudaError_t launch_unpack8(const Ctx& c, const lazymar_block8& q, const MatOut& x, int rows, int cols) {
   if (rows == 0) return cudaSuccess;
-  const int nblk = (cols + kBlk - 1) / kBlk;
-  const bool vec = x.ld % 4 == 0 && reinterpret_cast<uintptr_t>(x.p) % (x.dtype == LAZYMAR_F32 ? 16 : 8) == 0;
-  long long ctas = ((long long)rows * nblk + 31) / 32;
-  if (ctas > kSMs * 16) ctas = kSMs * 16;
+  const int nchunk = (cols + kChunk - 1) / kChunk;
+  long long ctas = ((long long)rows * nchunk + 31) / 32;
+  if (ctas > kSMs * 8) ctas = kSMs * 8;
   if (x.dtype == LAZYMAR_F32)
     return launch_pdl(unpack8_kernel<float>, dim3((unsigned)ctas), dim3(256), 0, c.stream, q, static_cast<float*>(x.p),
-                      x.ld, rows, cols, nblk, vec);
+                      x.ld, rows, cols, nchunk, x.vec);
   return launch_pdl(unpack8_kernel<bf16>, dim3((unsigned)ctas), dim3(256), 0, c.stream, q, static_cast<bf16*>(x.p),
-                    x.ld, rows, cols, nblk, vec);
+                    x.ld, rows, cols, nchunk, x.vec);
 }
 
 cudaError_t launch_pack_weight8(const Ctx& c, const Mat& w, const lazymar_block8& q, const lazymar_block8& qt, int N,
                                 int K) {
-  const bool vec = w.ld % 4 == 0 && reinterpret_cast<uintptr_t>(w.p) % (w.dtype == LAZYMAR_F32 ? 16 : 8) == 0;
   const dim3 grid((unsigned)((K + kBlk - 1) / kBlk), (unsigned)((N + kBlk - 1) / kBlk));
-  return launch_pdl(pack_weight8_kernel, grid, dim3(256), 0, c.stream, w, q, qt, N, K, vec);
+  return launch_pdl(pack_weight8_kernel, grid, dim3(256), 0, c.stream, w, q, qt, N, K);
 }
 
 }  // namespace lm

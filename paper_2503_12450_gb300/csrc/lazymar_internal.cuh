@@ -364,6 +364,14 @@ __device__ __forceinline__ void tma_store_2d(const void* tmap, const void* src, 
                "r"(c0), "r"(c1), "r"(smem_u32(src))
                : "memory");
 }
+// `bytes` (a multiple of 16) from 16-byte aligned global to 16-byte aligned shared
+// memory, completing on `bar`.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                   smem_u32(dst)),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Waits until the committed bulk stores of this thread have read their
 // shared-memory source (the buffer may be rewritten).

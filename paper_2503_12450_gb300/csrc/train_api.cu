@@ -23,8 +23,10 @@ lazymar_status check_mat(const void* p, int dtype, int ld, int cols, const char*
   if (!float_type(dtype) || ld < cols || !at(p, elem(dtype)) || !is_device_ptr(p)) return bad(msg);
   return LAZYMAR_OK;
 }
-// Rows on boundaries of four elements (absent tensors are).
-bool vec4(const void* p, int dtype, int ld) { return !p || (ld % 4 == 0 && at(p, 4 * elem(dtype))); }
+// Rows on boundaries of eight elements (absent tensors' are).
+bool vec8(const void* p, int dtype, int ld) { return !p || (ld % 8 == 0 && at(p, 8 * elem(dtype))); }
+Mat mat(const void* p, int ld, int dtype) { return Mat{p, ld, dtype, vec8(p, dtype, ld)}; }
+MatOut mat_out(void* p, int ld, int dtype) { return MatOut{p, ld, dtype, vec8(p, dtype, ld)}; }
 
 lazymar_status check_block8(const lazymar_block8* q, int cols, int scale_rows, const char* msg) {
   if (!q->q || !q->scale || q->ldq % 16 != 0 || q->ldq < cols || q->lds < scale_rows || !at(q->q, 16) ||
@@ -65,10 +67,10 @@ extern "C" lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, 
   Ctx c;
   TR_TRY(component_ctx(stream, &c));
   LnForward p{};
-  p.x = Mat{x, ldx, x_dtype};
+  p.x = mat(x, ldx, x_dtype);
   p.g = g;
   p.b = b;
-  p.y = MatOut{y, ldy, y_dtype};
+  p.y = mat_out(y, ldy, y_dtype);
   p.y8 = given(y8);
   p.x8 = given(x8);
   p.mean = mean;
@@ -76,7 +78,6 @@ extern "C" lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, 
   p.M = M;
   p.D = D;
   p.eps = eps;
-  p.vec = vec4(x, x_dtype, ldx) && vec4(y, y_dtype, ldy);
   return done(launch_ln_forward(c, p), "LayerNorm forward kernel");
 }
 
@@ -110,22 +111,20 @@ extern "C" lazymar_status lazymar_layernorm_backward(int dy_dtype, const void* d
   Ctx c;
   TR_TRY(component_ctx(stream, &c));
   LnBackward p{};
-  p.dy = Mat{dy, lddy, dy_dtype};
-  p.x = Mat{x, ldx, x_dtype};
+  p.dy = mat(dy, lddy, dy_dtype);
+  p.x = mat(x, ldx, x_dtype);
   p.x8 = given(x8);
   p.mean = mean;
   p.rstd = rstd;
   p.g = g;
-  p.dres = Mat{dres, lddres, LAZYMAR_F32};
-  p.dx = MatOut{dx, lddx, dx_dtype};
+  p.dres = mat(dres, lddres, LAZYMAR_F32);
+  p.dx = mat_out(dx, lddx, dx_dtype);
   p.dg = dg;
   p.db = db;
   p.accumulate = accumulate != 0;
   p.M = M;
   p.D = D;
   p.ws = static_cast<float*>(workspace);
-  p.vec = vec4(dy, dy_dtype, lddy) && vec4(x, x_dtype, ldx) && vec4(dres, LAZYMAR_F32, lddres) &&
-          vec4(dx, dx_dtype, lddx);
   return done(launch_ln_backward(c, p), "LayerNorm backward kernel");
 }
 
@@ -139,11 +138,10 @@ extern "C" lazymar_status lazymar_block8_pack(int dtype, const void* x, int ldx,
   Ctx c;
   TR_TRY(component_ctx(stream, &c));
   Rows8 p{};
-  p.in = Mat{x, ldx, dtype};
+  p.in = mat(x, ldx, dtype);
   p.out8 = *q;
   p.rows = rows;
   p.cols = cols;
-  p.vec = vec4(x, dtype, ldx);
   return done(launch_rows8(c, p), "8-bit pack kernel");
 }
 
@@ -156,7 +154,7 @@ extern "C" lazymar_status lazymar_block8_unpack(const lazymar_block8* q, int dty
   TR_TRY(check_mat(x, dtype, ldx, cols, "x: fp32 or bf16 device tensor, ldx >= cols required"));
   Ctx c;
   TR_TRY(component_ctx(stream, &c));
-  return done(launch_unpack8(c, *q, MatOut{x, ldx, dtype}, rows, cols), "8-bit unpack kernel");
+  return done(launch_unpack8(c, *q, mat_out(x, ldx, dtype), rows, cols), "8-bit unpack kernel");
 }
 
 extern "C" lazymar_status lazymar_block8_pack_weight(int dtype, const void* w, int ldw, const lazymar_block8* q,
@@ -173,7 +171,7 @@ extern "C" lazymar_status lazymar_block8_pack_weight(int dtype, const void* w, i
                         "qt: device tensors, 16-byte aligned, ldq % 16 == 0, ldq >= N, lds >= ceil(K / 128)"));
   Ctx c;
   TR_TRY(component_ctx(stream, &c));
-  return done(launch_pack_weight8(c, Mat{w, ldw, dtype}, given(q), given(qt), N, K), "8-bit weight pack kernel");
+  return done(launch_pack_weight8(c, mat(w, ldw, dtype), given(q), given(qt), N, K), "8-bit weight pack kernel");
 }
 
 extern "C" size_t lazymar_block8_gelu_backward_workspace(int rows, int cols) { return rows8_workspace(rows, cols); }
@@ -200,16 +198,15 @@ extern "C" lazymar_status lazymar_block8_gelu_backward(int dtype, const void* da
   Ctx c;
   TR_TRY(component_ctx(stream, &c));
   Rows8 p{};
-  p.in = Mat{da, ldda, dtype};
+  p.in = mat(da, ldda, dtype);
   p.u = given(u);
-  p.out = MatOut{du, lddu, du_dtype};
+  p.out = mat_out(du, lddu, du_dtype);
   p.out8 = given(du8);
   p.db = db;
   p.accumulate = accumulate != 0;
   p.rows = rows;
   p.cols = cols;
   p.ws = static_cast<float*>(workspace);
-  p.vec = vec4(da, dtype, ldda) && vec4(du, du_dtype, lddu);
   return done(launch_rows8(c, p), "GELU gradient kernel");
 }
 
@@ -246,8 +243,8 @@ extern "C" lazymar_status lazymar_block8_linear(int epilogue, const lazymar_bloc
   p.a = *a;
   p.w = *w;
   p.bias = bias;
-  p.residual = Mat{residual, ldr, LAZYMAR_F32};
-  p.out = MatOut{out, ldo, out_dtype};
+  p.residual = mat(residual, ldr, LAZYMAR_F32);
+  p.out = mat_out(out, ldo, out_dtype);
   p.out8 = given(out8);
   p.u8 = given(u8);
   p.M = M;
