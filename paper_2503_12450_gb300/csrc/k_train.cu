@@ -311,6 +311,8 @@ cudaError_t column_sums(const Ctx& c, const float* part, int P, int n, int n1, f
 // registers (a lane owns its columns), so that the column sums cost one pass
 // over 2 D floats a CTA instead of one over the data.
 
+constexpr int kRing = 4;  // most rows of a warp's ring
+
 // dg and db of the CTA's row groups added in turn, to its row of the workspace.
 template <int NC, int WPR>
 __device__ __forceinline__ void put_columns(const LnBackward& p, float* cols, const float (&dg)[NC][8],
@@ -337,113 +339,118 @@ __device__ __forceinline__ void put_columns(const LnBackward& p, float* cols, co
   for (int i = threadIdx.x; i < 2 * p.D; i += blockDim.x) o[i] = i < p.D ? cols[i] : cols[W + i - p.D];
 }
 
-// Widths that are a multiple of eight up to 1280 with rows on boundaries: a warp
-// a row. The rows of dy, x and dres come by bulk copies into the warp's ring in
-// shared memory, so that the next rows are on their way while this one is worked
-// on and nothing of them waits in registers; a row is read twice from there, for
-// the sums and for dx.
-template <int NC>
+// Widths that are a multiple of eight up to 1280 with rows on boundaries: WPR
+// warps a row, NB blocks of 128 columns a warp, four consecutive columns of a
+// block a lane. The rows of dy, x and dres come by bulk copies into the warp's
+// ring in shared memory, so that the next rows are on their way while this one
+// is worked on and nothing of them waits in registers.
+template <int NB, int WPR>
 __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackward p, int depth, uint32_t row_bytes,
                                                                   uint32_t x_at, uint32_t r_at, unsigned* err) {
-  extern __shared__ __align__(128) uint8_t ring_smem[];  // g [NC 256] fp32, then [warps][depth][row_bytes]
-  __shared__ uint64_t bars[8][4];
+  extern __shared__ __align__(128) uint8_t ring_smem[];  // [warps][depth][row_bytes]
+  __shared__ uint64_t bars[8][kRing];
+  __shared__ float red[2][8 / WPR][2][WPR];
   __shared__ int abort_word;
   volatile int* abort_flag = &abort_word;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5, D = p.D;
-  float* gs = reinterpret_cast<float*>(ring_smem);
-  uint8_t* ring = ring_smem + NC * kChunk * 4 + (size_t)warp * depth * row_bytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
+  const int groups = (int)(blockDim.x >> 5) / WPR, D = p.D, c0 = part * NB * kBlk;
+  const int mine = min(NB * kBlk, D - c0);  // columns of this warp
+  uint8_t* ring = ring_smem + (size_t)warp * depth * row_bytes;
   if (threadIdx.x == 0) abort_word = 0;
   if (lane == 0)
     for (int s = 0; s < depth; ++s) mbar_init(&bars[warp][s], 1);
   fence_mbar_init();
   pdl_wait();
   pdl_trigger();
-  for (int i = threadIdx.x; i < NC * kChunk; i += blockDim.x) gs[i] = i < D ? (p.g ? p.g[i] : 1.f) : 0.f;
   __syncthreads();
-  const int step = (int)gridDim.x * warps, first = (int)blockIdx.x * warps + warp;
+  const int step = (int)gridDim.x * groups, first = (int)blockIdx.x * groups + grp;
   const size_t dy_e = p.dy.dtype == LAZYMAR_F32 ? 4 : 2, x_e = p.x.dtype == LAZYMAR_F32 ? 4 : 2;
-  const uint32_t dy_b = (uint32_t)(D * dy_e), x_b = p.x.p ? (uint32_t)(D * x_e) : (uint32_t)((D + 15) & ~15);
-  const uint32_t r_b = p.dres.p ? (uint32_t)D * 4 : 0u;
-  auto fetch = [&](int row, int s) {
+  const uint32_t dy_b = (uint32_t)(mine * dy_e);
+  const uint32_t x_b = p.x.p ? (uint32_t)(mine * x_e) : (uint32_t)((mine + 15) & ~15);
+  const uint32_t r_b = p.dres.p ? (uint32_t)mine * 4 : 0u;
+  auto fetch = [&](long long row, int s) {
     uint8_t* dst = ring + (size_t)s * row_bytes;
     uint64_t* bar = &bars[warp][s];
     mbar_arrive_expect_tx(bar, dy_b + x_b + r_b);
-    bulk_load(dst, static_cast<const uint8_t*>(p.dy.p) + (size_t)row * p.dy.ld * dy_e, dy_b, bar);
+    bulk_load(dst, static_cast<const uint8_t*>(p.dy.p) + ((size_t)row * p.dy.ld + c0) * dy_e, dy_b, bar);
     bulk_load(dst + x_at,
-              p.x.p ? static_cast<const uint8_t*>(p.x.p) + (size_t)row * p.x.ld * x_e
-                    : static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq,
+              p.x.p ? static_cast<const uint8_t*>(p.x.p) + ((size_t)row * p.x.ld + c0) * x_e
+                    : static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq + c0,
               x_b, bar);
-    if (r_b) bulk_load(dst + r_at, static_cast<const float*>(p.dres.p) + (size_t)row * p.dres.ld, r_b, bar);
+    if (r_b) bulk_load(dst + r_at, static_cast<const float*>(p.dres.p) + (size_t)row * p.dres.ld + c0, r_b, bar);
   };
   if (lane == 0)
     for (int s = 0; s < depth; ++s)
-      if ((long long)first + (long long)s * step < p.M) fetch(first + s * step, s);
-  // scales (lane: block), mean and rstd of the next row
+      if (first + (long long)s * step < p.M) fetch(first + (long long)s * step, s);
+  // mean, rstd and the scales (lane: block) of the next row
   float mean = 0.f, rstd = 0.f;
   uint32_t sb = 0;
   auto statistics = [&](long long row) {
     if (row >= p.M) return;
     mean = p.mean[row];
     rstd = p.rstd[row];
-    if (!p.x.p && lane * kBlk < D && lane < 2 * NC) sb = p.x8.scale[(size_t)lane * p.x8.lds + row];
+    if (!p.x.p && lane < NB && lane * kBlk < mine) sb = p.x8.scale[(size_t)(part * NB + lane) * p.x8.lds + row];
   };
   statistics(first);
-
-  float dg[NC][8], db[NC][8];
+  float g[NB][4], dg[NB][4], db[NB][4];
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int j = 0; j < NB; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.f;
-  int slot = 0;
+    for (int i = 0; i < 4; ++i) {
+      const int c = j * kBlk + 4 * lane + i;
+      g[j][i] = c < mine ? (p.g ? p.g[c0 + c] : 1.f) : 0.f;
+      dg[j][i] = db[j][i] = 0.f;
+    }
+  int slot = 0, it = 0;
   uint32_t phase = 0;
-  for (long long row = first; row < p.M; row += step) {
+  bool dead = false;  // a wait ran out: the rows are not written any more
+  for (long long row = first; row < p.M; row += step, it ^= 1) {
     const float mu = mean, rs = rstd;
     const uint32_t scales = sb;
     statistics(row + step);
     const bool ok = mbar_wait(&bars[warp][slot], phase, abort_flag, err);
-    if (!__all_sync(0xffffffffu, ok)) break;
+    dead |= !__all_sync(0xffffffffu, ok);
     const uint8_t* src = ring + (size_t)slot * row_bytes;
-    auto take = [&](int c, float (&y)[8], float (&h)[8]) {
-      const int at = c * kChunk + 8 * lane;
+    float y[NB][4], h[NB][4], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int c = j * kBlk + 4 * lane;
       if (p.dy.dtype == LAZYMAR_F32) {
-        const float4* f = reinterpret_cast<const float4*>(src + 4 * at);
-        const float4 a = f[0], b = f[1];
-        y[0] = a.x; y[1] = a.y; y[2] = a.z; y[3] = a.w; y[4] = b.x; y[5] = b.y; y[6] = b.z; y[7] = b.w;
+        const float4 a = *reinterpret_cast<const float4*>(src + 4 * c);
+        y[j][0] = a.x; y[j][1] = a.y; y[j][2] = a.z; y[j][3] = a.w;
       } else {
-        bf16x8(*reinterpret_cast<const uint4*>(src + 2 * at), y);
+        const uint2 a = *reinterpret_cast<const uint2*>(src + 2 * c);
+        y[j][0] = __uint_as_float(a.x << 16); y[j][1] = __uint_as_float(a.x & 0xFFFF0000u);
+        y[j][2] = __uint_as_float(a.y << 16); y[j][3] = __uint_as_float(a.y & 0xFFFF0000u);
       }
       if (!p.x.p) {
-        const uint32_t byte = __shfl_sync(0xffffffffu, scales, 2 * c + (lane >> 4));
-        block8_values(*reinterpret_cast<const uint2*>(src + x_at + at), block8_scale(byte), h);
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(src + x_at + c);
+        const float s = block8_scale(__shfl_sync(0xffffffffu, scales, j));
+        const float2 a = e4m3x2_to_f2(w & 0xFFFFu), b = e4m3x2_to_f2(w >> 16);
+        h[j][0] = a.x * s; h[j][1] = a.y * s; h[j][2] = b.x * s; h[j][3] = b.y * s;
       } else if (p.x.dtype == LAZYMAR_F32) {
-        const float4* f = reinterpret_cast<const float4*>(src + x_at + 4 * at);
-        const float4 a = f[0], b = f[1];
-        h[0] = a.x; h[1] = a.y; h[2] = a.z; h[3] = a.w; h[4] = b.x; h[5] = b.y; h[6] = b.z; h[7] = b.w;
+        const float4 a = *reinterpret_cast<const float4*>(src + x_at + 4 * c);
+        h[j][0] = a.x; h[j][1] = a.y; h[j][2] = a.z; h[j][3] = a.w;
       } else {
-        bf16x8(*reinterpret_cast<const uint4*>(src + x_at + 2 * at), h);
+        const uint2 a = *reinterpret_cast<const uint2*>(src + x_at + 2 * c);
+        h[j][0] = __uint_as_float(a.x << 16); h[j][1] = __uint_as_float(a.x & 0xFFFF0000u);
+        h[j][2] = __uint_as_float(a.y << 16); h[j][3] = __uint_as_float(a.y & 0xFFFF0000u);
       }
-      if (at >= D) {  // what a shorter row leaves of the ring's last columns
+      if (c >= mine) {  // what a shorter row leaves of the ring's last columns
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = h[i] = 0.f;
+        for (int i = 0; i < 4; ++i) {
+          y[j][i] = 0.f;
+          h[j][i] = mu;
+        }
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = (h[i] - mu) * rs;
-    };
-    float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      float y[8], h[8];
-      take(c, y, h);
-      const float4* gp = reinterpret_cast<const float4*>(gs + c * kChunk + 8 * lane);
-      const float4 g0 = gp[0], g1 = gp[1];
-      const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float a = y[i] * g[i];
-        dg[c][i] = fmaf(y[i], h[i], dg[c][i]);
-        db[c][i] += y[i];
-        s1 += a;
-        s2 = fmaf(a, h[i], s2);
+      for (int i = 0; i < 4; ++i) {
+        h[j][i] = (h[j][i] - mu) * rs;
+        dg[j][i] = fmaf(y[j][i], h[j][i], dg[j][i]);
+        db[j][i] += y[j][i];
+        y[j][i] *= g[j][i];
+        s1 += y[j][i];
+        s2 = fmaf(y[j][i], h[j][i], s2);
       }
     }
 #pragma unroll
@@ -451,40 +458,66 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
       s1 += __shfl_xor_sync(0xffffffffu, s1, o);
       s2 += __shfl_xor_sync(0xffffffffu, s2, o);
     }
+    if constexpr (WPR > 1) {
+      if (lane == 0) {
+        red[it][grp][0][part] = s1;
+        red[it][grp][1][part] = s2;
+      }
+      asm volatile("bar.sync %0, %1;" ::"r"(grp + 1), "n"(WPR * 32) : "memory");  // the row's warps
+      s1 = s2 = 0.f;
+#pragma unroll
+      for (int i = 0; i < WPR; ++i) {
+        s1 += red[it][grp][0][i];
+        s2 += red[it][grp][1][i];
+      }
+    }
     s1 /= (float)D;
     s2 /= (float)D;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int at = c * kChunk + 8 * lane;
-      float y[8], h[8];
-      take(c, y, h);
-      if (at < D) {
-        const float4* gp = reinterpret_cast<const float4*>(gs + at);
-        const float4 g0 = gp[0], g1 = gp[1];
-        const float g[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w};
+    for (int j = 0; j < NB; ++j) {
+      const int c = j * kBlk + 4 * lane;
+      if (c >= mine) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = rs * (fmaf(y[i], g[i], -s1) - h[i] * s2);
-        if (r_b) {
-          const float4* rp = reinterpret_cast<const float4*>(src + r_at + 4 * at);
-          const float4 r0 = rp[0], r1 = rp[1];
-          const float r[8] = {r0.x, r0.y, r0.z, r0.w, r1.x, r1.y, r1.z, r1.w};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] += r[i];
-        }
-        if (p.dx.dtype == LAZYMAR_F32) st8a(static_cast<float*>(p.dx.p) + (size_t)row * p.dx.ld + at, y);
-        else st8a(static_cast<bf16*>(p.dx.p) + (size_t)row * p.dx.ld + at, y);
+      for (int i = 0; i < 4; ++i) y[j][i] = rs * (y[j][i] - s1 - h[j][i] * s2);
+      if (r_b) {
+        const float4 r = *reinterpret_cast<const float4*>(src + r_at + 4 * c);
+        y[j][0] += r.x; y[j][1] += r.y; y[j][2] += r.z; y[j][3] += r.w;
       }
+      if (dead) continue;
+      if (p.dx.dtype == LAZYMAR_F32)
+        *reinterpret_cast<float4*>(static_cast<float*>(p.dx.p) + (size_t)row * p.dx.ld + c0 + c) =
+            make_float4(y[j][0], y[j][1], y[j][2], y[j][3]);
+      else
+        *reinterpret_cast<uint2*>(static_cast<bf16*>(p.dx.p) + (size_t)row * p.dx.ld + c0 + c) =
+            make_uint2(pack_bf16(y[j][0], y[j][1]), pack_bf16(y[j][2], y[j][3]));
     }
     __syncwarp();  // every lane has read the row
-    if (lane == 0 && row + (long long)depth * step < p.M) {
+    if (lane == 0 && !dead && row + (long long)depth * step < p.M) {
       fence_proxy_async_smem();
-      fetch((int)(row + (long long)depth * step), slot);
+      fetch(row + (long long)depth * step, slot);
     }
     if (++slot == depth) { slot = 0; phase ^= 1u; }
   }
   if (!p.dg) return;
-  __syncthreads();  // the ring is free: the column sums take its place
-  put_columns<NC, 1>(p, gs, dg, db);
+  // the groups' sums in turn, where the ring was, to the CTA's row of the workspace
+  constexpr int W = NB * WPR * kBlk;
+  float* cols = reinterpret_cast<float*>(ring_smem);
+  for (int k = 0; k < groups; ++k) {
+    __syncthreads();
+    if (k == grp) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        float4* s = reinterpret_cast<float4*>(cols + c0 + j * kBlk + 4 * lane);
+        float4* t = reinterpret_cast<float4*>(cols + W + c0 + j * kBlk + 4 * lane);
+        const float4 u = k ? *s : make_float4(0.f, 0.f, 0.f, 0.f), w = k ? *t : make_float4(0.f, 0.f, 0.f, 0.f);
+        *s = make_float4(u.x + dg[j][0], u.y + dg[j][1], u.z + dg[j][2], u.w + dg[j][3]);
+        *t = make_float4(w.x + db[j][0], w.y + db[j][1], w.z + db[j][2], w.w + db[j][3]);
+      }
+    }
+  }
+  __syncthreads();
+  float* o = p.ws + (size_t)blockIdx.x * 2 * D;
+  for (int i = threadIdx.x; i < 2 * D; i += blockDim.x) o[i] = i < D ? cols[i] : cols[W + i - D];
 }
 
 // Any width, stride and alignment: WPR warps a row, NC chunks of 256 columns a
@@ -595,33 +628,30 @@ cudaError_t big_smem(const void* kernel, size_t smem) {
                           : cudaSuccess;
 }
 
-// Rows in shared memory: as many a warp, up to four, as let two CTAs of eight
-// warps live on an SM, or one CTA, or one of four warps.
-template <int NC>
+// Rows in shared memory: as many a warp as let two CTAs of eight warps live on
+// an SM with two rows a warp at least, otherwise one CTA.
+template <int NB, int WPR>
 cudaError_t ln_backward_ring_run(const Ctx& c, const LnBackward& p, int* ctas) {
-  const uint32_t dy_b = (uint32_t)NC * kChunk * (p.dy.dtype == LAZYMAR_F32 ? 4 : 2);
-  const uint32_t x_b = (uint32_t)NC * kChunk * (p.x.p ? (p.x.dtype == LAZYMAR_F32 ? 4 : 2) : 1);
-  const uint32_t r_b = p.dres.p ? (uint32_t)NC * kChunk * 4 : 0u, row_b = dy_b + x_b + r_b;
-  const size_t fixed = (size_t)NC * kChunk * 4, sums = (size_t)2 * NC * kChunk * 4;
-  int warps = 8, per_sm = 2;
-  long long depth = ((long long)110 * 1024 - (long long)fixed) / ((long long)warps * row_b);
+  constexpr uint32_t W = NB * kBlk;
+  const uint32_t dy_b = W * (p.dy.dtype == LAZYMAR_F32 ? 4 : 2);
+  const uint32_t x_b = W * (p.x.p ? (p.x.dtype == LAZYMAR_F32 ? 4 : 2) : 1);
+  const uint32_t r_b = p.dres.p ? W * 4 : 0u, row_b = dy_b + x_b + r_b;
+  int warps = 8, per_sm = 2, depth = (int)(110 * 1024 / (warps * row_b));
   if (depth < 2) {
     per_sm = 1;
-    depth = ((long long)220 * 1024 - (long long)fixed) / ((long long)warps * row_b);
+    depth = (int)(220 * 1024 / (warps * row_b));
   }
-  if (depth < 2) {
-    warps = 4;
-    depth = ((long long)220 * 1024 - (long long)fixed) / ((long long)warps * row_b);
-  }
-  if (depth > 4) depth = 4;
-  size_t smem = fixed + (size_t)warps * depth * row_b;
+  if (depth > kRing) depth = kRing;
+  size_t smem = (size_t)warps * depth * row_b;
+  const size_t sums = (size_t)2 * W * WPR * 4;
   if (smem < sums) smem = sums;
-  const int need = (p.M + warps - 1) / warps, most = per_sm * kSMs;
+  const int groups = warps / WPR, need = (p.M + groups - 1) / groups, most = per_sm * kSMs;
   *ctas = need < most ? need : most;
-  cudaError_t e = big_smem(reinterpret_cast<const void*>(ln_backward_ring_kernel<NC>), smem);
+  const auto kernel = ln_backward_ring_kernel<NB, WPR>;
+  cudaError_t e = big_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
-  return launch_pdl(ln_backward_ring_kernel<NC>, dim3((unsigned)*ctas), dim3((unsigned)warps * 32), smem, c.stream, p,
-                    (int)depth, row_b, dy_b, dy_b + x_b, c.err);
+  return launch_pdl(kernel, dim3((unsigned)*ctas), dim3((unsigned)warps * 32), smem, c.stream, p, depth, row_b, dy_b,
+                    dy_b + x_b, c.err);
 }
 
 template <int NC, int WPR>
@@ -664,18 +694,20 @@ __device__ __forceinline__ float gelu_grad_at(const float* tab, float x) {
 
 // in [rows, cols] through an optional GELU' of the checkpoint u, to `out`
 // and / or block8, with optional column sums. A warp owns 256 columns and a
-// stride of rows, kRowsU at a time, so that the column sums stay in its
-// registers; neighbouring warps take neighbouring columns of the same rows.
-constexpr int kRowsU = 4;
-
-template <typename T, bool HAS_U>
-__global__ void __launch_bounds__(256, 3) rows8_kernel(const Rows8 p, int nchunk, int groups) {
+// stride of rows, U at a time (bytes in flight), so that the column sums stay in its registers;
+// neighbouring warps take neighbouring columns of the same rows.
+// VEC: rows on boundaries and cols a multiple of eight, so that a lane's columns
+// all exist or none does; otherwise a row at a time, through shared memory
+// where it is off the boundary.
+template <typename T, bool HAS_U, bool VEC>
+__global__ void __launch_bounds__(256, 4) rows8_kernel(const Rows8 p, int nchunk, int groups) {
+  constexpr int U = !VEC ? 1 : HAS_U || sizeof(T) == 4 ? 2 : 4;  // rows in flight, as registers allow
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int task = (int)blockIdx.x * 8 + warp;
   const int grp = task / nchunk, c0 = (task - grp * nchunk) * kChunk, col = c0 + 8 * lane, cols = p.cols;
   __shared__ float grad[HAS_U ? kGradSize : 1];
-  __shared__ float stage[8][kChunk];
-  float* sm = stage[warp];
+  __shared__ float stage[VEC ? 1 : 8][kChunk];
+  float* sm = stage[VEC ? 0 : warp];
   if (HAS_U) {
     gelu_grad_table(grad);
     __syncthreads();
@@ -686,44 +718,43 @@ __global__ void __launch_bounds__(256, 3) rows8_kernel(const Rows8 p, int nchunk
   float acc[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+  const bool on = col < cols;
+  const int at = on ? col : 0;
   const T* in = static_cast<const T*>(p.in.p);
-  const bool whole = p.in.vec && col + 8 <= cols;
-  const uint8_t* us = HAS_U ? p.u.scale + (size_t)(min(col, cols - 1) / kBlk) * p.u.lds : nullptr;
-  for (long long r0 = (long long)grp * kRowsU; r0 < p.rows; r0 += (long long)groups * kRowsU) {
+  const uint8_t* us = HAS_U ? p.u.scale + (size_t)(at / kBlk) * p.u.lds : nullptr;
+  for (int r0 = grp * U; r0 < p.rows; r0 += groups * U) {
     constexpr int W = sizeof(T) / 2;
-    uint4 raw[kRowsU][W];
-    uint2 uq[kRowsU];
-    uint32_t ub[kRowsU];
+    uint4 raw[U][W];
+    uint2 uq[U];
+    uint32_t ub[U];
 #pragma unroll
-    for (int j = 0; j < kRowsU; ++j) {
-      const size_t r = (size_t)min(r0 + j, (long long)p.rows - 1);
-      if (whole) {
-        const uint4* src = reinterpret_cast<const uint4*>(in + r * p.in.ld + col);
+    for (int j = 0; j < U; ++j) {
+      const size_t r = (size_t)min(r0 + j, p.rows - 1);
+      if (VEC) {
+        const uint4* src = reinterpret_cast<const uint4*>(in + r * p.in.ld + at);
 #pragma unroll
         for (int k = 0; k < W; ++k) raw[j][k] = src[k];
       }
       if (HAS_U) {
-        uq[j] = ldq8(static_cast<const uint8_t*>(p.u.q) + r * p.u.ldq, col, cols);
+        const uint8_t* q = static_cast<const uint8_t*>(p.u.q) + r * p.u.ldq;
+        uq[j] = VEC ? *reinterpret_cast<const uint2*>(q + at) : ldq8(q, col, cols);
         ub[j] = us[r];
       }
     }
 #pragma unroll
-    for (int j = 0; j < kRowsU; ++j) {
+    for (int j = 0; j < U; ++j) {
       if (r0 + j >= p.rows) break;
       const size_t r = (size_t)(r0 + j);
       float v[8];
-      if (whole) {
-        if constexpr (W == 1) {
-          bf16x8(raw[j][0], v);
-        } else {
-          const uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w,
-                                 raw[j][1].x, raw[j][1].y, raw[j][1].z, raw[j][1].w};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-        }
-      }
-      if (!p.in.vec || c0 + kChunk > cols) {  // (uniform over the warp; whole lanes read again)
+      if constexpr (!VEC) {
         ld8<T>(in + r * p.in.ld, c0, cols, p.in.vec, sm, v);
+      } else if constexpr (W == 1) {
+        bf16x8(raw[j][0], v);
+      } else {
+        const uint32_t w[8] = {raw[j][0].x, raw[j][0].y, raw[j][0].z, raw[j][0].w,
+                               raw[j][W - 1].x, raw[j][W - 1].y, raw[j][W - 1].z, raw[j][W - 1].w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
       }
       if (HAS_U) {
         float u[8];
@@ -731,12 +762,31 @@ __global__ void __launch_bounds__(256, 3) rows8_kernel(const Rows8 p, int nchunk
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= gelu_grad_at(grad, u[i]);
       }
+      if (VEC && !on) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+      }
       if (p.db) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc[i] += v[i];
       }
-      if (p.out.p) st_mat<false>(p.out, r, c0, cols, sm, v);
-      if (p.out8.q) put8<false>(p.out8, r, c0, cols, v);
+      if (VEC) {
+        if (p.out.p && on) {
+          if (p.out.dtype == LAZYMAR_F32) st8a(static_cast<float*>(p.out.p) + r * p.out.ld + col, v);
+          else st8a(static_cast<bf16*>(p.out.p) + r * p.out.ld + col, v);
+        }
+        if (p.out8.q) {
+          uint2 w;
+          const uint32_t byte = block8_quantize(v, w);
+          if (on) {
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.out8.q) + r * p.out8.ldq + col) = w;
+            if ((lane & 15) == 0) p.out8.scale[(size_t)(col / kBlk) * p.out8.lds + r] = (uint8_t)byte;
+          }
+        }
+      } else {
+        if (p.out.p) st_mat<false>(p.out, r, c0, cols, sm, v);
+        if (p.out8.q) put8<false>(p.out8, r, c0, cols, v);
+      }
     }
   }
   if (p.db) {
@@ -747,9 +797,9 @@ __global__ void __launch_bounds__(256, 3) rows8_kernel(const Rows8 p, int nchunk
   }
 }
 
-// Row groups of a launch: the 24 warps that fit on every SM, once.
+// Row groups of a launch: the 32 warps that fit on every SM, once.
 int rows8_groups(int rows, int nchunk) {
-  const int want = kSMs * 24 / nchunk, most = (rows + kRowsU - 1) / kRowsU;
+  const int want = kSMs * 32 / nchunk, most = (rows + 1) / 2;
   return want < 1 ? 1 : want < most ? want : most;
 }
 
@@ -902,11 +952,13 @@ cudaError_t launch_ln_backward(const Ctx& c, const LnBackward& p) {
   int ctas = 0;
   cudaError_t e;
   if (nc <= 5 && p.D % 8 == 0 && p.dy.vec && p.x.vec && p.dres.vec && p.dx.vec) {
-    e = nc <= 1   ? ln_backward_ring_run<1>(c, p, &ctas)
-        : nc <= 2 ? ln_backward_ring_run<2>(c, p, &ctas)
-        : nc <= 3 ? ln_backward_ring_run<3>(c, p, &ctas)
-        : nc <= 4 ? ln_backward_ring_run<4>(c, p, &ctas)
-                  : ln_backward_ring_run<5>(c, p, &ctas);
+    const int nb = (p.D + kBlk - 1) / kBlk;
+    e = nb <= 1   ? ln_backward_ring_run<1, 1>(c, p, &ctas)
+        : nb <= 2 ? ln_backward_ring_run<2, 1>(c, p, &ctas)
+        : nb <= 4 ? ln_backward_ring_run<2, 2>(c, p, &ctas)
+        : nb <= 6 ? ln_backward_ring_run<3, 2>(c, p, &ctas)
+        : nb <= 8 ? ln_backward_ring_run<4, 2>(c, p, &ctas)
+                  : ln_backward_ring_run<5, 2>(c, p, &ctas);
   } else {
     e = nc <= 1    ? ln_backward_run<1, 1>(c, p, &ctas)
         : nc <= 2  ? ln_backward_run<2, 1>(c, p, &ctas)
@@ -932,13 +984,13 @@ cudaError_t launch_rows8(const Ctx& c, const Rows8& p) {
   }
   const int nchunk = (p.cols + kChunk - 1) / kChunk, groups = rows8_groups(p.rows, nchunk);
   const dim3 grid((unsigned)(((long long)nchunk * groups + 7) / 8)), block(256);
-  cudaError_t e;
-  if (p.in.dtype == LAZYMAR_F32)
-    e = p.u.q ? launch_pdl(rows8_kernel<float, true>, grid, block, 0, c.stream, p, nchunk, groups)
-              : launch_pdl(rows8_kernel<float, false>, grid, block, 0, c.stream, p, nchunk, groups);
-  else
-    e = p.u.q ? launch_pdl(rows8_kernel<bf16, true>, grid, block, 0, c.stream, p, nchunk, groups)
-              : launch_pdl(rows8_kernel<bf16, false>, grid, block, 0, c.stream, p, nchunk, groups);
+  const bool vec = p.in.vec && p.out.vec && p.cols % 8 == 0;
+#define LM_ROWS8(T, HAS_U)                                                                                \
+  (vec ? launch_pdl(rows8_kernel<T, HAS_U, true>, grid, block, 0, c.stream, p, nchunk, groups)             \
+       : launch_pdl(rows8_kernel<T, HAS_U, false>, grid, block, 0, c.stream, p, nchunk, groups))
+  const cudaError_t e = p.in.dtype == LAZYMAR_F32 ? (p.u.q ? LM_ROWS8(float, true) : LM_ROWS8(float, false))
+                                                  : (p.u.q ? LM_ROWS8(bf16, true) : LM_ROWS8(bf16, false));
+#undef LM_ROWS8
   if (e != cudaSuccess || !p.db) return e;
   return column_sums(c, p.ws, groups, p.cols, p.cols, p.db, nullptr, p.accumulate);
 }

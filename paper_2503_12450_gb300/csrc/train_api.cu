@@ -139,6 +139,7 @@ extern "C" lazymar_status lazymar_block8_pack(int dtype, const void* x, int ldx,
   TR_TRY(component_ctx(stream, &c));
   Rows8 p{};
   p.in = mat(x, ldx, dtype);
+  p.out = mat_out(nullptr, 0, dtype);
   p.out8 = *q;
   p.rows = rows;
   p.cols = cols;
