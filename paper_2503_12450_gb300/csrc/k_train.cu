@@ -270,12 +270,16 @@ cudaError_t ln_forward_run(const Ctx& c, const LnForward& p) {
 // Column sums of per-CTA partial rows
 // ---------------------------------------------------------------------------
 // out[c] (+)= sum over the P rows of part [P, n], in row order within each of
-// eight slices and slice order after that: the same result for the same sizes.
-// Columns from n1 on belong to out2.
-__global__ void __launch_bounds__(256) column_sums_kernel(const float* __restrict__ part, int P, int n, int n1,
+// kSlices slices and slice order after that: the same result for the same sizes.
+// Columns from n1 on belong to out2. Short chains of loads, because a launch
+// over the few hundred partial rows is all latency (304 rows of 1554: 8 slices
+// 9.3 us cold).
+constexpr int kSlices = 32;
+
+__global__ void __launch_bounds__(32 * kSlices) column_sums_kernel(const float* __restrict__ part, int P, int n, int n1,
                                                           float* __restrict__ out, float* __restrict__ out2,
                                                           bool accumulate) {
-  __shared__ float red[8][32];
+  __shared__ float red[kSlices][32];
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   pdl_wait();
   pdl_trigger();
@@ -283,13 +287,13 @@ __global__ void __launch_bounds__(256) column_sums_kernel(const float* __restric
   if (col < n) {
     const float* p = part + col;
 #pragma unroll 8
-    for (int r = slice; r < P; r += 8) s += p[(size_t)r * n];
+    for (int r = slice; r < P; r += kSlices) s += p[(size_t)r * n];
   }
   red[slice][lane] = s;
   __syncthreads();
   if (slice == 0 && col < n) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += red[i][lane];
+    for (int i = 1; i < kSlices; ++i) s += red[i][lane];
     float* o = col < n1 ? out + col : out2 + (col - n1);
     if (accumulate) s += *o;
     *o = s;
@@ -298,7 +302,7 @@ __global__ void __launch_bounds__(256) column_sums_kernel(const float* __restric
 
 cudaError_t column_sums(const Ctx& c, const float* part, int P, int n, int n1, float* out, float* out2,
                         bool accumulate) {
-  return launch_pdl(column_sums_kernel, dim3((unsigned)((n + 31) / 32)), dim3(256), 0, c.stream, part, P, n, n1, out,
+  return launch_pdl(column_sums_kernel, dim3((unsigned)((n + 31) / 32)), dim3(32 * kSlices), 0, c.stream, part, P, n, n1, out,
                     out2, accumulate);
 }
 
@@ -313,33 +317,7 @@ cudaError_t column_sums(const Ctx& c, const float* part, int P, int n, int n1, f
 
 constexpr int kRing = 4;  // most rows of a warp's ring
 
-// dg and db of the CTA's row groups added in turn, to its row of the workspace.
-template <int NC, int WPR>
-__device__ __forceinline__ void put_columns(const LnBackward& p, float* cols, const float (&dg)[NC][8],
-                                            const float (&db)[NC][8]) {
-  constexpr int W = NC * WPR * kChunk;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
-  const int groups = (int)(blockDim.x >> 5) / WPR;
-  for (int g = 0; g < groups; ++g) {
-    __syncthreads();
-    if (g == grp) {
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        float* s = cols + (part * NC + c) * kChunk + 8 * lane;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          s[i] = g == 0 ? dg[c][i] : s[i] + dg[c][i];
-          s[W + i] = g == 0 ? db[c][i] : s[W + i] + db[c][i];
-        }
-      }
-    }
-  }
-  __syncthreads();
-  float* o = p.ws + (size_t)blockIdx.x * 2 * p.D;
-  for (int i = threadIdx.x; i < 2 * p.D; i += blockDim.x) o[i] = i < p.D ? cols[i] : cols[W + i - p.D];
-}
-
-// Widths that are a multiple of eight up to 1280 with rows on boundaries: WPR
+// Widths that are a multiple of eight up to 4096 with rows on boundaries: WPR
 // warps a row, NB blocks of 128 columns a warp, four consecutive columns of a
 // block a lane. The rows of dy, x and dres come by bulk copies into the warp's
 // ring in shared memory, so that the next rows are on their way while this one
@@ -354,7 +332,7 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
   volatile int* abort_flag = &abort_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
   const int groups = (int)(blockDim.x >> 5) / WPR, D = p.D, c0 = part * NB * kBlk;
-  const int mine = min(NB * kBlk, D - c0);  // columns of this warp
+  const int mine = max(0, min(NB * kBlk, D - c0));  // columns of this warp; the last ones of eight may have none
   uint8_t* ring = ring_smem + (size_t)warp * depth * row_bytes;
   if (threadIdx.x == 0) abort_word = 0;
   if (lane == 0)
@@ -379,7 +357,7 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
               x_b, bar);
     if (r_b) bulk_load(dst + r_at, static_cast<const float*>(p.dres.p) + (size_t)row * p.dres.ld + c0, r_b, bar);
   };
-  if (lane == 0)
+  if (lane == 0 && mine > 0)
     for (int s = 0; s < depth; ++s)
       if (first + (long long)s * step < p.M) fetch(first + (long long)s * step, s);
   // mean, rstd and the scales (lane: block) of the next row
@@ -408,7 +386,7 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
     const float mu = mean, rs = rstd;
     const uint32_t scales = sb;
     statistics(row + step);
-    const bool ok = mbar_wait(&bars[warp][slot], phase, abort_flag, err);
+    const bool ok = mine == 0 || mbar_wait(&bars[warp][slot], phase, abort_flag, err);
     dead |= !__all_sync(0xffffffffu, ok);
     const uint8_t* src = ring + (size_t)slot * row_bytes;
     float y[NB][4], h[NB][4], s1 = 0.f, s2 = 0.f;
@@ -492,7 +470,7 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
             make_uint2(pack_bf16(y[j][0], y[j][1]), pack_bf16(y[j][2], y[j][3]));
     }
     __syncwarp();  // every lane has read the row
-    if (lane == 0 && !dead && row + (long long)depth * step < p.M) {
+    if (lane == 0 && mine > 0 && !dead && row + (long long)depth * step < p.M) {
       fence_proxy_async_smem();
       fetch(row + (long long)depth * step, slot);
     }
@@ -521,15 +499,26 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
 }
 
 // Any width, stride and alignment: WPR warps a row, NC chunks of 256 columns a
-// warp, dy and x in registers.
+// warp, every 32nd column of a chunk a lane (so that a warp's accesses are
+// contiguous without a boundary), dy and x in registers.
+template <typename T>
+__device__ __forceinline__ void ld8s(const T* row, int c0, int D, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int c = c0 + 32 * i + (int)(threadIdx.x & 31);
+    v[i] = c < D ? to_f(row[c]) : 0.f;
+  }
+}
+__device__ __forceinline__ void ld8s(const Mat& m, size_t row, int c0, int D, float (&v)[8]) {
+  if (m.dtype == LAZYMAR_F32) ld8s(static_cast<const float*>(m.p) + row * m.ld, c0, D, v);
+  else ld8s(static_cast<const bf16*>(m.p) + row * m.ld, c0, D, v);
+}
 template <int NC, int WPR>
-__global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256) ln_backward_kernel(const LnBackward p) {
-  constexpr int WARPS = WPR > 8 ? WPR : 8, GROUPS = WARPS / WPR;
-  extern __shared__ float cols[];  // [2][NC WPR 256]
+__global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_backward_kernel(const LnBackward p) {
+  constexpr int WARPS = WPR > 8 ? WPR : 8, GROUPS = WARPS / WPR, W = NC * WPR * kChunk;
+  extern __shared__ float cols[];  // [2][W]
   __shared__ float red[2][2][GROUPS][WPR];
-  __shared__ float stage[WARPS][kChunk];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
-  float* sm = stage[warp];
   const int D = p.D, c0 = part * NC * kChunk;
   pdl_wait();
   pdl_trigger();
@@ -550,33 +539,34 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256) ln_backward_kernel(c
       rstd = p.rstd[row];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const int cc = c0 + c * kChunk, col = cc + 8 * lane;
-        ld_mat<false>(p.dy, row, cc, D, sm, a[c]);
-        if (!p.x.p) {
-          const uint2 w = ldq8(static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq, col, D);
-          const uint32_t byte = col < D ? p.x8.scale[(size_t)(col / kBlk) * p.x8.lds + row] : 127u;
-          block8_values(w, block8_scale(byte), h[c]);
+        const int cc = c0 + c * kChunk;
+        ld8s(p.dy, row, cc, D, a[c]);
+        if (p.x.p) {
+          ld8s(p.x, row, cc, D, h[c]);
         } else {
-          ld_mat<false>(p.x, row, cc, D, sm, h[c]);
+          const uint8_t* q = static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq;
+          const int blk = min(cc, D - 1) / kBlk, more = cc + kBlk < D ? 1 : 0;  // the chunk's blocks
+          const float sc[2] = {block8_scale(p.x8.scale[(size_t)blk * p.x8.lds + row]),
+                               block8_scale(p.x8.scale[(size_t)(blk + more) * p.x8.lds + row])};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int k = cc + 32 * i + lane;
+            h[c][i] = e4m3x2_to_f2(k < D ? q[k] : 0u).x * sc[i >> 2];
+          }
         }
       }
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const int col = c0 + c * kChunk + 8 * lane;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[c][i] = (h[c][i] - mean) * rstd;
-        mask8<false>(h[c], col, D);
-        float g[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = 1.f;
-        if (p.g) ld_param<false>(p.g, col, D, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          dg[c][i] = fmaf(a[c][i], h[c][i], dg[c][i]);
+          const int k = c0 + c * kChunk + 32 * i + lane;
+          const float x = k < D ? (h[c][i] - mean) * rstd : 0.f, g = p.g && k < D ? p.g[k] : 1.f;
+          h[c][i] = x;
+          dg[c][i] = fmaf(a[c][i], x, dg[c][i]);
           db[c][i] += a[c][i];
-          a[c][i] *= g[i];
+          a[c][i] *= g;
           s1 += a[c][i];
-          s2 = fmaf(a[c][i], h[c][i], s2);
+          s2 = fmaf(a[c][i], x, s2);
         }
       }
     }
@@ -600,21 +590,36 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256) ln_backward_kernel(c
       s2 /= (float)D;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const int cc = c0 + c * kChunk;
-        if (cc >= D) break;  // (uniform over the warp)
-        float o[8], r[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = rstd * (a[c][i] - s1 - h[c][i] * s2);
-        if (p.dres.p) {
-          ld_mat<false>(p.dres, row, cc, D, sm, r);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] += r[i];
+        for (int i = 0; i < 8; ++i) {
+          const int k = c0 + c * kChunk + 32 * i + lane;
+          if (k >= D) continue;
+          float o = rstd * (a[c][i] - s1 - h[c][i] * s2);
+          if (p.dres.p) o += static_cast<const float*>(p.dres.p)[(size_t)row * p.dres.ld + k];
+          if (p.dx.dtype == LAZYMAR_F32) static_cast<float*>(p.dx.p)[(size_t)row * p.dx.ld + k] = o;
+          else static_cast<bf16*>(p.dx.p)[(size_t)row * p.dx.ld + k] = from_f<bf16>(o);
         }
-        st_mat<false>(p.dx, row, cc, D, sm, o);
       }
     }
   }
-  if (p.dg) put_columns<NC, WPR>(p, cols, dg, db);
+  if (!p.dg) return;
+  // the groups' sums in turn, to the CTA's row of the workspace
+  for (int n = 0; n < GROUPS; ++n) {
+    __syncthreads();
+    if (n == grp) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float* s = cols + c0 + c * kChunk + 32 * i + lane;
+          s[0] = n ? s[0] + dg[c][i] : dg[c][i];
+          s[W] = n ? s[W] + db[c][i] : db[c][i];
+        }
+    }
+  }
+  __syncthreads();
+  float* o = p.ws + (size_t)blockIdx.x * 2 * D;
+  for (int i = threadIdx.x; i < 2 * D; i += blockDim.x) o[i] = i < D ? cols[i] : cols[W + i - D];
 }
 
 // CTAs of a backward launch: at most two resident ones for every SM.
@@ -951,14 +956,17 @@ cudaError_t launch_ln_backward(const Ctx& c, const LnBackward& p) {
   const int nc = (p.D + kChunk - 1) / kChunk;
   int ctas = 0;
   cudaError_t e;
-  if (nc <= 5 && p.D % 8 == 0 && p.dy.vec && p.x.vec && p.dres.vec && p.dx.vec) {
+  if (p.D <= 4096 && p.D % 8 == 0 && p.dy.vec && p.x.vec && p.dres.vec && p.dx.vec) {
     const int nb = (p.D + kBlk - 1) / kBlk;
     e = nb <= 1   ? ln_backward_ring_run<1, 1>(c, p, &ctas)
         : nb <= 2 ? ln_backward_ring_run<2, 1>(c, p, &ctas)
         : nb <= 4 ? ln_backward_ring_run<2, 2>(c, p, &ctas)
         : nb <= 6 ? ln_backward_ring_run<3, 2>(c, p, &ctas)
         : nb <= 8 ? ln_backward_ring_run<4, 2>(c, p, &ctas)
-                  : ln_backward_ring_run<5, 2>(c, p, &ctas);
+        : nb <= 10 ? ln_backward_ring_run<5, 2>(c, p, &ctas)
+        : nb <= 12 ? ln_backward_ring_run<3, 4>(c, p, &ctas)
+        : nb <= 16 ? ln_backward_ring_run<4, 4>(c, p, &ctas)
+                   : ln_backward_ring_run<4, 8>(c, p, &ctas);
   } else {
     e = nc <= 1    ? ln_backward_run<1, 1>(c, p, &ctas)
         : nc <= 2  ? ln_backward_run<2, 1>(c, p, &ctas)

@@ -333,6 +333,12 @@ def test_layernorm_backward(M, D, pad, offset, dy_dtype, x_kind, dx_dtype, res):
         assert torch.equal(dres, first)
 
 
+@pytest.mark.parametrize("D", [1288, 1536, 1664, 2056, 2176, 2568, 3080, 3592, 4096, 4104])
+def test_layernorm_backward_of_wide_rows(D):
+    """Widths beyond 1280, among them those that leave some of a row's warps without columns."""
+    test_layernorm_backward(1300, D, 0, 0, "bf16", "block8", "fp32", True)
+
+
 def test_layernorm_backward_without_rows():
     torch = torch_cuda()
     dg, db = vec(np.ones(300)), vec(np.ones(300))
