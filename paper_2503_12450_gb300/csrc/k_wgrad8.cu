@@ -27,27 +27,30 @@ namespace lm {
 // k_gemm.cu
 bool make_tmap_bf16(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint64_t pitch_bytes,
                     uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swz);
+bool make_tmap_u8(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint64_t pitch_bytes,
+                  uint32_t box_inner, uint32_t box_outer, CUtensorMapSwizzle swz);
 
 namespace w8 {
 
 constexpr int TOK = 64;               // tokens of a pipeline stage
-constexpr int STAGES = 6;
+constexpr int STAGES = 4;
 constexpr uint32_t PIECE = TOK * 128; // 64 columns of a stage, in bytes
 constexpr uint32_t OP_BYTES = 2 * PIECE;  // 128 columns of an operand
+constexpr uint32_t Q_BYTES = TOK * 128;   // the checkpoint's bytes behind it
+constexpr uint32_t STAGE_BYTES = 2 * OP_BYTES + Q_BYTES;
 constexpr int CHUNK = 8;              // stages between two additions in registers
 constexpr int EPI_WARPS = 8, CONV_WARPS = 8;
 constexpr uint32_t STG_BYTES = 32 * 128;
-constexpr size_t SMEM = 1024 + STAGES * 2 * OP_BYTES + EPI_WARPS * STG_BYTES + 512;
-constexpr int THREADS = 128 + 32 * (EPI_WARPS + CONV_WARPS);  // warps 0 TMA, 1 MMA, 4-11 converters, 12-19 epilogue
+constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STG_BYTES + STAGES * TOK * 4 + 512;
+constexpr int THREADS = 128 + 32 * (EPI_WARPS + CONV_WARPS);  // warps 0 TMA, 1 MMA, 2 scales, 4-11 converters, 12-19 epilogue
 // Registers: 640 threads launch with 96.
 constexpr int REGS_LAUNCH = 96, REGS_EPI = 168, REGS_CONV = 56, REGS_REST = 32;
 static_assert(REGS_EPI * 256 + REGS_CONV * 256 + REGS_REST * 128 <= REGS_LAUNCH * THREADS,
               "the register split must fit what the launch holds");
 
 struct Params {
-  const uint8_t* q;
   const uint8_t* scale;
-  int ldq, lds;
+  int lds;
   float* out;          // dw, or the partial sums [split, N, K]
   long long out_split; // distance between the partial sums of two splits
   int ldo;
@@ -68,12 +71,6 @@ __device__ __forceinline__ uint64_t desc(uint32_t saddr) {
          ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
-// Two E4M3 bytes (the low ones of `two`) times s as packed bf16, exactly.
-__device__ __forceinline__ uint32_t to_bf16x2(uint32_t two, float s) {
-  const float2 f = e4m3x2_to_f2(two);
-  return pack_bf16(f.x * s, f.y * s);
-}
-
 // mbar_wait where other CTAs of the cluster have written what is waited for.
 __device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned* err) {
   const bool ok = mbar_wait(bar, parity, abort_flag, err);
@@ -87,15 +84,19 @@ __device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, vol
 // own 128 rows, and each converts 128 of the columns. Otherwise 128 x 128 tiles.
 template <bool PAIR>
 __global__ void __launch_bounds__(w8::THREADS, 1)
-    wgrad8_kernel(const __grid_constant__ CUtensorMap tmY, const w8::Params p, unsigned* err) {
+    wgrad8_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmX, const w8::Params p,
+                  unsigned* err) {
   using namespace w8;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sA = smem;
   uint8_t* sB = smem + STAGES * OP_BYTES;
-  uint8_t* sStg = smem + STAGES * 2 * OP_BYTES;
-  uint64_t* full_a = reinterpret_cast<uint64_t*>(sStg + EPI_WARPS * STG_BYTES);
-  uint64_t* full_b = full_a + STAGES;
+  uint8_t* sQ = smem + STAGES * 2 * OP_BYTES;
+  uint8_t* sStg = smem + STAGES * STAGE_BYTES;
+  float* sScale = reinterpret_cast<float*>(sStg + EPI_WARPS * STG_BYTES);
+  uint64_t* full_a = reinterpret_cast<uint64_t*>(sScale + STAGES * TOK);
+  uint64_t* full_q = full_a + STAGES;
+  uint64_t* full_b = full_q + STAGES;
   uint64_t* empty = full_b + STAGES;
   uint64_t* acc_full = empty + STAGES;
   uint64_t* acc_empty = acc_full + 2;
@@ -120,6 +121,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&full_a[s], 1);
+      mbar_init(&full_q[s], 2);  // the bytes and the scales
       mbar_init(&full_b[s], PAIR ? 2 * CONV_WARPS : CONV_WARPS);
       mbar_init(&empty[s], 1);
     }
@@ -130,6 +132,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tmap(&tmY);
+    prefetch_tmap(&tmX);
   }
   if (warp == 1) {
     if (PAIR) {
@@ -151,7 +154,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_REST));
     if (warp == 0 && lane == 0) {
-      // ---------------- TMA producer: dy ----------------
+      // ---------------- TMA producer: dy and the checkpoint's bytes ----------------
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
@@ -161,6 +164,8 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, err)) { ok = false; break; }
           uint8_t* dst = sA + stage * OP_BYTES;
           const int n = t.n + rank * 128, m = t.m + s * TOK;
+          mbar_arrive_expect_tx(&full_q[stage], Q_BYTES);
+          tma_load_2d(&tmX, &full_q[stage], sQ + stage * Q_BYTES, t.k + rank * 128, m);
           if (PAIR) {
             if (rank == 0) mbar_arrive_expect_tx(&full_a[stage], 2 * OP_BYTES);
             const uint32_t bar = cluster_map(smem_u32(&full_a[stage]), 0);
@@ -171,6 +176,29 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
             tma_load_2d(&tmY, &full_a[stage], dst, n, m);
             tma_load_2d(&tmY, &full_a[stage], dst + PIECE, n + 64, m);
           }
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+    } else if (warp == 2) {
+      // ---------------- scales of a stage's tokens, as numbers ----------------
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int i = first; i < items && ok; i += step) {
+        const Item t = item_at(i);
+        const uint8_t* sc = p.scale + (size_t)min((t.k + rank * 128) / kBlk, (p.K - 1) / kBlk) * p.lds;
+        uint32_t b0 = sc[min(t.m + lane, p.M - 1)], b1 = sc[min(t.m + 32 + lane, p.M - 1)];
+        for (int s = 0; s < t.stages; ++s) {
+          const uint32_t c0 = b0, c1 = b1;
+          const int next = t.m + (s + 1) * TOK + lane;
+          b0 = sc[min(next, p.M - 1)];
+          b1 = sc[min(next + 32, p.M - 1)];
+          const bool done = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, err);
+          if (!__all_sync(0xffffffffu, done)) { ok = false; break; }
+          sScale[stage * TOK + lane] = block8_scale(c0);
+          sScale[stage * TOK + 32 + lane] = block8_scale(c1);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&full_q[stage]);
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
       }
@@ -221,56 +249,36 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   } else if (warp < 4 + CONV_WARPS) {
     // ---------------- converters: the checkpoint's bytes to bf16 ----------------
     // A lane takes eight columns of a token (16 lanes a token of 128 columns),
-    // four tokens a stage; the bytes of the next stage are in flight meanwhile.
+    // four tokens a stage. What lies beyond M or K has come as zero bytes.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CONV));
     const int cw = warp - 4, col = 8 * (lane & 15), t0 = 2 * cw + (lane >> 4);  // tokens t0, t0 + 16, + 32, + 48
-    uint2 w[4];
-    uint32_t sb[4];
-    auto load = [&](const Item& t, int s) {
-      const int k = t.k + rank * 128 + col;
-      const uint8_t* sc = p.scale + (size_t)((t.k + rank * 128) / kBlk) * p.lds;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int m = t.m + s * TOK + t0 + 16 * j;
-        w[j] = make_uint2(0u, 0u);
-        sb[j] = 127u;
-        if (m < p.M && k < p.K) {
-          w[j] = *reinterpret_cast<const uint2*>(p.q + (size_t)m * p.ldq + k);
-          sb[j] = sc[m];
-        }
-      }
-    };
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    if (first < items) load(item_at(first), 0);
     for (int i = first; i < items && ok; i += step) {
-      const Item t = item_at(i);
-      const int past = t.k + rank * 128 + col + 8 - p.K;  // of this lane's columns, those beyond K
-      for (int s = 0; s < t.stages; ++s) {
-        uint4 v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (past > 0) {
-            if (past >= 4) w[j].y = 0u;
-            else w[j].y &= 0xFFFFFFFFu >> (8 * past);
-            if (past > 4) w[j].x = past >= 8 ? 0u : w[j].x & (0xFFFFFFFFu >> (8 * (past - 4)));
-          }
-          const float f = block8_scale(sb[j]);
-          v[j] = make_uint4(to_bf16x2(w[j].x & 0xFFFFu, f), to_bf16x2(w[j].x >> 16, f),
-                            to_bf16x2(w[j].y & 0xFFFFu, f), to_bf16x2(w[j].y >> 16, f));
-        }
-        if (s + 1 < t.stages) load(t, s + 1);
-        else if (i + step < items) load(item_at(i + step), 0);
-        const bool done = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, err);
+      const int stages = item_at(i).stages;
+      for (int s = 0; s < stages; ++s) {
+        const bool done = mbar_wait(&full_q[stage], phase, abort_flag, err);
         if (!__all_sync(0xffffffffu, done)) { ok = false; break; }
+        const uint8_t* src = sQ + stage * Q_BYTES + col;
+        const float* sc = sScale + stage * TOK;
         // row (token) r, 16-byte piece c of its 64 columns at piece c ^ (r & 7)
         uint8_t* dst = sB + stage * OP_BYTES + (col >> 6) * PIECE;
         const int c = (col >> 3) & 7;
+        uint2 w[4];
+        float f[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j] = *reinterpret_cast<const uint2*>(src + (t0 + 16 * j) * 128);
+          f[j] = sc[t0 + 16 * j];
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int r = t0 + 16 * j;
-          *reinterpret_cast<uint4*>(dst + r * 128 + ((c ^ (r & 7)) << 4)) = v[j];
+          float v[8];
+          block8_values(w[j], f[j], v);
+          *reinterpret_cast<uint4*>(dst + r * 128 + ((c ^ (r & 7)) << 4)) =
+              make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -440,13 +448,12 @@ cudaError_t launch_wgrad8(const Ctx& c, const Wgrad8& x) {
                       x.N, x.K, false);
   }
   const Plan pl = plan_wgrad8(x.M, x.N, x.K);
-  CUtensorMap ty;
-  if (!make_tmap_bf16(&ty, x.dy, x.N, x.M, (uint64_t)x.lddy * 2, 64, TOK, CU_TENSOR_MAP_SWIZZLE_128B))
+  CUtensorMap ty, tx;
+  if (!make_tmap_bf16(&ty, x.dy, x.N, x.M, (uint64_t)x.lddy * 2, 64, TOK, CU_TENSOR_MAP_SWIZZLE_128B) ||
+      !make_tmap_u8(&tx, x.x.q, x.K, x.M, x.x.ldq, 128, TOK, CU_TENSOR_MAP_SWIZZLE_NONE))
     return cudaErrorInvalidValue;
   Params p{};
-  p.q = static_cast<const uint8_t*>(x.x.q);
   p.scale = x.x.scale;
-  p.ldq = x.x.ldq;
   p.lds = x.x.lds;
   p.M = x.M;
   p.N = x.N;
@@ -470,10 +477,10 @@ cudaError_t launch_wgrad8(const Ctx& c, const Wgrad8& x) {
   cudaError_t e;
   if (pl.pair) {
     if ((e = prepare_wgrad8<true>()) != cudaSuccess) return e;
-    e = launch_pdl_cluster(wgrad8_kernel<true>, dim3(2 * grid), dim3(THREADS), SMEM, 2, c.stream, ty, p, c.err);
+    e = launch_pdl_cluster(wgrad8_kernel<true>, dim3(2 * grid), dim3(THREADS), SMEM, 2, c.stream, ty, tx, p, c.err);
   } else {
     if ((e = prepare_wgrad8<false>()) != cudaSuccess) return e;
-    e = launch_pdl(wgrad8_kernel<false>, dim3(grid), dim3(THREADS), SMEM, c.stream, ty, p, c.err);
+    e = launch_pdl(wgrad8_kernel<false>, dim3(grid), dim3(THREADS), SMEM, c.stream, ty, tx, p, c.err);
   }
   if (e != cudaSuccess || pl.split == 1) return e;
   return launch_pdl(wgrad8_sum_kernel, dim3(sum_grid), dim3(256), 0, c.stream, (const float*)x.ws, pl.split, x.dw, x.lddw,
