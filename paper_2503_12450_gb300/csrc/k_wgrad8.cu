@@ -39,10 +39,10 @@ constexpr uint32_t OP_BYTES = 2 * PIECE;  // 128 columns of an operand
 constexpr uint32_t Q_BYTES = TOK * 128;   // the checkpoint's bytes behind it
 constexpr uint32_t STAGE_BYTES = 2 * OP_BYTES + Q_BYTES;
 constexpr int CHUNK = 8;              // stages between two additions in registers
-constexpr int EPI_WARPS = 8, CONV_WARPS = 8;
+constexpr int EPI_WARPS = 8, CONV_WARPS = 8, CONV_GROUP = 4;
 constexpr uint32_t STG_BYTES = 32 * 128;
 constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STG_BYTES + STAGES * TOK * 4 + 512;
-constexpr int THREADS = 128 + 32 * (EPI_WARPS + CONV_WARPS);  // warps 0 TMA, 1 MMA, 2 scales, 4-11 converters, 12-19 epilogue
+constexpr int THREADS = 128 + 32 * (EPI_WARPS + CONV_WARPS);  // warps 0 TMA, 1 MMA, 2 scales, 3 relay, 4-11 converters, 12-19 epilogue
 // Registers: 640 threads launch with 96.
 constexpr int REGS_LAUNCH = 96, REGS_EPI = 168, REGS_CONV = 56, REGS_REST = 32;
 static_assert(REGS_EPI * 256 + REGS_CONV * 256 + REGS_REST * 128 <= REGS_LAUNCH * THREADS,
@@ -71,11 +71,32 @@ __device__ __forceinline__ uint64_t desc(uint32_t saddr) {
          ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
-// mbar_wait where other CTAs of the cluster have written what is waited for.
+// mbar_wait for what another CTA of the cluster has released.
 __device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned* err) {
-  const bool ok = mbar_wait(bar, parity, abort_flag, err);
-  asm volatile("fence.acq_rel.cluster;" ::: "memory");
-  return ok;
+  auto tried = [&] {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity), "r"(1000000u)
+        : "memory");
+    return ok != 0;
+  };
+  if (tried()) return true;
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t i = 1;; ++i) {
+    if (tried()) return true;
+    if ((i & 63u) == 0) {
+      if (*abort_flag) return false;
+      if (globaltimer_ns() - t0 > kWaitLimitNs) {
+        *abort_flag = 1;
+        atomicOr(err, ERR_TIMEOUT);
+        return false;
+      }
+    }
+  }
 }
 
 }  // namespace w8
@@ -97,7 +118,8 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   uint64_t* full_a = reinterpret_cast<uint64_t*>(sScale + STAGES * TOK);
   uint64_t* full_q = full_a + STAGES;
   uint64_t* full_b = full_q + STAGES;
-  uint64_t* empty = full_b + STAGES;
+  uint64_t* done_b = full_b + STAGES;  // of a pair's odd CTA: its converters, for the relay
+  uint64_t* empty = done_b + STAGES;
   uint64_t* acc_full = empty + STAGES;
   uint64_t* acc_empty = acc_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
@@ -122,7 +144,8 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&full_a[s], 1);
       mbar_init(&full_q[s], 2);  // the bytes and the scales
-      mbar_init(&full_b[s], PAIR ? 2 * CONV_WARPS : CONV_WARPS);
+      mbar_init(&full_b[s], PAIR ? CONV_GROUP + 1 : CONV_GROUP);
+      mbar_init(&done_b[s], CONV_GROUP);
       mbar_init(&empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -202,6 +225,25 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
       }
+    } else if (PAIR && warp == 3 && rank == 1) {
+      // ---------------- relay ----------------
+      // A release to the other CTA waits for what the thread has seen written,
+      // which would hold up a converter in every stage (membar stalls: 0.99 us a
+      // stage). So the converters release within the CTA, and this thread on.
+      if (lane == 0) {
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int i = first; i < items && ok; i += step) {
+          const int stages = item_at(i).stages;
+          for (int s = 0; s < stages; ++s) {
+            if (!mbar_wait(&done_b[stage], phase, abort_flag, err)) { ok = false; break; }
+            mbar_arrive_cluster(cluster_map(smem_u32(&full_b[stage]), 0));
+            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+      __syncwarp();
     } else if (warp == 1 && rank == 0) {
       // ---------------- MMA issuer (of a pair: the even CTA's) ----------------
       const bool lead = elect_one();
@@ -248,43 +290,44 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
     __syncwarp();
   } else if (warp < 4 + CONV_WARPS) {
     // ---------------- converters: the checkpoint's bytes to bf16 ----------------
-    // A lane takes eight columns of a token (16 lanes a token of 128 columns),
-    // four tokens a stage. What lies beyond M or K has come as zero bytes.
+    // Two groups of four warps take the stages in turn, so that one group's
+    // waits and fences pass while the other converts. A lane takes eight columns
+    // of a token (16 lanes a token of 128 columns), eight tokens a stage. What
+    // lies beyond M or K has come as zero bytes.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CONV));
-    const int cw = warp - 4, col = 8 * (lane & 15), t0 = 2 * cw + (lane >> 4);  // tokens t0, t0 + 16, + 32, + 48
-    int stage = 0;
+    const int cw = (warp - 4) & (CONV_GROUP - 1), group = (warp - 4) / CONV_GROUP;
+    const int col = 8 * (lane & 15), t0 = 2 * cw + (lane >> 4);  // tokens t0 + 8 j
+    int stage = 0, turn = 0;
     uint32_t phase = 0;
     bool ok = true;
     for (int i = first; i < items && ok; i += step) {
       const int stages = item_at(i).stages;
-      for (int s = 0; s < stages; ++s) {
-        const bool done = mbar_wait(&full_q[stage], phase, abort_flag, err);
-        if (!__all_sync(0xffffffffu, done)) { ok = false; break; }
-        const uint8_t* src = sQ + stage * Q_BYTES + col;
-        const float* sc = sScale + stage * TOK;
-        // row (token) r, 16-byte piece c of its 64 columns at piece c ^ (r & 7)
-        uint8_t* dst = sB + stage * OP_BYTES + (col >> 6) * PIECE;
-        const int c = (col >> 3) & 7;
-        uint2 w[4];
-        float f[4];
+      for (int s = 0; s < stages; ++s, turn ^= 1) {
+        if (turn == group) {
+          const bool done = mbar_wait(&full_q[stage], phase, abort_flag, err);
+          if (!__all_sync(0xffffffffu, done)) { ok = false; break; }
+          const uint8_t* src = sQ + stage * Q_BYTES + col;
+          const float* sc = sScale + stage * TOK;
+          // row (token) r, 16-byte piece c of its 64 columns at piece c ^ (r & 7)
+          uint8_t* dst = sB + stage * OP_BYTES + (col >> 6) * PIECE;
+          const int c = ((col >> 3) & 7) ^ (t0 & 7);  // (the same for all of the lane's tokens)
+          uint2 w[8];
+          float f[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[j] = *reinterpret_cast<const uint2*>(src + (t0 + 16 * j) * 128);
-          f[j] = sc[t0 + 16 * j];
-        }
+          for (int j = 0; j < 8; ++j) {
+            w[j] = *reinterpret_cast<const uint2*>(src + (t0 + 8 * j) * 128);
+            f[j] = sc[t0 + 8 * j];
+          }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = t0 + 16 * j;
-          float v[8];
-          block8_values(w[j], f[j], v);
-          *reinterpret_cast<uint4*>(dst + r * 128 + ((c ^ (r & 7)) << 4)) =
-              make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          if (PAIR) mbar_arrive_cluster(cluster_map(smem_u32(&full_b[stage]), 0));
-          else mbar_arrive(&full_b[stage]);
+          for (int j = 0; j < 8; ++j) {
+            float v[8];
+            block8_values(w[j], f[j], v);
+            *reinterpret_cast<uint4*>(dst + (t0 + 8 * j) * 128 + (c << 4)) =
+                make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(PAIR && rank == 1 ? &done_b[stage] : &full_b[stage]);
         }
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
       }
