@@ -42,7 +42,7 @@ constexpr int CHUNK = 8;              // stages between two additions in registe
 constexpr int EPI_WARPS = 8, CONV_WARPS = 8, CONV_GROUP = 4;
 constexpr uint32_t STG_BYTES = 32 * 128;
 constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STG_BYTES + STAGES * TOK * 4 + 512;
-constexpr int THREADS = 128 + 32 * (EPI_WARPS + CONV_WARPS);  // warps 0 TMA, 1 MMA, 2 scales, 3 relay, 4-11 converters, 12-19 epilogue
+constexpr int THREADS = 128 + 32 * (EPI_WARPS + CONV_WARPS);  // warps 0 TMA, 1 MMA, 2 scales, 4-11 converters, 12-19 epilogue
 // Registers: 640 threads launch with 96.
 constexpr int REGS_LAUNCH = 96, REGS_EPI = 168, REGS_CONV = 56, REGS_REST = 32;
 static_assert(REGS_EPI * 256 + REGS_CONV * 256 + REGS_REST * 128 <= REGS_LAUNCH * THREADS,
@@ -71,32 +71,13 @@ __device__ __forceinline__ uint64_t desc(uint32_t saddr) {
          ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
-// mbar_wait for what another CTA of the cluster has released.
-__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned* err) {
-  auto tried = [&] {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity), "r"(1000000u)
-        : "memory");
-    return ok != 0;
-  };
-  if (tried()) return true;
-  const uint64_t t0 = globaltimer_ns();
-  for (uint32_t i = 1;; ++i) {
-    if (tried()) return true;
-    if ((i & 63u) == 0) {
-      if (*abort_flag) return false;
-      if (globaltimer_ns() - t0 > kWaitLimitNs) {
-        *abort_flag = 1;
-        atomicOr(err, ERR_TIMEOUT);
-        return false;
-      }
-    }
-  }
+// Arrives on a barrier of the pair's even CTA for operand bytes that this
+// thread's warp has written and fenced for the asynchronous proxy in its own
+// shared memory. They are read by this SM's half of the MMA alone, never by the
+// other CTA's threads, so the release need not reach beyond this CTA; one that
+// does (release.cluster) waits for the SM's writes and held a stage up by 0.3 us.
+__device__ __forceinline__ void arrive_even(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_map(smem_u32(bar), 0)) : "memory");
 }
 
 }  // namespace w8
@@ -118,8 +99,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   uint64_t* full_a = reinterpret_cast<uint64_t*>(sScale + STAGES * TOK);
   uint64_t* full_q = full_a + STAGES;
   uint64_t* full_b = full_q + STAGES;
-  uint64_t* done_b = full_b + STAGES;  // of a pair's odd CTA: its converters, for the relay
-  uint64_t* empty = done_b + STAGES;
+  uint64_t* empty = full_b + STAGES;
   uint64_t* acc_full = empty + STAGES;
   uint64_t* acc_empty = acc_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
@@ -144,8 +124,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&full_a[s], 1);
       mbar_init(&full_q[s], 2);  // the bytes and the scales
-      mbar_init(&full_b[s], PAIR ? CONV_GROUP + 1 : CONV_GROUP);
-      mbar_init(&done_b[s], CONV_GROUP);
+      mbar_init(&full_b[s], PAIR ? 2 * CONV_GROUP : CONV_GROUP);
       mbar_init(&empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -225,25 +204,6 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
       }
-    } else if (PAIR && warp == 3 && rank == 1) {
-      // ---------------- relay ----------------
-      // A release to the other CTA waits for what the thread has seen written,
-      // which would hold up a converter in every stage (membar stalls: 0.99 us a
-      // stage). So the converters release within the CTA, and this thread on.
-      if (lane == 0) {
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (int i = first; i < items && ok; i += step) {
-          const int stages = item_at(i).stages;
-          for (int s = 0; s < stages; ++s) {
-            if (!mbar_wait(&done_b[stage], phase, abort_flag, err)) { ok = false; break; }
-            mbar_arrive_cluster(cluster_map(smem_u32(&full_b[stage]), 0));
-            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-          }
-        }
-      }
-      __syncwarp();
     } else if (warp == 1 && rank == 0) {
       // ---------------- MMA issuer (of a pair: the even CTA's) ----------------
       const bool lead = elect_one();
@@ -257,9 +217,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           const bool fresh = s % CHUNK == 0, last = s % CHUNK == CHUNK - 1 || s == stages - 1;
           if (fresh && !(ok = all(mbar_wait(&acc_empty[buf], use ^ 1u, abort_flag, err)))) break;
           if (!(ok = all(mbar_wait(&full_a[stage], phase, abort_flag, err)))) break;
-          if (!(ok = all(PAIR ? wait_cluster(&full_b[stage], phase, abort_flag, err)
-                              : mbar_wait(&full_b[stage], phase, abort_flag, err))))
-            break;
+          if (!(ok = all(mbar_wait(&full_b[stage], phase, abort_flag, err)))) break;
           tc_fence_after();
           if (lead) {
             const uint64_t a0 = desc(smem_u32(sA + stage * OP_BYTES)), b0 = desc(smem_u32(sB + stage * OP_BYTES));
@@ -327,7 +285,10 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           }
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive(PAIR && rank == 1 ? &done_b[stage] : &full_b[stage]);
+          if (lane == 0) {
+            if (PAIR) arrive_even(&full_b[stage]);
+            else mbar_arrive(&full_b[stage]);
+          }
         }
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
       }
