@@ -27,16 +27,16 @@ namespace l8 {
 
 constexpr int BM = 128;               // rows of a CTA's tile
 constexpr int KB_BYTES = 128;         // K of a pipeline stage: one scale block, one swizzle atom
-constexpr int STAGES = 6;
+constexpr int STAGES = 5;
 constexpr uint32_t A_BYTES = BM * KB_BYTES;
 constexpr uint32_t B_BYTES = 128 * KB_BYTES;  // rows of w in a CTA's shared memory: the tile's, or a pair's half
 constexpr uint32_t STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int EPI_WARPS = 8;
-constexpr uint32_t STG_BYTES = 32 * 128;      // a warp's staging: 32 rows of 128 bytes
-constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STG_BYTES + 512;
+constexpr uint32_t STG_BYTES = 32 * 128;      // one of a warp's two staging buffers: 32 rows of 128 bytes
+constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * STG_BYTES + 512;
 constexpr int THREADS = 512;  // warps 0 TMA, 1 MMA, 4-7 scales, 8-15 epilogue
 // Registers: 512 threads launch with 128; the epilogue holds a row's 128 values.
-constexpr int REGS_EPI = 200, REGS_REST = 48;
+constexpr int REGS_EPI = 208, REGS_REST = 48;
 static_assert((REGS_EPI + REGS_REST) * 256 <= 128 * THREADS, "the register split must fit what the launch holds");
 constexpr int SF_SLOTS = 4;           // scale slots of 16 tensor-memory columns: 4 of a, 8 of w
 constexpr uint32_t SF_BASE = 256;     // behind the accumulator's columns
@@ -94,12 +94,14 @@ __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&r)[4])
 }
 
 // A row's 128 values to E4M3 words and the scale byte. The scale is that of the
-// finite values; infinities become NaN.
+// finite values; infinities become NaN (with NaN, apart from the fast path).
 __device__ __forceinline__ uint32_t quantize_row(const float (&v)[128], uint32_t (&w)[32]) {
-  float m = 0.f;
+  float m[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < 128; i += 2) m = fmax3(m, fabsf(v[i]), fabsf(v[i + 1]));
-  uint32_t amax = __float_as_uint(m);
+  for (int i = 0; i < 128; i += 8)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = fmax3(m[j], fabsf(v[i + 2 * j]), fabsf(v[i + 2 * j + 1]));
+  uint32_t amax = __float_as_uint(fmax3(fmaxf(m[0], m[1]), m[2], m[3]));
   const bool special = amax >= 0x7F800000u;
   if (special) {
     amax = 0;
@@ -111,14 +113,18 @@ __device__ __forceinline__ uint32_t quantize_row(const float (&v)[128], uint32_t
   }
   const uint32_t byte = block8_exp(amax);
   const float s = block8_inv(byte);
+  const unsigned long long ss = f32x2_pack(s, s);
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
-    w[i] = e4m3x4(v[4 * i] * s, v[4 * i + 1] * s, v[4 * i + 2] * s, v[4 * i + 3] * s);
-    if (special) {
+    float a, b, c, d;
+    f32x2_unpack(f32x2_mul(f32x2_pack(v[4 * i], v[4 * i + 1]), ss), a, b);
+    f32x2_unpack(f32x2_mul(f32x2_pack(v[4 * i + 2], v[4 * i + 3]), ss), c, d);
+    w[i] = e4m3x4(a, b, c, d);
+  }
+  if (special) {  // (saturated to 448 above)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if ((__float_as_uint(v[4 * i + j]) & 0x7F800000u) == 0x7F800000u) w[i] |= 0x7Fu << (8 * j);
-    }
+    for (int i = 0; i < 128; ++i)
+      if ((__float_as_uint(v[i]) & 0x7F800000u) == 0x7F800000u) w[i / 4] |= 0x7Fu << (8 * (i % 4));
   }
   return byte;
 }
@@ -142,7 +148,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
   uint8_t* sA = smem;
   uint8_t* sB = smem + STAGES * A_BYTES;
   uint8_t* sStg = smem + STAGES * STAGE_BYTES;
-  uint64_t* full = reinterpret_cast<uint64_t*>(sStg + EPI_WARPS * STG_BYTES);
+  uint64_t* full = reinterpret_cast<uint64_t*>(sStg + EPI_WARPS * 2 * STG_BYTES);
   uint64_t* empty = full + STAGES;
   uint64_t* sf_full = empty + STAGES;
   uint64_t* sf_empty = sf_full + SF_SLOTS;
@@ -315,14 +321,37 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
     // ---------------- epilogue ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
     const int quarter = warp & 3, unit = (warp - 8) >> 2;  // lane quarter, 128 columns of the accumulator
-    uint8_t* stg = sStg + (warp - 8) * STG_BYTES;
-    int it = 0;
+    uint8_t* const stg2 = sStg + (warp - 8) * 2 * STG_BYTES;
+    int flip = 0, it = 0;
     for (int tile = first; tile < tiles; tile += step, ++it) {
       // single CTAs: the tiles alternate between the two units
       if (!PAIR && (it & 1) != unit) continue;
       const uint32_t use = PAIR ? (uint32_t)it & 1u : (uint32_t)(it >> 1) & 1u;
       const int rbase = (tile / num_n) * TM + rank * BM + quarter * 32;
       const int n0 = (tile % num_n) * TN + (PAIR ? unit * 128 : 0);
+      const int lr0 = lane >> 3, cq = lane & 7;  // row of four and 16-byte piece in the output passes
+      // the residual of 32 columns, eight passes of four rows; the first ones'
+      // before the accumulator is ready
+      float4 res[8];
+      auto load_res = [&](int c) {
+        const int col = n0 + 32 * c + 4 * cq;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int r = rbase + 4 * q + lr0;
+          res[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (r >= p.M || col >= p.N) continue;
+          const float* x = p.residual + (size_t)r * p.ldr + col;
+          if (p.res_vec && col + 4 <= p.N) {
+            res[q] = *reinterpret_cast<const float4*>(x);
+          } else {
+            res[q].x = x[0];
+            if (col + 1 < p.N) res[q].y = x[1];
+            if (col + 2 < p.N) res[q].z = x[2];
+            if (col + 3 < p.N) res[q].w = x[3];
+          }
+        }
+      };
+      if (p.epilogue == LAZYMAR_EPI_RESIDUAL) load_res(0);
       const bool done = mbar_wait(&acc_full[PAIR ? 0 : unit], use, abort_flag, err);
       if (!__all_sync(0xffffffffu, done)) break;
       tc_fence_after();
@@ -366,13 +395,19 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
         uint32_t w[32];
         const uint32_t byte = quantize_row(v, w);
         if (row < p.M) scale[(size_t)(n0 / kBlk) * lds + row] = (uint8_t)byte;
-        if (lane == 0) bulk_wait_read();
+        uint8_t* stg = stg2 + flip * STG_BYTES;
+        flip ^= 1;
+        const bool tma = (p.N & 15) == 0 || n0 + 128 <= p.N;
+        if (lane == 0) {  // what this buffer held has been stored
+          if (tma) bulk_wait_read_but_one();
+          else bulk_wait_read();
+        }
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           *reinterpret_cast<uint4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) =
               make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-        if ((p.N & 15) == 0 || n0 + 128 <= p.N) {
+        if (tma) {
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
@@ -404,59 +439,59 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       if (p.out) {
         // 32 columns at a time through the staging buffer, so that stores and
         // residual loads cover whole rows of it
-        const int lr0 = lane >> 3, cq = lane & 7;
+        if (lane == 0) bulk_wait_read();
+        __syncwarp();
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const int col = n0 + 32 * c + 4 * cq;
           if (n0 + 32 * c >= p.N) break;
-          if (lane == 0) bulk_wait_read();
-          __syncwarp();
+          uint8_t* stg = stg2 + (c & 1) * STG_BYTES;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             *reinterpret_cast<float4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) =
                 make_float4(v[32 * c + 4 * j], v[32 * c + 4 * j + 1], v[32 * c + 4 * j + 2], v[32 * c + 4 * j + 3]);
           __syncwarp();
+          float4 o[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
-            const int lr = 4 * q + lr0, r = rbase + lr;
-            float4 o = *reinterpret_cast<const float4*>(stg + lr * 128 + ((cq ^ (lr & 7)) << 4));
+            const int lr = 4 * q + lr0;
+            o[q] = *reinterpret_cast<const float4*>(stg + lr * 128 + ((cq ^ (lr & 7)) << 4));
+          }
+          if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              o[q] = make_float4(o[q].x + res[q].x, o[q].y + res[q].y, o[q].z + res[q].z, o[q].w + res[q].w);
+            // (other columns than those stored below, so in place is fine)
+            if (c < 3 && n0 + 32 * (c + 1) < p.N) load_res(c + 1);
+          }
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const int r = rbase + 4 * q + lr0;
             if (r >= p.M || col >= p.N) continue;
-            if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
-              const float* x = p.residual + (size_t)r * p.ldr + col;
-              if (p.res_vec && col + 4 <= p.N) {
-                const float4 z = *reinterpret_cast<const float4*>(x);
-                o = make_float4(o.x + z.x, o.y + z.y, o.z + z.z, o.w + z.w);
-              } else {
-                o.x += x[0];
-                if (col + 1 < p.N) o.y += x[1];
-                if (col + 2 < p.N) o.z += x[2];
-                if (col + 3 < p.N) o.w += x[3];
-              }
-            }
             if (p.out_dtype == LAZYMAR_F32) {
               float* y = static_cast<float*>(p.out) + (size_t)r * p.ldo + col;
               if (p.out_vec && col + 4 <= p.N) {
-                *reinterpret_cast<float4*>(y) = o;
+                *reinterpret_cast<float4*>(y) = o[q];
               } else {
-                y[0] = o.x;
-                if (col + 1 < p.N) y[1] = o.y;
-                if (col + 2 < p.N) y[2] = o.z;
-                if (col + 3 < p.N) y[3] = o.w;
+                y[0] = o[q].x;
+                if (col + 1 < p.N) y[1] = o[q].y;
+                if (col + 2 < p.N) y[2] = o[q].z;
+                if (col + 3 < p.N) y[3] = o[q].w;
               }
             } else {
               bf16* y = static_cast<bf16*>(p.out) + (size_t)r * p.ldo + col;
               if (p.out_vec && col + 4 <= p.N) {
-                *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+                *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(o[q].x, o[q].y), pack_bf16(o[q].z, o[q].w));
               } else {
-                y[0] = from_f<bf16>(o.x);
-                if (col + 1 < p.N) y[1] = from_f<bf16>(o.y);
-                if (col + 2 < p.N) y[2] = from_f<bf16>(o.z);
-                if (col + 3 < p.N) y[3] = from_f<bf16>(o.w);
+                y[0] = from_f<bf16>(o[q].x);
+                if (col + 1 < p.N) y[1] = from_f<bf16>(o[q].y);
+                if (col + 2 < p.N) y[2] = from_f<bf16>(o[q].z);
+                if (col + 3 < p.N) y[3] = from_f<bf16>(o[q].w);
               }
             }
           }
-          __syncwarp();
         }
+        __syncwarp();
       }
     }
     if (lane == 0) bulk_wait_all();
