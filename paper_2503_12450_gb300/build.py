@@ -23,7 +23,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O3",
                      "--expt-relaxed-constexpr", "-I", INCLUDE]
 SOURCES = ["lazymar_api.cu", "k_gemm.cu", "k_attention.cu", "k_rowwise.cu", "k_select.cu", "k_head.cu",
-           "train_api.cu", "k_train.cu", "k_linear8.cu", "k_wgrad8.cu"]
+           "train_api.cu", "k_train.cu", "k_linear8.cu", "k_linear8_rows.cu", "k_wgrad8.cu"]
 
 
 def nvcc():

@@ -168,6 +168,9 @@ struct Linear8 {
   int M, N, K;
 };
 cudaError_t launch_linear8(const Ctx& c, const Linear8& p);
+// The same for at most kLinear8FewRows rows of a.
+constexpr int kLinear8FewRows = 32;
+cudaError_t launch_linear8_rows(const Ctx& c, const Linear8& p);
 
 // The weight gradient (lazymar_block8_wgrad).
 struct Wgrad8 {

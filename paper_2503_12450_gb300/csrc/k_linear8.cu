@@ -38,6 +38,9 @@ constexpr int THREADS = 512;  // warps 0 TMA, 1 MMA, 4-7 scales, 8-15 epilogue
 // Registers: 512 threads launch with 128; the epilogue holds a row's 128 values.
 constexpr int REGS_EPI = 208, REGS_REST = 48;
 static_assert((REGS_EPI + REGS_REST) * 256 <= 128 * THREADS, "the register split must fit what the launch holds");
+// Kinds of output: fp32 or bf16; the same with a residual; 8-bit tensors (and
+// fp32 or bf16 next to them).
+enum { OUT_PLAIN = 0, OUT_RESIDUAL = 1, OUT_BLOCK8 = 2 };
 constexpr int SF_SLOTS = 4;           // scale slots of 16 tensor-memory columns: 4 of a, 8 of w
 constexpr uint32_t SF_BASE = 256;     // behind the accumulator's columns
 
@@ -137,7 +140,8 @@ __device__ __forceinline__ uint32_t quantize_row(const float (&v)[128], uint32_t
 // Accumulator: 256 columns, a pair's whole tile or two single tiles in turn. The
 // epilogue warps (two for each lane quarter, one for each 128 columns) take a
 // row's 128 columns into registers and hand the accumulator back at once.
-template <bool PAIR>
+// OUT: what the epilogue writes, so that each kind has the registers it needs.
+template <bool PAIR, int OUT>
 __global__ void __launch_bounds__(l8::THREADS, 1)
     linear8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmO8, const __grid_constant__ CUtensorMap tmU8,
@@ -351,7 +355,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
           }
         }
       };
-      if (p.epilogue == LAZYMAR_EPI_RESIDUAL) load_res(0);
+      if (OUT == OUT_RESIDUAL) load_res(0);
       const bool done = mbar_wait(&acc_full[PAIR ? 0 : unit], use, abort_flag, err);
       if (!__all_sync(0xffffffffu, done)) break;
       tc_fence_after();
@@ -430,12 +434,12 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
         }
         __syncwarp();
       };
-      if (p.u8) put8(&tmU8, p.u8, p.ldu8, p.u8_scale, p.lds_u8);
-      if (p.epilogue == LAZYMAR_EPI_GELU) {
+      if (OUT == OUT_BLOCK8 && p.u8) put8(&tmU8, p.u8, p.ldu8, p.u8_scale, p.lds_u8);
+      if (OUT != OUT_RESIDUAL && p.epilogue == LAZYMAR_EPI_GELU) {
 #pragma unroll
         for (int i = 0; i < 64; ++i) gelu_erf_x2(v[2 * i], v[2 * i + 1]);
       }
-      if (p.out8) put8(&tmO8, p.out8, p.ldout8, p.out8_scale, p.lds_out8);
+      if (OUT == OUT_BLOCK8 && p.out8) put8(&tmO8, p.out8, p.ldout8, p.out8_scale, p.lds_out8);
       if (p.out) {
         // 32 columns at a time through the staging buffer, so that stores and
         // residual loads cover whole rows of it
@@ -457,7 +461,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
             const int lr = 4 * q + lr0;
             o[q] = *reinterpret_cast<const float4*>(stg + lr * 128 + ((cq ^ (lr & 7)) << 4));
           }
-          if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
+          if (OUT == OUT_RESIDUAL) {
 #pragma unroll
             for (int q = 0; q < 8; ++q)
               o[q] = make_float4(o[q].x + res[q].x, o[q].y + res[q].y, o[q].z + res[q].z, o[q].w + res[q].w);
@@ -508,27 +512,44 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
 
 namespace {
 
-// Shared-memory size and, once for each device, the check that the launch holds
-// the registers that the kernel's warps share out.
-template <bool PAIR>
-cudaError_t prepare_linear8() {
+// Once for each device: the shared-memory size, and the check that the launch
+// holds the registers that the kernel's warps share out.
+template <bool PAIR, int OUT>
+cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to,
+                        const CUtensorMap& tu, const l8::Params& p, long long tiles) {
+  using namespace l8;
+  const auto kernel = linear8_kernel<PAIR, OUT>;
   static int ready[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  if (dev >= 0 && dev < 64 && ready[dev]) return cudaSuccess;
-  cudaFuncAttributes a;
-  if ((e = cudaFuncGetAttributes(&a, linear8_kernel<PAIR>)) != cudaSuccess) return e;
-  if (a.numRegs * l8::THREADS < (l8::REGS_EPI + l8::REGS_REST) * 256) return cudaErrorInvalidConfiguration;
-  e = cudaFuncSetAttribute(linear8_kernel<PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l8::SMEM);
-  if (e == cudaSuccess && dev >= 0 && dev < 64) ready[dev] = 1;
-  return e;
+  if (dev < 0 || dev >= 64 || !ready[dev]) {
+    cudaFuncAttributes a;
+    if ((e = cudaFuncGetAttributes(&a, kernel)) != cudaSuccess) return e;
+    if (a.numRegs * THREADS < (REGS_EPI + REGS_REST) * 256) return cudaErrorInvalidConfiguration;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM)) != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) ready[dev] = 1;
+  }
+  const int slots = PAIR ? c.num_sms / 2 : c.num_sms;
+  const unsigned grid = (unsigned)(tiles < slots ? tiles : slots);
+  if (PAIR)
+    return launch_pdl_cluster(kernel, dim3(2 * grid), dim3(THREADS), SMEM, 2, c.stream, ta, tb, to, tu, p, c.err);
+  return launch_pdl(kernel, dim3(grid), dim3(THREADS), SMEM, c.stream, ta, tb, to, tu, p, c.err);
+}
+
+template <bool PAIR>
+cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to,
+                        const CUtensorMap& tu, const l8::Params& p, long long tiles) {
+  if (p.out8 || p.u8) return run_linear8<PAIR, l8::OUT_BLOCK8>(c, ta, tb, to, tu, p, tiles);
+  if (p.epilogue == LAZYMAR_EPI_RESIDUAL) return run_linear8<PAIR, l8::OUT_RESIDUAL>(c, ta, tb, to, tu, p, tiles);
+  return run_linear8<PAIR, l8::OUT_PLAIN>(c, ta, tb, to, tu, p, tiles);
 }
 
 }  // namespace
 
 cudaError_t launch_linear8(const Ctx& c, const Linear8& x) {
   using namespace l8;
+  if (x.M <= kLinear8FewRows) return launch_linear8_rows(c, x);
   CUtensorMap ta, tb, to, tu;
   std::memset(&to, 0, sizeof to);
   std::memset(&tu, 0, sizeof tu);
@@ -566,17 +587,8 @@ cudaError_t launch_linear8(const Ctx& c, const Linear8& x) {
   p.out_vec = x.out.ld % 4 == 0 && at(x.out.p, x.out.dtype == LAZYMAR_F32 ? 16 : 8);
   p.res_vec = x.residual.ld % 4 == 0 && at(x.residual.p, 16);
   const long long pair_tiles = (long long)((x.M + 255) / 256) * ((x.N + 255) / 256);
-  const int pairs = c.num_sms / 2;
-  cudaError_t e;
-  if (pair_tiles >= pairs) {
-    if ((e = prepare_linear8<true>()) != cudaSuccess) return e;
-    return launch_pdl_cluster(linear8_kernel<true>, dim3((unsigned)(2 * pairs)), dim3(THREADS), SMEM, 2, c.stream, ta, tb,
-                              to, tu, p, c.err);
-  }
-  const long long tiles = (long long)((x.M + 127) / 128) * ((x.N + 127) / 128);
-  if ((e = prepare_linear8<false>()) != cudaSuccess) return e;
-  return launch_pdl(linear8_kernel<false>, dim3((unsigned)(tiles < c.num_sms ? tiles : c.num_sms)), dim3(THREADS), SMEM,
-                    c.stream, ta, tb, to, tu, p, c.err);
+  if (pair_tiles >= c.num_sms / 2) return run_linear8<true>(c, ta, tb, to, tu, p, pair_tiles);
+  return run_linear8<false>(c, ta, tb, to, tu, p, (long long)((x.M + 127) / 128) * ((x.N + 127) / 128));
 }
 
 }  // namespace lm
