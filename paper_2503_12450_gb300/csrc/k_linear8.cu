@@ -33,7 +33,8 @@ constexpr uint32_t B_BYTES = 128 * KB_BYTES;  // rows of w in a CTA's shared mem
 constexpr uint32_t STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int EPI_WARPS = 8;
 constexpr uint32_t STG_BYTES = 32 * 128;      // one of a warp's two staging buffers: 32 rows of 128 bytes
-constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * STG_BYTES + 512;
+constexpr uint32_t SCALE_BYTES = 2 * 132 * 4;   // two groups' scales on their way between the scale warps
+constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * STG_BYTES + SCALE_BYTES + 512;
 constexpr int THREADS = 512;  // warps 0 TMA, 1 MMA, 4-7 scales, 8-15 epilogue
 // Registers: 512 threads launch with 128; the epilogue holds a row's 128 values.
 constexpr int REGS_EPI = 208, REGS_REST = 48;
@@ -152,7 +153,8 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
   uint8_t* sA = smem;
   uint8_t* sB = smem + STAGES * A_BYTES;
   uint8_t* sStg = smem + STAGES * STAGE_BYTES;
-  uint64_t* full = reinterpret_cast<uint64_t*>(sStg + EPI_WARPS * 2 * STG_BYTES);
+  uint8_t* sScale = sStg + EPI_WARPS * 2 * STG_BYTES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sScale + SCALE_BYTES);
   uint64_t* empty = full + STAGES;
   uint64_t* sf_full = empty + STAGES;
   uint64_t* sf_empty = sf_full + SF_SLOTS;
@@ -276,37 +278,60 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       }
     } else if (warp >= 4) {
       // ---------------- scales: global memory to tensor memory ----------------
-      const uint32_t lane_quarter = (uint32_t)((warp & 3) * 32) << 16;
-      const int nblk = (p.N + kBlk - 1) / kBlk;
-      int slot = 0;
-      uint32_t sf_phase = 0;
-      bool ok = true;
-      for (int tile = first; tile < tiles && ok; tile += step) {
-        const int m0 = (tile / num_n) * TM + rank * BM, b0 = (tile % num_n) * (TN / kBlk);
-        for (int kb0 = 0; kb0 < KB; kb0 += 4) {
-          uint32_t wa[4] = {0, 0, 0, 0}, wb[TN / kBlk];
+      // Each warp writes its own quarter of the lanes, and each quarter takes all
+      // of a group's scales (128 rows, four K blocks). So a warp fetches one K
+      // block, and they exchange them through shared memory, a 32-bit word a row.
+      // The bytes come from L2 or DRAM, and a group is due every four stages: they
+      // are fetched AHEAD groups early (fetched when due, the MMAs waited for
+      // scales a third of the time).
+      constexpr int AHEAD = 3, HALVES = TN / kBlk;
+      const int sw = warp & 3, nblk = (p.N + kBlk - 1) / kBlk, per_tile = (KB + 3) / 4;
+      const uint32_t lane_quarter = (uint32_t)(sw * 32) << 16;
+      uint8_t* const words = reinterpret_cast<uint8_t*>(sScale);  // [2][128 rows + HALVES][4]
+      uint32_t fa[AHEAD][4], fb[AHEAD];
+      int ftile = first, fgroup = 0;  // the next group to fetch
+      auto fetch = [&](uint32_t (&wa)[4], uint32_t& wb) {
+        if (ftile < tiles) {
+          const int kb = min(4 * fgroup + sw, KB - 1);
+          const int m0 = (ftile / num_n) * TM + rank * BM, b0 = (ftile % num_n) * HALVES;
+          const uint8_t* sa = p.a_scale + (size_t)kb * p.lds_a;
 #pragma unroll
-          for (int h = 0; h < TN / kBlk; ++h) wb[h] = 0;
-          const int here = min(4, KB - kb0);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (j < here) {
-              const uint8_t* sa = p.a_scale + (size_t)(kb0 + j) * p.lds_a;
-              const uint8_t* sw = p.w_scale + (size_t)(kb0 + j) * p.lds_w;
-#pragma unroll
-              for (int c = 0; c < 4; ++c) wa[c] |= (uint32_t)sa[min(m0 + 32 * c + lane, p.M - 1)] << (8 * j);
-#pragma unroll
-              for (int h = 0; h < TN / kBlk; ++h) wb[h] |= (uint32_t)sw[min(b0 + h, nblk - 1)] << (8 * j);
-            }
+          for (int c = 0; c < 4; ++c) wa[c] = sa[min(m0 + 32 * c + lane, p.M - 1)];
+          if (lane < HALVES) wb = p.w_scale[(size_t)kb * p.lds_w + min(b0 + lane, nblk - 1)];
+          if (++fgroup == per_tile) {
+            fgroup = 0;
+            ftile += step;
           }
-          const bool done = mbar_wait(&sf_empty[slot], sf_phase ^ 1u, abort_flag, err);
-          if (!__all_sync(0xffffffffu, done)) { ok = false; break; }
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) fa[i][c] = 127u;
+        fb[i] = 127u;
+        fetch(fa[i], fb[i]);
+      }
+      int slot = 0, half = 0;
+      uint32_t sf_phase = 0;
+      bool dead = false;  // a wait ran out: no more waits and writes, but the barrier below is kept
+      auto group = [&](uint32_t (&wa)[4], uint32_t& wb) {
+        uint8_t* const w = words + half * (128 + HALVES) * 4;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[(32 * c + lane) * 4 + sw] = (uint8_t)wa[c];
+        if (lane < HALVES) w[(128 + lane) * 4 + sw] = (uint8_t)wb;
+        fetch(wa, wb);
+        asm volatile("bar.sync 1, 128;" ::: "memory");  // the four scale warps
+        const uint32_t* r = reinterpret_cast<const uint32_t*>(w);
+        const uint32_t va[4] = {r[lane], r[32 + lane], r[64 + lane], r[96 + lane]};
+        half ^= 1;
+        if (!dead) dead = !__all_sync(0xffffffffu, mbar_wait(&sf_empty[slot], sf_phase ^ 1u, abort_flag, err));
+        if (!dead) {
           const uint32_t t = tmem_base + lane_quarter + SF_BASE + (uint32_t)(slot * 16);
           tc_fence_after();
-          tmem_st4(t, wa);
+          tmem_st4(t, va);
 #pragma unroll
-          for (int h = 0; h < TN / kBlk; ++h) {
-            const uint32_t w4[4] = {wb[h], wb[h], wb[h], wb[h]};
+          for (int h = 0; h < HALVES; ++h) {
+            const uint32_t v = r[128 + h], w4[4] = {v, v, v, v};
             tmem_st4(t + 4 + 4 * h, w4);
           }
           tmem_wait_st();
@@ -316,8 +341,15 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
             if (PAIR) mbar_arrive_cluster(cluster_map(smem_u32(&sf_full[slot]), 0));
             else mbar_arrive(&sf_full[slot]);
           }
-          if (++slot == SF_SLOTS) { slot = 0; sf_phase ^= 1u; }
         }
+        if (++slot == SF_SLOTS) { slot = 0; sf_phase ^= 1u; }
+      };
+      const int mine = first < tiles ? (tiles - first + step - 1) / step : 0;
+      const int groups = mine * per_tile;
+      for (int i = 0; i < groups; i += AHEAD) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+          if (i + j < groups) group(fa[j], fb[j]);
       }
     }
     __syncwarp();
