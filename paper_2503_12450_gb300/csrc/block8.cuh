@@ -101,6 +101,17 @@ __device__ __forceinline__ void block8_values(uint2 q, float s, float (&v)[8]) {
   f32x2_unpack(f32x2_mul(f32x2_pack(d.x, d.y), ss), v[6], v[7]);
 }
 
+// Arrives on a barrier of a CTA pair's even CTA for what this warp has written to,
+// or read from, its own CTA's shared or tensor memory (and fenced for the
+// asynchronous proxy or tcgen05). The MMA that the even CTA then issues touches it
+// through this SM's half alone, never through the other CTA's threads, so the
+// release need not reach beyond this CTA; one that does (release.cluster) waits
+// for every write of the warp that is under way, and held the weight gradient's
+// stages up by 0.3 us each.
+__device__ __forceinline__ void arrive_even(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_map(smem_u32(bar), 0)) : "memory");
+}
+
 // Tensors as the kernels take them. dtype LAZYMAR_F32 or LAZYMAR_BF16; vec:
 // rows start on boundaries of eight elements.
 struct Mat {

@@ -27,14 +27,15 @@ namespace l8 {
 
 constexpr int BM = 128;               // rows of a CTA's tile
 constexpr int KB_BYTES = 128;         // K of a pipeline stage: one scale block, one swizzle atom
-constexpr int STAGES = 5;
+constexpr int STAGES = 4;
 constexpr uint32_t A_BYTES = BM * KB_BYTES;
 constexpr uint32_t B_BYTES = 128 * KB_BYTES;  // rows of w in a CTA's shared memory: the tile's, or a pair's half
 constexpr uint32_t STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int EPI_WARPS = 8;
 constexpr uint32_t STG_BYTES = 32 * 128;      // one of a warp's two staging buffers: 32 rows of 128 bytes
 constexpr uint32_t SCALE_BYTES = 2 * 132 * 4;   // two groups' scales on their way between the scale warps
-constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * STG_BYTES + SCALE_BYTES + 512;
+constexpr uint32_t BIAS_BYTES = EPI_WARPS * 128 * 4;
+constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * STG_BYTES + BIAS_BYTES + SCALE_BYTES + 512;
 constexpr int THREADS = 512;  // warps 0 TMA, 1 MMA, 4-7 scales, 8-15 epilogue
 // Registers: 512 threads launch with 128; the epilogue holds a row's 128 values.
 constexpr int REGS_EPI = 208, REGS_REST = 48;
@@ -42,8 +43,14 @@ static_assert((REGS_EPI + REGS_REST) * 256 <= 128 * THREADS, "the register split
 // Kinds of output: fp32 or bf16; the same with a residual; 8-bit tensors (and
 // fp32 or bf16 next to them).
 enum { OUT_PLAIN = 0, OUT_RESIDUAL = 1, OUT_BLOCK8 = 2 };
-constexpr int SF_SLOTS = 4;           // scale slots of 16 tensor-memory columns: 4 of a, 8 of w
-constexpr uint32_t SF_BASE = 256;     // behind the accumulator's columns
+// Tensor memory: a pair's tile takes 256 columns, and two of them would leave
+// none for the scales. So they overlap by 32 columns: tile i starts at column 0
+// or 224 in turn, and its MMAs wait for the epilogue of tile i - 1 to have read
+// those 32 columns, which it reads first. Single tiles take 128 columns each.
+constexpr uint32_t ACC_SECOND = 224;
+constexpr int SF_SLOTS = 2;           // scale slots of 16 columns: 4 of a, 8 of w
+constexpr uint32_t SF_BASE = 480;     // behind the accumulators
+static_assert(ACC_SECOND + 256 <= SF_BASE && SF_BASE + 16 * SF_SLOTS <= 512, "tensor memory has 512 columns");
 
 struct Params {
   const uint8_t *a_scale, *w_scale;
@@ -138,9 +145,8 @@ __device__ __forceinline__ uint32_t quantize_row(const float (&v)[128], uint32_t
 // PAIR: two CTAs (a cluster of two) share a tile of 256 x 256, each its own 128
 // rows of a and half of the tile's rows of w; the even CTA issues the MMAs for
 // both. Otherwise tiles of 128 x 128 on single CTAs.
-// Accumulator: 256 columns, a pair's whole tile or two single tiles in turn. The
-// epilogue warps (two for each lane quarter, one for each 128 columns) take a
-// row's 128 columns into registers and hand the accumulator back at once.
+// The epilogue warps (two for each lane quarter, one for each 128 columns) take
+// a row's 128 columns into registers and hand the accumulator back at once.
 // OUT: what the epilogue writes, so that each kind has the registers it needs.
 template <bool PAIR, int OUT>
 __global__ void __launch_bounds__(l8::THREADS, 1)
@@ -153,14 +159,16 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
   uint8_t* sA = smem;
   uint8_t* sB = smem + STAGES * A_BYTES;
   uint8_t* sStg = smem + STAGES * STAGE_BYTES;
-  uint8_t* sScale = sStg + EPI_WARPS * 2 * STG_BYTES;
+  uint8_t* sBias = sStg + EPI_WARPS * 2 * STG_BYTES;
+  uint8_t* sScale = sBias + BIAS_BYTES;
   uint64_t* full = reinterpret_cast<uint64_t*>(sScale + SCALE_BYTES);
   uint64_t* empty = full + STAGES;
   uint64_t* sf_full = empty + STAGES;
   uint64_t* sf_empty = sf_full + SF_SLOTS;
   uint64_t* acc_full = sf_empty + SF_SLOTS;
   uint64_t* acc_empty = acc_full + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  uint64_t* lap = acc_empty + 2;  // the columns shared with the next tile are read (pairs)
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(lap + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -183,6 +191,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       mbar_init(&acc_full[b], 1);
       mbar_init(&acc_empty[b], PAIR ? 2 * EPI_WARPS : EPI_WARPS / 2);
     }
+    mbar_init(lap, EPI_WARPS);
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tmap(&tmA);
@@ -241,11 +250,12 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       uint32_t phase = 0, sf_phase = 0;
       bool ok = true;
       for (int tile = first; tile < tiles && ok; tile += step, ++it) {
-        const int buf = PAIR ? 0 : it & 1;
-        const uint32_t use = PAIR ? (uint32_t)it & 1u : (uint32_t)(it >> 1) & 1u;
+        const int buf = it & 1;
+        const uint32_t use = (uint32_t)(it >> 1) & 1u;
         if (!wait(&acc_empty[buf], use ^ 1u)) break;
+        if (PAIR && it > 0 && !wait(lap, (uint32_t)(it - 1) & 1u)) break;
         tc_fence_after();
-        const uint32_t d = tmem_base + (uint32_t)(buf * 128);
+        const uint32_t d = tmem_base + (uint32_t)buf * (PAIR ? ACC_SECOND : 128u);
         for (int kb = 0; kb < KB; ++kb) {
           if ((kb & 3) == 0 && !(ok = wait(&sf_full[slot], sf_phase))) break;
           if (!(ok = wait(&full[stage], phase))) break;
@@ -271,7 +281,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
         if (ok && lead) {
-          if (PAIR) umma_commit_pair(&acc_full[0]);
+          if (PAIR) umma_commit_pair(&acc_full[buf]);
           else umma_commit(&acc_full[buf]);
         }
         __syncwarp();
@@ -338,7 +348,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
-            if (PAIR) mbar_arrive_cluster(cluster_map(smem_u32(&sf_full[slot]), 0));
+            if (PAIR) arrive_even(&sf_full[slot]);
             else mbar_arrive(&sf_full[slot]);
           }
         }
@@ -357,12 +367,18 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
     // ---------------- epilogue ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
     const int quarter = warp & 3, unit = (warp - 8) >> 2;  // lane quarter, 128 columns of the accumulator
+    // A row's 128 values are taken 32 columns at a time from the rot-th 32 on, so
+    // that the columns that the next tile of a pair waits for come first: the last
+    // ones of the first tile, the first ones of the second.
+    const int rot = PAIR && unit == 1 ? 3 : 0;
     uint8_t* const stg2 = sStg + (warp - 8) * 2 * STG_BYTES;
+    float4* const bias = reinterpret_cast<float4*>(sBias) + (warp - 8) * 32;  // of the tile's 128 columns
     int flip = 0, it = 0;
     for (int tile = first; tile < tiles; tile += step, ++it) {
       // single CTAs: the tiles alternate between the two units
       if (!PAIR && (it & 1) != unit) continue;
-      const uint32_t use = PAIR ? (uint32_t)it & 1u : (uint32_t)(it >> 1) & 1u;
+      const int buf = it & 1;
+      const uint32_t use = (uint32_t)(it >> 1) & 1u;
       const int rbase = (tile / num_n) * TM + rank * BM + quarter * 32;
       const int n0 = (tile % num_n) * TN + (PAIR ? unit * 128 : 0);
       const int lr0 = lane >> 3, cq = lane & 7;  // row of four and 16-byte piece in the output passes
@@ -370,7 +386,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       // before the accumulator is ready
       float4 res[8];
       auto load_res = [&](int c) {
-        const int col = n0 + 32 * c + 4 * cq;
+        const int col = n0 + 32 * ((c + rot) & 3) + 4 * cq;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           const int r = rbase + 4 * q + lr0;
@@ -388,40 +404,60 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
         }
       };
       if (OUT == OUT_RESIDUAL) load_res(0);
-      const bool done = mbar_wait(&acc_full[PAIR ? 0 : unit], use, abort_flag, err);
+      if (p.bias) {
+        float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int col = n0 + 4 * lane;
+        if (p.bias_vec && col + 4 <= p.N) {
+          b = *reinterpret_cast<const float4*>(p.bias + col);
+        } else {
+          if (col < p.N) b.x = p.bias[col];
+          if (col + 1 < p.N) b.y = p.bias[col + 1];
+          if (col + 2 < p.N) b.z = p.bias[col + 2];
+          if (col + 3 < p.N) b.w = p.bias[col + 3];
+        }
+        __syncwarp();
+        bias[lane] = b;
+        __syncwarp();
+      }
+      const bool done = mbar_wait(&acc_full[buf], use, abort_flag, err);
       if (!__all_sync(0xffffffffu, done)) break;
       tc_fence_after();
       float v[128];
       {
-        const uint32_t t = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(unit * 128);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t r[32];
-          tmem_ld32(t + 32 * c, r);
-          tmem_wait_ld_regs(r);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[32 * c + i] = __uint_as_float(r[i]);
+        const uint32_t t = tmem_base + ((uint32_t)(quarter * 32) << 16) +
+                           (PAIR ? (uint32_t)buf * ACC_SECOND + (uint32_t)unit * 128u : (uint32_t)buf * 128u);
+        uint32_t r[4][32];
+        tmem_ld32(t + 32 * rot, r[0]);
+        tmem_wait_ld_regs(r[0]);
+        if (PAIR && unit != buf) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_even(lap);
         }
+#pragma unroll
+        for (int c = 1; c < 4; ++c) tmem_ld32(t + 32 * ((c + rot) & 3), r[c]);
+#pragma unroll
+        for (int c = 1; c < 4; ++c) tmem_wait_ld_regs(r[c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[32 * c + i] = __uint_as_float(r[c][i]);
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
-        if (PAIR) mbar_arrive_cluster(cluster_map(smem_u32(&acc_empty[0]), 0));
-        else mbar_arrive(&acc_empty[unit]);
+        if (PAIR) arrive_even(&acc_empty[buf]);
+        else mbar_arrive(&acc_empty[buf]);
       }
       if (n0 >= p.N || rbase >= p.M) continue;
       const int row = rbase + lane;
       if (p.bias) {
-        if (p.bias_vec && n0 + 128 <= p.N) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float4 b = *reinterpret_cast<const float4*>(p.bias + n0 + 4 * i);
-            v[4 * i] += b.x; v[4 * i + 1] += b.y; v[4 * i + 2] += b.z; v[4 * i + 3] += b.w;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (n0 + i < p.N) v[i] += p.bias[n0 + i];
+        for (int i = 0; i < 32; ++i) {
+          const float4 b = bias[(i + 8 * rot) & 31];
+          f32x2_unpack(f32x2_add(f32x2_pack(v[4 * i], v[4 * i + 1]), f32x2_pack(b.x, b.y)), v[4 * i], v[4 * i + 1]);
+          f32x2_unpack(f32x2_add(f32x2_pack(v[4 * i + 2], v[4 * i + 3]), f32x2_pack(b.z, b.w)), v[4 * i + 2],
+                       v[4 * i + 3]);
         }
       }
       // a row's 128 E4M3 bytes: staged with the TMA's 128-byte swizzle, one store
@@ -441,7 +477,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          *reinterpret_cast<uint4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+          *reinterpret_cast<uint4*>(stg + lane * 128 + ((((j + 2 * rot) & 7) ^ (lane & 7)) << 4)) =
               make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
         if (tma) {
           fence_proxy_async_smem();
@@ -479,8 +515,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
         __syncwarp();
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const int col = n0 + 32 * c + 4 * cq;
-          if (n0 + 32 * c >= p.N) break;
+          const int col = n0 + 32 * ((c + rot) & 3) + 4 * cq;
           uint8_t* stg = stg2 + (c & 1) * STG_BYTES;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
@@ -498,7 +533,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
             for (int q = 0; q < 8; ++q)
               o[q] = make_float4(o[q].x + res[q].x, o[q].y + res[q].y, o[q].z + res[q].z, o[q].w + res[q].w);
             // (other columns than those stored below, so in place is fine)
-            if (c < 3 && n0 + 32 * (c + 1) < p.N) load_res(c + 1);
+            if (c < 3) load_res(c + 1);
           }
 #pragma unroll
           for (int q = 0; q < 8; ++q) {

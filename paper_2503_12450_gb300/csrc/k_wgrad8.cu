@@ -71,15 +71,6 @@ __device__ __forceinline__ uint64_t desc(uint32_t saddr) {
          ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
 
-// Arrives on a barrier of the pair's even CTA for operand bytes that this
-// thread's warp has written and fenced for the asynchronous proxy in its own
-// shared memory. They are read by this SM's half of the MMA alone, never by the
-// other CTA's threads, so the release need not reach beyond this CTA; one that
-// does (release.cluster) waits for the SM's writes and held a stage up by 0.3 us.
-__device__ __forceinline__ void arrive_even(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_map(smem_u32(bar), 0)) : "memory");
-}
-
 }  // namespace w8
 
 // PAIR: two CTAs share a tile of 256 rows (n) by 256 columns (k) of dw: each its
@@ -324,7 +315,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if (PAIR) mbar_arrive_cluster(cluster_map(smem_u32(&acc_empty[buf]), 0));
+          if (PAIR) arrive_even(&acc_empty[buf]);
           else mbar_arrive(&acc_empty[buf]);
         }
         buf ^= 1;
