@@ -87,10 +87,9 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   uint8_t* sQ = smem + STAGES * 2 * OP_BYTES;
   uint8_t* sStg = smem + STAGES * STAGE_BYTES;
   float* sScale = reinterpret_cast<float*>(sStg + EPI_WARPS * STG_BYTES);
-  uint64_t* full_a = reinterpret_cast<uint64_t*>(sScale + STAGES * TOK);
-  uint64_t* full_q = full_a + STAGES;
-  uint64_t* full_b = full_q + STAGES;
-  uint64_t* empty = full_b + STAGES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sScale + STAGES * TOK);  // dy has come and x is converted
+  uint64_t* full_q = full + STAGES;
+  uint64_t* empty = full_q + STAGES;
   uint64_t* acc_full = empty + STAGES;
   uint64_t* acc_empty = acc_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
@@ -113,9 +112,8 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
-      mbar_init(&full_a[s], 1);
+      mbar_init(&full[s], 1 + (PAIR ? 2 * CONV_GROUP : CONV_GROUP));
       mbar_init(&full_q[s], 2);  // the bytes and the scales
-      mbar_init(&full_b[s], PAIR ? 2 * CONV_GROUP : CONV_GROUP);
       mbar_init(&empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -160,14 +158,14 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           mbar_arrive_expect_tx(&full_q[stage], Q_BYTES);
           tma_load_2d(&tmX, &full_q[stage], sQ + stage * Q_BYTES, t.k + rank * 128, m);
           if (PAIR) {
-            if (rank == 0) mbar_arrive_expect_tx(&full_a[stage], 2 * OP_BYTES);
-            const uint32_t bar = cluster_map(smem_u32(&full_a[stage]), 0);
+            if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * OP_BYTES);
+            const uint32_t bar = cluster_map(smem_u32(&full[stage]), 0);
             tma_load_2d_pair(&tmY, bar, dst, n, m);
             tma_load_2d_pair(&tmY, bar, dst + PIECE, n + 64, m);
           } else {
-            mbar_arrive_expect_tx(&full_a[stage], OP_BYTES);
-            tma_load_2d(&tmY, &full_a[stage], dst, n, m);
-            tma_load_2d(&tmY, &full_a[stage], dst + PIECE, n + 64, m);
+            mbar_arrive_expect_tx(&full[stage], OP_BYTES);
+            tma_load_2d(&tmY, &full[stage], dst, n, m);
+            tma_load_2d(&tmY, &full[stage], dst + PIECE, n + 64, m);
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
@@ -207,8 +205,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
         for (int s = 0; s < stages; ++s) {
           const bool fresh = s % CHUNK == 0, last = s % CHUNK == CHUNK - 1 || s == stages - 1;
           if (fresh && !(ok = all(mbar_wait(&acc_empty[buf], use ^ 1u, abort_flag, err)))) break;
-          if (!(ok = all(mbar_wait(&full_a[stage], phase, abort_flag, err)))) break;
-          if (!(ok = all(mbar_wait(&full_b[stage], phase, abort_flag, err)))) break;
+          if (!(ok = all(mbar_wait(&full[stage], phase, abort_flag, err)))) break;
           tc_fence_after();
           if (lead) {
             const uint64_t a0 = desc(smem_u32(sA + stage * OP_BYTES)), b0 = desc(smem_u32(sB + stage * OP_BYTES));
@@ -277,8 +274,8 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (PAIR) arrive_even(&full_b[stage]);
-            else mbar_arrive(&full_b[stage]);
+            if (PAIR) arrive_even(&full[stage]);
+            else mbar_arrive(&full[stage]);
           }
         }
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -365,25 +362,55 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   }
 }
 
-// dw (+)= sum of the splits' partial sums [split, N, K], in split order.
+// dw (+)= sum of the splits' partial sums [split, N, K], in split order. Threads
+// along a row, VEC columns each, and rows by CTA.
+template <int VEC>
 __global__ void __launch_bounds__(256) wgrad8_sum_kernel(const float* __restrict__ part, int split, float* dw, int lddw,
                                                          int N, int K, bool accumulate) {
+  const int col = ((int)blockIdx.x * 256 + (int)threadIdx.x) * VEC;
+  const size_t n = (size_t)N * K;
   pdl_wait();
   pdl_trigger();
-  const size_t n = (size_t)N * K;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
-    float s = 0.f;
+  if (col >= K) return;
+  for (int row = (int)blockIdx.y; row < N; row += (int)gridDim.y) {
+    const float* p = part + (size_t)row * K + col;
+    float* o = dw + (size_t)row * lddw + col;
+    float s[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s[i] = 0.f;
 #pragma unroll 4
-    for (int j = 0; j < split; ++j) s += part[(size_t)j * n + i];
-    float* o = dw + (i / K) * lddw + i % K;
-    *o = accumulate ? *o + s : s;
+    for (int j = 0; j < split; ++j) {
+      if constexpr (VEC == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p + (size_t)j * n);
+        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+      } else {
+        s[0] += p[(size_t)j * n];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) o[i] = accumulate ? o[i] + s[i] : s[i];
   }
+}
+
+cudaError_t wgrad8_sum(const Ctx& c, const float* part, int split, float* dw, int lddw, int N, int K, bool accumulate) {
+  const bool vec = K % 4 == 0;
+  const unsigned x = (unsigned)((K + 256 * (vec ? 4 : 1) - 1) / (256 * (vec ? 4 : 1))), y = (unsigned)(N < 4096 ? N : 4096);
+  return launch_pdl(vec ? wgrad8_sum_kernel<4> : wgrad8_sum_kernel<1>, dim3(x, y), dim3(256), 0, c.stream, part, split, dw,
+                    lddw, N, K, accumulate);
 }
 
 namespace {
 
 constexpr int kSMs = 152;
 
+// Tiles of 256 x 256 on pairs or 128 x 128 on single CTAs, and in how many parts
+// the tokens are summed, by the time that was measured: a stage of 64 tokens 0.42
+// us on a pair and 0.36 on a single CTA (a quarter of the work: its
+// short MMAs do not hide the stage's hand-over), 6 and 4 us for a launch, 1 us a
+// tile, and, if there are parts, 1 us and 0.35 us a MB of partial sums and result. (us
+// measured, pairs against single CTAs: 20480 x 4096 x 1024 142 : 242, 3211 x 1000 x 776
+// in 1, 2, 4 parts 26, 20, 17 : 22, 17, 18, 640 x 1024 x 256 10.6 : 7.5, 20480 x 1280 x 1280
+// in 1 and 3 parts 142, 63 : 122, 92.)
 struct Plan {
   bool pair;
   int split, per;
@@ -399,8 +426,8 @@ Plan plan_wgrad8(int M, int N, int K) {
       const long long per = (stages + split - 1) / split;
       if (split > 1 && (split - 1) * per >= stages) continue;  // an empty split
       const double rounds = (double)((tiles * split + slots - 1) / slots);
-      const double us = rounds * (per * (pair ? 0.36 : 0.20) + 2.0) +
-                        (split > 1 ? 3.0 + (2.0 * split + 1) * N * K * 4 / 4.5e6 : 0.0);
+      const double us = (pair ? 6.0 : 4.0) + rounds * (per * (pair ? 0.42 : 0.36) + 1.0) +
+                        (split > 1 ? 1.0 + 0.35e-6 * 4.0 * (split + 1) * N * K : 0.0);
       if (least == 0 || us < least) {
         least = us;
         best = Plan{pair != 0, split, (int)(per * w8::TOK)};
@@ -436,11 +463,9 @@ size_t wgrad8_workspace(int M, int N, int K) {
 cudaError_t launch_wgrad8(const Ctx& c, const Wgrad8& x) {
   using namespace w8;
   const size_t n = (size_t)x.N * x.K;
-  const unsigned sum_grid = (unsigned)((n + 255) / 256 < kSMs * 16 ? (n + 255) / 256 : kSMs * 16);
   if (x.M == 0) {
     if (x.accumulate) return cudaSuccess;
-    return launch_pdl(wgrad8_sum_kernel, dim3(sum_grid), dim3(256), 0, c.stream, (const float*)nullptr, 0, x.dw, x.lddw,
-                      x.N, x.K, false);
+    return wgrad8_sum(c, nullptr, 0, x.dw, x.lddw, x.N, x.K, false);
   }
   const Plan pl = plan_wgrad8(x.M, x.N, x.K);
   CUtensorMap ty, tx;
@@ -478,8 +503,7 @@ cudaError_t launch_wgrad8(const Ctx& c, const Wgrad8& x) {
     e = launch_pdl(wgrad8_kernel<false>, dim3(grid), dim3(THREADS), SMEM, c.stream, ty, tx, p, c.err);
   }
   if (e != cudaSuccess || pl.split == 1) return e;
-  return launch_pdl(wgrad8_sum_kernel, dim3(sum_grid), dim3(256), 0, c.stream, (const float*)x.ws, pl.split, x.dw, x.lddw,
-                    x.N, x.K, x.accumulate);
+  return wgrad8_sum(c, x.ws, pl.split, x.dw, x.lddw, x.N, x.K, x.accumulate);
 }
 
 }  // namespace lm
