@@ -52,6 +52,8 @@ constexpr int SF_SLOTS = 2;           // scale slots of 16 columns: 4 of a, 8 of
 constexpr uint32_t SF_BASE = 480;     // behind the accumulators
 static_assert(ACC_SECOND + 256 <= SF_BASE && SF_BASE + 16 * SF_SLOTS <= 512, "tensor memory has 512 columns");
 
+constexpr int kSplitCtas = 128;       // most CTAs of a launch that splits K
+
 struct Params {
   const uint8_t *a_scale, *w_scale;
   int lds_a, lds_w;
@@ -140,6 +142,37 @@ __device__ __forceinline__ uint32_t quantize_row(const float (&v)[128], uint32_t
   return byte;
 }
 
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(addr)
+               : "memory");
+  return v;
+}
+// A row's block of 128 columns, four a lane of the warp (those from N on are not
+// there), to E4M3 and its scale byte.
+__device__ __forceinline__ void put_row8(const float (&u)[4], uint8_t* q, uint8_t* scale, int col, int N) {
+  float x[4];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = col + i < N ? u[i] : 0.f;
+    const uint32_t b = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+    m = max(m, b < 0x7F800000u ? b : 0u);
+    x[i] = nonfinite_to(x[i], __uint_as_float(0x7FC00000u));
+  }
+  const uint32_t byte = block8_exp(__reduce_max_sync(0xffffffffu, m));
+  const float s = block8_inv(byte);
+  const uint32_t w = e4m3x4(x[0] * s, x[1] * s, x[2] * s, x[3] * s);
+  if (col + 4 <= N) {
+    *reinterpret_cast<uint32_t*>(q + col) = w;
+  } else {
+    for (int i = 0; col + i < N; ++i) q[col + i] = (uint8_t)(w >> (8 * i));
+  }
+  if ((threadIdx.x & 31) == 0) *scale = (uint8_t)byte;
+}
+
 }  // namespace l8
 
 // PAIR: two CTAs (a cluster of two) share a tile of 256 x 256, each its own 128
@@ -148,7 +181,11 @@ __device__ __forceinline__ uint32_t quantize_row(const float (&v)[128], uint32_t
 // The epilogue warps (two for each lane quarter, one for each 128 columns) take
 // a row's 128 columns into registers and hand the accumulator back at once.
 // OUT: what the epilogue writes, so that each kind has the registers it needs.
-template <bool PAIR, int OUT>
+// SPLIT (single CTAs): the CTAs of a cluster share a tile, each with a part of K.
+// They leave their partial sums in the shared memory that the operands have used,
+// and each finishes its share of the tile's rows, a row a warp: the sum over the
+// cluster through distributed shared memory, then every kind of output.
+template <bool PAIR, int OUT, bool SPLIT>
 __global__ void __launch_bounds__(l8::THREADS, 1)
     linear8_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmO8, const __grid_constant__ CUtensorMap tmU8,
@@ -174,9 +211,12 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int TM = PAIR ? 2 * BM : BM, TN = PAIR ? 256 : 128;
   const int num_n = (p.N + TN - 1) / TN, tiles = ((p.M + TM - 1) / TM) * num_n;
-  const int KB = (p.K + KB_BYTES - 1) / KB_BYTES;
+  const int all_kb = (p.K + KB_BYTES - 1) / KB_BYTES;
   const int rank = PAIR ? (int)cluster_ctarank() : 0;
-  const int first = PAIR ? (int)blockIdx.x / 2 : (int)blockIdx.x, step = PAIR ? (int)gridDim.x / 2 : (int)gridDim.x;
+  // CTAs that share a tile, this one's part of K: KB blocks from kb_first on
+  const int parts = SPLIT ? (int)cluster_nctarank() : 1, part = SPLIT ? (int)cluster_ctarank() : 0;
+  const int kb_first = SPLIT ? part * all_kb / parts : 0, KB = SPLIT ? (part + 1) * all_kb / parts - kb_first : all_kb;
+  const int ways = PAIR ? 2 : parts, first = (int)blockIdx.x / ways, step = (int)gridDim.x / ways;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -233,8 +273,8 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
             tma_load_2d_pair(&tmB, bar, db, kb * KB_BYTES, n0);
           } else {
             mbar_arrive_expect_tx(&full[stage], STAGE_BYTES);
-            tma_load_2d(&tmA, &full[stage], da, kb * KB_BYTES, m0);
-            tma_load_2d(&tmB, &full[stage], db, kb * KB_BYTES, n0);
+            tma_load_2d(&tmA, &full[stage], da, (kb_first + kb) * KB_BYTES, m0);
+            tma_load_2d(&tmB, &full[stage], db, (kb_first + kb) * KB_BYTES, n0);
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
@@ -302,7 +342,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       int ftile = first, fgroup = 0;  // the next group to fetch
       auto fetch = [&](uint32_t (&wa)[4], uint32_t& wb) {
         if (ftile < tiles) {
-          const int kb = min(4 * fgroup + sw, KB - 1);
+          const int kb = kb_first + min(4 * fgroup + sw, KB - 1);
           const int m0 = (ftile / num_n) * TM + rank * BM, b0 = (ftile % num_n) * HALVES;
           const uint8_t* sa = p.a_scale + (size_t)kb * p.lds_a;
 #pragma unroll
@@ -361,6 +401,27 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
         for (int j = 0; j < AHEAD; ++j)
           if (i + j < groups) group(fa[j], fb[j]);
       }
+    }
+    __syncwarp();
+  } else if constexpr (SPLIT) {
+    // ---------------- partial sums to shared memory ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
+    const int quarter = warp & 3, half = (warp - 8) >> 2;  // lane quarter, 64 of the tile's 128 columns
+    const bool done = mbar_wait(&acc_full[0], 0, abort_flag, err);
+    if (__all_sync(0xffffffffu, done)) {
+      tc_fence_after();
+      uint32_t r[2][32];
+      const uint32_t t = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 64);
+      tmem_ld32(t, r[0]);
+      tmem_ld32(t + 32, r[1]);
+      tmem_wait_ld_regs(r[0]);
+      tmem_wait_ld_regs(r[1]);
+      // (every load into the ring has been consumed) row of 512 bytes, 16-byte piece j at j ^ (row & 31)
+      uint8_t* row = smem + (quarter * 32 + lane) * 512;
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        *reinterpret_cast<uint4*>(row + (((16 * half + j) ^ lane) << 4)) =
+            make_uint4(r[j / 8][4 * (j % 8)], r[j / 8][4 * (j % 8) + 1], r[j / 8][4 * (j % 8) + 2], r[j / 8][4 * (j % 8) + 3]);
     }
     __syncwarp();
   } else {
@@ -568,6 +629,61 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
     if (lane == 0) bulk_wait_all();
     __syncwarp();
   }
+  if constexpr (SPLIT) {
+    cluster_sync();
+    if (warp >= 8) {
+      const int m0 = (first / num_n) * TM, n0 = (first % num_n) * TN, col = n0 + 4 * lane, each = BM / parts;
+      for (int r0 = warp - 8; r0 < each; r0 += EPI_WARPS) {
+        const int lr = part * each + r0, row = m0 + lr;
+        if (row >= p.M) break;
+        const uint32_t at = smem_u32(smem + lr * 512 + ((lane ^ (lr & 31)) << 4));
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < parts; ++k) {
+          const float4 x = ld_cluster_f4(cluster_map(at, (uint32_t)k));
+          v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+        }
+        float u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (col + i < p.N && p.bias) u[i] += p.bias[col + i];
+        if (p.u8) put_row8(u, p.u8 + (size_t)row * p.ldu8, p.u8_scale + (size_t)(n0 / kBlk) * p.lds_u8 + row, col, p.N);
+        if (p.epilogue == LAZYMAR_EPI_GELU) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) u[i] = gelu_erf(u[i]);
+        }
+        if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (col + i < p.N) u[i] += p.residual[(size_t)row * p.ldr + col + i];
+        }
+        if (p.out8)
+          put_row8(u, p.out8 + (size_t)row * p.ldout8, p.out8_scale + (size_t)(n0 / kBlk) * p.lds_out8 + row, col, p.N);
+        if (p.out && col < p.N) {
+          if (p.out_dtype == LAZYMAR_F32) {
+            float* y = static_cast<float*>(p.out) + (size_t)row * p.ldo + col;
+            if (p.out_vec && col + 4 <= p.N) {
+              *reinterpret_cast<float4*>(y) = make_float4(u[0], u[1], u[2], u[3]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (col + i < p.N) y[i] = u[i];
+            }
+          } else {
+            bf16* y = static_cast<bf16*>(p.out) + (size_t)row * p.ldo + col;
+            if (p.out_vec && col + 4 <= p.N) {
+              *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (col + i < p.N) y[i] = from_f<bf16>(u[i]);
+            }
+          }
+        }
+      }
+    }
+    __syncwarp();
+    cluster_sync();  // no CTA leaves while another may read its partial sums
+  }
   __syncthreads();
   if (PAIR) cluster_sync();
   if (warp == 1) {
@@ -581,11 +697,11 @@ namespace {
 
 // Once for each device: the shared-memory size, and the check that the launch
 // holds the registers that the kernel's warps share out.
-template <bool PAIR, int OUT>
+template <bool PAIR, int OUT, bool SPLIT>
 cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to,
-                        const CUtensorMap& tu, const l8::Params& p, long long tiles) {
+                        const CUtensorMap& tu, const l8::Params& p, long long tiles, int cluster) {
   using namespace l8;
-  const auto kernel = linear8_kernel<PAIR, OUT>;
+  const auto kernel = linear8_kernel<PAIR, OUT, SPLIT>;
   static int ready[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -597,19 +713,21 @@ cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& 
     if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM)) != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) ready[dev] = 1;
   }
-  const int slots = PAIR ? c.num_sms / 2 : c.num_sms;
-  const unsigned grid = (unsigned)(tiles < slots ? tiles : slots);
-  if (PAIR)
-    return launch_pdl_cluster(kernel, dim3(2 * grid), dim3(THREADS), SMEM, 2, c.stream, ta, tb, to, tu, p, c.err);
+  const int slots = c.num_sms / cluster;
+  const unsigned grid = (unsigned)((tiles < slots ? tiles : slots) * cluster);
+  if (cluster > 1)
+    return launch_pdl_cluster(kernel, dim3(grid), dim3(THREADS), SMEM, cluster, c.stream, ta, tb, to, tu, p, c.err);
   return launch_pdl(kernel, dim3(grid), dim3(THREADS), SMEM, c.stream, ta, tb, to, tu, p, c.err);
 }
 
 template <bool PAIR>
 cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to,
                         const CUtensorMap& tu, const l8::Params& p, long long tiles) {
-  if (p.out8 || p.u8) return run_linear8<PAIR, l8::OUT_BLOCK8>(c, ta, tb, to, tu, p, tiles);
-  if (p.epilogue == LAZYMAR_EPI_RESIDUAL) return run_linear8<PAIR, l8::OUT_RESIDUAL>(c, ta, tb, to, tu, p, tiles);
-  return run_linear8<PAIR, l8::OUT_PLAIN>(c, ta, tb, to, tu, p, tiles);
+  constexpr int CTAS = PAIR ? 2 : 1;
+  if (p.out8 || p.u8) return run_linear8<PAIR, l8::OUT_BLOCK8, false>(c, ta, tb, to, tu, p, tiles, CTAS);
+  if (p.epilogue == LAZYMAR_EPI_RESIDUAL)
+    return run_linear8<PAIR, l8::OUT_RESIDUAL, false>(c, ta, tb, to, tu, p, tiles, CTAS);
+  return run_linear8<PAIR, l8::OUT_PLAIN, false>(c, ta, tb, to, tu, p, tiles, CTAS);
 }
 
 }  // namespace
@@ -655,7 +773,13 @@ cudaError_t launch_linear8(const Ctx& c, const Linear8& x) {
   p.res_vec = x.residual.ld % 4 == 0 && at(x.residual.p, 16);
   const long long pair_tiles = (long long)((x.M + 255) / 256) * ((x.N + 255) / 256);
   if (pair_tiles >= c.num_sms / 2) return run_linear8<true>(c, ta, tb, to, tu, p, pair_tiles);
-  return run_linear8<false>(c, ta, tb, to, tu, p, (long long)((x.M + 127) / 128) * ((x.N + 127) / 128));
+  const long long tiles = (long long)((x.M + 127) / 128) * ((x.N + 127) / 128);
+  // Few tiles: K in parts of two blocks at least, one tile a cluster, as long as
+  // every cluster finds its SMs at once (a GPC holds two clusters of eight).
+  int parts = 8;
+  while (parts > 1 && (tiles * parts > kSplitCtas || x.K <= KB_BYTES * (2 * parts - 1))) parts /= 2;
+  if (parts > 1) return run_linear8<false, OUT_PLAIN, true>(c, ta, tb, to, tu, p, tiles, parts);
+  return run_linear8<false>(c, ta, tb, to, tu, p, tiles);
 }
 
 }  // namespace lm
