@@ -403,6 +403,10 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       }
     }
     __syncwarp();
+    if constexpr (SPLIT) {  // the epilogue's two meetings of the cluster
+      cluster_sync();
+      cluster_sync();
+    }
   } else if constexpr (SPLIT) {
     // ---------------- partial sums to shared memory ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
@@ -424,6 +428,61 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
             make_uint4(r[j / 8][4 * (j % 8)], r[j / 8][4 * (j % 8) + 1], r[j / 8][4 * (j % 8) + 2], r[j / 8][4 * (j % 8) + 3]);
     }
     __syncwarp();
+    // ---------------- this CTA's share of the rows ----------------
+    cluster_sync();
+    const int m0 = (first / num_n) * TM, n0 = (first % num_n) * TN, col = n0 + 4 * lane, each = BM / parts;
+#pragma unroll 2
+    for (int r0 = warp - 8; r0 < each; r0 += EPI_WARPS) {
+      const int lr = part * each + r0, row = m0 + lr;
+      if (row >= p.M) continue;
+      const uint32_t at = smem_u32(smem + lr * 512 + ((lane ^ (lr & 31)) << 4));
+      float4 x[8], v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)  // (all on their way before the first is used)
+        if (k < parts) x[k] = ld_cluster_f4(cluster_map(at, (uint32_t)k));
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < parts) v = make_float4(v.x + x[k].x, v.y + x[k].y, v.z + x[k].z, v.w + x[k].w);
+      float u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (col + i < p.N && p.bias) u[i] += p.bias[col + i];
+      if (p.u8) put_row8(u, p.u8 + (size_t)row * p.ldu8, p.u8_scale + (size_t)(n0 / kBlk) * p.lds_u8 + row, col, p.N);
+      if (p.epilogue == LAZYMAR_EPI_GELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = gelu_erf(u[i]);
+      }
+      if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (col + i < p.N) u[i] += p.residual[(size_t)row * p.ldr + col + i];
+      }
+      if (p.out8)
+        put_row8(u, p.out8 + (size_t)row * p.ldout8, p.out8_scale + (size_t)(n0 / kBlk) * p.lds_out8 + row, col, p.N);
+      if (p.out && col < p.N) {
+        if (p.out_dtype == LAZYMAR_F32) {
+          float* y = static_cast<float*>(p.out) + (size_t)row * p.ldo + col;
+          if (p.out_vec && col + 4 <= p.N) {
+            *reinterpret_cast<float4*>(y) = make_float4(u[0], u[1], u[2], u[3]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (col + i < p.N) y[i] = u[i];
+          }
+        } else {
+          bf16* y = static_cast<bf16*>(p.out) + (size_t)row * p.ldo + col;
+          if (p.out_vec && col + 4 <= p.N) {
+            *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (col + i < p.N) y[i] = from_f<bf16>(u[i]);
+          }
+        }
+      }
+    }
+    __syncwarp();
+    cluster_sync();  // no CTA leaves while another may read its partial sums
   } else {
     // ---------------- epilogue ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
@@ -629,61 +688,6 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
     if (lane == 0) bulk_wait_all();
     __syncwarp();
   }
-  if constexpr (SPLIT) {
-    cluster_sync();
-    if (warp >= 8) {
-      const int m0 = (first / num_n) * TM, n0 = (first % num_n) * TN, col = n0 + 4 * lane, each = BM / parts;
-      for (int r0 = warp - 8; r0 < each; r0 += EPI_WARPS) {
-        const int lr = part * each + r0, row = m0 + lr;
-        if (row >= p.M) break;
-        const uint32_t at = smem_u32(smem + lr * 512 + ((lane ^ (lr & 31)) << 4));
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < parts; ++k) {
-          const float4 x = ld_cluster_f4(cluster_map(at, (uint32_t)k));
-          v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
-        }
-        float u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (col + i < p.N && p.bias) u[i] += p.bias[col + i];
-        if (p.u8) put_row8(u, p.u8 + (size_t)row * p.ldu8, p.u8_scale + (size_t)(n0 / kBlk) * p.lds_u8 + row, col, p.N);
-        if (p.epilogue == LAZYMAR_EPI_GELU) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) u[i] = gelu_erf(u[i]);
-        }
-        if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (col + i < p.N) u[i] += p.residual[(size_t)row * p.ldr + col + i];
-        }
-        if (p.out8)
-          put_row8(u, p.out8 + (size_t)row * p.ldout8, p.out8_scale + (size_t)(n0 / kBlk) * p.lds_out8 + row, col, p.N);
-        if (p.out && col < p.N) {
-          if (p.out_dtype == LAZYMAR_F32) {
-            float* y = static_cast<float*>(p.out) + (size_t)row * p.ldo + col;
-            if (p.out_vec && col + 4 <= p.N) {
-              *reinterpret_cast<float4*>(y) = make_float4(u[0], u[1], u[2], u[3]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (col + i < p.N) y[i] = u[i];
-            }
-          } else {
-            bf16* y = static_cast<bf16*>(p.out) + (size_t)row * p.ldo + col;
-            if (p.out_vec && col + 4 <= p.N) {
-              *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]));
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (col + i < p.N) y[i] = from_f<bf16>(u[i]);
-            }
-          }
-        }
-      }
-    }
-    __syncwarp();
-    cluster_sync();  // no CTA leaves while another may read its partial sums
-  }
   __syncthreads();
   if (PAIR) cluster_sync();
   if (warp == 1) {
@@ -730,6 +734,43 @@ cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& 
   return run_linear8<PAIR, l8::OUT_PLAIN, false>(c, ta, tb, to, tu, p, tiles, CTAS);
 }
 
+// Tiles of 256 x 256 on pairs, of 128 x 128 on single CTAs, or of the latter with K
+// in parts, by the time that was measured (us): a pair's round 2.5 and 0.45 for each
+// 128 of K, a single CTA's 1 and 0.33 up to 12 of them, 0.65 after that (its ring then
+// waits for memory), a launch 4 and 5; parts cost 1 and 0.2 for each row a warp.
+// (Measured, pairs : single, N 4096, K 1024: M = 300 11.0 : 9.9, 1000 12.2 : 14.0, 2000 18.7 :
+// 21.5; N = K = 1280: 300 10.3 : 8.9 and 7.9 in four parts, 2000 11.0 : 13.0; N 1024, K 4096, M
+// = 300: 20.9 in one part, 10.6 in four.)
+struct Shape {
+  bool pair;
+  int parts;
+  long long tiles;
+};
+Shape choose(int sms, int M, int N, int K) {
+  const long long pair_tiles = (long long)((M + 255) / 256) * ((N + 255) / 256);
+  const long long tiles = (long long)((M + 127) / 128) * ((N + 127) / 128);
+  const int kb = (K + 127) / 128;
+  const auto rounds = [](long long t, int slots) { return (double)((t + slots - 1) / slots); };
+  const auto single = [](double k) { return k <= 12 ? 0.33 * k : 4.0 + 0.65 * (k - 12); };
+  Shape best{true, 1, pair_tiles};
+  double least = 4.0 + rounds(pair_tiles, sms / 2) * (2.5 + 0.45 * kb);
+  const double one = 5.0 + rounds(tiles, sms) * (1.0 + single(kb));
+  if (one < least) {
+    least = one;
+    best = Shape{false, 1, tiles};
+  }
+  // parts of two blocks at least, one tile a cluster, and every cluster finds its
+  // SMs at once (a GPC holds two clusters of eight)
+  for (int parts = 2; parts <= 8 && tiles * parts <= l8::kSplitCtas && kb >= 2 * parts; parts *= 2) {
+    const double us = 5.0 + 2.0 + 0.2 * (16 / parts) + single((double)kb / parts);
+    if (us < least) {
+      least = us;
+      best = Shape{false, parts, tiles};
+    }
+  }
+  return best;
+}
+
 }  // namespace
 
 cudaError_t launch_linear8(const Ctx& c, const Linear8& x) {
@@ -771,15 +812,10 @@ cudaError_t launch_linear8(const Ctx& c, const Linear8& x) {
   p.bias_vec = at(x.bias, 16);
   p.out_vec = x.out.ld % 4 == 0 && at(x.out.p, x.out.dtype == LAZYMAR_F32 ? 16 : 8);
   p.res_vec = x.residual.ld % 4 == 0 && at(x.residual.p, 16);
-  const long long pair_tiles = (long long)((x.M + 255) / 256) * ((x.N + 255) / 256);
-  if (pair_tiles >= c.num_sms / 2) return run_linear8<true>(c, ta, tb, to, tu, p, pair_tiles);
-  const long long tiles = (long long)((x.M + 127) / 128) * ((x.N + 127) / 128);
-  // Few tiles: K in parts of two blocks at least, one tile a cluster, as long as
-  // every cluster finds its SMs at once (a GPC holds two clusters of eight).
-  int parts = 8;
-  while (parts > 1 && (tiles * parts > kSplitCtas || x.K <= KB_BYTES * (2 * parts - 1))) parts /= 2;
-  if (parts > 1) return run_linear8<false, OUT_PLAIN, true>(c, ta, tb, to, tu, p, tiles, parts);
-  return run_linear8<false>(c, ta, tb, to, tu, p, tiles);
+  const Shape shape = choose(c.num_sms, x.M, x.N, x.K);
+  if (shape.pair) return run_linear8<true>(c, ta, tb, to, tu, p, shape.tiles);
+  if (shape.parts > 1) return run_linear8<false, OUT_PLAIN, true>(c, ta, tb, to, tu, p, shape.tiles, shape.parts);
+  return run_linear8<false>(c, ta, tb, to, tu, p, shape.tiles);
 }
 
 }  // namespace lm
