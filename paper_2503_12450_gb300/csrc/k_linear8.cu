@@ -27,7 +27,6 @@ namespace l8 {
 
 constexpr int BM = 128;               // rows of a CTA's tile
 constexpr int KB_BYTES = 128;         // K of a pipeline stage: one scale block, one swizzle atom
-constexpr int STAGES = 4;
 constexpr uint32_t A_BYTES = BM * KB_BYTES;
 constexpr uint32_t B_BYTES = 128 * KB_BYTES;  // rows of w in a CTA's shared memory: the tile's, or a pair's half
 constexpr uint32_t STAGE_BYTES = A_BYTES + B_BYTES;
@@ -35,7 +34,13 @@ constexpr int EPI_WARPS = 8;
 constexpr uint32_t STG_BYTES = 32 * 128;      // one of a warp's two staging buffers: 32 rows of 128 bytes
 constexpr uint32_t SCALE_BYTES = 2 * 132 * 4;   // two groups' scales on their way between the scale warps
 constexpr uint32_t BIAS_BYTES = EPI_WARPS * 128 * 4;
-constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * STG_BYTES + BIAS_BYTES + SCALE_BYTES + 512;
+// Pipeline stages and a warp's staging buffers: 8-bit outputs leave from two
+// buffers in turn, the others from one, which makes room for a stage.
+constexpr int stages(int out) { return out == 2 ? 4 : 5; }
+constexpr int buffers(int out) { return out == 2 ? 2 : 1; }
+constexpr size_t smem_bytes(int out) {
+  return 1024 + stages(out) * STAGE_BYTES + EPI_WARPS * buffers(out) * STG_BYTES + BIAS_BYTES + SCALE_BYTES + 512;
+}
 constexpr int THREADS = 512;  // warps 0 TMA, 1 MMA, 4-7 scales, 8-15 epilogue
 // Registers: 512 threads launch with 128; the epilogue holds a row's 128 values.
 constexpr int REGS_EPI = 208, REGS_REST = 48;
@@ -193,10 +198,11 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
   using namespace l8;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  constexpr int STAGES = stages(OUT), BUFFERS = buffers(OUT);
   uint8_t* sA = smem;
   uint8_t* sB = smem + STAGES * A_BYTES;
   uint8_t* sStg = smem + STAGES * STAGE_BYTES;
-  uint8_t* sBias = sStg + EPI_WARPS * 2 * STG_BYTES;
+  uint8_t* sBias = sStg + EPI_WARPS * BUFFERS * STG_BYTES;
   uint8_t* sScale = sBias + BIAS_BYTES;
   uint64_t* full = reinterpret_cast<uint64_t*>(sScale + SCALE_BYTES);
   uint64_t* empty = full + STAGES;
@@ -491,7 +497,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
     // that the columns that the next tile of a pair waits for come first: the last
     // ones of the first tile, the first ones of the second.
     const int rot = PAIR && unit == 1 ? 3 : 0;
-    uint8_t* const stg2 = sStg + (warp - 8) * 2 * STG_BYTES;
+    uint8_t* const stg2 = sStg + (warp - 8) * BUFFERS * STG_BYTES;
     float4* const bias = reinterpret_cast<float4*>(sBias) + (warp - 8) * 32;  // of the tile's 128 columns
     int flip = 0, it = 0;
     for (int tile = first; tile < tiles; tile += step, ++it) {
@@ -636,7 +642,8 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const int col = n0 + 32 * ((c + rot) & 3) + 4 * cq;
-          uint8_t* stg = stg2 + (c & 1) * STG_BYTES;
+          uint8_t* stg = stg2 + (c % BUFFERS) * STG_BYTES;
+          if (BUFFERS == 1) __syncwarp();  // the columns before have been read
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             *reinterpret_cast<float4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) =
@@ -706,6 +713,7 @@ cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& 
                         const CUtensorMap& tu, const l8::Params& p, long long tiles, int cluster) {
   using namespace l8;
   const auto kernel = linear8_kernel<PAIR, OUT, SPLIT>;
+  constexpr size_t smem = smem_bytes(OUT);
   static int ready[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -714,14 +722,14 @@ cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& 
     cudaFuncAttributes a;
     if ((e = cudaFuncGetAttributes(&a, kernel)) != cudaSuccess) return e;
     if (a.numRegs * THREADS < (REGS_EPI + REGS_REST) * 256) return cudaErrorInvalidConfiguration;
-    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM)) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) ready[dev] = 1;
   }
   const int slots = c.num_sms / cluster;
   const unsigned grid = (unsigned)((tiles < slots ? tiles : slots) * cluster);
   if (cluster > 1)
-    return launch_pdl_cluster(kernel, dim3(grid), dim3(THREADS), SMEM, cluster, c.stream, ta, tb, to, tu, p, c.err);
-  return launch_pdl(kernel, dim3(grid), dim3(THREADS), SMEM, c.stream, ta, tb, to, tu, p, c.err);
+    return launch_pdl_cluster(kernel, dim3(grid), dim3(THREADS), smem, cluster, c.stream, ta, tb, to, tu, p, c.err);
+  return launch_pdl(kernel, dim3(grid), dim3(THREADS), smem, c.stream, ta, tb, to, tu, p, c.err);
 }
 
 template <bool PAIR>
