@@ -1,0 +1,121 @@
+"""The training operators together: the MLP half of a block against fp64, its
+gradient against differences of the function that it computes, and the example."""
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+
+from oracle import training as T
+from _gpu import torch_cuda
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def _params(D, H, seed):
+    r = np.random.default_rng(seed)
+    n = lambda *s: r.standard_normal(s)  # noqa: E731
+    return dict(ln_g=1 + 0.1 * n(D), ln_b=0.02 * n(D), w1=n(H, D) / np.sqrt(D), b1=0.02 * n(H), w2=n(D, H) / np.sqrt(H),
+                b2=0.02 * n(D))
+
+
+def _exact(p, x, dy):
+    """y, dx and the parameters' gradients in fp64, with nothing rounded to 8 bits."""
+    h, mean, rstd = T.layernorm(x, p["ln_g"], p["ln_b"], 1e-6)
+    u = h @ p["w1"].T + p["b1"]
+    a = T.gelu(u)
+    y = x + a @ p["w2"].T + p["b2"]
+    du = (dy @ p["w2"]) * T.gelu_grad(u)
+    dx, dg, db = T.layernorm_grad(du @ p["w1"], x, mean, rstd, p["ln_g"])
+    return y, dx + dy, dict(ln_g=dg, ln_b=db, w1=du.T @ h, b1=du.sum(0), w2=dy.T @ a, b2=dy.sum(0))
+
+
+def _block(p):
+    torch = torch_cuda()
+    from paper_2503_12450_gb300.mlp_block8 import MlpBlock8
+    return MlpBlock8({k: torch.from_numpy(v.astype(np.float32)).cuda() for k, v in p.items()})
+
+
+@pytest.mark.parametrize("M,D,H", [(1, 128, 512), (333, 200, 800), (1500, 256, 1024), (64, 777, 1554)])
+def test_mlp_block_against_fp64(M, D, H):
+    """Every 8-bit tensor is off by at most 2^-4 of each element, about 2^-4 / sqrt(3) of its norm where the errors are
+    independent; a result passes through at most six such tensors, so its norm is off by at most
+    sqrt(6) 2^-4 / sqrt(3) < 9 %. y and dx carry the residual stream in fp32 besides."""
+    torch = torch_cuda()
+    p = _params(D, H, 1)
+    r = np.random.default_rng(M)
+    x, dy = r.standard_normal((M, D)), 1e-3 * r.standard_normal((M, D))
+    x, dy = x.astype(np.float32).astype(float), dy.astype(np.float32).astype(float)
+    b = _block(p)
+    y = b.forward(torch.from_numpy(x.astype(np.float32)).cuda())
+    dx = b.backward(torch.from_numpy(dy.astype(np.float32)).cuda())
+    torch.cuda.synchronize()
+    wy, wdx, wg = _exact(p, x, dy)
+    off = lambda a, w: np.linalg.norm(a.double().cpu().numpy() - w) / np.linalg.norm(w)  # noqa: E731
+    assert off(y, wy) < 0.09 and off(dx, wdx) < 0.09
+    for k, w in wg.items():
+        assert off(b.grads[k], w) < 0.09, k
+    # serving the same rows keeps nothing and gives the same
+    s = b.forward(torch.from_numpy(x.astype(np.float32)).cuda(), train=False)
+    assert torch.equal(s, y)
+    # accumulation adds a second pass's gradients
+    first = {k: v.clone() for k, v in b.grads.items()}
+    b.forward(torch.from_numpy(x.astype(np.float32)).cuda())
+    b.backward(torch.from_numpy(dy.astype(np.float32)).cuda(), accumulate=True)
+    for k, v in b.grads.items():
+        assert torch.equal(v, first[k] + first[k]), k
+
+
+def test_mlp_block_gradient_against_differences():
+    """The directional derivative of the loss along the gradient, by differences of the forward pass itself: rounding to
+    8 bits makes the loss a staircase, so the step is large against a stair and the agreement that of its noise."""
+    torch = torch_cuda()
+    D, H, M = 256, 1024, 2048
+    p = _params(D, H, 5)
+    b = _block(p)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x, t = (torch.randn((M, D), device="cuda", generator=g) for _ in range(2))
+
+    def loss():
+        return float(((b.forward(x) - t).double() ** 2).sum() / 2)
+    y = b.forward(x)
+    b.backward(y - t)
+    for k in ("w1", "w2", "b1", "ln_g"):
+        d = b.grads[k].clone()
+        slope = float((d.double() ** 2).sum())
+        h = 0.1 * float(b.p[k].norm() / d.norm())
+        keep = b.p[k].clone()
+        b.p[k].copy_(keep + h * d)
+        b.pack()
+        up = loss()
+        b.p[k].copy_(keep - h * d)
+        b.pack()
+        down = loss()
+        b.p[k].copy_(keep)
+        b.pack()
+        got = (up - down) / (2 * h)
+        # the third-order term of a 10 % step and the 8-bit noise of two losses
+        assert abs(got - slope) < 0.15 * slope, (k, got, slope)
+
+
+def test_example_learns():
+    torch_cuda()
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    try:
+        import tune_mlp
+    finally:
+        sys.path.pop(0)
+    losses, student, _ = tune_mlp.tune(256, 2048, 25)
+    assert losses[-1] < 0.5 * losses[0] and all(np.isfinite(losses))
+    assert student.saved_bytes() < 0.53 * 4 * 2048 * (256 + 1024)
+
+
+def test_example_runs_from_the_command_line():
+    torch_cuda()
+    r = subprocess.run([sys.executable, os.path.join(ROOT, "examples", "tune_mlp.py"), "--width", "256", "--rows", "640",
+                        "--steps", "4"], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert "ms a step" in r.stdout and "8 bits" in r.stdout
