@@ -101,6 +101,35 @@ __device__ __forceinline__ void block8_values(uint2 q, float s, float (&v)[8]) {
   f32x2_unpack(f32x2_mul(f32x2_pack(d.x, d.y), ss), v[6], v[7]);
 }
 
+// GELU in the erf form for the 8-bit product's epilogues: gelu_erf of
+// lazymar_internal.cuh with a tail polynomial of degree 6 (csrc/gen_gelu_poly.py),
+// within 1.1e-7 max(1, |x|) instead of 2.8e-7, which moves fewer values over an
+// E4M3 rounding boundary, for one more paired instruction.
+__device__ __forceinline__ void gelu_erf6_x2(float& x0, float& x1) {
+  constexpr float kGelu6P0 = -9.999947548e-01f;
+  constexpr float kGelu6P1 = -1.151182413e+00f;
+  constexpr float kGelu6P2 = -4.588403106e-01f;
+  constexpr float kGelu6P3 = -5.330511183e-02f;
+  constexpr float kGelu6P4 = 8.002257906e-03f;
+  constexpr float kGelu6P5 = -7.424726500e-04f;
+  constexpr float kGelu6P6 = 2.970655623e-05f;
+  // in v = -min(|x|, 6): the odd coefficients change sign
+  const float v0 = fmaxf(-fabsf(x0), -6.0f), v1 = fmaxf(-fabsf(x1), -6.0f);
+  const unsigned long long v = f32x2_pack(v0, v1);
+  unsigned long long p = f32x2_fma(f32x2_pack(kGelu6P6, kGelu6P6), v, f32x2_pack(-kGelu6P5, -kGelu6P5));
+  p = f32x2_fma(p, v, f32x2_pack(kGelu6P4, kGelu6P4));
+  p = f32x2_fma(p, v, f32x2_pack(-kGelu6P3, -kGelu6P3));
+  p = f32x2_fma(p, v, f32x2_pack(kGelu6P2, kGelu6P2));
+  p = f32x2_fma(p, v, f32x2_pack(-kGelu6P1, -kGelu6P1));
+  p = f32x2_fma(p, v, f32x2_pack(kGelu6P0, kGelu6P0));
+  float p0, p1;
+  f32x2_unpack(p, p0, p1);
+  const unsigned long long h = f32x2_pack(exp2_approx(p0), exp2_approx(p1));
+  const unsigned long long half = f32x2_mul(f32x2_add(f32x2_pack(x0, x1), f32x2_pack(fabsf(x0), fabsf(x1))),
+                                            f32x2_pack(0.5f, 0.5f));
+  f32x2_unpack(f32x2_fma(v, h, half), x0, x1);
+}
+
 // Arrives on a barrier of a CTA pair's even CTA for what this warp has written to,
 // or read from, its own CTA's shared or tensor memory (and fenced for the
 // asynchronous proxy or tcgen05). The MMA that the even CTA then issues touches it

@@ -455,8 +455,8 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
         if (col + i < p.N && p.bias) u[i] += p.bias[col + i];
       if (p.u8) put_row8(u, p.u8 + (size_t)row * p.ldu8, p.u8_scale + (size_t)(n0 / kBlk) * p.lds_u8 + row, col, p.N);
       if (p.epilogue == LAZYMAR_EPI_GELU) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = gelu_erf(u[i]);
+        gelu_erf6_x2(u[0], u[1]);
+        gelu_erf6_x2(u[2], u[3]);
       }
       if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
 #pragma unroll
@@ -631,7 +631,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       if (OUT == OUT_BLOCK8 && p.u8) put8(&tmU8, p.u8, p.ldu8, p.u8_scale, p.lds_u8);
       if (OUT != OUT_RESIDUAL && p.epilogue == LAZYMAR_EPI_GELU) {
 #pragma unroll
-        for (int i = 0; i < 64; ++i) gelu_erf_x2(v[2 * i], v[2 * i + 1]);
+        for (int i = 0; i < 64; ++i) gelu_erf6_x2(v[2 * i], v[2 * i + 1]);
       }
       if (OUT == OUT_BLOCK8 && p.out8) put8(&tmO8, p.out8, p.ldout8, p.out8_scale, p.lds_out8);
       if (p.out) {

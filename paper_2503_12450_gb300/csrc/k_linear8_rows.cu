@@ -156,9 +156,13 @@ __global__ void __launch_bounds__(kWarps * 32) linear8_rows_kernel(const RowsPar
       for (int k = 0; k < kWarps; ++k) s += part[k][m][c];
       if (p.bias) s += p.bias[n];
       u[e] = s;
-      y[e] = p.epilogue == LAZYMAR_EPI_GELU       ? gelu_erf(s)
-             : p.epilogue == LAZYMAR_EPI_RESIDUAL ? s + p.residual[(size_t)m * p.ldr + n]
-                                                  : s;
+      y[e] = s;
+      if (p.epilogue == LAZYMAR_EPI_GELU) {
+        float other = s;
+        gelu_erf6_x2(y[e], other);
+      } else if (p.epilogue == LAZYMAR_EPI_RESIDUAL) {
+        y[e] += p.residual[(size_t)m * p.ldr + n];
+      }
       if (p.out) {
         if (p.out_dtype == LAZYMAR_F32) static_cast<float*>(p.out)[(size_t)m * p.ldo + n] = y[e];
         else static_cast<bf16*>(p.out)[(size_t)m * p.ldo + n] = from_f<bf16>(y[e]);

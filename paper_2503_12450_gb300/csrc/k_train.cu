@@ -501,17 +501,17 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
 // Any width, stride and alignment: WPR warps a row, NC chunks of 256 columns a
 // warp, every 32nd column of a chunk a lane (so that a warp's accesses are
 // contiguous without a boundary), dy and x in registers.
-template <typename T>
-__device__ __forceinline__ void ld8s(const T* row, int c0, int D, float (&v)[8]) {
+// A row's elements as loaded, widened at their use: the next row is under way in
+// registers while this one is worked on (and a use would wait for it).
+__device__ __forceinline__ void ld8s(const Mat& m, size_t row, int c0, int D, uint32_t (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int c = c0 + 32 * i + (int)(threadIdx.x & 31);
-    v[i] = c < D ? to_f(row[c]) : 0.f;
+    v[i] = 0u;
+    if (c < D)
+      v[i] = m.dtype == LAZYMAR_F32 ? static_cast<const uint32_t*>(m.p)[row * m.ld + c]
+                                    : static_cast<const uint16_t*>(m.p)[row * m.ld + c];
   }
-}
-__device__ __forceinline__ void ld8s(const Mat& m, size_t row, int c0, int D, float (&v)[8]) {
-  if (m.dtype == LAZYMAR_F32) ld8s(static_cast<const float*>(m.p) + row * m.ld, c0, D, v);
-  else ld8s(static_cast<const bf16*>(m.p) + row * m.ld, c0, D, v);
 }
 template <int NC, int WPR>
 __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_backward_kernel(const LnBackward p) {
@@ -520,6 +520,7 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_
   __shared__ float red[2][2][GROUPS][WPR];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
   const int D = p.D, c0 = part * NC * kChunk;
+  const int dy_shift = p.dy.dtype == LAZYMAR_F32 ? 0 : 16, x_shift = p.x.dtype == LAZYMAR_F32 ? 0 : 16;
   pdl_wait();
   pdl_trigger();
   float dg[NC][8], db[NC][8];
@@ -528,33 +529,51 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_
 #pragma unroll
     for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.f;
   const int stride = (int)gridDim.x * GROUPS;
+  uint32_t ry[NC][8], rx[NC][8], rs[NC][2];
+  float rmean = 0.f, rrstd = 0.f;
+  auto fetch = [&](long long row) {
+    if (row >= p.M) return;
+    rmean = p.mean[row];
+    rrstd = p.rstd[row];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int cc = c0 + c * kChunk;
+      ld8s(p.dy, (size_t)row, cc, D, ry[c]);
+      if (p.x.p) {
+        ld8s(p.x, (size_t)row, cc, D, rx[c]);
+      } else {
+        const uint8_t* q = static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq;
+        const int blk = min(cc, D - 1) / kBlk, more = cc + kBlk < D ? 1 : 0;  // the chunk's blocks
+        rs[c][0] = p.x8.scale[(size_t)blk * p.x8.lds + row];
+        rs[c][1] = p.x8.scale[(size_t)(blk + more) * p.x8.lds + row];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int k = cc + 32 * i + lane;
+          rx[c][i] = k < D ? q[k] : 0u;
+        }
+      }
+    }
+  };
   int it = 0;
+  fetch((long long)blockIdx.x * GROUPS + grp);
   // (every warp makes the same number of rounds: the row sums are a CTA-wide step)
   for (long long base = (long long)blockIdx.x * GROUPS; base < p.M; base += stride, it ^= 1) {
     const long long row = base + grp;
     const bool live = row < p.M;
     float h[NC][8], a[NC][8], s1 = 0.f, s2 = 0.f, rstd = 0.f;
     if (live) {
-      const float mean = p.mean[row];
-      rstd = p.rstd[row];
+      const float mean = rmean;
+      rstd = rrstd;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const int cc = c0 + c * kChunk;
-        ld8s(p.dy, row, cc, D, a[c]);
-        if (p.x.p) {
-          ld8s(p.x, row, cc, D, h[c]);
-        } else {
-          const uint8_t* q = static_cast<const uint8_t*>(p.x8.q) + (size_t)row * p.x8.ldq;
-          const int blk = min(cc, D - 1) / kBlk, more = cc + kBlk < D ? 1 : 0;  // the chunk's blocks
-          const float sc[2] = {block8_scale(p.x8.scale[(size_t)blk * p.x8.lds + row]),
-                               block8_scale(p.x8.scale[(size_t)(blk + more) * p.x8.lds + row])};
+        const float sc[2] = {block8_scale(rs[c][0]), block8_scale(rs[c][1])};
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int k = cc + 32 * i + lane;
-            h[c][i] = e4m3x2_to_f2(k < D ? q[k] : 0u).x * sc[i >> 2];
-          }
+        for (int i = 0; i < 8; ++i) {
+          a[c][i] = __uint_as_float(ry[c][i] << dy_shift);
+          h[c][i] = p.x.p ? __uint_as_float(rx[c][i] << x_shift) : e4m3x2_to_f2(rx[c][i]).x * sc[i >> 2];
         }
       }
+      fetch(row + stride);
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
 #pragma unroll
@@ -971,7 +990,6 @@ cudaError_t launch_ln_backward(const Ctx& c, const LnBackward& p) {
     e = nc <= 1    ? ln_backward_run<1, 1>(c, p, &ctas)
         : nc <= 2  ? ln_backward_run<2, 1>(c, p, &ctas)
         : nc <= 4  ? ln_backward_run<2, 2>(c, p, &ctas)
-        : nc <= 6  ? ln_backward_run<3, 2>(c, p, &ctas)
         : nc <= 8  ? ln_backward_run<2, 4>(c, p, &ctas)
         : nc <= 16 ? ln_backward_run<2, 8>(c, p, &ctas)
                    : ln_backward_run<2, 16>(c, p, &ctas);

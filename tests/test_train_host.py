@@ -1,6 +1,7 @@
 """The training operators without a GPU: the oracle's pins (format, gradients
 against differences), exports, and the argument checks that need no device."""
 import ctypes
+import importlib.util
 import os
 import re
 
@@ -82,6 +83,20 @@ def test_layernorm_gradient_against_differences():
 def test_gelu_gradient_against_differences():
     x = np.linspace(-8, 8, 161)
     np.testing.assert_allclose(T.gelu_grad(x), (T.gelu(x + 1e-5) - T.gelu(x - 1e-5)) / 2e-5, atol=1e-9)
+
+
+def test_gelu_polynomial_of_degree_six_within_its_bound():
+    """The constants compiled into the 8-bit product's GELU, in the kernels' order of fp32 operations."""
+    special = pytest.importorskip("scipy.special")
+    csrc = os.path.join(ROOT, "paper_2503_12450_gb300", "csrc")
+    found = dict(re.findall(r"constexpr float kGelu6P(\d) = ([-+0-9.eE]+)f;", open(os.path.join(csrc, "block8.cuh")).read()))
+    c = np.array([np.float32(found[str(k)]) for k in range(7)])
+    spec = importlib.util.spec_from_file_location("gen_gelu_poly", os.path.join(csrc, "gen_gelu_poly.py"))
+    gen = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(gen)
+    x = np.linspace(-12, 12, 200001).astype(np.float32)
+    ref = 0.5 * x.astype(np.float64) * (1.0 + special.erf(x.astype(np.float64) / np.sqrt(2.0)))
+    assert (np.abs(gen.gelu_fp32(x, c) - ref) <= 1.1e-7 * np.maximum(1.0, np.abs(x))).all()
 
 
 # --------------------------------------------------------------------------
