@@ -36,13 +36,19 @@ constexpr int TOK = 64;               // tokens of a pipeline stage
 constexpr int STAGES = 4;
 constexpr uint32_t PIECE = TOK * 128; // 64 columns of a stage, in bytes
 constexpr uint32_t OP_BYTES = 2 * PIECE;  // 128 columns of an operand
-constexpr uint32_t Q_BYTES = TOK * 128;   // the checkpoint's bytes behind it
-constexpr uint32_t STAGE_BYTES = 2 * OP_BYTES + Q_BYTES;
+// The checkpoint's bytes have a ring of their own, deeper than the operands':
+// they are loaded long before the converters get to them, so that an operand
+// stage that falls free waits for dy and the conversion at the same time, not for
+// a load and then the conversion.
+constexpr uint32_t Q_BYTES = TOK * 128;
+constexpr int Q_STAGES = 6;
+constexpr uint32_t STAGE_BYTES = 2 * OP_BYTES;
 constexpr int CHUNK = 8;              // stages between two additions in registers
 constexpr int EPI_WARPS = 8, CONV_WARPS = 8, CONV_GROUP = 4;
 constexpr uint32_t STG_BYTES = 32 * 128;
-constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STG_BYTES + STAGES * TOK * 4 + 512;
-constexpr int THREADS = 128 + 32 * (EPI_WARPS + CONV_WARPS);  // warps 0 TMA, 1 MMA, 2 scales, 4-11 converters, 12-19 epilogue
+constexpr size_t SMEM =
+    1024 + STAGES * STAGE_BYTES + Q_STAGES * Q_BYTES + EPI_WARPS * STG_BYTES + Q_STAGES * TOK * 4 + 512;
+constexpr int THREADS = 128 + 32 * (EPI_WARPS + CONV_WARPS);  // warps 0 TMA of dy, 1 MMA, 2 scales, 3 TMA of x, 4-11 converters, 12-19 epilogue
 // Registers: 640 threads launch with 96.
 constexpr int REGS_LAUNCH = 96, REGS_EPI = 168, REGS_CONV = 56, REGS_REST = 32;
 static_assert(REGS_EPI * 256 + REGS_CONV * 256 + REGS_REST * 128 <= REGS_LAUNCH * THREADS,
@@ -85,12 +91,13 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   uint8_t* sA = smem;
   uint8_t* sB = smem + STAGES * OP_BYTES;
   uint8_t* sQ = smem + STAGES * 2 * OP_BYTES;
-  uint8_t* sStg = smem + STAGES * STAGE_BYTES;
+  uint8_t* sStg = sQ + Q_STAGES * Q_BYTES;
   float* sScale = reinterpret_cast<float*>(sStg + EPI_WARPS * STG_BYTES);
-  uint64_t* full = reinterpret_cast<uint64_t*>(sScale + STAGES * TOK);  // dy has come and x is converted
-  uint64_t* full_q = full + STAGES;
-  uint64_t* empty = full_q + STAGES;
-  uint64_t* acc_full = empty + STAGES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sScale + Q_STAGES * TOK);  // dy has come and x is converted
+  uint64_t* empty = full + STAGES;
+  uint64_t* full_q = empty + STAGES;
+  uint64_t* empty_q = full_q + Q_STAGES;
+  uint64_t* acc_full = empty_q + Q_STAGES;
   uint64_t* acc_empty = acc_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -113,8 +120,11 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(&full[s], 1 + (PAIR ? 2 * CONV_GROUP : CONV_GROUP));
-      mbar_init(&full_q[s], 2);  // the bytes and the scales
       mbar_init(&empty[s], 1);
+    }
+    for (int s = 0; s < Q_STAGES; ++s) {
+      mbar_init(&full_q[s], 2);  // the bytes and the scales
+      mbar_init(&empty_q[s], CONV_GROUP);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&acc_full[b], 1);
@@ -145,7 +155,7 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_REST));
     if (warp == 0 && lane == 0) {
-      // ---------------- TMA producer: dy and the checkpoint's bytes ----------------
+      // ---------------- TMA producer: dy ----------------
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
@@ -155,8 +165,6 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           if (!mbar_wait(&empty[stage], phase ^ 1u, abort_flag, err)) { ok = false; break; }
           uint8_t* dst = sA + stage * OP_BYTES;
           const int n = t.n + rank * 128, m = t.m + s * TOK;
-          mbar_arrive_expect_tx(&full_q[stage], Q_BYTES);
-          tma_load_2d(&tmX, &full_q[stage], sQ + stage * Q_BYTES, t.k + rank * 128, m);
           if (PAIR) {
             if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * OP_BYTES);
             const uint32_t bar = cluster_map(smem_u32(&full[stage]), 0);
@@ -184,13 +192,27 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           const int next = t.m + (s + 1) * TOK + lane;
           b0 = sc[min(next, p.M - 1)];
           b1 = sc[min(next + 32, p.M - 1)];
-          const bool done = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, err);
+          const bool done = mbar_wait(&empty_q[stage], phase ^ 1u, abort_flag, err);
           if (!__all_sync(0xffffffffu, done)) { ok = false; break; }
           sScale[stage * TOK + lane] = block8_scale(c0);
           sScale[stage * TOK + 32 + lane] = block8_scale(c1);
           __syncwarp();
           if (lane == 0) mbar_arrive(&full_q[stage]);
-          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          if (++stage == Q_STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+    } else if (warp == 3 && lane == 0) {
+      // ---------------- TMA producer: the checkpoint's bytes ----------------
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int i = first; i < items && ok; i += step) {
+        const Item t = item_at(i);
+        for (int s = 0; s < t.stages; ++s) {
+          if (!mbar_wait(&empty_q[stage], phase ^ 1u, abort_flag, err)) { ok = false; break; }
+          mbar_arrive_expect_tx(&full_q[stage], Q_BYTES);
+          tma_load_2d(&tmX, &full_q[stage], sQ + stage * Q_BYTES, t.k + rank * 128, t.m + s * TOK);
+          if (++stage == Q_STAGES) { stage = 0; phase ^= 1u; }
         }
       }
     } else if (warp == 1 && rank == 0) {
@@ -243,17 +265,18 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CONV));
     const int cw = (warp - 4) & (CONV_GROUP - 1), group = (warp - 4) / CONV_GROUP;
     const int col = 8 * (lane & 15), t0 = 2 * cw + (lane >> 4);  // tokens t0 + 8 j
-    int stage = 0, turn = 0;
-    uint32_t phase = 0;
+    int stage = 0, qstage = 0, turn = 0;
+    uint32_t phase = 0, qphase = 0;
     bool ok = true;
     for (int i = first; i < items && ok; i += step) {
       const int stages = item_at(i).stages;
       for (int s = 0; s < stages; ++s, turn ^= 1) {
         if (turn == group) {
-          const bool done = mbar_wait(&full_q[stage], phase, abort_flag, err);
+          bool done = mbar_wait(&full_q[qstage], qphase, abort_flag, err);
+          done = done && mbar_wait(&empty[stage], phase ^ 1u, abort_flag, err);
           if (!__all_sync(0xffffffffu, done)) { ok = false; break; }
-          const uint8_t* src = sQ + stage * Q_BYTES + col;
-          const float* sc = sScale + stage * TOK;
+          const uint8_t* src = sQ + qstage * Q_BYTES + col;
+          const float* sc = sScale + qstage * TOK;
           // row (token) r, 16-byte piece c of its 64 columns at piece c ^ (r & 7)
           uint8_t* dst = sB + stage * OP_BYTES + (col >> 6) * PIECE;
           const int c = ((col >> 3) & 7) ^ (t0 & 7);  // (the same for all of the lane's tokens)
@@ -276,9 +299,11 @@ __global__ void __launch_bounds__(w8::THREADS, 1)
           if (lane == 0) {
             if (PAIR) arrive_even(&full[stage]);
             else mbar_arrive(&full[stage]);
+            mbar_arrive(&empty_q[qstage]);
           }
         }
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        if (++qstage == Q_STAGES) { qstage = 0; qphase ^= 1u; }
       }
     }
     __syncwarp();
