@@ -470,7 +470,7 @@ lazymar_status lazymar_head_schedule(int n_train, int n_steps, int32_t *kept, fl
  * their columns and any element alignment (rows on boundaries of eight elements
  * are faster). Sums, statistics and parameter gradients are fp32. Results are
  * the same from call to call (no atomics). accumulate = 1 adds to the
- * parameter gradients instead of overwriting them.
+ * parameter gradients instead of overwriting them. At most 2^30 rows and columns.
  * ------------------------------------------------------------------------ */
 typedef struct lazymar_block8 {
   void* q;
@@ -524,7 +524,7 @@ lazymar_status lazymar_block8_pack_weight(int dtype, const void* w, int ldw, con
 /* Gradient through GELU (erf form) from the checkpoint u [rows, cols] of its
  * input: du = da * GELU'(u), da [rows, ldda] fp32 or bf16. u NULL: du = da (the
  * gradient of a linear layer's output). du goes to du [rows, lddu] (fp32 or
- * bf16; may be NULL) and / or du8 (may be NULL; the operand of the input
+ * bf16; may be NULL, or da itself with its type and stride) and / or du8 (may be NULL; the operand of the input
  * gradient's product); db [cols] fp32 (may be NULL) = sum over the rows of du,
  * the bias gradient. workspace:
  * lazymar_block8_gelu_backward_workspace(rows, cols) bytes, 16-byte aligned,

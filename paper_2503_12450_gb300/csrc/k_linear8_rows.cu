@@ -128,14 +128,15 @@ __global__ void __launch_bounds__(kWarps * 32) linear8_rows_kernel(const RowsPar
           }
         }
       }
+      // (one factor after the other: their product may leave fp32's range where the sum does not)
       const float ws = block8_scale(sw);
 #pragma unroll
       for (int j = 0; j < TILES; ++j) {  // accumulator: rows g and g + 8 of w, tokens 2 t and 2 t + 1
-        const float s0 = block8_scale(sa[j][0]) * ws, s1 = block8_scale(sa[j][1]) * ws;
-        sum[j][0] = fmaf(d[j][0], s0, sum[j][0]);
-        sum[j][1] = fmaf(d[j][1], s1, sum[j][1]);
-        sum[j][2] = fmaf(d[j][2], s0, sum[j][2]);
-        sum[j][3] = fmaf(d[j][3], s1, sum[j][3]);
+        const float s0 = block8_scale(sa[j][0]), s1 = block8_scale(sa[j][1]);
+        sum[j][0] = fmaf(d[j][0] * s0, ws, sum[j][0]);
+        sum[j][1] = fmaf(d[j][1] * s1, ws, sum[j][1]);
+        sum[j][2] = fmaf(d[j][2] * s0, ws, sum[j][2]);
+        sum[j][3] = fmaf(d[j][3] * s1, ws, sum[j][3]);
       }
     }
   }

@@ -14,6 +14,10 @@ lazymar_status bad(const char* msg) { return report_error(LAZYMAR_ERR_INVALID_AR
     if (s_ != LAZYMAR_OK) return s_; \
   } while (0)
 
+// Rows and columns that the kernels count in 32 bits with room for a launch's strides.
+constexpr int kMost = 1 << 30;
+lazymar_status too_large() { return report_error(LAZYMAR_ERR_UNSUPPORTED, "at most 2^30 rows and columns"); }
+
 bool float_type(int dtype) { return dtype == LAZYMAR_F32 || dtype == LAZYMAR_BF16; }
 size_t elem(int dtype) { return dtype == LAZYMAR_F32 ? 4 : 2; }
 bool at(const void* p, size_t align) { return reinterpret_cast<uintptr_t>(p) % align == 0; }
@@ -55,6 +59,7 @@ extern "C" lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, 
                                                     float eps, void* stream) {
   if (M < 0 || D < 1 || !(eps > 0.f)) return bad("M >= 0, D >= 1, eps > 0 required");
   if (D > kLnMaxWidth) return report_error(LAZYMAR_ERR_UNSUPPORTED, "D <= 8192 required");
+  if (M > kMost) return too_large();
   if (!y && !y8 && !x8 && !mean && !rstd) return bad("no output given");
   if (M == 0) return LAZYMAR_OK;
   TR_TRY(check_mat(x, x_dtype, ldx, D, "x: fp32 or bf16 device tensor, ldx >= D required"));
@@ -91,6 +96,7 @@ extern "C" lazymar_status lazymar_layernorm_backward(int dy_dtype, const void* d
                                                      size_t workspace_bytes, void* stream) {
   if (M < 0 || D < 1) return bad("M >= 0, D >= 1 required");
   if (D > kLnMaxWidth) return report_error(LAZYMAR_ERR_UNSUPPORTED, "D <= 8192 required");
+  if (M > kMost) return too_large();
   if ((dg == nullptr) != (db == nullptr)) return bad("dg and db: both or neither");
   if (M > 0) {
     if ((x == nullptr) == (x8 == nullptr)) return bad("exactly one of x and x8 required");
@@ -131,6 +137,7 @@ extern "C" lazymar_status lazymar_layernorm_backward(int dy_dtype, const void* d
 extern "C" lazymar_status lazymar_block8_pack(int dtype, const void* x, int ldx, const lazymar_block8* q, int rows,
                                               int cols, void* stream) {
   if (rows < 0 || cols < 1) return bad("rows >= 0, cols >= 1 required");
+  if (rows > kMost || cols > kMost) return too_large();
   if (!q) return bad("q required");
   if (rows == 0) return LAZYMAR_OK;
   TR_TRY(check_mat(x, dtype, ldx, cols, "x: fp32 or bf16 device tensor, ldx >= cols required"));
@@ -149,6 +156,7 @@ extern "C" lazymar_status lazymar_block8_pack(int dtype, const void* x, int ldx,
 extern "C" lazymar_status lazymar_block8_unpack(const lazymar_block8* q, int dtype, void* x, int ldx, int rows,
                                                 int cols, void* stream) {
   if (rows < 0 || cols < 1) return bad("rows >= 0, cols >= 1 required");
+  if (rows > kMost || cols > kMost) return too_large();
   if (!q) return bad("q required");
   if (rows == 0) return LAZYMAR_OK;
   TR_TRY(check_block8(q, cols, rows, "q: device tensors, 16-byte aligned, ldq % 16 == 0, ldq >= cols, lds >= rows"));
@@ -182,6 +190,7 @@ extern "C" lazymar_status lazymar_block8_gelu_backward(int dtype, const void* da
                                                        float* db, int accumulate, int rows, int cols, void* workspace,
                                                        size_t workspace_bytes, void* stream) {
   if (rows < 0 || cols < 1) return bad("rows >= 0, cols >= 1 required");
+  if (rows > kMost || cols > kMost) return too_large();
   if (!du && !du8 && !db) return bad("no output given");
   if (rows > 0) {
     TR_TRY(check_mat(da, dtype, ldda, cols, "da: fp32 or bf16 device tensor, ldda >= cols required"));
@@ -218,6 +227,7 @@ extern "C" lazymar_status lazymar_block8_linear(int epilogue, const lazymar_bloc
   if (epilogue != LAZYMAR_EPI_BIAS && epilogue != LAZYMAR_EPI_GELU && epilogue != LAZYMAR_EPI_RESIDUAL)
     return bad("epilogue: BIAS, GELU or RESIDUAL");
   if (M < 0 || N < 0 || K < 1) return bad("M >= 0, N >= 0, K >= 1 required");
+  if (M > kMost || N > kMost || K > kMost) return too_large();
   if (!a || !w) return bad("a and w required");
   if (!out && !out8) return bad("out or out8 required");
   if (epilogue == LAZYMAR_EPI_RESIDUAL) {
@@ -260,6 +270,7 @@ extern "C" lazymar_status lazymar_block8_wgrad(const void* dy, int lddy, const l
                                                int accumulate, int M, int N, int K, void* workspace,
                                                size_t workspace_bytes, void* stream) {
   if (M < 0 || N < 0 || K < 1) return bad("M >= 0, N >= 0, K >= 1 required");
+  if (M > kMost || N > kMost || K > kMost) return too_large();
   if (N == 0) return LAZYMAR_OK;
   TR_TRY(check_mat(dw, LAZYMAR_F32, lddw, K, "dw: fp32 device tensor, lddw >= K required"));
   if (M > 0) {

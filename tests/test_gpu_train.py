@@ -386,6 +386,19 @@ def test_gelu_backward(M, D, pad, offset, da_dtype, du_dtype, with8, with_u):
     assert torch.equal(db, first + first)
 
 
+@pytest.mark.parametrize("cols,pad", [(512, 0), (300, 1)])
+def test_gelu_backward_in_place(cols, pad):
+    torch = torch_cuda()
+    r = rng(23)
+    da, _ = dev(r.standard_normal((70, cols)), "bf16", pad)
+    h, _ = held(r.standard_normal((70, cols)))
+    du = out(70, cols, "bf16", pad)
+    lm.lazymar_block8_gelu_backward(1, da, cols + pad, h.d, 1, du, cols + pad, None, None, False, 70, cols, None, 0)
+    lm.lazymar_block8_gelu_backward(1, da, cols + pad, h.d, 1, da, cols + pad, None, None, False, 70, cols, None, 0)
+    sync()
+    assert torch.equal(da, du)
+
+
 def test_gelu_backward_keeps_nan():
     x = rng(9).standard_normal((4, 200)).astype(np.float32)
     da, _ = dev(x)
@@ -494,6 +507,27 @@ def test_linear_many_tiles(M, N, K):
     close(o, 2 * want, 2 * bound + 2 * U * np.abs(want))
     close8(u8, want, bound)
     close8(g8, T.gelu(want), bound * 1.13 + 4e-7 * np.maximum(1, np.abs(want)))
+
+
+@pytest.mark.parametrize("M", [3, 40, 400])
+def test_linear_scales_far_from_one(M):
+    """Factors whose product leaves fp32's range where the result does not: a zero stays zero, and large times small
+    is exact."""
+    r = rng(24)
+    x = r.standard_normal((M, 256))
+    x[:, :128] *= 2.0 ** 100
+    x[:, 128:] *= 2.0 ** -100
+    w = r.standard_normal((128, 256))
+    w[:, :128] *= 2.0 ** -100
+    w[:, 128:] *= 2.0 ** 100
+    x[1] = 0
+    a, av = held(x.astype(np.float32))
+    v, wv = held_weight(w.astype(np.float32))
+    y = out(M, 128)
+    lm.lazymar_block8_linear(0, a.d, v.d, None, None, 0, 0, y, 128, None, None, M, 128, 256)
+    sync()
+    close(y, av @ wv.T, _product_bound(np.abs(av) @ np.abs(wv).T, 256))
+    assert (y[1] == 0).all()
 
 
 def test_linear_ignores_padding_bytes_and_keeps_nan_in_its_row():

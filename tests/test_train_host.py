@@ -160,6 +160,8 @@ def _b8(q=0, scale=0, ldq=128, lds=4):
     (lambda L, q: L.lazymar_block8_linear(0, q.addr, q.addr, None, None, 0, 0, 16, 8, None, None, 4, 8, 0, None), 1,
      "K >= 1"),
     (lambda L, q: L.lazymar_block8_wgrad(16, 8, q.addr, 16, 8, 0, 4, 8, 0, None, 0, None), 1, "K >= 1"),
+    (lambda L, q: L.lazymar_block8_wgrad(16, 8, q.addr, 16, 8, 0, (1 << 30) + 1, 8, 8, None, 0, None), 6, "2^30"),
+    (lambda L, q: L.lazymar_block8_pack(0, 16, 8, q.addr, (1 << 30) + 1, 8, None), 6, "2^30"),
 ])
 def test_refusals_before_touching_the_device(lib, call, status, word):
     q = _b8()
