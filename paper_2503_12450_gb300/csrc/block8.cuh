@@ -55,8 +55,10 @@ __device__ __forceinline__ float4 f4_nonfinite_to(float4 v, float to) {
 // eight bytes. The scale is that of the finite values; infinities and NaN become
 // NaN, so an overflow stays visible and does not disturb its neighbours.
 __device__ __forceinline__ uint32_t block8_amax(const float (&v)[8]) {
-  const float m = fmax3(fmax3(fabsf(v[0]), fabsf(v[1]), fabsf(v[2])), fmax3(fabsf(v[3]), fabsf(v[4]), fabsf(v[5])),
-                        fmaxf(fabsf(v[6]), fabsf(v[7])));
+  // (plain fmaxf: the compiler folds the magnitudes into three-input maxima)
+  float m = fmaxf(fabsf(v[0]), fabsf(v[1]));
+#pragma unroll
+  for (int i = 2; i < 8; i += 2) m = fmaxf(fmaxf(m, fabsf(v[i])), fabsf(v[i + 1]));
   return __float_as_uint(m);
 }
 __device__ __forceinline__ float nonfinite_to(float x, float to) {
@@ -70,25 +72,26 @@ __device__ __forceinline__ uint32_t half_warp_max(uint32_t m, bool upper, uint32
 }
 __device__ __forceinline__ uint32_t block8_quantize(const float (&v)[8], uint2& q) {
   const bool upper = threadIdx.x & 16;
-  uint32_t both, amax = half_warp_max(block8_amax(v), upper, both);
-  float w[8];
+  auto scaled = [&](const float (&x)[8], uint32_t amax) {
+    const uint32_t byte = block8_exp(amax);
+    const float s = block8_inv(byte);
+    const unsigned long long ss = f32x2_pack(s, s);
+    float w[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = v[i];
-  if (both >= 0x7F800000u) {  // an infinity
-    float z[8];
+    for (int i = 0; i < 8; i += 2) f32x2_unpack(f32x2_mul(f32x2_pack(x[i], x[i + 1]), ss), w[i], w[i + 1]);
+    q = make_uint2(e4m3x4(w[0], w[1], w[2], w[3]), e4m3x4(w[4], w[5], w[6], w[7]));
+    return byte;
+  };
+  uint32_t both;
+  const uint32_t amax = half_warp_max(block8_amax(v), upper, both);
+  if (both < 0x7F800000u) return scaled(v, amax);
+  float z[8], n[8];  // an infinity
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = nonfinite_to(v[i], 0.f);
-    amax = half_warp_max(block8_amax(z), upper, both);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = nonfinite_to(v[i], __uint_as_float(0x7FC00000u));
+  for (int i = 0; i < 8; ++i) {
+    z[i] = nonfinite_to(v[i], 0.f);
+    n[i] = nonfinite_to(v[i], __uint_as_float(0x7FC00000u));
   }
-  const uint32_t byte = block8_exp(amax);
-  const float s = block8_inv(byte);
-  const unsigned long long ss = f32x2_pack(s, s);
-#pragma unroll
-  for (int i = 0; i < 8; i += 2) f32x2_unpack(f32x2_mul(f32x2_pack(w[i], w[i + 1]), ss), w[i], w[i + 1]);
-  q = make_uint2(e4m3x4(w[0], w[1], w[2], w[3]), e4m3x4(w[4], w[5], w[6], w[7]));
-  return byte;
+  return scaled(n, half_warp_max(block8_amax(z), upper, both));
 }
 // Eight E4M3 bytes times a scale.
 __device__ __forceinline__ void block8_values(uint2 q, float s, float (&v)[8]) {

@@ -168,7 +168,41 @@ __device__ __forceinline__ void mask8(float (&v)[8], int col, int D) {
     if (col + i >= D) v[i] = 0.f;
 }
 __device__ __forceinline__ float sum8(const float (&v)[8]) {
-  return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  const unsigned long long s =
+      f32x2_add(f32x2_add(f32x2_pack(v[0], v[1]), f32x2_pack(v[2], v[3])), f32x2_add(f32x2_pack(v[4], v[5]), f32x2_pack(v[6], v[7])));
+  float a, b;
+  f32x2_unpack(s, a, b);
+  return a + b;
+}
+
+// Eight values with paired fp32 instructions: v - m; v * s; v * a + b; sum of squares.
+__device__ __forceinline__ void sub8(float (&v)[8], float m) {
+  const unsigned long long mm = f32x2_pack(-m, -m);
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) f32x2_unpack(f32x2_add(f32x2_pack(v[i], v[i + 1]), mm), v[i], v[i + 1]);
+}
+__device__ __forceinline__ void scale8(const float (&v)[8], float s, float (&y)[8]) {
+  const unsigned long long ss = f32x2_pack(s, s);
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) f32x2_unpack(f32x2_mul(f32x2_pack(v[i], v[i + 1]), ss), y[i], y[i + 1]);
+}
+__device__ __forceinline__ void mul8(float (&y)[8], const float (&a)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2)
+    f32x2_unpack(f32x2_mul(f32x2_pack(y[i], y[i + 1]), f32x2_pack(a[i], a[i + 1])), y[i], y[i + 1]);
+}
+__device__ __forceinline__ void add8(float (&y)[8], const float (&a)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2)
+    f32x2_unpack(f32x2_add(f32x2_pack(y[i], y[i + 1]), f32x2_pack(a[i], a[i + 1])), y[i], y[i + 1]);
+}
+__device__ __forceinline__ float squares8(const float (&v)[8]) {
+  unsigned long long q = f32x2_mul(f32x2_pack(v[0], v[1]), f32x2_pack(v[0], v[1]));
+#pragma unroll
+  for (int i = 2; i < 8; i += 2) q = f32x2_fma(f32x2_pack(v[i], v[i + 1]), f32x2_pack(v[i], v[i + 1]), q);
+  float a, b;
+  f32x2_unpack(q, a, b);
+  return a + b;
 }
 
 // Sum of v over the WPR warps of a row (`red`: this row's slots in shared
@@ -220,11 +254,9 @@ __global__ void __launch_bounds__(256, 4) ln_forward_kernel(const LnForward p) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       if (p.x8.q && (FULL || c0 + c * kChunk < D)) put8<FULL>(p.x8, row, c0 + c * kChunk, D, v[c]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] -= mean;
+      sub8(v[c], mean);
       mask8<FULL>(v[c], c0 + c * kChunk + 8 * lane, D);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q = fmaf(v[c][i], v[c][i], q);
+      q += squares8(v[c]);
     }
   }
   const float rstd = rsqrtf(row_sum<WPR>(q, red[1][grp], part) / (float)D + p.eps);
@@ -239,17 +271,14 @@ __global__ void __launch_bounds__(256, 4) ln_forward_kernel(const LnForward p) {
     const int cc = c0 + c * kChunk, col = cc + 8 * lane;
     if (!FULL && cc >= D) break;  // (uniform over the warp)
     float y[8], t[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = v[c][i] * rstd;
+    scale8(v[c], rstd, y);
     if (p.g) {
       ld_param<FULL>(p.g, col, D, t);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] *= t[i];
+      mul8(y, t);
     }
     if (p.b) {
       ld_param<FULL>(p.b, col, D, t);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] += t[i];
+      add8(y, t);
     }
     mask8<FULL>(y, col, D);
     if (p.y8.q) put8<FULL>(p.y8, row, cc, D, y);
