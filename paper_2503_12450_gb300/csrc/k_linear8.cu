@@ -125,8 +125,8 @@ __device__ __forceinline__ uint32_t quantize_row(const float (&v)[128], uint32_t
 #pragma unroll
   for (int i = 0; i < 128; i += 8)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) m[j] = fmax3(m[j], fabsf(v[i + 2 * j]), fabsf(v[i + 2 * j + 1]));
-  uint32_t amax = __float_as_uint(fmax3(fmaxf(m[0], m[1]), m[2], m[3]));
+    for (int j = 0; j < 4; ++j) m[j] = fmaxf(fmaxf(m[j], fabsf(v[i + 2 * j])), fabsf(v[i + 2 * j + 1]));
+  uint32_t amax = __float_as_uint(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
   const bool special = amax >= 0x7F800000u;
   if (special) {
     amax = 0;
