@@ -227,8 +227,8 @@ __device__ __forceinline__ float row_sum(float v, float* red, int part) {
 // WPR warps a row, NC chunks of 256 columns a warp, the row in registers: one
 // read of x, mean and then the squared deviations from it (no cancellation).
 // FULL: D = 256 NC WPR and aligned rows, so that no column needs a check.
-// 40960 x 1024 fp32 with statistics, 8-bit output and 8-bit copy of the input: 47 us,
-// 5.4 TB/s (floor 37 at 6.8).
+// 40960 x 1024 fp32 with statistics, 8-bit output and 8-bit copy of the input: 43.7
+// us, 5.8 TB/s (floor 37 at 6.8); without paired instructions 47, four columns a lane 67.
 template <int NC, int WPR, bool FULL>
 __global__ void __launch_bounds__(256, 4) ln_forward_kernel(const LnForward p) {
   constexpr int GROUPS = 8 / WPR;
@@ -758,7 +758,7 @@ __device__ __forceinline__ float gelu_grad_at(const float* tab, float x) {
 // VEC: rows on boundaries and cols a multiple of eight, so that a lane's columns
 // all exist or none does; otherwise a row at a time, through shared memory
 // where it is off the boundary.
-// 40960 x 4096, bf16 in and out, 8-bit out, bias gradient: 172 us, 5.9 TB/s (floor
+// 40960 x 4096, bf16 in and out, 8-bit out, bias gradient: 168 us, 6.0 TB/s (floor
 // 148); four columns a lane and a polynomial for the gradient took 499.
 template <typename T, bool HAS_U, bool VEC>
 __global__ void __launch_bounds__(256, HAS_U ? 3 : 4) rows8_kernel(const Rows8 p, int nchunk, int groups) {
@@ -859,7 +859,7 @@ __global__ void __launch_bounds__(256, HAS_U ? 3 : 4) rows8_kernel(const Rows8 p
 }
 
 // Row groups of a launch: the warps that fit on every SM, once: 24 with four rows
-// in flight each for GELU's gradient (40960 x 4096: 171 us; 32 with two 180), 32
+// in flight each for GELU's gradient (40960 x 4096: 171 us then; 32 with two 180), 32
 // without it (pack of 20480 x 4096: 41 us; 24 warps 47).
 int rows8_groups(int rows, int nchunk, bool has_u) {
   const int want = kSMs * (has_u ? 24 : 32) / nchunk, most = (rows + 1) / 2;
