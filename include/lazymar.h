@@ -537,7 +537,8 @@ lazymar_status lazymar_block8_gelu_backward(int dtype, const void* da, int ldda,
 
 /* y = a w^T + bias with a [M, K] and w [N, K] in block8 (w with 128 x 128
  * blocks), accumulated in fp32 on the 8-bit tensor cores with the scales
- * applied there (kind::mxf8f6f4); bias fp32 [N] (may be NULL).
+ * applied there (kind::mxf8f6f4; above 32 rows the accumulator truncates, a
+ * relative bias towards zero of about 6e-11 K); bias fp32 [N] (may be NULL).
  *   LAZYMAR_EPI_BIAS      out = y
  *   LAZYMAR_EPI_GELU      out = GELU(y) (erf form)
  *   LAZYMAR_EPI_RESIDUAL  out = residual + y, residual [M, ldr] and out fp32

@@ -17,7 +17,14 @@
 // 97 and 100 us or so. What bounds it: the MMAs of a stage take 690 cycles alone
 // (512 nominal) and 900 next to the loads of the next stages and the epilogue,
 // which share shared and tensor memory with them; in a long run the 1400 W limit
-// (1365 W drawn, sw_power_cap active) makes it 123 and 150 us.
+// (1365 W drawn, sw_power_cap active) makes it 122 to 128 and 149 to 155 us.
+//
+// Accuracy: the accumulator of the tensor cores is fp32 and truncates, so a sum comes
+// out too small in magnitude by 6.9e-8 of itself at K = 1280, 3.3e-7 at 5120 and 4e-6
+// at 65536 (fp32 additions to nearest: no bias, 6.2e-8 to 6.5e-7 of noise). k_wgrad8.cu
+// adds its accumulator to registers every 512 terms; here that would be one more pass
+// over tensor memory for each step of an epilogue that the MMAs already wait for, for
+// operands that were rounded at 2^-4.
 #include <cuda.h>
 
 #include <cstring>
