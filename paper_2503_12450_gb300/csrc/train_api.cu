@@ -169,6 +169,7 @@ extern "C" lazymar_status lazymar_block8_unpack(const lazymar_block8* q, int dty
 extern "C" lazymar_status lazymar_block8_pack_weight(int dtype, const void* w, int ldw, const lazymar_block8* q,
                                                      const lazymar_block8* qt, int N, int K, void* stream) {
   if (N < 0 || K < 1 || N > 128 * 65535) return bad("0 <= N <= 8388480, K >= 1 required");
+  if (K > kMost) return too_large();
   if (!q && !qt) return bad("q or qt required");
   if (N == 0) return LAZYMAR_OK;
   TR_TRY(check_mat(w, dtype, ldw, K, "w: fp32 or bf16 device tensor, ldw >= K required"));

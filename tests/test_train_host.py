@@ -185,3 +185,10 @@ def test_workspaces_cover_small_and_large_sizes(lib):
     assert lm.lazymar_layernorm_backward_workspace(40960, 1280) <= 8 << 20
     assert lm.lazymar_block8_gelu_backward_workspace(0, 768) == 0
     assert lm.lazymar_block8_gelu_backward_workspace(40960, 5120) <= 16 << 20
+
+
+def test_weight_pack_refuses_more_columns_than_it_counts(lib):
+    q = _b8()
+    for k in ((1 << 30) + 1, (1 << 31) - 1):
+        assert lib.lazymar_block8_pack_weight(0, 16, k, q.addr, None, 8, k, None) == 6
+        assert "2^30" in lib.lazymar_last_error().decode()
