@@ -437,6 +437,9 @@ def lazymar_block8(q, scale, ldq=None, lds=None):
     [blocks of 128 columns, lds] bytes (weights: [blocks of K, blocks of N]). The
     strides are the tensors' own unless given. Keeps the tensors alive; make it
     once and use it again."""
+    for t in (q, scale):
+        if hasattr(t, "element_size") and (t.dim() != 2 or t.element_size() != 1 or (t.shape[1] > 1 and t.stride(1) != 1)):
+            raise LazymarError(1, "q and scale: tensors of two axes of bytes, consecutive along the last")
     if ldq is None:
         ldq = q.stride(0) if q.shape[0] > 1 else max(q.stride(0), q.shape[1])
     if lds is None:

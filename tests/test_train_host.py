@@ -192,3 +192,18 @@ def test_weight_pack_refuses_more_columns_than_it_counts(lib):
     for k in ((1 << 30) + 1, (1 << 31) - 1):
         assert lib.lazymar_block8_pack_weight(0, 16, k, q.addr, None, 8, k, None) == 6
         assert "2^30" in lib.lazymar_last_error().decode()
+
+
+def test_descriptor_takes_rows_of_bytes_only():
+    torch = pytest.importorskip("torch")
+    q, scale = torch.zeros((8, 256), dtype=torch.uint8), torch.zeros((2, 8), dtype=torch.uint8)
+    d = lm.lazymar_block8(q, scale)
+    assert (d.ldq, d.lds) == (256, 8)
+    d = lm.lazymar_block8(q[:, :128].view(torch.float8_e4m3fn), scale[:1])
+    assert (d.ldq, d.lds) == (256, 8)
+    d = lm.lazymar_block8(q[:0], scale[:, :0])
+    assert d.ldq == 256
+    for bad_q, bad_scale in ((q.float(), scale), (q, scale.float()), (q[:, ::2], scale), (q, scale[:, ::2]),
+                             (q.t(), scale), (q, scale.t()), (q[0], scale), (q, scale[0])):
+        with pytest.raises(lm.LazymarError, match="bytes"):
+            lm.lazymar_block8(bad_q, bad_scale)
