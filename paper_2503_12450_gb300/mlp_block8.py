@@ -38,7 +38,8 @@ class MlpBlock8:
         self.grads = {k: torch.zeros_like(v) for k, v in self.p.items()}
         self.w1, self.w1t = Tensor8(self.H, self.D, dev, True), Tensor8(self.D, self.H, dev, True)
         self.w2, self.w2t = Tensor8(self.D, self.H, dev, True), Tensor8(self.H, self.D, dev, True)
-        self.rows = 0
+        self.rows = self.serving_rows = None  # of the buffers for training, for serving
+        self.kept = False  # whether a forward pass has left what backward() reads
         self.pack()
 
     def pack(self):
@@ -46,6 +47,11 @@ class MlpBlock8:
         D, H = self.D, self.H
         lm.lazymar_block8_pack_weight(F32, self.p["w1"], D, self.w1.d, self.w1t.d, H, D)
         lm.lazymar_block8_pack_weight(F32, self.p["w2"], H, self.w2.d, self.w2t.d, D, H)
+
+    def _serving_buffers(self, M, dev):
+        if M != self.serving_rows:
+            self.h8s, self.a8s = Tensor8(M, self.D, dev), Tensor8(M, self.H, dev)
+            self.serving_rows = M
 
     def _buffers(self, M, dev):
         if M == self.rows:
@@ -64,21 +70,34 @@ class MlpBlock8:
         return sum(t.bytes() for t in (self.x8, self.h8, self.u8, self.a8))
 
     def forward(self, x, train=True):
-        """x [M, D] fp32, the residual stream. Returns y [M, D] fp32."""
+        """x [M, D] fp32, the residual stream. Returns y [M, D] fp32. Without `train` nothing is kept, and what an
+        earlier pass has kept stays."""
         M, D, H = x.shape[0], self.D, self.H
-        p, y = self.p, torch.empty_like(x)
-        self._buffers(M, x.device)
-        lm.lazymar_layernorm_forward(F32, x, x.stride(0), p["ln_g"], p["ln_b"], F32, None, 0, self.h8.d,
+        p, y = self.p, torch.empty((M, D), device=x.device)
+        if train:
+            self.kept = False
+            self._buffers(M, x.device)
+            h8, a8 = self.h8, self.a8
+        else:
+            self._serving_buffers(M, x.device)
+            h8, a8 = self.h8s, self.a8s
+        lm.lazymar_layernorm_forward(F32, x, x.stride(0), p["ln_g"], p["ln_b"], F32, None, 0, h8.d,
                                      self.x8.d if train else None, self.mean if train else None,
                                      self.rstd if train else None, M, D, self.eps)
-        lm.lazymar_block8_linear(lm.LAZYMAR_EPI_GELU, self.h8.d, self.w1.d, p["b1"], None, 0, F32, None, 0, self.a8.d,
+        lm.lazymar_block8_linear(lm.LAZYMAR_EPI_GELU, h8.d, self.w1.d, p["b1"], None, 0, F32, None, 0, a8.d,
                                  self.u8.d if train else None, M, H, D)
-        lm.lazymar_block8_linear(lm.LAZYMAR_EPI_RESIDUAL, self.a8.d, self.w2.d, p["b2"], x, x.stride(0), F32, y, D, None,
+        lm.lazymar_block8_linear(lm.LAZYMAR_EPI_RESIDUAL, a8.d, self.w2.d, p["b2"], x, x.stride(0), F32, y, D, None,
                                  None, M, D, H)
+        self.kept = self.kept or train
         return y
 
     def backward(self, dy, accumulate=False):
-        """dy [M, D] fp32. Returns dx [M, D] fp32 and leaves (or adds) the parameters' gradients."""
+        """dy [M, D] fp32, of the last forward pass with `train`. Returns dx [M, D] fp32 and leaves (or adds) the
+        parameters' gradients."""
+        if not self.kept:
+            raise lm.LazymarError(1, "backward() needs a forward pass with train=True")
+        if tuple(dy.shape) != (self.rows, self.D):
+            raise lm.LazymarError(1, "dy: [%d, %d], as the forward pass's rows" % (self.rows, self.D))
         M, D, H = dy.shape[0], self.D, self.H
         g, ws, n, dev = self.grads, self.ws, self.ws.numel(), dy.device
         dyb = torch.empty((M, -(-D // 8) * 8), dtype=torch.bfloat16, device=dev)

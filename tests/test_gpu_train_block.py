@@ -119,3 +119,40 @@ def test_example_runs_from_the_command_line():
                         "--steps", "4"], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
     assert "ms a step" in r.stdout and "8 bits" in r.stdout
+
+
+def _tensors(M, D, seed):
+    torch = torch_cuda()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return [torch.randn((M, D), device="cuda", generator=g) for _ in range(2)]
+
+
+def test_serving_between_forward_and_backward_leaves_what_was_kept():
+    torch = torch_cuda()
+    b = _block(_params(256, 1024, 7))
+    x, dy = _tensors(300, 256, 8)
+    b.forward(x)
+    want_dx = b.backward(dy)
+    want = {k: v.clone() for k, v in b.grads.items()}
+    for rows in (300, 7):  # as many rows as are kept, and another number
+        b.forward(x)
+        b.forward(3 * _tensors(rows, 256, 9)[0], train=False)
+        assert torch.equal(b.backward(dy), want_dx)
+        for k, v in b.grads.items():
+            assert torch.equal(v, want[k]), k
+
+
+def test_backward_needs_its_forward_pass():
+    torch_cuda()
+    from paper_2503_12450_gb300.lazymar import LazymarError
+    b = _block(_params(256, 1024, 7))
+    x, dy = _tensors(300, 256, 8)
+    with pytest.raises(LazymarError, match="forward"):
+        b.backward(dy)
+    b.forward(x, train=False)
+    with pytest.raises(LazymarError, match="forward"):
+        b.backward(dy)
+    b.forward(x)
+    for other in (dy[:299], dy[:, :255]):
+        with pytest.raises(LazymarError, match="dy"):
+            b.backward(other)
