@@ -60,8 +60,8 @@ extern "C" lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, 
   if (M < 0 || D < 1 || !(eps > 0.f)) return bad("M >= 0, D >= 1, eps > 0 required");
   if (D > kLnMaxWidth) return report_error(LAZYMAR_ERR_UNSUPPORTED, "D <= 8192 required");
   if (M > kMost) return too_large();
+  if (M == 0) return LAZYMAR_OK;  // (empty tensors have no address)
   if (!y && !y8 && !x8 && !mean && !rstd) return bad("no output given");
-  if (M == 0) return LAZYMAR_OK;
   TR_TRY(check_mat(x, x_dtype, ldx, D, "x: fp32 or bf16 device tensor, ldx >= D required"));
   if (y) TR_TRY(check_mat(y, y_dtype, ldy, D, "y: fp32 or bf16 device tensor, ldy >= D required"));
   if (y8) TR_TRY(check_block8(y8, D, M, "y8: device tensors, q 16-byte aligned, ldq % 16 == 0, ldq >= D, lds >= M"));
@@ -192,8 +192,8 @@ extern "C" lazymar_status lazymar_block8_gelu_backward(int dtype, const void* da
                                                        size_t workspace_bytes, void* stream) {
   if (rows < 0 || cols < 1) return bad("rows >= 0, cols >= 1 required");
   if (rows > kMost || cols > kMost) return too_large();
-  if (!du && !du8 && !db) return bad("no output given");
   if (rows > 0) {
+    if (!du && !du8 && !db) return bad("no output given");
     TR_TRY(check_mat(da, dtype, ldda, cols, "da: fp32 or bf16 device tensor, ldda >= cols required"));
     if (u)
       TR_TRY(check_block8(u, cols, rows, "u: device tensors, 16-byte aligned, ldq % 16 == 0, ldq >= cols, lds >= rows"));
@@ -230,14 +230,15 @@ extern "C" lazymar_status lazymar_block8_linear(int epilogue, const lazymar_bloc
   if (M < 0 || N < 0 || K < 1) return bad("M >= 0, N >= 0, K >= 1 required");
   if (M > kMost || N > kMost || K > kMost) return too_large();
   if (!a || !w) return bad("a and w required");
-  if (!out && !out8) return bad("out or out8 required");
+  const bool empty = M == 0 || N == 0;  // (empty tensors have no address)
+  if (!empty && !out && !out8) return bad("out or out8 required");
   if (epilogue == LAZYMAR_EPI_RESIDUAL) {
-    if (out8 || !out || out_dtype != LAZYMAR_F32) return bad("RESIDUAL: out fp32 and no out8");
+    if (out8 || (!out && !empty) || out_dtype != LAZYMAR_F32) return bad("RESIDUAL: out fp32 and no out8");
   } else if (residual) {
     return bad("residual is for LAZYMAR_EPI_RESIDUAL");
   }
   if (u8 && epilogue != LAZYMAR_EPI_GELU) return bad("u8 is for LAZYMAR_EPI_GELU");
-  if (M == 0 || N == 0) return LAZYMAR_OK;
+  if (empty) return LAZYMAR_OK;
   TR_TRY(check_block8(a, K, M, "a: device tensors, 16-byte aligned, ldq % 16 == 0, ldq >= K, lds >= M"));
   TR_TRY(check_block8(w, K, (N + 127) / 128,
                       "w: device tensors, 16-byte aligned, ldq % 16 == 0, ldq >= K, lds >= ceil(N / 128)"));

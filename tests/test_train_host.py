@@ -207,3 +207,14 @@ def test_descriptor_takes_rows_of_bytes_only():
                              (q.t(), scale), (q, scale.t()), (q[0], scale), (q, scale[0])):
         with pytest.raises(lm.LazymarError, match="bytes"):
             lm.lazymar_block8(bad_q, bad_scale)
+
+
+def test_empty_tensors_without_an_address_are_fine(lib):
+    q = _b8()
+    assert lib.lazymar_layernorm_forward(0, None, 8, None, None, 0, None, 8, None, None, None, None, 0, 8, 1e-6, None) == 0
+    for epilogue in (0, 1, 2):
+        assert lib.lazymar_block8_linear(epilogue, q.addr, q.addr, None, None, 8, 0, None, 8, None, None, 0, 8, 8, None) == 0
+        assert lib.lazymar_block8_linear(epilogue, q.addr, q.addr, None, None, 8, 0, None, 8, None, None, 4, 0, 8, None) == 0
+    # what cannot be meant is refused all the same
+    assert lib.lazymar_block8_linear(2, q.addr, q.addr, None, None, 8, 1, None, 8, None, None, 0, 8, 8, None) == 1
+    assert lib.lazymar_block8_linear(0, q.addr, None, None, None, 8, 0, None, 8, None, None, 0, 8, 8, None) == 1
