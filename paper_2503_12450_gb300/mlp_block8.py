@@ -27,6 +27,13 @@ class Tensor8:
         return self.q.numel() + self.scale.numel()
 
 
+def _row_stride(t, cols, name):
+    """The stride of fp32 rows of `cols` consecutive elements; refuses anything else."""
+    if t.dim() != 2 or t.shape[1] != cols or t.dtype != torch.float32 or (cols > 1 and t.stride(1) != 1):
+        raise lm.LazymarError(1, "%s: fp32 [rows, %d] with consecutive columns required" % (name, cols))
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), cols)
+
+
 class MlpBlock8:
     """Parameters and gradients: dicts of fp32 tensors ln_g, ln_b [D], w1 [H, D], b1 [H], w2 [D, H], b2 [D]."""
 
@@ -72,6 +79,7 @@ class MlpBlock8:
     def forward(self, x, train=True):
         """x [M, D] fp32, the residual stream. Returns y [M, D] fp32. Without `train` nothing is kept, and what an
         earlier pass has kept stays."""
+        ldx = _row_stride(x, self.D, "x")
         M, D, H = x.shape[0], self.D, self.H
         p, y = self.p, torch.empty((M, D), device=x.device)
         if train:
@@ -81,13 +89,13 @@ class MlpBlock8:
         else:
             self._serving_buffers(M, x.device)
             h8, a8 = self.h8s, self.a8s
-        lm.lazymar_layernorm_forward(F32, x, x.stride(0), p["ln_g"], p["ln_b"], F32, None, 0, h8.d,
+        lm.lazymar_layernorm_forward(F32, x, ldx, p["ln_g"], p["ln_b"], F32, None, 0, h8.d,
                                      self.x8.d if train else None, self.mean if train else None,
                                      self.rstd if train else None, M, D, self.eps)
         lm.lazymar_block8_linear(lm.LAZYMAR_EPI_GELU, h8.d, self.w1.d, p["b1"], None, 0, F32, None, 0, a8.d,
                                  self.u8.d if train else None, M, H, D)
-        lm.lazymar_block8_linear(lm.LAZYMAR_EPI_RESIDUAL, a8.d, self.w2.d, p["b2"], x, x.stride(0), F32, y, D, None,
-                                 None, M, D, H)
+        lm.lazymar_block8_linear(lm.LAZYMAR_EPI_RESIDUAL, a8.d, self.w2.d, p["b2"], x, ldx, F32, y, D, None, None, M,
+                                 D, H)
         self.kept = self.kept or train
         return y
 
@@ -98,13 +106,14 @@ class MlpBlock8:
             raise lm.LazymarError(1, "backward() needs a forward pass with train=True")
         if tuple(dy.shape) != (self.rows, self.D):
             raise lm.LazymarError(1, "dy: [%d, %d], as the forward pass's rows" % (self.rows, self.D))
+        lddy = _row_stride(dy, self.D, "dy")
         M, D, H = dy.shape[0], self.D, self.H
         g, ws, n, dev = self.grads, self.ws, self.ws.numel(), dy.device
         dyb = torch.empty((M, -(-D // 8) * 8), dtype=torch.bfloat16, device=dev)
         da = torch.empty((M, -(-H // 8) * 8), dtype=torch.bfloat16, device=dev)
         dh, dx = torch.empty_like(dyb), torch.empty((M, D), device=dev)
         ldd, ldh = dyb.stride(0), da.stride(0)
-        lm.lazymar_block8_gelu_backward(F32, dy, dy.stride(0), None, BF16, dyb, ldd, self.dy8.d, g["b2"], accumulate, M,
+        lm.lazymar_block8_gelu_backward(F32, dy, lddy, None, BF16, dyb, ldd, self.dy8.d, g["b2"], accumulate, M,
                                         D, ws, n)
         lm.lazymar_block8_wgrad(dyb, ldd, self.a8.d, g["w2"], H, accumulate, M, D, H, ws, n)
         lm.lazymar_block8_linear(lm.LAZYMAR_EPI_BIAS, self.dy8.d, self.w2t.d, None, None, 0, BF16, da, ldh, None, None, M,
@@ -115,5 +124,5 @@ class MlpBlock8:
         lm.lazymar_block8_linear(lm.LAZYMAR_EPI_BIAS, self.du8.d, self.w1t.d, None, None, 0, BF16, dh, ldd, None, None, M,
                                  D, H)
         lm.lazymar_layernorm_backward(BF16, dh, ldd, F32, None, 0, self.x8.d, self.mean, self.rstd, self.p["ln_g"], dy,
-                                      dy.stride(0), F32, dx, D, g["ln_g"], g["ln_b"], accumulate, M, D, ws, n)
+                                      lddy, F32, dx, D, g["ln_g"], g["ln_b"], accumulate, M, D, ws, n)
         return dx

@@ -156,3 +156,44 @@ def test_backward_needs_its_forward_pass():
     for other in (dy[:299], dy[:, :255]):
         with pytest.raises(LazymarError, match="dy"):
             b.backward(other)
+
+
+def test_block_takes_fp32_rows_of_any_stride_only():
+    torch = torch_cuda()
+    from paper_2503_12450_gb300.lazymar import LazymarError
+    b = _block(_params(256, 1024, 7))
+    x, dy = _tensors(300, 256, 8)
+    y = b.forward(x)
+    dx = b.backward(dy)
+    wide = [torch.zeros((300, 301), device="cuda") for _ in range(2)]
+    for w, v in zip(wide, (x, dy)):
+        w[:, 1:257] = v
+    assert torch.equal(b.forward(wide[0][:, 1:257]), y)
+    # (the gradient of the residual stream comes in rows off the boundary, which another kernel sums)
+    got = b.backward(wide[1][:, 1:257])
+    assert float((got - dx).norm() / dx.norm()) < 1e-5
+    one = torch.empty((1, 512), device="cuda")[:, :256].copy_(x[:1])
+    assert torch.equal(b.forward(one), b.forward(x[:1]))
+    for other in (x.double(), x.bfloat16(), x[:, :255], x[0], torch.zeros((300, 512), device="cuda")[:, ::2]):
+        with pytest.raises(LazymarError, match="x:"):
+            b.forward(other)
+        with pytest.raises(LazymarError, match="x:"):
+            b.forward(other, train=False)
+    b.forward(x)
+    for other in (dy.double(), dy.bfloat16(), torch.zeros((300, 512), device="cuda")[:, ::2]):
+        with pytest.raises(LazymarError, match="dy"):
+            b.backward(other)
+
+
+def test_block_without_rows():
+    torch = torch_cuda()
+    b = _block(_params(256, 1024, 7))
+    none = torch.empty((0, 256), device="cuda")
+    assert b.forward(none, train=False).shape == (0, 256)
+    assert b.forward(none).shape == (0, 256)
+    for v in b.grads.values():
+        v.fill_(1.0)
+    assert b.backward(none).shape == (0, 256)
+    torch.cuda.synchronize()
+    for k, v in b.grads.items():
+        assert not v.any(), k
