@@ -26,7 +26,7 @@ def tune(width, rows, steps, mlp_ratio=4, seed=0):
     lr = 0.03 / width ** 0.5  # a tenth of the disturbance
     teacher = MlpBlock8(random_params(width, mlp_ratio * width, seed))
     noise = random_params(width, mlp_ratio * width, seed + 1)
-    student = MlpBlock8({k: v + 0.3 * noise[k] if k.startswith("w") else v for k, v in teacher.p.items()})
+    student = MlpBlock8({k: v + 0.3 * noise[k] if k.startswith("w") else v.clone() for k, v in teacher.p.items()})
     g = torch.Generator(device="cuda").manual_seed(seed + 2)
     opt = torch.optim.Adam(list(student.p.values()), lr=lr)
     for k, v in student.p.items():

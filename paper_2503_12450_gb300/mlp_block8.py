@@ -35,7 +35,9 @@ def _row_stride(t, cols, name):
 
 
 class MlpBlock8:
-    """Parameters and gradients: dicts of fp32 tensors ln_g, ln_b [D], w1 [H, D], b1 [H], w2 [D, H], b2 [D]."""
+    """Parameters and gradients: dicts of fp32 tensors ln_g, ln_b [D], w1 [H, D], b1 [H], w2 [D, H], b2 [D]. Contiguous
+    fp32 parameters are used where they are, not copied: an optimizer over them, or over `p`, updates both. An object
+    has one workspace and belongs to one stream at a time."""
 
     def __init__(self, params, eps=1e-6):
         self.p = {k: v.detach().float().contiguous() for k, v in params.items()}

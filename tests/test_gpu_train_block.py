@@ -197,3 +197,23 @@ def test_block_without_rows():
     torch.cuda.synchronize()
     for k, v in b.grads.items():
         assert not v.any(), k
+
+
+def test_example_leaves_its_teacher(monkeypatch):
+    torch = torch_cuda()
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    try:
+        import tune_mlp
+    finally:
+        sys.path.pop(0)
+    made = []
+
+    class Kept(tune_mlp.MlpBlock8):
+        def __init__(self, *args):
+            super().__init__(*args)
+            made.append((self, {k: v.clone() for k, v in self.p.items()}))
+    monkeypatch.setattr(tune_mlp, "MlpBlock8", Kept)
+    tune_mlp.tune(256, 512, 3)
+    teacher, was = made[0]
+    for k, v in teacher.p.items():
+        assert torch.equal(v, was[k]), k
