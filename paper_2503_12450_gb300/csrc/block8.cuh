@@ -40,15 +40,6 @@ __device__ __forceinline__ float2 e4m3x2_to_f2(uint32_t two) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
-__device__ __forceinline__ float4 e4m3x4_to_f4(uint32_t four, float s) {
-  const float2 a = e4m3x2_to_f2(four & 0xFFFFu), b = e4m3x2_to_f2(four >> 16);
-  return make_float4(a.x * s, a.y * s, b.x * s, b.y * s);
-}
-
-__device__ __forceinline__ float4 f4_nonfinite_to(float4 v, float to) {
-  auto f = [&](float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u ? to : x; };
-  return make_float4(f(v.x), f(v.y), f(v.z), f(v.w));
-}
 
 // Two blocks of 128 columns in a warp, one in each half, eight consecutive
 // columns a lane, to E4M3: the scale byte of the lane's block and the lane's
