@@ -542,7 +542,7 @@ lazymar_status lazymar_block8_gelu_backward(int dtype, const void* da, int ldda,
  *   LAZYMAR_EPI_BIAS      out = y
  *   LAZYMAR_EPI_GELU      out = GELU(y) (erf form)
  *   LAZYMAR_EPI_RESIDUAL  out = residual + y, residual [M, ldr] and out fp32
- *                         (out may be residual itself)
+ *                         (out may be residual itself, ldo = ldr)
  * out [M, ldo] fp32 or bf16 (may be NULL) and / or out8 [M, N] (may be NULL; not
  * for RESIDUAL); u8 [M, N] (GELU only, may be NULL) receives y, the checkpoint
  * for lazymar_block8_gelu_backward. Any M, N >= 0 and K >= 1. */

@@ -194,6 +194,7 @@ extern "C" lazymar_status lazymar_block8_gelu_backward(int dtype, const void* da
   if (rows > kMost || cols > kMost) return too_large();
   if (rows > 0) {
     if (!du && !du8 && !db) return bad("no output given");
+    if (du && du == da && (du_dtype != dtype || (rows > 1 && lddu != ldda))) return bad("du in place of da: the same type and stride required");
     TR_TRY(check_mat(da, dtype, ldda, cols, "da: fp32 or bf16 device tensor, ldda >= cols required"));
     if (u)
       TR_TRY(check_block8(u, cols, rows, "u: device tensors, 16-byte aligned, ldq % 16 == 0, ldq >= cols, lds >= rows"));
@@ -239,6 +240,7 @@ extern "C" lazymar_status lazymar_block8_linear(int epilogue, const lazymar_bloc
   }
   if (u8 && epilogue != LAZYMAR_EPI_GELU) return bad("u8 is for LAZYMAR_EPI_GELU");
   if (empty) return LAZYMAR_OK;
+  if (residual && out == residual && M > 1 && ldo != ldr) return bad("out in place of residual: the same stride required");
   TR_TRY(check_block8(a, K, M, "a: device tensors, 16-byte aligned, ldq % 16 == 0, ldq >= K, lds >= M"));
   TR_TRY(check_block8(w, K, (N + 127) / 128,
                       "w: device tensors, 16-byte aligned, ldq % 16 == 0, ldq >= K, lds >= ceil(N / 128)"));

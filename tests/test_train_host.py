@@ -218,3 +218,12 @@ def test_empty_tensors_without_an_address_are_fine(lib):
     # what cannot be meant is refused all the same
     assert lib.lazymar_block8_linear(2, q.addr, q.addr, None, None, 8, 1, None, 8, None, None, 0, 8, 8, None) == 1
     assert lib.lazymar_block8_linear(0, q.addr, None, None, None, 8, 0, None, 8, None, None, 0, 8, 8, None) == 1
+
+
+def test_in_place_needs_the_same_layout(lib):
+    q = _b8()
+    for dtype, ld in ((0, 8), (1, 16)):
+        assert lib.lazymar_block8_gelu_backward(1, 16, 8, None, dtype, 16, ld, None, None, 0, 4, 8, None, 0, None) == 1
+        assert "in place" in lib.lazymar_last_error().decode()
+    assert lib.lazymar_block8_linear(2, q.addr, q.addr, None, 16, 8, 0, 16, 16, None, None, 4, 8, 8, None) == 1
+    assert "in place" in lib.lazymar_last_error().decode()
