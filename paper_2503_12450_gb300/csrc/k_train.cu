@@ -17,6 +17,10 @@ namespace {
 
 constexpr int kSMs = 152;
 constexpr int kChunk = 256;  // columns of a warp: two blocks
+// A chunk in shared memory on its way between lanes: one float more after every 32,
+// so that neither every 32nd column a lane nor eight consecutive ones meet in a bank.
+constexpr int kStage = kChunk + kChunk / 32;
+__device__ __forceinline__ int staged(int i) { return i + (i >> 5); }
 
 // ---------------------------------------------------------------------------
 // Eight columns of a row
@@ -47,7 +51,7 @@ __device__ __forceinline__ void st8a(bf16* p, const float (&v)[8]) {
       make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 // A warp's 256 columns from c0 on, eight a lane; columns from D on read as zero
-// and are not written. Rows off the boundary go through the warp's 256 floats of
+// and are not written. Rows off the boundary go through the warp's kStage floats of
 // shared memory, so that the accesses of a warp stay contiguous. Every lane of
 // the warp takes part.
 template <typename T>
@@ -66,11 +70,11 @@ __device__ __forceinline__ void ld8(const T* row, int c0, int D, bool vec, float
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int c = c0 + 32 * i + lane;
-    sm[32 * i + lane] = c < D ? to_f(row[c]) : 0.f;
+    sm[33 * i + lane] = c < D ? to_f(row[c]) : 0.f;
   }
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = sm[8 * lane + i];
+  for (int i = 0; i < 8; ++i) v[i] = sm[staged(8 * lane) + i];
 }
 template <typename T>
 __device__ __forceinline__ void st8(T* row, int c0, int D, bool vec, float* sm, const float (&v)[8]) {
@@ -87,12 +91,12 @@ __device__ __forceinline__ void st8(T* row, int c0, int D, bool vec, float* sm, 
   }
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sm[8 * lane + i] = v[i];
+  for (int i = 0; i < 8; ++i) sm[staged(8 * lane) + i] = v[i];
   __syncwarp();
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int c = c0 + 32 * i + lane;
-    if (c < D) row[c] = from_f<T>(sm[32 * i + lane]);
+    if (c < D) row[c] = from_f<T>(sm[33 * i + lane]);
   }
 }
 // FULL: every column exists and the row is on the boundary.
@@ -233,7 +237,7 @@ template <int NC, int WPR, bool FULL>
 __global__ void __launch_bounds__(256, 4) ln_forward_kernel(const LnForward p) {
   constexpr int GROUPS = 8 / WPR;
   __shared__ float red[2][GROUPS][WPR];
-  __shared__ float stage[FULL ? 1 : 8][kChunk];
+  __shared__ float stage[FULL ? 1 : 8][kStage];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
   float* sm = stage[FULL ? 0 : warp];
   const int D = p.D, row = blockIdx.x * GROUPS + grp, c0 = part * NC * kChunk;
@@ -767,7 +771,7 @@ __global__ void __launch_bounds__(256, HAS_U ? 3 : 4) rows8_kernel(const Rows8 p
   const int task = (int)blockIdx.x * 8 + warp;
   const int grp = task / nchunk, c0 = (task - grp * nchunk) * kChunk, col = c0 + 8 * lane, cols = p.cols;
   __shared__ float grad[HAS_U ? kGradSize : 1];
-  __shared__ float stage[VEC ? 1 : 8][kChunk];
+  __shared__ float stage[VEC ? 1 : 8][kStage];
   float* sm = stage[VEC ? 0 : warp];
   if (HAS_U) {
     gelu_grad_table(grad);
@@ -872,7 +876,7 @@ int rows8_groups(int rows, int nchunk, bool has_u) {
 template <typename T>
 __global__ void __launch_bounds__(256, 4) unpack8_kernel(const lazymar_block8 q, T* __restrict__ x, int ld, int rows,
                                                          int cols, int nchunk, bool vec) {
-  __shared__ float stage[8][kChunk];
+  __shared__ float stage[8][kStage];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_wait();
   pdl_trigger();
