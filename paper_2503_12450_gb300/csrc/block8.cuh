@@ -151,6 +151,7 @@ struct MatOut {
 struct LnForward {
   Mat x;
   const float *g, *b;
+  bool params_vec;         // g and b on boundaries of eight elements (or NULL)
   MatOut y;                // p may be NULL
   lazymar_block8 y8, x8;   // q may be NULL
   float *mean, *rstd;      // may be NULL

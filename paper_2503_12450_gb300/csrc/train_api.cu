@@ -75,6 +75,7 @@ extern "C" lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, 
   p.x = mat(x, ldx, x_dtype);
   p.g = g;
   p.b = b;
+  p.params_vec = at(g, 32) && at(b, 32);
   p.y = mat_out(y, ldy, y_dtype);
   p.y8 = given(y8);
   p.x8 = given(x8);
