@@ -86,7 +86,8 @@ struct Params {
   int ldout8, ldu8;
   uint8_t *out8_scale, *u8_scale;
   int lds_out8, lds_u8;
-  bool bias_vec, out_vec, res_vec;
+  bool bias_vec;
+  bool rows_vec;  // rows of out and residual on boundaries of four elements
 };
 
 // Instruction descriptor of kind::mxf8f6f4: E4M3 operands (format 0), K-major,
@@ -482,7 +483,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       if (p.out && col < p.N) {
         if (p.out_dtype == LAZYMAR_F32) {
           float* y = static_cast<float*>(p.out) + (size_t)row * p.ldo + col;
-          if (p.out_vec && col + 4 <= p.N) {
+          if (p.rows_vec && col + 4 <= p.N) {
             *reinterpret_cast<float4*>(y) = make_float4(u[0], u[1], u[2], u[3]);
           } else {
 #pragma unroll
@@ -491,7 +492,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
           }
         } else {
           bf16* y = static_cast<bf16*>(p.out) + (size_t)row * p.ldo + col;
-          if (p.out_vec && col + 4 <= p.N) {
+          if (p.rows_vec && col + 4 <= p.N) {
             *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]));
           } else {
 #pragma unroll
@@ -525,7 +526,16 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
       // the residual of 32 columns, eight passes of four rows; the first ones'
       // before the accumulator is ready
       float4 res[8];
+      // (rows off the boundary: a row an access, lane = column, so that the accesses
+      // stay contiguous; row r is the r % 4th of res[r / 4])
       auto load_res = [&](int c) {
+        if (!p.rows_vec) {
+          const int col = n0 + 32 * ((c + rot) & 3) + lane;
+          auto at = [&](int r) { return col < p.N && rbase + r < p.M ? p.residual[(size_t)(rbase + r) * p.ldr + col] : 0.f; };
+#pragma unroll
+          for (int q = 0; q < 8; ++q) res[q] = make_float4(at(4 * q), at(4 * q + 1), at(4 * q + 2), at(4 * q + 3));
+          return;
+        }
         const int col = n0 + 32 * ((c + rot) & 3) + 4 * cq;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
@@ -533,7 +543,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
           res[q] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (r >= p.M || col >= p.N) continue;
           const float* x = p.residual + (size_t)r * p.ldr + col;
-          if (p.res_vec && col + 4 <= p.N) {
+          if (col + 4 <= p.N) {
             res[q] = *reinterpret_cast<const float4*>(x);
           } else {
             res[q].x = x[0];
@@ -663,6 +673,35 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
             *reinterpret_cast<float4*>(stg + lane * 128 + ((j ^ (lane & 7)) << 4)) =
                 make_float4(v[32 * c + 4 * j], v[32 * c + 4 * j + 1], v[32 * c + 4 * j + 2], v[32 * c + 4 * j + 3]);
           __syncwarp();
+          if (!p.rows_vec) {
+            // a row an access, lane = column: four scalars a lane would touch four times
+            // the sectors (37823 x 699 x 768, bf16 and a checkpoint: 85 us)
+            const int one = n0 + 32 * ((c + rot) & 3) + lane;
+            float e[32];
+#pragma unroll
+            for (int r = 0; r < 32; ++r)
+              e[r] = *reinterpret_cast<const float*>(stg + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + ((lane & 3) << 2));
+            if (OUT == OUT_RESIDUAL) {
+#pragma unroll
+              for (int q = 0; q < 8; ++q) {
+                e[4 * q] += res[q].x;
+                e[4 * q + 1] += res[q].y;
+                e[4 * q + 2] += res[q].z;
+                e[4 * q + 3] += res[q].w;
+              }
+              if (c < 3) load_res(c + 1);
+            }
+            if (one < p.N) {
+              const size_t first_at = (size_t)rbase * p.ldo + one;
+#pragma unroll
+              for (int r = 0; r < 32; ++r) {
+                if (rbase + r >= p.M) break;
+                if (p.out_dtype == LAZYMAR_F32) static_cast<float*>(p.out)[first_at + (size_t)r * p.ldo] = e[r];
+                else static_cast<bf16*>(p.out)[first_at + (size_t)r * p.ldo] = from_f<bf16>(e[r]);
+              }
+            }
+            continue;
+          }
           float4 o[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
@@ -682,7 +721,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
             if (r >= p.M || col >= p.N) continue;
             if (p.out_dtype == LAZYMAR_F32) {
               float* y = static_cast<float*>(p.out) + (size_t)r * p.ldo + col;
-              if (p.out_vec && col + 4 <= p.N) {
+              if (col + 4 <= p.N) {
                 *reinterpret_cast<float4*>(y) = o[q];
               } else {
                 y[0] = o[q].x;
@@ -692,7 +731,7 @@ __global__ void __launch_bounds__(l8::THREADS, 1)
               }
             } else {
               bf16* y = static_cast<bf16*>(p.out) + (size_t)r * p.ldo + col;
-              if (p.out_vec && col + 4 <= p.N) {
+              if (col + 4 <= p.N) {
                 *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16(o[q].x, o[q].y), pack_bf16(o[q].z, o[q].w));
               } else {
                 y[0] = from_f<bf16>(o[q].x);
@@ -832,8 +871,8 @@ cudaError_t launch_linear8(const Ctx& c, const Linear8& x) {
   p.ldu8 = x.u8.ldq;
   const auto at = [](const void* q, size_t n) { return reinterpret_cast<uintptr_t>(q) % n == 0; };
   p.bias_vec = at(x.bias, 16);
-  p.out_vec = x.out.ld % 4 == 0 && at(x.out.p, x.out.dtype == LAZYMAR_F32 ? 16 : 8);
-  p.res_vec = x.residual.ld % 4 == 0 && at(x.residual.p, 16);
+  p.rows_vec = x.out.ld % 4 == 0 && at(x.out.p, x.out.dtype == LAZYMAR_F32 ? 16 : 8) && x.residual.ld % 4 == 0 &&
+               at(x.residual.p, 16);
   const Shape shape = choose(c.num_sms, x.M, x.N, x.K);
   if (shape.pair) return run_linear8<true>(c, ta, tb, to, tu, p, shape.tiles);
   if (shape.parts > 1) return run_linear8<false, OUT_PLAIN, true>(c, ta, tb, to, tu, p, shape.tiles, shape.parts);
