@@ -50,28 +50,38 @@ __device__ __forceinline__ void st8a(bf16* p, const float (&v)[8]) {
   *reinterpret_cast<uint4*>(p) =
       make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
-// A warp's 256 columns from c0 on, eight a lane; columns from D on read as zero
-// and are not written. Rows off the boundary go through the warp's kStage floats of
-// shared memory, so that the accesses of a warp stay contiguous. Every lane of
-// the warp takes part.
+// A warp's 256 columns from c0 on, eight consecutive ones a lane; columns from D on
+// read as zero and are not written. Rows off the boundary are loaded with every 32nd
+// column a lane (ld8s), so that the accesses of a warp stay contiguous, and turned
+// through the warp's kStage floats of shared memory. That is a step of its own
+// (turn8), and the elements are widened there, so that all loads are under way
+// before the first is waited for. Every lane of the warp takes part.
 template <typename T>
-__device__ __forceinline__ void ld8(const T* row, int c0, int D, bool vec, float* sm, float (&v)[8]) {
-  const int lane = threadIdx.x & 31, col = c0 + 8 * lane;
-  if (vec) {
-    if (col + 8 <= D) {
-      ld8a(row + col, v);
-    } else {
+__device__ __forceinline__ void ld8(const T* row, int c0, int D, float (&v)[8]) {
+  const int col = c0 + 8 * (int)(threadIdx.x & 31);
+  if (col + 8 <= D) {
+    ld8a(row + col, v);
+  } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = col + i < D ? to_f(row[col + i]) : 0.f;
-    }
-    return;
+    for (int i = 0; i < 8; ++i) v[i] = col + i < D ? to_f(row[col + i]) : 0.f;
   }
-  __syncwarp();
+}
+__device__ __forceinline__ void ld8s(const Mat& m, size_t row, int c0, int D, uint32_t (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int c = c0 + 32 * i + lane;
-    sm[33 * i + lane] = c < D ? to_f(row[c]) : 0.f;
+    const int c = c0 + 32 * i + (int)(threadIdx.x & 31);
+    v[i] = 0u;
+    if (c < D)
+      v[i] = m.dtype == LAZYMAR_F32 ? static_cast<const uint32_t*>(m.p)[row * m.ld + c]
+                                    : static_cast<const uint16_t*>(m.p)[row * m.ld + c];
   }
+}
+// Every 32nd column a lane, as loaded, to eight consecutive ones.
+__device__ __forceinline__ void turn8(float* sm, const uint32_t (&raw)[8], int shift, float (&v)[8]) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sm[33 * i + lane] = __uint_as_float(raw[i] << shift);
   __syncwarp();
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = sm[staged(8 * lane) + i];
@@ -101,15 +111,15 @@ __device__ __forceinline__ void st8(T* row, int c0, int D, bool vec, float* sm, 
 }
 // FULL: every column exists and the row is on the boundary.
 template <bool FULL>
-__device__ __forceinline__ void ld_mat(const Mat& m, size_t row, int c0, int D, float* sm, float (&v)[8]) {
+__device__ __forceinline__ void ld_mat(const Mat& m, size_t row, int c0, int D, float (&v)[8]) {
   if (m.dtype == LAZYMAR_F32) {
     const float* r = static_cast<const float*>(m.p) + row * m.ld;
     if (FULL) ld8a(r + c0 + 8 * (threadIdx.x & 31), v);
-    else ld8<float>(r, c0, D, m.vec, sm, v);
+    else ld8<float>(r, c0, D, v);
   } else {
     const bf16* r = static_cast<const bf16*>(m.p) + row * m.ld;
     if (FULL) ld8a(r + c0 + 8 * (threadIdx.x & 31), v);
-    else ld8<bf16>(r, c0, D, m.vec, sm, v);
+    else ld8<bf16>(r, c0, D, v);
   }
 }
 template <bool FULL>
@@ -235,6 +245,7 @@ __device__ __forceinline__ float row_sum(float v, float* red, int part) {
 // FULL: D = 256 NC WPR and aligned rows, so that no column needs a check.
 // 40960 x 1024 fp32 with statistics, 8-bit output and 8-bit copy of the input: 43.7
 // us, 5.8 TB/s (floor 37 at 6.8); without paired instructions 47, four columns a lane 67.
+// 40000 x 1013, off the boundary: 76 (floor 36); with a wait for each chunk 99.
 template <int NC, int WPR, bool FULL>
 __global__ void __launch_bounds__(256, 4) ln_forward_kernel(const LnForward p) {
   constexpr int GROUPS = 8 / WPR;
@@ -250,7 +261,17 @@ __global__ void __launch_bounds__(256, 4) ln_forward_kernel(const LnForward p) {
   float s = 0.f;
   if (live) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) ld_mat<FULL>(p.x, row, c0 + c * kChunk, D, sm, v[c]);
+    for (int c = 0; c < NC; ++c) {
+      if (FULL || p.x.vec) ld_mat<FULL>(p.x, row, c0 + c * kChunk, D, v[c]);
+    }
+    if (!FULL && !p.x.vec) {
+      const int shift = p.x.dtype == LAZYMAR_F32 ? 0 : 16;
+      uint32_t raw[NC][8];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) ld8s(p.x, row, c0 + c * kChunk, D, raw[c]);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) turn8(sm, raw[c], shift, v[c]);
+    }
 #pragma unroll
     for (int c = 0; c < NC; ++c) s += sum8(v[c]);
   }
@@ -540,18 +561,8 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
 // contiguous without a boundary), dy and x in registers, the next row's on their
 // way. 4801 x 777 bf16: 17 us, four rounds of a row's latency (24 without the next
 // row ahead; floor 3.3).
-// A row's elements as loaded, widened at their use: the next row is under way in
-// registers while this one is worked on (and a use would wait for it).
-__device__ __forceinline__ void ld8s(const Mat& m, size_t row, int c0, int D, uint32_t (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int c = c0 + 32 * i + (int)(threadIdx.x & 31);
-    v[i] = 0u;
-    if (c < D)
-      v[i] = m.dtype == LAZYMAR_F32 ? static_cast<const uint32_t*>(m.p)[row * m.ld + c]
-                                    : static_cast<const uint16_t*>(m.p)[row * m.ld + c];
-  }
-}
+// (The elements are widened at their use: the next row is under way in registers
+// while this one is worked on, and a use would wait for it.)
 template <int NC, int WPR>
 __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_backward_kernel(const LnBackward p) {
   constexpr int WARPS = WPR > 8 ? WPR : 8, GROUPS = WARPS / WPR, W = NC * WPR * kChunk;
@@ -760,13 +771,13 @@ __device__ __forceinline__ float gelu_grad_at(const float* tab, float x) {
 // stride of rows, U at a time (bytes in flight), so that the column sums stay in its registers;
 // neighbouring warps take neighbouring columns of the same rows.
 // VEC: rows on boundaries and cols a multiple of eight, so that a lane's columns
-// all exist or none does; otherwise a row at a time, through shared memory
-// where it is off the boundary.
+// all exist or none does; otherwise every 32nd column a lane, turned in shared
+// memory (20480 x 4001 bf16 to 8 bits 63 us; with one row in flight 94).
 // 40960 x 4096, bf16 in and out, 8-bit out, bias gradient: 168 us, 6.0 TB/s (floor
 // 148); four columns a lane and a polynomial for the gradient took 499.
 template <typename T, bool HAS_U, bool VEC>
 __global__ void __launch_bounds__(256, HAS_U ? 3 : 4) rows8_kernel(const Rows8 p, int nchunk, int groups) {
-  constexpr int U = !VEC ? 1 : sizeof(T) == 4 ? 2 : 4;  // rows in flight, as registers allow
+  constexpr int U = sizeof(T) == 4 ? 2 : 4;  // rows in flight, as registers allow
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int task = (int)blockIdx.x * 8 + warp;
   const int grp = task / nchunk, c0 = (task - grp * nchunk) * kChunk, col = c0 + 8 * lane, cols = p.cols;
@@ -789,7 +800,8 @@ __global__ void __launch_bounds__(256, HAS_U ? 3 : 4) rows8_kernel(const Rows8 p
   const uint8_t* us = HAS_U ? p.u.scale + (size_t)(at / kBlk) * p.u.lds : nullptr;
   for (int r0 = grp * U; r0 < p.rows; r0 += groups * U) {
     constexpr int W = sizeof(T) / 2;
-    uint4 raw[U][W];
+    uint4 raw[VEC ? U : 1][W];
+    uint32_t one[VEC ? 1 : U][8];  // every 32nd column
     uint2 uq[U];
     uint32_t ub[U];
 #pragma unroll
@@ -799,6 +811,8 @@ __global__ void __launch_bounds__(256, HAS_U ? 3 : 4) rows8_kernel(const Rows8 p
         const uint4* src = reinterpret_cast<const uint4*>(in + r * p.in.ld + at);
 #pragma unroll
         for (int k = 0; k < W; ++k) raw[j][k] = src[k];
+      } else {
+        ld8s(Mat{p.in.p, p.in.ld, W == 1 ? LAZYMAR_BF16 : LAZYMAR_F32, false}, r, c0, cols, one[j]);
       }
       if (HAS_U) {
         const uint8_t* q = static_cast<const uint8_t*>(p.u.q) + r * p.u.ldq;
@@ -812,7 +826,7 @@ __global__ void __launch_bounds__(256, HAS_U ? 3 : 4) rows8_kernel(const Rows8 p
       const size_t r = (size_t)(r0 + j);
       float v[8];
       if constexpr (!VEC) {
-        ld8<T>(in + r * p.in.ld, c0, cols, p.in.vec, sm, v);
+        turn8(sm, one[j], W == 1 ? 16 : 0, v);
       } else if constexpr (W == 1) {
         bf16x8(raw[j][0], v);
       } else {
