@@ -559,13 +559,23 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
 // Any width, stride and alignment: WPR warps a row, NC chunks of 256 columns a
 // warp, every 32nd column of a chunk a lane (so that a warp's accesses are
 // contiguous without a boundary), dy and x in registers, the next row's on their
-// way. 4801 x 777 bf16: 17 us, four rounds of a row's latency (24 without the next
-// row ahead; floor 3.3).
+// way. Up to 1280 columns one chunk a warp: as many warps as the width needs, and the
+// gains stay in registers. Only a row's own warps wait for each other. Measured (us, in
+// brackets with two chunks a warp, all of a CTA waiting, and the residual loaded where it
+// is added): 4801 x 777 bf16 13.3 (16.8; floor 3.3), 36071 x 1254 94 (174; floor 67), 20000
+// x 777 from 8 bits with residual 45 (188; floor 21), 20000 x 1013 fp32 47 (62; floor 36).
 // (The elements are widened at their use: the next row is under way in registers
 // while this one is worked on, and a use would wait for it.)
+// Warps of a CTA and CTAs on an SM, so that a thread has 128 registers (ten warps with
+// 96 each spill: 185 us at 36071 x 1254 instead of 107).
+template <int WPR>
+constexpr int kLnWarps = WPR > 8 ? 16 : WPR == 5 ? 5 : 8;
+template <int WPR>
+constexpr int kLnCtas = WPR > 8 ? 1 : WPR == 5 ? 3 : 2;
+
 template <int NC, int WPR>
-__global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_backward_kernel(const LnBackward p) {
-  constexpr int WARPS = WPR > 8 ? WPR : 8, GROUPS = WARPS / WPR, W = NC * WPR * kChunk;
+__global__ void __launch_bounds__(kLnWarps<WPR> * 32, kLnCtas<WPR>) ln_backward_kernel(const LnBackward p) {
+  constexpr int GROUPS = kLnWarps<WPR> / WPR, W = NC * WPR * kChunk;
   extern __shared__ float cols[];  // [2][W]
   __shared__ float red[2][2][GROUPS][WPR];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
@@ -578,7 +588,13 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_
   for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dg[c][i] = db[c][i] = 0.f;
-  const int stride = (int)gridDim.x * GROUPS;
+  float g[NC == 1 ? 8 : 1];
+  if constexpr (NC == 1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = p.g && c0 + 32 * i + lane < D ? p.g[c0 + 32 * i + lane] : 1.f;
+  }
+  const int step = (int)gridDim.x * GROUPS;
+  const long long first = (long long)blockIdx.x * GROUPS + grp;
   uint32_t ry[NC][8], rx[NC][8], rs[NC][2];
   float rmean = 0.f, rrstd = 0.f;
   auto fetch = [&](long long row) {
@@ -605,38 +621,46 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_
     }
   };
   int it = 0;
-  fetch((long long)blockIdx.x * GROUPS + grp);
-  // (every warp makes the same number of rounds: the row sums are a CTA-wide step)
-  for (long long base = (long long)blockIdx.x * GROUPS; base < p.M; base += stride, it ^= 1) {
-    const long long row = base + grp;
-    const bool live = row < p.M;
-    float h[NC][8], a[NC][8], s1 = 0.f, s2 = 0.f, rstd = 0.f;
-    if (live) {
-      const float mean = rmean;
-      rstd = rrstd;
+  fetch(first);
+  for (long long row = first; row < p.M; row += step, it ^= 1) {
+    float h[NC][8], a[NC][8], s1 = 0.f, s2 = 0.f;
+    const float mean = rmean, rstd = rrstd;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const float sc[2] = {block8_scale(rs[c][0]), block8_scale(rs[c][1])};
+    for (int c = 0; c < NC; ++c) {
+      const float sc[2] = {block8_scale(rs[c][0]), block8_scale(rs[c][1])};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          a[c][i] = __uint_as_float(ry[c][i] << dy_shift);
-          h[c][i] = p.x.p ? __uint_as_float(rx[c][i] << x_shift) : e4m3x2_to_f2(rx[c][i]).x * sc[i >> 2];
-        }
+      for (int i = 0; i < 8; ++i) {
+        a[c][i] = __uint_as_float(ry[c][i] << dy_shift);
+        h[c][i] = p.x.p ? __uint_as_float(rx[c][i] << x_shift) : e4m3x2_to_f2(rx[c][i]).x * sc[i >> 2];
       }
-      fetch(row + stride);
+    }
+    fetch(row + step);
+    // the residual's row: all of it under way before the first is added (dx's stores
+    // would wait for each), with one chunk a warp already during the sums
+    float r[NC][8];
+    auto residual = [&] {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int k = c0 + c * kChunk + 32 * i + lane;
-          const float x = k < D ? (h[c][i] - mean) * rstd : 0.f, g = p.g && k < D ? p.g[k] : 1.f;
-          h[c][i] = x;
-          dg[c][i] = fmaf(a[c][i], x, dg[c][i]);
-          db[c][i] += a[c][i];
-          a[c][i] *= g;
-          s1 += a[c][i];
-          s2 = fmaf(a[c][i], x, s2);
+          r[c][i] = k < D ? static_cast<const float*>(p.dres.p)[(size_t)row * p.dres.ld + k] : 0.f;
         }
+    };
+    if (NC == 1 && p.dres.p) residual();
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = c0 + c * kChunk + 32 * i + lane;
+        const float x = k < D ? (h[c][i] - mean) * rstd : 0.f;
+        const float gain = NC == 1 ? g[i & (NC == 1 ? 7 : 0)] : p.g && k < D ? p.g[k] : 1.f;
+        h[c][i] = x;
+        dg[c][i] = fmaf(a[c][i], x, dg[c][i]);
+        db[c][i] += a[c][i];
+        a[c][i] *= gain;
+        s1 += a[c][i];
+        s2 = fmaf(a[c][i], x, s2);
       }
     }
     s1 = warp_sum(s1);
@@ -646,7 +670,7 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_
         red[it][0][grp][part] = s1;
         red[it][1][grp][part] = s2;
       }
-      __syncthreads();
+      asm volatile("bar.sync %0, %1;" ::"r"(grp + 1), "n"(WPR * 32) : "memory");  // the row's warps
       s1 = s2 = 0.f;
 #pragma unroll
       for (int i = 0; i < WPR; ++i) {
@@ -654,20 +678,28 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_
         s2 += red[it][1][grp][i];
       }
     }
-    if (live) {
-      s1 /= (float)D;
-      s2 /= (float)D;
+    s1 /= (float)D;
+    s2 /= (float)D;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int k = c0 + c * kChunk + 32 * i + lane;
-          if (k >= D) continue;
-          float o = rstd * (a[c][i] - s1 - h[c][i] * s2);
-          if (p.dres.p) o += static_cast<const float*>(p.dres.p)[(size_t)row * p.dres.ld + k];
-          if (p.dx.dtype == LAZYMAR_F32) static_cast<float*>(p.dx.p)[(size_t)row * p.dx.ld + k] = o;
-          else static_cast<bf16*>(p.dx.p)[(size_t)row * p.dx.ld + k] = from_f<bf16>(o);
-        }
+      for (int i = 0; i < 8; ++i) a[c][i] = rstd * (a[c][i] - s1 - h[c][i] * s2);
+    if (p.dres.p) {
+      if (NC > 1) residual();
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[c][i] += r[c][i];
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = c0 + c * kChunk + 32 * i + lane;
+        if (k >= D) continue;
+        const float o = a[c][i];
+        if (p.dx.dtype == LAZYMAR_F32) static_cast<float*>(p.dx.p)[(size_t)row * p.dx.ld + k] = o;
+        else static_cast<bf16*>(p.dx.p)[(size_t)row * p.dx.ld + k] = from_f<bf16>(o);
       }
     }
   }
@@ -691,9 +723,9 @@ __global__ void __launch_bounds__(WPR > 8 ? WPR * 32 : 256, WPR > 8 ? 1 : 2) ln_
   for (int i = threadIdx.x; i < 2 * D; i += blockDim.x) o[i] = i < D ? cols[i] : cols[W + i - D];
 }
 
-// CTAs of a backward launch: at most two resident ones for every SM.
-int ln_backward_ctas(int M, int groups) {
-  const int need = (M + groups - 1) / groups, most = 2 * kSMs;
+// CTAs of a backward launch: the resident ones of every SM (three at most), as far as there are rows.
+int ln_backward_ctas(int M, int groups, int per_sm) {
+  const int need = (M - 1) / groups + 1, most = per_sm * kSMs;
   return need < most ? need : most;
 }
 
@@ -719,8 +751,7 @@ cudaError_t ln_backward_ring_run(const Ctx& c, const LnBackward& p, int* ctas) {
   size_t smem = (size_t)warps * depth * row_b;
   const size_t sums = (size_t)2 * W * WPR * 4;
   if (smem < sums) smem = sums;
-  const int groups = warps / WPR, need = (p.M + groups - 1) / groups, most = per_sm * kSMs;
-  *ctas = need < most ? need : most;
+  *ctas = ln_backward_ctas(p.M, warps / WPR, per_sm);
   const auto kernel = ln_backward_ring_kernel<NB, WPR>;
   cudaError_t e = big_smem(reinterpret_cast<const void*>(kernel), smem);
   if (e != cudaSuccess) return e;
@@ -730,9 +761,9 @@ cudaError_t ln_backward_ring_run(const Ctx& c, const LnBackward& p, int* ctas) {
 
 template <int NC, int WPR>
 cudaError_t ln_backward_run(const Ctx& c, const LnBackward& p, int* ctas) {
-  constexpr int WARPS = WPR > 8 ? WPR : 8;
+  constexpr int WARPS = kLnWarps<WPR>;
   constexpr size_t smem = (size_t)2 * NC * WPR * kChunk * sizeof(float);
-  *ctas = ln_backward_ctas(p.M, WARPS / WPR);
+  *ctas = ln_backward_ctas(p.M, WARPS / WPR, kLnCtas<WPR>);
   cudaError_t e = big_smem(reinterpret_cast<const void*>(ln_backward_kernel<NC, WPR>), smem);
   if (e != cudaSuccess) return e;
   return launch_pdl(ln_backward_kernel<NC, WPR>, dim3((unsigned)*ctas), dim3(WARPS * 32), smem, c.stream, p);
@@ -1021,7 +1052,7 @@ cudaError_t launch_ln_forward(const Ctx& c, const LnForward& p) {
 }
 
 size_t ln_backward_workspace(int M, int D) {
-  return M > 0 && D > 0 ? (size_t)ln_backward_ctas(M, 1) * 2 * D * sizeof(float) : 0;
+  return M > 0 && D > 0 ? (size_t)ln_backward_ctas(M, 1, 3) * 2 * D * sizeof(float) : 0;
 }
 
 cudaError_t launch_ln_backward(const Ctx& c, const LnBackward& p) {
@@ -1045,8 +1076,9 @@ cudaError_t launch_ln_backward(const Ctx& c, const LnBackward& p) {
                    : ln_backward_ring_run<4, 8>(c, p, &ctas);
   } else {
     e = nc <= 1    ? ln_backward_run<1, 1>(c, p, &ctas)
-        : nc <= 2  ? ln_backward_run<2, 1>(c, p, &ctas)
-        : nc <= 4  ? ln_backward_run<2, 2>(c, p, &ctas)
+        : nc <= 2  ? ln_backward_run<1, 2>(c, p, &ctas)
+        : nc <= 4  ? ln_backward_run<1, 4>(c, p, &ctas)
+        : nc <= 5  ? ln_backward_run<1, 5>(c, p, &ctas)
         : nc <= 8  ? ln_backward_run<2, 4>(c, p, &ctas)
         : nc <= 16 ? ln_backward_run<2, 8>(c, p, &ctas)
                    : ln_backward_run<2, 16>(c, p, &ctas);
