@@ -559,11 +559,12 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
 // Any width, stride and alignment: WPR warps a row, NC chunks of 256 columns a
 // warp, every 32nd column of a chunk a lane (so that a warp's accesses are
 // contiguous without a boundary), dy and x in registers, the next row's on their
-// way. Up to 1280 columns one chunk a warp: as many warps as the width needs, and the
-// gains stay in registers. Only a row's own warps wait for each other. Measured (us, in
+// way. Up to 4096 columns one chunk a warp, so that nothing spills and the gains stay
+// in registers. Only a row's own warps wait for each other. Measured (us, in
 // brackets with two chunks a warp, all of a CTA waiting, and the residual loaded where it
 // is added): 4801 x 777 bf16 13.3 (16.8; floor 3.3), 36071 x 1254 94 (174; floor 67), 20000
-// x 777 from 8 bits with residual 45 (188; floor 21), 20000 x 1013 fp32 47 (62; floor 36).
+// x 777 from 8 bits with residual 45 (188; floor 21), x 1601 the same 87 (183; floor 52), 20000 x
+// 1013 fp32 47 (62; floor 36), 5000 x 4001 bf16 44 (54; floor 18).
 // (The elements are widened at their use: the next row is under way in registers
 // while this one is worked on, and a use would wait for it.)
 // Warps of a CTA and CTAs on an SM, so that a thread has 128 registers (ten warps with
@@ -1079,8 +1080,8 @@ cudaError_t launch_ln_backward(const Ctx& c, const LnBackward& p) {
         : nc <= 2  ? ln_backward_run<1, 2>(c, p, &ctas)
         : nc <= 4  ? ln_backward_run<1, 4>(c, p, &ctas)
         : nc <= 5  ? ln_backward_run<1, 5>(c, p, &ctas)
-        : nc <= 8  ? ln_backward_run<2, 4>(c, p, &ctas)
-        : nc <= 16 ? ln_backward_run<2, 8>(c, p, &ctas)
+        : nc <= 8  ? ln_backward_run<1, 8>(c, p, &ctas)
+        : nc <= 16 ? ln_backward_run<1, 16>(c, p, &ctas)
                    : ln_backward_run<2, 16>(c, p, &ctas);
   }
   if (e != cudaSuccess || !p.dg) return e;
