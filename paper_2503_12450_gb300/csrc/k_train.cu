@@ -730,10 +730,13 @@ int ln_backward_ctas(int M, int groups, int per_sm) {
   return need < most ? need : most;
 }
 
-cudaError_t big_smem(const void* kernel, size_t smem) {
-  return smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)
+// Lets a kernel have up to `most` bytes of dynamic shared memory, the same at every call.
+// (The 48 KB that need no leave count a kernel's static shared memory too.)
+cudaError_t big_smem(const void* kernel, size_t most) {
+  return most > 32 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most)
                           : cudaSuccess;
 }
+constexpr int kRingBytes = 220 * 1024;  // most of a CTA
 
 // Rows in shared memory: as many a warp as let two CTAs of eight warps live on
 // an SM with two rows a warp at least, otherwise one CTA.
@@ -746,7 +749,7 @@ cudaError_t ln_backward_ring_run(const Ctx& c, const LnBackward& p, int* ctas) {
   int warps = 8, per_sm = 2, depth = (int)(110 * 1024 / (warps * row_b));
   if (depth < 2) {
     per_sm = 1;
-    depth = (int)(220 * 1024 / (warps * row_b));
+    depth = (int)(kRingBytes / (warps * row_b));
   }
   if (depth > kRing) depth = kRing;
   size_t smem = (size_t)warps * depth * row_b;
@@ -754,7 +757,7 @@ cudaError_t ln_backward_ring_run(const Ctx& c, const LnBackward& p, int* ctas) {
   if (smem < sums) smem = sums;
   *ctas = ln_backward_ctas(p.M, warps / WPR, per_sm);
   const auto kernel = ln_backward_ring_kernel<NB, WPR>;
-  cudaError_t e = big_smem(reinterpret_cast<const void*>(kernel), smem);
+  cudaError_t e = big_smem(reinterpret_cast<const void*>(kernel), kRingBytes);
   if (e != cudaSuccess) return e;
   return launch_pdl(kernel, dim3((unsigned)*ctas), dim3((unsigned)warps * 32), smem, c.stream, p, depth, row_b, dy_b,
                     dy_b + x_b, c.err);

@@ -217,3 +217,45 @@ def test_example_leaves_its_teacher(monkeypatch):
     teacher, was = made[0]
     for k, v in teacher.p.items():
         assert torch.equal(v, was[k]), k
+
+
+FIRST_CALLS = """
+import torch
+from paper_2503_12450_gb300 import lazymar as lm
+F, B = (lm.LAZYMAR_F32, torch.float32), (lm.LAZYMAR_BF16, torch.bfloat16)
+bad = []
+for D, dy_t, x_t, res in %s:
+    M = 40
+    dy_t = {"f": F, "b": B}[dy_t]
+    dy = torch.zeros((M, D), dtype=dy_t[1], device="cuda")
+    x, x8 = None, None
+    if x_t == "8":
+        q, s = torch.zeros((M, D), dtype=torch.uint8, device="cuda"), torch.ones((-(-D // 128), M), dtype=torch.uint8, device="cuda")
+        x8 = lm.lazymar_block8(q, s)
+        x_t = F
+    else:
+        x_t = {"f": F, "b": B}[x_t]
+        x = torch.zeros((M, D), dtype=x_t[1], device="cuda")
+    mean, rstd = torch.zeros(M, device="cuda"), torch.ones(M, device="cuda")
+    dres = torch.zeros((M, D), device="cuda") if res else None
+    dx = torch.ones((M, D), device="cuda")
+    try:
+        lm.lazymar_layernorm_backward(dy_t[0], dy, D, x_t[0], x, D, x8, mean, rstd, None, dres, D, F[0], dx, D, None,
+                                      None, False, M, D, None, 0)
+        torch.cuda.synchronize()
+        assert not dx.any()
+    except Exception as e:
+        bad.append((D, str(e)))
+assert not bad, bad
+"""
+
+
+@pytest.mark.parametrize("calls", [
+    [(128, "f", "f", True), (256, "b", "f", False), (512, "b", "f", False), (768, "b", "b", False),
+     (1536, "b", "b", False), (1024, "b", "8", False), (2048, "b", "8", False), (4096, "b", "8", False)],
+    [(256, "f", "b", False), (512, "f", "b", False), (1280, "b", "8", True), (640, "b", "f", True)]])
+def test_first_layernorm_backward_of_a_process(calls):
+    """Every kernel's first call: what an earlier, larger call has set up does not carry it."""
+    torch_cuda()
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS % calls], capture_output=True, text=True, timeout=300, cwd=ROOT)
+    assert r.returncode == 0, r.stderr[-2000:]
