@@ -497,7 +497,8 @@ lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, int ldx, co
  * dy [M, lddy] fp32 or bf16; the input either as x [M, ldx] (fp32 or bf16) or as
  * its checkpoint x8 (exactly one of the two); mean, rstd from the forward
  * pass; g may be NULL. dres [M, lddres] fp32 (may be NULL; the residual
- * stream's gradient) is added; dx [M, lddx] fp32 or bf16 may be dres itself.
+ * stream's gradient) is added; dx [M, lddx] fp32 or bf16 (fp32 with lddx =
+ * lddres it may be dres itself).
  * dg and db [D] fp32 are both given or both NULL. workspace:
  * lazymar_layernorm_backward_workspace(M, D) bytes, 16-byte aligned, not needed
  * without dg and db. */

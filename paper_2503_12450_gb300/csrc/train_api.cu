@@ -101,6 +101,9 @@ extern "C" lazymar_status lazymar_layernorm_backward(int dy_dtype, const void* d
   if ((dg == nullptr) != (db == nullptr)) return bad("dg and db: both or neither");
   if (M > 0) {
     if ((x == nullptr) == (x8 == nullptr)) return bad("exactly one of x and x8 required");
+    // (rows are worked on side by side: in another layout dx would overwrite rows of dres that are still to be read)
+    if (dres && dx == dres && (dx_dtype != LAZYMAR_F32 || (M > 1 && lddx != lddres)))
+      return bad("dx in place of dres: fp32 with the same stride required");
     TR_TRY(check_mat(dy, dy_dtype, lddy, D, "dy: fp32 or bf16 device tensor, lddy >= D required"));
     if (x) TR_TRY(check_mat(x, x_dtype, ldx, D, "x: fp32 or bf16 device tensor, ldx >= D required"));
     if (x8) TR_TRY(check_block8(x8, D, M, "x8: device tensors, q 16-byte aligned, ldq % 16 == 0, ldq >= D, lds >= M"));

@@ -227,3 +227,16 @@ def test_in_place_needs_the_same_layout(lib):
         assert "in place" in lib.lazymar_last_error().decode()
     assert lib.lazymar_block8_linear(2, q.addr, q.addr, None, 16, 8, 0, 16, 16, None, None, 4, 8, 8, None) == 1
     assert "in place" in lib.lazymar_last_error().decode()
+
+
+def test_layernorm_backward_in_place_of_the_residual_needs_its_layout(lib):
+    """dx over dres as bf16, or in rows further apart, would overwrite rows of dres that are still to be read."""
+    def call(dx_dtype, lddx, M=4):
+        return lib.lazymar_layernorm_backward(1, 32, 8, 1, 64, 8, None, 128, 256, None, 16, 8, dx_dtype, 16, lddx, None,
+                                              None, 0, M, 8, None, 0, None)
+    for dx_dtype, lddx, M in ((1, 8, 4), (1, 16, 4), (0, 16, 4), (1, 8, 1)):
+        assert call(dx_dtype, lddx, M) == 1
+        assert "in place" in lib.lazymar_last_error().decode()
+    for lddx, M in ((8, 4), (16, 1)):  # its own layout: refused only for what is no device memory here
+        assert call(0, lddx, M) == 1
+        assert "in place" not in lib.lazymar_last_error().decode()
