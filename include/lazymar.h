@@ -482,10 +482,10 @@ typedef struct lazymar_block8 {
 /* LayerNorm over D of x [M, ldx] (fp32 or bf16) with its statistics:
  *   mean[m], rstd[m] = 1 / sqrt(var + eps)   (fp32, each may be NULL)
  *   y = (x - mean) rstd g + b                (g, b fp32 [D], each may be NULL)
- * y goes to y [M, ldy] (fp32 or bf16; may be NULL) and / or y8 (may be NULL),
- * the operand of lazymar_block8_linear; x8 (may be NULL) receives x itself, the
- * checkpoint for lazymar_layernorm_backward. At least one of y, y8, x8 and the
- * statistics is given. 1 <= D <= 8192. */
+ * y goes to y [M, ldy] (fp32 or bf16; may be NULL, or x itself with its type and
+ * stride) and / or y8 (may be NULL), the operand of lazymar_block8_linear; x8 (may
+ * be NULL) receives x itself, the checkpoint for lazymar_layernorm_backward. At
+ * least one of y, y8, x8 and the statistics is given. 1 <= D <= 8192. */
 lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, int ldx, const float* g, const float* b,
                                          int y_dtype, void* y, int ldy, const lazymar_block8* y8,
                                          const lazymar_block8* x8, float* mean, float* rstd, int M, int D, float eps,
@@ -497,11 +497,10 @@ lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, int ldx, co
  * dy [M, lddy] fp32 or bf16; the input either as x [M, ldx] (fp32 or bf16) or as
  * its checkpoint x8 (exactly one of the two); mean, rstd from the forward
  * pass; g may be NULL. dres [M, lddres] fp32 (may be NULL; the residual
- * stream's gradient) is added; dx [M, lddx] fp32 or bf16 (fp32 with lddx =
- * lddres it may be dres itself).
- * dg and db [D] fp32 are both given or both NULL. workspace:
- * lazymar_layernorm_backward_workspace(M, D) bytes, 16-byte aligned, not needed
- * without dg and db. */
+ * stream's gradient) is added; dx [M, lddx] fp32 or bf16 may be dy, x or dres
+ * itself with its type and stride. dg and db [D] fp32 are both given or both
+ * NULL. workspace: lazymar_layernorm_backward_workspace(M, D) bytes, 16-byte
+ * aligned, not needed without dg and db. */
 size_t lazymar_layernorm_backward_workspace(int M, int D);
 lazymar_status lazymar_layernorm_backward(int dy_dtype, const void* dy, int lddy, int x_dtype, const void* x, int ldx,
                                           const lazymar_block8* x8, const float* mean, const float* rstd,

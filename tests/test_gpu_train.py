@@ -721,3 +721,34 @@ def test_refusals():
     refuses(lambda: lm.lazymar_layernorm_backward(0, x, 256, 0, x, 256, None, db, db, None, None, 0, 0, x, 256, db, db,
                                                   False, 4, 256, x, 64), "workspace")
     sync()  # none of them has launched anything
+
+
+@pytest.mark.parametrize("M,D,pad", [(1, 512, 0), (300, 1024, 0), (300, 1280, 8), (301, 777, 0), (40, 5000, 3)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_layernorm_in_place_of_its_input(M, D, pad, dtype):
+    """y over x and dx over dy or x, with their type and stride, give what they give elsewhere."""
+    torch = torch_cuda()
+    r = rng(M, D, 30)
+    x, _ = dev(r.standard_normal((M, D)), dtype, pad)
+    dy, _ = dev(r.standard_normal((M, D)), dtype, pad)
+    t, ld, g = DT[dtype], D + pad, vec(1 + 0.1 * r.standard_normal(D))
+    mean, rstd = vec(np.zeros(M)), vec(np.zeros(M))
+
+    def forward(x, y):
+        lm.lazymar_layernorm_forward(t, x, ld, g, None, t, y, ld, None, None, mean, rstd, M, D, EPS)
+
+    def backward(dy, x, dx):
+        lm.lazymar_layernorm_backward(t, dy, ld, t, x, ld, None, mean, rstd, g, None, 0, t, dx, ld, None, None, False, M,
+                                      D, None, 0)
+    y, dx = out(M, D, dtype, pad), out(M, D, dtype, pad)
+    forward(x, y)
+    backward(dy, x, dx)
+    for over_x in (False, True):
+        a, b = dev(dy.float().cpu().numpy(), dtype, pad)[0], dev(x.float().cpu().numpy(), dtype, pad)[0]
+        backward(a, b, b if over_x else a)
+        sync()
+        assert torch.equal(b if over_x else a, dx)
+    z, _ = dev(x.float().cpu().numpy(), dtype, pad)
+    forward(z, z)
+    sync()
+    assert torch.equal(z, y)

@@ -240,3 +240,17 @@ def test_layernorm_backward_in_place_of_the_residual_needs_its_layout(lib):
     for lddx, M in ((8, 4), (16, 1)):  # its own layout: refused only for what is no device memory here
         assert call(0, lddx, M) == 1
         assert "in place" not in lib.lazymar_last_error().decode()
+
+
+def test_layernorm_in_place_of_its_input_needs_the_same_layout(lib):
+    """y over x, dx over dy or x: another type or stride would overwrite rows that are still to be read."""
+    def forward(dtype, ldy, M=4):
+        return lib.lazymar_layernorm_forward(1, 16, 8, None, None, dtype, 16, ldy, None, None, None, None, M, 8, 1e-6, None)
+
+    def backward(dy, x, dtype, lddx, M=4):
+        return lib.lazymar_layernorm_backward(1, dy, 8, 1, x, 8, None, 128, 256, None, None, 0, dtype, 16, lddx, None, None,
+                                              0, M, 8, None, 0, None)
+    for f in (forward, lambda *a: backward(16, 32, *a), lambda *a: backward(32, 16, *a)):
+        for dtype, ld, M, refused in ((0, 8, 4, True), (1, 16, 4, True), (1, 8, 4, False), (1, 16, 1, False)):
+            assert f(dtype, ld, M) == 1
+            assert ("in place" in lib.lazymar_last_error().decode()) == refused, (dtype, ld, M)
