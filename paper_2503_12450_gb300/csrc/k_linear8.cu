@@ -30,6 +30,7 @@
 #include <cstring>
 
 #include "block8.cuh"
+#include "linear8_shape.h"
 
 namespace lm {
 
@@ -70,8 +71,6 @@ constexpr uint32_t ACC_SECOND = 224;
 constexpr int SF_SLOTS = 2;           // scale slots of 16 columns: 4 of a, 8 of w
 constexpr uint32_t SF_BASE = 480;     // behind the accumulators
 static_assert(ACC_SECOND + 256 <= SF_BASE && SF_BASE + 16 * SF_SLOTS <= 512, "tensor memory has 512 columns");
-
-constexpr int kSplitCtas = 128;       // most CTAs of a launch that splits K
 
 struct Params {
   const uint8_t *a_scale, *w_scale;
@@ -778,8 +777,9 @@ cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& 
     if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) ready[dev] = 1;
   }
+  // (with K in parts a cluster takes one tile, so there are as many of them)
   const int slots = c.num_sms / cluster;
-  const unsigned grid = (unsigned)((tiles < slots ? tiles : slots) * cluster);
+  const unsigned grid = (unsigned)((SPLIT || tiles < slots ? tiles : slots) * cluster);
   if (cluster > 1)
     return launch_pdl_cluster(kernel, dim3(grid), dim3(THREADS), smem, cluster, c.stream, ta, tb, to, tu, p, c.err);
   return launch_pdl(kernel, dim3(grid), dim3(THREADS), smem, c.stream, ta, tb, to, tu, p, c.err);
@@ -793,43 +793,6 @@ cudaError_t run_linear8(const Ctx& c, const CUtensorMap& ta, const CUtensorMap& 
   if (p.epilogue == LAZYMAR_EPI_RESIDUAL)
     return run_linear8<PAIR, l8::OUT_RESIDUAL, false>(c, ta, tb, to, tu, p, tiles, CTAS);
   return run_linear8<PAIR, l8::OUT_PLAIN, false>(c, ta, tb, to, tu, p, tiles, CTAS);
-}
-
-// Tiles of 256 x 256 on pairs, of 128 x 128 on single CTAs, or of the latter with K
-// in parts, by the time that was measured (us): a pair's round 2.5 and 0.45 for each
-// 128 of K, a single CTA's 1 and 0.33 up to 12 of them, 0.65 after that (its ring then
-// waits for memory), a launch 4 and 5; parts cost 1 and 0.2 for each row a warp.
-// (Measured, pairs : single, N 4096, K 1024: M = 300 11.0 : 9.9, 1000 12.2 : 14.0, 2000 18.7 :
-// 21.5; N = K = 1280: 300 10.3 : 8.9 and 7.9 in four parts, 2000 11.0 : 13.0; N 1024, K 4096, M
-// = 300: 20.9 in one part, 10.6 in four.)
-struct Shape {
-  bool pair;
-  int parts;
-  long long tiles;
-};
-Shape choose(int sms, int M, int N, int K) {
-  const long long pair_tiles = (long long)((M + 255) / 256) * ((N + 255) / 256);
-  const long long tiles = (long long)((M + 127) / 128) * ((N + 127) / 128);
-  const int kb = (K + 127) / 128;
-  const auto rounds = [](long long t, int slots) { return (double)((t + slots - 1) / slots); };
-  const auto single = [](double k) { return k <= 12 ? 0.33 * k : 4.0 + 0.65 * (k - 12); };
-  Shape best{true, 1, pair_tiles};
-  double least = 4.0 + rounds(pair_tiles, sms / 2) * (2.5 + 0.45 * kb);
-  const double one = 5.0 + rounds(tiles, sms) * (1.0 + single(kb));
-  if (one < least) {
-    least = one;
-    best = Shape{false, 1, tiles};
-  }
-  // parts of two blocks at least, one tile a cluster, and every cluster finds its
-  // SMs at once (a GPC holds two clusters of eight)
-  for (int parts = 2; parts <= 8 && tiles * parts <= l8::kSplitCtas && kb >= 2 * parts; parts *= 2) {
-    const double us = 5.0 + 2.0 + 0.2 * (16 / parts) + single((double)kb / parts);
-    if (us < least) {
-      least = us;
-      best = Shape{false, parts, tiles};
-    }
-  }
-  return best;
 }
 
 }  // namespace

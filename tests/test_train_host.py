@@ -4,6 +4,7 @@ import ctypes
 import importlib.util
 import os
 import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -254,3 +255,40 @@ def test_layernorm_in_place_of_its_input_needs_the_same_layout(lib):
         for dtype, ld, M, refused in ((0, 8, 4, True), (1, 16, 4, True), (1, 8, 4, False), (1, 16, 1, False)):
             assert f(dtype, ld, M) == 1
             assert ("in place" in lib.lazymar_last_error().decode()) == refused, (dtype, ld, M)
+
+
+def _host_program(tmp_path, source):
+    """Compiles C++ that includes the library's host headers and returns what it prints."""
+    src, exe = tmp_path / "host.cpp", tmp_path / "host"
+    src.write_text(source)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), "-I",
+                    os.path.join(ROOT, "paper_2503_12450_gb300", "csrc"), str(src), "-o", str(exe)], check=True, timeout=120)
+    return subprocess.run([str(exe)], check=True, capture_output=True, text=True, timeout=120).stdout
+
+
+def test_product_in_parts_of_k_fits_the_device(tmp_path):
+    """A launch with K in parts has one cluster a tile, all at once, on devices with fewer SMs too; and parts are still
+    chosen on a whole one."""
+    text = _host_program(tmp_path, r"""
+#include <cstdio>
+#include <initializer_list>
+#include "linear8_shape.h"
+int main() {
+  for (int sms : {2, 8, 20, 60, 76, 100, 127, 132, 152})
+    for (int M : {33, 100, 128, 300, 500, 1000, 4000})
+      for (int N : {1, 128, 250, 1024, 1280, 2048, 5120})
+        for (int K : {1, 128, 512, 1024, 2048, 4096, 16384}) {
+          const lm::l8::Shape s = lm::l8::choose(sms, M, N, K);
+          std::printf("%d %d %d %d %d %d %lld\n", sms, M, N, K, (int)s.pair, s.parts, s.tiles);
+        }
+}
+""")
+    split = 0
+    for line in text.splitlines():
+        sms, M, N, K, pair, parts, tiles = map(int, line.split())
+        t = 256 if pair else 128
+        assert tiles == -(-M // t) * -(-N // t)
+        if parts > 1:
+            assert not pair and parts in (2, 4, 8) and tiles * parts <= min(sms, 128), line
+            split += sms == 152
+    assert split >= 20
