@@ -5,7 +5,7 @@
 // of w, the warps take its K blocks in turn, and all loads of a warp's block are in
 // flight at once. Measured (us, against the tcgen05 kernel on single CTAs): 2 x 4096
 // x 1024 3.1 : 9.2 (the weights' 4 MB: 0.6), 8 x 1024 x 4096 5.1 : 17.4, 32 x 1024 x 4096
-// 8.2 : 18.5 and 7.4 with K in parts, 32 x 4096 x 1024 4.8 : 9.6.
+// 8.5 : 18.5 and 7.4 with K in parts, 32 x 4096 x 1024 4.8 : 9.6.
 //
 // E4M3 is exact in fp16, so the products run as fp16 warp MMAs (m16n8k16, w as the
 // 16-row operand, tokens as the 8 columns) with fp32 sums; a block's sum is scaled
@@ -128,15 +128,19 @@ __global__ void __launch_bounds__(kWarps * 32) linear8_rows_kernel(const RowsPar
           }
         }
       }
-      // (one factor after the other: their product may leave fp32's range where the sum does not)
+      // One factor after the other (their product may leave fp32's range where the sum does
+      // not), the smaller one first: d is a multiple of 2^-18 below 2^25, so d times a factor
+      // below one is exact and finite, and if both are one or more, a step that overflows
+      // only does what the result does.
       const float ws = block8_scale(sw);
 #pragma unroll
       for (int j = 0; j < TILES; ++j) {  // accumulator: rows g and g + 8 of w, tokens 2 t and 2 t + 1
         const float s0 = block8_scale(sa[j][0]), s1 = block8_scale(sa[j][1]);
-        sum[j][0] = fmaf(d[j][0] * s0, ws, sum[j][0]);
-        sum[j][1] = fmaf(d[j][1] * s1, ws, sum[j][1]);
-        sum[j][2] = fmaf(d[j][2] * s0, ws, sum[j][2]);
-        sum[j][3] = fmaf(d[j][3] * s1, ws, sum[j][3]);
+        const float l0 = fminf(s0, ws), l1 = fminf(s1, ws), h0 = fmaxf(s0, ws), h1 = fmaxf(s1, ws);
+        sum[j][0] = fmaf(d[j][0] * l0, h0, sum[j][0]);
+        sum[j][1] = fmaf(d[j][1] * l1, h1, sum[j][1]);
+        sum[j][2] = fmaf(d[j][2] * l0, h0, sum[j][2]);
+        sum[j][3] = fmaf(d[j][3] * l1, h1, sum[j][3]);
       }
     }
   }

@@ -752,3 +752,25 @@ def test_layernorm_in_place_of_its_input(M, D, pad, dtype):
     forward(z, z)
     sync()
     assert torch.equal(z, y)
+
+
+@pytest.mark.parametrize("M", [3, 20, 32, 40, 400, 2700])
+@pytest.mark.parametrize("ea,ew,small", [(119, -115, False), (112, -108, False), (-115, 119, False), (-125, 100, True),
+                                         (-120, 112, True), (100, -125, True)])
+def test_linear_scales_at_both_ends(M, ea, ew, small):
+    """Scales near the ends of their range whose product is an ordinary number: neither factor may be applied to a
+    block's sum on its own (2^24 2^112 overflows, 2^-18 2^-126 loses digits). `small`: E4M3's subnormals alone."""
+    r = rng(M, ea + 200, 25)
+    N, K = 136, 384
+    a, w = Held(M, K), Held(N, K, scale_rows=2)
+    q = np.r_[1:8, 0x81:0x88] if small else np.r_[1:0x7F, 0x81:0xFF]  # no NaN
+
+    def fill(h, rows, e, scales):
+        h.set(r.choice(q, (rows, K)).astype(np.uint8), (127 + r.integers(e - 1, e + 2, (3, scales))).astype(np.uint8))
+    fill(a, M, ea, M)
+    fill(w, N, ew, 2)
+    av, wv = T.unpack(*a.get()), T.unpack_weight(*w.get())
+    y = out(M, N)
+    lm.lazymar_block8_linear(0, a.d, w.d, None, None, 0, 0, y, N, None, None, M, N, K)
+    sync()
+    close(y, av @ wv.T, _product_bound(np.abs(av) @ np.abs(wv).T, K))
