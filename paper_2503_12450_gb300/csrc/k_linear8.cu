@@ -832,10 +832,9 @@ cudaError_t launch_linear8(const Ctx& c, const Linear8& x) {
   p.u8 = static_cast<uint8_t*>(x.u8.q);
   p.ldout8 = x.out8.ldq;
   p.ldu8 = x.u8.ldq;
-  const auto at = [](const void* q, size_t n) { return reinterpret_cast<uintptr_t>(q) % n == 0; };
-  p.bias_vec = at(x.bias, 16);
-  p.rows_vec = x.out.ld % 4 == 0 && at(x.out.p, x.out.dtype == LAZYMAR_F32 ? 16 : 8) && x.residual.ld % 4 == 0 &&
-               at(x.residual.p, 16);
+  p.bias_vec = reinterpret_cast<uintptr_t>(x.bias) % 16 == 0;
+  p.rows_vec = rows_on_four(x.out.p, x.out.ld, x.out.dtype == LAZYMAR_F32 ? 4 : 2) &&
+               rows_on_four(x.residual.p, x.residual.ld, 4);
   const Shape shape = choose(c.num_sms, x.M, x.N, x.K);
   if (shape.pair) return run_linear8<true>(c, ta, tb, to, tu, p, shape.tiles);
   if (shape.parts > 1) return run_linear8<false, OUT_PLAIN, true>(c, ta, tb, to, tu, p, shape.tiles, shape.parts);

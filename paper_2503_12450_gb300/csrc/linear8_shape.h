@@ -1,6 +1,8 @@
 // Host only: how lazymar_block8_linear above the few-row kernel cuts a product
-// into tiles (k_linear8.cu).
+// into tiles, and which rows its epilogue takes by whole accesses (k_linear8.cu).
 #pragma once
+
+#include <cstdint>
 
 namespace lm {
 namespace l8 {
@@ -43,6 +45,12 @@ inline Shape choose(int sms, int M, int N, int K) {
     }
   }
   return best;
+}
+
+// Rows on boundaries of four elements (those of an absent tensor are, whatever its
+// stride says).
+inline bool rows_on_four(const void* p, int ld, int elem_bytes) {
+  return !p || (ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4u * (unsigned)elem_bytes) == 0);
 }
 
 }  // namespace l8

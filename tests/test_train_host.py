@@ -292,3 +292,22 @@ int main() {
             assert not pair and parts in (2, 4, 8) and tiles * parts <= min(sms, 128), line
             split += sms == 152
     assert split >= 20
+
+
+def test_absent_tensors_do_not_take_the_product_off_whole_accesses(tmp_path):
+    """Without a residual its stride says nothing about the output's rows."""
+    text = _host_program(tmp_path, r"""
+#include <cstdio>
+#include "linear8_shape.h"
+int main() {
+  using lm::l8::rows_on_four;
+  void* const p = reinterpret_cast<void*>(uintptr_t(1024));
+  void* const q = reinterpret_cast<void*>(uintptr_t(1024 + 8));
+  std::printf("%d%d%d%d %d%d%d%d", rows_on_four(nullptr, 7, 4), rows_on_four(nullptr, 0, 2), rows_on_four(p, 8, 4),
+              rows_on_four(q, 8, 2), rows_on_four(q, 8, 4), rows_on_four(p, 7, 4), rows_on_four(p, 6, 2),
+              rows_on_four(nullptr, 8, 4));
+}
+""")
+    assert text == "1111 0001"
+    source = open(os.path.join(ROOT, "paper_2503_12450_gb300", "csrc", "k_linear8.cu")).read()
+    assert "rows_on_four(x.out.p" in source and "rows_on_four(x.residual.p" in source
