@@ -459,9 +459,11 @@ lazymar_status lazymar_head_schedule(int n_train, int n_steps, int32_t *kept, fl
  * scale[(col / 128) * lds + row]; value = q * 2^(scale - 127). A block's
  * exponent is the smallest e >= -126 with max |x| <= 448 * 2^e over its finite
  * values, q = E4M3(x * 2^-e), to nearest even; infinities and NaN become NaN.
- * The values are exact in bf16 (numbers that round to 2^128 read back as
- * infinity). A weight matrix [N, K] has one scale for each
- * 128 x 128 block, at scale[(k / 128) * lds + n / 128].
+ * The values are exact in fp32 and, from 2^-130 on in magnitude, in bf16; smaller
+ * ones are multiples of 2^-135, which bf16 (where they are unpacked to it, and in
+ * the weight gradient) rounds to multiples of 2^-133. Numbers that round to 2^128
+ * read back as infinity. A weight matrix [N, K] has one scale for each 128 x 128
+ * block, at scale[(k / 128) * lds + n / 128].
  * q is 16-byte aligned, ldq a multiple of 16 and >= cols (bytes between cols
  * and ldq are neither read as values nor written); lds >= rows (weights:
  * >= ceil(N / 128)).
@@ -554,7 +556,7 @@ lazymar_status lazymar_block8_linear(int epilogue, const lazymar_block8* a, cons
 /* Weight gradient of a linear layer from its output's gradient and the 8-bit
  * checkpoint of its input: dw[n, k] (+)= sum_m dy[m, n] x[m, k]; dy [M, lddy]
  * bf16 (16-byte aligned, lddy a multiple of 8), x block8 [M, K], dw [N, lddw]
- * fp32. Products of bf16 values (the checkpoint's are exact there), summed in
+ * fp32. Products of bf16 values (the checkpoint's as said above), summed in
  * fp32. workspace: lazymar_block8_wgrad_workspace(M, N, K) bytes, 16-byte
  * aligned. */
 size_t lazymar_block8_wgrad_workspace(int M, int N, int K);

@@ -7,8 +7,9 @@
 // rounding it up to a power of two gives at most one binade of E4M3's 17 away
 // and leaves the relative precision (2^-4) as it is, because E4M3 is itself
 // floating. In return x 2^-e is exact (one rounding, to E4M3), q 2^e is exact
-// in bf16 (the weight gradient's product takes the checkpoint without another
-// rounding), a scale is a byte, and the tensor cores apply it themselves.
+// in bf16 from 2^-130 on (the weight gradient's product takes the checkpoint
+// without another rounding; below, bf16 has only multiples of 2^-133), a scale is a
+// byte, and the tensor cores apply it themselves.
 #pragma once
 
 #include <cuda_fp8.h>

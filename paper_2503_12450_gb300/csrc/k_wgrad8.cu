@@ -3,7 +3,7 @@
 //
 // The sum runs over tokens, and a checkpoint's scales differ from token to
 // token, so the 8-bit tensor cores cannot apply them. But E4M3 times a power of
-// two is exact in bf16: converter warps turn the checkpoint's bytes into the
+// two is exact in bf16 (from 2^-130 on; subnormals count): converter warps turn the checkpoint's bytes into the
 // bf16 operand in shared memory, and the product runs at the bf16 rate without
 // the activation ever being written out in 16 bits.
 //

@@ -774,3 +774,30 @@ def test_linear_scales_at_both_ends(M, ea, ew, small):
     lm.lazymar_block8_linear(0, a.d, w.d, None, None, 0, 0, y, N, None, None, M, N, K)
     sync()
     close(y, av @ wv.T, _product_bound(np.abs(av) @ np.abs(wv).T, K))
+
+
+def test_smallest_scales_in_bf16():
+    """Every byte under the smallest scales: fp32 holds their values, bf16 those in steps of 2^-133 (all of them from
+    scales of 2^-124 on, and from 2^-130 on under any), others rounded to nearest even. The weight gradient's operand
+    is the same."""
+    torch = torch_cuda()
+    rows = 8
+    q = np.arange(256, dtype=np.uint8)[None].repeat(rows, 0)
+    q[(q & 0x7F) == 0x7F] = 0
+    h = Held(rows, 256).set(q, np.arange(1, rows + 1, dtype=np.uint8)[None].repeat(2, 0))
+    x = T.unpack(*h.get())
+    wide, narrow = out(rows, 256), out(rows, 256, "bf16")
+    lm.lazymar_block8_unpack(h.d, 0, wide, 256, rows, 256)
+    lm.lazymar_block8_unpack(h.d, 1, narrow, 256, rows, 256)
+    step = np.maximum(np.exp2(np.floor(np.log2(np.maximum(np.abs(x), 2.0 ** -140))) - 7), 2.0 ** -133)
+    held16 = np.rint(x / step) * step  # rint: ties to even
+    assert (held16[2:] == x[2:]).all() and (held16 == x)[np.abs(x) >= 2.0 ** -130].all() and (held16 != x).any()
+    dy, dyv = dev(np.eye(rows) * 2.0 ** 60, "bf16")
+    dw = out(rows, 256)
+    n = lm.lazymar_block8_wgrad_workspace(rows, rows, 256)
+    lm.lazymar_block8_wgrad(dy, rows, h.d, dw, 256, False, rows, rows, 256, torch.empty(n + 16, dtype=torch.uint8,
+                                                                                        device="cuda"), n)
+    sync()
+    assert (wide.double().cpu().numpy() == x).all()
+    assert (narrow.double().cpu().numpy() == held16).all()
+    assert (dw.double().cpu().numpy() == dyv.T @ held16).all()
