@@ -542,7 +542,9 @@ lazymar_status lazymar_block8_gelu_backward(int dtype, const void* da, int ldda,
  * applied there (kind::mxf8f6f4; above 32 rows the accumulator truncates, a
  * relative bias towards zero of about 6e-11 K); bias fp32 [N] (may be NULL).
  *   LAZYMAR_EPI_BIAS      out = y
- *   LAZYMAR_EPI_GELU      out = GELU(y) (erf form)
+ *   LAZYMAR_EPI_GELU      out = GELU(y) (erf form) within 1.6e-7 max(1, |y|), before
+ *                         out's own rounding. (Of GELU(y) itself that is 4e-6
+ *                         above -2, 1e-3 at -4, 3 % at -6; below -6 out is -5.8e-9.)
  *   LAZYMAR_EPI_RESIDUAL  out = residual + y, residual [M, ldr] and out fp32
  *                         (out may be residual itself, ldo = ldr)
  * out [M, ldo] fp32 or bf16 (may be NULL) and / or out8 [M, N] (may be NULL; not

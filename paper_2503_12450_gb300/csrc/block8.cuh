@@ -98,8 +98,10 @@ __device__ __forceinline__ void block8_values(uint2 q, float s, float (&v)[8]) {
 
 // GELU in the erf form for the 8-bit product's epilogues: gelu_erf of
 // lazymar_internal.cuh with a tail polynomial of degree 6 (csrc/gen_gelu_poly.py),
-// within 1.1e-7 max(1, |x|) instead of 2.8e-7, which moves fewer values over an
-// E4M3 rounding boundary, for one more paired instruction.
+// within 1.1e-7 max(1, |x|) instead of 2.8e-7 (and 4e-8 for exp2_approx), which moves
+// fewer values over an E4M3 rounding boundary, for one more paired instruction. The
+// bound is absolute: relative to GELU itself 4e-6 above -2, 1e-3 at -4, 3 % at -6,
+// and below -6 the result stays at -5.8e-9.
 __device__ __forceinline__ void gelu_erf6_x2(float& x0, float& x1) {
   constexpr float kGelu6P0 = -9.999947548e-01f;
   constexpr float kGelu6P1 = -1.151182413e+00f;

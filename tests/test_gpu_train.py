@@ -801,3 +801,20 @@ def test_smallest_scales_in_bf16():
     assert (wide.double().cpu().numpy() == x).all()
     assert (narrow.double().cpu().numpy() == held16).all()
     assert (dw.double().cpu().numpy() == dyv.T @ held16).all()
+
+
+@pytest.mark.parametrize("M", [1, 20, 40, 400, 2700])
+@pytest.mark.parametrize("out_dtype", ["fp32", "bf16"])
+def test_linear_gelu_within_its_bound(M, out_dtype):
+    """With a zero operand GELU's argument is the bias, exactly. The polynomial of degree six is within
+    1.1e-7 max(1, |u|) in fp32 arithmetic, exp2's approximation adds 2^-22 of |u| h(|u|) <= 0.17."""
+    N = 4097
+    b = np.linspace(-12, 12, N).astype(np.float32)
+    a, w = held(np.zeros((M, 128)))[0], held_weight(rng(27).standard_normal((N, 128)))[0]
+    y = out(M, N, out_dtype)
+    lm.lazymar_block8_linear(1, a.d, w.d, vec(b), None, 0, DT[out_dtype], y, N, None, None, M, N, 128)
+    sync()
+    u = b.astype(float)[None].repeat(M, 0)
+    want = T.gelu(u[:1]).repeat(M, 0)
+    bound = 1.1e-7 * np.maximum(1, np.abs(u)) + 0.17 * 2.0 ** -22 + U * np.abs(want)
+    close(y, want, rounded(bound, want, out_dtype))
