@@ -818,3 +818,225 @@ def test_linear_gelu_within_its_bound(M, out_dtype):
     want = T.gelu(u[:1]).repeat(M, 0)
     bound = 1.1e-7 * np.maximum(1, np.abs(u)) + 0.17 * 2.0 ** -22 + U * np.abs(want)
     close(y, want, rounded(bound, want, out_dtype))
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 136, 384), (12, 300, 384), (32, 136, 384), (400, 136, 384), (128, 640, 4096),
+                                   (2700, 2000, 384)])
+@pytest.mark.parametrize("gelu", [False, True])
+def test_linear_overflow_stays_in_its_element(M, N, K, gelu):
+    """A sum beyond fp32's range is infinite (or NaN after GELU) in fp32 and NaN in the 8-bit outputs, whose scale is
+    that of the block's finite values."""
+    torch = torch_cuda()
+    r = rng(M, N, K, 26)
+    x, v = r.standard_normal((M, K)).astype(np.float32), 0.05 * r.standard_normal((N, K)).astype(np.float32)
+    x[1, :128], v[:, :128] = 3.0, 0
+    v[3, :128], v[70, :128] = 2.0, -2.0
+    a, w = held(x)[0], held_weight(v)[0]
+    a.scale[0, 1], w.scale[0, 0] = 247, 127 + 100
+    av, wv = T.unpack(*a.get()), T.unpack_weight(*w.get())
+    u, mag = av @ wv.T, np.abs(av) @ np.abs(wv).T
+    inf = np.abs(u) > 2.0 ** 128
+    assert inf.sum() == 2 and (np.abs(u[~inf]) < 2.0 ** 127).all()
+    y, y8, u8 = out(M, N), Held(M, N), Held(M, N)
+    lm.lazymar_block8_linear(int(gelu), a.d, w.d, None, None, 0, 0, y, N, y8.d, u8.d if gelu else None, M, N, K)
+    sync()
+    bound = np.where(inf, 0, _product_bound(mag, K))
+    finite = np.where(inf, 0, u)
+    got = y.cpu().numpy()
+    assert (np.isfinite(got) == ~inf).all()
+    assert got[1, 3] == np.inf and (np.isnan(got[1, 70]) if gelu else got[1, 70] == -np.inf)
+    for h, want, b in ((y8, T.gelu(finite) if gelu else finite,
+                        np.where(inf, 0, bound * 1.13 + 4e-7 * np.maximum(1, np.abs(finite))) if gelu else bound),
+                       (u8, finite, bound))[:1 + gelu]:
+        q, _ = h.get()
+        assert (((q & 0x7F) == 0x7F) == inf).all()
+        h.q[:, :N][torch.from_numpy(inf).cuda()] = 0
+        close8(h, want, b)
+
+
+@pytest.mark.parametrize("D,x_kind", [(1024, "bf16"), (1024, "block8"), (777, "fp32"), (777, "block8"), (4104, "bf16")])
+def test_layernorm_backward_of_rows_that_are_not_finite(D, x_kind):
+    """NaN in a row's input or infinity in its gradient: that row of dx is lost, and of dg and db what it adds to; the
+    other rows are as without it."""
+    torch = torch_cuda()
+    r = rng(D, 28)
+    M = 70
+    x, g = r.standard_normal((M, D)).astype(np.float32), vec(1 + 0.1 * r.standard_normal(D))
+    dy = r.standard_normal((M, D)).astype(np.float32)
+    ws = torch.empty(lm.lazymar_layernorm_backward_workspace(M, D), dtype=torch.uint8, device="cuda")
+
+    def run(x, dy):
+        if x_kind == "block8":
+            h, v = held(x)
+            t = None
+        else:
+            h, (t, v) = None, dev(x, x_kind)
+        with np.errstate(invalid="ignore"):
+            _, mean, rstd = T.layernorm(v, None, None, EPS)
+        dx, dg, db = out(M, D), vec(np.zeros(D)), vec(np.zeros(D))
+        td, _ = dev(dy)
+        lm.lazymar_layernorm_backward(0, td, D, DT.get(x_kind, 0), t, D, h.d if h else None, vec(mean), vec(rstd), g, None,
+                                      0, 0, dx, D, dg, db, False, M, D, ws, ws.numel())
+        sync()
+        return [a.cpu().numpy() for a in (dx, dg, db)]
+    clean = run(x, dy)
+    assert all(np.isfinite(a).all() for a in clean)
+    others = np.arange(M) != 9
+    bad = x.copy()
+    bad[9, 5] = np.nan
+    dx, dg, db = run(bad, dy)
+    assert np.isnan(dx[9]).all() and (dx[others] == clean[0][others]).all()
+    assert np.isnan(dg).all() and (db == clean[2]).all()
+    bad = dy.copy()
+    bad[9, 5] = np.inf
+    dx, dg, db = run(x, bad)
+    assert not np.isfinite(dx[9]).any() and (dx[others] == clean[0][others]).all()
+    there = np.arange(D) == 5
+    for got, was in ((dg, clean[1]), (db, clean[2])):
+        assert np.isinf(got[there]).all() and (got[~there] == was[~there]).all()
+
+
+def _spread(a, dtype, ld):
+    """A device tensor whose rows are `ld` elements apart, with nothing set between them."""
+    torch = torch_cuda()
+    t = {"fp32": torch.float32, "bf16": torch.bfloat16, "byte": torch.uint8}[dtype]
+    v = torch.empty(a.shape[0] * ld, dtype=t, device="cuda").view(a.shape[0], ld)[:, :a.shape[1]]
+    v.copy_(torch.from_numpy(a).cuda())
+    return v
+
+
+@pytest.mark.parametrize("D,ld", [(640, (1 << 26) + 8), (636, (1 << 26) + 5)])
+def test_backward_offsets_beyond_32_bits(D, ld):
+    """LayerNorm's and GELU's gradients and the weight gradient of rows that start more than 2^32 bytes into their
+    buffers: the same as from rows next to each other."""
+    torch = torch_cuda()
+    M, N, ld8 = 40, 48, (1 << 27) + 16
+    r = rng(D, 29)
+    x, dy, res = (r.standard_normal((M, D)).astype(np.float32) for _ in range(3))
+    near, v = held(x)
+    q, s = near.get()
+    far = lm.lazymar_block8(_spread(q, "byte", ld8), near.scale)
+    _, mean, rstd = T.layernorm(v, None, None, EPS)
+    tm, tr = vec(mean), vec(rstd)
+    n = max(lm.lazymar_layernorm_backward_workspace(M, D), lm.lazymar_block8_gelu_backward_workspace(M, D),
+            lm.lazymar_block8_wgrad_workspace(M, N, D), 16)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    outs = []
+    for h, stride, make in ((near.d, D, lambda a, t: dev(a, t)[0]), (far, ld, lambda a, t: _spread(a, t, ld))):
+        tdy, tres = make(dy, "bf16"), make(res, "fp32")
+        dx = make(np.zeros_like(x), "fp32")
+        dg, db, du_db = (vec(np.zeros(D)) for _ in range(3))
+        lm.lazymar_layernorm_backward(1, tdy, stride, 0, None, 0, h, tm, tr, None, tres, stride, 0, dx, stride, dg, db,
+                                      False, M, D, ws, n)
+        du = make(np.zeros_like(x), "bf16")
+        lm.lazymar_block8_gelu_backward(1, tdy, stride, h, 1, du, stride, None, du_db, False, M, D, ws, n)
+        sync()
+        outs.append([a.clone() for a in (dx, dg, db, du, du_db)])
+        del tdy, tres, dx, du
+    want, wg, wb = T.layernorm_grad(dev(dy, "bf16")[1], v, mean.astype(np.float32).astype(float),
+                                    rstd.astype(np.float32).astype(float), None)
+    xh = (v - mean.astype(np.float32)[:, None]) * rstd.astype(np.float32)[:, None]
+    bx, bg, bb = _ln_grad_bounds(dev(dy, "bf16")[1], xh, rstd, None)
+    for dx, dg, db, du, du_db in outs:
+        close(dx, want + res, bx + 2 * U * np.abs(want + res))
+        close(dg, wg, bg)
+        close(db, wb, bb)
+    assert torch.equal(outs[0][3], outs[1][3])
+    grad = dev(dy, "bf16")[1] * T.gelu_grad(v)
+    bound = np.abs(dev(dy, "bf16")[1]) * 5e-7 + 4 * U * np.abs(grad) + 1e-30
+    for o in outs:
+        close(o[4], grad.sum(0), bound.sum(0) + (M + 16) * U * np.abs(grad).sum(0))
+    # the weight gradient: dy in rows of multiples of eight
+    dn = r.standard_normal((M, N)).astype(np.float32)
+    a, b = out(N, D), out(N, D)
+    lm.lazymar_block8_wgrad(dev(dn, "bf16")[0], N, near.d, a, D, False, M, N, D, ws, n)
+    lm.lazymar_block8_wgrad(_spread(dn, "bf16", (1 << 26) + 8), (1 << 26) + 8, far, b, D, False, M, N, D, ws, n)
+    sync()
+    assert torch.equal(a, b)
+
+
+def test_product_offsets_beyond_32_bits():
+    """The product of more rows than the few-row kernel takes, every operand and output with rows that start more than
+    2^32 bytes into its buffer."""
+    torch = torch_cuda()
+    M, N, K, ld8, ld = 40, 160, 384, (1 << 27) + 16, (1 << 26) + 4
+    a, w, b, want, mag = _product(M, N, K, 31)
+    tb = vec(b)
+    far = lm.lazymar_block8(_spread(a.get()[0], "byte", ld8), a.scale)
+    far_w = lm.lazymar_block8(_spread(w.get()[0], "byte", ld8), w.scale)
+    zeros = np.zeros((M, N), np.float32)
+    y, z = out(M, N), _spread(zeros, "fp32", ld)
+    y8, z8 = Held(M, N), _spread(zeros.astype(np.uint8), "byte", ld8)
+    s8 = torch.zeros((2, M), dtype=torch.uint8, device="cuda")
+    lm.lazymar_block8_linear(0, a.d, w.d, tb, None, 0, 0, y, N, y8.d, None, M, N, K)
+    lm.lazymar_block8_linear(0, far, far_w, tb, None, 0, 0, z, ld, lm.lazymar_block8(z8, s8), None, M, N, K)
+    sync()
+    close(z, want, _product_bound(mag, K))
+    assert torch.equal(y, z) and torch.equal(y8.q[:, :N], z8) and torch.equal(y8.scale, s8)
+    lm.lazymar_block8_linear(2, far, far_w, tb, z, ld, 0, z, ld, None, None, M, N, K)
+    sync()
+    close(z, 2 * want, 2 * _product_bound(mag, K) + 2 * U * np.abs(want))
+
+
+def _backward_calls():
+    """LayerNorm's, GELU's and the weight gradient with workspaces, as a function of no arguments, its inputs and its
+    outputs."""
+    torch = torch_cuda()
+    M, D, N = 3000, 320, 256
+    r = rng(32)
+    h, v = held(r.standard_normal((M, D)))
+    _, mean, rstd = T.layernorm(v, None, None, EPS)
+    tm, tr = vec(mean), vec(rstd)
+    dy, dn = dev(r.standard_normal((M, D)), "bf16")[0], dev(r.standard_normal((M, N)), "bf16")[0]
+    ws = [torch.empty(n + 16, dtype=torch.uint8, device="cuda") for n in (
+        lm.lazymar_layernorm_backward_workspace(M, D), lm.lazymar_block8_gelu_backward_workspace(M, D),
+        lm.lazymar_block8_wgrad_workspace(M, N, D))]
+    assert ws[2].numel() > 16  # in parts, with a sum of its own
+    outs = [out(M, D), vec(np.zeros(D)), vec(np.zeros(D)), out(M, D, "bf16"), vec(np.zeros(D)), out(N, D)]
+    dx, dg, db, du, dbu, dw = outs
+
+    def call():
+        lm.lazymar_layernorm_backward(1, dy, D, 0, None, 0, h.d, tm, tr, None, None, 0, 0, dx, D, dg, db, False, M, D,
+                                      ws[0], ws[0].numel())
+        lm.lazymar_block8_gelu_backward(1, dy, D, h.d, 1, du, D, None, dbu, False, M, D, ws[1], ws[1].numel())
+        lm.lazymar_block8_wgrad(dn, N, h.d, dw, D, False, M, N, D, ws[2], ws[2].numel())
+    return call, (h.q, dy, dn), outs
+
+
+def test_calls_with_workspaces_can_be_captured():
+    torch = torch_cuda()
+    call, _, outs = _backward_calls()
+    call()
+    sync()
+    want = [t.clone() for t in outs]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for t in outs:
+        t.zero_()
+    g.replay()
+    sync()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_calls_with_workspaces_follow_the_callers_stream():
+    """On a side stream, behind work that is still running there and then sets their inputs."""
+    torch = torch_cuda()
+    call, inputs, outs = _backward_calls()
+    call()
+    sync()
+    want, kept = [t.clone() for t in outs], [t.clone() for t in inputs]
+    for t in inputs + tuple(outs):
+        t.zero_()
+    big = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        for _ in range(8):
+            big = big @ big * 1e-3
+        for t, k in zip(inputs, kept):
+            t.copy_(k)
+        call()
+    st.synchronize()
+    lm.lazymar_device_check()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
