@@ -444,7 +444,8 @@ __global__ void __launch_bounds__(256, 2) ln_backward_ring_kernel(const LnBackwa
     const float mu = mean, rs = rstd;
     const uint32_t scales = sb;
     statistics(row + step);
-    const bool ok = mine == 0 || mbar_wait(&bars[warp][slot], phase, abort_flag, err);
+    // (once a wait has run out, no more: they would take 64 ms for each row that is left)
+    const bool ok = mine == 0 || dead || mbar_wait(&bars[warp][slot], phase, abort_flag, err);
     dead |= !__all_sync(0xffffffffu, ok);
     const uint8_t* src = ring + (size_t)slot * row_bytes;
     float y[NB][4], h[NB][4], s1 = 0.f, s2 = 0.f;
