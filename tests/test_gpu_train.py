@@ -1040,3 +1040,34 @@ def test_calls_with_workspaces_follow_the_callers_stream():
     st.synchronize()
     lm.lazymar_device_check()
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_calls_in_a_row_do_not_see_each_others_workspace():
+    """Two sets of inputs in turn through one workspace, launched without a wait in between: every result is its own."""
+    torch = torch_cuda()
+    M, D, N = 3000, 320, 256
+    r = rng(33)
+    sets = []
+    for scale in (1.0, 3.0):
+        h, v = held(scale * r.standard_normal((M, D)))
+        _, mean, rstd = T.layernorm(v, None, None, EPS)
+        sets.append((h, vec(mean), vec(rstd), dev(r.standard_normal((M, D)), "bf16")[0], dev(r.standard_normal((M, N)), "bf16")[0]))
+    n = max(lm.lazymar_layernorm_backward_workspace(M, D), lm.lazymar_block8_gelu_backward_workspace(M, D),
+            lm.lazymar_block8_wgrad_workspace(M, N, D))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+
+    def run(o, h, mean, rstd, dy, dn):
+        lm.lazymar_layernorm_backward(1, dy, D, 0, None, 0, h.d, mean, rstd, None, None, 0, 0, o[0], D, o[1], o[2], False, M,
+                                      D, ws, n)
+        lm.lazymar_block8_gelu_backward(1, dy, D, h.d, 0, None, 0, None, o[3], False, M, D, ws, n)
+        lm.lazymar_block8_wgrad(dn, N, h.d, o[4], D, False, M, N, D, ws, n)
+    made = [[out(M, D), vec(np.zeros(D)), vec(np.zeros(D)), vec(np.zeros(D)), out(N, D)] for _ in range(42)]
+    want = made[:2]
+    for o, s in zip(want, sets):
+        run(o, *s)
+        sync()
+    for i, o in enumerate(made[2:]):
+        run(o, *sets[i % 2])
+    sync()
+    for i, o in enumerate(made[2:]):
+        assert all(torch.equal(a, b) for a, b in zip(o, want[i % 2])), i
