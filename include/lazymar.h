@@ -448,7 +448,7 @@ lazymar_status lazymar_head_schedule(int n_train, int n_steps, int32_t *kept, fl
 
 /* ------------------------------------------------------------------------
  * Training a block with 8-bit activations. The paper trains nothing; these
- * entry points are what tuning a block of the transformer needs next to the
+ * entry points are what tuning the MLP half of a block needs next to the
  * decoding step: LayerNorm's gradient, activations kept for the backward pass
  * in 8 bits, and 8-bit matrix products with a scale for each block of 128.
  * Device pointers only; no call allocates; a workspace is the caller's.

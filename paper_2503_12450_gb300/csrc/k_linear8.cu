@@ -12,12 +12,13 @@
 // row % 32, column = row / 32, the same in each quarter of the lanes) and eight for
 // 256 rows of w, written by tcgen05.st straight from the scale bytes.
 //
-// Measured: 20480 x 5120 x 1280 with GELU and two 8-bit outputs 112 us (2400 TFLOP/s),
-// 40960 x 1024 x 4096 with fp32 residual and output 134 us (2570); without any output
-// 97 and 100 us or so. What bounds it: the MMAs of a stage take 690 cycles alone
-// (512 nominal) and 900 next to the loads of the next stages and the epilogue,
-// which share shared and tensor memory with them; in a long run the 1400 W limit
-// (1365 W drawn, sw_power_cap active) makes it 122 to 128 and 149 to 155 us.
+// Measured: 20480 x 5120 x 1280 with GELU and two 8-bit outputs 111 us (2410 TFLOP/s) in
+// short runs and 124 in long ones, 40960 x 1024 x 4096 with fp32 residual and output
+// 131 (2620) and 151; without any output 97 and 100 us or so. What bounds it: in a long
+// run the 1400 W limit (sw_power_cap active, SM clock 1755 and 1462 MHz of 2070); in a
+// short one the MMAs of a stage, 690 cycles alone (512 nominal; the difference is not
+// explained) and 900 next to the loads of the next stages and the epilogue, which
+// share shared and tensor memory with them.
 //
 // Accuracy: the accumulator of the tensor cores is fp32 and truncates, so a sum comes
 // out too small in magnitude by 6.9e-8 of itself at K = 1280, 3.3e-7 at 5120 and 4e-6

@@ -5,7 +5,8 @@
 // of w, the warps take its K blocks in turn, and all loads of a warp's block are in
 // flight at once. Measured (us, against the tcgen05 kernel on single CTAs): 2 x 4096
 // x 1024 3.1 : 9.2 (the weights' 4 MB: 0.6), 8 x 1024 x 4096 5.1 : 17.4, 32 x 1024 x 4096
-// 8.5 : 18.5 and 7.4 with K in parts, 32 x 4096 x 1024 4.8 : 9.6.
+// 8.5 : 18.5 (and 7.4 with K in parts: the limit of 32 rows is not the best at every K),
+// 32 x 4096 x 1024 4.8 : 9.6.
 //
 // E4M3 is exact in fp16, so the products run as fp16 warp MMAs (m16n8k16, w as the
 // 16-row operand, tokens as the 8 columns) with fp32 sums; a block's sum is scaled

@@ -3,9 +3,9 @@
 //
 // The sum runs over tokens, and a checkpoint's scales differ from token to
 // token, so the 8-bit tensor cores cannot apply them. But E4M3 times a power of
-// two is exact in bf16 (from 2^-130 on; subnormals count): converter warps turn the checkpoint's bytes into the
-// bf16 operand in shared memory, and the product runs at the bf16 rate without
-// the activation ever being written out in 16 bits.
+// two is exact in bf16 (from 2^-130 on; subnormals count): converter warps turn
+// the checkpoint's bytes into the bf16 operand in shared memory, and the product
+// runs at the bf16 rate without the activation ever being written out in 16 bits.
 //
 // Both operands are "MN-major" (the reduced axis is the rows of the tensors):
 // an operand tile is 64-column pieces of 128-byte rows, one row a token, in the
@@ -17,8 +17,8 @@
 // warps, rounding to nearest, while the next 512 run into the other half of
 // tensor memory (2.2e-7 at 20480 tokens; an fp32 library product 8.5e-7).
 //
-// Measured: 20480 tokens x 4096 x 1024 130 us, 1322 TFLOP/s on 64 of 76 CTA pairs
-// (a library's bf16 product at its best: 1901 on all). Bound by the converters: 8 warps need 0.29 us for
+// Measured: 20480 tokens x 4096 x 1024 130 us, 1320 TFLOP/s on 64 of 76 CTA pairs
+// (a library's bf16 product at its best: 1901 on all), 135 in long runs. Bound by the converters: 8 warps need 0.29 us for
 // a stage's 64 x 128 bytes, the MMAs 0.2 to 0.25.
 #include <cuda.h>
 
