@@ -62,7 +62,7 @@ extern "C" lazymar_status lazymar_layernorm_forward(int x_dtype, const void* x, 
   if (M > kMost) return too_large();
   if (M == 0) return LAZYMAR_OK;  // (empty tensors have no address)
   if (!y && !y8 && !x8 && !mean && !rstd) return bad("no output given");
-  if (x == y && M > 1 && (x_dtype != y_dtype || ldx != ldy))  // (as below)
+  if (y && x == y && M > 1 && (x_dtype != y_dtype || ldx != ldy))  // (as below)
     return bad("y in place of x: y_dtype = x_dtype and ldy = ldx required");
   TR_TRY(check_mat(x, x_dtype, ldx, D, "x: fp32 or bf16 device tensor, ldx >= D required"));
   if (y) TR_TRY(check_mat(y, y_dtype, ldy, D, "y: fp32 or bf16 device tensor, ldy >= D required"));
@@ -104,7 +104,7 @@ extern "C" lazymar_status lazymar_layernorm_backward(int dy_dtype, const void* d
   if (M > 0) {
     if ((x == nullptr) == (x8 == nullptr)) return bad("exactly one of x and x8 required");
     // (rows are worked on side by side: in another layout dx would overwrite rows that are still to be read)
-    if (M > 1 && ((dx == dy && (dx_dtype != dy_dtype || lddx != lddy)) || (dx == x && (dx_dtype != x_dtype || lddx != ldx))))
+    if (dx && M > 1 && ((dx == dy && (dx_dtype != dy_dtype || lddx != lddy)) || (dx == x && (dx_dtype != x_dtype || lddx != ldx))))
       return bad("dx in place of dy or x: the same type and stride required");
     if (dres && dx == dres && (dx_dtype != LAZYMAR_F32 || (M > 1 && lddx != lddres)))
       return bad("dx in place of dres: fp32 with the same stride required");

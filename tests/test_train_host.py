@@ -311,3 +311,12 @@ int main() {
     assert text == "1111 0001"
     source = open(os.path.join(ROOT, "paper_2503_12450_gb300", "csrc", "k_linear8.cu")).read()
     assert "rows_on_four(x.out.p" in source and "rows_on_four(x.residual.p" in source
+
+
+def test_missing_tensors_are_not_taken_for_calls_in_place(lib):
+    q = _b8()
+    assert lib.lazymar_layernorm_forward(0, None, 8, None, None, 1, None, 0, q.addr, None, None, None, 4, 8, 1e-6, None) == 1
+    assert "x:" in lib.lazymar_last_error().decode() and "in place" not in lib.lazymar_last_error().decode()
+    assert lib.lazymar_layernorm_backward(1, None, 8, 0, None, 0, q.addr, 16, 16, None, None, 0, 0, None, 8, None, None, 0,
+                                          4, 8, None, 0, None) == 1
+    assert "dy:" in lib.lazymar_last_error().decode()
