@@ -104,7 +104,8 @@ extern "C" lazymar_status lazymar_layernorm_backward(int dy_dtype, const void* d
   if (M > 0) {
     if ((x == nullptr) == (x8 == nullptr)) return bad("exactly one of x and x8 required");
     // (rows are worked on side by side: in another layout dx would overwrite rows that are still to be read)
-    if (dx && M > 1 && ((dx == dy && (dx_dtype != dy_dtype || lddx != lddy)) || (dx == x && (dx_dtype != x_dtype || lddx != ldx))))
+    if (dx && M > 1 && ((dx == dy && (dx_dtype != dy_dtype || lddx != lddy)) ||
+                        (dx == x && (dx_dtype != x_dtype || lddx != ldx))))
       return bad("dx in place of dy or x: the same type and stride required");
     if (dres && dx == dres && (dx_dtype != LAZYMAR_F32 || (M > 1 && lddx != lddres)))
       return bad("dx in place of dres: fp32 with the same stride required");
