@@ -42,8 +42,8 @@
  *     nothing. Errors detected on the device (bounded waits that expired,
  *     out-of-range indices or labels) are latched in a device error word and
  *     reported by lazymar_sync / lazymar_device_check.
- *   - No call allocates device memory except lazymar_create and
- *     lazymar_head_create.
+ *   - No call allocates device memory except lazymar_create,
+ *     lazymar_head_create and lazymar_params_create.
  *   - A handle is not thread-safe; distinct handles are independent.
  */
 #ifndef LAZYMAR_H
@@ -565,6 +565,154 @@ size_t lazymar_block8_wgrad_workspace(int M, int N, int K);
 lazymar_status lazymar_block8_wgrad(const void* dy, int lddy, const lazymar_block8* x, float* dw, int lddw,
                                     int accumulate, int M, int N, int K, void* workspace, size_t workspace_bytes,
                                     void* stream);
+
+/* ------------------------------------------------------------------------
+ * The residual join: what stands between two branches of a transformer, or of
+ * the diffusion head's MLP, in one pass over the rows. For row m of M, with the
+ * modulation's row r = m / group (group 0: the one row that all share),
+ *   u = post(y)                         the branch's output behind its norm
+ *   z = res x + gate[r] (u post_g + post_b)
+ *   h = (pre(z) pre_g + pre_b) (1 + scale[r]) + shift[r]
+ * with post and pre one of
+ *   LAZYMAR_NORM_NONE   v
+ *   LAZYMAR_NORM_LAYER  (v - mean) rstd,  rstd = 1 / sqrt(mean((v - mean)^2) + eps)
+ *   LAZYMAR_NORM_RMS    v rstd,           rstd = 1 / sqrt(mean(v^2) + eps)
+ * Absent (p or pointer NULL): gate, scale, post_g, pre_g count as 1, 0, 1, 1,
+ * shift, post_b and pre_b as 0; without y, z = res x. Everything between the inputs and
+ * an output is fp32 and each output is rounded once: h comes from z before
+ * z's own rounding. The conventions of the training operators hold (device
+ * pointers, strides, alignment, no allocation, the same results from call to
+ * call). 1 <= D <= 8192.
+ * ------------------------------------------------------------------------ */
+enum { LAZYMAR_NORM_NONE = 0, LAZYMAR_NORM_LAYER = 1, LAZYMAR_NORM_RMS = 2 };
+
+/* Rows of D columns: fp32 or bf16 with row stride ld (elements), or
+ * LAZYMAR_E4M3, a block8 tensor (q at p with ldq = ld, its scales at scale with
+ * lds). p NULL: absent. */
+typedef struct lazymar_rows {
+  void* p;
+  uint8_t* scale;  /* LAZYMAR_E4M3 only */
+  int dtype, ld, lds;
+} lazymar_rows;
+
+typedef struct lazymar_join_args {
+  int M, D;          /* rows, columns */
+  int group;         /* rows that share a row of gate, scale and shift: ceil(M / group) rows of each; 0: one row */
+  int post, pre;     /* LAZYMAR_NORM_* */
+  float res, eps;    /* eps > 0, of both norms */
+  lazymar_rows x;    /* [M, D] fp32 or bf16: the residual stream */
+  lazymar_rows y;    /* [M, D] fp32, bf16 or E4M3: the branch's output; absent: post, gate, post_g, post_b are too */
+  lazymar_rows gate, scale, shift;             /* fp32 or bf16; scale and shift need pre */
+  const float *post_g, *post_b, *pre_g, *pre_b; /* [D]; pre_g and pre_b need pre */
+  lazymar_rows z;    /* [M, D] fp32 or bf16; may be x or y itself, with its type and stride */
+  lazymar_rows h;    /* [M, D] fp32 or bf16; the same */
+  lazymar_rows h8, z8, y8; /* E4M3: h as the operand of lazymar_block8_linear, z and y as checkpoints */
+  float *y_mean, *y_rstd;  /* [M] statistics of post (may be NULL); means of LAZYMAR_NORM_RMS are 0 */
+  float *z_mean, *z_rstd;  /* [M] those of pre */
+} lazymar_join_args;
+
+/* At least one output is given; h and h8 need pre. */
+lazymar_status lazymar_join(const lazymar_join_args* a, void* stream);
+
+/* Its gradient. With dh the gradient of h, dz that of z from elsewhere (the
+ * residual stream), n = pre(z), and norm' the norm's gradient with the statistics of
+ * the forward pass,
+ *   Z = dz + pre'(dh (1 + scale) pre_g)    dx = res Z
+ *   V = Z gate                             dy = post'(V post_g)
+ *   dgate = sum Z (u post_g + post_b)      dpost_g = sum V u,  dpost_b = sum V
+ *   dscale = sum dh (n pre_g + pre_b)      dpre_g = sum dh (1 + scale) n
+ *   dshift = sum dh                        dpre_b = sum dh (1 + scale)
+ * The sums of gate, scale and shift run over the rows that share one, the
+ * others over all rows. (dpost_b without a norm is also the gradient of a bias that
+ * y already contains.) */
+typedef struct lazymar_join_grad_args {
+  int M, D, group, post, pre;
+  float res;
+  int accumulate;    /* 1: dgate .. dpre_b are added to */
+  lazymar_rows dh;   /* [M, D] fp32 or bf16; given exactly if pre is not NONE */
+  lazymar_rows dz;   /* [M, D] fp32 or bf16; may be absent if dh is given */
+  lazymar_rows z;    /* [M, D] fp32, bf16 or E4M3; needed with pre */
+  lazymar_rows y;    /* [M, D] fp32, bf16 or E4M3; needed with post, dgate or dpost_g */
+  lazymar_rows gate, scale;
+  const float *post_g, *post_b, *pre_g, *pre_b;
+  const float *y_mean, *y_rstd, *z_mean, *z_rstd;  /* of the norms that there are; means not with LAZYMAR_NORM_RMS */
+  lazymar_rows dx;   /* [M, D] fp32 or bf16; may be absent, or dz, dh, z or y itself with its type and stride */
+  lazymar_rows dy;   /* the same */
+  lazymar_rows dy8;  /* [M, D] E4M3: dy as the operand of the input gradient's product */
+  lazymar_rows dgate, dscale, dshift;              /* [ceil(M / group) or 1, D] fp32 or bf16; may be absent */
+  float *dpost_g, *dpost_b, *dpre_g, *dpre_b;      /* [D]; may be NULL */
+  void* workspace;   /* 16-byte aligned; needed if one of dgate .. dpre_b is given */
+  size_t workspace_bytes;  /* >= lazymar_join_grad_workspace(M, D, group) */
+} lazymar_join_grad_args;
+
+size_t lazymar_join_grad_workspace(int M, int D, int group);
+lazymar_status lazymar_join_grad(const lazymar_join_grad_args* a, void* stream);
+
+/* ------------------------------------------------------------------------
+ * The end of a training step, over a list of tensors: the norm of all
+ * gradients with the factor that clips it, the clipped gradients, and the
+ * weights' update. What the step depends on stays on the device: nothing is
+ * copied to the host, and the calls can be captured into a graph.
+ * ------------------------------------------------------------------------ */
+typedef struct lazymar_param {
+  long long n;       /* elements, consecutive in each of the tensors; may be 0 */
+  const void* g;     /* the gradient */
+  int g_dtype;       /* LAZYMAR_F32 or LAZYMAR_BF16 */
+  int out_dtype;
+  void* out;         /* target of lazymar_clip_grads, out_dtype fp32 or bf16; NULL: g itself */
+  float *p, *m, *v;  /* weights, first and second moments (lazymar_adamw; all or none) */
+  float* ema;        /* averaged weights (may be NULL) */
+  void* copy;        /* bf16 copy of the weights (may be NULL) */
+  float lr_scale;    /* factor of the learning rate */
+  float weight_decay;
+} lazymar_param;
+
+/* A list of `count` tensors, on the current device. The handle keeps the
+ * addresses (not the values) in device memory, so the tensors stay where they are
+ * while it lives; tensors of a list do not overlap. The calls on it take its
+ * own scratch: one stream at a time, and no two graphs that run at once.
+ * At most 2^20 tensors and 2^40 elements. Addresses on boundaries of 32 bytes (bf16: 16)
+ * are faster. */
+typedef struct lazymar_params lazymar_params;
+lazymar_status lazymar_params_create(const lazymar_param* list, int count, lazymar_params** out);
+void lazymar_params_destroy(lazymar_params* h);
+
+/* What the calls leave for each other, in device memory of the caller (4-byte
+ * aligned): zeros before the first step. */
+typedef struct lazymar_step_state {
+  float norm;        /* of the last lazymar_grad_norm */
+  float factor;      /* what a gradient is multiplied by; 0: this step is skipped */
+  int32_t steps;     /* calls with a finite norm */
+  int32_t skipped;   /* other calls */
+} lazymar_step_state;
+
+/* norm = scale sqrt(sum of g^2 over the list), factor = scale min(1, max_norm / norm),
+ * steps += 1; where the norm is not finite (an infinity or NaN among the gradients, or
+ * 2^128 and more) factor = 0 and skipped += 1 instead. scale > 0 (1 / loss scale, 1 / number
+ * of accumulated batches), max_norm > 0, infinity: no clipping. Squares do not
+ * overflow or vanish at any size of the gradients; sums are fp64, the same from
+ * call to call. */
+lazymar_status lazymar_grad_norm(lazymar_params* h, float scale, float max_norm, lazymar_step_state* state, void* stream);
+
+/* out = factor g (zeros where factor is 0), rounded once. */
+lazymar_status lazymar_clip_grads(lazymar_params* h, const lazymar_step_state* state, void* stream);
+
+/* AdamW with g' = factor g, t = steps, and l = lr lr_scale of the tensor:
+ *   m += (1 - beta1) (g' - m)        v += (1 - beta2) (g'^2 - v)
+ *   p -= l (weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ *   ema += (1 - ema_decay) (p - ema)   copy = bf16(p)
+ * With factor 0 nothing is changed. state NULL: factor and t are the arguments'.
+ * lr_device (may be NULL): the learning rate in device memory, which replaces lr
+ * (a schedule under a captured graph). fp32 throughout. 0 <= beta < 1, eps > 0,
+ * 0 <= ema_decay <= 1. */
+typedef struct lazymar_adamw_args {
+  double lr, beta1, beta2, eps, ema_decay;
+  const float* lr_device;
+  double factor;     /* without state: > 0 */
+  int steps;         /* without state: t >= 1 */
+} lazymar_adamw_args;
+lazymar_status lazymar_adamw(lazymar_params* h, const lazymar_adamw_args* a, const lazymar_step_state* state,
+                             void* stream);
 
 /* Per kernel class: kernel launches, algorithmic flops and bytes, and (while
  * profiling is on) device time from CUDA events recorded around each call on

@@ -1,6 +1,13 @@
 // C ABI of the training operators (include/lazymar.h, "Training a block with
-// 8-bit activations"): argument checks and dispatch.
+// 8-bit activations", "The residual join" and "The end of a training step"):
+// argument checks and dispatch.
 #include "block8.cuh"
+#include "join.cuh"
+#include "optim.cuh"
+
+#include <cmath>
+#include <new>
+#include <vector>
 
 using namespace lm;
 
@@ -307,4 +314,367 @@ extern "C" lazymar_status lazymar_block8_wgrad(const void* dy, int lddy, const l
   p.K = K;
   p.ws = static_cast<float*>(workspace);
   return done(launch_wgrad8(c, p), "weight gradient kernel");
+}
+
+// ---------------------------------------------------------------------------
+// The residual join
+// ---------------------------------------------------------------------------
+namespace {
+
+// What a call may be given: [rows, cols] of fp32 or bf16, of E4M3 as well, of E4M3 alone.
+enum { ROWS_FLOAT, ROWS_ANY, ROWS_8 };
+lazymar_status check_rows(const lazymar_rows& r, int kind, int rows, int cols, const char* msg) {
+  if (!r.p) return LAZYMAR_OK;
+  if (r.dtype == LAZYMAR_E4M3 && kind != ROWS_FLOAT) {
+    const lazymar_block8 q{r.p, r.scale, r.ld, r.lds};
+    return check_block8(&q, cols, rows, msg);
+  }
+  if (kind == ROWS_8) return bad(msg);
+  return check_mat(r.p, r.dtype, r.ld, cols, msg);
+}
+Rows rows_of(const lazymar_rows& r) {
+  const bool e8 = r.dtype == LAZYMAR_E4M3;
+  return Rows{r.p, r.scale, r.ld, r.lds, r.dtype, e8 || vec8(r.p, r.dtype, r.ld)};
+}
+MatOut out_of(const lazymar_rows& r) { return mat_out(r.p, r.ld, r.dtype); }
+lazymar_block8 eight_of(const lazymar_rows& r) { return lazymar_block8{r.p, r.scale, r.ld, r.lds}; }
+
+// An output in place of an input: rows are worked on side by side, so in another layout they
+// would overwrite rows that are still to be read.
+bool displaced(const lazymar_rows& out, const lazymar_rows& in, int M) {
+  return out.p && out.p == in.p && (out.dtype != in.dtype || (M > 1 && out.ld != in.ld));
+}
+bool norm_kind(int k) { return k == LAZYMAR_NORM_NONE || k == LAZYMAR_NORM_LAYER || k == LAZYMAR_NORM_RMS; }
+int mod_rows(int M, int group) { return group > 0 ? (int)(((long long)M + group - 1) / group) : 1; }
+
+#define CHECK_ROWS(field, kind, rows)                                                                            \
+  TR_TRY(check_rows(a->field, kind, rows, a->D,                                                                  \
+                    kind == ROWS_8 ? #field ": E4M3 device tensor, 16-byte aligned, ld % 16 == 0, ld >= D, lds >= rows required" \
+                    : kind == ROWS_ANY                                                                           \
+                        ? #field ": fp32, bf16 or E4M3 device tensor, ld >= D (E4M3: 16-byte aligned, ld % 16 == 0, lds >= rows) required" \
+                        : #field ": fp32 or bf16 device tensor, ld >= D required"))
+
+}  // namespace
+
+extern "C" lazymar_status lazymar_join(const lazymar_join_args* a, void* stream) {
+  if (!a) return bad("a required");
+  if (a->M < 0 || a->D < 1 || a->group < 0) return bad("M >= 0, D >= 1, group >= 0 required");
+  if (!norm_kind(a->post) || !norm_kind(a->pre)) return bad("post and pre: LAZYMAR_NORM_NONE, _LAYER or _RMS");
+  if (!(a->eps > 0.f) || !std::isfinite(a->eps) || !std::isfinite(a->res)) return bad("eps > 0 and a finite res required");
+  if (a->D > kLnMaxWidth) return report_error(LAZYMAR_ERR_UNSUPPORTED, "D <= 8192 required");
+  if (a->M > kMost) return too_large();
+  if (a->M == 0) return LAZYMAR_OK;  // (empty tensors have no address)
+  if (!a->z.p && !a->h.p && !a->h8.p && !a->z8.p && !a->y8.p && !a->y_mean && !a->y_rstd && !a->z_mean && !a->z_rstd)
+    return bad("no output given");
+  if (!a->y.p && (a->post || a->gate.p || a->post_g || a->post_b || a->y8.p || a->y_mean || a->y_rstd))
+    return bad("post, gate, post_g, post_b, y8 and y's statistics need y");
+  if (!a->post && (a->y_mean || a->y_rstd)) return bad("y_mean and y_rstd need post");
+  if (!a->pre && (a->h.p || a->h8.p || a->scale.p || a->shift.p || a->pre_g || a->pre_b || a->z_mean || a->z_rstd))
+    return bad("h, h8, scale, shift, pre_g, pre_b and z's statistics need pre");
+  if (!a->x.p) return bad("x: fp32 or bf16 device tensor, ld >= D required");
+  if (a->z.p && a->z.p == a->h.p) return bad("z and h in one place");
+  for (const lazymar_rows* out : {&a->z, &a->h})
+    for (const lazymar_rows* in : {&a->x, &a->y})
+      if (displaced(*out, *in, a->M)) return bad("z or h in place of x or y: the same type and stride required");
+  const int mods = mod_rows(a->M, a->group);
+  CHECK_ROWS(x, ROWS_FLOAT, a->M);
+  CHECK_ROWS(y, ROWS_ANY, a->M);
+  CHECK_ROWS(gate, ROWS_FLOAT, mods);
+  CHECK_ROWS(scale, ROWS_FLOAT, mods);
+  CHECK_ROWS(shift, ROWS_FLOAT, mods);
+  CHECK_ROWS(z, ROWS_FLOAT, a->M);
+  CHECK_ROWS(h, ROWS_FLOAT, a->M);
+  CHECK_ROWS(h8, ROWS_8, a->M);
+  CHECK_ROWS(z8, ROWS_8, a->M);
+  CHECK_ROWS(y8, ROWS_8, a->M);
+  for (const float* q : {a->post_g, a->post_b, a->pre_g, a->pre_b, (const float*)a->y_mean, (const float*)a->y_rstd,
+                         (const float*)a->z_mean, (const float*)a->z_rstd})
+    if (q) TR_TRY(check_f32(q, "parameters and statistics must be fp32 device pointers"));
+  Ctx c;
+  TR_TRY(component_ctx(stream, &c));
+  Join p{};
+  p.M = a->M;
+  p.D = a->D;
+  p.group = a->group;
+  p.post = a->post;
+  p.pre = a->pre;
+  p.res = a->res;
+  p.eps = a->eps;
+  p.x = rows_of(a->x);
+  p.y = rows_of(a->y);
+  p.gate = rows_of(a->gate);
+  p.scale = rows_of(a->scale);
+  p.shift = rows_of(a->shift);
+  p.post_g = a->post_g;
+  p.post_b = a->post_b;
+  p.pre_g = a->pre_g;
+  p.pre_b = a->pre_b;
+  p.params_vec = at(p.post_g, 32) && at(p.post_b, 32) && at(p.pre_g, 32) && at(p.pre_b, 32);
+  p.z = out_of(a->z);
+  p.h = out_of(a->h);
+  p.h8 = eight_of(a->h8);
+  p.z8 = eight_of(a->z8);
+  p.y8 = eight_of(a->y8);
+  p.y_mean = a->y_mean;
+  p.y_rstd = a->y_rstd;
+  p.z_mean = a->z_mean;
+  p.z_rstd = a->z_rstd;
+  return done(launch_join(c, p), "residual join kernel");
+}
+
+extern "C" size_t lazymar_join_grad_workspace(int M, int D, int group) { return join_grad_workspace(M, D, group); }
+
+extern "C" lazymar_status lazymar_join_grad(const lazymar_join_grad_args* a, void* stream) {
+  if (!a) return bad("a required");
+  if (a->M < 0 || a->D < 1 || a->group < 0) return bad("M >= 0, D >= 1, group >= 0 required");
+  if (!norm_kind(a->post) || !norm_kind(a->pre)) return bad("post and pre: LAZYMAR_NORM_NONE, _LAYER or _RMS");
+  if (!std::isfinite(a->res)) return bad("a finite res required");
+  if (a->D > kLnMaxWidth) return report_error(LAZYMAR_ERR_UNSUPPORTED, "D <= 8192 required");
+  if (a->M > kMost) return too_large();
+  const bool sums = a->dgate.p || a->dscale.p || a->dshift.p || a->dpost_g || a->dpost_b || a->dpre_g || a->dpre_b;
+  if (!sums && a->M == 0) return LAZYMAR_OK;
+  if (!sums && !a->dx.p && !a->dy.p && !a->dy8.p) return bad("no output given");
+  if (!a->pre && (a->scale.p || a->pre_g || a->pre_b || a->dscale.p || a->dshift.p || a->dpre_g || a->dpre_b))
+    return bad("scale, pre_g, pre_b and the gradients of these and of shift need pre");
+  const int mods = mod_rows(a->M, a->group);
+  if (a->M > 0) {
+    if ((a->dh.p != nullptr) != (a->pre != LAZYMAR_NORM_NONE)) return bad("dh: given exactly with pre");
+    if (!a->dh.p && !a->dz.p) return bad("dh or dz required");
+    if (a->pre && (!a->z.p || !a->z_rstd || (a->pre == LAZYMAR_NORM_LAYER && !a->z_mean)))
+      return bad("pre needs z and its statistics");
+    if ((a->post || a->dgate.p || a->dpost_g) && !a->y.p) return bad("post, dgate and dpost_g need y");
+    if (a->post && (!a->y_rstd || (a->post == LAZYMAR_NORM_LAYER && !a->y_mean))) return bad("post needs y's statistics");
+    if (a->dx.p && a->dx.p == a->dy.p) return bad("dx and dy in one place");
+    for (const lazymar_rows* out : {&a->dx, &a->dy})
+      for (const lazymar_rows* in : {&a->dh, &a->dz, &a->z, &a->y})
+        if (displaced(*out, *in, a->M)) return bad("dx or dy in place of an input: the same type and stride required");
+    for (const lazymar_rows* out : {&a->dgate, &a->dscale, &a->dshift})
+      for (const lazymar_rows* in : {&a->gate, &a->scale})
+        if (out->p && out->p == in->p) return bad("gradients of gate, scale and shift in place of gate or scale");
+    CHECK_ROWS(dh, ROWS_FLOAT, a->M);
+    CHECK_ROWS(dz, ROWS_FLOAT, a->M);
+    CHECK_ROWS(z, ROWS_ANY, a->M);
+    CHECK_ROWS(y, ROWS_ANY, a->M);
+    CHECK_ROWS(gate, ROWS_FLOAT, mods);
+    CHECK_ROWS(scale, ROWS_FLOAT, mods);
+    CHECK_ROWS(dx, ROWS_FLOAT, a->M);
+    CHECK_ROWS(dy, ROWS_FLOAT, a->M);
+    CHECK_ROWS(dy8, ROWS_8, a->M);
+    for (const float* q : {a->post_g, a->post_b, a->pre_g, a->pre_b, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd})
+      if (q) TR_TRY(check_f32(q, "parameters and statistics must be fp32 device pointers"));
+  }
+  if (mods > 0) {
+    CHECK_ROWS(dgate, ROWS_FLOAT, mods);
+    CHECK_ROWS(dscale, ROWS_FLOAT, mods);
+    CHECK_ROWS(dshift, ROWS_FLOAT, mods);
+  }
+  for (const float* q : {a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b})
+    if (q) TR_TRY(check_f32(q, "dpost_g, dpost_b, dpre_g and dpre_b must be fp32 device pointers"));
+  if (sums) TR_TRY(check_workspace(a->workspace, a->workspace_bytes, join_grad_workspace(a->M, a->D, a->group)));
+  Ctx c;
+  TR_TRY(component_ctx(stream, &c));
+  JoinGrad p{};
+  p.M = a->M;
+  p.D = a->D;
+  p.group = a->group;
+  p.post = a->post;
+  p.pre = a->pre;
+  p.res = a->res;
+  p.accumulate = a->accumulate != 0;
+  p.dh = rows_of(a->dh);
+  p.dz = rows_of(a->dz);
+  p.z = rows_of(a->z);
+  p.y = rows_of(a->y);
+  if (!a->post && !a->dgate.p && !a->dpost_g) p.y.p = nullptr;  // (nothing depends on it)
+  p.gate = rows_of(a->gate);
+  p.scale = rows_of(a->scale);
+  p.y_mean = a->y_mean;
+  p.y_rstd = a->y_rstd;
+  p.z_mean = a->z_mean;
+  p.z_rstd = a->z_rstd;
+  p.post_g = a->post_g;
+  p.post_b = a->post_b;
+  p.pre_g = a->pre_g;
+  p.pre_b = a->pre_b;
+  p.params_vec = at(p.post_g, 32) && at(p.post_b, 32) && at(p.pre_g, 32) && at(p.pre_b, 32);
+  p.dx = out_of(a->dx);
+  p.dy = out_of(a->dy);
+  p.dy8 = eight_of(a->dy8);
+  p.dgate = out_of(a->dgate);
+  p.dscale = out_of(a->dscale);
+  p.dshift = out_of(a->dshift);
+  p.dpost_g = a->dpost_g;
+  p.dpost_b = a->dpost_b;
+  p.dpre_g = a->dpre_g;
+  p.dpre_b = a->dpre_b;
+  p.ws = static_cast<float*>(a->workspace);
+  return done(launch_join_grad(c, p), "residual join gradient kernel");
+}
+
+// ---------------------------------------------------------------------------
+// The end of a training step
+// ---------------------------------------------------------------------------
+struct lazymar_params {
+  int device = 0;
+  bool has_weights = false;
+  void* memory = nullptr;
+  ParamList list{};
+};
+
+namespace {
+
+constexpr int kMostParams = 1 << 20;
+
+lazymar_status check_param(const lazymar_param& t, bool weights) {
+  if (t.n < 0 || t.n > (1ll << 40)) return bad("n: 0 .. 2^40 elements");
+  if (!float_type(t.g_dtype)) return bad("g_dtype: fp32 or bf16");
+  if (t.out && !float_type(t.out_dtype)) return bad("out_dtype: fp32 or bf16");
+  if (t.out && t.out == t.g && t.out_dtype != t.g_dtype) return bad("out in place of g: the same type required");
+  if (!std::isfinite(t.lr_scale) || !std::isfinite(t.weight_decay)) return bad("finite lr_scale and weight_decay required");
+  if (t.n == 0) return LAZYMAR_OK;  // (empty tensors have no address)
+  if ((t.p != nullptr) != weights || (t.m != nullptr) != weights || (t.v != nullptr) != weights)
+    return bad("p, m and v: all or none, alike for the whole list");
+  if ((t.ema || t.copy) && !weights) return bad("ema and copy need p, m and v");
+  const void* fs[] = {t.p, t.m, t.v, t.ema};
+  for (const void* q : fs)
+    if (q && (!at(q, 4) || !is_device_ptr(q))) return bad("p, m, v and ema must be fp32 device pointers");
+  if (!at(t.g, elem(t.g_dtype)) || !is_device_ptr(t.g)) return bad("g must be a device pointer");
+  if (t.out && (!at(t.out, elem(t.out_dtype)) || !is_device_ptr(t.out))) return bad("out must be a device pointer");
+  if (t.copy && (!at(t.copy, 2) || !is_device_ptr(t.copy))) return bad("copy must be a bf16 device pointer");
+  return LAZYMAR_OK;
+}
+
+Param param_of(const lazymar_param& t) {
+  Param p{};
+  p.g = t.g;
+  p.out = t.out ? t.out : const_cast<void*>(t.g);
+  p.p = t.p;
+  p.m = t.m;
+  p.v = t.v;
+  p.ema = t.ema;
+  p.copy = static_cast<bf16*>(t.copy);
+  p.n = t.n;
+  p.lr_scale = t.lr_scale;
+  p.weight_decay = t.weight_decay;
+  const int out_dtype = t.out ? t.out_dtype : t.g_dtype;
+  const bool g8 = at(p.g, 8 * elem(t.g_dtype));
+  p.flags = (t.g_dtype == LAZYMAR_BF16 ? PARAM_G_BF16 : 0u) | (out_dtype == LAZYMAR_BF16 ? PARAM_OUT_BF16 : 0u) |
+            (g8 ? PARAM_VEC_G : 0u) | (g8 && at(p.out, 8 * elem(out_dtype)) ? PARAM_VEC_OUT : 0u) |
+            (g8 && at(t.p, 32) && at(t.m, 32) && at(t.v, 32) && at(t.ema, 32) && at(t.copy, 16) ? PARAM_VEC_ALL : 0u);
+  return p;
+}
+
+lazymar_status params_create(const lazymar_param* list, int count, lazymar_params** out) {
+  bool weights = false;
+  long long total = 0;
+  for (int i = 0; i < count; ++i) weights |= list[i].n > 0 && list[i].p != nullptr;
+  for (int i = 0; i < count; ++i) {
+    TR_TRY(check_param(list[i], weights));
+    total += list[i].n;
+    if (total > (1ll << 40)) return report_error(LAZYMAR_ERR_UNSUPPORTED, "at most 2^40 elements");
+  }
+  // pieces of a multiple of kPiece, at most about kMostPieces of them
+  const long long piece = kPiece * (1 + total / (kPiece * kMostPieces));
+  std::vector<Param> params;
+  std::vector<Piece> pieces;
+  for (int i = 0; i < count; ++i) {
+    if (list[i].n == 0) continue;
+    for (long long k = 0; k * piece < list[i].n; ++k) pieces.push_back(Piece{(unsigned)params.size(), (unsigned)k});
+    params.push_back(param_of(list[i]));
+  }
+  Ctx c;
+  TR_TRY(component_ctx(nullptr, &c));
+  const size_t a = params.size() * sizeof(Param), b = pieces.size() * sizeof(Piece);
+  const size_t at_pieces = (a + 255) / 256 * 256, at_partial = at_pieces + (b + 255) / 256 * 256;
+  const size_t bytes = at_partial + (size_t)c.num_sms * kNormCtasPerSm * sizeof(double);
+  lazymar_params* h = new lazymar_params;
+  cudaError_t e = cudaGetDevice(&h->device);
+  if (e == cudaSuccess) e = cudaMalloc(&h->memory, bytes);
+  char* m = static_cast<char*>(h->memory);
+  if (e == cudaSuccess && a) e = cudaMemcpy(m, params.data(), a, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess && b) e = cudaMemcpy(m + at_pieces, pieces.data(), b, cudaMemcpyHostToDevice);
+  if (e != cudaSuccess) {
+    lazymar_params_destroy(h);
+    return e == cudaErrorMemoryAllocation ? report_error(LAZYMAR_ERR_OOM, "device memory of the list") : report_cuda(e, "list");
+  }
+  h->has_weights = weights;
+  h->list = ParamList{reinterpret_cast<Param*>(m), reinterpret_cast<Piece*>(m + at_pieces),
+                      reinterpret_cast<double*>(m + at_partial), (int)pieces.size(), (int)piece};
+  *out = h;
+  return LAZYMAR_OK;
+}
+
+// The list's call: its handle, the state, the device.
+lazymar_status check_list(const lazymar_params* h, const lazymar_step_state* state, bool needed) {
+  if (!h) return bad("a list required");
+  if (!state && needed) return bad("state required");
+  if (state && (!at(state, 4) || !is_device_ptr(state))) return bad("state must be a 4-byte aligned device pointer");
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return report_cuda(e, "cudaGetDevice");
+  if (dev != h->device) return bad("the list was made on another device");
+  return LAZYMAR_OK;
+}
+
+}  // namespace
+
+extern "C" lazymar_status lazymar_params_create(const lazymar_param* list, int count, lazymar_params** out) {
+  if (!out) return bad("out required");
+  *out = nullptr;
+  if (count < 0 || (count > 0 && !list)) return bad("count >= 0 and a list required");
+  if (count > kMostParams) return report_error(LAZYMAR_ERR_UNSUPPORTED, "at most 2^20 tensors");
+  try {
+    return params_create(list, count, out);
+  } catch (const std::bad_alloc&) {
+    return report_error(LAZYMAR_ERR_OOM, "host memory of the list");
+  }
+}
+
+extern "C" void lazymar_params_destroy(lazymar_params* h) {
+  if (!h) return;
+  cudaFree(h->memory);
+  delete h;
+}
+
+extern "C" lazymar_status lazymar_grad_norm(lazymar_params* h, float scale, float max_norm, lazymar_step_state* state,
+                                            void* stream) {
+  if (!(scale > 0.f) || !std::isfinite(scale) || !(max_norm > 0.f)) return bad("scale > 0, finite, and max_norm > 0 required");
+  TR_TRY(check_list(h, state, true));
+  Ctx c;
+  TR_TRY(component_ctx(stream, &c));
+  return done(launch_grad_norm(c, h->list, scale, max_norm, state), "gradient norm kernel");
+}
+
+extern "C" lazymar_status lazymar_clip_grads(lazymar_params* h, const lazymar_step_state* state, void* stream) {
+  TR_TRY(check_list(h, state, true));
+  Ctx c;
+  TR_TRY(component_ctx(stream, &c));
+  return done(launch_clip_grads(c, h->list, state), "clipping kernel");
+}
+
+extern "C" lazymar_status lazymar_adamw(lazymar_params* h, const lazymar_adamw_args* a, const lazymar_step_state* state,
+                                        void* stream) {
+  if (!a) return bad("a required");
+  if (!(a->beta1 >= 0 && a->beta1 < 1 && a->beta2 >= 0 && a->beta2 < 1)) return bad("0 <= beta < 1 required");
+  if (!((float)a->eps > 0.f) || !std::isfinite((float)a->eps) || !std::isfinite((float)a->lr)) return bad("eps > 0 and a finite lr required");
+  if (!(a->ema_decay >= 0 && a->ema_decay <= 1)) return bad("0 <= ema_decay <= 1 required");
+  if (!state && (!((float)a->factor > 0.f) || !std::isfinite((float)a->factor) || a->steps < 1))
+    return bad("without state: factor > 0, finite, and steps >= 1 required");
+  if (a->lr_device) TR_TRY(check_f32(a->lr_device, "lr_device must be an fp32 device pointer"));
+  TR_TRY(check_list(h, state, false));
+  if (!h->has_weights && h->list.n_pieces > 0) return bad("the list has no weights");
+  Ctx c;
+  TR_TRY(component_ctx(stream, &c));
+  AdamW p{};
+  p.lr = (float)a->lr;
+  p.eps = (float)a->eps;
+  p.more1 = (float)(1 - a->beta1);
+  p.more2 = (float)(1 - a->beta2);
+  p.more_ema = (float)(1 - a->ema_decay);
+  p.log1 = (float)std::log(a->beta1);
+  p.log2 = (float)std::log(a->beta2);
+  p.lr_device = a->lr_device;
+  p.factor = (float)a->factor;
+  p.steps = a->steps;
+  return done(launch_adamw(c, h->list, p, state), "AdamW kernel");
 }

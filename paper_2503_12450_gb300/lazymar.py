@@ -17,6 +17,7 @@ LAZYMAR_CRITERION_VALUE, LAZYMAR_CRITERION_FEATURE = 0, 1
 LAZYMAR_SELECT_LEAST_SIMILAR, LAZYMAR_SELECT_MOST_SIMILAR, LAZYMAR_SELECT_RANDOM = 0, 1, 2
 LAZYMAR_CFG_GUIDE, LAZYMAR_CFG_REFRESH, LAZYMAR_CFG_REUSE = 0, 1, 2
 LAZYMAR_EPI_BIAS, LAZYMAR_EPI_GELU, LAZYMAR_EPI_RESIDUAL, LAZYMAR_EPI_QKV, LAZYMAR_EPI_SILU = 0, 1, 2, 3, 4
+LAZYMAR_NORM_NONE, LAZYMAR_NORM_LAYER, LAZYMAR_NORM_RMS = 0, 1, 2
 KERNEL_CLASSES = ["gemm", "attention", "layernorm", "select", "embed", "cfg", "other"]
 STATUS = {0: "LAZYMAR_OK", 1: "LAZYMAR_ERR_INVALID_ARG", 2: "LAZYMAR_ERR_OOM", 3: "LAZYMAR_ERR_CUDA",
           4: "LAZYMAR_ERR_STATE", 5: "LAZYMAR_ERR_TIMEOUT", 6: "LAZYMAR_ERR_UNSUPPORTED", 7: "LAZYMAR_ERR_DEVICE"}
@@ -87,6 +88,43 @@ class lazymar_block8_desc(ctypes.Structure):
     _fields_ = [("q", _FP), ("scale", _FP), ("ldq", ctypes.c_int), ("lds", ctypes.c_int)]
 
 
+class lazymar_rows_desc(ctypes.Structure):
+    """struct lazymar_rows; `keep` is what it points to."""
+    _fields_ = [("p", _FP), ("scale", _FP), ("dtype", ctypes.c_int), ("ld", ctypes.c_int), ("lds", ctypes.c_int)]
+
+
+class lazymar_join_desc(ctypes.Structure):
+    """struct lazymar_join_args; `addr` is its address, `keep` what it points to."""
+    _fields_ = [(n, ctypes.c_int) for n in ("M", "D", "group", "post", "pre")] + [
+        ("res", ctypes.c_float), ("eps", ctypes.c_float)] + [
+        (n, lazymar_rows_desc) for n in ("x", "y", "gate", "scale", "shift")] + [
+        (n, _FP) for n in ("post_g", "post_b", "pre_g", "pre_b")] + [
+        (n, lazymar_rows_desc) for n in ("z", "h", "h8", "z8", "y8")] + [
+        (n, _FP) for n in ("y_mean", "y_rstd", "z_mean", "z_rstd")]
+
+
+class lazymar_join_grad_desc(ctypes.Structure):
+    """struct lazymar_join_grad_args; `addr` is its address, `keep` what it points to."""
+    _fields_ = [(n, ctypes.c_int) for n in ("M", "D", "group", "post", "pre")] + [
+        ("res", ctypes.c_float), ("accumulate", ctypes.c_int)] + [
+        (n, lazymar_rows_desc) for n in ("dh", "dz", "z", "y", "gate", "scale")] + [
+        (n, _FP) for n in ("post_g", "post_b", "pre_g", "pre_b", "y_mean", "y_rstd", "z_mean", "z_rstd")] + [
+        (n, lazymar_rows_desc) for n in ("dx", "dy", "dy8", "dgate", "dscale", "dshift")] + [
+        (n, _FP) for n in ("dpost_g", "dpost_b", "dpre_g", "dpre_b", "workspace")] + [
+        ("workspace_bytes", ctypes.c_size_t)]
+
+
+class lazymar_param(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_longlong), ("g", _FP), ("g_dtype", ctypes.c_int), ("out_dtype", ctypes.c_int)] + [
+        (n, _FP) for n in ("out", "p", "m", "v", "ema", "copy")] + [
+        ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float)]
+
+
+class lazymar_adamw_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "ema_decay")] + [
+        ("lr_device", _FP), ("factor", ctypes.c_double), ("steps", ctypes.c_int)]
+
+
 _lib = None
 
 
@@ -146,6 +184,14 @@ def lib():
         "lazymar_block8_linear": (st, [i, vp, vp, vp, vp, i, i, vp, i, vp, vp, i, i, i, vp]),
         "lazymar_block8_wgrad_workspace": (sz, [i, i, i]),
         "lazymar_block8_wgrad": (st, [vp, i, vp, vp, i, i, i, i, i, vp, sz, vp]),
+        "lazymar_join": (st, [vp, vp]),
+        "lazymar_join_grad_workspace": (sz, [i, i, i]),
+        "lazymar_join_grad": (st, [vp, vp]),
+        "lazymar_params_create": (st, [ctypes.POINTER(lazymar_param), i, ctypes.POINTER(vp)]),
+        "lazymar_params_destroy": (None, [vp]),
+        "lazymar_grad_norm": (st, [vp, f, f, vp, vp]),
+        "lazymar_clip_grads": (st, [vp, vp, vp]),
+        "lazymar_adamw": (st, [vp, ctypes.POINTER(lazymar_adamw_desc), vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -506,6 +552,145 @@ def lazymar_block8_wgrad_workspace(M, N, K):
 def lazymar_block8_wgrad(dy, lddy, x, dw, lddw, accumulate, M, N, K, workspace, workspace_bytes, stream=None):
     _check(lib().lazymar_block8_wgrad(_ptr(dy), lddy, _desc(x), _ptr(dw), lddw, int(accumulate), M, N, K,
                                       _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# The residual join
+# ---------------------------------------------------------------------------
+
+def lazymar_rows(t, scale=None, ld=None, lds=None):
+    """Describes rows to lazymar_join_args and lazymar_join_grad_args: an fp32 or bf16 tensor [rows, D] whose columns
+    are consecutive, or with `scale` an 8-bit one (as for lazymar_block8)."""
+    if scale is not None:
+        q = lazymar_block8(t, scale, ld, lds)
+        d = lazymar_rows_desc(q.q, q.scale, LAZYMAR_E4M3, q.ldq, q.lds)
+    else:
+        dtype = {"torch.float32": LAZYMAR_F32, "torch.bfloat16": LAZYMAR_BF16}.get(str(t.dtype))
+        if dtype is None or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise LazymarError(1, "rows: fp32 or bf16 tensors of two axes, consecutive along the last")
+        if ld is None:
+            ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+        d = lazymar_rows_desc(_ptr(t), None, dtype, int(ld), 0)
+    d.keep = (t, scale)
+    return d
+
+
+def _filled(d, fields):
+    """Fields of an argument struct: numbers, lazymar_rows, tensors (their addresses), None (absent). Keeps them alive."""
+    kinds = dict(d._fields_)
+    for n, v in fields.items():
+        if n not in kinds:
+            raise TypeError("no argument %s" % n)
+        if v is None:
+            continue
+        if kinds[n] is _FP:
+            t = str(getattr(v, "dtype", "torch.float32"))
+            if n != "workspace" and (t != "torch.float32" or not getattr(v, "is_contiguous", lambda: True)()):
+                raise LazymarError(1, "%s: consecutive fp32 elements required" % n)
+            v = _ptr(v)
+        elif kinds[n] is lazymar_rows_desc and not isinstance(v, lazymar_rows_desc):
+            v = lazymar_rows(v)
+            fields = dict(fields, **{n: v})
+        setattr(d, n, v)
+    d.keep = fields
+    d.addr = ctypes.addressof(d)
+    return d
+
+
+def lazymar_join_args(M, D, x, y=None, group=0, post=LAZYMAR_NORM_NONE, pre=LAZYMAR_NORM_NONE, res=1.0, eps=1e-6, **more):
+    """The arguments of lazymar_join: rows as lazymar_rows or tensors, parameters and statistics as fp32 tensors. Make
+    it once for buffers that stay, and use it again."""
+    return _filled(lazymar_join_desc(), dict(more, M=M, D=D, x=x, y=y, group=group, post=post, pre=pre, res=res, eps=eps))
+
+
+def lazymar_join(args, stream=None):
+    _check(lib().lazymar_join(args.addr, _stream(stream)))
+
+
+def lazymar_join_grad_workspace(M, D, group):
+    return lib().lazymar_join_grad_workspace(M, D, group)
+
+
+def lazymar_join_grad_args(M, D, group=0, post=LAZYMAR_NORM_NONE, pre=LAZYMAR_NORM_NONE, res=1.0, accumulate=False,
+                           workspace=None, workspace_bytes=None, **more):
+    """The arguments of lazymar_join_grad, as for lazymar_join_args."""
+    if workspace is not None and workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
+    return _filled(lazymar_join_grad_desc(), dict(more, M=M, D=D, group=group, post=post, pre=pre, res=res,
+                                                  accumulate=int(accumulate), workspace=workspace,
+                                                  workspace_bytes=workspace_bytes))
+
+
+def lazymar_join_grad(args, stream=None):
+    _check(lib().lazymar_join_grad(args.addr, _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# The end of a training step
+# ---------------------------------------------------------------------------
+
+def lazymar_params_create(entries):
+    """A list of tensors: dicts with g and, as far as they are used, out, p, m, v, ema, copy (tensors of as many
+    consecutive elements), lr_scale and weight_decay. Returns a ParamsHandle, which keeps the tensors alive."""
+    entries = [dict(e) for e in entries]
+    list_ = (lazymar_param * max(1, len(entries)))()
+    dtypes = {"torch.float32": LAZYMAR_F32, "torch.bfloat16": LAZYMAR_BF16}
+    for d, e in zip(list_, entries):
+        d.n = e["g"].numel()
+        for k in ("g", "out", "p", "m", "v", "ema", "copy"):
+            t = e.get(k)
+            if t is None:
+                continue
+            dtype = dtypes.get(str(t.dtype))
+            if t.numel() != d.n or not t.is_contiguous():
+                raise LazymarError(1, "%s: %d consecutive elements required" % (k, d.n))
+            if dtype is None or (k in ("p", "m", "v", "ema") and dtype != LAZYMAR_F32) or (k == "copy" and dtype != LAZYMAR_BF16):
+                raise LazymarError(1, "%s: g and out fp32 or bf16, copy bf16, the others fp32" % k)
+            setattr(d, k, _ptr(t) or None)
+            if k in ("g", "out"):
+                setattr(d, k + "_dtype", dtype)
+        d.lr_scale, d.weight_decay = float(e.get("lr_scale", 1.0)), float(e.get("weight_decay", 0.0))
+    h = ctypes.c_void_p()
+    _check(lib().lazymar_params_create(list_, len(entries), ctypes.byref(h)))
+    return ParamsHandle(h.value, entries)
+
+
+def lazymar_params_destroy(h):
+    h.close()
+
+
+def lazymar_grad_norm(h, state, max_norm, scale=1.0, stream=None):
+    """state: 16 bytes on the device (norm and factor fp32, steps and skipped int32), zeros before the first step."""
+    _check(lib().lazymar_grad_norm(h.ptr, scale, max_norm, _ptr(state), _stream(stream)))
+
+
+def lazymar_clip_grads(h, state, stream=None):
+    _check(lib().lazymar_clip_grads(h.ptr, _ptr(state), _stream(stream)))
+
+
+def lazymar_adamw(h, state, lr, beta1=0.9, beta2=0.999, eps=1e-8, ema_decay=0.0, lr_device=None, factor=1.0, steps=0,
+                  stream=None):
+    a = lazymar_adamw_desc(lr, beta1, beta2, eps, ema_decay, _ptr(lr_device), factor, steps)
+    _check(lib().lazymar_adamw(h.ptr, ctypes.byref(a), _ptr(state), _stream(stream)))
+
+
+class ParamsHandle:
+    """Owns a lazymar_params; destroyed with the object or by close()."""
+
+    def __init__(self, ptr, keep):
+        self.ptr = ptr
+        self.keep = keep
+
+    def close(self):
+        if self.ptr:
+            lib().lazymar_params_destroy(self.ptr)
+            self.ptr = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class HeadHandle:
