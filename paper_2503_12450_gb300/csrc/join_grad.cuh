@@ -1,0 +1,449 @@
+// The gradient of the residual join (lazymar_join_grad).
+//
+// A row is worked on by WPR warps (a team), NC chunks of 256 columns a warp. The teams of
+// the launch divide the rows into consecutive ranges, so that a group's rows (those with one
+// row of modulation) meet in one team or a few neighbouring ones. A lane keeps four sums
+// of each of its columns while the group lasts,
+//   A = sum dh, B = sum dh n, P = sum Z, Q = sum Z u,
+// from which all gradients of modulation and parameters follow. A group that lies in
+// one team's range is finished there; the others leave their sums in the workspace, two
+// places a team (the group that its range begins in, and the one that it ends in), and
+// a second kernel adds them in the teams' order. ROWWISE (every row has its own
+// modulation): the modulation's gradients are written with the row, and the four
+// sums, weighted, are those of the parameters.
+// The rows come by bulk copies into a ring in shared memory (join_rows.cuh).
+#pragma once
+
+#include "join_rows.cuh"
+
+namespace lm {
+
+enum { SUM_A = 0, SUM_B = 1, SUM_P = 2, SUM_Q = 3 };
+
+// What a launch computes besides dx and dy: the sums (bits 1 << SUM_*) that modulation and parameters need.
+struct JoinSums {
+  unsigned mods, params;
+};
+
+template <int WPR>
+constexpr int kGradWarps = WPR == 5 ? 5 : WPR > 8 ? 16 : 8;
+template <int WPR>
+constexpr int kGradCtas = WPR > 8 ? 1 : WPR == 5 ? 3 : 2;
+
+namespace {
+
+// Sums of a and b over the warp, both in every lane: the halves of the warp take one each after the first exchange.
+__device__ __forceinline__ float2 warp_sum2(float a, float b) {
+  const bool upper = threadIdx.x & 16;
+  float x = upper ? b : a;
+  x += __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  const float y = __shfl_xor_sync(0xffffffffu, x, 16);
+  return upper ? make_float2(y, x) : make_float2(x, y);
+}
+// The same over the row's warps (`red`: one place for each).
+template <int WPR>
+__device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int grp, int part) {
+  float2 s = warp_sum2(a, b);
+  if constexpr (WPR > 1) {
+    if ((threadIdx.x & 31) == 0) red[part] = s;
+    row_barrier<WPR>(grp);
+    s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < WPR; ++i) {
+      s.x += red[i].x;
+      s.y += red[i].y;
+    }
+  }
+  return s;
+}
+
+template <int NC, int WPR, bool WHOLE, bool ROWWISE>
+__global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
+    join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, int teams, JoinSums need,
+                     unsigned* err) {
+  constexpr int WARPS = kGradWarps<WPR>, GROUPS = WARPS / WPR;
+  extern __shared__ __align__(128) uint8_t ring_smem[];
+  __shared__ uint64_t bars[WARPS][kMostStages];
+  __shared__ float2 red[2][2][GROUPS][WPR];
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
+  const int D = p.D, c0 = part * NC * kChunk, team = (int)blockIdx.x * GROUPS + grp;
+  if (threadIdx.x == 0) abort_word = 0;
+  RowRing<WHOLE> ring;
+  ring.init(ring_smem + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(NC * kChunk, D - c0));
+  pdl_wait();
+  pdl_trigger();
+  __syncthreads();
+  if (team >= teams) return;
+  const long long first = team_start(p.M, teams, team), end = team_start(p.M, teams, team + 1);
+  for (int s = 0; s < plan.depth; ++s)
+    if (first + s < end) ring.fetch(plan, first + s, s, p.M);
+  const bool pre = p.pre != LAZYMAR_NORM_NONE, post = p.post != LAZYMAR_NORM_NONE;
+  const bool pre_layer = p.pre == LAZYMAR_NORM_LAYER, post_layer = p.post == LAZYMAR_NORM_LAYER;
+  const unsigned sums_of = need.mods | need.params;
+  const bool ab = ROWWISE ? need.params & 3u : sums_of & 3u, pq = ROWWISE ? need.params >> 2 : sums_of >> 2;
+
+  // statistics and 8-bit scales (lanes: the warp's blocks, of z and then of y) of the next row
+  float next_ym = 0.f, next_yr = 1.f, next_zm = 0.f, next_zr = 1.f;
+  uint32_t next_s = 0;
+  auto statistics = [&](long long row) {
+    if (row >= end) return;
+    if (pre) {
+      if (pre_layer) next_zm = p.z_mean[row];
+      next_zr = p.z_rstd[row];
+    }
+    if (post) {
+      if (post_layer) next_ym = p.y_mean[row];
+      next_yr = p.y_rstd[row];
+    }
+    const int b = lane & (2 * NC - 1);
+    if (lane < 4 * NC && c0 + kBlk * b < D) {
+      const Rows& m = lane < 2 * NC ? p.z : p.y;
+      if (m.p && m.dtype == LAZYMAR_E4M3) next_s = m.scale[(size_t)(c0 / kBlk + b) * m.lds + row];
+    }
+  };
+  statistics(first);
+
+  float sums[4][NC][8], gate[NC][8], scale[NC][8];  // scale: 1 + scale
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sums[0][c][i] = sums[1][c][i] = sums[2][c][i] = sums[3][c][i] = 0.f;
+      gate[c][i] = scale[c][i] = 1.f;
+    }
+  bool dead = false;  // a wait ran out: nothing is written any more
+  // out (+)= v for a row of a modulation's gradient
+  auto put = [&](const MatOut& o, size_t r, int cc, float (&v)[8]) {
+    if (p.accumulate) {
+      float t[8];
+      load_row<WHOLE>(Rows{o.p, nullptr, o.ld, 0, o.dtype, o.vec}, r, cc, D, t);
+      add8(v, t);
+    }
+    if (!dead) store_row<WHOLE>(o, r, cc, D, v);
+  };
+  auto put_sum = [&](float* o, int cc, const float (&v)[8]) {
+    if (!dead) store_row<WHOLE>(MatOut{o, 0, LAZYMAR_F32, true}, 0, cc, D, v);
+  };
+  float* const slots = p.ws + (size_t)team * 8 * D;
+  float* const param = p.ws + (ROWWISE ? 0 : (size_t)teams * 8 * D) + (size_t)team * 4 * D;
+
+  // The end of a group, or of its part in this range: rows start .. stop.
+  auto flush = [&](long long start, long long stop) {
+    const long long q = p.group > 0 ? start / p.group : 0;
+    const long long g0 = p.group > 0 ? q * p.group : 0;
+    const long long g1 = p.group > 0 ? min(g0 + p.group, (long long)p.M) : p.M;
+    const bool whole = start == g0 && stop == g1;
+    float* slot = slots + (size_t)(start > first) * 4 * D;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int cc = c0 + c * kChunk;
+      float v[8], t[8];
+      // the parameters' sums go on in the workspace, group by group
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (!(need.params >> k & 1u)) continue;
+        copy8(v, sums[k][c]);
+        mul8(v, k < 2 ? scale[c] : gate[c]);
+        if (start > first) {
+          load_param<WHOLE>(param + (size_t)k * D, cc, D, t);
+          add8(v, t);
+        }
+        put_sum(param + (size_t)k * D, cc, v);
+      }
+      if (whole) {
+        if (p.dshift.p) {
+          copy8(v, sums[SUM_A][c]);
+          put(p.dshift, q, cc, v);
+        }
+        if (p.dscale.p) {
+          copy8(v, sums[SUM_B][c]);
+          if (p.pre_g) {
+            load_param<WHOLE>(p.pre_g, cc, D, t);
+            mul8(v, t);
+          }
+          if (p.pre_b) {
+            load_param<WHOLE>(p.pre_b, cc, D, t);
+            acc8(v, t, sums[SUM_A][c]);
+          }
+          put(p.dscale, q, cc, v);
+        }
+        if (p.dgate.p) {
+          copy8(v, sums[SUM_Q][c]);
+          if (p.post_g) {
+            load_param<WHOLE>(p.post_g, cc, D, t);
+            mul8(v, t);
+          }
+          if (p.post_b) {
+            load_param<WHOLE>(p.post_b, cc, D, t);
+            acc8(v, t, sums[SUM_P][c]);
+          }
+          put(p.dgate, q, cc, v);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (need.mods >> k & 1u) put_sum(slot + (size_t)k * D, cc, sums[k][c]);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sums[k][c][i] = 0.f;
+    }
+  };
+
+  int it = 0;
+  long long start = first, stop = first;  // of the group's part
+  for (long long row = first; row < end; ++row, it ^= 1) {
+    if (!ROWWISE && row == stop) {
+      if (row > first) flush(start, stop);
+      start = row;
+      stop = p.group > 0 ? min(end, (row / p.group + 1) * p.group) : end;
+      const size_t r = p.group > 0 ? (size_t)(row / p.group) : 0;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        if (p.gate.p) load_row<WHOLE>(p.gate, r, c0 + c * kChunk, D, gate[c]);
+        if (p.scale.p) {
+          load_row<WHOLE>(p.scale, r, c0 + c * kChunk, D, scale[c]);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) scale[c][i] += 1.f;
+        }
+      }
+    }
+    const float ym = next_ym, yr = next_yr, zm = next_zm, zr = next_zr;
+    const uint32_t sb = next_s;
+    statistics(row + 1);
+    const bool ok = dead || ring.wait(abort_flag, err);
+    dead |= !__all_sync(0xffffffffu, ok);
+    const uint8_t* st = ring.row();
+    float d[NC][8], n[NC][8], Z[NC][8], u[NC][8];
+    {
+      int i = 0;
+      const auto from = [&](const Rows& m, int scales, float (&to)[NC][8]) {
+        const RowStream& t = plan.t[i++];
+        const uint32_t sh = RowRing<WHOLE>::shift(t, (size_t)row, c0);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          uint32_t s0 = 0, s1 = 0;
+          if (m.dtype == LAZYMAR_E4M3) {
+            s0 = __shfl_sync(0xffffffffu, sb, scales + 2 * c);
+            s1 = __shfl_sync(0xffffffffu, sb, scales + 2 * c + 1);
+          }
+          load_stage<WHOLE>(st + t.at + (size_t)c * kChunk * t.e, m.dtype, sh, s0, s1, to[c]);
+          mask_columns<WHOLE>(to[c], c0 + c * kChunk, D);
+        }
+      };
+      const auto none = [&](float (&to)[NC][8]) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) to[c][k] = 0.f;
+      };
+      if (pre) {
+        from(p.dh, 0, d);
+        from(p.z, 0, n);
+      }
+      if (p.dz.p) from(p.dz, 0, Z);
+      else none(Z);
+      if (p.y.p) from(p.y, 2 * NC, u);
+      else none(u);
+      if (ROWWISE) {
+        if (p.gate.p) from(p.gate, 0, gate);
+        if (p.scale.p) {
+          from(p.scale, 0, scale);
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) scale[c][k] += 1.f;
+        }
+      }
+    }
+    ring.next(plan, row + plan.depth, end, p.M, dead);
+    if (pre) {
+      float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int cc = c0 + c * kChunk;
+        float t[8];
+        sub8(n[c], zm);
+        scale8(n[c], zr, n[c]);
+        mask_columns<WHOLE>(n[c], cc, D);
+        if (ROWWISE) {
+          if (p.dscale.p) {
+            float v[8];
+            copy8(v, n[c]);
+            if (p.pre_g) {
+              load_param<WHOLE>(p.pre_g, cc, D, t);
+              mul8(v, t);
+            }
+            if (p.pre_b) {
+              load_param<WHOLE>(p.pre_b, cc, D, t);
+              add8(v, t);
+            }
+            mul8(v, d[c]);
+            put(p.dscale, row, cc, v);
+          }
+          if (p.dshift.p) {
+            copy8(t, d[c]);
+            put(p.dshift, row, cc, t);
+          }
+          mul8(d[c], scale[c]);
+        }
+        if (ab) {
+          add8(sums[SUM_A][c], d[c]);
+          acc8(sums[SUM_B][c], d[c], n[c]);
+        }
+        if (!ROWWISE) mul8(d[c], scale[c]);
+        if (p.pre_g) {
+          load_param<WHOLE>(p.pre_g, cc, D, t);
+          mul8(d[c], t);
+        }
+        s1 += sum8(d[c]);
+        s2 += dot8(d[c], n[c]);
+      }
+      const float2 s = row_sum2<WPR>(s1, s2, red[it][0][grp], grp, part);
+      s1 = pre_layer ? s.x / (float)D : 0.f;
+      s2 = -s.y / (float)D;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const float m2[8] = {s2, s2, s2, s2, s2, s2, s2, s2}, r[8] = {zr, zr, zr, zr, zr, zr, zr, zr};
+        sub8(d[c], s1);
+        acc8(d[c], n[c], m2);
+        acc8(Z[c], d[c], r);
+        mask_columns<WHOLE>(Z[c], c0 + c * kChunk, D);
+      }
+    }
+    float s3 = 0.f, s4 = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int cc = c0 + c * kChunk;
+      float t[8];
+      if (p.dx.p && !dead) {
+        scale8(Z[c], p.res, t);
+        store_row<WHOLE>(p.dx, row, cc, D, t);
+      }
+      if (post) {
+        sub8(u[c], ym);
+        scale8(u[c], yr, u[c]);
+        mask_columns<WHOLE>(u[c], cc, D);
+      }
+      if (ROWWISE) {
+        if (p.dgate.p) {
+          float v[8];
+          copy8(v, u[c]);
+          if (p.post_g) {
+            load_param<WHOLE>(p.post_g, cc, D, t);
+            mul8(v, t);
+          }
+          if (p.post_b) {
+            load_param<WHOLE>(p.post_b, cc, D, t);
+            add8(v, t);
+          }
+          mul8(v, Z[c]);
+          put(p.dgate, row, cc, v);
+        }
+        mul8(Z[c], gate[c]);
+      }
+      if (pq) {
+        add8(sums[SUM_P][c], Z[c]);
+        acc8(sums[SUM_Q][c], Z[c], u[c]);
+      }
+      if (!ROWWISE) mul8(Z[c], gate[c]);
+      if (p.post_g) {
+        load_param<WHOLE>(p.post_g, cc, D, t);
+        mul8(Z[c], t);
+      }
+      if (post) {
+        s3 += sum8(Z[c]);
+        s4 += dot8(Z[c], u[c]);
+      }
+    }
+    if (!p.dy.p && !p.dy8.q) continue;
+    if (post) {
+      const float2 s = row_sum2<WPR>(s3, s4, red[it][1][grp], grp, part);
+      s3 = post_layer ? s.x / (float)D : 0.f;
+      s4 = -s.y / (float)D;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const float m2[8] = {s4, s4, s4, s4, s4, s4, s4, s4};
+        sub8(Z[c], s3);
+        acc8(Z[c], u[c], m2);
+        scale8(Z[c], yr, Z[c]);
+        mask_columns<WHOLE>(Z[c], c0 + c * kChunk, D);
+      }
+    }
+    if (dead) continue;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int cc = c0 + c * kChunk;
+      if (p.dy.p) store_row<WHOLE>(p.dy, row, cc, D, Z[c]);
+      if (p.dy8.q) store_row8<WHOLE>(p.dy8, row, cc, D, Z[c]);
+    }
+  }
+  if (!ROWWISE) {
+    flush(start, stop);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (need.params >> k & 1u)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) put_sum(param + (size_t)k * D, c0 + c * kChunk, sums[k][c]);
+  }
+}
+
+// A launch for rows with a modulation of their own, or shared by groups.
+template <int NC, int WPR, bool ROWWISE>
+cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int teams) {
+  constexpr int WARPS = kGradWarps<WPR>, GROUPS = WARPS / WPR;
+  RingPlan plan{};
+  const auto add = [&](const Rows& r) {
+    if (!r.p) return;
+    const uint32_t e = r.dtype == LAZYMAR_F32 ? 4 : r.dtype == LAZYMAR_BF16 ? 2 : 1;
+    plan.t[plan.n++] = RowStream{static_cast<const uint8_t*>(r.p), (size_t)r.ld * e, plan.stage, e};
+    plan.stage += NC * kChunk * e + 32;
+  };
+  if (p.pre != LAZYMAR_NORM_NONE) {
+    add(p.dh);
+    add(p.z);
+  }
+  add(p.dz);
+  add(p.y);
+  if (ROWWISE) {
+    add(p.gate);
+    add(p.scale);
+  }
+  constexpr int kRoom = 210 * 1024 / kGradCtas<WPR>;
+  plan.depth = kRoom / (WARPS * (int)plan.stage);
+  if (plan.depth > 4) plan.depth = 4;
+  const auto run = [&](auto kernel) {
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kernel, dim3((unsigned)((teams + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
+                      (size_t)WARPS * plan.depth * plan.stage, c.stream, p, plan, teams, need, c.err);
+  };
+  return whole ? run(join_grad_kernel<NC, WPR, true, ROWWISE>) : run(join_grad_kernel<NC, WPR, false, ROWWISE>);
+}
+
+template <bool ROWWISE>
+cudaError_t join_grad_launch(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, int teams) {
+  switch (wpr) {
+    case 1: return join_grad_run<1, 1, ROWWISE>(c, p, need, whole, teams);
+    case 2: return join_grad_run<1, 2, ROWWISE>(c, p, need, whole, teams);
+    case 4: return join_grad_run<1, 4, ROWWISE>(c, p, need, whole, teams);
+    case 5: return join_grad_run<1, 5, ROWWISE>(c, p, need, whole, teams);
+    case 8: return join_grad_run<1, 8, ROWWISE>(c, p, need, whole, teams);
+    default:
+      return p.D <= 16 * kChunk ? join_grad_run<1, 16, ROWWISE>(c, p, need, whole, teams)
+                                : join_grad_run<2, 16, ROWWISE>(c, p, need, whole, teams);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_join_grad_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, int teams);
+
+}  // namespace lm

@@ -1,0 +1,10 @@
+// The residual join's gradient where every row has a modulation of its own.
+#include "join_grad.cuh"
+
+namespace lm {
+
+cudaError_t launch_join_grad_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, int teams) {
+  return join_grad_launch<true>(c, p, need, whole, wpr, teams);
+}
+
+}  // namespace lm

@@ -129,6 +129,33 @@ def test_join_types_and_strides(M, D, group, x, y, z, h, mod, pad, offset):
     close(ht, o["h"], rounded(b["h"], o["h"], h))  # from z before its own rounding
 
 
+@pytest.mark.parametrize("x,y,z,h,mod,pad,offset", [
+    ("fp32", "bf16", "fp32", "bf16", "bf16", 0, 0), ("bf16", "bf16", "bf16", "bf16", "fp32", 8, 0),
+    ("fp32", "e4m3", "bf16", "fp32", "bf16", 0, 0), ("bf16", "bf16", "bf16", "bf16", "bf16", 1, 3),
+    ("fp32", "fp32", "fp32", "fp32", "fp32", 3, 1), ("bf16", "e4m3", "fp32", "bf16", "fp32", 5, 0)])
+@pytest.mark.parametrize("M,D,group", [(1300, 1024, 320), (2000, 256, 0), (1999, 130, 1), (2500, 512, 2), (1500, 1280, 11),
+                                       (700, 4096, 100), (900, 2048, 1), (5000, 104, 3), (1200, 777, 7), (400, 5001, 9),
+                                       (1000, 1281, 1)])
+def test_join_many_rows(M, D, group, x, y, z, h, mod, pad, offset):
+    """More rows than teams: several rows in a row, groups inside a team's range and across them, rows on and off
+    the boundary, among them the tensor's first and last, whose neighbours are NaN here."""
+    t, v = make(M, D, group, x, y, mod, pad, offset, seed=30, eight=y == "e4m3")
+    zt, ht, h8, st = out(M, D, z, pad, offset), out(M, D, h, pad, offset), Held(M, D, more=16), stats(M)
+    lm.lazymar_join(lm.lazymar_join_args(M, D, group=group, post=NORM["layer"], pre=NORM["rms"], res=0.75, eps=EPS, z=zt, h=ht,
+                                         h8=lm.lazymar_rows(h8.q, h8.scale), **t, **st))
+    sync()
+    o = T.join(post="layer", pre="rms", group=group, res=0.75, eps=EPS, **v)
+    b = join_bounds(v, o, "layer", "rms", group, 0.75)
+    close(zt, o["z"], rounded(b["z"], o["z"], z))
+    close(ht, o["h"], rounded(b["h"], o["h"], h))
+    close8(h8, o["h"], b["h"])
+    for k in st:
+        close(st[k], o[k], b[k])
+    if pad:  # what lies between the rows stays
+        for a in (zt, ht):
+            assert torch_cuda().isnan(a.as_strided((M - 1, pad), (D + pad, 1), a.storage_offset() + D)).all()
+
+
 @pytest.mark.parametrize("fields", [("gate",), ("scale",), ("post_g",), ("post_b",), ("pre_g",), ("pre_b",), ("shift",), ()])
 def test_join_with_some_of_its_parts(fields):
     M, D, group = 11, 777, 3
@@ -161,11 +188,11 @@ def test_join_without_a_branch_or_without_a_norm(D):
     close(z, o["z"], join_bounds(v, o, "layer", "none", 2, 1.0)["z"])
 
 
+@pytest.mark.parametrize("M", [70, 2000])
 @pytest.mark.parametrize("D,pad,offset", [(1024, 0, 0), (777, 2, 1), (4099, 0, 0)])
-def test_join_in_place(D, pad, offset):
+def test_join_in_place(D, pad, offset, M):
     """z over x, h over y, with their types and strides; the rows around them stay."""
     torch = torch_cuda()
-    M = 70
     t, v = make(M, D, 7, "fp32", "bf16", pad=pad, offset=offset, seed=6)
     z, h = out(M, D), out(M, D, "bf16")
     kw = dict(group=7, post=NORM["layer"], pre=NORM["rms"], eps=EPS)
@@ -177,23 +204,23 @@ def test_join_in_place(D, pad, offset):
         assert torch.isnan(t["x"].as_strided((M, pad), (D + pad, 1), t["x"].storage_offset() + D)).all()
 
 
+@pytest.mark.parametrize("M,D", [(12, 1000), (1200, 1000), (1200, 999)])
 @pytest.mark.parametrize("post,pre", [("layer", "layer"), ("rms", "rms")])
-def test_join_rows_that_are_not_finite_stay_alone(post, pre):
+def test_join_rows_that_are_not_finite_stay_alone(post, pre, M, D):
     torch = torch_cuda()
-    M, D = 12, 1000
     t, v = make(M, D, 0, seed=7)
     z, h, h8 = out(M, D), out(M, D), Held(M, D)
     kw = dict(post=NORM[post], pre=NORM[pre], eps=EPS, z=z, h=h, h8=lm.lazymar_rows(h8.q, h8.scale))
     lm.lazymar_join(lm.lazymar_join_args(M, D, **t, **kw))
     sync()
     want_z, want_h, want_q = z.clone(), h.clone(), h8.q.clone()
-    t["x"][2, 5], t["y"][4, 999], t["x"][6, 0], t["y"][8] = float("nan"), float("inf"), -float("inf"), 0.0
+    t["x"][2, 5], t["y"][4, D - 1], t["x"][6, 0], t["y"][8] = float("nan"), float("inf"), -float("inf"), 0.0
     lm.lazymar_join(lm.lazymar_join_args(M, D, **t, **kw))
     sync()
     for i in (2, 4, 6):
         assert torch.isnan(h[i]).all() or not torch.isfinite(h[i]).all()
     assert torch.isnan(h[2]).all() and torch.isfinite(h[8]).all()
-    same = [0, 1, 3, 5, 7, 9, 10, 11]
+    same = [i for i in range(M) if i not in (2, 4, 6, 8)]
     assert torch.equal(z[same], want_z[same]) and torch.equal(h[same], want_h[same]) and torch.equal(h8.q[same], want_q[same])
 
 
