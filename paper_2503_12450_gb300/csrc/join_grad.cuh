@@ -61,7 +61,7 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int gr
 
 template <int NC, int WPR, bool WHOLE, bool ROWWISE>
 __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
-    join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, int teams, JoinSums need,
+    join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, const Teams teams, JoinSums need,
                      unsigned* err) {
   constexpr int WARPS = kGradWarps<WPR>, GROUPS = WARPS / WPR;
   extern __shared__ __align__(128) uint8_t ring_smem[];
@@ -77,10 +77,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
   pdl_wait();
   pdl_trigger();
   __syncthreads();
-  if (team >= teams) return;
-  const long long first = team_start(p.M, teams, team), end = team_start(p.M, teams, team + 1);
+  if (team >= teams.n) return;
+  const int first = team_start(teams, team), end = team_start(teams, team + 1);
   for (int s = 0; s < plan.depth; ++s)
-    if (first + s < end) ring.fetch(plan, first + s, s, p.M);
+    if (first + s < end) ring.fetch(plan, first + s, s, c0, p.M);
+  const float per_D = 1.f / (float)D;
   const bool pre = p.pre != LAZYMAR_NORM_NONE, post = p.post != LAZYMAR_NORM_NONE;
   const bool pre_layer = p.pre == LAZYMAR_NORM_LAYER, post_layer = p.post == LAZYMAR_NORM_LAYER;
   const unsigned sums_of = need.mods | need.params;
@@ -89,7 +90,13 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
   // statistics and 8-bit scales (lanes: the warp's blocks, of z and then of y) of the next row
   float next_ym = 0.f, next_yr = 1.f, next_zm = 0.f, next_zr = 1.f;
   uint32_t next_s = 0;
-  auto statistics = [&](long long row) {
+  const uint8_t* scales = nullptr;
+  if (lane < 4 * NC) {
+    const Rows& m = lane < 2 * NC ? p.z : p.y;
+    const int blk = c0 / kBlk + (lane & (2 * NC - 1));
+    if (m.p && m.dtype == LAZYMAR_E4M3 && blk * kBlk < D) scales = m.scale + (size_t)blk * m.lds;
+  }
+  auto statistics = [&](int row) {
     if (row >= end) return;
     if (pre) {
       if (pre_layer) next_zm = p.z_mean[row];
@@ -99,11 +106,7 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
       if (post_layer) next_ym = p.y_mean[row];
       next_yr = p.y_rstd[row];
     }
-    const int b = lane & (2 * NC - 1);
-    if (lane < 4 * NC && c0 + kBlk * b < D) {
-      const Rows& m = lane < 2 * NC ? p.z : p.y;
-      if (m.p && m.dtype == LAZYMAR_E4M3) next_s = m.scale[(size_t)(c0 / kBlk + b) * m.lds + row];
-    }
+    if (scales) next_s = scales[row];
   };
   statistics(first);
 
@@ -117,30 +120,30 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
     }
   bool dead = false;  // a wait ran out: nothing is written any more
   // out (+)= v for a row of a modulation's gradient
-  auto put = [&](const MatOut& o, size_t r, int cc, float (&v)[8]) {
+  auto put = [&](const MatOut& o, unsigned r, const Columns<WHOLE>& cc, float (&v)[8]) {
     if (p.accumulate) {
       float t[8];
-      load_row<WHOLE>(Rows{o.p, nullptr, o.ld, 0, o.dtype, o.vec}, r, cc, D, t);
+      load_row<WHOLE>(o.p, o.ld, o.dtype, r, cc, t);
       add8(v, t);
     }
-    if (!dead) store_row<WHOLE>(o, r, cc, D, v);
+    if (!dead) store_row<WHOLE>(o, r, cc, v);
   };
-  auto put_sum = [&](float* o, int cc, const float (&v)[8]) {
-    if (!dead) store_row<WHOLE>(MatOut{o, 0, LAZYMAR_F32, true}, 0, cc, D, v);
+  auto put_sum = [&](float* o, const Columns<WHOLE>& cc, const float (&v)[8]) {
+    if (!dead) store_row<WHOLE>(MatOut{o, 0, LAZYMAR_F32, true}, 0u, cc, v);
   };
   float* const slots = p.ws + (size_t)team * 8 * D;
-  float* const param = p.ws + (ROWWISE ? 0 : (size_t)teams * 8 * D) + (size_t)team * 4 * D;
+  float* const param = p.ws + (ROWWISE ? 0 : (size_t)teams.n * 8 * D) + (size_t)team * 4 * D;
 
   // The end of a group, or of its part in this range: rows start .. stop.
-  auto flush = [&](long long start, long long stop) {
-    const long long q = p.group > 0 ? start / p.group : 0;
-    const long long g0 = p.group > 0 ? q * p.group : 0;
-    const long long g1 = p.group > 0 ? min(g0 + p.group, (long long)p.M) : p.M;
+  auto flush = [&](int start, int stop) {
+    const int q = p.group > 0 ? start / p.group : 0;
+    const int g0 = p.group > 0 ? q * p.group : 0;
+    const int g1 = p.group > 0 ? g0 + min(p.group, p.M - g0) : p.M;
     const bool whole = start == g0 && stop == g1;
     float* slot = slots + (size_t)(start > first) * 4 * D;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int cc = c0 + c * kChunk;
+      const Columns<WHOLE> cc(c0 + c * kChunk, D);
       float v[8], t[8];
       // the parameters' sums go on in the workspace, group by group
 #pragma unroll
@@ -149,7 +152,7 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         copy8(v, sums[k][c]);
         mul8(v, k < 2 ? scale[c] : gate[c]);
         if (start > first) {
-          load_param<WHOLE>(param + (size_t)k * D, cc, D, t);
+          load_param<WHOLE>(param + (size_t)k * D, cc, t);
           add8(v, t);
         }
         put_sum(param + (size_t)k * D, cc, v);
@@ -162,11 +165,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         if (p.dscale.p) {
           copy8(v, sums[SUM_B][c]);
           if (p.pre_g) {
-            load_param<WHOLE>(p.pre_g, cc, D, t);
+            load_param<WHOLE>(p.pre_g, cc, t);
             mul8(v, t);
           }
           if (p.pre_b) {
-            load_param<WHOLE>(p.pre_b, cc, D, t);
+            load_param<WHOLE>(p.pre_b, cc, t);
             acc8(v, t, sums[SUM_A][c]);
           }
           put(p.dscale, q, cc, v);
@@ -174,11 +177,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         if (p.dgate.p) {
           copy8(v, sums[SUM_Q][c]);
           if (p.post_g) {
-            load_param<WHOLE>(p.post_g, cc, D, t);
+            load_param<WHOLE>(p.post_g, cc, t);
             mul8(v, t);
           }
           if (p.post_b) {
-            load_param<WHOLE>(p.post_b, cc, D, t);
+            load_param<WHOLE>(p.post_b, cc, t);
             acc8(v, t, sums[SUM_P][c]);
           }
           put(p.dgate, q, cc, v);
@@ -196,18 +199,19 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
   };
 
   int it = 0;
-  long long start = first, stop = first;  // of the group's part
-  for (long long row = first; row < end; ++row, it ^= 1) {
+  int start = first, stop = first;  // of the group's part
+  for (int row = first; row < end; ++row, it ^= 1) {
     if (!ROWWISE && row == stop) {
       if (row > first) flush(start, stop);
       start = row;
-      stop = p.group > 0 ? min(end, (row / p.group + 1) * p.group) : end;
-      const size_t r = p.group > 0 ? (size_t)(row / p.group) : 0;
+      const int r = p.group > 0 ? row / p.group : 0;
+      stop = p.group > 0 ? min(end - r * p.group, p.group) + r * p.group : end;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        if (p.gate.p) load_row<WHOLE>(p.gate, r, c0 + c * kChunk, D, gate[c]);
+        const Columns<WHOLE> cc(c0 + c * kChunk, D);
+        if (p.gate.p) load_row<WHOLE>(p.gate, r, cc, gate[c]);
         if (p.scale.p) {
-          load_row<WHOLE>(p.scale, r, c0 + c * kChunk, D, scale[c]);
+          load_row<WHOLE>(p.scale, r, cc, scale[c]);
 #pragma unroll
           for (int i = 0; i < 8; ++i) scale[c][i] += 1.f;
         }
@@ -218,23 +222,21 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
     statistics(row + 1);
     const bool ok = dead || ring.wait(abort_flag, err);
     dead |= !__all_sync(0xffffffffu, ok);
-    const uint8_t* st = ring.row();
     float d[NC][8], n[NC][8], Z[NC][8], u[NC][8];
     {
       int i = 0;
-      const auto from = [&](const Rows& m, int scales, float (&to)[NC][8]) {
-        const RowStream& t = plan.t[i++];
-        const uint32_t sh = RowRing<WHOLE>::shift(t, (size_t)row, c0);
+      const auto from = [&](const Rows& m, int first_scale, float (&to)[NC][8]) {
+        const uint8_t* st = ring.piece(plan, i, row, c0);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           uint32_t s0 = 0, s1 = 0;
           if (m.dtype == LAZYMAR_E4M3) {
-            s0 = __shfl_sync(0xffffffffu, sb, scales + 2 * c);
-            s1 = __shfl_sync(0xffffffffu, sb, scales + 2 * c + 1);
+            s0 = __shfl_sync(0xffffffffu, sb, first_scale + 2 * c);
+            s1 = __shfl_sync(0xffffffffu, sb, first_scale + 2 * c + 1);
           }
-          load_stage<WHOLE>(st + t.at + (size_t)c * kChunk * t.e, m.dtype, sh, s0, s1, to[c]);
-          mask_columns<WHOLE>(to[c], c0 + c * kChunk, D);
+          load_stage<WHOLE>(st + (uint32_t)c * kChunk * plan.t[i].e, m.dtype, s0, s1, Columns<WHOLE>(c0 + c * kChunk, D), to[c]);
         }
+        ++i;
       };
       const auto none = [&](float (&to)[NC][8]) {
 #pragma unroll
@@ -261,26 +263,26 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         }
       }
     }
-    ring.next(plan, row + plan.depth, end, p.M, dead);
+    ring.next(plan, row + plan.depth, end, c0, p.M, dead);
     if (pre) {
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const int cc = c0 + c * kChunk;
+        const Columns<WHOLE> cc(c0 + c * kChunk, D);
         float t[8];
         sub8(n[c], zm);
         scale8(n[c], zr, n[c]);
-        mask_columns<WHOLE>(n[c], cc, D);
+        cc.mask(n[c]);
         if (ROWWISE) {
           if (p.dscale.p) {
             float v[8];
             copy8(v, n[c]);
             if (p.pre_g) {
-              load_param<WHOLE>(p.pre_g, cc, D, t);
+              load_param<WHOLE>(p.pre_g, cc, t);
               mul8(v, t);
             }
             if (p.pre_b) {
-              load_param<WHOLE>(p.pre_b, cc, D, t);
+              load_param<WHOLE>(p.pre_b, cc, t);
               add8(v, t);
             }
             mul8(v, d[c]);
@@ -298,48 +300,48 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         }
         if (!ROWWISE) mul8(d[c], scale[c]);
         if (p.pre_g) {
-          load_param<WHOLE>(p.pre_g, cc, D, t);
+          load_param<WHOLE>(p.pre_g, cc, t);
           mul8(d[c], t);
         }
         s1 += sum8(d[c]);
         s2 += dot8(d[c], n[c]);
       }
       const float2 s = row_sum2<WPR>(s1, s2, red[it][0][grp], grp, part);
-      s1 = pre_layer ? s.x / (float)D : 0.f;
-      s2 = -s.y / (float)D;
+      s1 = pre_layer ? s.x * per_D : 0.f;
+      s2 = -s.y * per_D;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const float m2[8] = {s2, s2, s2, s2, s2, s2, s2, s2}, r[8] = {zr, zr, zr, zr, zr, zr, zr, zr};
         sub8(d[c], s1);
         acc8(d[c], n[c], m2);
         acc8(Z[c], d[c], r);
-        mask_columns<WHOLE>(Z[c], c0 + c * kChunk, D);
+        Columns<WHOLE>(c0 + c * kChunk, D).mask(Z[c]);
       }
     }
     float s3 = 0.f, s4 = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int cc = c0 + c * kChunk;
+      const Columns<WHOLE> cc(c0 + c * kChunk, D);
       float t[8];
       if (p.dx.p && !dead) {
         scale8(Z[c], p.res, t);
-        store_row<WHOLE>(p.dx, row, cc, D, t);
+        store_row<WHOLE>(p.dx, row, cc, t);
       }
       if (post) {
         sub8(u[c], ym);
         scale8(u[c], yr, u[c]);
-        mask_columns<WHOLE>(u[c], cc, D);
+        cc.mask(u[c]);
       }
       if (ROWWISE) {
         if (p.dgate.p) {
           float v[8];
           copy8(v, u[c]);
           if (p.post_g) {
-            load_param<WHOLE>(p.post_g, cc, D, t);
+            load_param<WHOLE>(p.post_g, cc, t);
             mul8(v, t);
           }
           if (p.post_b) {
-            load_param<WHOLE>(p.post_b, cc, D, t);
+            load_param<WHOLE>(p.post_b, cc, t);
             add8(v, t);
           }
           mul8(v, Z[c]);
@@ -353,7 +355,7 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
       }
       if (!ROWWISE) mul8(Z[c], gate[c]);
       if (p.post_g) {
-        load_param<WHOLE>(p.post_g, cc, D, t);
+        load_param<WHOLE>(p.post_g, cc, t);
         mul8(Z[c], t);
       }
       if (post) {
@@ -364,23 +366,23 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
     if (!p.dy.p && !p.dy8.q) continue;
     if (post) {
       const float2 s = row_sum2<WPR>(s3, s4, red[it][1][grp], grp, part);
-      s3 = post_layer ? s.x / (float)D : 0.f;
-      s4 = -s.y / (float)D;
+      s3 = post_layer ? s.x * per_D : 0.f;
+      s4 = -s.y * per_D;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const float m2[8] = {s4, s4, s4, s4, s4, s4, s4, s4};
         sub8(Z[c], s3);
         acc8(Z[c], u[c], m2);
         scale8(Z[c], yr, Z[c]);
-        mask_columns<WHOLE>(Z[c], c0 + c * kChunk, D);
+        Columns<WHOLE>(c0 + c * kChunk, D).mask(Z[c]);
       }
     }
     if (dead) continue;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int cc = c0 + c * kChunk;
-      if (p.dy.p) store_row<WHOLE>(p.dy, row, cc, D, Z[c]);
-      if (p.dy8.q) store_row8<WHOLE>(p.dy8, row, cc, D, Z[c]);
+      const Columns<WHOLE> cc(c0 + c * kChunk, D);
+      if (p.dy.p) store_row<WHOLE>(p.dy, row, cc, Z[c]);
+      if (p.dy8.q) store_row8<WHOLE>(p.dy8, row, cc, Z[c]);
     }
   }
   if (!ROWWISE) {
@@ -390,13 +392,13 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
     for (int k = 0; k < 4; ++k)
       if (need.params >> k & 1u)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) put_sum(param + (size_t)k * D, c0 + c * kChunk, sums[k][c]);
+        for (int c = 0; c < NC; ++c) put_sum(param + (size_t)k * D, Columns<WHOLE>(c0 + c * kChunk, D), sums[k][c]);
   }
 }
 
 // A launch for rows with a modulation of their own, or shared by groups.
 template <int NC, int WPR, bool ROWWISE>
-cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int teams) {
+cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams) {
   constexpr int WARPS = kGradWarps<WPR>, GROUPS = WARPS / WPR;
   RingPlan plan{};
   const auto add = [&](const Rows& r) {
@@ -422,14 +424,14 @@ cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need,
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3((unsigned)((teams + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
+    return launch_pdl(kernel, dim3((unsigned)((teams.n + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
                       (size_t)WARPS * plan.depth * plan.stage, c.stream, p, plan, teams, need, c.err);
   };
   return whole ? run(join_grad_kernel<NC, WPR, true, ROWWISE>) : run(join_grad_kernel<NC, WPR, false, ROWWISE>);
 }
 
 template <bool ROWWISE>
-cudaError_t join_grad_launch(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, int teams) {
+cudaError_t join_grad_launch(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, const Teams& teams) {
   switch (wpr) {
     case 1: return join_grad_run<1, 1, ROWWISE>(c, p, need, whole, teams);
     case 2: return join_grad_run<1, 2, ROWWISE>(c, p, need, whole, teams);
@@ -444,6 +446,6 @@ cudaError_t join_grad_launch(const Ctx& c, const JoinGrad& p, const JoinSums& ne
 
 }  // namespace
 
-cudaError_t launch_join_grad_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, int teams);
+cudaError_t launch_join_grad_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, const Teams& teams);
 
 }  // namespace lm

@@ -39,17 +39,24 @@ __device__ __forceinline__ void row_barrier(int grp) {
 // are contiguous over the warp and free of bank conflicts. Other rows: every 32nd column.
 // Either way values 0..3 are of the first block, 4..7 of the second.
 template <bool WHOLE>
-__device__ __forceinline__ int column(int k) {
-  const int lane = threadIdx.x & 31;
-  return WHOLE ? kBlk * (k >> 2) + 4 * lane + (k & 3) : 32 * k + lane;
-}
-template <bool WHOLE>
-__device__ __forceinline__ void mask_columns(float (&v)[8], int c0, int D) {
-  if (c0 + kChunk <= D) return;
+struct Columns {
+  int c0;     // first column of the chunk
+  int left;   // columns that the chunk has from the lane's first one on
+  bool full;  // all 256
+
+  __device__ __forceinline__ Columns(int chunk, int D)
+      : c0(chunk), left(D - chunk - (WHOLE ? 4 : 1) * (int)(threadIdx.x & 31)), full(chunk + kChunk <= D) {}
+  __device__ __forceinline__ int first() const { return c0 + (WHOLE ? 4 : 1) * (int)(threadIdx.x & 31); }
+  // From the lane's first column to its k-th.
+  __device__ __forceinline__ static constexpr int offset(int k) { return WHOLE ? kBlk * (k >> 2) + (k & 3) : 32 * k; }
+  __device__ __forceinline__ bool on(int k) const { return offset(k) < left; }
+  __device__ __forceinline__ void mask(float (&v)[8]) const {
+    if (full) return;  // (uniform over the warp)
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (c0 + column<WHOLE>(k) >= D) v[k] = 0.f;
-}
+    for (int k = 0; k < 8; ++k)
+      if (!on(k)) v[k] = 0.f;
+  }
+};
 __device__ __forceinline__ void widen4(uint2 u, float* v) {
   v[0] = __uint_as_float(u.x << 16);
   v[1] = __uint_as_float(u.x & 0xFFFF0000u);
@@ -59,130 +66,165 @@ __device__ __forceinline__ void widen4(uint2 u, float* v) {
 __device__ __forceinline__ void put4(float4 a, float* v) {
   v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
 }
-// From global memory: row `row` of m (fp32 or bf16), columns from c0 on; those from D on read as zero.
+__device__ __forceinline__ size_t row_offset(unsigned row, int ld) { return (size_t)row * (unsigned)ld; }
+
+// From global memory: a row of fp32 or bf16; columns from D on read as zero.
 template <bool WHOLE>
-__device__ __forceinline__ void load_row(const Rows& m, size_t row, int c0, int D, float (&v)[8]) {
+__device__ __forceinline__ void load_row(const void* base, int ld, int dtype, unsigned row, const Columns<WHOLE>& c,
+                                         float (&v)[8]) {
+  const size_t at = row_offset(row, ld) + c.first();
 #pragma unroll
   for (int k = 0; k < 8; ++k) v[k] = 0.f;
-  if (WHOLE) {
+  if (dtype == LAZYMAR_F32) {
+    const float* p = static_cast<const float*>(base) + at;
+    if (WHOLE) {
+      if (c.on(0)) put4(*reinterpret_cast<const float4*>(p), v);
+      if (c.on(4)) put4(*reinterpret_cast<const float4*>(p + kBlk), v + 4);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int col = c0 + column<true>(4 * j);
-      if (col >= D) continue;
-      if (m.dtype == LAZYMAR_F32)
-        put4(*reinterpret_cast<const float4*>(static_cast<const float*>(m.p) + row * m.ld + col), v + 4 * j);
-      else
-        widen4(*reinterpret_cast<const uint2*>(static_cast<const bf16*>(m.p) + row * m.ld + col), v + 4 * j);
+      for (int k = 0; k < 8; ++k)
+        if (c.on(k)) v[k] = p[32 * k];
     }
   } else {
+    const bf16* p = static_cast<const bf16*>(base) + at;
+    if (WHOLE) {
+      if (c.on(0)) widen4(*reinterpret_cast<const uint2*>(p), v);
+      if (c.on(4)) widen4(*reinterpret_cast<const uint2*>(p + kBlk), v + 4);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int col = c0 + column<false>(k);
-      if (col >= D) continue;
-      v[k] = m.dtype == LAZYMAR_F32 ? static_cast<const float*>(m.p)[row * m.ld + col]
-                                    : to_f(static_cast<const bf16*>(m.p)[row * m.ld + col]);
+      for (int k = 0; k < 8; ++k)
+        if (c.on(k)) v[k] = to_f(p[32 * k]);
     }
   }
 }
 template <bool WHOLE>
-__device__ __forceinline__ void load_param(const float* p, int c0, int D, float (&v)[8]) {
-  load_row<WHOLE>(Rows{p, nullptr, 0, 0, LAZYMAR_F32, true}, 0, c0, D, v);
+__device__ __forceinline__ void load_row(const Rows& m, unsigned row, const Columns<WHOLE>& c, float (&v)[8]) {
+  load_row<WHOLE>(m.p, m.ld, m.dtype, row, c, v);
 }
-// From a warp's stage. `shift`: the row's first byte in it (rows that are not whole).
 template <bool WHOLE>
-__device__ __forceinline__ void load_stage(const uint8_t* st, int dtype, uint32_t shift, uint32_t s0, uint32_t s1,
+__device__ __forceinline__ void load_param(const float* p, const Columns<WHOLE>& c, float (&v)[8]) {
+  load_row<WHOLE>(p, 0, LAZYMAR_F32, 0u, c, v);
+}
+template <bool WHOLE>
+__device__ __forceinline__ void store_row(const MatOut& m, unsigned row, const Columns<WHOLE>& c, const float (&v)[8]) {
+  const size_t at = row_offset(row, m.ld) + c.first();
+  if (m.dtype == LAZYMAR_F32) {
+    float* p = static_cast<float*>(m.p) + at;
+    if (WHOLE) {
+      if (c.on(0)) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+      if (c.on(4)) *reinterpret_cast<float4*>(p + kBlk) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c.on(k)) p[32 * k] = v[k];
+    }
+  } else {
+    bf16* p = static_cast<bf16*>(m.p) + at;
+    if (WHOLE) {
+      if (c.on(0)) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+      if (c.on(4)) *reinterpret_cast<uint2*>(p + kBlk) = make_uint2(pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; k += 2) {
+        const uint32_t two = pack_bf16(v[k], v[k + 1]);
+        uint16_t* q = reinterpret_cast<uint16_t*>(p);
+        if (c.on(k)) q[32 * k] = (uint16_t)two;
+        if (c.on(k + 1)) q[32 * (k + 1)] = (uint16_t)(two >> 16);
+      }
+    }
+  }
+}
+__device__ __forceinline__ void copy8(float (&y)[8], const float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = v[i];
+}
+// To block8: a block is four values of each lane of the warp. Columns from D on hold zero.
+template <bool WHOLE>
+__device__ __forceinline__ void store_row8(const lazymar_block8& o, unsigned row, const Columns<WHOLE>& c, const float (&v)[8]) {
+  const int lane = threadIdx.x & 31;
+  uint8_t* q = static_cast<uint8_t*>(o.q) + row_offset(row, o.ldq) + c.first();
+  uint32_t amax[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    amax[j] = __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(fmaxf(fabsf(v[4 * j]), fabsf(v[4 * j + 1])),
+                                                                   fmaxf(fabsf(v[4 * j + 2]), fabsf(v[4 * j + 3])))));
+  float w[8];
+  copy8(w, v);
+  if (max(amax[0], amax[1]) >= 0x7F800000u) {  // an infinity: the finite values' maxima
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float m = 0.f;
+#pragma unroll
+      for (int i = 4 * j; i < 4 * j + 4; ++i) {
+        m = fmaxf(m, fabsf(nonfinite_to(w[i], 0.f)));
+        w[i] = nonfinite_to(w[i], __uint_as_float(0x7FC00000u));
+      }
+      amax[j] = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float s = block8_inv(block8_exp(amax[j]));
+    const unsigned long long ss = f32x2_pack(s, s);
+    f32x2_unpack(f32x2_mul(f32x2_pack(w[4 * j], w[4 * j + 1]), ss), w[4 * j], w[4 * j + 1]);
+    f32x2_unpack(f32x2_mul(f32x2_pack(w[4 * j + 2], w[4 * j + 3]), ss), w[4 * j + 2], w[4 * j + 3]);
+    const uint32_t b = e4m3x4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    if (WHOLE) {
+      if (c.on(4 * j)) *reinterpret_cast<uint32_t*>(q + kBlk * j) = b;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c.on(4 * j + i)) q[32 * (4 * j + i)] = (uint8_t)(b >> (8 * i));
+    }
+  }
+  // (lane 0 the first block's scale, lane 1 the second's)
+  const uint32_t byte = block8_exp(lane == 0 ? amax[0] : amax[1]);
+  if (lane < 2 && c.c0 + kBlk * lane < c.left + c.first()) o.scale[(size_t)(unsigned)(c.c0 / kBlk + lane) * (unsigned)o.lds + row] = (uint8_t)byte;
+}
+// From a warp's stage. `st`: the row's chunk in it; s0, s1: the scales of an 8-bit row.
+template <bool WHOLE>
+__device__ __forceinline__ void load_stage(const uint8_t* st, int dtype, uint32_t s0, uint32_t s1, const Columns<WHOLE>& c,
                                            float (&v)[8]) {
   const int lane = threadIdx.x & 31;
-  if (dtype == LAZYMAR_E4M3) {
+  if (dtype == LAZYMAR_F32) {
+    if (WHOLE) {
+      const float4* p = reinterpret_cast<const float4*>(st) + lane;
+      put4(p[0], v);
+      put4(p[32], v + 4);
+    } else {
+      const float* p = reinterpret_cast<const float*>(st) + lane;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = p[32 * k];
+    }
+  } else if (dtype == LAZYMAR_BF16) {
+    if (WHOLE) {
+      const uint2* p = reinterpret_cast<const uint2*>(st) + lane;
+      widen4(p[0], v);
+      widen4(p[32], v + 4);
+    } else {
+      const uint16_t* p = reinterpret_cast<const uint16_t*>(st) + lane;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = __uint_as_float((uint32_t)p[32 * k] << 16);
+    }
+  } else {
     const float s[2] = {block8_scale(s0), block8_scale(s1)};
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       uint32_t w;
       if (WHOLE) {
-        w = *reinterpret_cast<const uint32_t*>(st + kBlk * j + 4 * lane);
+        w = reinterpret_cast<const uint32_t*>(st)[32 * j + lane];
       } else {
         w = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w |= (uint32_t)st[kBlk * j + 32 * i + lane] << (8 * i);
       }
       const float2 a = e4m3x2_to_f2(w & 0xFFFFu), b = e4m3x2_to_f2(w >> 16);
-      v[4 * j] = a.x * s[j]; v[4 * j + 1] = a.y * s[j]; v[4 * j + 2] = b.x * s[j]; v[4 * j + 3] = b.y * s[j];
-    }
-  } else if (WHOLE) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if (dtype == LAZYMAR_F32) put4(*reinterpret_cast<const float4*>(st + 4 * (kBlk * j + 4 * lane)), v + 4 * j);
-      else widen4(*reinterpret_cast<const uint2*>(st + 2 * (kBlk * j + 4 * lane)), v + 4 * j);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      v[k] = dtype == LAZYMAR_F32 ? *reinterpret_cast<const float*>(st + shift + 4 * (32 * k + lane))
-                                  : __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(st + shift + 2 * (32 * k + lane)) << 16);
-  }
-}
-template <bool WHOLE>
-__device__ __forceinline__ void store_row(const MatOut& m, size_t row, int c0, int D, const float (&v)[8]) {
-  if (WHOLE) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int col = c0 + column<true>(4 * j);
-      if (col >= D) continue;
-      if (m.dtype == LAZYMAR_F32)
-        *reinterpret_cast<float4*>(static_cast<float*>(m.p) + row * m.ld + col) =
-            make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-      else
-        *reinterpret_cast<uint2*>(static_cast<bf16*>(m.p) + row * m.ld + col) =
-            make_uint2(pack_bf16(v[4 * j], v[4 * j + 1]), pack_bf16(v[4 * j + 2], v[4 * j + 3]));
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int col = c0 + column<false>(k);
-      if (col >= D) continue;
-      if (m.dtype == LAZYMAR_F32) static_cast<float*>(m.p)[row * m.ld + col] = v[k];
-      else static_cast<bf16*>(m.p)[row * m.ld + col] = from_f<bf16>(v[k]);
+      const unsigned long long ss = f32x2_pack(s[j], s[j]);
+      f32x2_unpack(f32x2_mul(f32x2_pack(a.x, a.y), ss), v[4 * j], v[4 * j + 1]);
+      f32x2_unpack(f32x2_mul(f32x2_pack(b.x, b.y), ss), v[4 * j + 2], v[4 * j + 3]);
     }
   }
-}
-// To block8: a block is four values of each lane of the warp. Columns from D on hold zero.
-template <bool WHOLE>
-__device__ __forceinline__ void store_row8(const lazymar_block8& o, size_t row, int c0, int D, const float (&v)[8]) {
-  const int lane = threadIdx.x & 31;
-  uint8_t* q = static_cast<uint8_t*>(o.q) + row * o.ldq;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    if (c0 + kBlk * j >= D) break;  // (uniform over the warp)
-    float w[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-    uint32_t amax = __float_as_uint(fmaxf(fmaxf(fabsf(w[0]), fabsf(w[1])), fmaxf(fabsf(w[2]), fabsf(w[3]))));
-    amax = __reduce_max_sync(0xffffffffu, amax);
-    if (amax >= 0x7F800000u) {  // an infinity: the finite values' maximum
-      float m = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        m = fmaxf(m, fabsf(nonfinite_to(w[i], 0.f)));
-        w[i] = nonfinite_to(w[i], __uint_as_float(0x7FC00000u));
-      }
-      amax = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
-    }
-    const uint32_t byte = block8_exp(amax);
-    const float s = block8_inv(byte);
-    const unsigned long long ss = f32x2_pack(s, s);
-    f32x2_unpack(f32x2_mul(f32x2_pack(w[0], w[1]), ss), w[0], w[1]);
-    f32x2_unpack(f32x2_mul(f32x2_pack(w[2], w[3]), ss), w[2], w[3]);
-    const uint32_t b = e4m3x4(w[0], w[1], w[2], w[3]);
-    if (WHOLE) {
-      const int col = c0 + column<true>(4 * j);
-      if (col < D) *reinterpret_cast<uint32_t*>(q + col) = b;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int col = c0 + column<false>(4 * j + i);
-        if (col < D) q[col] = (uint8_t)(b >> (8 * i));
-      }
-    }
-    if (lane == 0) o.scale[(size_t)((c0 + kBlk * j) / kBlk) * o.lds + row] = (uint8_t)byte;
-  }
+  c.mask(v);
 }
 
 // y = v a + b; paired
@@ -207,84 +249,97 @@ __device__ __forceinline__ float dot8(const float (&v)[8], const float (&a)[8]) 
   f32x2_unpack(q, x, y);
   return x + y;
 }
-__device__ __forceinline__ void copy8(float (&y)[8], const float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = v[i];
-}
 
 // ---------------------------------------------------------------------------
 // A warp's ring of row pieces: its columns of every tensor, `depth` rows ahead, by bulk
-// copies. Rows that are not on a 16-byte boundary are copied from the boundary before
-// to the one behind, which are the row's neighbours' bytes; the first and the last row, whose
-// neighbours are not the tensor's, come element by element.
+// copies, one lane a tensor. Rows that are not on a 16-byte boundary are copied from the
+// boundary before to the one behind, which are the row's neighbours' bytes; the first and the
+// last row, whose neighbours are not the tensor's, come element by element.
 // ---------------------------------------------------------------------------
 template <bool WHOLE>
 struct RowRing {
   uint8_t* base;
   uint64_t* bars;
-  int depth, mine, c0, slot;
+  int depth, mine, slot, streams;
   uint32_t stage, phase;
+  // this lane's tensor: the piece of row 0, bytes from row to row and of a row, its place in a stage
+  uintptr_t src;
+  size_t pitch;
+  uint32_t bytes, at, total;
 
   __device__ __forceinline__ void init(uint8_t* smem, uint64_t* b, const RingPlan& plan, int first_column, int columns) {
+    const int lane = threadIdx.x & 31;
     base = smem;
     bars = b;
     depth = plan.depth;
     stage = plan.stage;
-    c0 = first_column;
     mine = columns;
     slot = 0;
     phase = 0;
-    if ((threadIdx.x & 31) == 0)
+    streams = plan.n;
+    bytes = 0;
+    if (lane < streams) {
+      const RowStream& t = plan.t[lane];
+      src = reinterpret_cast<uintptr_t>(t.p) + (size_t)first_column * t.e;
+      pitch = t.pitch;
+      bytes = (uint32_t)max(mine, 0) * t.e;
+      at = t.at;
+    }
+    if (WHOLE) {
+      bytes = (bytes + 15u) & ~15u;
+      total = __reduce_add_sync(0xffffffffu, bytes);
+    }
+    if (lane == 0)
       for (int s = 0; s < depth; ++s) mbar_init(&bars[s], 1);
     fence_mbar_init();
   }
-  __device__ __forceinline__ static uint32_t shift(const RowStream& t, size_t row, int c0) {
-    return WHOLE ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(t.p) + row * t.pitch + (size_t)c0 * t.e) & 15u;
-  }
   // Row `row` into stage s. All lanes call it.
-  __device__ __forceinline__ void fetch(const RingPlan& plan, long long row, int s, int M) {
+  __device__ __forceinline__ void fetch(const RingPlan& plan, int row, int s, int first_column, int M) {
     if (mine <= 0) return;
     const int lane = threadIdx.x & 31;
-    uint8_t* dst = base + (size_t)s * stage;
+    uint8_t* dst = base + (uint32_t)s * stage;
     if (!WHOLE && (row == 0 || row == M - 1)) {
       for (int i = 0; i < plan.n; ++i) {
         const RowStream& t = plan.t[i];
-        const uint8_t* src = t.p + (size_t)row * t.pitch + (size_t)c0 * t.e;
-        uint8_t* to = dst + t.at + shift(t, (size_t)row, c0);
+        const uint8_t* from = t.p + (size_t)row * t.pitch + (size_t)first_column * t.e;
+        uint8_t* to = dst + t.at + (reinterpret_cast<uintptr_t>(from) & 15u);
         for (int c = lane; c < mine; c += 32) {
-          if (t.e == 4) reinterpret_cast<float*>(to)[c] = reinterpret_cast<const float*>(src)[c];
-          else if (t.e == 2) reinterpret_cast<uint16_t*>(to)[c] = reinterpret_cast<const uint16_t*>(src)[c];
-          else to[c] = src[c];
+          if (t.e == 4) reinterpret_cast<float*>(to)[c] = reinterpret_cast<const float*>(from)[c];
+          else if (t.e == 2) reinterpret_cast<uint16_t*>(to)[c] = reinterpret_cast<const uint16_t*>(from)[c];
+          else to[c] = from[c];
         }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars[s]);
       return;
     }
-    if (lane != 0) return;
-    uint32_t total = 0;
-    for (int i = 0; i < plan.n; ++i) {
-      const RowStream& t = plan.t[i];
-      total += (shift(t, (size_t)row, c0) + (uint32_t)mine * t.e + 15u) & ~15u;
+    uintptr_t p = src + (size_t)(unsigned)row * pitch;
+    uint32_t n = bytes, sum = total;
+    if (!WHOLE) {
+      n = lane < streams ? (((uint32_t)p & 15u) + bytes + 15u) & ~15u : 0u;
+      p &= ~(uintptr_t)15;
+      sum = __reduce_add_sync(0xffffffffu, n);
     }
-    mbar_arrive_expect_tx(&bars[s], total);
-    for (int i = 0; i < plan.n; ++i) {
-      const RowStream& t = plan.t[i];
-      const uint32_t sh = shift(t, (size_t)row, c0);
-      bulk_load(dst + t.at, t.p + (size_t)row * t.pitch + (size_t)c0 * t.e - sh, (sh + (uint32_t)mine * t.e + 15u) & ~15u,
-                &bars[s]);
-    }
+    if (lane == 0) mbar_arrive_expect_tx(&bars[s], sum);
+    __syncwarp();
+    if (lane < streams) bulk_load(dst + at, reinterpret_cast<const void*>(p), n, &bars[s]);
   }
   __device__ __forceinline__ bool wait(volatile int* abort_flag, unsigned* err) {
     return mine <= 0 || mbar_wait(&bars[slot], phase, abort_flag, err);
   }
-  __device__ __forceinline__ const uint8_t* row() const { return base + (size_t)slot * stage; }
-  // The row has been read by every lane: its stage takes the row `ahead`, if there is one.
-  __device__ __forceinline__ void next(const RingPlan& plan, long long ahead, long long end, int M, bool dead) {
+  // Tensor i's piece of the row that has come.
+  __device__ __forceinline__ const uint8_t* piece(const RingPlan& plan, int i, int row, int first_column) const {
+    const RowStream& t = plan.t[i];
+    const uint8_t* st = base + (uint32_t)slot * stage + t.at;
+    if (WHOLE) return st;
+    return st + (((uint32_t)reinterpret_cast<uintptr_t>(t.p) + (uint32_t)first_column * t.e + (uint32_t)row * (uint32_t)t.pitch) & 15u);
+  }
+  // The row has been read by every lane: its stage takes row `ahead`, if there is one.
+  __device__ __forceinline__ void next(const RingPlan& plan, int ahead, int end, int first_column, int M, bool dead) {
     __syncwarp();
     if (!dead && ahead < end) {
       fence_proxy_async_smem();
-      fetch(plan, ahead, slot, M);
+      fetch(plan, ahead, slot, first_column, M);
     }
     if (++slot == depth) {
       slot = 0;
@@ -296,9 +351,17 @@ struct RowRing {
 }  // namespace
 
 // Ranges of consecutive rows, one for each team (the warps that work on a row together).
-__host__ __device__ __forceinline__ long long team_start(int M, int teams, int t) { return (long long)M * t / teams; }
-__host__ __device__ __forceinline__ int team_of(int M, int teams, long long row) {
-  return (int)(((row + 1) * teams - 1) / M);
+struct Teams {
+  int n, rows, more;  // the first `more` teams have one row more
+};
+inline Teams teams_of(int M, int most) {
+  const int n = M < most ? M : most;
+  return Teams{n, M / n, M % n};
+}
+__host__ __device__ __forceinline__ int team_start(const Teams& t, int i) { return i * t.rows + (i < t.more ? i : t.more); }
+__host__ __device__ __forceinline__ int team_of(const Teams& t, int row) {
+  const int edge = t.more * (t.rows + 1);
+  return row < edge ? row / (t.rows + 1) : t.more + (row - edge) / t.rows;
 }
 
 }  // namespace lm
