@@ -25,10 +25,9 @@ struct JoinSums {
   unsigned mods, params;
 };
 
-template <int WPR>
-constexpr int kGradWarps = WPR == 5 ? 5 : WPR > 8 ? 16 : 8;
-template <int WPR>
-constexpr int kGradCtas = WPR > 8 ? 1 : WPR == 5 ? 3 : 2;
+// PLAIN: no norm of y, no parameters and none of their gradients (the modulated norm of a block).
+// Warps on an SM, by what a lane keeps: P is not needed then, and ROWWISE no sum at all.
+constexpr int grad_sm_warps(bool plain, bool rowwise) { return plain ? (rowwise ? 24 : 20) : 16; }
 
 namespace {
 
@@ -59,11 +58,11 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int gr
   return s;
 }
 
-template <int NC, int WPR, bool WHOLE, bool ROWWISE>
-__global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
+template <int NC, int WPR, bool WHOLE, bool ROWWISE, bool PLAIN>
+__global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warps(PLAIN, ROWWISE)))
     join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, const Teams teams, JoinSums need,
                      unsigned* err) {
-  constexpr int WARPS = kGradWarps<WPR>, GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR), GROUPS = WARPS / WPR;
   extern __shared__ __align__(128) uint8_t ring_smem[];
   __shared__ uint64_t bars[WARPS][kMostStages];
   __shared__ float2 red[2][2][GROUPS][WPR];
@@ -82,10 +81,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
   for (int s = 0; s < plan.depth; ++s)
     if (first + s < end) ring.fetch(plan, first + s, s, c0, p.M);
   const float per_D = 1.f / (float)D;
-  const bool pre = p.pre != LAZYMAR_NORM_NONE, post = p.post != LAZYMAR_NORM_NONE;
+  const bool pre = PLAIN || p.pre != LAZYMAR_NORM_NONE, post = !PLAIN && p.post != LAZYMAR_NORM_NONE;
   const bool pre_layer = p.pre == LAZYMAR_NORM_LAYER, post_layer = p.post == LAZYMAR_NORM_LAYER;
   const unsigned sums_of = need.mods | need.params;
-  const bool ab = ROWWISE ? need.params & 3u : sums_of & 3u, pq = ROWWISE ? need.params >> 2 : sums_of >> 2;
+  const bool ab = !(PLAIN && ROWWISE) && (ROWWISE ? need.params & 3u : sums_of & 3u);
+  const bool pq = !(PLAIN && ROWWISE) && (ROWWISE ? need.params >> 2 : sums_of >> 2);
 
   // statistics and 8-bit scales (lanes: the warp's blocks, of z and then of y) of the next row
   float next_ym = 0.f, next_yr = 1.f, next_zm = 0.f, next_zr = 1.f;
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
       // the parameters' sums go on in the workspace, group by group
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        if (!(need.params >> k & 1u)) continue;
+        if (PLAIN || !(need.params >> k & 1u)) continue;
         copy8(v, sums[k][c]);
         mul8(v, k < 2 ? scale[c] : gate[c]);
         if (start > first) {
@@ -164,11 +164,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         }
         if (p.dscale.p) {
           copy8(v, sums[SUM_B][c]);
-          if (p.pre_g) {
+          if (!PLAIN && p.pre_g) {
             load_param<WHOLE>(p.pre_g, cc, t);
             mul8(v, t);
           }
-          if (p.pre_b) {
+          if (!PLAIN && p.pre_b) {
             load_param<WHOLE>(p.pre_b, cc, t);
             acc8(v, t, sums[SUM_A][c]);
           }
@@ -176,11 +176,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         }
         if (p.dgate.p) {
           copy8(v, sums[SUM_Q][c]);
-          if (p.post_g) {
+          if (!PLAIN && p.post_g) {
             load_param<WHOLE>(p.post_g, cc, t);
             mul8(v, t);
           }
-          if (p.post_b) {
+          if (!PLAIN && p.post_b) {
             load_param<WHOLE>(p.post_b, cc, t);
             acc8(v, t, sums[SUM_P][c]);
           }
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
       } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (need.mods >> k & 1u) put_sum(slot + (size_t)k * D, cc, sums[k][c]);
+          if (!(PLAIN && k == SUM_P) && (need.mods >> k & 1u)) put_sum(slot + (size_t)k * D, cc, sums[k][c]);
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k)
@@ -223,47 +223,50 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
     const bool ok = dead || ring.wait(abort_flag, err);
     dead |= !__all_sync(0xffffffffu, ok);
     float d[NC][8], n[NC][8], Z[NC][8], u[NC][8];
-    {
-      int i = 0;
-      const auto from = [&](const Rows& m, int first_scale, float (&to)[NC][8]) {
-        const uint8_t* st = ring.piece(plan, i, row, c0);
+    int i = 0;
+    const auto from = [&](const Rows& m, int first_scale, float (&to)[NC][8]) {
+      const uint8_t* st = ring.piece(plan, i, row, c0);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          uint32_t s0 = 0, s1 = 0;
-          if (m.dtype == LAZYMAR_E4M3) {
-            s0 = __shfl_sync(0xffffffffu, sb, first_scale + 2 * c);
-            s1 = __shfl_sync(0xffffffffu, sb, first_scale + 2 * c + 1);
-          }
-          load_stage<WHOLE>(st + (uint32_t)c * kChunk * plan.t[i].e, m.dtype, s0, s1, Columns<WHOLE>(c0 + c * kChunk, D), to[c]);
+      for (int c = 0; c < NC; ++c) {
+        uint32_t s0 = 0, s1 = 0;
+        if (m.dtype == LAZYMAR_E4M3) {
+          s0 = __shfl_sync(0xffffffffu, sb, first_scale + 2 * c);
+          s1 = __shfl_sync(0xffffffffu, sb, first_scale + 2 * c + 1);
         }
-        ++i;
-      };
-      const auto none = [&](float (&to)[NC][8]) {
+        load_stage<WHOLE>(st + (uint32_t)c * kChunk * plan.t[i].e, m.dtype, s0, s1, Columns<WHOLE>(c0 + c * kChunk, D), to[c]);
+      }
+      ++i;
+    };
+    const auto none = [&](float (&to)[NC][8]) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) to[c][k] = 0.f;
+    };
+    if (pre) {
+      from(p.dh, 0, d);
+      from(p.z, 0, n);
+    }
+    if (ROWWISE) {
+      i = p.gate.p || p.scale.p ? plan.n - (p.gate.p != nullptr) - (p.scale.p != nullptr) : i;
+      if (p.gate.p) from(p.gate, 0, gate);
+      if (p.scale.p) {
+        from(p.scale, 0, scale);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) to[c][k] = 0.f;
-      };
-      if (pre) {
-        from(p.dh, 0, d);
-        from(p.z, 0, n);
+          for (int k = 0; k < 8; ++k) scale[c][k] += 1.f;
       }
+      i = pre ? 2 : 0;
+    }
+    // dz and y are read, and the stage given on, when they are needed: fewer registers
+    auto rest = [&] {
       if (p.dz.p) from(p.dz, 0, Z);
       else none(Z);
       if (p.y.p) from(p.y, 2 * NC, u);
       else none(u);
-      if (ROWWISE) {
-        if (p.gate.p) from(p.gate, 0, gate);
-        if (p.scale.p) {
-          from(p.scale, 0, scale);
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) scale[c][k] += 1.f;
-        }
-      }
-    }
-    ring.next(plan, row + plan.depth, end, c0, p.M, dead);
+      ring.next(plan, row + plan.depth, end, c0, p.M, dead);
+    };
     if (pre) {
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -277,11 +280,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
           if (p.dscale.p) {
             float v[8];
             copy8(v, n[c]);
-            if (p.pre_g) {
+            if (!PLAIN && p.pre_g) {
               load_param<WHOLE>(p.pre_g, cc, t);
               mul8(v, t);
             }
-            if (p.pre_b) {
+            if (!PLAIN && p.pre_b) {
               load_param<WHOLE>(p.pre_b, cc, t);
               add8(v, t);
             }
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
           acc8(sums[SUM_B][c], d[c], n[c]);
         }
         if (!ROWWISE) mul8(d[c], scale[c]);
-        if (p.pre_g) {
+        if (!PLAIN && p.pre_g) {
           load_param<WHOLE>(p.pre_g, cc, t);
           mul8(d[c], t);
         }
@@ -309,6 +312,7 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
       const float2 s = row_sum2<WPR>(s1, s2, red[it][0][grp], grp, part);
       s1 = pre_layer ? s.x * per_D : 0.f;
       s2 = -s.y * per_D;
+      rest();
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const float m2[8] = {s2, s2, s2, s2, s2, s2, s2, s2}, r[8] = {zr, zr, zr, zr, zr, zr, zr, zr};
@@ -317,6 +321,8 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         acc8(Z[c], d[c], r);
         Columns<WHOLE>(c0 + c * kChunk, D).mask(Z[c]);
       }
+    } else {
+      rest();
     }
     float s3 = 0.f, s4 = 0.f;
 #pragma unroll
@@ -336,11 +342,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         if (p.dgate.p) {
           float v[8];
           copy8(v, u[c]);
-          if (p.post_g) {
+          if (!PLAIN && p.post_g) {
             load_param<WHOLE>(p.post_g, cc, t);
             mul8(v, t);
           }
-          if (p.post_b) {
+          if (!PLAIN && p.post_b) {
             load_param<WHOLE>(p.post_b, cc, t);
             add8(v, t);
           }
@@ -350,11 +356,11 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
         mul8(Z[c], gate[c]);
       }
       if (pq) {
-        add8(sums[SUM_P][c], Z[c]);
+        if (!PLAIN) add8(sums[SUM_P][c], Z[c]);
         acc8(sums[SUM_Q][c], Z[c], u[c]);
       }
       if (!ROWWISE) mul8(Z[c], gate[c]);
-      if (p.post_g) {
+      if (!PLAIN && p.post_g) {
         load_param<WHOLE>(p.post_g, cc, t);
         mul8(Z[c], t);
       }
@@ -387,7 +393,7 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
   }
   if (!ROWWISE) {
     flush(start, stop);
-  } else {
+  } else if (!PLAIN) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (need.params >> k & 1u)
@@ -396,30 +402,17 @@ __global__ void __launch_bounds__(kGradWarps<WPR> * 32, kGradCtas<WPR>)
   }
 }
 
-// A launch for rows with a modulation of their own, or shared by groups.
-template <int NC, int WPR, bool ROWWISE>
+template <int NC, int WPR, bool ROWWISE, bool PLAIN>
 cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams) {
-  constexpr int WARPS = kGradWarps<WPR>, GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR), GROUPS = WARPS / WPR;
   RingPlan plan{};
-  const auto add = [&](const Rows& r) {
-    if (!r.p) return;
-    const uint32_t e = r.dtype == LAZYMAR_F32 ? 4 : r.dtype == LAZYMAR_BF16 ? 2 : 1;
-    plan.t[plan.n++] = RowStream{static_cast<const uint8_t*>(r.p), (size_t)r.ld * e, plan.stage, e};
-    plan.stage += NC * kChunk * e + 32;
-  };
-  if (p.pre != LAZYMAR_NORM_NONE) {
-    add(p.dh);
-    add(p.z);
-  }
-  add(p.dz);
-  add(p.y);
-  if (ROWWISE) {
-    add(p.gate);
-    add(p.scale);
-  }
-  constexpr int kRoom = 210 * 1024 / kGradCtas<WPR>;
-  plan.depth = kRoom / (WARPS * (int)plan.stage);
-  if (plan.depth > 4) plan.depth = 4;
+  if (p.pre != LAZYMAR_NORM_NONE)
+    for (const Rows* r : {&p.dh, &p.z}) add_stream(plan, *r, NC * kChunk);
+  for (const Rows* r : {&p.dz, &p.y}) add_stream(plan, *r, NC * kChunk);
+  if (ROWWISE)
+    for (const Rows* r : {&p.gate, &p.scale}) add_stream(plan, *r, NC * kChunk);
+  constexpr int kRoom = 210 * 1024 / sm_ctas(WPR, grad_sm_warps(PLAIN, ROWWISE));
+  set_depth(plan, kRoom, WARPS);
   const auto run = [&](auto kernel) {
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
@@ -427,25 +420,29 @@ cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need,
     return launch_pdl(kernel, dim3((unsigned)((teams.n + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
                       (size_t)WARPS * plan.depth * plan.stage, c.stream, p, plan, teams, need, c.err);
   };
-  return whole ? run(join_grad_kernel<NC, WPR, true, ROWWISE>) : run(join_grad_kernel<NC, WPR, false, ROWWISE>);
+  return whole ? run(join_grad_kernel<NC, WPR, true, ROWWISE, PLAIN>) : run(join_grad_kernel<NC, WPR, false, ROWWISE, PLAIN>);
 }
 
-template <bool ROWWISE>
-cudaError_t join_grad_launch(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, const Teams& teams) {
-  switch (wpr) {
-    case 1: return join_grad_run<1, 1, ROWWISE>(c, p, need, whole, teams);
-    case 2: return join_grad_run<1, 2, ROWWISE>(c, p, need, whole, teams);
-    case 4: return join_grad_run<1, 4, ROWWISE>(c, p, need, whole, teams);
-    case 5: return join_grad_run<1, 5, ROWWISE>(c, p, need, whole, teams);
-    case 8: return join_grad_run<1, 8, ROWWISE>(c, p, need, whole, teams);
+template <bool ROWWISE, bool PLAIN>
+cudaError_t join_grad_launch(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams) {
+  switch (row_warps(p.D)) {
+    case 1: return join_grad_run<1, 1, ROWWISE, PLAIN>(c, p, need, whole, teams);
+    case 2: return join_grad_run<1, 2, ROWWISE, PLAIN>(c, p, need, whole, teams);
+    case 3: return join_grad_run<1, 3, ROWWISE, PLAIN>(c, p, need, whole, teams);
+    case 4: return join_grad_run<1, 4, ROWWISE, PLAIN>(c, p, need, whole, teams);
+    case 5: return join_grad_run<1, 5, ROWWISE, PLAIN>(c, p, need, whole, teams);
+    case 8: return join_grad_run<1, 8, ROWWISE, PLAIN>(c, p, need, whole, teams);
     default:
-      return p.D <= 16 * kChunk ? join_grad_run<1, 16, ROWWISE>(c, p, need, whole, teams)
-                                : join_grad_run<2, 16, ROWWISE>(c, p, need, whole, teams);
+      return p.D <= 16 * kChunk ? join_grad_run<1, 16, ROWWISE, PLAIN>(c, p, need, whole, teams)
+                                : join_grad_run<2, 16, ROWWISE, PLAIN>(c, p, need, whole, teams);
   }
 }
 
 }  // namespace
 
-cudaError_t launch_join_grad_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, int wpr, const Teams& teams);
+cudaError_t launch_join_grad_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams);
+cudaError_t launch_join_grad_plain(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams);
+cudaError_t launch_join_grad_plain_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole,
+                                           const Teams& teams);
 
 }  // namespace lm

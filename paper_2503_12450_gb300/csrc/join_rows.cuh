@@ -350,6 +350,31 @@ struct RowRing {
 
 }  // namespace
 
+inline bool on_eight(const Rows& r) { return !r.p || r.vec; }
+inline bool on_eight(const MatOut& r) { return !r.p || r.vec; }
+
+// The streams of a launch; stages for as many rows as `room` bytes hold for a CTA's warps, four at most.
+inline void add_stream(RingPlan& plan, const Rows& r, int columns) {
+  if (!r.p) return;
+  const uint32_t e = r.dtype == LAZYMAR_F32 ? 4 : r.dtype == LAZYMAR_BF16 ? 2 : 1;
+  plan.t[plan.n++] = RowStream{static_cast<const uint8_t*>(r.p), (size_t)r.ld * e, plan.stage, e};
+  plan.stage += (uint32_t)columns * e + 32;
+}
+inline void set_depth(RingPlan& plan, int room, int warps) {
+  plan.depth = room / (warps * (int)plan.stage);
+  if (plan.depth > 4) plan.depth = 4;
+}
+
+// Warps of a row of D columns, warps of a CTA (whole teams, and a multiple of four, so that the SM's four
+// schedulers have as many each: with CTAs of five warps 40960 x 1280 took 200 us instead of 154), and CTAs
+// on an SM for about `warps` warps there.
+inline int row_warps(int D) {
+  const int nc = (D + kChunk - 1) / kChunk;
+  return nc <= 5 ? nc : nc <= 8 ? 8 : 16;
+}
+constexpr int cta_warps(int wpr) { return wpr <= 2 ? 4 : wpr % 4 ? 4 * wpr : wpr; }
+constexpr int sm_ctas(int wpr, int warps) { return warps / cta_warps(wpr) > 0 ? warps / cta_warps(wpr) : 1; }
+
 // Ranges of consecutive rows, one for each team (the warps that work on a row together).
 struct Teams {
   int n, rows, more;  // the first `more` teams have one row more

@@ -6,98 +6,116 @@ namespace lm {
 
 namespace {
 
-// The sums that several teams have part of: the parameters' (blockIdx.y 0, if there are any),
-// and those of each group that may be divided. A warp has 128 columns. `slices` warps share
-// a task, each adds every so many teams', and they are added in order: all 32 warps of a
-// CTA for the parameters and for groups with many teams, otherwise one, and a CTA has 32 groups.
-constexpr int kFinishWarps = 32;
+// out (+)= v
+__device__ __forceinline__ void put_one(const MatOut& o, unsigned row, int col, float v, bool accumulate) {
+  const size_t at = row_offset(row, o.ld) + col;
+  if (o.dtype == LAZYMAR_F32) {
+    float* d = static_cast<float*>(o.p) + at;
+    *d = accumulate ? *d + v : v;
+  } else {
+    bf16* d = static_cast<bf16*>(o.p) + at;
+    *d = from_f<bf16>(accumulate ? to_f(*d) + v : v);
+  }
+}
 
-__global__ void __launch_bounds__(32 * kFinishWarps) join_grad_finish_kernel(const __grid_constant__ JoinGrad p, const Teams teams,
-                                                                             int groups, int tasks, bool rowwise, JoinSums need,
-                                                                             int group_slices) {
-  __shared__ float red[4][kFinishWarps][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x * 128 + lane, D = p.D;
-  const bool param = need.params && blockIdx.y == 0;
-  const int slices = param ? kFinishWarps : group_slices, slice = warp % slices;
-  const int y = param ? 0 : ((int)blockIdx.y - (need.params ? 1 : 0)) * (kFinishWarps / slices) + warp / slices;
-  const unsigned sums = param ? need.params : need.mods;
+// Sums over many teams: of all of them for the parameters, of those that a group of very many
+// rows is divided among for the modulation. A CTA has 32 columns of one result (blockIdx.y: 0..3 dpre_b,
+// dpre_g, dpost_b, dpost_g; 4..6 dshift, dscale, dgate) of one group (blockIdx.z); each of 32 slices adds every 32nd
+// team's, and the slices are added in order. Short chains of loads: it is all latency (40 columns of 608
+// teams: 4 us).
+constexpr int kSlices = 32;
+
+__global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __grid_constant__ JoinGrad p, const Teams teams,
+                                                                      bool rowwise, int first_result) {
+  __shared__ float red[2][kSlices][32];
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + lane, D = p.D;
+  const int result = (int)blockIdx.y + first_result, q = (int)blockIdx.z;
   pdl_wait();
   pdl_trigger();
-  int t0 = 0, t1 = teams.n - 1, q = 0, g0 = 0;
-  bool live = param || y < tasks;
-  if (!param && live) {
-    if (groups < teams.n) {
-      q = y;
-    } else {  // the group that teams y and y + 1 share, if y is the first to have some of it
-      const int b = team_start(teams, y + 1);
-      live = b % p.group != 0;
-      q = b / p.group;
-    }
-    if (p.group > 0) g0 = q * p.group;
+  const bool param = result < 4;
+  float* const params[4] = {p.dpre_b, p.dpre_g, p.dpost_b, p.dpost_g};
+  MatOut o = result == 4 ? p.dshift : result == 5 ? p.dscale : p.dgate;
+  const float *g = result == 5 ? p.pre_g : result == 6 ? p.post_g : nullptr, *b = result == 5 ? p.pre_b : result == 6 ? p.post_b : nullptr;
+  if (param) o = MatOut{params[result], 0, LAZYMAR_F32, true};
+  if (!o.p || (param && q > 0)) return;
+  // sums of the result: k0 and, times the shift b, k1
+  const int k0 = param ? result : result == 4 ? SUM_A : result == 5 ? SUM_B : SUM_Q, k1 = k0 - 1;
+  int t0 = 0, t1 = teams.n - 1, g0 = 0;
+  if (!param && p.group > 0) {
+    g0 = q * p.group;
     t0 = team_of(teams, g0);
-    t1 = team_of(teams, p.group > 0 ? g0 + min(p.group, p.M - g0) - 1 : p.M - 1);
-    live = live && t0 != t1 && (groups < teams.n || t0 == y);
+    t1 = team_of(teams, g0 + min(p.group, p.M - g0) - 1);
+    if (t0 == t1) return;  // (done there)
   }
+  float s0 = 0.f, s1 = 0.f;
+  if (col < D) {
+#pragma unroll 4
+    for (int t = t0 + slice; t <= t1; t += kSlices) {
+      const float* w = param ? p.ws + (rowwise ? 0 : (size_t)teams.n * 8 * D) + (size_t)t * 4 * D
+                             : p.ws + ((size_t)t * 2 + (g0 > team_start(teams, t))) * 4 * D;
+      s0 += w[(size_t)k0 * D + col];
+      if (b) s1 += w[(size_t)k1 * D + col];
+    }
+  }
+  red[0][slice][lane] = s0;
+  red[1][slice][lane] = s1;
+  __syncthreads();
+  if (slice != 0 || col >= D) return;
+#pragma unroll
+  for (int i = 1; i < kSlices; ++i) {
+    s0 += red[0][i][lane];
+    s1 += red[1][i][lane];
+  }
+  if (g) s0 *= g[col];
+  if (b) s0 = fmaf(b[col], s1, s0);
+  put_one(o, param ? 0u : (unsigned)q, col, s0, p.accumulate);
+}
+
+// Sums of the groups that a few neighbouring teams share: a warp has 128 columns of one group.
+// Groups are counted one by one, or where there are more of them than teams, by the teams that begin inside one.
+__global__ void __launch_bounds__(128) join_grad_groups_kernel(const __grid_constant__ JoinGrad p, const Teams teams, int groups,
+                                                               unsigned sums) {
+  const int lane = threadIdx.x & 31, c0 = blockIdx.x * 128 + lane, D = p.D, y = (int)blockIdx.y * 4 + (int)(threadIdx.x >> 5);
+  const int group = p.group > 0 ? p.group : p.M;
+  pdl_wait();
+  pdl_trigger();
+  int q = y;
+  if (groups >= teams.n) {
+    if (y + 1 >= teams.n) return;
+    const int b = team_start(teams, y + 1);
+    if (b % group == 0) return;
+    q = b / group;
+  }
+  if (q >= groups) return;
+  const int g0 = q * group, t0 = team_of(teams, g0), t1 = team_of(teams, g0 + min(group, p.M - g0) - 1);
+  if (t0 == t1 || (groups >= teams.n && t0 != y)) return;  // done there; another task's
   float s[4][4];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[k][i] = 0.f;
-  if (live) {
 #pragma unroll 2
-    for (int t = t0 + slice; t <= t1; t += slices) {
-      const float* o = param ? p.ws + (rowwise ? 0 : (size_t)teams.n * 8 * D) + (size_t)t * 4 * D
-                             : p.ws + ((size_t)t * 2 + (g0 > team_start(teams, t))) * 4 * D;
+  for (int t = t0; t <= t1; ++t) {
+    const float* w = p.ws + ((size_t)t * 2 + (g0 > team_start(teams, t))) * 4 * D;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (!(sums >> k & 1u)) continue;
+    for (int k = 0; k < 4; ++k) {
+      if (!(sums >> k & 1u)) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (c0 + 32 * i < D) s[k][i] += o[(size_t)k * D + c0 + 32 * i];
-      }
+      for (int i = 0; i < 4; ++i)
+        if (c0 + 32 * i < D) s[k][i] += w[(size_t)k * D + c0 + 32 * i];
     }
   }
-  if (slices > 1) {  // (uniform over the CTA)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < 4; ++k) red[k][warp][lane] = s[k][i];
-      __syncthreads();
-      if (slice == 0) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          for (int j = 1; j < slices; ++j) s[k][i] += red[k][j][lane];
-      }
-    }
-    if (slice != 0) return;
-  }
-  if (!live) return;
-  auto put = [&](const MatOut& o, int col, float v) {
-    if (!o.p) return;
-    const size_t at = row_offset(q, o.ld) + col;
-    if (o.dtype == LAZYMAR_F32) {
-      float* d = static_cast<float*>(o.p) + at;
-      *d = p.accumulate ? *d + v : v;
-    } else {
-      bf16* d = static_cast<bf16*>(o.p) + at;
-      *d = from_f<bf16>(p.accumulate ? to_f(*d) + v : v);
-    }
-  };
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int col = c0 + 32 * i;
     if (col >= D) continue;
-    if (param) {
-      float* const out[4] = {p.dpre_b, p.dpre_g, p.dpost_b, p.dpost_g};
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (out[k]) out[k][col] = p.accumulate ? out[k][col] + s[k][i] : s[k][i];
-      continue;
-    }
-    put(p.dshift, col, s[SUM_A][i]);
-    put(p.dscale, col, (p.pre_g ? p.pre_g[col] : 1.f) * s[SUM_B][i] + (p.pre_b ? p.pre_b[col] * s[SUM_A][i] : 0.f));
-    put(p.dgate, col, (p.post_g ? p.post_g[col] : 1.f) * s[SUM_Q][i] + (p.post_b ? p.post_b[col] * s[SUM_P][i] : 0.f));
+    if (p.dshift.p) put_one(p.dshift, q, col, s[SUM_A][i], p.accumulate);
+    if (p.dscale.p)
+      put_one(p.dscale, q, col, (p.pre_g ? p.pre_g[col] : 1.f) * s[SUM_B][i] + (p.pre_b ? p.pre_b[col] * s[SUM_A][i] : 0.f),
+              p.accumulate);
+    if (p.dgate.p)
+      put_one(p.dgate, q, col, (p.post_g ? p.post_g[col] : 1.f) * s[SUM_Q][i] + (p.post_b ? p.post_b[col] * s[SUM_P][i] : 0.f),
+              p.accumulate);
   }
 }
 
@@ -118,24 +136,17 @@ __global__ void __launch_bounds__(256) join_grad_empty_kernel(const JoinGrad p) 
   }
 }
 
-bool on_eight(const Rows& r) { return !r.p || r.vec; }
-bool on_eight(const MatOut& r) { return !r.p || r.vec; }
-
-// Warps of a row, and teams of a launch: those that live on every SM at once, as far as there are rows.
-int row_warps(int D) {
-  const int nc = (D + kChunk - 1) / kChunk;
-  return nc <= 1 ? 1 : nc <= 2 ? 2 : nc <= 4 ? 4 : nc <= 5 ? 5 : nc <= 8 ? 8 : 16;
-}
-Teams grad_teams(int M, int D) {
+// Teams of a launch: those that live on every SM at once, as far as there are rows.
+Teams grad_teams(int M, int D, int sm_warps) {
   const int wpr = row_warps(D);
-  return teams_of(M, kSMs * (wpr > 8 ? 1 : wpr == 5 ? 3 : 2 * (8 / wpr)));
+  return teams_of(M, kSMs * sm_ctas(wpr, sm_warps) * (cta_warps(wpr) / wpr));
 }
 
 }  // namespace
 
 size_t join_grad_workspace(int M, int D, int group) {
   if (M < 1 || D < 1 || D > kLnMaxWidth || group < 0) return 0;
-  return (size_t)grad_teams(M, D).n * (group == 1 ? 4 : 12) * D * sizeof(float);
+  return (size_t)grad_teams(M, D, grad_sm_warps(true, true)).n * (group == 1 ? 4 : 12) * D * sizeof(float);  // (the most)
 }
 
 cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
@@ -152,20 +163,27 @@ cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
   if (p.dpre_g) need.params |= 1u << SUM_B;
   if (p.dpost_b) need.params |= 1u << SUM_P;
   if (p.dpost_g) need.params |= 1u << SUM_Q;
-  const int wpr = row_warps(p.D), groups = p.group > 0 ? (p.M - 1) / p.group + 1 : 1;
-  const Teams teams = grad_teams(p.M, p.D);
+  const bool rowwise = p.group == 1;
+  const bool plain = p.pre && !p.post && !p.post_g && !p.post_b && !p.pre_g && !p.pre_b && !need.params;
+  const Teams teams = grad_teams(p.M, p.D, grad_sm_warps(plain, rowwise));
+  const int groups = p.group > 0 ? (p.M - 1) / p.group + 1 : 1;
   const bool whole = p.D % 8 == 0 && on_eight(p.dh) && on_eight(p.dz) && on_eight(p.z) && on_eight(p.y) &&
                      on_eight(p.gate) && on_eight(p.scale) && on_eight(p.dx) && on_eight(p.dy) && on_eight(p.dgate) &&
                      on_eight(p.dscale) && on_eight(p.dshift) && p.params_vec;
-  const cudaError_t e = p.group == 1 ? launch_join_grad_rowwise(c, p, need, whole, wpr, teams)
-                                     : join_grad_launch<false>(c, p, need, whole, wpr, teams);
+  cudaError_t e = rowwise ? (plain ? launch_join_grad_plain_rowwise(c, p, need, whole, teams)
+                                   : launch_join_grad_rowwise(c, p, need, whole, teams))
+                          : (plain ? launch_join_grad_plain(c, p, need, whole, teams)
+                                   : join_grad_launch<false, false>(c, p, need, whole, teams));
   if (e != cudaSuccess) return e;
-  const int divided = p.group == 1 || !need.mods || teams.n == 1 ? 0 : groups < teams.n ? groups : teams.n - 1;
-  if (!divided && !need.params) return cudaSuccess;
-  const int slices = teams.n / groups >= 32 ? kFinishWarps : 1, each = kFinishWarps / slices;
-  return launch_pdl(join_grad_finish_kernel,
-                    dim3((unsigned)((p.D + 127) / 128), (unsigned)((divided + each - 1) / each + (need.params ? 1 : 0))),
-                    dim3(32 * kFinishWarps), 0, c.stream, p, teams, groups, divided, p.group == 1, need, slices);
+  const unsigned columns = (unsigned)((p.D + 31) / 32);
+  const bool divided = !rowwise && need.mods && teams.n > 1, many = divided && teams.n / groups >= kSlices;
+  if (need.params || many)
+    e = launch_pdl(join_grad_sums_kernel, dim3(columns, (many ? 7u : 4u) - (need.params ? 0u : 4u), many ? (unsigned)groups : 1u),
+                   dim3(32 * kSlices), 0, c.stream, p, teams, rowwise, need.params ? 0 : 4);
+  if (e != cudaSuccess || !divided || many) return e;
+  const int tasks = groups < teams.n ? groups : teams.n - 1;
+  return launch_pdl(join_grad_groups_kernel, dim3((unsigned)((p.D + 127) / 128), (unsigned)((tasks + 3) / 4)), dim3(128), 0,
+                    c.stream, p, teams, groups, need.mods);
 }
 
 }  // namespace lm

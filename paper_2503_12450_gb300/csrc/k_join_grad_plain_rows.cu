@@ -1,0 +1,10 @@
+// The residual join's gradient without a norm of y and without parameters: a modulation for every row.
+#include "join_grad.cuh"
+
+namespace lm {
+
+cudaError_t launch_join_grad_plain_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams) {
+  return join_grad_launch<true, true>(c, p, need, whole, teams);
+}
+
+}  // namespace lm
