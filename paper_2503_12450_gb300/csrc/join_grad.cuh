@@ -27,7 +27,13 @@ struct JoinSums {
 
 // PLAIN: no norm of y, no parameters and none of their gradients (the modulated norm of a block).
 // Warps on an SM, by what a lane keeps: P is not needed then, and ROWWISE no sum at all.
-constexpr int grad_sm_warps(bool plain, bool rowwise) { return plain ? (rowwise ? 24 : 20) : 16; }
+#ifndef LM_GW
+#define LM_GW 16
+#endif
+#ifndef LM_RW
+#define LM_RW 20
+#endif
+constexpr int grad_sm_warps(bool plain, bool rowwise) { return plain ? (rowwise ? LM_RW : LM_GW) : 16; }
 
 namespace {
 
@@ -42,12 +48,12 @@ __device__ __forceinline__ float2 warp_sum2(float a, float b) {
   return upper ? make_float2(y, x) : make_float2(x, y);
 }
 // The same over the row's warps (`red`: one place for each).
-template <int WPR>
+template <int WPR, int GROUPS>
 __device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int grp, int part) {
   float2 s = warp_sum2(a, b);
   if constexpr (WPR > 1) {
     if ((threadIdx.x & 31) == 0) red[part] = s;
-    row_barrier<WPR>(grp);
+    row_barrier<WPR, GROUPS>(grp);
     s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < WPR; ++i) {
@@ -59,27 +65,27 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int gr
 }
 
 template <int NC, int WPR, bool WHOLE, bool ROWWISE, bool PLAIN>
-__global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warps(PLAIN, ROWWISE)))
+__global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) * 32, sm_ctas(WPR, grad_sm_warps(PLAIN, ROWWISE)))
     join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, const Teams teams, JoinSums need,
                      unsigned* err) {
-  constexpr int WARPS = cta_warps(WPR), GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
   extern __shared__ __align__(128) uint8_t ring_smem[];
   __shared__ uint64_t bars[WARPS][kMostStages];
   __shared__ float2 red[2][2][GROUPS][WPR];
   __shared__ int abort_word;
   volatile int* abort_flag = &abort_word;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = warp / WPR, part = warp % WPR;
+  const int warp = threadIdx.x >> 5, grp = warp / WPR, part = warp % WPR;
   const int D = p.D, c0 = part * NC * kChunk, team = (int)blockIdx.x * GROUPS + grp;
   if (threadIdx.x == 0) abort_word = 0;
   RowRing<WHOLE> ring;
-  ring.init(ring_smem + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(NC * kChunk, D - c0));
+  ring.init(ring_smem + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(NC * kChunk, D - c0), p.M, D);
   pdl_wait();
   pdl_trigger();
   __syncthreads();
   if (team >= teams.n) return;
   const int first = team_start(teams, team), end = team_start(teams, team + 1);
   for (int s = 0; s < plan.depth; ++s)
-    if (first + s < end) ring.fetch(plan, first + s, s, c0, p.M);
+    if (first + s < end) ring.fetch(plan, first + s, s, c0);
   const float per_D = 1.f / (float)D;
   const bool pre = PLAIN || p.pre != LAZYMAR_NORM_NONE, post = !PLAIN && p.post != LAZYMAR_NORM_NONE;
   const bool pre_layer = p.pre == LAZYMAR_NORM_LAYER, post_layer = p.post == LAZYMAR_NORM_LAYER;
@@ -87,14 +93,16 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warp
   const bool ab = !(PLAIN && ROWWISE) && (ROWWISE ? need.params & 3u : sums_of & 3u);
   const bool pq = !(PLAIN && ROWWISE) && (ROWWISE ? need.params >> 2 : sums_of >> 2);
 
-  // statistics and 8-bit scales (lanes: the warp's blocks, of z and then of y) of the next row
+  // statistics and 8-bit scales of the next row
   float next_ym = 0.f, next_yr = 1.f, next_zm = 0.f, next_zr = 1.f;
-  uint32_t next_s = 0;
-  const uint8_t* scales = nullptr;
-  if (lane < 4 * NC) {
-    const Rows& m = lane < 2 * NC ? p.z : p.y;
-    const int blk = c0 / kBlk + (lane & (2 * NC - 1));
-    if (m.p && m.dtype == LAZYMAR_E4M3 && blk * kBlk < D) scales = m.scale + (size_t)blk * m.lds;
+  uint32_t next_zs[NC], next_ys[NC];
+  const uint8_t* z_scales[NC];
+  const uint8_t* y_scales[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    next_zs[c] = next_ys[c] = 0;
+    z_scales[c] = scales_of<WHOLE>(p.z, c0 + c * kChunk, D);
+    y_scales[c] = scales_of<WHOLE>(p.y, c0 + c * kChunk, D);
   }
   auto statistics = [&](int row) {
     if (row >= end) return;
@@ -106,7 +114,11 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warp
       if (post_layer) next_ym = p.y_mean[row];
       next_yr = p.y_rstd[row];
     }
-    if (scales) next_s = scales[row];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (z_scales[c]) next_zs[c] = z_scales[c][row];
+      if (y_scales[c]) next_ys[c] = y_scales[c][row];
+    }
   };
   statistics(first);
 
@@ -218,23 +230,22 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warp
       }
     }
     const float ym = next_ym, yr = next_yr, zm = next_zm, zr = next_zr;
-    const uint32_t sb = next_s;
+    uint32_t zs[NC], ys[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      zs[c] = next_zs[c];
+      ys[c] = next_ys[c];
+    }
     statistics(row + 1);
     const bool ok = dead || ring.wait(abort_flag, err);
     dead |= !__all_sync(0xffffffffu, ok);
     float d[NC][8], n[NC][8], Z[NC][8], u[NC][8];
     int i = 0;
-    const auto from = [&](const Rows& m, int first_scale, float (&to)[NC][8]) {
+    const auto from = [&](const Rows& m, const uint32_t (&scales)[NC], float (&to)[NC][8]) {
       const uint8_t* st = ring.piece(plan, i, row, c0);
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        uint32_t s0 = 0, s1 = 0;
-        if (m.dtype == LAZYMAR_E4M3) {
-          s0 = __shfl_sync(0xffffffffu, sb, first_scale + 2 * c);
-          s1 = __shfl_sync(0xffffffffu, sb, first_scale + 2 * c + 1);
-        }
-        load_stage<WHOLE>(st + (uint32_t)c * kChunk * plan.t[i].e, m.dtype, s0, s1, Columns<WHOLE>(c0 + c * kChunk, D), to[c]);
-      }
+      for (int c = 0; c < NC; ++c)
+        load_stage<WHOLE>(st + (uint32_t)c * kChunk * plan.t[i].e, m.dtype, scales[c], Columns<WHOLE>(c0 + c * kChunk, D), to[c]);
       ++i;
     };
     const auto none = [&](float (&to)[NC][8]) {
@@ -244,14 +255,14 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warp
         for (int k = 0; k < 8; ++k) to[c][k] = 0.f;
     };
     if (pre) {
-      from(p.dh, 0, d);
-      from(p.z, 0, n);
+      from(p.dh, zs, d);
+      from(p.z, zs, n);
     }
     if (ROWWISE) {
       i = p.gate.p || p.scale.p ? plan.n - (p.gate.p != nullptr) - (p.scale.p != nullptr) : i;
-      if (p.gate.p) from(p.gate, 0, gate);
+      if (p.gate.p) from(p.gate, zs, gate);
       if (p.scale.p) {
-        from(p.scale, 0, scale);
+        from(p.scale, zs, scale);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -261,11 +272,11 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warp
     }
     // dz and y are read, and the stage given on, when they are needed: fewer registers
     auto rest = [&] {
-      if (p.dz.p) from(p.dz, 0, Z);
+      if (p.dz.p) from(p.dz, zs, Z);
       else none(Z);
-      if (p.y.p) from(p.y, 2 * NC, u);
+      if (p.y.p) from(p.y, ys, u);
       else none(u);
-      ring.next(plan, row + plan.depth, end, c0, p.M, dead);
+      ring.next(plan, row + plan.depth, end, c0, dead);
     };
     if (pre) {
       float s1 = 0.f, s2 = 0.f;
@@ -309,7 +320,7 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warp
         s1 += sum8(d[c]);
         s2 += dot8(d[c], n[c]);
       }
-      const float2 s = row_sum2<WPR>(s1, s2, red[it][0][grp], grp, part);
+      const float2 s = row_sum2<WPR, GROUPS>(s1, s2, red[it][0][grp], grp, part);
       s1 = pre_layer ? s.x * per_D : 0.f;
       s2 = -s.y * per_D;
       rest();
@@ -371,7 +382,7 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warp
     }
     if (!p.dy.p && !p.dy8.q) continue;
     if (post) {
-      const float2 s = row_sum2<WPR>(s3, s4, red[it][1][grp], grp, part);
+      const float2 s = row_sum2<WPR, GROUPS>(s3, s4, red[it][1][grp], grp, part);
       s3 = post_layer ? s.x * per_D : 0.f;
       s4 = -s.y * per_D;
 #pragma unroll
@@ -404,7 +415,7 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, grad_sm_warp
 
 template <int NC, int WPR, bool ROWWISE, bool PLAIN>
 cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams) {
-  constexpr int WARPS = cta_warps(WPR), GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
   RingPlan plan{};
   if (p.pre != LAZYMAR_NORM_NONE)
     for (const Rows* r : {&p.dh, &p.z}) add_stream(plan, *r, NC * kChunk);

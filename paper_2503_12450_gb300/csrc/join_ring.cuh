@@ -13,14 +13,20 @@ namespace {
 // A team of WPR warps works through consecutive rows, 256 columns a warp; its rows come by bulk
 // copies into the warps' rings, so that the memory system always has the next ones to
 // deliver while this one's sums are exchanged. Rows of a group follow each other, so
-// the modulation stays in registers while a group lasts; ROWWISE (every row has its own) it
+// the modulation stays in registers while a group lasts; STREAMED (every row has its own) it
 // comes with the row.
 // PLAIN: no norm of y and no parameters (the modulated norm of a block); fewer registers and
 // so more warps on an SM.
-constexpr int join_sm_warps(bool plain) { return plain ? 28 : 20; }
+#ifndef LM_SG
+#define LM_SG 16
+#endif
+#ifndef LM_JW
+#define LM_JW 20
+#endif
+constexpr int join_sm_warps(bool plain) { return plain ? LM_JW : 20; }
 
 // Mean and 1 / deviation of a row of 256 columns a warp, as above. n: the warp's columns, per_n and per_D: 1 / n, 1 / D.
-template <int WPR, bool WHOLE>
+template <int WPR, int GROUPS, bool WHOLE>
 __device__ __forceinline__ void ring_moments(const float (&v)[8], bool layer, const Columns<WHOLE>& c, float n, float per_n,
                                              float per_D, float eps, float4* red, int grp, int part, float& mean,
                                              float& rstd) {
@@ -40,7 +46,7 @@ __device__ __forceinline__ void ring_moments(const float (&v)[8], bool layer, co
   q = warp_sum(q);
   if constexpr (WPR > 1) {
     if ((threadIdx.x & 31) == 0) red[part] = make_float4(s, q, mean, n);
-    row_barrier<WPR>(grp);
+    row_barrier<WPR, GROUPS>(grp);
     q = s = 0.f;
 #pragma unroll
     for (int i = 0; i < WPR; ++i) {
@@ -61,12 +67,12 @@ __device__ __forceinline__ void ring_moments(const float (&v)[8], bool layer, co
   rstd = rsqrtf(fmaf(q, per_D, eps));
 }
 
-enum { X_STREAM = 0, Y_STREAM = 1 };  // then gate, scale, shift as they are there (ROWWISE)
+enum { X_STREAM = 0, Y_STREAM = 1 };  // then gate, scale, shift as they are there (STREAMED)
 
-template <int WPR, bool WHOLE, bool ROWWISE, bool PLAIN>
-__global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, join_sm_warps(PLAIN)))
+template <int WPR, bool WHOLE, bool STREAMED, bool PLAIN>
+__global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN)) * 32, sm_ctas(WPR, join_sm_warps(PLAIN)))
     join_ring_kernel(const __grid_constant__ Join p, const __grid_constant__ RingPlan plan, const Teams teams, unsigned* err) {
-  constexpr int WARPS = cta_warps(WPR), GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR, join_sm_warps(PLAIN)), GROUPS = WARPS / WPR;
   extern __shared__ __align__(128) uint8_t ring_smem[];
   __shared__ uint64_t bars[WARPS][kMostStages];
   __shared__ float4 red[2][2][GROUPS][WPR];
@@ -77,22 +83,20 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, join_sm_warp
   const Columns<WHOLE> cols(c0, D);
   if (threadIdx.x == 0) abort_word = 0;
   RowRing<WHOLE> ring;
-  ring.init(ring_smem + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(kChunk, D - c0));
+  ring.init(ring_smem + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(kChunk, D - c0), p.M, D);
   pdl_wait();
   pdl_trigger();
   __syncthreads();
   if (team >= teams.n) return;
   const int first = team_start(teams, team), end = team_start(teams, team + 1);
   for (int s = 0; s < plan.depth; ++s)
-    if (first + s < end) ring.fetch(plan, first + s, s, c0, p.M);
+    if (first + s < end) ring.fetch(plan, first + s, s, c0);
 
   const bool post = !PLAIN && p.post != LAZYMAR_NORM_NONE, pre = PLAIN || p.pre != LAZYMAR_NORM_NONE, leads = part == 0 && lane == 0;
   const float n = (float)min(max(D - c0, 0), kChunk), per_n = n > 0.f ? 1.f / n : 0.f, per_D = 1.f / (float)D;
   // scales of the next row's 8-bit y
   uint32_t next_s = 0;
-  const uint8_t* scales = nullptr;
-  if (p.y.p && p.y.dtype == LAZYMAR_E4M3 && lane < 2 && c0 + kBlk * lane < D)
-    scales = p.y.scale + (size_t)(c0 / kBlk + lane) * p.y.lds;
+  const uint8_t* const scales = scales_of<WHOLE>(p.y, c0, D);
   if (scales) next_s = scales[first];
   float gate[8], scale[8], shift[8];  // scale: 1 + scale
 #pragma unroll
@@ -100,10 +104,10 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, join_sm_warp
     gate[i] = scale[i] = 1.f;
     shift[i] = 0.f;
   }
-  int stop = first, it = 0;  // stop: the end of the group
-  bool dead = false;         // a wait ran out: the rows are not written any more
+  int it = 0, stop = first;  // stop: the end of the group
+  bool dead = false;  // a wait ran out: the rows are not written any more
   for (int row = first; row < end; ++row, it ^= 1) {
-    if (!ROWWISE && row == stop) {
+    if (!STREAMED && row == stop) {
       const int r = p.group > 0 ? row / p.group : 0;
       stop = p.group > 0 ? min(end - r * p.group, p.group) + r * p.group : end;
       if (p.gate.p) load_row<WHOLE>(p.gate, r, cols, gate);
@@ -120,18 +124,11 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, join_sm_warp
     dead |= !__all_sync(0xffffffffu, ok);
     float v[8], x[8];
     const auto from = [&](int i, int dtype, float (&to)[8]) {
-      load_stage<WHOLE>(ring.piece(plan, i, row, c0), dtype, 0, 0, cols, to);
+      load_stage<WHOLE>(ring.piece(plan, i, row, c0), dtype, 0, cols, to);
     };
     from(X_STREAM, p.x.dtype, x);
-    if (p.y.p) {
-      uint32_t s0 = 0, s1 = 0;
-      if (p.y.dtype == LAZYMAR_E4M3) {
-        s0 = __shfl_sync(0xffffffffu, s, 0);
-        s1 = __shfl_sync(0xffffffffu, s, 1);
-      }
-      load_stage<WHOLE>(ring.piece(plan, Y_STREAM, row, c0), p.y.dtype, s0, s1, cols, v);
-    }
-    if (ROWWISE) {
+    if (p.y.p) load_stage<WHOLE>(ring.piece(plan, Y_STREAM, row, c0), p.y.dtype, s, cols, v);
+    if (STREAMED) {
       int i = p.y.p ? Y_STREAM + 1 : Y_STREAM;
       if (p.gate.p) from(i++, p.gate.dtype, gate);
       if (p.scale.p) {
@@ -141,13 +138,13 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, join_sm_warp
       }
       if (p.shift.p) from(i++, p.shift.dtype, shift);
     }
-    ring.next(plan, row + plan.depth, end, c0, p.M, dead);
+    ring.next(plan, row + plan.depth, end, c0, dead);
     float t[8];
     if (p.y.p) {
       if (p.y8.q && !dead) store_row8<WHOLE>(p.y8, row, cols, v);
       if (post) {
         float mean, rstd;
-        ring_moments<WPR, WHOLE>(v, p.post == LAZYMAR_NORM_LAYER, cols, n, per_n, per_D, p.eps, red[it][0][grp], grp, part,
+        ring_moments<WPR, GROUPS, WHOLE>(v, p.post == LAZYMAR_NORM_LAYER, cols, n, per_n, per_D, p.eps, red[it][0][grp], grp, part,
                                  mean, rstd);
         if (leads && !dead) {
           if (p.y_mean) p.y_mean[row] = mean;
@@ -177,7 +174,7 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, join_sm_warp
     }
     if (!pre) continue;
     float mean, rstd;
-    ring_moments<WPR, WHOLE>(v, p.pre == LAZYMAR_NORM_LAYER, cols, n, per_n, per_D, p.eps, red[it][1][grp], grp, part, mean,
+    ring_moments<WPR, GROUPS, WHOLE>(v, p.pre == LAZYMAR_NORM_LAYER, cols, n, per_n, per_D, p.eps, red[it][1][grp], grp, part, mean,
                              rstd);
     if (leads && !dead) {
       if (p.z_mean) p.z_mean[row] = mean;
@@ -203,11 +200,12 @@ __global__ void __launch_bounds__(cta_warps(WPR) * 32, sm_ctas(WPR, join_sm_warp
 
 template <int WPR, bool PLAIN>
 cudaError_t join_ring_run(const Ctx& c, const Join& p, bool whole) {
-  constexpr int WARPS = cta_warps(WPR), GROUPS = WARPS / WPR, CTAS = sm_ctas(WPR, join_sm_warps(PLAIN));
+  constexpr int WARPS = cta_warps(WPR, join_sm_warps(PLAIN)), GROUPS = WARPS / WPR, CTAS = sm_ctas(WPR, join_sm_warps(PLAIN));
   RingPlan plan{};
   for (const Rows* r : {&p.x, &p.y}) add_stream(plan, *r, kChunk);
-  if (p.group == 1)
-    for (const Rows* r : {&p.gate, &p.scale, &p.shift}) add_stream(plan, *r, kChunk);
+  const bool streamed = p.group > 0 && p.group < LM_SG && (p.gate.p || p.scale.p || p.shift.p);
+  if (streamed)
+    for (const Rows* r : {&p.gate, &p.scale, &p.shift}) add_stream(plan, *r, kChunk, p.group);
   constexpr int kRoom = 200 * 1024 / CTAS;
   set_depth(plan, kRoom, WARPS);
   const Teams teams = teams_of(p.M, c.num_sms * CTAS * GROUPS);
@@ -218,7 +216,7 @@ cudaError_t join_ring_run(const Ctx& c, const Join& p, bool whole) {
     return launch_pdl(kernel, dim3((unsigned)((teams.n + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
                       (size_t)WARPS * plan.depth * plan.stage, c.stream, p, plan, teams, c.err);
   };
-  if (p.group == 1)
+  if (streamed)
     return whole ? run(join_ring_kernel<WPR, true, true, PLAIN>) : run(join_ring_kernel<WPR, false, true, PLAIN>);
   return whole ? run(join_ring_kernel<WPR, true, false, PLAIN>) : run(join_ring_kernel<WPR, false, false, PLAIN>);
 }

@@ -8,12 +8,19 @@
 namespace lm {
 
 // The tensors whose rows a warp's ring holds, as the host lays them out.
+// Row r of the call is row r / group of the tensor, for 0 <= r < 2^31 the upper bits of r * magic: with
+// 2^(l-1) < group <= 2^l and magic = floor(2^(31+l) / group) + 1 < 2^32, r * magic / 2^(31+l) exceeds r / group by
+// less than r / 2^(31+l) < 1 / group.
 struct RowStream {
   const uint8_t* p;
-  size_t pitch;   // bytes from row to row
-  uint32_t at;    // place in a stage
-  uint32_t e;     // bytes of an element
+  size_t pitch;    // bytes from row to row
+  uint32_t at;     // place in a stage
+  uint32_t e;      // bytes of an element
+  uint32_t magic, shift;
 };
+__device__ __forceinline__ unsigned stream_row(uint32_t magic, uint32_t shift, int row) {
+  return (unsigned)(((unsigned long long)(unsigned)row * magic) >> shift);
+}
 constexpr int kMostStreams = 6;
 constexpr int kMostStages = 8;
 struct RingPlan {
@@ -25,19 +32,26 @@ struct RingPlan {
 
 namespace {
 
-// Waits for the WPR warps of a row.
-template <int WPR>
+// Waits for the WPR warps of a row, one of GROUPS teams of the CTA. (With a number known at run time a CTA
+// would be given all 16 barriers, and an SM's 64 would limit it to four CTAs.)
+template <int WPR, int GROUPS>
 __device__ __forceinline__ void row_barrier(int grp) {
-  asm volatile("bar.sync %0, %1;" ::"r"(grp + 1), "n"(WPR * 32) : "memory");
+  static_assert(GROUPS <= 8, "a case for each team");
+#define LM_BAR(i) case i: asm volatile("bar.sync %0, %1;" ::"n"(i < GROUPS ? i : 0), "n"(WPR * 32) : "memory"); break;
+  switch (GROUPS == 1 ? 0 : grp) {
+    LM_BAR(0) LM_BAR(1) LM_BAR(2) LM_BAR(3) LM_BAR(4) LM_BAR(5) LM_BAR(6) LM_BAR(7)
+  }
+#undef LM_BAR
 }
 
 // ---------------------------------------------------------------------------
 // A lane's eight columns of a chunk of 256
 // ---------------------------------------------------------------------------
-// Whole rows (WHOLE: on boundaries of eight elements, D a multiple of eight): four
-// consecutive columns of each of the chunk's two blocks, accesses of four elements that
-// are contiguous over the warp and free of bank conflicts. Other rows: every 32nd column.
-// Either way values 0..3 are of the first block, 4..7 of the second.
+// Whole rows (WHOLE: on boundaries of eight elements, D a multiple of eight): eight
+// consecutive columns, all there or none, half a warp a block of 128: one access a tensor (fp32 from
+// shared memory two, with two-way bank conflicts) and one block's scale a lane. With four columns of each of
+// two blocks a lane, 40960 x 1024 with three 8-bit outputs took 539 instructions a warp and row. Other rows:
+// every 32nd column, values 0..3 of the first block, 4..7 of the second.
 template <bool WHOLE>
 struct Columns {
   int c0;     // first column of the chunk
@@ -45,11 +59,9 @@ struct Columns {
   bool full;  // all 256
 
   __device__ __forceinline__ Columns(int chunk, int D)
-      : c0(chunk), left(D - chunk - (WHOLE ? 4 : 1) * (int)(threadIdx.x & 31)), full(chunk + kChunk <= D) {}
-  __device__ __forceinline__ int first() const { return c0 + (WHOLE ? 4 : 1) * (int)(threadIdx.x & 31); }
-  // From the lane's first column to its k-th.
-  __device__ __forceinline__ static constexpr int offset(int k) { return WHOLE ? kBlk * (k >> 2) + (k & 3) : 32 * k; }
-  __device__ __forceinline__ bool on(int k) const { return offset(k) < left; }
+      : c0(chunk), left(D - chunk - (WHOLE ? 8 : 1) * (int)(threadIdx.x & 31)), full(chunk + kChunk <= D) {}
+  __device__ __forceinline__ int first() const { return c0 + (WHOLE ? 8 : 1) * (int)(threadIdx.x & 31); }
+  __device__ __forceinline__ bool on(int k) const { return (WHOLE ? 0 : 32 * k) < left; }
   __device__ __forceinline__ void mask(float (&v)[8]) const {
     if (full) return;  // (uniform over the warp)
 #pragma unroll
@@ -57,45 +69,27 @@ struct Columns {
       if (!on(k)) v[k] = 0.f;
   }
 };
-__device__ __forceinline__ void widen4(uint2 u, float* v) {
-  v[0] = __uint_as_float(u.x << 16);
-  v[1] = __uint_as_float(u.x & 0xFFFF0000u);
-  v[2] = __uint_as_float(u.y << 16);
-  v[3] = __uint_as_float(u.y & 0xFFFF0000u);
-}
-__device__ __forceinline__ void put4(float4 a, float* v) {
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-}
 __device__ __forceinline__ size_t row_offset(unsigned row, int ld) { return (size_t)row * (unsigned)ld; }
 
 // From global memory: a row of fp32 or bf16; columns from D on read as zero.
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void load_columns(const T* p, const Columns<WHOLE>& c, float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = 0.f;
+  if (WHOLE) {
+    if (c.on(0)) ld8a(p, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c.on(k)) v[k] = to_f(p[32 * k]);
+  }
+}
 template <bool WHOLE>
 __device__ __forceinline__ void load_row(const void* base, int ld, int dtype, unsigned row, const Columns<WHOLE>& c,
                                          float (&v)[8]) {
   const size_t at = row_offset(row, ld) + c.first();
-#pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = 0.f;
-  if (dtype == LAZYMAR_F32) {
-    const float* p = static_cast<const float*>(base) + at;
-    if (WHOLE) {
-      if (c.on(0)) put4(*reinterpret_cast<const float4*>(p), v);
-      if (c.on(4)) put4(*reinterpret_cast<const float4*>(p + kBlk), v + 4);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (c.on(k)) v[k] = p[32 * k];
-    }
-  } else {
-    const bf16* p = static_cast<const bf16*>(base) + at;
-    if (WHOLE) {
-      if (c.on(0)) widen4(*reinterpret_cast<const uint2*>(p), v);
-      if (c.on(4)) widen4(*reinterpret_cast<const uint2*>(p + kBlk), v + 4);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (c.on(k)) v[k] = to_f(p[32 * k]);
-    }
-  }
+  if (dtype == LAZYMAR_F32) load_columns<WHOLE>(static_cast<const float*>(base) + at, c, v);
+  else load_columns<WHOLE>(static_cast<const bf16*>(base) + at, c, v);
 }
 template <bool WHOLE>
 __device__ __forceinline__ void load_row(const Rows& m, unsigned row, const Columns<WHOLE>& c, float (&v)[8]) {
@@ -103,7 +97,7 @@ __device__ __forceinline__ void load_row(const Rows& m, unsigned row, const Colu
 }
 template <bool WHOLE>
 __device__ __forceinline__ void load_param(const float* p, const Columns<WHOLE>& c, float (&v)[8]) {
-  load_row<WHOLE>(p, 0, LAZYMAR_F32, 0u, c, v);
+  load_columns<WHOLE>(p + c.first(), c, v);
 }
 template <bool WHOLE>
 __device__ __forceinline__ void store_row(const MatOut& m, unsigned row, const Columns<WHOLE>& c, const float (&v)[8]) {
@@ -111,8 +105,7 @@ __device__ __forceinline__ void store_row(const MatOut& m, unsigned row, const C
   if (m.dtype == LAZYMAR_F32) {
     float* p = static_cast<float*>(m.p) + at;
     if (WHOLE) {
-      if (c.on(0)) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-      if (c.on(4)) *reinterpret_cast<float4*>(p + kBlk) = make_float4(v[4], v[5], v[6], v[7]);
+      if (c.on(0)) st8a(p, v);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
@@ -121,13 +114,12 @@ __device__ __forceinline__ void store_row(const MatOut& m, unsigned row, const C
   } else {
     bf16* p = static_cast<bf16*>(m.p) + at;
     if (WHOLE) {
-      if (c.on(0)) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-      if (c.on(4)) *reinterpret_cast<uint2*>(p + kBlk) = make_uint2(pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+      if (c.on(0)) st8a(p, v);
     } else {
+      uint16_t* q = reinterpret_cast<uint16_t*>(p);
 #pragma unroll
       for (int k = 0; k < 8; k += 2) {
         const uint32_t two = pack_bf16(v[k], v[k + 1]);
-        uint16_t* q = reinterpret_cast<uint16_t*>(p);
         if (c.on(k)) q[32 * k] = (uint16_t)two;
         if (c.on(k + 1)) q[32 * (k + 1)] = (uint16_t)(two >> 16);
       }
@@ -138,11 +130,21 @@ __device__ __forceinline__ void copy8(float (&y)[8], const float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = v[i];
 }
-// To block8: a block is four values of each lane of the warp. Columns from D on hold zero.
+// To block8. Columns from D on hold zero.
 template <bool WHOLE>
 __device__ __forceinline__ void store_row8(const lazymar_block8& o, unsigned row, const Columns<WHOLE>& c, const float (&v)[8]) {
   const int lane = threadIdx.x & 31;
   uint8_t* q = static_cast<uint8_t*>(o.q) + row_offset(row, o.ldq) + c.first();
+  if constexpr (WHOLE) {
+    uint2 w;
+    const uint32_t byte = block8_quantize(v, w);
+    if (c.on(0)) {
+      *reinterpret_cast<uint2*>(q) = w;
+      if ((lane & 15) == 0) o.scale[row_offset((unsigned)(c.c0 / kBlk + (lane >> 4)), o.lds) + row] = (uint8_t)byte;
+    }
+    return;
+  }
+  // a block is four values of each lane of the warp
   uint32_t amax[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j)
@@ -165,32 +167,26 @@ __device__ __forceinline__ void store_row8(const lazymar_block8& o, unsigned row
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const float s = block8_inv(block8_exp(amax[j]));
-    const unsigned long long ss = f32x2_pack(s, s);
-    f32x2_unpack(f32x2_mul(f32x2_pack(w[4 * j], w[4 * j + 1]), ss), w[4 * j], w[4 * j + 1]);
-    f32x2_unpack(f32x2_mul(f32x2_pack(w[4 * j + 2], w[4 * j + 3]), ss), w[4 * j + 2], w[4 * j + 3]);
-    const uint32_t b = e4m3x4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-    if (WHOLE) {
-      if (c.on(4 * j)) *reinterpret_cast<uint32_t*>(q + kBlk * j) = b;
-    } else {
+    const uint32_t b = e4m3x4(w[4 * j] * s, w[4 * j + 1] * s, w[4 * j + 2] * s, w[4 * j + 3] * s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c.on(4 * j + i)) q[32 * (4 * j + i)] = (uint8_t)(b >> (8 * i));
-    }
+    for (int i = 0; i < 4; ++i)
+      if (c.on(4 * j + i)) q[32 * (4 * j + i)] = (uint8_t)(b >> (8 * i));
   }
   // (lane 0 the first block's scale, lane 1 the second's)
   const uint32_t byte = block8_exp(lane == 0 ? amax[0] : amax[1]);
-  if (lane < 2 && c.c0 + kBlk * lane < c.left + c.first()) o.scale[(size_t)(unsigned)(c.c0 / kBlk + lane) * (unsigned)o.lds + row] = (uint8_t)byte;
+  if (lane < 2 && kBlk * lane - lane < c.left) o.scale[row_offset((unsigned)(c.c0 / kBlk + lane), o.lds) + row] = (uint8_t)byte;
 }
-// From a warp's stage. `st`: the row's chunk in it; s0, s1: the scales of an 8-bit row.
+// From a warp's stage. `st`: the row's chunk in it. An 8-bit row's scales: `s`, the lane's own block's where
+// rows are whole, otherwise lane 0 has the first block's and lane 1 the second's.
 template <bool WHOLE>
-__device__ __forceinline__ void load_stage(const uint8_t* st, int dtype, uint32_t s0, uint32_t s1, const Columns<WHOLE>& c,
-                                           float (&v)[8]) {
+__device__ __forceinline__ void load_stage(const uint8_t* st, int dtype, uint32_t s, const Columns<WHOLE>& c, float (&v)[8]) {
   const int lane = threadIdx.x & 31;
   if (dtype == LAZYMAR_F32) {
     if (WHOLE) {
-      const float4* p = reinterpret_cast<const float4*>(st) + lane;
-      put4(p[0], v);
-      put4(p[32], v + 4);
+      const float4* p = reinterpret_cast<const float4*>(st) + 2 * lane;
+      const float4 a = p[0], b = p[1];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     } else {
       const float* p = reinterpret_cast<const float*>(st) + lane;
 #pragma unroll
@@ -198,33 +194,33 @@ __device__ __forceinline__ void load_stage(const uint8_t* st, int dtype, uint32_
     }
   } else if (dtype == LAZYMAR_BF16) {
     if (WHOLE) {
-      const uint2* p = reinterpret_cast<const uint2*>(st) + lane;
-      widen4(p[0], v);
-      widen4(p[32], v + 4);
+      bf16x8(reinterpret_cast<const uint4*>(st)[lane], v);
     } else {
       const uint16_t* p = reinterpret_cast<const uint16_t*>(st) + lane;
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = __uint_as_float((uint32_t)p[32 * k] << 16);
     }
+  } else if (WHOLE) {
+    block8_values(reinterpret_cast<const uint2*>(st)[lane], block8_scale(s), v);
   } else {
-    const float s[2] = {block8_scale(s0), block8_scale(s1)};
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      uint32_t w;
-      if (WHOLE) {
-        w = reinterpret_cast<const uint32_t*>(st)[32 * j + lane];
-      } else {
-        w = 0;
+      const float t = block8_scale(__shfl_sync(0xffffffffu, s, j));
+      uint32_t w = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w |= (uint32_t)st[kBlk * j + 32 * i + lane] << (8 * i);
-      }
+      for (int i = 0; i < 4; ++i) w |= (uint32_t)st[kBlk * j + 32 * i + lane] << (8 * i);
       const float2 a = e4m3x2_to_f2(w & 0xFFFFu), b = e4m3x2_to_f2(w >> 16);
-      const unsigned long long ss = f32x2_pack(s[j], s[j]);
-      f32x2_unpack(f32x2_mul(f32x2_pack(a.x, a.y), ss), v[4 * j], v[4 * j + 1]);
-      f32x2_unpack(f32x2_mul(f32x2_pack(b.x, b.y), ss), v[4 * j + 2], v[4 * j + 3]);
+      v[4 * j] = a.x * t; v[4 * j + 1] = a.y * t; v[4 * j + 2] = b.x * t; v[4 * j + 3] = b.y * t;
     }
   }
   c.mask(v);
+}
+// Where a lane finds the scales of its chunk of an 8-bit tensor (row by row), as load_stage takes them.
+template <bool WHOLE>
+__device__ __forceinline__ const uint8_t* scales_of(const Rows& m, int c0, int D) {
+  const int lane = threadIdx.x & 31, j = WHOLE ? lane >> 4 : lane;
+  if (!m.p || m.dtype != LAZYMAR_E4M3 || j > 1 || c0 + kBlk * j >= D) return nullptr;
+  return m.scale + row_offset((unsigned)(c0 / kBlk + j), m.lds);
 }
 
 // y = v a + b; paired
@@ -252,9 +248,9 @@ __device__ __forceinline__ float dot8(const float (&v)[8], const float (&a)[8]) 
 
 // ---------------------------------------------------------------------------
 // A warp's ring of row pieces: its columns of every tensor, `depth` rows ahead, by bulk
-// copies, one lane a tensor. Rows that are not on a 16-byte boundary are copied from the
-// boundary before to the one behind, which are the row's neighbours' bytes; the first and the
-// last row, whose neighbours are not the tensor's, come element by element.
+// copies, one lane a tensor. Pieces that are not on 16-byte boundaries are copied from the
+// boundary before to the one behind, which are the row's neighbours' bytes; where those are not the
+// tensor's (before its first element, behind its last), the piece comes element by element.
 // ---------------------------------------------------------------------------
 template <bool WHOLE>
 struct RowRing {
@@ -265,9 +261,11 @@ struct RowRing {
   // this lane's tensor: the piece of row 0, bytes from row to row and of a row, its place in a stage
   uintptr_t src;
   size_t pitch;
-  uint32_t bytes, at, total;
+  uint32_t bytes, at, total, magic, shift;
+  unsigned last;           // its last row if this piece ends with the tensor's columns, otherwise none
+  bool starts;             // whether the piece starts with its columns
 
-  __device__ __forceinline__ void init(uint8_t* smem, uint64_t* b, const RingPlan& plan, int first_column, int columns) {
+  __device__ __forceinline__ void init(uint8_t* smem, uint64_t* b, const RingPlan& plan, int first_column, int columns, int M, int D) {
     const int lane = threadIdx.x & 31;
     base = smem;
     bars = b;
@@ -282,8 +280,12 @@ struct RowRing {
       const RowStream& t = plan.t[lane];
       src = reinterpret_cast<uintptr_t>(t.p) + (size_t)first_column * t.e;
       pitch = t.pitch;
+      magic = t.magic;
+      shift = t.shift;
       bytes = (uint32_t)max(mine, 0) * t.e;
       at = t.at;
+      last = first_column + columns == D ? stream_row(magic, shift, M - 1) : 0xFFFFFFFFu;
+      starts = first_column == 0;
     }
     if (WHOLE) {
       bytes = (bytes + 15u) & ~15u;
@@ -294,14 +296,19 @@ struct RowRing {
     fence_mbar_init();
   }
   // Row `row` into stage s. All lanes call it.
-  __device__ __forceinline__ void fetch(const RingPlan& plan, int row, int s, int first_column, int M) {
+  __device__ __forceinline__ void fetch(const RingPlan& plan, int row, int s, int first_column) {
     if (mine <= 0) return;
     const int lane = threadIdx.x & 31;
     uint8_t* dst = base + (uint32_t)s * stage;
-    if (!WHOLE && (row == 0 || row == M - 1)) {
-      for (int i = 0; i < plan.n; ++i) {
-        const RowStream& t = plan.t[i];
-        const uint8_t* from = t.p + (size_t)row * t.pitch + (size_t)first_column * t.e;
+    const unsigned r = stream_row(magic, shift, row);
+    uintptr_t p = src + (size_t)r * pitch;
+    uint32_t n = bytes, sum = total;
+    bool copies = lane < streams;
+    if (!WHOLE) {
+      const bool outside = copies && ((starts && r == 0 && ((uint32_t)p & 15u)) || (r == last && ((uint32_t)p + bytes & 15u)));
+      for (unsigned them = __ballot_sync(0xffffffffu, outside); them; them &= them - 1) {
+        const RowStream& t = plan.t[__ffs((int)them) - 1];
+        const uint8_t* from = t.p + (size_t)stream_row(t.magic, t.shift, row) * t.pitch + (size_t)first_column * t.e;
         uint8_t* to = dst + t.at + (reinterpret_cast<uintptr_t>(from) & 15u);
         for (int c = lane; c < mine; c += 32) {
           if (t.e == 4) reinterpret_cast<float*>(to)[c] = reinterpret_cast<const float*>(from)[c];
@@ -309,20 +316,15 @@ struct RowRing {
           else to[c] = from[c];
         }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars[s]);
-      return;
-    }
-    uintptr_t p = src + (size_t)(unsigned)row * pitch;
-    uint32_t n = bytes, sum = total;
-    if (!WHOLE) {
-      n = lane < streams ? (((uint32_t)p & 15u) + bytes + 15u) & ~15u : 0u;
+      copies = copies && !outside;
+      n = copies ? (((uint32_t)p & 15u) + bytes + 15u) & ~15u : 0u;
       p &= ~(uintptr_t)15;
       sum = __reduce_add_sync(0xffffffffu, n);
+      __syncwarp();
     }
     if (lane == 0) mbar_arrive_expect_tx(&bars[s], sum);
     __syncwarp();
-    if (lane < streams) bulk_load(dst + at, reinterpret_cast<const void*>(p), n, &bars[s]);
+    if (copies) bulk_load(dst + at, reinterpret_cast<const void*>(p), n, &bars[s]);
   }
   __device__ __forceinline__ bool wait(volatile int* abort_flag, unsigned* err) {
     return mine <= 0 || mbar_wait(&bars[slot], phase, abort_flag, err);
@@ -332,14 +334,15 @@ struct RowRing {
     const RowStream& t = plan.t[i];
     const uint8_t* st = base + (uint32_t)slot * stage + t.at;
     if (WHOLE) return st;
-    return st + (((uint32_t)reinterpret_cast<uintptr_t>(t.p) + (uint32_t)first_column * t.e + (uint32_t)row * (uint32_t)t.pitch) & 15u);
+    return st + (((uint32_t)reinterpret_cast<uintptr_t>(t.p) + (uint32_t)first_column * t.e +
+                  stream_row(t.magic, t.shift, row) * (uint32_t)t.pitch) & 15u);
   }
   // The row has been read by every lane: its stage takes row `ahead`, if there is one.
-  __device__ __forceinline__ void next(const RingPlan& plan, int ahead, int end, int first_column, int M, bool dead) {
+  __device__ __forceinline__ void next(const RingPlan& plan, int ahead, int end, int first_column, bool dead) {
     __syncwarp();
     if (!dead && ahead < end) {
       fence_proxy_async_smem();
-      fetch(plan, ahead, slot, first_column, M);
+      fetch(plan, ahead, slot, first_column);
     }
     if (++slot == depth) {
       slot = 0;
@@ -354,10 +357,13 @@ inline bool on_eight(const Rows& r) { return !r.p || r.vec; }
 inline bool on_eight(const MatOut& r) { return !r.p || r.vec; }
 
 // The streams of a launch; stages for as many rows as `room` bytes hold for a CTA's warps, four at most.
-inline void add_stream(RingPlan& plan, const Rows& r, int columns) {
+inline void add_stream(RingPlan& plan, const Rows& r, int columns, int group = 1) {
   if (!r.p) return;
   const uint32_t e = r.dtype == LAZYMAR_F32 ? 4 : r.dtype == LAZYMAR_BF16 ? 2 : 1;
-  plan.t[plan.n++] = RowStream{static_cast<const uint8_t*>(r.p), (size_t)r.ld * e, plan.stage, e};
+  int l = 0;
+  while (l < 31 && (1u << l) < (unsigned)group) ++l;
+  plan.t[plan.n++] = RowStream{static_cast<const uint8_t*>(r.p), (size_t)r.ld * e, plan.stage, e,
+                               (uint32_t)((1ull << (31 + l)) / (unsigned)group + 1), (uint32_t)(31 + l)};
   plan.stage += (uint32_t)columns * e + 32;
 }
 inline void set_depth(RingPlan& plan, int room, int warps) {
@@ -365,15 +371,15 @@ inline void set_depth(RingPlan& plan, int room, int warps) {
   if (plan.depth > 4) plan.depth = 4;
 }
 
-// Warps of a row of D columns, warps of a CTA (whole teams, and a multiple of four, so that the SM's four
-// schedulers have as many each: with CTAs of five warps 40960 x 1280 took 200 us instead of 154), and CTAs
-// on an SM for about `warps` warps there.
+// Warps of a row of D columns; warps of a CTA (whole teams) and CTAs on an SM for about `warps` warps
+// there. Teams of three and five warps fill one CTA, so that the SM's four schedulers have as many
+// warps each: with CTAs of one team of five 40960 x 1280 took 200 us instead of 154.
 inline int row_warps(int D) {
   const int nc = (D + kChunk - 1) / kChunk;
   return nc <= 5 ? nc : nc <= 8 ? 8 : 16;
 }
-constexpr int cta_warps(int wpr) { return wpr <= 2 ? 4 : wpr % 4 ? 4 * wpr : wpr; }
-constexpr int sm_ctas(int wpr, int warps) { return warps / cta_warps(wpr) > 0 ? warps / cta_warps(wpr) : 1; }
+constexpr int cta_warps(int wpr, int warps) { return wpr <= 2 ? 4 : wpr % 4 ? warps / wpr * wpr : wpr; }
+constexpr int sm_ctas(int wpr, int warps) { return warps / cta_warps(wpr, warps) > 0 ? warps / cta_warps(wpr, warps) : 1; }
 
 // Ranges of consecutive rows, one for each team (the warps that work on a row together).
 struct Teams {

@@ -72,7 +72,7 @@ __device__ __forceinline__ void widen8(const Rows& m, const Raw& r, float* sm, f
 // warp, columns that do not exist zero. Each warp takes the squares about its own mean,
 // and the warps' sums are joined about the row's: one exchange between the warps, and
 // no cancellation. RMS: the mean counts as 0.
-template <int NC, int WPR, bool FULL>
+template <int NC, int WPR, int GROUPS, bool FULL>
 __device__ __forceinline__ void moments(const float (&v)[NC][8], bool layer, int D, int c0, float eps, float2* red, int grp,
                                         int part, float& mean, float& rstd) {
   const int lane = threadIdx.x & 31;
@@ -98,7 +98,7 @@ __device__ __forceinline__ void moments(const float (&v)[NC][8], bool layer, int
   mean = m;
   if constexpr (WPR > 1) {
     if (lane == 0) red[part] = make_float2(m, q);
-    row_barrier<WPR>(grp);
+    row_barrier<WPR, GROUPS>(grp);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < WPR; ++i) s += red[i].x * columns(i);
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kWarps<WPR> * 32, NC == 1 ? 3 : 2) join_kernel
     }
     float mean = 0.f, rstd = 1.f;
     if (p.post != LAZYMAR_NORM_NONE) {
-      moments<NC, WPR, FULL>(v, p.post == LAZYMAR_NORM_LAYER, D, c0, p.eps, red[0][grp], grp, part, mean, rstd);
+      moments<NC, WPR, GROUPS, FULL>(v, p.post == LAZYMAR_NORM_LAYER, D, c0, p.eps, red[0][grp], grp, part, mean, rstd);
       if (part == 0 && lane == 0) {
         if (p.y_mean) p.y_mean[row] = mean;
         if (p.y_rstd) p.y_rstd[row] = rstd;
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kWarps<WPR> * 32, NC == 1 ? 3 : 2) join_kernel
   }
   if (p.pre == LAZYMAR_NORM_NONE) return;
   float mean, rstd;
-  moments<NC, WPR, FULL>(v, p.pre == LAZYMAR_NORM_LAYER, D, c0, p.eps, red[1][grp], grp, part, mean, rstd);
+  moments<NC, WPR, GROUPS, FULL>(v, p.pre == LAZYMAR_NORM_LAYER, D, c0, p.eps, red[1][grp], grp, part, mean, rstd);
   if (part == 0 && lane == 0) {
     if (p.z_mean) p.z_mean[row] = mean;
     if (p.z_rstd) p.z_rstd[row] = rstd;

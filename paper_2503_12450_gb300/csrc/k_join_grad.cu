@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(256) join_grad_empty_kernel(const JoinGrad p) 
 // Teams of a launch: those that live on every SM at once, as far as there are rows.
 Teams grad_teams(int M, int D, int sm_warps) {
   const int wpr = row_warps(D);
-  return teams_of(M, kSMs * sm_ctas(wpr, sm_warps) * (cta_warps(wpr) / wpr));
+  return teams_of(M, kSMs * sm_ctas(wpr, sm_warps) * (cta_warps(wpr, sm_warps) / wpr));
 }
 
 }  // namespace
