@@ -27,13 +27,9 @@ struct JoinSums {
 
 // PLAIN: no norm of y, no parameters and none of their gradients (the modulated norm of a block).
 // Warps on an SM, by what a lane keeps: P is not needed then, and ROWWISE no sum at all.
-#ifndef LM_GW
-#define LM_GW 16
-#endif
-#ifndef LM_RW
-#define LM_RW 20
-#endif
-constexpr int grad_sm_warps(bool plain, bool rowwise) { return plain ? (rowwise ? LM_RW : LM_GW) : 16; }
+// (40960 x 1280 with 320 rows a group: 20 warps 155 us, 16 165; from 20 warps on the other forms spill.)
+constexpr int grad_sm_warps(bool plain, bool rowwise) { return plain ? (rowwise ? 24 : 20) : 16; }
+constexpr int kMostGradWarps = 24;
 
 namespace {
 
@@ -65,11 +61,13 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int gr
 }
 
 template <int NC, int WPR, bool WHOLE, bool ROWWISE, bool PLAIN>
-__global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) * 32, sm_ctas(WPR, grad_sm_warps(PLAIN, ROWWISE)))
+__global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) * 32, 1)
     join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, const Teams teams, JoinSums need,
                      unsigned* err) {
   constexpr int WARPS = cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
-  extern __shared__ __align__(128) uint8_t ring_smem[];
+  // the four parameters (NC 1; of wider rows they stay where they are), each warp's modulation (gate, 1 + scale), the rings
+  constexpr int W = NC * WPR * kChunk, PARAMS = PLAIN || NC > 1 ? 0 : 4 * W, MODS = ROWWISE ? 0 : 2 * NC * kLaneChunk;
+  extern __shared__ __align__(128) float row_smem[];
   __shared__ uint64_t bars[WARPS][kMostStages];
   __shared__ float2 red[2][2][GROUPS][WPR];
   __shared__ int abort_word;
@@ -77,13 +75,31 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
   const int warp = threadIdx.x >> 5, grp = warp / WPR, part = warp % WPR;
   const int D = p.D, c0 = part * NC * kChunk, team = (int)blockIdx.x * GROUPS + grp;
   if (threadIdx.x == 0) abort_word = 0;
-  RowRing<WHOLE> ring;
-  ring.init(ring_smem + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(NC * kChunk, D - c0), p.M, D);
+  const bool live = team < teams.n;
+  const int first = live ? team_start(teams, team) : 0, end = live ? team_start(teams, team + 1) : 0;
+  RowRing<WHOLE, false> ring;
+  float* const params = row_smem + part * kLaneChunk;
+  float* const mods = row_smem + PARAMS + warp * MODS;
+  uint8_t* const rings = reinterpret_cast<uint8_t*>(row_smem + PARAMS + WARPS * MODS);
+  ring.init(rings + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(NC * kChunk, D - c0), p.M, D, first);
   pdl_wait();
   pdl_trigger();
+  if (PARAMS > 0 && grp == 0) {
+    const float* const given[4] = {p.post_g, p.post_b, p.pre_g, p.pre_b};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (!given[k]) continue;
+      float t[8];
+      load_param<WHOLE>(given[k], Columns<WHOLE>(c0, D), t);
+      lane_put(params + k * W, t);
+    }
+  }
   __syncthreads();
-  if (team >= teams.n) return;
-  const int first = team_start(teams, team), end = team_start(teams, team + 1);
+  // parameter k (post_g, post_b, pre_g, pre_b) of chunk c
+  const auto parameter = [&](int k, const float* at, int c, float (&t)[8]) {
+    if (PARAMS > 0) lane_get(params + k * W, t);
+    else load_param<WHOLE>(at, Columns<WHOLE>(c0 + c * kChunk, D), t);
+  };
   for (int s = 0; s < plan.depth; ++s)
     if (first + s < end) ring.fetch(plan, first + s, s, c0);
   const float per_D = 1.f / (float)D;
@@ -120,16 +136,13 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
       if (y_scales[c]) next_ys[c] = y_scales[c][row];
     }
   };
-  statistics(first);
+  if (live) statistics(first);
 
-  float sums[4][NC][8], gate[NC][8], scale[NC][8];  // scale: 1 + scale
+  float sums[4][NC][8];
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sums[0][c][i] = sums[1][c][i] = sums[2][c][i] = sums[3][c][i] = 0.f;
-      gate[c][i] = scale[c][i] = 1.f;
-    }
+    for (int i = 0; i < 8; ++i) sums[0][c][i] = sums[1][c][i] = sums[2][c][i] = sums[3][c][i] = 0.f;
   bool dead = false;  // a wait ran out: nothing is written any more
   // out (+)= v for a row of a modulation's gradient
   auto put = [&](const MatOut& o, unsigned r, const Columns<WHOLE>& cc, float (&v)[8]) {
@@ -144,13 +157,11 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
     if (!dead) store_row<WHOLE>(MatOut{o, 0, LAZYMAR_F32, true}, 0u, cc, v);
   };
   float* const slots = p.ws + (size_t)team * 8 * D;
-  float* const param = p.ws + (ROWWISE ? 0 : (size_t)teams.n * 8 * D) + (size_t)team * 4 * D;
+  float* const param = p.ws + (size_t)teams.n * 8 * D + (size_t)team * 4 * D;
 
   // The end of a group, or of its part in this range: rows start .. stop.
   auto flush = [&](int start, int stop) {
-    const int q = p.group > 0 ? start / p.group : 0;
-    const int g0 = p.group > 0 ? q * p.group : 0;
-    const int g1 = p.group > 0 ? g0 + min(p.group, p.M - g0) : p.M;
+    const int q = start / p.group, g0 = q * p.group, g1 = g0 + min(p.group, p.M - g0);
     const bool whole = start == g0 && stop == g1;
     float* slot = slots + (size_t)(start > first) * 4 * D;
 #pragma unroll
@@ -162,7 +173,10 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
       for (int k = 0; k < 4; ++k) {
         if (PLAIN || !(need.params >> k & 1u)) continue;
         copy8(v, sums[k][c]);
-        mul8(v, k < 2 ? scale[c] : gate[c]);
+        if (k < 2 ? p.scale.p : p.gate.p) {
+          lane_get(mods + (k < 2 ? NC + c : c) * kLaneChunk, t);
+          mul8(v, t);
+        }
         if (start > first) {
           load_param<WHOLE>(param + (size_t)k * D, cc, t);
           add8(v, t);
@@ -177,11 +191,11 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
         if (p.dscale.p) {
           copy8(v, sums[SUM_B][c]);
           if (!PLAIN && p.pre_g) {
-            load_param<WHOLE>(p.pre_g, cc, t);
+            parameter(2, p.pre_g, c, t);
             mul8(v, t);
           }
           if (!PLAIN && p.pre_b) {
-            load_param<WHOLE>(p.pre_b, cc, t);
+            parameter(3, p.pre_b, c, t);
             acc8(v, t, sums[SUM_A][c]);
           }
           put(p.dscale, q, cc, v);
@@ -189,11 +203,11 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
         if (p.dgate.p) {
           copy8(v, sums[SUM_Q][c]);
           if (!PLAIN && p.post_g) {
-            load_param<WHOLE>(p.post_g, cc, t);
+            parameter(0, p.post_g, c, t);
             mul8(v, t);
           }
           if (!PLAIN && p.post_b) {
-            load_param<WHOLE>(p.post_b, cc, t);
+            parameter(1, p.post_b, c, t);
             acc8(v, t, sums[SUM_P][c]);
           }
           put(p.dgate, q, cc, v);
@@ -221,11 +235,16 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const Columns<WHOLE> cc(c0 + c * kChunk, D);
-        if (p.gate.p) load_row<WHOLE>(p.gate, r, cc, gate[c]);
+        float t[8];
+        if (p.gate.p) {
+          load_row<WHOLE>(p.gate, r, cc, t);
+          lane_put(mods + c * kLaneChunk, t);
+        }
         if (p.scale.p) {
-          load_row<WHOLE>(p.scale, r, cc, scale[c]);
+          load_row<WHOLE>(p.scale, r, cc, t);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) scale[c][i] += 1.f;
+          for (int i = 0; i < 8; ++i) t[i] += 1.f;
+          lane_put(mods + (NC + c) * kLaneChunk, t);
         }
       }
     }
@@ -258,26 +277,17 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
       from(p.dh, zs, d);
       from(p.z, zs, n);
     }
-    if (ROWWISE) {
-      i = p.gate.p || p.scale.p ? plan.n - (p.gate.p != nullptr) - (p.scale.p != nullptr) : i;
-      if (p.gate.p) from(p.gate, zs, gate);
-      if (p.scale.p) {
-        from(p.scale, zs, scale);
+    float mod[NC][8];  // ROWWISE: 1 + scale, then gate
+    if (ROWWISE && p.scale.p) {
+      i = plan.n - 1;
+      from(p.scale, zs, mod);
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) scale[c][k] += 1.f;
-      }
+        for (int k = 0; k < 8; ++k) mod[c][k] += 1.f;
       i = pre ? 2 : 0;
     }
-    // dz and y are read, and the stage given on, when they are needed: fewer registers
-    auto rest = [&] {
-      if (p.dz.p) from(p.dz, zs, Z);
-      else none(Z);
-      if (p.y.p) from(p.y, ys, u);
-      else none(u);
-      ring.next(plan, row + plan.depth, end, c0, dead);
-    };
+    // (dz and y are read when they are needed: fewer registers)
     if (pre) {
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -292,11 +302,11 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
             float v[8];
             copy8(v, n[c]);
             if (!PLAIN && p.pre_g) {
-              load_param<WHOLE>(p.pre_g, cc, t);
+              parameter(2, p.pre_g, c, t);
               mul8(v, t);
             }
             if (!PLAIN && p.pre_b) {
-              load_param<WHOLE>(p.pre_b, cc, t);
+              parameter(3, p.pre_b, c, t);
               add8(v, t);
             }
             mul8(v, d[c]);
@@ -306,15 +316,18 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
             copy8(t, d[c]);
             put(p.dshift, row, cc, t);
           }
-          mul8(d[c], scale[c]);
+          if (p.scale.p) mul8(d[c], mod[c]);
         }
         if (ab) {
           add8(sums[SUM_A][c], d[c]);
           acc8(sums[SUM_B][c], d[c], n[c]);
         }
-        if (!ROWWISE) mul8(d[c], scale[c]);
+        if (!ROWWISE && p.scale.p) {
+          lane_get(mods + (NC + c) * kLaneChunk, t);
+          mul8(d[c], t);
+        }
         if (!PLAIN && p.pre_g) {
-          load_param<WHOLE>(p.pre_g, cc, t);
+          parameter(2, p.pre_g, c, t);
           mul8(d[c], t);
         }
         s1 += sum8(d[c]);
@@ -323,7 +336,8 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
       const float2 s = row_sum2<WPR, GROUPS>(s1, s2, red[it][0][grp], grp, part);
       s1 = pre_layer ? s.x * per_D : 0.f;
       s2 = -s.y * per_D;
-      rest();
+      if (p.dz.p) from(p.dz, zs, Z);
+      else none(Z);
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const float m2[8] = {s2, s2, s2, s2, s2, s2, s2, s2}, r[8] = {zr, zr, zr, zr, zr, zr, zr, zr};
@@ -333,8 +347,12 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
         Columns<WHOLE>(c0 + c * kChunk, D).mask(Z[c]);
       }
     } else {
-      rest();
+      from(p.dz, zs, Z);
     }
+    if (p.y.p) from(p.y, ys, u);
+    else none(u);
+    if (ROWWISE && p.gate.p) from(p.gate, zs, mod);
+    ring.next(plan, row + plan.depth, end, c0, dead);
     float s3 = 0.f, s4 = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -354,25 +372,28 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
           float v[8];
           copy8(v, u[c]);
           if (!PLAIN && p.post_g) {
-            load_param<WHOLE>(p.post_g, cc, t);
+            parameter(0, p.post_g, c, t);
             mul8(v, t);
           }
           if (!PLAIN && p.post_b) {
-            load_param<WHOLE>(p.post_b, cc, t);
+            parameter(1, p.post_b, c, t);
             add8(v, t);
           }
           mul8(v, Z[c]);
           put(p.dgate, row, cc, v);
         }
-        mul8(Z[c], gate[c]);
+        if (p.gate.p) mul8(Z[c], mod[c]);
       }
       if (pq) {
         if (!PLAIN) add8(sums[SUM_P][c], Z[c]);
         acc8(sums[SUM_Q][c], Z[c], u[c]);
       }
-      if (!ROWWISE) mul8(Z[c], gate[c]);
+      if (!ROWWISE && p.gate.p) {
+        lane_get(mods + c * kLaneChunk, t);
+        mul8(Z[c], t);
+      }
       if (!PLAIN && p.post_g) {
-        load_param<WHOLE>(p.post_g, cc, t);
+        parameter(0, p.post_g, c, t);
         mul8(Z[c], t);
       }
       if (post) {
@@ -402,14 +423,30 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
       if (p.dy8.q) store_row8<WHOLE>(p.dy8, row, cc, Z[c]);
     }
   }
-  if (!ROWWISE) {
-    flush(start, stop);
-  } else if (!PLAIN) {
+  if (!ROWWISE && p.group > 0) {
+    if (live) flush(start, stop);
+    return;
+  }
+  // One group, or none: the teams' sums in turn, through shared memory, to the CTA's place.
+  const unsigned of = ROWWISE ? need.params : need.mods | need.params;
+  if ((PLAIN && ROWWISE) || !of) return;
+  float* const mem = reinterpret_cast<float*>(rings);  // [4][GROUPS][W]
+  __syncthreads();  // (the rings are done with)
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (need.params >> k & 1u)
+  for (int k = 0; k < 4; ++k) {
+    if ((PLAIN && k == SUM_P) || !(of >> k & 1u)) continue;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) put_sum(param + (size_t)k * D, Columns<WHOLE>(c0 + c * kChunk, D), sums[k][c]);
+    for (int c = 0; c < NC; ++c) lane_put(mem + (k * GROUPS + grp) * W + (part * NC + c) * kLaneChunk, sums[k][c]);
+  }
+  __syncthreads();
+  if (*abort_flag) return;
+  for (int i = threadIdx.x; i < 4 * W; i += WARPS * 32) {
+    const int k = i / W, at = i % W, col = at / kLaneChunk * kChunk + lane_column<WHOLE>(at % kLaneChunk);
+    if (col >= D || !(of >> k & 1u)) continue;
+    float s = 0.f;
+#pragma unroll 4
+    for (int j = 0; j < GROUPS; ++j) s += mem[(k * GROUPS + j) * W + at];
+    p.ws[((size_t)blockIdx.x * 4 + k) * D + col] = s;
   }
 }
 
@@ -422,14 +459,16 @@ cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need,
   for (const Rows* r : {&p.dz, &p.y}) add_stream(plan, *r, NC * kChunk);
   if (ROWWISE)
     for (const Rows* r : {&p.gate, &p.scale}) add_stream(plan, *r, NC * kChunk);
-  constexpr int kRoom = 210 * 1024 / sm_ctas(WPR, grad_sm_warps(PLAIN, ROWWISE));
-  set_depth(plan, kRoom, WARPS);
+  constexpr int W = NC * WPR * kChunk, FIXED = (PLAIN || NC > 1 ? 0 : 16 * W) + (ROWWISE ? 0 : WARPS * 2 * NC * kLaneChunk * 4);
+  set_depth(plan, kSmemRoom - FIXED, WARPS);
+  const size_t rings = (size_t)WARPS * plan.depth * plan.stage, sums = (size_t)16 * GROUPS * W;
+  const size_t smem = FIXED + (rings < sums ? sums : rings);
   const auto run = [&](auto kernel) {
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemRoom);
     if (e != cudaSuccess) return e;
     return launch_pdl(kernel, dim3((unsigned)((teams.n + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
-                      (size_t)WARPS * plan.depth * plan.stage, c.stream, p, plan, teams, need, c.err);
+                      smem, c.stream, p, plan, teams, need, c.err);
   };
   return whole ? run(join_grad_kernel<NC, WPR, true, ROWWISE, PLAIN>) : run(join_grad_kernel<NC, WPR, false, ROWWISE, PLAIN>);
 }

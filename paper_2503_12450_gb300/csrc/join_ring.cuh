@@ -17,13 +17,9 @@ namespace {
 // comes with the row.
 // PLAIN: no norm of y and no parameters (the modulated norm of a block); fewer registers and
 // so more warps on an SM.
-#ifndef LM_SG
-#define LM_SG 16
-#endif
-#ifndef LM_JW
-#define LM_JW 20
-#endif
-constexpr int join_sm_warps(bool plain) { return plain ? LM_JW : 20; }
+// Warps on an SM, as many as need no spills, which cost more than more warps give. 40960 x 1024 with three 8-bit
+// outputs: 28 warps 99 us, 24 105, 20 110; with a row of modulation for each row 20 warps 134, 28 (which spill) 153.
+constexpr int join_sm_warps(bool plain, bool streamed) { return plain && !streamed ? 28 : 20; }
 
 // Mean and 1 / deviation of a row of 256 columns a warp, as above. n: the warp's columns, per_n and per_D: 1 / n, 1 / D.
 template <int WPR, int GROUPS, bool WHOLE>
@@ -70,10 +66,12 @@ __device__ __forceinline__ void ring_moments(const float (&v)[8], bool layer, co
 enum { X_STREAM = 0, Y_STREAM = 1 };  // then gate, scale, shift as they are there (STREAMED)
 
 template <int WPR, bool WHOLE, bool STREAMED, bool PLAIN>
-__global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN)) * 32, sm_ctas(WPR, join_sm_warps(PLAIN)))
+__global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN, STREAMED)) * 32, 1)
     join_ring_kernel(const __grid_constant__ Join p, const __grid_constant__ RingPlan plan, const Teams teams, unsigned* err) {
-  constexpr int WARPS = cta_warps(WPR, join_sm_warps(PLAIN)), GROUPS = WARPS / WPR;
-  extern __shared__ __align__(128) uint8_t ring_smem[];
+  constexpr int WARPS = cta_warps(WPR, join_sm_warps(PLAIN, STREAMED)), GROUPS = WARPS / WPR;
+  // the four parameters, each warp's modulation (gate, 1 + scale, shift), the rings
+  constexpr int PARAMS = PLAIN ? 0 : 4 * WPR * kLaneChunk, MODS = STREAMED ? 0 : 3 * kLaneChunk;
+  extern __shared__ __align__(128) float row_smem[];
   __shared__ uint64_t bars[WARPS][kMostStages];
   __shared__ float4 red[2][2][GROUPS][WPR];
   __shared__ int abort_word;
@@ -82,13 +80,26 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN)) * 32, sm_
   const int D = p.D, c0 = part * kChunk, team = (int)blockIdx.x * GROUPS + grp;
   const Columns<WHOLE> cols(c0, D);
   if (threadIdx.x == 0) abort_word = 0;
-  RowRing<WHOLE> ring;
-  ring.init(ring_smem + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(kChunk, D - c0), p.M, D);
+  const bool live = team < teams.n;
+  const int first = live ? team_start(teams, team) : 0, end = live ? team_start(teams, team + 1) : 0;
+  RowRing<WHOLE, STREAMED> ring;
+  float* const params = row_smem + part * kLaneChunk;
+  float* const mods = row_smem + PARAMS + warp * MODS;
+  ring.init(reinterpret_cast<uint8_t*>(row_smem + PARAMS + WARPS * MODS) + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(kChunk, D - c0), p.M, D, first);
   pdl_wait();
   pdl_trigger();
+  if (!PLAIN && grp == 0) {
+    const float* const given[4] = {p.post_g, p.post_b, p.pre_g, p.pre_b};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (!given[k]) continue;
+      float t[8];
+      load_param<WHOLE>(given[k], cols, t);
+      lane_put(params + k * WPR * kLaneChunk, t);
+    }
+  }
   __syncthreads();
-  if (team >= teams.n) return;
-  const int first = team_start(teams, team), end = team_start(teams, team + 1);
+  if (!live) return;
   for (int s = 0; s < plan.depth; ++s)
     if (first + s < end) ring.fetch(plan, first + s, s, c0);
 
@@ -98,24 +109,26 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN)) * 32, sm_
   uint32_t next_s = 0;
   const uint8_t* const scales = scales_of<WHOLE>(p.y, c0, D);
   if (scales) next_s = scales[first];
-  float gate[8], scale[8], shift[8];  // scale: 1 + scale
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    gate[i] = scale[i] = 1.f;
-    shift[i] = 0.f;
-  }
   int it = 0, stop = first;  // stop: the end of the group
   bool dead = false;  // a wait ran out: the rows are not written any more
   for (int row = first; row < end; ++row, it ^= 1) {
     if (!STREAMED && row == stop) {
       const int r = p.group > 0 ? row / p.group : 0;
       stop = p.group > 0 ? min(end - r * p.group, p.group) + r * p.group : end;
-      if (p.gate.p) load_row<WHOLE>(p.gate, r, cols, gate);
-      if (p.shift.p) load_row<WHOLE>(p.shift, r, cols, shift);
+      float t[8];
+      if (p.gate.p) {
+        load_row<WHOLE>(p.gate, r, cols, t);
+        lane_put(mods, t);
+      }
       if (p.scale.p) {
-        load_row<WHOLE>(p.scale, r, cols, scale);
+        load_row<WHOLE>(p.scale, r, cols, t);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) scale[i] += 1.f;
+        for (int i = 0; i < 8; ++i) t[i] += 1.f;
+        lane_put(mods + kLaneChunk, t);
+      }
+      if (p.shift.p) {
+        load_row<WHOLE>(p.shift, r, cols, t);
+        lane_put(mods + 2 * kLaneChunk, t);
       }
     }
     const uint32_t s = next_s;
@@ -128,6 +141,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN)) * 32, sm_
     };
     from(X_STREAM, p.x.dtype, x);
     if (p.y.p) load_stage<WHOLE>(ring.piece(plan, Y_STREAM, row, c0), p.y.dtype, s, cols, v);
+    float gate[8], scale[8], shift[8];  // (STREAMED)
     if (STREAMED) {
       int i = p.y.p ? Y_STREAM + 1 : Y_STREAM;
       if (p.gate.p) from(i++, p.gate.dtype, gate);
@@ -154,14 +168,17 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN)) * 32, sm_
         scale8(v, rstd, v);
       }
       if (!PLAIN && p.post_g) {
-        load_param<WHOLE>(p.post_g, cols, t);
+        lane_get(params + 0, t);
         mul8(v, t);
       }
       if (!PLAIN && p.post_b) {
-        load_param<WHOLE>(p.post_b, cols, t);
+        lane_get(params + WPR * kLaneChunk, t);
         add8(v, t);
       }
-      mul8(v, gate);
+      if (p.gate.p) {
+        if (!STREAMED) lane_get(mods, gate);
+        mul8(v, gate);
+      }
       const float res[8] = {p.res, p.res, p.res, p.res, p.res, p.res, p.res, p.res};
       acc8(v, x, res);
       cols.mask(v);
@@ -183,14 +200,21 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN)) * 32, sm_
     sub8(v, mean);
     scale8(v, rstd, v);
     if (!PLAIN && p.pre_g) {
-      load_param<WHOLE>(p.pre_g, cols, t);
+      lane_get(params + 2 * WPR * kLaneChunk, t);
       mul8(v, t);
     }
     if (!PLAIN && p.pre_b) {
-      load_param<WHOLE>(p.pre_b, cols, t);
+      lane_get(params + 3 * WPR * kLaneChunk, t);
       add8(v, t);
     }
-    fma8(v, scale, shift);
+    if (p.scale.p) {
+      if (!STREAMED) lane_get(mods + kLaneChunk, scale);
+      mul8(v, scale);
+    }
+    if (p.shift.p) {
+      if (!STREAMED) lane_get(mods + 2 * kLaneChunk, shift);
+      add8(v, shift);
+    }
     cols.mask(v);
     if (dead) continue;
     if (p.h.p) store_row<WHOLE>(p.h, row, cols, v);
@@ -198,40 +222,41 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN)) * 32, sm_
   }
 }
 
-template <int WPR, bool PLAIN>
+template <int WPR, bool PLAIN, bool STREAMED>
 cudaError_t join_ring_run(const Ctx& c, const Join& p, bool whole) {
-  constexpr int WARPS = cta_warps(WPR, join_sm_warps(PLAIN)), GROUPS = WARPS / WPR, CTAS = sm_ctas(WPR, join_sm_warps(PLAIN));
+  constexpr int WARPS = cta_warps(WPR, join_sm_warps(PLAIN, STREAMED)), GROUPS = WARPS / WPR;
+  constexpr int FIXED = (PLAIN ? 0 : 4 * WPR * kLaneChunk * 4) + (STREAMED ? 0 : WARPS * 3 * kLaneChunk * 4);
   RingPlan plan{};
   for (const Rows* r : {&p.x, &p.y}) add_stream(plan, *r, kChunk);
-  const bool streamed = p.group > 0 && p.group < LM_SG && (p.gate.p || p.scale.p || p.shift.p);
-  if (streamed)
+  if (STREAMED)
     for (const Rows* r : {&p.gate, &p.scale, &p.shift}) add_stream(plan, *r, kChunk, p.group);
-  constexpr int kRoom = 200 * 1024 / CTAS;
-  set_depth(plan, kRoom, WARPS);
-  const Teams teams = teams_of(p.M, c.num_sms * CTAS * GROUPS);
+  set_depth(plan, kSmemRoom - FIXED, WARPS);
+  const Teams teams = teams_of(p.M, c.num_sms * GROUPS);
   const auto run = [&](auto kernel) {
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, kRoom);
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemRoom);
     if (e != cudaSuccess) return e;
     return launch_pdl(kernel, dim3((unsigned)((teams.n + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
-                      (size_t)WARPS * plan.depth * plan.stage, c.stream, p, plan, teams, c.err);
+                      (size_t)FIXED + (size_t)WARPS * plan.depth * plan.stage, c.stream, p, plan, teams, c.err);
   };
-  if (streamed)
-    return whole ? run(join_ring_kernel<WPR, true, true, PLAIN>) : run(join_ring_kernel<WPR, false, true, PLAIN>);
-  return whole ? run(join_ring_kernel<WPR, true, false, PLAIN>) : run(join_ring_kernel<WPR, false, false, PLAIN>);
+  return whole ? run(join_ring_kernel<WPR, true, STREAMED, PLAIN>) : run(join_ring_kernel<WPR, false, STREAMED, PLAIN>);
 }
 
 template <bool PLAIN>
 cudaError_t join_ring_launch(const Ctx& c, const Join& p, bool whole) {
+  // (with 16 rows a group and more, fetching the modulation with each row costs more than waiting for it once)
+  const bool streamed = p.group > 0 && p.group < 16 && (p.gate.p || p.scale.p || p.shift.p);
+#define LM_RUN(wpr) (streamed ? join_ring_run<wpr, PLAIN, true>(c, p, whole) : join_ring_run<wpr, PLAIN, false>(c, p, whole))
   switch (row_warps(p.D)) {
-    case 1: return join_ring_run<1, PLAIN>(c, p, whole);
-    case 2: return join_ring_run<2, PLAIN>(c, p, whole);
-    case 3: return join_ring_run<3, PLAIN>(c, p, whole);
-    case 4: return join_ring_run<4, PLAIN>(c, p, whole);
-    case 5: return join_ring_run<5, PLAIN>(c, p, whole);
-    case 8: return join_ring_run<8, PLAIN>(c, p, whole);
-    default: return join_ring_run<16, PLAIN>(c, p, whole);
+    case 1: return LM_RUN(1);
+    case 2: return LM_RUN(2);
+    case 3: return LM_RUN(3);
+    case 4: return LM_RUN(4);
+    case 5: return LM_RUN(5);
+    case 8: return LM_RUN(8);
+    default: return LM_RUN(16);
   }
+#undef LM_RUN
 }
 
 }  // namespace

@@ -32,14 +32,16 @@ struct RingPlan {
 
 namespace {
 
-// Waits for the WPR warps of a row, one of GROUPS teams of the CTA. (With a number known at run time a CTA
-// would be given all 16 barriers, and an SM's 64 would limit it to four CTAs.)
+// Waits for the WPR warps of a row, one of GROUPS teams of the CTA: barriers 1 .. 15, because 0 is __syncthreads's,
+// with another number of threads. (With a number known at run time a CTA would be given all 16
+// barriers, and an SM's 64 would limit it to four CTAs.)
 template <int WPR, int GROUPS>
 __device__ __forceinline__ void row_barrier(int grp) {
-  static_assert(GROUPS <= 8, "a case for each team");
-#define LM_BAR(i) case i: asm volatile("bar.sync %0, %1;" ::"n"(i < GROUPS ? i : 0), "n"(WPR * 32) : "memory"); break;
+  static_assert(WPR == 1 || GROUPS <= 15, "a barrier for each team");
+#define LM_BAR(i) case i: asm volatile("bar.sync %0, %1;" ::"n"(i < GROUPS ? i + 1 : 1), "n"(WPR * 32) : "memory"); break;
   switch (GROUPS == 1 ? 0 : grp) {
     LM_BAR(0) LM_BAR(1) LM_BAR(2) LM_BAR(3) LM_BAR(4) LM_BAR(5) LM_BAR(6) LM_BAR(7)
+    LM_BAR(8) LM_BAR(9) LM_BAR(10) LM_BAR(11) LM_BAR(12) LM_BAR(13) LM_BAR(14)
   }
 #undef LM_BAR
 }
@@ -71,6 +73,26 @@ struct Columns {
 };
 __device__ __forceinline__ size_t row_offset(unsigned row, int ld) { return (size_t)row * (unsigned)ld; }
 
+// A chunk that a lane keeps its eight values of in shared memory: two accesses without bank conflicts.
+constexpr int kLaneChunk = kChunk;  // floats
+__device__ __forceinline__ void lane_put(float* m, const float (&v)[8]) {
+  float4* p = reinterpret_cast<float4*>(m) + (threadIdx.x & 31);
+  p[0] = make_float4(v[0], v[1], v[2], v[3]);
+  p[32] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void lane_get(const float* m, float (&v)[8]) {
+  const float4* p = reinterpret_cast<const float4*>(m) + (threadIdx.x & 31);
+  const float4 a = p[0], b = p[32];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+  v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+// The column, from the chunk's first one, that place i of such a chunk is of.
+template <bool WHOLE>
+__device__ __forceinline__ int lane_column(int i) {
+  const int lane = (i & 127) >> 2, k = (i >> 7) * 4 + (i & 3);
+  return WHOLE ? 8 * lane + k : 32 * k + lane;
+}
+
 // From global memory: a row of fp32 or bf16; columns from D on read as zero.
 template <bool WHOLE, typename T>
 __device__ __forceinline__ void load_columns(const T* p, const Columns<WHOLE>& c, float (&v)[8]) {
@@ -78,6 +100,9 @@ __device__ __forceinline__ void load_columns(const T* p, const Columns<WHOLE>& c
   for (int k = 0; k < 8; ++k) v[k] = 0.f;
   if (WHOLE) {
     if (c.on(0)) ld8a(p, v);
+  } else if (c.full) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = to_f(p[32 * k]);
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -106,6 +131,9 @@ __device__ __forceinline__ void store_row(const MatOut& m, unsigned row, const C
     float* p = static_cast<float*>(m.p) + at;
     if (WHOLE) {
       if (c.on(0)) st8a(p, v);
+    } else if (c.full) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) p[32 * k] = v[k];
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k)
@@ -117,11 +145,20 @@ __device__ __forceinline__ void store_row(const MatOut& m, unsigned row, const C
       if (c.on(0)) st8a(p, v);
     } else {
       uint16_t* q = reinterpret_cast<uint16_t*>(p);
+      if (c.full) {
 #pragma unroll
-      for (int k = 0; k < 8; k += 2) {
-        const uint32_t two = pack_bf16(v[k], v[k + 1]);
-        if (c.on(k)) q[32 * k] = (uint16_t)two;
-        if (c.on(k + 1)) q[32 * (k + 1)] = (uint16_t)(two >> 16);
+        for (int k = 0; k < 8; k += 2) {
+          const uint32_t two = pack_bf16(v[k], v[k + 1]);
+          q[32 * k] = (uint16_t)two;
+          q[32 * (k + 1)] = (uint16_t)(two >> 16);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+          const uint32_t two = pack_bf16(v[k], v[k + 1]);
+          if (c.on(k)) q[32 * k] = (uint16_t)two;
+          if (c.on(k + 1)) q[32 * (k + 1)] = (uint16_t)(two >> 16);
+        }
       }
     }
   }
@@ -252,60 +289,62 @@ __device__ __forceinline__ float dot8(const float (&v)[8], const float (&a)[8]) 
 // boundary before to the one behind, which are the row's neighbours' bytes; where those are not the
 // tensor's (before its first element, behind its last), the piece comes element by element.
 // ---------------------------------------------------------------------------
-template <bool WHOLE>
+// DIVIDED: some tensors have a row for each group of rows; otherwise a lane's pointer moves on by a row each time.
+template <bool WHOLE, bool DIVIDED>
 struct RowRing {
   uint8_t* base;
   uint64_t* bars;
-  int depth, mine, slot, streams;
-  uint32_t stage, phase;
-  // this lane's tensor: the piece of row 0, bytes from row to row and of a row, its place in a stage
+  int mine, slot;
+  uint32_t phase;
+  // this lane's tensor: the piece of row 0 or of the row to be fetched next, bytes from row to row
+  // and of a row, those of all tensors
   uintptr_t src;
   size_t pitch;
-  uint32_t bytes, at, total, magic, shift;
-  unsigned last;           // its last row if this piece ends with the tensor's columns, otherwise none
-  bool starts;             // whether the piece starts with its columns
+  uint32_t bytes, total, magic, shift;
+  uintptr_t last;  // its last row's piece, if that ends with the tensor's columns, otherwise none
+  uintptr_t start; // its first row's, if it starts with them
 
-  __device__ __forceinline__ void init(uint8_t* smem, uint64_t* b, const RingPlan& plan, int first_column, int columns, int M, int D) {
+  // first: the first row that will be fetched
+  __device__ __forceinline__ void init(uint8_t* smem, uint64_t* b, const RingPlan& plan, int first_column, int columns, int M, int D,
+                                       int first) {
     const int lane = threadIdx.x & 31;
     base = smem;
     bars = b;
-    depth = plan.depth;
-    stage = plan.stage;
     mine = columns;
     slot = 0;
     phase = 0;
-    streams = plan.n;
     bytes = 0;
-    if (lane < streams) {
+    if (lane < plan.n) {
       const RowStream& t = plan.t[lane];
       src = reinterpret_cast<uintptr_t>(t.p) + (size_t)first_column * t.e;
       pitch = t.pitch;
       magic = t.magic;
       shift = t.shift;
       bytes = (uint32_t)max(mine, 0) * t.e;
-      at = t.at;
-      last = first_column + columns == D ? stream_row(magic, shift, M - 1) : 0xFFFFFFFFu;
-      starts = first_column == 0;
+      start = first_column == 0 ? src : 0;
+      last = first_column + columns == D ? src + (size_t)stream_row(magic, shift, M - 1) * pitch : 0;
+      if (!DIVIDED) src += (size_t)(unsigned)first * pitch;
     }
     if (WHOLE) {
       bytes = (bytes + 15u) & ~15u;
       total = __reduce_add_sync(0xffffffffu, bytes);
     }
     if (lane == 0)
-      for (int s = 0; s < depth; ++s) mbar_init(&bars[s], 1);
+      for (int s = 0; s < plan.depth; ++s) mbar_init(&bars[s], 1);
     fence_mbar_init();
   }
   // Row `row` into stage s. All lanes call it.
   __device__ __forceinline__ void fetch(const RingPlan& plan, int row, int s, int first_column) {
     if (mine <= 0) return;
     const int lane = threadIdx.x & 31;
-    uint8_t* dst = base + (uint32_t)s * stage;
-    const unsigned r = stream_row(magic, shift, row);
-    uintptr_t p = src + (size_t)r * pitch;
+    uint8_t* dst = base + (uint32_t)s * plan.stage;
+    uintptr_t p = src;
+    if (DIVIDED) p += (size_t)stream_row(magic, shift, row) * pitch;
+    else src += pitch;
     uint32_t n = bytes, sum = total;
-    bool copies = lane < streams;
+    bool copies = lane < plan.n;
     if (!WHOLE) {
-      const bool outside = copies && ((starts && r == 0 && ((uint32_t)p & 15u)) || (r == last && ((uint32_t)p + bytes & 15u)));
+      const bool outside = copies && ((p == start && ((uint32_t)p & 15u)) || (p == last && (((uint32_t)p + bytes) & 15u)));
       for (unsigned them = __ballot_sync(0xffffffffu, outside); them; them &= them - 1) {
         const RowStream& t = plan.t[__ffs((int)them) - 1];
         const uint8_t* from = t.p + (size_t)stream_row(t.magic, t.shift, row) * t.pitch + (size_t)first_column * t.e;
@@ -324,7 +363,7 @@ struct RowRing {
     }
     if (lane == 0) mbar_arrive_expect_tx(&bars[s], sum);
     __syncwarp();
-    if (copies) bulk_load(dst + at, reinterpret_cast<const void*>(p), n, &bars[s]);
+    if (copies) bulk_load(dst + plan.t[lane].at, reinterpret_cast<const void*>(p), n, &bars[s]);
   }
   __device__ __forceinline__ bool wait(volatile int* abort_flag, unsigned* err) {
     return mine <= 0 || mbar_wait(&bars[slot], phase, abort_flag, err);
@@ -332,10 +371,10 @@ struct RowRing {
   // Tensor i's piece of the row that has come.
   __device__ __forceinline__ const uint8_t* piece(const RingPlan& plan, int i, int row, int first_column) const {
     const RowStream& t = plan.t[i];
-    const uint8_t* st = base + (uint32_t)slot * stage + t.at;
+    const uint8_t* st = base + (uint32_t)slot * plan.stage + t.at;
     if (WHOLE) return st;
     return st + (((uint32_t)reinterpret_cast<uintptr_t>(t.p) + (uint32_t)first_column * t.e +
-                  stream_row(t.magic, t.shift, row) * (uint32_t)t.pitch) & 15u);
+                  (DIVIDED ? stream_row(t.magic, t.shift, row) : (uint32_t)row) * (uint32_t)t.pitch) & 15u);
   }
   // The row has been read by every lane: its stage takes row `ahead`, if there is one.
   __device__ __forceinline__ void next(const RingPlan& plan, int ahead, int end, int first_column, bool dead) {
@@ -344,7 +383,7 @@ struct RowRing {
       fence_proxy_async_smem();
       fetch(plan, ahead, slot, first_column);
     }
-    if (++slot == depth) {
+    if (++slot == plan.depth) {
       slot = 0;
       phase ^= 1u;
     }
@@ -371,15 +410,15 @@ inline void set_depth(RingPlan& plan, int room, int warps) {
   if (plan.depth > 4) plan.depth = 4;
 }
 
-// Warps of a row of D columns; warps of a CTA (whole teams) and CTAs on an SM for about `warps` warps
-// there. Teams of three and five warps fill one CTA, so that the SM's four schedulers have as many
-// warps each: with CTAs of one team of five 40960 x 1280 took 200 us instead of 154.
+// Warps of a row of D columns, and of a CTA: whole teams, one CTA an SM, so that parameters are in
+// shared memory once, and that the SM's four schedulers have as many warps each (with CTAs of one team of
+// five warps 40960 x 1280 took 200 us instead of 154).
 inline int row_warps(int D) {
   const int nc = (D + kChunk - 1) / kChunk;
   return nc <= 5 ? nc : nc <= 8 ? 8 : 16;
 }
-constexpr int cta_warps(int wpr, int warps) { return wpr <= 2 ? 4 : wpr % 4 ? warps / wpr * wpr : wpr; }
-constexpr int sm_ctas(int wpr, int warps) { return warps / cta_warps(wpr, warps) > 0 ? warps / cta_warps(wpr, warps) : 1; }
+constexpr int cta_warps(int wpr, int warps) { return warps < wpr ? wpr : warps / wpr * wpr; }
+constexpr int kSmemRoom = 215 * 1024;  // of a CTA
 
 // Ranges of consecutive rows, one for each team (the warps that work on a row together).
 struct Teams {

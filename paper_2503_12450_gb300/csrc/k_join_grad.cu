@@ -18,15 +18,15 @@ __device__ __forceinline__ void put_one(const MatOut& o, unsigned row, int col, 
   }
 }
 
-// Sums over many teams: of all of them for the parameters, of those that a group of very many
-// rows is divided among for the modulation. A CTA has 32 columns of one result (blockIdx.y: 0..3 dpre_b,
-// dpre_g, dpost_b, dpost_g; 4..6 dshift, dscale, dgate) of one group (blockIdx.z); each of 32 slices adds every 32nd
-// team's, and the slices are added in order. Short chains of loads: it is all latency (40 columns of 608
-// teams: 4 us).
+// Sums over many partial rows: of the CTAs where all rows share one modulation or none does, otherwise of the
+// teams, all of them for the parameters, those that a group of very many rows is divided among for the
+// modulation. A CTA has 32 columns of one result (blockIdx.y: 0..3 dpre_b, dpre_g, dpost_b, dpost_g; 4..6 dshift,
+// dscale, dgate) of one group (blockIdx.z); each of 32 slices adds every 32nd partial row, and the slices are
+// added in order. Short chains of loads: it is all latency.
 constexpr int kSlices = 32;
 
 __global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __grid_constant__ JoinGrad p, const Teams teams,
-                                                                      bool rowwise, int first_result) {
+                                                                      int ctas, int first_result) {
   __shared__ float red[2][kSlices][32];
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + lane, D = p.D;
   const int result = (int)blockIdx.y + first_result, q = (int)blockIdx.z;
@@ -40,8 +40,8 @@ __global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __gr
   if (!o.p || (param && q > 0)) return;
   // sums of the result: k0 and, times the shift b, k1
   const int k0 = param ? result : result == 4 ? SUM_A : result == 5 ? SUM_B : SUM_Q, k1 = k0 - 1;
-  int t0 = 0, t1 = teams.n - 1, g0 = 0;
-  if (!param && p.group > 0) {
+  int t0 = 0, t1 = (ctas ? ctas : teams.n) - 1, g0 = 0;
+  if (!param && !ctas) {
     g0 = q * p.group;
     t0 = team_of(teams, g0);
     t1 = team_of(teams, g0 + min(p.group, p.M - g0) - 1);
@@ -51,8 +51,9 @@ __global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __gr
   if (col < D) {
 #pragma unroll 4
     for (int t = t0 + slice; t <= t1; t += kSlices) {
-      const float* w = param ? p.ws + (rowwise ? 0 : (size_t)teams.n * 8 * D) + (size_t)t * 4 * D
-                             : p.ws + ((size_t)t * 2 + (g0 > team_start(teams, t))) * 4 * D;
+      const float* w = p.ws + (ctas    ? (size_t)t * 4 * D
+                               : param ? ((size_t)teams.n * 8 + (size_t)t * 4) * D
+                                       : ((size_t)t * 2 + (g0 > team_start(teams, t))) * 4 * D);
       s0 += w[(size_t)k0 * D + col];
       if (b) s1 += w[(size_t)k1 * D + col];
     }
@@ -66,6 +67,13 @@ __global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __gr
     s0 += red[0][i][lane];
     s1 += red[1][i][lane];
   }
+  if (param && p.group == 0) {  // (the one modulation times the sums without it)
+    const Rows& m = result < 2 ? p.scale : p.gate;
+    if (m.p) {
+      const float v = m.dtype == LAZYMAR_F32 ? static_cast<const float*>(m.p)[col] : to_f(static_cast<const bf16*>(m.p)[col]);
+      s0 *= result < 2 ? 1.f + v : v;
+    }
+  }
   if (g) s0 *= g[col];
   if (b) s0 = fmaf(b[col], s1, s0);
   put_one(o, param ? 0u : (unsigned)q, col, s0, p.accumulate);
@@ -76,7 +84,7 @@ __global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __gr
 __global__ void __launch_bounds__(128) join_grad_groups_kernel(const __grid_constant__ JoinGrad p, const Teams teams, int groups,
                                                                unsigned sums) {
   const int lane = threadIdx.x & 31, c0 = blockIdx.x * 128 + lane, D = p.D, y = (int)blockIdx.y * 4 + (int)(threadIdx.x >> 5);
-  const int group = p.group > 0 ? p.group : p.M;
+  const int group = p.group;
   pdl_wait();
   pdl_trigger();
   int q = y;
@@ -136,17 +144,16 @@ __global__ void __launch_bounds__(256) join_grad_empty_kernel(const JoinGrad p) 
   }
 }
 
-// Teams of a launch: those that live on every SM at once, as far as there are rows.
-Teams grad_teams(int M, int D, int sm_warps) {
-  const int wpr = row_warps(D);
-  return teams_of(M, kSMs * sm_ctas(wpr, sm_warps) * (cta_warps(wpr, sm_warps) / wpr));
-}
+// Teams of a CTA, and of a launch: one CTA an SM, as far as there are rows.
+int cta_teams(int D, int sm_warps) { return cta_warps(row_warps(D), sm_warps) / row_warps(D); }
+Teams grad_teams(int M, int D, int sm_warps) { return teams_of(M, kSMs * cta_teams(D, sm_warps)); }
 
 }  // namespace
 
 size_t join_grad_workspace(int M, int D, int group) {
   if (M < 1 || D < 1 || D > kLnMaxWidth || group < 0) return 0;
-  return (size_t)grad_teams(M, D, grad_sm_warps(true, true)).n * (group == 1 ? 4 : 12) * D * sizeof(float);  // (the most)
+  const size_t rows = group > 1 ? 12 * (size_t)grad_teams(M, D, kMostGradWarps).n : 4 * (size_t)kSMs;
+  return rows * D * sizeof(float);
 }
 
 cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
@@ -175,11 +182,12 @@ cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
                           : (plain ? launch_join_grad_plain(c, p, need, whole, teams)
                                    : join_grad_launch<false, false>(c, p, need, whole, teams));
   if (e != cudaSuccess) return e;
-  const unsigned columns = (unsigned)((p.D + 31) / 32);
-  const bool divided = !rowwise && need.mods && teams.n > 1, many = divided && teams.n / groups >= kSlices;
+  const int each = cta_teams(p.D, grad_sm_warps(plain, rowwise)), ctas = p.group > 1 ? 0 : (teams.n + each - 1) / each;
+  const bool divided = !rowwise && need.mods && (ctas || teams.n > 1), many = divided && (ctas || teams.n / groups >= kSlices);
   if (need.params || many)
-    e = launch_pdl(join_grad_sums_kernel, dim3(columns, (many ? 7u : 4u) - (need.params ? 0u : 4u), many ? (unsigned)groups : 1u),
-                   dim3(32 * kSlices), 0, c.stream, p, teams, rowwise, need.params ? 0 : 4);
+    e = launch_pdl(join_grad_sums_kernel,
+                   dim3((unsigned)((p.D + 31) / 32), (many ? 7u : 4u) - (need.params ? 0u : 4u), many ? (unsigned)groups : 1u),
+                   dim3(32 * kSlices), 0, c.stream, p, teams, ctas, need.params ? 0 : 4);
   if (e != cudaSuccess || !divided || many) return e;
   const int tasks = groups < teams.n ? groups : teams.n - 1;
   return launch_pdl(join_grad_groups_kernel, dim3((unsigned)((p.D + 127) / 128), (unsigned)((tasks + 3) / 4)), dim3(128), 0,
