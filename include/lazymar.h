@@ -671,8 +671,8 @@ typedef struct lazymar_param {
  * addresses (not the values) in device memory, so the tensors stay where they are
  * while it lives; tensors of a list do not overlap. The calls on it take its
  * own scratch: one stream at a time, and no two graphs that run at once.
- * At most 2^20 tensors and 2^40 elements. Addresses on boundaries of 32 bytes (bf16: 16)
- * are faster. */
+ * At most 2^20 tensors and 2^40 elements. A tensor's addresses that are as far from a boundary
+ * of eight elements as its gradient's are faster. Waits for the device; not during a capture. */
 typedef struct lazymar_params lazymar_params;
 lazymar_status lazymar_params_create(const lazymar_param* list, int count, lazymar_params** out);
 void lazymar_params_destroy(lazymar_params* h);

@@ -544,6 +544,13 @@ lazymar_status check_param(const lazymar_param& t, bool weights) {
   return LAZYMAR_OK;
 }
 
+// Elements of g in front of its first boundary of eight, where p lies on that boundary too.
+int head_of(const lazymar_param& t) {
+  const size_t e = elem(t.g_dtype);
+  return (int)((8 - reinterpret_cast<uintptr_t>(t.g) / e % 8) % 8);
+}
+bool lies_alike(const void* p, size_t e, int head) { return !p || at(static_cast<const char*>(p) + head * e, 8 * e); }
+
 Param param_of(const lazymar_param& t) {
   Param p{};
   p.g = t.g;
@@ -553,14 +560,15 @@ Param param_of(const lazymar_param& t) {
   p.v = t.v;
   p.ema = t.ema;
   p.copy = static_cast<bf16*>(t.copy);
-  p.n = t.n;
   p.lr_scale = t.lr_scale;
   p.weight_decay = t.weight_decay;
-  const int out_dtype = t.out ? t.out_dtype : t.g_dtype;
-  const bool g8 = at(p.g, 8 * elem(t.g_dtype));
+  const int out_dtype = t.out ? t.out_dtype : t.g_dtype, head = head_of(t);
   p.flags = (t.g_dtype == LAZYMAR_BF16 ? PARAM_G_BF16 : 0u) | (out_dtype == LAZYMAR_BF16 ? PARAM_OUT_BF16 : 0u) |
-            (g8 ? PARAM_VEC_G : 0u) | (g8 && at(p.out, 8 * elem(out_dtype)) ? PARAM_VEC_OUT : 0u) |
-            (g8 && at(t.p, 32) && at(t.m, 32) && at(t.v, 32) && at(t.ema, 32) && at(t.copy, 16) ? PARAM_VEC_ALL : 0u);
+            (lies_alike(p.out, elem(out_dtype), head) ? PARAM_VEC_OUT : 0u) |
+            (lies_alike(t.p, 4, head) && lies_alike(t.m, 4, head) && lies_alike(t.v, 4, head) &&
+                     lies_alike(t.ema, 4, head) && lies_alike(t.copy, 2, head)
+                 ? PARAM_VEC_ALL
+                 : 0u);
   return p;
 }
 
@@ -578,28 +586,38 @@ lazymar_status params_create(const lazymar_param* list, int count, lazymar_param
   std::vector<Param> params;
   std::vector<Piece> pieces;
   for (int i = 0; i < count; ++i) {
-    if (list[i].n == 0) continue;
-    for (long long k = 0; k * piece < list[i].n; ++k) pieces.push_back(Piece{(unsigned)params.size(), (unsigned)k});
-    params.push_back(param_of(list[i]));
+    const lazymar_param& t = list[i];
+    if (t.n == 0) continue;
+    const int head = head_of(t);
+    for (long long from = 0; from < t.n;) {
+      const long long most = piece + (from == 0 ? head : 0), n = t.n - from < most ? t.n - from : most;
+      const int in_front = from > 0 ? 0 : n < head ? (int)n : head;
+      pieces.push_back(piece_of(static_cast<const char*>(t.g) + from * (long long)elem(t.g_dtype), (unsigned)params.size(), (int)n,
+                                in_front, t.g_dtype == LAZYMAR_BF16));
+      from += n;
+    }
+    params.push_back(param_of(t));
   }
   Ctx c;
   TR_TRY(component_ctx(nullptr, &c));
   const size_t a = params.size() * sizeof(Param), b = pieces.size() * sizeof(Piece);
-  const size_t at_pieces = (a + 255) / 256 * 256, at_partial = at_pieces + (b + 255) / 256 * 256;
-  const size_t bytes = at_partial + (size_t)c.num_sms * kNormCtasPerSm * sizeof(double);
+  const size_t at_pieces = (a + 255) / 256 * 256, at_partial = at_pieces + (b + 255) / 256 * 256 + 256;
+  const size_t bytes = at_partial + (size_t)c.num_sms * kMostNormCtas * sizeof(double) + sizeof(unsigned);
   lazymar_params* h = new lazymar_params;
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaMalloc(&h->memory, bytes);
   char* m = static_cast<char*>(h->memory);
+  if (e == cudaSuccess) e = cudaMemset(m, 0, bytes);
   if (e == cudaSuccess && a) e = cudaMemcpy(m, params.data(), a, cudaMemcpyHostToDevice);
   if (e == cudaSuccess && b) e = cudaMemcpy(m + at_pieces, pieces.data(), b, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();  // (for calls on streams that do not wait for the default one)
   if (e != cudaSuccess) {
     lazymar_params_destroy(h);
     return e == cudaErrorMemoryAllocation ? report_error(LAZYMAR_ERR_OOM, "device memory of the list") : report_cuda(e, "list");
   }
   h->has_weights = weights;
-  h->list = ParamList{reinterpret_cast<Param*>(m), reinterpret_cast<Piece*>(m + at_pieces),
-                      reinterpret_cast<double*>(m + at_partial), (int)pieces.size(), (int)piece};
+  h->list = ParamList{reinterpret_cast<Param*>(m), reinterpret_cast<Piece*>(m + at_pieces), reinterpret_cast<double*>(m + at_partial),
+                      reinterpret_cast<unsigned*>(m + bytes - sizeof(unsigned)), (int)pieces.size()};
   *out = h;
   return LAZYMAR_OK;
 }
