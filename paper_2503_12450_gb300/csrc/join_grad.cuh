@@ -1,14 +1,14 @@
 // The gradient of the residual join (lazymar_join_grad).
 //
-// A row is worked on by WPR warps (a team), NC chunks of 256 columns a warp. The teams of
-// the launch divide the rows into consecutive ranges, so that a group's rows (those with one
-// row of modulation) meet in one team or a few neighbouring ones. A lane keeps four sums
+// A row is worked on by WPR warps (a team), NC chunks of 256 columns a warp. The rows are divided into consecutive
+// ranges, so that a group's rows (those with one row of modulation) meet in one place. A lane keeps four sums
 // of each of its columns while the group lasts,
 //   A = sum dh, B = sum dh n, P = sum Z, Q = sum Z u,
-// from which all gradients of modulation and parameters follow. A group that lies in
-// one team's range is finished there; the others leave their sums in the workspace, two
-// places a team (the group that its range begins in, and the one that it ends in), and
-// a second kernel adds them in the teams' order. ROWWISE (every row has its own
+// from which all gradients of modulation and parameters follow. TOGETHER (groups of kTogether rows or more, or one
+// for all): a CTA has a range, its teams take the rows in turn and join their sums in shared memory at a group's
+// end; otherwise each team has a range of its own. A group that lies in one range is finished there; the others leave
+// their sums in the workspace, two places a range (the group that it begins in, and the one that it ends in), and
+// a second kernel adds them in the ranges' order. ROWWISE (every row has its own
 // modulation): the modulation's gradients are written with the row, and the four
 // sums, weighted, are those of the parameters.
 // The rows come by bulk copies into a ring in shared memory (join_rows.cuh).
@@ -30,6 +30,7 @@ struct JoinSums {
 // (40960 x 1280 with 320 rows a group: 20 warps 155 us, 16 165; from 20 warps on the other forms spill.)
 constexpr int grad_sm_warps(bool plain, bool rowwise) { return plain ? (rowwise ? 24 : 20) : 16; }
 constexpr int kMostGradWarps = 24;
+constexpr int kTogether = 192;
 
 namespace {
 
@@ -62,26 +63,32 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int gr
 
 template <int NC, int WPR, bool WHOLE, bool ROWWISE, bool PLAIN>
 __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) * 32, 1)
-    join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, const Teams teams, JoinSums need,
-                     unsigned* err) {
+    join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, const Teams ranges, int together,
+                     JoinSums need, unsigned* err) {
   constexpr int WARPS = cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
   // the four parameters (NC 1; of wider rows they stay where they are), each warp's modulation (gate, 1 + scale), the rings
   constexpr int W = NC * WPR * kChunk, PARAMS = PLAIN || NC > 1 ? 0 : 4 * W, MODS = ROWWISE ? 0 : 2 * NC * kLaneChunk;
+  constexpr int JOINED = ROWWISE || GROUPS == 1 ? 0 : 4 * W;
   extern __shared__ __align__(128) float row_smem[];
   __shared__ uint64_t bars[WARPS][kMostStages];
   __shared__ float2 red[2][2][GROUPS][WPR];
   __shared__ int abort_word;
   volatile int* abort_flag = &abort_word;
   const int warp = threadIdx.x >> 5, grp = warp / WPR, part = warp % WPR;
-  const int D = p.D, c0 = part * NC * kChunk, team = (int)blockIdx.x * GROUPS + grp;
+  // together: GROUPS, the steps of a team's rows, otherwise 1
+  const int D = p.D, c0 = part * NC * kChunk;
+  const int range = together > 1 || GROUPS == 1 ? (int)blockIdx.x : (int)blockIdx.x * GROUPS + grp;
   if (threadIdx.x == 0) abort_word = 0;
-  const bool live = team < teams.n;
-  const int first = live ? team_start(teams, team) : 0, end = live ? team_start(teams, team + 1) : 0;
+  const bool live = range < ranges.n;
+  const int begin = live ? team_start(ranges, range) : 0, end = live ? team_start(ranges, range + 1) : 0;
+  const int first = begin + (together > 1 ? grp : 0);
   RowRing<WHOLE, false> ring;
   float* const params = row_smem + part * kLaneChunk;
   float* const mods = row_smem + PARAMS + warp * MODS;
-  uint8_t* const rings = reinterpret_cast<uint8_t*>(row_smem + PARAMS + WARPS * MODS);
-  ring.init(rings + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(NC * kChunk, D - c0), p.M, D, first);
+  float* const joined = row_smem + PARAMS + WARPS * MODS + part * NC * kLaneChunk;  // sums of a CTA's teams
+  uint8_t* const rings = reinterpret_cast<uint8_t*>(row_smem + PARAMS + WARPS * MODS + JOINED);
+  ring.init(rings + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(NC * kChunk, D - c0), p.M, D, first,
+            together);
   pdl_wait();
   pdl_trigger();
   if (PARAMS > 0 && grp == 0) {
@@ -101,7 +108,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
     else load_param<WHOLE>(at, Columns<WHOLE>(c0 + c * kChunk, D), t);
   };
   for (int s = 0; s < plan.depth; ++s)
-    if (first + s < end) ring.fetch(plan, first + s, s, c0);
+    if (first + s * together < end) ring.fetch(plan, first + s * together, s, c0);
   const float per_D = 1.f / (float)D;
   const bool pre = PLAIN || p.pre != LAZYMAR_NORM_NONE, post = !PLAIN && p.post != LAZYMAR_NORM_NONE;
   const bool pre_layer = p.pre == LAZYMAR_NORM_LAYER, post_layer = p.post == LAZYMAR_NORM_LAYER;
@@ -136,7 +143,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
       if (y_scales[c]) next_ys[c] = y_scales[c][row];
     }
   };
-  if (live) statistics(first);
+  statistics(first);
 
   float sums[4][NC][8];
 #pragma unroll
@@ -156,14 +163,47 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
   auto put_sum = [&](float* o, const Columns<WHOLE>& cc, const float (&v)[8]) {
     if (!dead) store_row<WHOLE>(MatOut{o, 0, LAZYMAR_F32, true}, 0u, cc, v);
   };
-  float* const slots = p.ws + (size_t)team * 8 * D;
-  float* const param = p.ws + (size_t)teams.n * 8 * D + (size_t)team * 4 * D;
+  float* const slots = p.ws + (size_t)range * 8 * D;
+  float* const param = p.ws + (size_t)ranges.n * 8 * D + (size_t)range * 4 * D;
 
   // The end of a group, or of its part in this range: rows start .. stop.
   auto flush = [&](int start, int stop) {
+    if (together > 1) {
+      for (int g = 0; g < GROUPS; ++g) {
+        if (g == grp) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if ((PLAIN && k == SUM_P) || !(sums_of >> k & 1u)) continue;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+              float* at = joined + k * W + c * kLaneChunk;
+              if (g > 0) {
+                float t[8];
+                lane_get(at, t);
+                add8(sums[k][c], t);
+              }
+              lane_put(at, sums[k][c]);
+            }
+          }
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if (grp == 0 && !(PLAIN && k == SUM_P) && (sums_of >> k & 1u)) {
+            lane_get(joined + k * W + c * kLaneChunk, sums[k][c]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums[k][c][i] = 0.f;
+          }
+        }
+      if (grp > 0) return;
+    }
     const int q = start / p.group, g0 = q * p.group, g1 = g0 + min(p.group, p.M - g0);
     const bool whole = start == g0 && stop == g1;
-    float* slot = slots + (size_t)(start > first) * 4 * D;
+    float* slot = slots + (size_t)(start > begin) * 4 * D;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const Columns<WHOLE> cc(c0 + c * kChunk, D);
@@ -177,7 +217,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
           lane_get(mods + (k < 2 ? NC + c : c) * kLaneChunk, t);
           mul8(v, t);
         }
-        if (start > first) {
+        if (start > begin) {
           load_param<WHOLE>(param + (size_t)k * D, cc, t);
           add8(v, t);
         }
@@ -224,14 +264,12 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
     }
   };
 
-  int it = 0;
-  int start = first, stop = first;  // of the group's part
-  for (int row = first; row < end; ++row, it ^= 1) {
-    if (!ROWWISE && row == stop) {
-      if (row > first) flush(start, stop);
-      start = row;
-      const int r = p.group > 0 ? row / p.group : 0;
-      stop = p.group > 0 ? min(end - r * p.group, p.group) + r * p.group : end;
+  int it = 0, row = first;
+  for (int start = begin, stop; start < end; start = stop) {  // group by group
+    stop = end;
+    if (!ROWWISE) {
+      const int r = p.group > 0 ? start / p.group : 0;
+      if (p.group > 0) stop = min(end - r * p.group, p.group) + r * p.group;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const Columns<WHOLE> cc(c0 + c * kChunk, D);
@@ -248,185 +286,185 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
         }
       }
     }
-    const float ym = next_ym, yr = next_yr, zm = next_zm, zr = next_zr;
-    uint32_t zs[NC], ys[NC];
+    for (; row < stop; row += together, it ^= 1) {
+      const float ym = next_ym, yr = next_yr, zm = next_zm, zr = next_zr;
+      uint32_t zs[NC], ys[NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      zs[c] = next_zs[c];
-      ys[c] = next_ys[c];
-    }
-    statistics(row + 1);
-    const bool ok = dead || ring.wait(abort_flag, err);
-    dead |= !__all_sync(0xffffffffu, ok);
-    float d[NC][8], n[NC][8], Z[NC][8], u[NC][8];
-    int i = 0;
-    const auto from = [&](const Rows& m, const uint32_t (&scales)[NC], float (&to)[NC][8]) {
-      const uint8_t* st = ring.piece(plan, i, row, c0);
+      for (int c = 0; c < NC; ++c) {
+        zs[c] = next_zs[c];
+        ys[c] = next_ys[c];
+      }
+      statistics(row + together);
+      const bool ok = dead || ring.wait(abort_flag, err);
+      dead |= !__all_sync(0xffffffffu, ok);
+      float d[NC][8], n[NC][8], Z[NC][8], u[NC][8];
+      int i = 0;
+      const auto from = [&](const Rows& m, const uint32_t (&scales)[NC], float (&to)[NC][8]) {
+        const uint8_t* st = ring.piece(plan, i, row, c0);
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
-        load_stage<WHOLE>(st + (uint32_t)c * kChunk * plan.t[i].e, m.dtype, scales[c], Columns<WHOLE>(c0 + c * kChunk, D), to[c]);
-      ++i;
-    };
-    const auto none = [&](float (&to)[NC][8]) {
+        for (int c = 0; c < NC; ++c)
+          load_stage<WHOLE>(st + (uint32_t)c * kChunk * plan.t[i].e, m.dtype, scales[c], Columns<WHOLE>(c0 + c * kChunk, D), to[c]);
+        ++i;
+      };
+      const auto none = [&](float (&to)[NC][8]) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) to[c][k] = 0.f;
-    };
-    if (pre) {
-      from(p.dh, zs, d);
-      from(p.z, zs, n);
-    }
-    float mod[NC][8];  // ROWWISE: 1 + scale, then gate
-    if (ROWWISE && p.scale.p) {
-      i = plan.n - 1;
-      from(p.scale, zs, mod);
+          for (int k = 0; k < 8; ++k) to[c][k] = 0.f;
+      };
+      if (pre) {
+        from(p.dh, zs, d);
+        from(p.z, zs, n);
+      }
+      float mod[NC][8];  // ROWWISE: 1 + scale, then gate
+      if (ROWWISE && p.scale.p) {
+        i = plan.n - 1;
+        from(p.scale, zs, mod);
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) mod[c][k] += 1.f;
-      i = pre ? 2 : 0;
-    }
-    // (dz and y are read when they are needed: fewer registers)
-    if (pre) {
-      float s1 = 0.f, s2 = 0.f;
+          for (int k = 0; k < 8; ++k) mod[c][k] += 1.f;
+        i = pre ? 2 : 0;
+      }
+      // (dz and y are read when they are needed: fewer registers)
+      if (pre) {
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const Columns<WHOLE> cc(c0 + c * kChunk, D);
+          float t[8];
+          sub8(n[c], zm);
+          scale8(n[c], zr, n[c]);
+          cc.mask(n[c]);
+          if (ROWWISE) {
+            if (p.dscale.p) {
+              float v[8];
+              copy8(v, n[c]);
+              if (!PLAIN && p.pre_g) {
+                parameter(2, p.pre_g, c, t);
+                mul8(v, t);
+              }
+              if (!PLAIN && p.pre_b) {
+                parameter(3, p.pre_b, c, t);
+                add8(v, t);
+              }
+              mul8(v, d[c]);
+              put(p.dscale, row, cc, v);
+            }
+            if (p.dshift.p) {
+              copy8(t, d[c]);
+              put(p.dshift, row, cc, t);
+            }
+            if (p.scale.p) mul8(d[c], mod[c]);
+          }
+          if (ab) {
+            add8(sums[SUM_A][c], d[c]);
+            acc8(sums[SUM_B][c], d[c], n[c]);
+          }
+          if (!ROWWISE && p.scale.p) {
+            lane_get(mods + (NC + c) * kLaneChunk, t);
+            mul8(d[c], t);
+          }
+          if (!PLAIN && p.pre_g) {
+            parameter(2, p.pre_g, c, t);
+            mul8(d[c], t);
+          }
+          s1 += sum8(d[c]);
+          s2 += dot8(d[c], n[c]);
+        }
+        const float2 s = row_sum2<WPR, GROUPS>(s1, s2, red[it][0][grp], grp, part);
+        s1 = pre_layer ? s.x * per_D : 0.f;
+        s2 = -s.y * per_D;
+        if (p.dz.p) from(p.dz, zs, Z);
+        else none(Z);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const float m2[8] = {s2, s2, s2, s2, s2, s2, s2, s2}, r[8] = {zr, zr, zr, zr, zr, zr, zr, zr};
+          sub8(d[c], s1);
+          acc8(d[c], n[c], m2);
+          acc8(Z[c], d[c], r);
+          Columns<WHOLE>(c0 + c * kChunk, D).mask(Z[c]);
+        }
+      } else {
+        from(p.dz, zs, Z);
+      }
+      if (p.y.p) from(p.y, ys, u);
+      else none(u);
+      if (ROWWISE && p.gate.p) from(p.gate, zs, mod);
+      ring.next(plan, row + plan.depth * together, end, c0, dead);
+      float s3 = 0.f, s4 = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const Columns<WHOLE> cc(c0 + c * kChunk, D);
         float t[8];
-        sub8(n[c], zm);
-        scale8(n[c], zr, n[c]);
-        cc.mask(n[c]);
+        if (p.dx.p && !dead) {
+          scale8(Z[c], p.res, t);
+          store_row<WHOLE>(p.dx, row, cc, t);
+        }
+        if (post) {
+          sub8(u[c], ym);
+          scale8(u[c], yr, u[c]);
+          cc.mask(u[c]);
+        }
         if (ROWWISE) {
-          if (p.dscale.p) {
+          if (p.dgate.p) {
             float v[8];
-            copy8(v, n[c]);
-            if (!PLAIN && p.pre_g) {
-              parameter(2, p.pre_g, c, t);
+            copy8(v, u[c]);
+            if (!PLAIN && p.post_g) {
+              parameter(0, p.post_g, c, t);
               mul8(v, t);
             }
-            if (!PLAIN && p.pre_b) {
-              parameter(3, p.pre_b, c, t);
+            if (!PLAIN && p.post_b) {
+              parameter(1, p.post_b, c, t);
               add8(v, t);
             }
-            mul8(v, d[c]);
-            put(p.dscale, row, cc, v);
+            mul8(v, Z[c]);
+            put(p.dgate, row, cc, v);
           }
-          if (p.dshift.p) {
-            copy8(t, d[c]);
-            put(p.dshift, row, cc, t);
-          }
-          if (p.scale.p) mul8(d[c], mod[c]);
+          if (p.gate.p) mul8(Z[c], mod[c]);
         }
-        if (ab) {
-          add8(sums[SUM_A][c], d[c]);
-          acc8(sums[SUM_B][c], d[c], n[c]);
+        if (pq) {
+          if (!PLAIN) add8(sums[SUM_P][c], Z[c]);
+          acc8(sums[SUM_Q][c], Z[c], u[c]);
         }
-        if (!ROWWISE && p.scale.p) {
-          lane_get(mods + (NC + c) * kLaneChunk, t);
-          mul8(d[c], t);
+        if (!ROWWISE && p.gate.p) {
+          lane_get(mods + c * kLaneChunk, t);
+          mul8(Z[c], t);
         }
-        if (!PLAIN && p.pre_g) {
-          parameter(2, p.pre_g, c, t);
-          mul8(d[c], t);
+        if (!PLAIN && p.post_g) {
+          parameter(0, p.post_g, c, t);
+          mul8(Z[c], t);
         }
-        s1 += sum8(d[c]);
-        s2 += dot8(d[c], n[c]);
+        if (post) {
+          s3 += sum8(Z[c]);
+          s4 += dot8(Z[c], u[c]);
+        }
       }
-      const float2 s = row_sum2<WPR, GROUPS>(s1, s2, red[it][0][grp], grp, part);
-      s1 = pre_layer ? s.x * per_D : 0.f;
-      s2 = -s.y * per_D;
-      if (p.dz.p) from(p.dz, zs, Z);
-      else none(Z);
+      if (!p.dy.p && !p.dy8.q) continue;
+      if (post) {
+        const float2 s = row_sum2<WPR, GROUPS>(s3, s4, red[it][1][grp], grp, part);
+        s3 = post_layer ? s.x * per_D : 0.f;
+        s4 = -s.y * per_D;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const float m2[8] = {s4, s4, s4, s4, s4, s4, s4, s4};
+          sub8(Z[c], s3);
+          acc8(Z[c], u[c], m2);
+          scale8(Z[c], yr, Z[c]);
+          Columns<WHOLE>(c0 + c * kChunk, D).mask(Z[c]);
+        }
+      }
+      if (dead) continue;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const float m2[8] = {s2, s2, s2, s2, s2, s2, s2, s2}, r[8] = {zr, zr, zr, zr, zr, zr, zr, zr};
-        sub8(d[c], s1);
-        acc8(d[c], n[c], m2);
-        acc8(Z[c], d[c], r);
-        Columns<WHOLE>(c0 + c * kChunk, D).mask(Z[c]);
-      }
-    } else {
-      from(p.dz, zs, Z);
-    }
-    if (p.y.p) from(p.y, ys, u);
-    else none(u);
-    if (ROWWISE && p.gate.p) from(p.gate, zs, mod);
-    ring.next(plan, row + plan.depth, end, c0, dead);
-    float s3 = 0.f, s4 = 0.f;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const Columns<WHOLE> cc(c0 + c * kChunk, D);
-      float t[8];
-      if (p.dx.p && !dead) {
-        scale8(Z[c], p.res, t);
-        store_row<WHOLE>(p.dx, row, cc, t);
-      }
-      if (post) {
-        sub8(u[c], ym);
-        scale8(u[c], yr, u[c]);
-        cc.mask(u[c]);
-      }
-      if (ROWWISE) {
-        if (p.dgate.p) {
-          float v[8];
-          copy8(v, u[c]);
-          if (!PLAIN && p.post_g) {
-            parameter(0, p.post_g, c, t);
-            mul8(v, t);
-          }
-          if (!PLAIN && p.post_b) {
-            parameter(1, p.post_b, c, t);
-            add8(v, t);
-          }
-          mul8(v, Z[c]);
-          put(p.dgate, row, cc, v);
-        }
-        if (p.gate.p) mul8(Z[c], mod[c]);
-      }
-      if (pq) {
-        if (!PLAIN) add8(sums[SUM_P][c], Z[c]);
-        acc8(sums[SUM_Q][c], Z[c], u[c]);
-      }
-      if (!ROWWISE && p.gate.p) {
-        lane_get(mods + c * kLaneChunk, t);
-        mul8(Z[c], t);
-      }
-      if (!PLAIN && p.post_g) {
-        parameter(0, p.post_g, c, t);
-        mul8(Z[c], t);
-      }
-      if (post) {
-        s3 += sum8(Z[c]);
-        s4 += dot8(Z[c], u[c]);
+        const Columns<WHOLE> cc(c0 + c * kChunk, D);
+        if (p.dy.p) store_row<WHOLE>(p.dy, row, cc, Z[c]);
+        if (p.dy8.q) store_row8<WHOLE>(p.dy8, row, cc, Z[c]);
       }
     }
-    if (!p.dy.p && !p.dy8.q) continue;
-    if (post) {
-      const float2 s = row_sum2<WPR, GROUPS>(s3, s4, red[it][1][grp], grp, part);
-      s3 = post_layer ? s.x * per_D : 0.f;
-      s4 = -s.y * per_D;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const float m2[8] = {s4, s4, s4, s4, s4, s4, s4, s4};
-        sub8(Z[c], s3);
-        acc8(Z[c], u[c], m2);
-        scale8(Z[c], yr, Z[c]);
-        Columns<WHOLE>(c0 + c * kChunk, D).mask(Z[c]);
-      }
-    }
-    if (dead) continue;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const Columns<WHOLE> cc(c0 + c * kChunk, D);
-      if (p.dy.p) store_row<WHOLE>(p.dy, row, cc, Z[c]);
-      if (p.dy8.q) store_row8<WHOLE>(p.dy8, row, cc, Z[c]);
-    }
+    if (!ROWWISE && p.group > 0) flush(start, stop);
   }
-  if (!ROWWISE && p.group > 0) {
-    if (live) flush(start, stop);
-    return;
-  }
+  if (!ROWWISE && p.group > 0) return;
   // One group, or none: the teams' sums in turn, through shared memory, to the CTA's place.
   const unsigned of = ROWWISE ? need.params : need.mods | need.params;
   if ((PLAIN && ROWWISE) || !of) return;
@@ -451,7 +489,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
 }
 
 template <int NC, int WPR, bool ROWWISE, bool PLAIN>
-cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams) {
+cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& ranges, bool together) {
   constexpr int WARPS = cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
   RingPlan plan{};
   if (p.pre != LAZYMAR_NORM_NONE)
@@ -459,7 +497,8 @@ cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need,
   for (const Rows* r : {&p.dz, &p.y}) add_stream(plan, *r, NC * kChunk);
   if (ROWWISE)
     for (const Rows* r : {&p.gate, &p.scale}) add_stream(plan, *r, NC * kChunk);
-  constexpr int W = NC * WPR * kChunk, FIXED = (PLAIN || NC > 1 ? 0 : 16 * W) + (ROWWISE ? 0 : WARPS * 2 * NC * kLaneChunk * 4);
+  constexpr int W = NC * WPR * kChunk, FIXED = (PLAIN || NC > 1 ? 0 : 16 * W) + (ROWWISE ? 0 : WARPS * 2 * NC * kLaneChunk * 4) +
+                  (ROWWISE || GROUPS == 1 ? 0 : 16 * W);
   set_depth(plan, kSmemRoom - FIXED, WARPS);
   const size_t rings = (size_t)WARPS * plan.depth * plan.stage, sums = (size_t)16 * GROUPS * W;
   const size_t smem = FIXED + (rings < sums ? sums : rings);
@@ -467,32 +506,32 @@ cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need,
     const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemRoom);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3((unsigned)((teams.n + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
-                      smem, c.stream, p, plan, teams, need, c.err);
+    return launch_pdl(kernel, dim3((unsigned)(together ? ranges.n : (ranges.n + GROUPS - 1) / GROUPS)), dim3(WARPS * 32),
+                      smem, c.stream, p, plan, ranges, together ? GROUPS : 1, need, c.err);
   };
   return whole ? run(join_grad_kernel<NC, WPR, true, ROWWISE, PLAIN>) : run(join_grad_kernel<NC, WPR, false, ROWWISE, PLAIN>);
 }
 
 template <bool ROWWISE, bool PLAIN>
-cudaError_t join_grad_launch(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams) {
+cudaError_t join_grad_launch(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& ranges, bool together) {
   switch (row_warps(p.D)) {
-    case 1: return join_grad_run<1, 1, ROWWISE, PLAIN>(c, p, need, whole, teams);
-    case 2: return join_grad_run<1, 2, ROWWISE, PLAIN>(c, p, need, whole, teams);
-    case 3: return join_grad_run<1, 3, ROWWISE, PLAIN>(c, p, need, whole, teams);
-    case 4: return join_grad_run<1, 4, ROWWISE, PLAIN>(c, p, need, whole, teams);
-    case 5: return join_grad_run<1, 5, ROWWISE, PLAIN>(c, p, need, whole, teams);
-    case 8: return join_grad_run<1, 8, ROWWISE, PLAIN>(c, p, need, whole, teams);
+    case 1: return join_grad_run<1, 1, ROWWISE, PLAIN>(c, p, need, whole, ranges, together);
+    case 2: return join_grad_run<1, 2, ROWWISE, PLAIN>(c, p, need, whole, ranges, together);
+    case 3: return join_grad_run<1, 3, ROWWISE, PLAIN>(c, p, need, whole, ranges, together);
+    case 4: return join_grad_run<1, 4, ROWWISE, PLAIN>(c, p, need, whole, ranges, together);
+    case 5: return join_grad_run<1, 5, ROWWISE, PLAIN>(c, p, need, whole, ranges, together);
+    case 8: return join_grad_run<1, 8, ROWWISE, PLAIN>(c, p, need, whole, ranges, together);
     default:
-      return p.D <= 16 * kChunk ? join_grad_run<1, 16, ROWWISE, PLAIN>(c, p, need, whole, teams)
-                                : join_grad_run<2, 16, ROWWISE, PLAIN>(c, p, need, whole, teams);
+      return p.D <= 16 * kChunk ? join_grad_run<1, 16, ROWWISE, PLAIN>(c, p, need, whole, ranges, together)
+                                : join_grad_run<2, 16, ROWWISE, PLAIN>(c, p, need, whole, ranges, together);
   }
 }
 
 }  // namespace
 
-cudaError_t launch_join_grad_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams);
-cudaError_t launch_join_grad_plain(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams);
+cudaError_t launch_join_grad_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& ranges, bool together);
+cudaError_t launch_join_grad_plain(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& ranges, bool together);
 cudaError_t launch_join_grad_plain_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole,
-                                           const Teams& teams);
+                                           const Teams& ranges, bool together);
 
 }  // namespace lm

@@ -304,9 +304,9 @@ struct RowRing {
   uintptr_t last;  // its last row's piece, if that ends with the tensor's columns, otherwise none
   uintptr_t start; // its first row's, if it starts with them
 
-  // first: the first row that will be fetched
+  // first: the first row that will be fetched; step: from one to the next
   __device__ __forceinline__ void init(uint8_t* smem, uint64_t* b, const RingPlan& plan, int first_column, int columns, int M, int D,
-                                       int first) {
+                                       int first, int step = 1) {
     const int lane = threadIdx.x & 31;
     base = smem;
     bars = b;
@@ -323,7 +323,10 @@ struct RowRing {
       bytes = (uint32_t)max(mine, 0) * t.e;
       start = first_column == 0 ? src : 0;
       last = first_column + columns == D ? src + (size_t)stream_row(magic, shift, M - 1) * pitch : 0;
-      if (!DIVIDED) src += (size_t)(unsigned)first * pitch;
+      if (!DIVIDED) {
+        src += (size_t)(unsigned)first * pitch;
+        pitch *= (unsigned)step;
+      }
     }
     if (WHOLE) {
       bytes = (bytes + 15u) & ~15u;

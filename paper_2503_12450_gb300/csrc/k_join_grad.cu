@@ -144,15 +144,14 @@ __global__ void __launch_bounds__(256) join_grad_empty_kernel(const JoinGrad p) 
   }
 }
 
-// Teams of a CTA, and of a launch: one CTA an SM, as far as there are rows.
+// Teams of a CTA, one CTA an SM.
 int cta_teams(int D, int sm_warps) { return cta_warps(row_warps(D), sm_warps) / row_warps(D); }
-Teams grad_teams(int M, int D, int sm_warps) { return teams_of(M, kSMs * cta_teams(D, sm_warps)); }
 
 }  // namespace
 
 size_t join_grad_workspace(int M, int D, int group) {
   if (M < 1 || D < 1 || D > kLnMaxWidth || group < 0) return 0;
-  const size_t rows = group > 1 ? 12 * (size_t)grad_teams(M, D, kMostGradWarps).n : 4 * (size_t)kSMs;
+  const size_t rows = group > 1 ? 12 * (size_t)teams_of(M, kSMs * cta_teams(D, kMostGradWarps)).n : 4 * (size_t)kSMs;
   return rows * D * sizeof(float);
 }
 
@@ -172,26 +171,31 @@ cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
   if (p.dpost_g) need.params |= 1u << SUM_Q;
   const bool rowwise = p.group == 1;
   const bool plain = p.pre && !p.post && !p.post_g && !p.post_b && !p.pre_g && !p.pre_b && !need.params;
-  const Teams teams = grad_teams(p.M, p.D, grad_sm_warps(plain, rowwise));
+  const int each = cta_teams(p.D, grad_sm_warps(plain, rowwise));
+  // (With few rows a group, joining the teams' sums costs more than writing them out: 40960 x 1280 with 64 rows a
+  // group 166 us together, 153 apart; with 320 154 and 155, at 768 columns 104 and 121.)
+  const bool together = p.group == 0 || p.group >= kTogether;
+  const Teams ranges = teams_of(p.M, together ? kSMs : kSMs * each);
   const int groups = p.group > 0 ? (p.M - 1) / p.group + 1 : 1;
   const bool whole = p.D % 8 == 0 && on_eight(p.dh) && on_eight(p.dz) && on_eight(p.z) && on_eight(p.y) &&
                      on_eight(p.gate) && on_eight(p.scale) && on_eight(p.dx) && on_eight(p.dy) && on_eight(p.dgate) &&
                      on_eight(p.dscale) && on_eight(p.dshift) && p.params_vec;
-  cudaError_t e = rowwise ? (plain ? launch_join_grad_plain_rowwise(c, p, need, whole, teams)
-                                   : launch_join_grad_rowwise(c, p, need, whole, teams))
-                          : (plain ? launch_join_grad_plain(c, p, need, whole, teams)
-                                   : join_grad_launch<false, false>(c, p, need, whole, teams));
+  cudaError_t e = rowwise ? (plain ? launch_join_grad_plain_rowwise(c, p, need, whole, ranges, together)
+                                   : launch_join_grad_rowwise(c, p, need, whole, ranges, together))
+                          : (plain ? launch_join_grad_plain(c, p, need, whole, ranges, together)
+                                   : join_grad_launch<false, false>(c, p, need, whole, ranges, together));
   if (e != cudaSuccess) return e;
-  const int each = cta_teams(p.D, grad_sm_warps(plain, rowwise)), ctas = p.group > 1 ? 0 : (teams.n + each - 1) / each;
-  const bool divided = !rowwise && need.mods && (ctas || teams.n > 1), many = divided && (ctas || teams.n / groups >= kSlices);
+  // partial rows of CTAs (one group or none), otherwise of ranges
+  const int ctas = p.group > 1 ? 0 : together ? ranges.n : (ranges.n + each - 1) / each;
+  const bool divided = !rowwise && need.mods && (ctas || ranges.n > 1), many = divided && (ctas || ranges.n / groups >= kSlices);
   if (need.params || many)
     e = launch_pdl(join_grad_sums_kernel,
                    dim3((unsigned)((p.D + 31) / 32), (many ? 7u : 4u) - (need.params ? 0u : 4u), many ? (unsigned)groups : 1u),
-                   dim3(32 * kSlices), 0, c.stream, p, teams, ctas, need.params ? 0 : 4);
+                   dim3(32 * kSlices), 0, c.stream, p, ranges, ctas, need.params ? 0 : 4);
   if (e != cudaSuccess || !divided || many) return e;
-  const int tasks = groups < teams.n ? groups : teams.n - 1;
+  const int tasks = groups < ranges.n ? groups : ranges.n - 1;
   return launch_pdl(join_grad_groups_kernel, dim3((unsigned)((p.D + 127) / 128), (unsigned)((tasks + 3) / 4)), dim3(128), 0,
-                    c.stream, p, teams, groups, need.mods);
+                    c.stream, p, ranges, groups, need.mods);
 }
 
 }  // namespace lm

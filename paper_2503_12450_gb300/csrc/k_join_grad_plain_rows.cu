@@ -3,8 +3,8 @@
 
 namespace lm {
 
-cudaError_t launch_join_grad_plain_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& teams) {
-  return join_grad_launch<true, true>(c, p, need, whole, teams);
+cudaError_t launch_join_grad_plain_rowwise(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& ranges, bool together) {
+  return join_grad_launch<true, true>(c, p, need, whole, ranges, together);
 }
 
 }  // namespace lm
