@@ -11,6 +11,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2503_12450_gb300 import lazymar as lm  # noqa: E402
+from paper_2503_12450_gb300.adamw import AdamW  # noqa: E402
 from paper_2503_12450_gb300.mlp_block8 import MlpBlock8  # noqa: E402
 
 
@@ -28,9 +29,7 @@ def tune(width, rows, steps, mlp_ratio=4, seed=0):
     noise = random_params(width, mlp_ratio * width, seed + 1)
     student = MlpBlock8({k: v + 0.3 * noise[k] if k.startswith("w") else v.clone() for k, v in teacher.p.items()})
     g = torch.Generator(device="cuda").manual_seed(seed + 2)
-    opt = torch.optim.Adam(list(student.p.values()), lr=lr)
-    for k, v in student.p.items():
-        v.grad = student.grads[k]
+    opt = AdamW(student.p, student.grads, lr)
     losses, a, b = [], torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     for i in range(steps):
         x = torch.randn((rows, width), device="cuda", generator=g)

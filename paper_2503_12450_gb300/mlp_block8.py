@@ -5,8 +5,8 @@ Kept for the backward pass are the block's input, the LayerNorm's output and
 GELU's input and output, each as E4M3 bytes with one scale per 128 columns: 2 D +
 2 H bytes a token instead of 4 D + 4 H in bf16. Weights are fp32; their 8-bit copies
 (and the transposed ones that the input gradients need) are packed after each
-update by pack(). PyTorch holds the memory and its optimizers update the weights;
-every product and row-wise pass runs in liblazymar.so.
+update by pack(). PyTorch holds the memory; adamw.AdamW or one of its optimizers updates the
+weights. Every product and row-wise pass runs in liblazymar.so.
 """
 import torch
 
