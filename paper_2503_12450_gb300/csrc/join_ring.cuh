@@ -13,13 +13,17 @@ namespace {
 // A team of WPR warps works through consecutive rows, 256 columns a warp; its rows come by bulk
 // copies into the warps' rings, so that the memory system always has the next ones to
 // deliver while this one's sums are exchanged. Rows of a group follow each other, so
-// the modulation stays in registers while a group lasts; STREAMED (every row has its own) it
-// comes with the row.
-// PLAIN: no norm of y and no parameters (the modulated norm of a block); fewer registers and
-// so more warps on an SM.
+// the modulation stays in shared memory while a group lasts; STREAMED (groups of one or two rows) it
+// comes with the row. PLAIN: no norm of y and no parameters (the modulated norm of a block).
+// 40960 x 1024, fp32 stream, bf16 branch, three 8-bit outputs, 320 rows a group: 95 us, 5.8 TB/s (floor 81);
+// instructions bound it next to HBM (450 a warp and row). The row in registers without a ring, 16 warps: 223 us. Both
+// norms with parameters, 40000 x 777 in bf16: 104 us (floor 37), elements loaded and stored one by one.
 // Warps on an SM, as many as need no spills, which cost more than more warps give. 40960 x 1024 with three 8-bit
-// outputs: 28 warps 99 us, 24 105, 20 110; with a row of modulation for each row 20 warps 134, 28 (which spill) 153.
-constexpr int join_sm_warps(bool plain, bool streamed) { return plain && !streamed ? 28 : 20; }
+// outputs: 28 warps 95 us, 24 101; x 1280 30 warps 117, 28 122; with a row of modulation for each row 24 warps 129, 28
+// 143; both norms at 40000 x 1024 in bf16 28 warps 88, 24 93.
+constexpr int join_sm_warps(int wpr, bool plain, bool streamed) {
+  return plain ? (streamed ? 24 : wpr >= 3 ? 30 : 28) : (streamed ? 20 : 28);
+}
 
 // Mean and 1 / deviation of a row of 256 columns a warp, as above. n: the warp's columns, per_n and per_D: 1 / n, 1 / D.
 template <int WPR, int GROUPS, bool WHOLE>
@@ -66,9 +70,9 @@ __device__ __forceinline__ void ring_moments(const float (&v)[8], bool layer, co
 enum { X_STREAM = 0, Y_STREAM = 1 };  // then gate, scale, shift as they are there (STREAMED)
 
 template <int WPR, bool WHOLE, bool STREAMED, bool PLAIN>
-__global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN, STREAMED)) * 32, 1)
+__global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREAMED)) * 32, 1)
     join_ring_kernel(const __grid_constant__ Join p, const __grid_constant__ RingPlan plan, const Teams teams, unsigned* err) {
-  constexpr int WARPS = cta_warps(WPR, join_sm_warps(PLAIN, STREAMED)), GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREAMED)), GROUPS = WARPS / WPR;
   // the four parameters, each warp's modulation (gate, 1 + scale, shift), the rings
   constexpr int PARAMS = PLAIN ? 0 : 4 * WPR * kLaneChunk, MODS = STREAMED ? 0 : 3 * kLaneChunk;
   extern __shared__ __align__(128) float row_smem[];
@@ -135,31 +139,19 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN, STREAMED))
     if (scales && row + 1 < end) next_s = scales[row + 1];
     const bool ok = dead || ring.wait(abort_flag, err);
     dead |= !__all_sync(0xffffffffu, ok);
-    float v[8], x[8];
-    const auto from = [&](int i, int dtype, float (&to)[8]) {
-      load_stage<WHOLE>(ring.piece(plan, i, row, c0), dtype, 0, cols, to);
+    // each piece is read when it is needed, and the stage given on after the last: fewer registers
+    float v[8], t[8];
+    const int mod = p.y.p ? Y_STREAM + 1 : Y_STREAM;  // the first stream of the modulation
+    const auto from = [&](int i, int dtype, uint32_t scale, float (&to)[8]) {
+      load_stage<WHOLE>(ring.piece(plan, i, row, c0), dtype, scale, cols, to);
     };
-    from(X_STREAM, p.x.dtype, x);
-    if (p.y.p) load_stage<WHOLE>(ring.piece(plan, Y_STREAM, row, c0), p.y.dtype, s, cols, v);
-    float gate[8], scale[8], shift[8];  // (STREAMED)
-    if (STREAMED) {
-      int i = p.y.p ? Y_STREAM + 1 : Y_STREAM;
-      if (p.gate.p) from(i++, p.gate.dtype, gate);
-      if (p.scale.p) {
-        from(i++, p.scale.dtype, scale);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) scale[k] += 1.f;
-      }
-      if (p.shift.p) from(i++, p.shift.dtype, shift);
-    }
-    ring.next(plan, row + plan.depth, end, c0, dead);
-    float t[8];
     if (p.y.p) {
+      from(Y_STREAM, p.y.dtype, s, v);
       if (p.y8.q && !dead) store_row8<WHOLE>(p.y8, row, cols, v);
       if (post) {
         float mean, rstd;
         ring_moments<WPR, GROUPS, WHOLE>(v, p.post == LAZYMAR_NORM_LAYER, cols, n, per_n, per_D, p.eps, red[it][0][grp], grp, part,
-                                 mean, rstd);
+                                         mean, rstd);
         if (leads && !dead) {
           if (p.y_mean) p.y_mean[row] = mean;
           if (p.y_rstd) p.y_rstd[row] = rstd;
@@ -168,7 +160,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN, STREAMED))
         scale8(v, rstd, v);
       }
       if (!PLAIN && p.post_g) {
-        lane_get(params + 0, t);
+        lane_get(params, t);
         mul8(v, t);
       }
       if (!PLAIN && p.post_b) {
@@ -176,20 +168,27 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN, STREAMED))
         add8(v, t);
       }
       if (p.gate.p) {
-        if (!STREAMED) lane_get(mods, gate);
-        mul8(v, gate);
+        if (STREAMED) from(mod, p.gate.dtype, 0, t);
+        else lane_get(mods, t);
+        mul8(v, t);
       }
+      from(X_STREAM, p.x.dtype, 0, t);
       const float res[8] = {p.res, p.res, p.res, p.res, p.res, p.res, p.res, p.res};
-      acc8(v, x, res);
+      acc8(v, t, res);
       cols.mask(v);
     } else {
-      scale8(x, p.res, v);
+      from(X_STREAM, p.x.dtype, 0, t);
+      scale8(t, p.res, v);
     }
+    if (!STREAMED) ring.next(plan, row + plan.depth, end, c0, dead);
     if (!dead) {
       if (p.z.p) store_row<WHOLE>(p.z, row, cols, v);
       if (p.z8.q) store_row8<WHOLE>(p.z8, row, cols, v);
     }
-    if (!pre) continue;
+    if (!pre) {
+      if (STREAMED) ring.next(plan, row + plan.depth, end, c0, dead);
+      continue;
+    }
     float mean, rstd;
     ring_moments<WPR, GROUPS, WHOLE>(v, p.pre == LAZYMAR_NORM_LAYER, cols, n, per_n, per_D, p.eps, red[it][1][grp], grp, part, mean,
                              rstd);
@@ -207,14 +206,23 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN, STREAMED))
       lane_get(params + 3 * WPR * kLaneChunk, t);
       add8(v, t);
     }
+    int i = mod + (p.gate.p != nullptr);
     if (p.scale.p) {
-      if (!STREAMED) lane_get(mods + kLaneChunk, scale);
-      mul8(v, scale);
+      if (STREAMED) {
+        from(i++, p.scale.dtype, 0, t);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] += 1.f;
+      } else {
+        lane_get(mods + kLaneChunk, t);
+      }
+      mul8(v, t);
     }
     if (p.shift.p) {
-      if (!STREAMED) lane_get(mods + 2 * kLaneChunk, shift);
-      add8(v, shift);
+      if (STREAMED) from(i, p.shift.dtype, 0, t);
+      else lane_get(mods + 2 * kLaneChunk, t);
+      add8(v, t);
     }
+    if (STREAMED) ring.next(plan, row + plan.depth, end, c0, dead);
     cols.mask(v);
     if (dead) continue;
     if (p.h.p) store_row<WHOLE>(p.h, row, cols, v);
@@ -224,7 +232,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(PLAIN, STREAMED))
 
 template <int WPR, bool PLAIN, bool STREAMED>
 cudaError_t join_ring_run(const Ctx& c, const Join& p, bool whole) {
-  constexpr int WARPS = cta_warps(WPR, join_sm_warps(PLAIN, STREAMED)), GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREAMED)), GROUPS = WARPS / WPR;
   constexpr int FIXED = (PLAIN ? 0 : 4 * WPR * kLaneChunk * 4) + (STREAMED ? 0 : WARPS * 3 * kLaneChunk * 4);
   RingPlan plan{};
   for (const Rows* r : {&p.x, &p.y}) add_stream(plan, *r, kChunk);
@@ -244,8 +252,9 @@ cudaError_t join_ring_run(const Ctx& c, const Join& p, bool whole) {
 
 template <bool PLAIN>
 cudaError_t join_ring_launch(const Ctx& c, const Join& p, bool whole) {
-  // (with 16 rows a group and more, fetching the modulation with each row costs more than waiting for it once)
-  const bool streamed = p.group > 0 && p.group < 16 && (p.gate.p || p.scale.p || p.shift.p);
+  // Fetching the modulation with each row costs more than waiting for it at each group's first, except for very small
+  // groups: 40960 x 1024 in groups of 2 118 us with the rows, 131 without, of 3 117 and 117, of 8 117 and 101.
+  const bool streamed = p.group > 0 && p.group < 3 && (p.gate.p || p.scale.p || p.shift.p);
 #define LM_RUN(wpr) (streamed ? join_ring_run<wpr, PLAIN, true>(c, p, whole) : join_ring_run<wpr, PLAIN, false>(c, p, whole))
   switch (row_warps(p.D)) {
     case 1: return LM_RUN(1);
