@@ -604,8 +604,9 @@ typedef struct lazymar_join_args {
   lazymar_rows y;    /* [M, D] fp32, bf16 or E4M3: the branch's output; absent: post, gate, post_g, post_b are too */
   lazymar_rows gate, scale, shift;             /* fp32 or bf16; scale and shift need pre */
   const float *post_g, *post_b, *pre_g, *pre_b; /* [D]; pre_g and pre_b need pre */
-  lazymar_rows z;    /* [M, D] fp32 or bf16; may be x or y itself, with its type and stride */
-  lazymar_rows h;    /* [M, D] fp32 or bf16; the same */
+  /* No two outputs in one place; each may be x or y itself, with its type and stride. */
+  lazymar_rows z;    /* [M, D] fp32 or bf16 */
+  lazymar_rows h;    /* [M, D] fp32 or bf16 */
   lazymar_rows h8, z8, y8; /* E4M3: h as the operand of lazymar_block8_linear, z and y as checkpoints */
   float *y_mean, *y_rstd;  /* [M] statistics of post (may be NULL); means of LAZYMAR_NORM_RMS are 0 */
   float *z_mean, *z_rstd;  /* [M] those of pre */
@@ -636,11 +637,12 @@ typedef struct lazymar_join_grad_args {
   lazymar_rows gate, scale;
   const float *post_g, *post_b, *pre_g, *pre_b;
   const float *y_mean, *y_rstd, *z_mean, *z_rstd;  /* of the norms that there are; means not with LAZYMAR_NORM_RMS */
-  lazymar_rows dx;   /* [M, D] fp32 or bf16; may be absent, or dz, dh, z or y itself with its type and stride */
-  lazymar_rows dy;   /* the same */
+  /* Any of these may be absent, dx, dy and dy8 each dz, dh, z or y itself with its type and stride; no two in one place. */
+  lazymar_rows dx;   /* [M, D] fp32 or bf16 */
+  lazymar_rows dy;   /* [M, D] fp32 or bf16 */
   lazymar_rows dy8;  /* [M, D] E4M3: dy as the operand of the input gradient's product */
-  lazymar_rows dgate, dscale, dshift;              /* [ceil(M / group) or 1, D] fp32 or bf16; may be absent */
-  float *dpost_g, *dpost_b, *dpre_g, *dpre_b;      /* [D]; may be NULL */
+  lazymar_rows dgate, dscale, dshift;              /* [ceil(M / group) or 1, D] fp32 or bf16 */
+  float *dpost_g, *dpost_b, *dpre_g, *dpre_b;      /* [D] */
   void* workspace;   /* 16-byte aligned; needed if one of dgate .. dpre_b is given */
   size_t workspace_bytes;  /* >= lazymar_join_grad_workspace(M, D, group) */
 } lazymar_join_grad_args;
@@ -672,7 +674,8 @@ typedef struct lazymar_param {
  * while it lives; tensors of a list do not overlap. The calls on it take its
  * own scratch: one stream at a time, and no two graphs that run at once.
  * At most 2^20 tensors and 2^40 elements. A tensor's addresses that are as far from a boundary
- * of eight elements as its gradient's are faster. Waits for the device; not during a capture. */
+ * of eight elements as its gradient's are faster. Creating a list waits for the default stream; not during
+ * a capture. */
 typedef struct lazymar_params lazymar_params;
 lazymar_status lazymar_params_create(const lazymar_param* list, int count, lazymar_params** out);
 void lazymar_params_destroy(lazymar_params* h);

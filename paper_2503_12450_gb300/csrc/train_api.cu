@@ -6,6 +6,8 @@
 #include "optim.cuh"
 
 #include <cmath>
+#include <cstring>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -344,6 +346,13 @@ lazymar_block8 eight_of(const lazymar_rows& r) { return lazymar_block8{r.p, r.sc
 bool displaced(const lazymar_rows& out, const lazymar_rows& in, int M) {
   return out.p && out.p == in.p && (out.dtype != in.dtype || (M > 1 && out.ld != in.ld));
 }
+// Two outputs in one place.
+bool twice(std::initializer_list<const void*> outputs) {
+  for (auto a = outputs.begin(); a != outputs.end(); ++a)
+    for (auto b = outputs.begin(); b != a; ++b)
+      if (*a && *a == *b) return true;
+  return false;
+}
 bool norm_kind(int k) { return k == LAZYMAR_NORM_NONE || k == LAZYMAR_NORM_LAYER || k == LAZYMAR_NORM_RMS; }
 int mod_rows(int M, int group) { return group > 0 ? (int)(((long long)M + group - 1) / group) : 1; }
 
@@ -372,10 +381,11 @@ extern "C" lazymar_status lazymar_join(const lazymar_join_args* a, void* stream)
   if (!a->pre && (a->h.p || a->h8.p || a->scale.p || a->shift.p || a->pre_g || a->pre_b || a->z_mean || a->z_rstd))
     return bad("h, h8, scale, shift, pre_g, pre_b and z's statistics need pre");
   if (!a->x.p) return bad("x: fp32 or bf16 device tensor, ld >= D required");
-  if (a->z.p && a->z.p == a->h.p) return bad("z and h in one place");
-  for (const lazymar_rows* out : {&a->z, &a->h})
+  if (twice({a->z.p, a->h.p, a->h8.p, a->z8.p, a->y8.p, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd}))
+    return bad("two outputs in one place");
+  for (const lazymar_rows* out : {&a->z, &a->h, &a->h8, &a->z8, &a->y8})
     for (const lazymar_rows* in : {&a->x, &a->y})
-      if (displaced(*out, *in, a->M)) return bad("z or h in place of x or y: the same type and stride required");
+      if (displaced(*out, *in, a->M)) return bad("an output in place of x or y: the same type and stride required");
   const int mods = mod_rows(a->M, a->group);
   CHECK_ROWS(x, ROWS_FLOAT, a->M);
   CHECK_ROWS(y, ROWS_ANY, a->M);
@@ -444,10 +454,11 @@ extern "C" lazymar_status lazymar_join_grad(const lazymar_join_grad_args* a, voi
       return bad("pre needs z and its statistics");
     if ((a->post || a->dgate.p || a->dpost_g) && !a->y.p) return bad("post, dgate and dpost_g need y");
     if (a->post && (!a->y_rstd || (a->post == LAZYMAR_NORM_LAYER && !a->y_mean))) return bad("post needs y's statistics");
-    if (a->dx.p && a->dx.p == a->dy.p) return bad("dx and dy in one place");
-    for (const lazymar_rows* out : {&a->dx, &a->dy})
+    if (twice({a->dx.p, a->dy.p, a->dy8.p, a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b}))
+      return bad("two outputs in one place");
+    for (const lazymar_rows* out : {&a->dx, &a->dy, &a->dy8})
       for (const lazymar_rows* in : {&a->dh, &a->dz, &a->z, &a->y})
-        if (displaced(*out, *in, a->M)) return bad("dx or dy in place of an input: the same type and stride required");
+        if (displaced(*out, *in, a->M)) return bad("dx, dy or dy8 in place of an input: the same type and stride required");
     for (const lazymar_rows* out : {&a->dgate, &a->dscale, &a->dshift})
       for (const lazymar_rows* in : {&a->gate, &a->scale})
         if (out->p && out->p == in->p) return bad("gradients of gate, scale and shift in place of gate or scale");
@@ -603,14 +614,16 @@ lazymar_status params_create(const lazymar_param* list, int count, lazymar_param
   const size_t a = params.size() * sizeof(Param), b = pieces.size() * sizeof(Piece);
   const size_t at_pieces = (a + 255) / 256 * 256, at_partial = at_pieces + (b + 255) / 256 * 256 + 256;
   const size_t bytes = at_partial + (size_t)c.num_sms * kMostNormCtas * sizeof(double) + sizeof(unsigned);
+  std::vector<char> image(bytes, 0);
+  if (a) std::memcpy(image.data(), params.data(), a);
+  if (b) std::memcpy(image.data() + at_pieces, pieces.data(), b);
   lazymar_params* h = new lazymar_params;
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaMalloc(&h->memory, bytes);
   char* m = static_cast<char*>(h->memory);
-  if (e == cudaSuccess) e = cudaMemset(m, 0, bytes);
-  if (e == cudaSuccess && a) e = cudaMemcpy(m, params.data(), a, cudaMemcpyHostToDevice);
-  if (e == cudaSuccess && b) e = cudaMemcpy(m + at_pieces, pieces.data(), b, cudaMemcpyHostToDevice);
-  if (e == cudaSuccess) e = cudaDeviceSynchronize();  // (for calls on streams that do not wait for the default one)
+  if (e == cudaSuccess) e = cudaMemcpy(m, image.data(), bytes, cudaMemcpyHostToDevice);
+  // (done before the calls on streams that do not wait for the default one)
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);
   if (e != cudaSuccess) {
     lazymar_params_destroy(h);
     return e == cudaErrorMemoryAllocation ? report_error(LAZYMAR_ERR_OOM, "device memory of the list") : report_cuda(e, "list");

@@ -204,6 +204,25 @@ def test_join_in_place(D, pad, offset, M):
         assert torch.isnan(t["x"].as_strided((M, pad), (D + pad, 1), t["x"].storage_offset() + D)).all()
 
 
+@pytest.mark.parametrize("M", [40, 900])
+def test_join_8_bit_outputs_in_place(M):
+    """h8 over an 8-bit y, and dy8 over it in the gradient."""
+    torch = torch_cuda()
+    D = 520
+    t, v = make(M, D, 9, eight=True, seed=31)
+    h8 = Held(M, D)
+    kw = dict(group=9, pre=NORM["layer"], eps=EPS)
+    lm.lazymar_join(lm.lazymar_join_args(M, D, h8=lm.lazymar_rows(h8.q, h8.scale), **t, **kw))
+    y = t["y"].keep[0]
+    lm.lazymar_join(lm.lazymar_join_args(M, D, h8=t["y"], **t, **kw))
+    sync()
+    assert torch.equal(y[:, :D], h8.q[:, :D]) and torch.equal(t["y"].keep[1], h8.scale)
+    g = Grad(M, D, 9, "rms", "layer", y="e4m3", seed=32).check()
+    lm.lazymar_join_grad(g.args(dy8=g.t["y"]))
+    sync()
+    assert torch.equal(g.t["y"].keep[0][:, :D], g.dy8.q[:, :D]) and torch.equal(g.t["y"].keep[1], g.dy8.scale)
+
+
 @pytest.mark.parametrize("M,D", [(12, 1000), (1200, 1000), (1200, 999)])
 @pytest.mark.parametrize("post,pre", [("layer", "layer"), ("rms", "rms")])
 def test_join_rows_that_are_not_finite_stay_alone(post, pre, M, D):

@@ -135,6 +135,9 @@ JOIN = [
     (dict(pre_b=256, **X), 1, "need pre"),
     (dict(z_rstd=256, **X), 1, "need pre"),
     (dict(pre=RMS, x=_rows(64), z=_rows(128), h=_rows(128)), 1, "one place"),
+    (dict(y=_rows(256), y8=_rows(512, 2, 16, 8, 640), z8=_rows(512, 2, 16, 8, 640), **X), 1, "one place"),
+    (dict(pre=LAYER, z_mean=256, z_rstd=256, **X), 1, "one place"),
+    (dict(pre=LAYER, y=_rows(96, 2, 16, 8, 512), h8=_rows(96, 2, 32, 8, 512), **X), 1, "in place"),
     (dict(x=_rows(64), z=_rows(64, 1)), 1, "in place"),
     (dict(x=_rows(64), z=_rows(64, 0, 16)), 1, "in place"),
     (dict(x=_rows(64), y=_rows(96, 1), pre=RMS, h=_rows(96, 0)), 1, "in place"),
@@ -173,6 +176,9 @@ JOIN_GRAD = [
     (dict(dgate=_rows(512)), 1, "need y"),
     (dict(post=LAYER, y=_rows(512), y_rstd=16), 1, "y's statistics"),
     (dict(dy=_rows(256)), 1, "one place"),
+    (dict(dscale=_rows(512), dshift=_rows(512)), 1, "one place"),
+    (dict(dpre_g=512, dpre_b=512), 1, "one place"),
+    (dict(y=_rows(512, 2, 16, 8, 640), dy8=_rows(512, 2, 32, 8, 640)), 1, "in place"),
     (dict(dx=_rows(64, 1)), 1, "in place"),
     (dict(dx=_rows(64, 0, 16)), 1, "in place"),
     (dict(dy=_rows(128, 0, 16)), 1, "in place"),
