@@ -14,7 +14,8 @@ namespace {
 // copies into the warps' rings, so that the memory system always has the next ones to
 // deliver while this one's sums are exchanged. Rows of a group follow each other, so
 // the modulation stays in shared memory while a group lasts; STREAMED (groups of one or two rows) it
-// comes with the row. PLAIN: no norm of y and no parameters (the modulated norm of a block).
+// comes with the row. PLAIN: a modulated
+// block's, with y, gate, scale and shift, without a norm of y and parameters.
 // 40960 x 1024, fp32 stream, bf16 branch, three 8-bit outputs, 320 rows a group: 95 us, 5.8 TB/s (floor 81);
 // instructions bound it next to HBM (450 a warp and row). The row in registers without a ring, 16 warps: 223 us. Both
 // norms with parameters, 40000 x 777 in bf16: 104 us (floor 37), elements loaded and stored one by one.
@@ -108,6 +109,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREA
     if (first + s < end) ring.fetch(plan, first + s, s, c0);
 
   const bool post = !PLAIN && p.post != LAZYMAR_NORM_NONE, pre = PLAIN || p.pre != LAZYMAR_NORM_NONE, leads = part == 0 && lane == 0;
+  const bool has_y = PLAIN || p.y.p, has_gate = PLAIN || p.gate.p, has_scale = PLAIN || p.scale.p, has_shift = PLAIN || p.shift.p;
   const float n = (float)min(max(D - c0, 0), kChunk), per_n = n > 0.f ? 1.f / n : 0.f, per_D = 1.f / (float)D;
   // scales of the next row's 8-bit y
   uint32_t next_s = 0;
@@ -120,17 +122,17 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREA
       const int r = p.group > 0 ? row / p.group : 0;
       stop = p.group > 0 ? min(end - r * p.group, p.group) + r * p.group : end;
       float t[8];
-      if (p.gate.p) {
+      if (has_gate) {
         load_row<WHOLE>(p.gate, r, cols, t);
         lane_put(mods, t);
       }
-      if (p.scale.p) {
+      if (has_scale) {
         load_row<WHOLE>(p.scale, r, cols, t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) t[i] += 1.f;
         lane_put(mods + kLaneChunk, t);
       }
-      if (p.shift.p) {
+      if (has_shift) {
         load_row<WHOLE>(p.shift, r, cols, t);
         lane_put(mods + 2 * kLaneChunk, t);
       }
@@ -141,11 +143,11 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREA
     dead |= !__all_sync(0xffffffffu, ok);
     // each piece is read when it is needed, and the stage given on after the last: fewer registers
     float v[8], t[8];
-    const int mod = p.y.p ? Y_STREAM + 1 : Y_STREAM;  // the first stream of the modulation
+    const int mod = has_y ? Y_STREAM + 1 : Y_STREAM;  // the first stream of the modulation
     const auto from = [&](int i, int dtype, uint32_t scale, float (&to)[8]) {
       load_stage<WHOLE>(ring.piece(plan, i, row, c0), dtype, scale, cols, to);
     };
-    if (p.y.p) {
+    if (has_y) {
       from(Y_STREAM, p.y.dtype, s, v);
       if (p.y8.q && !dead) store_row8<WHOLE>(p.y8, row, cols, v);
       if (post) {
@@ -167,7 +169,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREA
         lane_get(params + WPR * kLaneChunk, t);
         add8(v, t);
       }
-      if (p.gate.p) {
+      if (has_gate) {
         if (STREAMED) from(mod, p.gate.dtype, 0, t);
         else lane_get(mods, t);
         mul8(v, t);
@@ -206,8 +208,8 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREA
       lane_get(params + 3 * WPR * kLaneChunk, t);
       add8(v, t);
     }
-    int i = mod + (p.gate.p != nullptr);
-    if (p.scale.p) {
+    int i = mod + (has_gate ? 1 : 0);
+    if (has_scale) {
       if (STREAMED) {
         from(i++, p.scale.dtype, 0, t);
 #pragma unroll
@@ -217,7 +219,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREA
       }
       mul8(v, t);
     }
-    if (p.shift.p) {
+    if (has_shift) {
       if (STREAMED) from(i, p.shift.dtype, 0, t);
       else lane_get(mods + 2 * kLaneChunk, t);
       add8(v, t);

@@ -1,8 +1,8 @@
-// The residual join and its gradient: the norm behind a branch, its gate, the
-// residual addition and the modulated norm in front of the next branch, each tensor
-// read and written once. Bound by HBM bandwidth (13 bytes an element forward with an fp32
-// stream, a bf16 branch and three 8-bit outputs, 17 backward), and next to it by
-// instruction issue.
+// The residual join: the norm behind a branch, its gate, the residual addition and the
+// modulated norm in front of the next branch, each tensor read and written once (13 bytes an element with
+// an fp32 stream, a bf16 branch and three 8-bit outputs). Here the kernel for few rows, up to two an SM, and for more than
+// 4096 columns: the row in the registers of a few warps, all loads under way at once. That of many rows is in
+// join_ring.cuh.
 #include "join_ring.cuh"
 
 namespace lm {
@@ -118,10 +118,12 @@ template <int WPR>
 constexpr int kWarps = WPR == 5 ? 10 : WPR > 8 ? 16 : 8;
 
 // ---------------------------------------------------------------------------
-// Forward
+// Few rows
 // ---------------------------------------------------------------------------
 // WPR warps a row, NC chunks of 256 columns a warp, the row in registers throughout.
-// FULL: D = 256 NC WPR and every row on a boundary, so that no column needs a check.
+// FULL: D = 256 NC WPR and every row on a boundary, so that no column needs a check. Bound by latency: 2 x 1024 with a
+// modulation for each row 3.1 us, 304 x 1024 with three 8-bit outputs 3.9 (through the rings of the other kernel 4.8), 608 rows
+// 4.8 (5.0 there), 1216 rows 7.6 (7.1).
 template <int NC, int WPR, bool FULL>
 __global__ void __launch_bounds__(kWarps<WPR> * 32, NC == 1 ? 3 : 2) join_kernel(const Join p) {
   constexpr int GROUPS = kWarps<WPR> / WPR;
@@ -259,7 +261,8 @@ cudaError_t launch_join(const Ctx& c, const Join& p) {
   if (nc <= 16 && p.M > c.num_sms * 2) {
     const bool whole = p.D % 8 == 0 && on_eight(p.x) && on_eight(p.y) && on_eight(p.gate) && on_eight(p.scale) &&
                        on_eight(p.shift) && on_eight(p.z) && on_eight(p.h) && p.params_vec;
-    const bool plain = !p.post && p.pre && !p.post_g && !p.post_b && !p.pre_g && !p.pre_b;
+    const bool plain = !p.post && p.pre && !p.post_g && !p.post_b && !p.pre_g && !p.pre_b && p.y.p && p.gate.p && p.scale.p &&
+                       p.shift.p;
     return plain ? launch_join_plain(c, p, whole) : join_ring_launch<false>(c, p, whole);
   }
   if (nc <= 1) return join_run<1, 1>(c, p);
