@@ -13,8 +13,8 @@
 // sums, weighted, are those of the parameters.
 // The rows come by bulk copies into a ring in shared memory (join_rows.cuh); a piece is read when it is needed, which
 // keeps a lane's registers to what lets 20 warps live on an SM (24 without sums, 16 with all four).
-// 40960 x 1280 from two 8-bit checkpoints, bf16 dh, fp32 dz, modulation of 320 rows a group, dy in bf16 and 8 bits: 154
-// us, 5.1 TB/s (floor 116), bound by instruction issue (62 %) and the latency of a row's exchange. 16384 x 1024 with a modulation and
+// 40960 x 1280 from two 8-bit checkpoints, bf16 dh, fp32 dz, modulation of 320 rows a group, dy in bf16 and 8 bits: 144
+// us, 5.5 TB/s (floor 116), bound by instruction issue (62 %) and the latency of a row's exchange. 16384 x 1024 with a modulation and
 // its gradients for each row: 81 (floor 69). Both norms, 4801 x 777 in bf16: 32 (floor 6.6), elements loaded and stored one by
 // one, eight rows a team. Two chunks a warp and half the warps: 178 instead of 155; the next row in registers
 // instead of a ring: 574.
@@ -33,8 +33,8 @@ struct JoinSums {
 
 // PLAIN: a modulated block's: dh, dz, z, y, gate, scale, dx and dy given, no norm of y, no parameters and none of their gradients.
 // Warps on an SM, by what a lane keeps: P is not needed then, and ROWWISE no sum at all.
-// (40960 x 1280 with 320 rows a group: 20 warps 155 us, 16 165; from 20 warps on the other forms spill.)
-constexpr int grad_sm_warps(bool plain, bool rowwise) { return plain ? (rowwise ? 24 : 20) : 16; }
+// (40960 x 1280 with 320 rows a group: 20 warps 155 us, 16 165; x 768 15 warps 98, 18 107. More of them spill.)
+constexpr int grad_sm_warps(int wpr, bool plain, bool rowwise) { return plain ? (rowwise ? 24 : wpr == 3 ? 15 : 20) : 16; }
 constexpr int kMostGradWarps = 24;
 constexpr int kTogether = 192;
 
@@ -68,10 +68,10 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, float2* red, int gr
 }
 
 template <int NC, int WPR, bool WHOLE, bool ROWWISE, bool PLAIN>
-__global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) * 32, 1)
+__global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(WPR, PLAIN, ROWWISE)) * 32, 1)
     join_grad_kernel(const __grid_constant__ JoinGrad p, const __grid_constant__ RingPlan plan, const Teams ranges, int together,
                      JoinSums need, unsigned* err) {
-  constexpr int WARPS = cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR, grad_sm_warps(WPR, PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
   // the four parameters (NC 1; of wider rows they stay where they are), each warp's modulation (gate, 1 + scale), the rings
   constexpr int W = NC * WPR * kChunk, PARAMS = PLAIN || NC > 1 ? 0 : 4 * W, MODS = ROWWISE ? 0 : 2 * NC * kLaneChunk;
   constexpr int JOINED = ROWWISE || GROUPS == 1 ? 0 : 4 * W;
@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)) 
 
 template <int NC, int WPR, bool ROWWISE, bool PLAIN>
 cudaError_t join_grad_run(const Ctx& c, const JoinGrad& p, const JoinSums& need, bool whole, const Teams& ranges, bool together) {
-  constexpr int WARPS = cta_warps(WPR, grad_sm_warps(PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
+  constexpr int WARPS = cta_warps(WPR, grad_sm_warps(WPR, PLAIN, ROWWISE)), GROUPS = WARPS / WPR;
   RingPlan plan{};
   if (p.pre != LAZYMAR_NORM_NONE)
     for (const Rows* r : {&p.dh, &p.z}) add_stream(plan, *r, NC * kChunk);

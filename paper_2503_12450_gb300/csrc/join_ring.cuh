@@ -16,14 +16,14 @@ namespace {
 // the modulation stays in shared memory while a group lasts; STREAMED (groups of one or two rows) it
 // comes with the row. PLAIN: a modulated
 // block's, with y, gate, scale and shift, without a norm of y and parameters.
-// 40960 x 1024, fp32 stream, bf16 branch, three 8-bit outputs, 320 rows a group: 95 us, 5.8 TB/s (floor 81);
+// 40960 x 1024, fp32 stream, bf16 branch, three 8-bit outputs, 320 rows a group: 94 us, 5.8 TB/s (floor 81);
 // instructions bound it next to HBM (450 a warp and row). The row in registers without a ring, 16 warps: 223 us. Both
 // norms with parameters, 40000 x 777 in bf16: 104 us (floor 37), elements loaded and stored one by one.
 // Warps on an SM, as many as need no spills, which cost more than more warps give. 40960 x 1024 with three 8-bit
-// outputs: 28 warps 95 us, 24 101; x 1280 30 warps 117, 28 122; with a row of modulation for each row 24 warps 129, 28
-// 143; both norms at 40000 x 1024 in bf16 28 warps 88, 24 93.
+// outputs: 28 warps 94 us, 24 101; x 1280 30 warps 114, 28 122; both norms at 40000 x 1024 in bf16 28 warps 88, 24 93, x 1280 20 warps 120, 25 (which spill) 143. With
+// a row of modulation for each row, which is at HBM's rate, fewer rows at a time are better: 20 warps 121, 24 139.
 constexpr int join_sm_warps(int wpr, bool plain, bool streamed) {
-  return plain ? (streamed ? 24 : wpr >= 3 ? 30 : 28) : (streamed ? 20 : 28);
+  return streamed || (!plain && wpr == 5) ? 20 : plain && wpr >= 3 ? 30 : 28;
 }
 
 // Mean and 1 / deviation of a row of 256 columns a warp, as above. n: the warp's columns, per_n and per_D: 1 / n, 1 / D.
@@ -255,7 +255,7 @@ cudaError_t join_ring_run(const Ctx& c, const Join& p, bool whole) {
 template <bool PLAIN>
 cudaError_t join_ring_launch(const Ctx& c, const Join& p, bool whole) {
   // Fetching the modulation with each row costs more than waiting for it at each group's first, except for very small
-  // groups: 40960 x 1024 in groups of 2 118 us with the rows, 131 without, of 3 117 and 117, of 8 117 and 101.
+  // groups: 40960 x 1024 in groups of 2 120 us with the rows, 131 without, of 3 117 and 117, of 8 117 and 101.
   const bool streamed = p.group > 0 && p.group < 3 && (p.gate.p || p.scale.p || p.shift.p);
 #define LM_RUN(wpr) (streamed ? join_ring_run<wpr, PLAIN, true>(c, p, whole) : join_ring_run<wpr, PLAIN, false>(c, p, whole))
   switch (row_warps(p.D)) {

@@ -125,7 +125,7 @@ constexpr int kWarps = WPR == 5 ? 10 : WPR > 8 ? 16 : 8;
 // modulation for each row 3.1 us, 304 x 1024 with three 8-bit outputs 3.9 (through the rings of the other kernel 4.8), 608 rows
 // 4.8 (5.0 there), 1216 rows 7.6 (7.1).
 template <int NC, int WPR, bool FULL>
-__global__ void __launch_bounds__(kWarps<WPR> * 32, NC == 1 ? 3 : 2) join_kernel(const Join p) {
+__global__ void __launch_bounds__(kWarps<WPR> * 32, NC == 1 ? 3 : WPR > 8 ? 1 : 2) join_kernel(const Join p) {
   constexpr int GROUPS = kWarps<WPR> / WPR;
   __shared__ float2 red[2][GROUPS][WPR];
   __shared__ float stage[FULL ? 1 : kWarps<WPR>][kStage];

@@ -172,7 +172,7 @@ cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
   const bool rowwise = p.group == 1;
   const bool plain = p.pre && !p.post && !p.post_g && !p.post_b && !p.pre_g && !p.pre_b && !need.params && p.dz.p && p.y.p &&
                      p.gate.p && p.scale.p && p.dx.p && p.dy.p;
-  const int each = cta_teams(p.D, grad_sm_warps(plain, rowwise));
+  const int each = cta_teams(p.D, grad_sm_warps(row_warps(p.D), plain, rowwise));
   // (With few rows a group, joining the teams' sums costs more than writing them out: 40960 x 1280 with 64 rows a
   // group 166 us together, 153 apart; with 320 154 and 155, at 768 columns 104 and 121.)
   const bool together = p.group == 0 || p.group >= kTogether;
