@@ -13,7 +13,7 @@
 // sums, weighted, are those of the parameters.
 // The rows come by bulk copies into a ring in shared memory (join_rows.cuh); a piece is read when it is needed, which
 // keeps a lane's registers to what lets 20 warps live on an SM (24 without sums, 16 with all four).
-// 40960 x 1280 from two 8-bit checkpoints, bf16 dh, fp32 dz, modulation of 320 rows a group, dy in bf16 and 8 bits: 144
+// 40960 x 1280 from two 8-bit checkpoints, bf16 dh, fp32 dz, modulation of 320 rows a group, dy in bf16 and 8 bits: 141
 // us, 5.5 TB/s (floor 116), bound by instruction issue (62 %) and the latency of a row's exchange. 16384 x 1024 with a modulation and
 // its gradients for each row: 81 (floor 69). Both norms, 4801 x 777 in bf16: 32 (floor 6.6), elements loaded and stored one by
 // one, eight rows a team. Two chunks a warp and half the warps: 178 instead of 155; the next row in registers
