@@ -156,6 +156,23 @@ def test_join_many_rows(M, D, group, x, y, z, h, mod, pad, offset):
             assert torch_cuda().isnan(a.as_strided((M - 1, pad), (D + pad, 1), a.storage_offset() + D)).all()
 
 
+@pytest.mark.parametrize("pad,offset", [(0, 0), (0, 1), (1, 3)])
+@pytest.mark.parametrize("D,group", [(1, 0), (1, 400), (2, 1), (3, 7), (5, 2), (7, 300)])
+def test_join_and_gradient_of_narrow_rows(D, group, pad, offset):
+    """Several rows lie between two 16-byte boundaries."""
+    M = 1000
+    t, v = make(M, D, group, "bf16", "bf16", "bf16", pad, offset)
+    st = stats(M)
+    z, h = out(M, D, "bf16", pad, offset), out(M, D, "bf16", pad, offset)
+    lm.lazymar_join(lm.lazymar_join_args(M, D, group=group, post=NORM["rms"], pre=NORM["rms"], res=0.75, eps=EPS, z=z, h=h, **t, **st))
+    sync()
+    o = T.join(post="rms", pre="rms", group=group, res=0.75, eps=EPS, **v)
+    b = join_bounds(v, o, "rms", "rms", group, 0.75)
+    close(z, o["z"], rounded(b["z"], o["z"], "bf16"))
+    close(h, o["h"], rounded(b["h"], o["h"], "bf16"))
+    Grad(M, D, group, "rms", "rms", "bf16", "bf16", "bf16", "bf16", "bf16", "bf16", "bf16", pad, offset, seed=21).check()
+
+
 @pytest.mark.parametrize("fields", [("gate",), ("scale",), ("post_g",), ("post_b",), ("pre_g",), ("pre_b",), ("shift",), ()])
 def test_join_with_some_of_its_parts(fields):
     M, D, group = 11, 777, 3
