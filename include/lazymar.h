@@ -604,7 +604,7 @@ typedef struct lazymar_join_args {
   lazymar_rows y;    /* [M, D] fp32, bf16 or E4M3: the branch's output; absent: post, gate, post_g, post_b are too */
   lazymar_rows gate, scale, shift;             /* fp32 or bf16; scale and shift need pre */
   const float *post_g, *post_b, *pre_g, *pre_b; /* [D]; pre_g and pre_b need pre */
-  /* No two outputs in one place; each may be x or y itself, with its type and stride. */
+  /* No two outputs in one place; z, h, h8, z8 and y8 may each be x or y itself, with its type and stride, and no other input. */
   lazymar_rows z;    /* [M, D] fp32 or bf16 */
   lazymar_rows h;    /* [M, D] fp32 or bf16 */
   lazymar_rows h8, z8, y8; /* E4M3: h as the operand of lazymar_block8_linear, z and y as checkpoints */
@@ -637,7 +637,8 @@ typedef struct lazymar_join_grad_args {
   lazymar_rows gate, scale;
   const float *post_g, *post_b, *pre_g, *pre_b;
   const float *y_mean, *y_rstd, *z_mean, *z_rstd;  /* of the norms that there are; means not with LAZYMAR_NORM_RMS */
-  /* Any of these may be absent, dx, dy and dy8 each dz, dh, z or y itself with its type and stride; no two in one place. */
+  /* Any of these may be absent, dx, dy and dy8 each dz, dh, z or y itself with its type and stride, and no other input;
+   * no two in one place. */
   lazymar_rows dx;   /* [M, D] fp32 or bf16 */
   lazymar_rows dy;   /* [M, D] fp32 or bf16 */
   lazymar_rows dy8;  /* [M, D] E4M3: dy as the operand of the input gradient's product */
@@ -671,7 +672,7 @@ typedef struct lazymar_param {
 
 /* A list of `count` tensors, on the current device. The handle keeps the
  * addresses (not the values) in device memory, so the tensors stay where they are
- * while it lives; tensors of a list do not overlap. The calls on it take its
+ * while it lives; tensors of a list do not overlap (out may be g). The calls on it take its
  * own scratch: one stream at a time, and no two graphs that run at once.
  * At most 2^20 tensors and 2^40 elements. A tensor's addresses that are as far from a boundary
  * of eight elements as its gradient's are faster. Creating a list waits for the default stream; not during
@@ -693,7 +694,7 @@ typedef struct lazymar_step_state {
  * steps += 1; where the norm is not finite (an infinity or NaN among the gradients, or
  * 2^128 and more) factor = 0 and skipped += 1 instead. scale > 0 (1 / loss scale, 1 / number
  * of accumulated batches), max_norm > 0, infinity: no clipping. Squares do not
- * overflow or vanish at any size of the gradients; sums are fp64, the same from
+ * overflow or vanish at any size of the gradients; sums are held in two fp32 numbers or in fp64, the same from
  * call to call. */
 lazymar_status lazymar_grad_norm(lazymar_params* h, float scale, float max_norm, lazymar_step_state* state, void* stream);
 

@@ -42,7 +42,7 @@ __device__ __forceinline__ long long offset_of(const Param& t, const Piece& q) {
 // Squares are summed in fp32 over eight elements, and those sums in two fp32 numbers (the sum and what its roundings
 // have lost), because one conversion to fp64 and one addition for every 16 elements already bound the norm of bf16
 // gradients (403 million: 292 us, floor 119). Where a sum of eight says that squares may have left fp32's range, or that the
-// sum of all could (from 2^96 on, or below 2^-90 without being a sum of zeros), they are squared in fp64.
+// sum of all could (from 2^96 on, or below 2^-90 without being all zeros), they are squared in fp64.
 struct Squares {
   float sum = 0.f, lost = 0.f;
   double rest = 0.0;
@@ -54,7 +54,11 @@ struct Squares {
       lost += (sum - (t - b)) + (s - b);
       sum = t;
     } else {
-      for (int i = 0; i < 8; ++i) rest += (double)a[i] * a[i];
+      uint32_t any = 0;  // (gradients that are all zero, as behind a gate of zero, stay cheap)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) any |= __float_as_uint(a[i]) << 1;
+      if (any)
+        for (int i = 0; i < 8; ++i) rest += (double)a[i] * a[i];
     }
   }
   __device__ __forceinline__ double total() const { return rest + (double)sum + (double)lost; }

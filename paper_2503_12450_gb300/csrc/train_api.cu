@@ -5,10 +5,12 @@
 #include "join.cuh"
 #include "optim.cuh"
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <initializer_list>
 #include <new>
+#include <utility>
 #include <vector>
 
 using namespace lm;
@@ -344,7 +346,16 @@ lazymar_block8 eight_of(const lazymar_rows& r) { return lazymar_block8{r.p, r.sc
 // An output in place of an input: rows are worked on side by side, so in another layout they
 // would overwrite rows that are still to be read.
 bool displaced(const lazymar_rows& out, const lazymar_rows& in, int M) {
-  return out.p && out.p == in.p && (out.dtype != in.dtype || (M > 1 && out.ld != in.ld));
+  return out.p && out.p == in.p &&
+         (out.dtype != in.dtype || (M > 1 && out.ld != in.ld) ||
+          (out.dtype == LAZYMAR_E4M3 && out.scale == in.scale && out.lds != in.lds));
+}
+// An output in place of an input that several rows, or several kernels, read.
+bool shared(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+  for (const void* o : outputs)
+    for (const void* i : inputs)
+      if (o && o == i) return true;
+  return false;
 }
 // Two outputs in one place.
 bool twice(std::initializer_list<const void*> outputs) {
@@ -386,6 +397,10 @@ extern "C" lazymar_status lazymar_join(const lazymar_join_args* a, void* stream)
   for (const lazymar_rows* out : {&a->z, &a->h, &a->h8, &a->z8, &a->y8})
     for (const lazymar_rows* in : {&a->x, &a->y})
       if (displaced(*out, *in, a->M)) return bad("an output in place of x or y: the same type and stride required");
+  if (shared({a->z.p, a->h.p, a->h8.p, a->z8.p, a->y8.p, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd},
+             {a->gate.p, a->scale.p, a->shift.p, a->post_g, a->post_b, a->pre_g, a->pre_b}) ||
+      shared({a->y_mean, a->y_rstd, a->z_mean, a->z_rstd}, {a->x.p, a->y.p}))
+    return bad("an output in place of an input other than x or y");
   const int mods = mod_rows(a->M, a->group);
   CHECK_ROWS(x, ROWS_FLOAT, a->M);
   CHECK_ROWS(y, ROWS_ANY, a->M);
@@ -459,9 +474,11 @@ extern "C" lazymar_status lazymar_join_grad(const lazymar_join_grad_args* a, voi
     for (const lazymar_rows* out : {&a->dx, &a->dy, &a->dy8})
       for (const lazymar_rows* in : {&a->dh, &a->dz, &a->z, &a->y})
         if (displaced(*out, *in, a->M)) return bad("dx, dy or dy8 in place of an input: the same type and stride required");
-    for (const lazymar_rows* out : {&a->dgate, &a->dscale, &a->dshift})
-      for (const lazymar_rows* in : {&a->gate, &a->scale})
-        if (out->p && out->p == in->p) return bad("gradients of gate, scale and shift in place of gate or scale");
+    if (shared({a->dx.p, a->dy.p, a->dy8.p, a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b},
+               {a->gate.p, a->scale.p, a->post_g, a->post_b, a->pre_g, a->pre_b, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd}) ||
+        shared({a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b},
+               {a->dh.p, a->dz.p, a->z.p, a->y.p}))
+      return bad("an output in place of an input, other than dx, dy and dy8 of dz, dh, z and y");
     CHECK_ROWS(dh, ROWS_FLOAT, a->M);
     CHECK_ROWS(dz, ROWS_FLOAT, a->M);
     CHECK_ROWS(z, ROWS_ANY, a->M);
@@ -583,6 +600,28 @@ Param param_of(const lazymar_param& t) {
   return p;
 }
 
+// Whether tensors of a list overlap, other than an out that is its g. (A weight that is in it twice would be updated by
+// two threads at once.)
+bool overlaps(const lazymar_param* list, int count) {
+  std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+  const auto add = [&](const void* p, long long n, size_t e) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    if (p) spans.emplace_back(at, at + (uintptr_t)n * e);
+  };
+  for (int i = 0; i < count; ++i) {
+    const lazymar_param& t = list[i];
+    if (t.n == 0) continue;
+    add(t.g, t.n, elem(t.g_dtype));
+    if (t.out != t.g) add(t.out, t.n, elem(t.out_dtype));
+    for (const float* p : {t.p, t.m, t.v, t.ema}) add(p, t.n, 4);
+    add(t.copy, t.n, 2);
+  }
+  std::sort(spans.begin(), spans.end());
+  for (size_t i = 1; i < spans.size(); ++i)
+    if (spans[i].first < spans[i - 1].second) return true;
+  return false;
+}
+
 lazymar_status params_create(const lazymar_param* list, int count, lazymar_params** out) {
   bool weights = false;
   long long total = 0;
@@ -592,6 +631,7 @@ lazymar_status params_create(const lazymar_param* list, int count, lazymar_param
     total += list[i].n;
     if (total > (1ll << 40)) return report_error(LAZYMAR_ERR_UNSUPPORTED, "at most 2^40 elements");
   }
+  if (overlaps(list, count)) return bad("tensors of a list overlap");
   // pieces of a multiple of kPiece, at most about kMostPieces of them
   const long long piece = kPiece * (1 + total / (kPiece * kMostPieces));
   std::vector<Param> params;

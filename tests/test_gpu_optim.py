@@ -322,6 +322,35 @@ def test_adamw_needs_weights():
     h.close()
 
 
+def test_lists_refuse_overlapping_tensors():
+    """A weight that is in a list twice would be updated twice at once."""
+    torch = torch_cuda()
+    new = lambda: torch.zeros(100, device="cuda")  # noqa: E731
+    one = lambda **k: dict(dict(g=new(), p=new(), m=new(), v=new()), **k)  # noqa: E731
+    a, buf = one(), torch.zeros(300, device="cuda")
+    for entries in ([a, a], [a, one(p=a["p"])], [one(m=a["m"], v=a["m"])], [one(g=buf[:100], p=buf[99:199])], [one(out=a["p"], p=a["p"])],
+                    [one(), one(p=buf[:100], ema=buf[50:150])]):
+        with pytest.raises(lm.LazymarError, match="overlap"):
+            lm.lazymar_params_create(entries)
+    lm.lazymar_params_create([one(g=buf[:100], p=buf[100:200], m=buf[200:300]), one(out=None)]).close()
+    g = new()
+    lm.lazymar_params_create([dict(g=g, out=g), dict(g=buf[:0]), dict(g=buf[:100], out=buf[100:200])]).close()
+
+
+def test_norm_of_zeros_with_a_few_others():
+    torch = torch_cuda()
+    for t in (torch.float32, torch.bfloat16):
+        x = torch.zeros(200001, dtype=t, device="cuda")
+        h, s = lm.lazymar_params_create([dict(g=x)]), state()
+        for values in ({}, {17: 1e-38, 199999: -1e-38}, {5: -0.0, 100000: 3.0}):
+            x.zero_()
+            for i, w in values.items():
+                x[i] = w
+            want = math.sqrt(float((x.double() ** 2).sum()))
+            lm.lazymar_grad_norm(h, s, math.inf)
+            assert abs(read(s)[0] - want) <= 2 * U * want  # the squares' sum is exact, or in fp64
+
+
 def test_lists_mix_tensors_with_and_without_averages():
     torch = torch_cuda()
     e, vals, _ = weights([4096, 4096, 100], seed=7)

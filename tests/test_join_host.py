@@ -142,6 +142,10 @@ JOIN = [
     (dict(x=_rows(64), z=_rows(64, 0, 16)), 1, "in place"),
     (dict(x=_rows(64), y=_rows(96, 1), pre=RMS, h=_rows(96, 0)), 1, "in place"),
     (dict(x=_rows(64), y=_rows(96, 2, 16, 8, 512), z=_rows(96, 1, 16)), 1, "in place"),
+    (dict(y=_rows(96, 2, 16, 8, 512), y8=_rows(96, 2, 16, 16, 512), **X), 1, "in place"),
+    (dict(y=_rows(96), gate=_rows(128), **X), 1, "in place"),
+    (dict(pre=LAYER, pre_g=256, x=_rows(64), h=_rows(256)), 1, "in place"),
+    (dict(pre=LAYER, x=_rows(64), z_rstd=64), 1, "in place"),
     (dict(x=_rows(64, 2, 16, 8, 512), z=_rows(128)), 1, "x:"),
     (dict(x=_rows(64, 0, 7), z=_rows(128)), 1, "x:"),
     (dict(x=_rows(66), z=_rows(128)), 1, "x:"),
@@ -184,6 +188,11 @@ JOIN_GRAD = [
     (dict(dy=_rows(128, 0, 16)), 1, "in place"),
     (dict(scale=_rows(512), dscale=_rows(512)), 1, "in place"),
     (dict(gate=_rows(512), y=_rows(640), dshift=_rows(512)), 1, "in place"),
+    (dict(scale=_rows(256)), 1, "in place"),
+    (dict(pre_g=512, dpre_g=512), 1, "in place"),
+    (dict(dshift=_rows(64)), 1, "in place"),
+    (dict(dpre_b=16), 1, "in place"),
+    (dict(y=_rows(512, 2, 16, 8, 640), dy8=_rows(512, 2, 16, 16, 640)), 1, "in place"),
     (dict(dh=_rows(64, 2, 16, 8, 512)), 1, "dh:"),
     (dict(dh=_rows(64, 0, 4)), 1, "dh:"),
 ]
