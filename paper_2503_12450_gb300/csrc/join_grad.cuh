@@ -14,10 +14,10 @@
 // The rows come by bulk copies into a ring in shared memory (join_rows.cuh); a piece is read when it is needed, which
 // keeps a lane's registers to what lets 20 warps live on an SM (24 without sums, 16 with all four).
 // 40960 x 1280 from two 8-bit checkpoints, bf16 dh, fp32 dz, modulation of 320 rows a group, dy in bf16 and 8 bits: 141
-// us, 5.5 TB/s (floor 116), bound by instruction issue (62 %) and the latency of a row's exchange. 16384 x 1024 with a modulation and
-// its gradients for each row: 81 (floor 69). Both norms, 4801 x 777 in bf16: 32 (floor 6.6), elements loaded and stored one by
-// one, eight rows a team. Two chunks a warp and half the warps: 178 instead of 155; the next row in registers
-// instead of a ring: 574.
+// us, 5.6 TB/s (floor 116), bound by instruction issue (57 % under ncu) and the latency of a row's exchange. 16384 x 1024
+// with a modulation and its gradients for each row: 81 (floor 69). Both norms, 4801 x 777 in bf16: 33 (floor 6.6),
+// elements loaded and stored one by one, eight rows a team. Two chunks a warp and half the warps: 178 where one chunk
+// took 155; the next row in registers instead of a ring: 574.
 #pragma once
 
 #include "join_rows.cuh"
@@ -33,7 +33,7 @@ struct JoinSums {
 
 // PLAIN: a modulated block's: dh, dz, z, y, gate, scale, dx and dy given, no norm of y, no parameters and none of their gradients.
 // Warps on an SM, by what a lane keeps: P is not needed then, and ROWWISE no sum at all.
-// (40960 x 1280 with 320 rows a group: 20 warps 155 us, 16 165; x 768 15 warps 98, 18 107. More of them spill.)
+// (40960 x 1280 with 320 rows a group: 20 warps 141 us, 16 152; x 768 15 warps 96, 18 105. More of them spill.)
 constexpr int grad_sm_warps(int wpr, bool plain, bool rowwise) { return plain ? (rowwise ? 24 : wpr == 3 ? 15 : 20) : 16; }
 constexpr int kMostGradWarps = 24;
 constexpr int kTogether = 192;

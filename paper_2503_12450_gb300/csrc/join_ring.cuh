@@ -20,8 +20,9 @@ namespace {
 // instructions bound it next to HBM (450 a warp and row). The row in registers without a ring, 16 warps: 223 us. Both
 // norms with parameters, 40000 x 777 in bf16: 104 us (floor 37), elements loaded and stored one by one.
 // Warps on an SM, as many as need no spills, which cost more than more warps give. 40960 x 1024 with three 8-bit
-// outputs: 28 warps 94 us, 24 101; x 1280 30 warps 114, 28 122; both norms at 40000 x 1024 in bf16 28 warps 88, 24 93, x 1280 20 warps 120, 25 (which spill) 143. With
-// a row of modulation for each row, which is at HBM's rate, fewer rows at a time are better: 20 warps 121, 24 139.
+// outputs: 28 warps 94 us, 24 101; x 1280 30 warps 114, 28 122; both norms at 40000 x 1024 in bf16 28 warps 88, 24 93, x 1280
+// 20 warps 120, 25 (which spill) 143. With a row of modulation for each row, which is at HBM's rate, fewer rows at a
+// time are better: 20 warps 121, 24 139.
 constexpr int join_sm_warps(int wpr, bool plain, bool streamed) {
   return streamed || (!plain && wpr == 5) ? 20 : plain && wpr >= 3 ? 30 : 28;
 }
@@ -90,7 +91,8 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREA
   RowRing<WHOLE, STREAMED> ring;
   float* const params = row_smem + part * kLaneChunk;
   float* const mods = row_smem + PARAMS + warp * MODS;
-  ring.init(reinterpret_cast<uint8_t*>(row_smem + PARAMS + WARPS * MODS) + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(kChunk, D - c0), p.M, D, first);
+  uint8_t* const rings = reinterpret_cast<uint8_t*>(row_smem + PARAMS + WARPS * MODS);
+  ring.init(rings + (size_t)warp * plan.depth * plan.stage, bars[warp], plan, c0, min(kChunk, D - c0), p.M, D, first);
   pdl_wait();
   pdl_trigger();
   if (!PLAIN && grp == 0) {

@@ -414,7 +414,7 @@ inline void set_depth(RingPlan& plan, int room, int warps) {
 
 // Warps of a row of D columns, and of a CTA: whole teams, one CTA an SM, so that parameters are in
 // shared memory once, and that the SM's four schedulers have as many warps each (with CTAs of one team of
-// five warps 40960 x 1280 took 200 us instead of 154).
+// five warps 40960 x 1280 took 200 us where this took 154).
 inline int row_warps(int D) {
   const int nc = (D + kChunk - 1) / kChunk;
   return nc <= 5 ? nc : nc <= 8 ? 8 : 16;

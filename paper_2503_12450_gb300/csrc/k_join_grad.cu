@@ -35,7 +35,8 @@ __global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __gr
   const bool param = result < 4;
   float* const params[4] = {p.dpre_b, p.dpre_g, p.dpost_b, p.dpost_g};
   MatOut o = result == 4 ? p.dshift : result == 5 ? p.dscale : p.dgate;
-  const float *g = result == 5 ? p.pre_g : result == 6 ? p.post_g : nullptr, *b = result == 5 ? p.pre_b : result == 6 ? p.post_b : nullptr;
+  const float* const g = result == 5 ? p.pre_g : result == 6 ? p.post_g : nullptr;
+  const float* const b = result == 5 ? p.pre_b : result == 6 ? p.post_b : nullptr;
   if (param) o = MatOut{params[result], 0, LAZYMAR_F32, true};
   if (!o.p || (param && q > 0)) return;
   // sums of the result: k0 and, times the shift b, k1
@@ -93,7 +94,8 @@ __global__ void __launch_bounds__(128) join_grad_groups_kernel(const __grid_cons
   pdl_wait();
   pdl_trigger();
   const MatOut o = result == 0 ? p.dshift : result == 1 ? p.dscale : p.dgate;
-  const float *g = result == 1 ? p.pre_g : result == 2 ? p.post_g : nullptr, *b = result == 1 ? p.pre_b : result == 2 ? p.post_b : nullptr;
+  const float* const g = result == 1 ? p.pre_g : result == 2 ? p.post_g : nullptr;
+  const float* const b = result == 1 ? p.pre_b : result == 2 ? p.post_b : nullptr;
   const int k0 = result == 0 ? SUM_A : result == 1 ? SUM_B : SUM_Q;
   if (!o.p) return;
   int q = y;
@@ -197,7 +199,8 @@ cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
                      p.gate.p && p.scale.p && p.dx.p && p.dy.p;
   const int each = cta_teams(p.D, grad_sm_warps(row_warps(p.D), plain, rowwise));
   // (With few rows a group, joining the teams' sums costs more than writing them out: 40960 x 1280 with 64 rows a
-  // group 166 us together, 153 apart; with 320 154 and 155, at 768 columns 104 and 121.)
+  // group 153 us together, 144 apart; with 320 141 and 142, and of 5000 rows 28 and 41, because a group then has five
+  // times as many ranges.)
   const bool together = p.group == 0 || p.group >= kTogether;
   const Teams ranges = teams_of(p.M, together ? kSMs : kSMs * each);
   const int groups = p.group > 0 ? (p.M - 1) / p.group + 1 : 1;
