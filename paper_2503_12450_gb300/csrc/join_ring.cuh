@@ -66,7 +66,7 @@ __device__ __forceinline__ void ring_moments(const float (&v)[8], bool layer, co
       }
     }
   }
-  rstd = rsqrtf(fmaf(q, per_D, eps));
+  rstd = inv_sqrt(fmaf(q, per_D, eps));
 }
 
 enum { X_STREAM = 0, Y_STREAM = 1 };  // then gate, scale, shift as they are there (STREAMED)

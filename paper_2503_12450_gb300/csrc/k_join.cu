@@ -111,7 +111,7 @@ __device__ __forceinline__ void moments(const float (&v)[NC][8], bool layer, int
       q += r.y + columns(i) * off * off;
     }
   }
-  rstd = rsqrtf(q / (float)D + eps);
+  rstd = inv_sqrt(q / (float)D + eps);
 }
 
 template <int WPR>
