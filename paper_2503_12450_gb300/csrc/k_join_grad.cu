@@ -18,18 +18,17 @@ __device__ __forceinline__ void put_one(const MatOut& o, unsigned row, int col, 
   }
 }
 
-// Sums over many partial rows: of the CTAs where all rows share one modulation or none does, otherwise of the
-// teams, all of them for the parameters, those that a group of very many rows is divided among for the
-// modulation. A CTA has 32 columns of one result (blockIdx.y: 0..3 dpre_b, dpre_g, dpost_b, dpost_g; 4..6 dshift,
-// dscale, dgate) of one group (blockIdx.z); each of 32 slices adds every 32nd partial row, and the slices are
-// added in order. Short chains of loads: it is all latency.
+// Sums over all partial rows: of the parameters, and of the modulation where all rows share one. Partial rows
+// are of the CTAs where all rows share one modulation or none does, otherwise of the ranges. A CTA has 32
+// columns of one result (blockIdx.y: 0..3 dpre_b, dpre_g, dpost_b, dpost_g; 4..6 dshift, dscale, dgate); each of 32
+// slices adds every 32nd partial row, and the slices are added in order. Short chains of loads: it is all latency.
 constexpr int kSlices = 32;
 
-__global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __grid_constant__ JoinGrad p, const Teams teams,
-                                                                      int ctas, int first_result) {
+__global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __grid_constant__ JoinGrad p, int ranges, int ctas,
+                                                                      int first_result) {
   __shared__ float red[2][kSlices][32];
   const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + lane, D = p.D;
-  const int result = (int)blockIdx.y + first_result, q = (int)blockIdx.z;
+  const int result = (int)blockIdx.y + first_result, n = ctas ? ctas : ranges;
   pdl_wait();
   pdl_trigger();
   const bool param = result < 4;
@@ -38,23 +37,14 @@ __global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __gr
   const float* const g = result == 5 ? p.pre_g : result == 6 ? p.post_g : nullptr;
   const float* const b = result == 5 ? p.pre_b : result == 6 ? p.post_b : nullptr;
   if (param) o = MatOut{params[result], 0, LAZYMAR_F32, true};
-  if (!o.p || (param && q > 0)) return;
+  if (!o.p) return;
   // sums of the result: k0 and, times the shift b, k1
   const int k0 = param ? result : result == 4 ? SUM_A : result == 5 ? SUM_B : SUM_Q, k1 = k0 - 1;
-  int t0 = 0, t1 = (ctas ? ctas : teams.n) - 1, g0 = 0;
-  if (!param && !ctas) {
-    g0 = q * p.group;
-    t0 = team_of(teams, g0);
-    t1 = team_of(teams, g0 + min(p.group, p.M - g0) - 1);
-    if (t0 == t1) return;  // (done there)
-  }
   float s0 = 0.f, s1 = 0.f;
   if (col < D) {
 #pragma unroll 4
-    for (int t = t0 + slice; t <= t1; t += kSlices) {
-      const float* w = p.ws + (ctas    ? (size_t)t * 4 * D
-                               : param ? ((size_t)teams.n * 8 + (size_t)t * 4) * D
-                                       : ((size_t)t * 2 + (g0 > team_start(teams, t))) * 4 * D);
+    for (int t = slice; t < n; t += kSlices) {
+      const float* w = p.ws + ((ctas ? 0 : (size_t)ranges * 8) + (size_t)t * 4) * D;
       s0 += w[(size_t)k0 * D + col];
       if (b) s1 += w[(size_t)k1 * D + col];
     }
@@ -77,17 +67,18 @@ __global__ void __launch_bounds__(32 * kSlices) join_grad_sums_kernel(const __gr
   }
   if (g) s0 *= g[col];
   if (b) s0 = fmaf(b[col], s1, s0);
-  put_one(o, param ? 0u : (unsigned)q, col, s0, p.accumulate);
+  put_one(o, 0u, col, s0, p.accumulate);
 }
 
-// Sums of the groups that a few neighbouring ranges share: a warp has 128 columns of one result (dshift, dscale, dgate) of one
-// group; with SLICES 4 (groups in four ranges or more on average) a CTA's four warps add every fourth range. Groups are counted one by
-// one, or where there are more of them than ranges, by the ranges that begin inside one. All loads of a step are
-// under way at once, without branches: 2000 x 1280 with 320 rows a group, where 22 ranges share one, 19 us with the gradient's
-// kernel before it; range after range, with a branch for each sum, 49.
+// Sums of the groups that several neighbouring ranges share: a warp has 128 columns of one result (dshift, dscale, dgate) of
+// one group, and adds every SLICES-th range's: four warps share the ranges of a group where it has four or more on average,
+// 16 where it has 32 or more. Groups are counted one by one, or where there are more of them than ranges, by the ranges that begin
+// inside one. All loads of a step are under way at once, without branches: 2000 x 1280 with 320 rows a group, where 22 ranges share
+// one, 19 us with the gradient's kernel before it; range after range, with a branch for each sum, 49.
 template <int SLICES>
-__global__ void __launch_bounds__(128) join_grad_groups_kernel(const __grid_constant__ JoinGrad p, const Teams teams, int groups) {
-  __shared__ float red[2][4][128];
+__global__ void __launch_bounds__(SLICES == 1 ? 128 : 32 * SLICES)
+    join_grad_groups_kernel(const __grid_constant__ JoinGrad p, const Teams teams, int groups) {
+  __shared__ float red[2][SLICES][128];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x * 128 + lane, D = p.D;
   const int y = SLICES == 1 ? (int)blockIdx.y * 4 + warp : (int)blockIdx.y, slice = SLICES == 1 ? 0 : warp;
   const int group = p.group, result = (int)blockIdx.z;
@@ -198,11 +189,11 @@ cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
   const bool plain = p.pre && !p.post && !p.post_g && !p.post_b && !p.pre_g && !p.pre_b && !need.params && p.dz.p && p.y.p &&
                      p.gate.p && p.scale.p && p.dx.p && p.dy.p;
   const int each = cta_teams(p.D, grad_sm_warps(row_warps(p.D), plain, rowwise));
-  // (With few rows a group, joining the teams' sums costs more than writing them out: 40960 x 1280 with 64 rows a
-  // group 153 us together, 144 apart; with 320 141 and 142, and of 5000 rows 28 and 41, because a group then has five
-  // times as many ranges.)
+  // (Joining the teams' sums costs where groups are short, and gains where few rows are divided among many ranges: 40960
+  // x 1280 with 64 rows a group 153 us together, 144 apart; with 320 141 and 142, and of 320 rows 8.5 and 11.8.)
   const bool together = p.group == 0 || p.group >= kTogether;
-  const Teams ranges = teams_of(p.M, together ? kSMs : kSMs * each);
+  const int each_cta = (p.M - 1) / each + 1;  // CTAs of one row a team
+  const Teams ranges = teams_of(p.M, together ? (each_cta < kSMs ? each_cta : kSMs) : kSMs * each);
   const int groups = p.group > 0 ? (p.M - 1) / p.group + 1 : 1;
   const bool whole = p.D % 8 == 0 && on_eight(p.dh) && on_eight(p.dz) && on_eight(p.z) && on_eight(p.y) &&
                      on_eight(p.gate) && on_eight(p.scale) && on_eight(p.dx) && on_eight(p.dy) && on_eight(p.dgate) &&
@@ -214,18 +205,20 @@ cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {
   if (e != cudaSuccess) return e;
   // partial rows of CTAs (one group or none), otherwise of ranges
   const int ctas = p.group > 1 ? 0 : together ? ranges.n : (ranges.n + each - 1) / each;
-  const bool divided = !rowwise && need.mods && (ctas || ranges.n > 1), many = divided && (ctas || ranges.n / groups >= kSlices);
-  if (need.params || many)
-    e = launch_pdl(join_grad_sums_kernel,
-                   dim3((unsigned)((p.D + 31) / 32), (many ? 7u : 4u) - (need.params ? 0u : 4u), many ? (unsigned)groups : 1u),
-                   dim3(32 * kSlices), 0, c.stream, p, ranges, ctas, need.params ? 0 : 4);
-  if (e != cudaSuccess || !divided || many) return e;
-  const int tasks = groups < ranges.n ? groups : ranges.n - 1;
-  const auto run = [&](auto kernel, int of_cta) {
-    return launch_pdl(kernel, dim3((unsigned)((p.D + 127) / 128), (unsigned)((tasks + of_cta - 1) / of_cta), 3), dim3(128), 0,
-                      c.stream, p, ranges, groups);
+  const bool one = p.group == 0 && need.mods;
+  if (need.params || one)
+    e = launch_pdl(join_grad_sums_kernel, dim3((unsigned)((p.D + 31) / 32), (one ? 7u : 4u) - (need.params ? 0u : 4u)),
+                   dim3(32 * kSlices), 0, c.stream, p, ranges.n, ctas, need.params ? 0 : 4);
+  if (e != cudaSuccess || ctas || !need.mods || ranges.n == 1) return e;
+  const int tasks = groups < ranges.n ? groups : ranges.n - 1, shared = ranges.n / groups;
+  const auto run = [&](auto kernel, int slices) {
+    const int of_cta = slices == 1 ? 4 : 1;
+    return launch_pdl(kernel, dim3((unsigned)((p.D + 127) / 128), (unsigned)((tasks + of_cta - 1) / of_cta), 3),
+                      dim3(slices == 1 ? 128 : 32 * slices), 0, c.stream, p, ranges, groups);
   };
-  return ranges.n / groups >= 4 ? run(join_grad_groups_kernel<4>, 1) : run(join_grad_groups_kernel<1>, 4);
+  return shared >= 32 ? run(join_grad_groups_kernel<16>, 16)
+         : shared >= 4 ? run(join_grad_groups_kernel<4>, 4)
+                       : run(join_grad_groups_kernel<1>, 1);
 }
 
 }  // namespace lm
