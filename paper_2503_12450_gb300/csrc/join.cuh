@@ -2,6 +2,7 @@
 #pragma once
 
 #include "block8.cuh"
+#include "join_host.h"
 
 namespace lm {
 
@@ -36,7 +37,7 @@ struct JoinGrad {
   lazymar_block8 dy8;
   MatOut dgate, dscale, dshift;
   float *dpost_g, *dpost_b, *dpre_g, *dpre_b;
-  float* ws;
+  float* ws;  // on a boundary of kSumsAlign bytes
 };
 
 cudaError_t launch_join(const Ctx& c, const Join& p);

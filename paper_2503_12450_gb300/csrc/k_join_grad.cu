@@ -168,7 +168,7 @@ int cta_teams(int D, int sm_warps) { return cta_warps(row_warps(D), sm_warps) / 
 size_t join_grad_workspace(int M, int D, int group) {
   if (M < 1 || D < 1 || D > kLnMaxWidth || group < 0) return 0;
   const size_t rows = group > 1 ? 12 * (size_t)teams_of(M, kSMs * cta_teams(D, kMostGradWarps)).n : 4 * (size_t)kSMs;
-  return rows * D * sizeof(float);
+  return join_sums_bytes(rows * D);
 }
 
 cudaError_t launch_join_grad(const Ctx& c, const JoinGrad& p) {

@@ -535,7 +535,7 @@ extern "C" lazymar_status lazymar_join_grad(const lazymar_join_grad_args* a, voi
   p.dpost_b = a->dpost_b;
   p.dpre_g = a->dpre_g;
   p.dpre_b = a->dpre_b;
-  p.ws = static_cast<float*>(a->workspace);
+  p.ws = join_sums_at(a->workspace);
   return done(launch_join_grad(c, p), "residual join gradient kernel");
 }
 
