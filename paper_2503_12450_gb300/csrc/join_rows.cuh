@@ -294,7 +294,8 @@ __device__ __forceinline__ float inv_sqrt(float a) {
 // A warp's ring of row pieces: its columns of every tensor, `depth` rows ahead, by bulk
 // copies, one lane a tensor. Pieces that are not on 16-byte boundaries are copied from the
 // boundary before to the one behind, which are the row's neighbours' bytes; where those are not the
-// tensor's (before its first element, behind its last: rows of a few bytes have several such), the piece comes element by element.
+// tensor's (before its first element, behind its last: rows of a few bytes have several such, and so has a row whose last
+// piece is of a few bytes), the piece comes element by element.
 // ---------------------------------------------------------------------------
 // DIVIDED: some tensors have a row for each group of rows; otherwise a lane's pointer moves on by a row each time.
 template <bool WHOLE, bool DIVIDED>
@@ -308,7 +309,7 @@ struct RowRing {
   uintptr_t src;
   size_t pitch;
   uint32_t bytes, total, magic, shift;
-  uintptr_t lowest, behind;  // where the tensor's first row starts, if this piece is a row's first, and where its last one ends
+  uintptr_t lowest, tensor_end;  // where the tensor's first row starts, and where its last one ends
 
   // first: the first row that will be fetched; step: from one to the next
   __device__ __forceinline__ void init(uint8_t* smem, uint64_t* b, const RingPlan& plan, int first_column, int columns, int M, int D,
@@ -327,8 +328,8 @@ struct RowRing {
       magic = t.magic;
       shift = t.shift;
       bytes = (uint32_t)max(mine, 0) * t.e;
-      lowest = first_column == 0 ? src : 0;
-      behind = first_column + columns == D ? src + (size_t)stream_row(magic, shift, M - 1) * pitch + bytes : ~(uintptr_t)0;
+      lowest = reinterpret_cast<uintptr_t>(t.p);
+      tensor_end = rows_end(lowest, stream_row(magic, shift, M - 1), pitch, D, t.e);
       if (!DIVIDED) {
         src += (size_t)(unsigned)first * pitch;
         pitch *= (unsigned)step;
@@ -353,7 +354,7 @@ struct RowRing {
     uint32_t n = bytes, sum = total;
     bool copies = lane < plan.n;
     if (!WHOLE) {
-      const bool outside = copies && ((p & ~(uintptr_t)15) < lowest || ((p + bytes + 15) & ~(uintptr_t)15) > behind);
+      const bool outside = copies && piece_reaches_out(p, bytes, lowest, tensor_end);
       for (unsigned them = __ballot_sync(0xffffffffu, outside); them; them &= them - 1) {
         const RowStream& t = plan.t[__ffs((int)them) - 1];
         const uint8_t* from = t.p + (size_t)stream_row(t.magic, t.shift, row) * t.pitch + (size_t)first_column * t.e;

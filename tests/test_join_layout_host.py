@@ -48,3 +48,40 @@ int main() {
     assert text == "1"
     source = open(os.path.join(ROOT, "paper_2503_12450_gb300", "csrc", "train_api.cu")).read()
     assert "p.ws = join_sums_at(a->workspace)" in source
+
+
+def test_no_piece_of_a_row_is_copied_from_outside_its_tensor(tmp_path):
+    """Pieces of 256 columns, rounded to 16-byte units, at all alignments: those that would reach outside the tensor's bytes
+    are told apart, the last row's one but last among them, where the last has fewer bytes than fill the unit (257 to 262
+    columns of two bytes, 257 and 258 of four); and no others are."""
+    text = _host_program(tmp_path, r"""
+#include <cstdio>
+#include <initializer_list>
+#include "join_host.h"
+int main() {
+  int wrong = 0, inner = 0;
+  for (int e : {1, 2, 4})
+    for (int D : {1, 3, 8, 255, 256, 257, 258, 259, 262, 263, 264, 511, 513, 777, 1281})
+      for (int pad : {0, 1, 3, 8})
+        for (int offset = 0; offset < 16; offset += e)
+          for (int M : {1, 2, 306}) {
+            const uintptr_t base = 4096 + offset;
+            const size_t pitch = (size_t)(D + pad) * e;
+            const uintptr_t end = lm::rows_end(base, M - 1, pitch, D, e);
+            for (int row : {0, 1, M / 2, M - 2, M - 1})
+              for (int c0 = 0; c0 < D && row >= 0 && row < M; c0 += 256) {
+                const int n = (D - c0 < 256 ? D - c0 : 256) * e;
+                const uintptr_t p = base + row * pitch + (size_t)c0 * e;
+                const uintptr_t from = p / 16 * 16, to = (p + n + 15) / 16 * 16;
+                const bool out = from < base || to > base + (M - 1) * pitch + (size_t)D * e;
+                wrong += out != lm::piece_reaches_out(p, n, base, end);
+                inner += out && c0 + 256 < D;
+              }
+          }
+  std::printf("%d %d", wrong, inner > 0);
+}
+""")
+    assert text == "0 1"
+    source = open(os.path.join(ROOT, "paper_2503_12450_gb300", "csrc", "join_rows.cuh")).read()
+    assert "piece_reaches_out(p, bytes, lowest, tensor_end)" in source
+    assert "tensor_end = rows_end(lowest, stream_row(magic, shift, M - 1), pitch, D, t.e)" in source
