@@ -659,19 +659,33 @@ def lazymar_params_destroy(h):
     h.close()
 
 
+def _step_state(t):
+    """The address of a step's state; a tensor of it holds 16 bytes or more, as words of four bytes or as bytes."""
+    f = getattr(t, "data_ptr", None)
+    if f is None:
+        return _ptr(t)
+    if t.element_size() not in (4, 1) or t.nbytes < 16 or not t.is_contiguous():
+        raise LazymarError(1, "state: 16 consecutive bytes as fp32, int32 or uint8 required")
+    return f()
+
+
 def lazymar_grad_norm(h, state, max_norm, scale=1.0, stream=None):
     """state: 16 bytes on the device (norm and factor fp32, steps and skipped int32), zeros before the first step."""
-    _check(lib().lazymar_grad_norm(h.ptr, scale, max_norm, _ptr(state), _stream(stream)))
+    _check(lib().lazymar_grad_norm(h.ptr, scale, max_norm, _step_state(state), _stream(stream)))
 
 
 def lazymar_clip_grads(h, state, stream=None):
-    _check(lib().lazymar_clip_grads(h.ptr, _ptr(state), _stream(stream)))
+    _check(lib().lazymar_clip_grads(h.ptr, _step_state(state), _stream(stream)))
 
 
 def lazymar_adamw(h, state, lr, beta1=0.9, beta2=0.999, eps=1e-8, ema_decay=0.0, lr_device=None, factor=1.0, steps=0,
                   stream=None):
+    """lr_device: a learning rate on the device, an fp32 tensor of one element, in place of lr. state None: factor and
+    steps are the arguments'."""
+    if hasattr(lr_device, "data_ptr") and (lr_device.element_size() != 4 or not lr_device.is_floating_point() or lr_device.numel() != 1):
+        raise LazymarError(1, "lr_device: an fp32 tensor of one element required")
     a = lazymar_adamw_desc(lr, beta1, beta2, eps, ema_decay, _ptr(lr_device), factor, steps)
-    _check(lib().lazymar_adamw(h.ptr, ctypes.byref(a), _ptr(state), _stream(stream)))
+    _check(lib().lazymar_adamw(h.ptr, ctypes.byref(a), _step_state(state), _stream(stream)))
 
 
 class ParamsHandle:

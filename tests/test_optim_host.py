@@ -1,0 +1,50 @@
+"""The end of a training step without a GPU: what the binding and AdamW refuse, against a library that is not called."""
+import pytest
+
+from paper_2503_12450_gb300 import lazymar as lm
+
+torch = pytest.importorskip("torch")
+
+
+class Handle:
+    ptr = 16
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Stands in for the library: counts the calls that reach it."""
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: made.append(name) or 0
+    monkeypatch.setattr(lm, "lib", lambda: Library())
+    return made
+
+
+def test_a_learning_rate_of_another_type_is_refused(calls):
+    """Its bytes would be read as fp32: a rate of 1e-3 in fp64 as 2.4e-13."""
+    for lr in (torch.tensor(1e-3, dtype=torch.float64), torch.tensor([1e-3], dtype=torch.bfloat16), torch.tensor([1]),
+               torch.tensor([1], dtype=torch.int32), torch.tensor([1e-3, 1e-3]), torch.empty(0)):
+        with pytest.raises(lm.LazymarError, match="lr_device"):
+            lm.lazymar_adamw(Handle, torch.zeros(4), 0.0, lr_device=lr)
+    assert not calls
+    for lr in (torch.tensor(1e-3), torch.tensor([1e-3]), torch.tensor([[1e-3]]), None, 4096):
+        lm.lazymar_adamw(Handle, torch.zeros(4), 0.0, lr_device=lr)
+    assert calls == ["lazymar_adamw"] * 5
+
+
+def test_a_state_of_another_type_or_size_is_refused(calls):
+    ways = [lambda s: lm.lazymar_grad_norm(Handle, s, 1.0), lambda s: lm.lazymar_clip_grads(Handle, s),
+            lambda s: lm.lazymar_adamw(Handle, s, 1e-3)]
+    for f in ways:
+        for s in (torch.zeros(4, dtype=torch.float64), torch.zeros(2), torch.zeros(4, dtype=torch.bfloat16), torch.zeros(8)[::2],
+                  torch.zeros(2, dtype=torch.int64), torch.zeros(15, dtype=torch.uint8)):
+            with pytest.raises(lm.LazymarError, match="state"):
+                f(s)
+    assert not calls
+    for f in ways:
+        for s in (torch.zeros(4), torch.zeros(4, dtype=torch.int32), torch.zeros(16, dtype=torch.uint8), torch.zeros((1, 4)), 4096):
+            f(s)
+    assert len(calls) == 15
+    lm.lazymar_adamw(Handle, None, 1e-3, steps=1)
