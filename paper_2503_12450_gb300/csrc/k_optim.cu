@@ -122,8 +122,8 @@ __device__ __forceinline__ void finish_norm(double squares, double scale, double
   const float f = (float)norm;
   state->norm = f;
   if (isfinite(f)) {
-    // (never 0, which says that the step is skipped)
-    state->factor = fmaxf((float)(norm > max_norm ? scale * (max_norm / norm) : scale), 0x1p-126f);
+    // (a subnormal number where gradients are near fp32's end, but never 0, which says that the step is skipped)
+    state->factor = fmaxf((float)(norm > max_norm ? scale * (max_norm / norm) : scale), 0x1p-149f);
     state->steps += 1;
   } else {
     state->factor = 0.f;

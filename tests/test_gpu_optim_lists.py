@@ -39,6 +39,24 @@ def test_norm_around_a_piece(offset, dtype):
         assert abs(norm - want) <= 4 * U * want and abs(factor - f) <= 6 * U * f and steps == 1
 
 
+@pytest.mark.parametrize("scale,most", [(1.0, 1.0), (1.0, 0.25), (2.0 ** -10, 1e-5), (0.5, 3.0)])
+def test_factors_below_the_smallest_normal_number(scale, most):
+    """Gradients near fp32's end: max_norm / norm is subnormal, a multiple of 2^-149, and clips to max_norm all the same."""
+    torch = torch_cuda()
+    g = torch.tensor([2.5e38, -1e38, 3e37, 1e30, 0.0], device="cuda")
+    v = g.double().cpu().numpy()
+    h, s = lm.lazymar_params_create([dict(g=g)]), state()
+    lm.lazymar_grad_norm(h, s, most, scale)
+    want, f = T.clip_factor([v], scale, most)
+    norm, factor, steps, _ = read(s)
+    assert f < 2.0 ** -126 and abs(norm - want) <= 4 * U * want and steps == 1
+    off = 2.0 ** -150 + 4 * U * f  # half a step of fp32's subnormal numbers
+    assert abs(factor - f) <= off
+    lm.lazymar_clip_grads(h, s)
+    sync()
+    close(g, v * f, np.abs(v) * off + U * np.abs(v * f) + 2.0 ** -150)
+
+
 @pytest.mark.parametrize("src,dst", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16"), ("bf16", "fp32")])
 @pytest.mark.parametrize("from_, to", [(0, 1), (3, 0), (1, 2), (7, 4), (5, 5), (0, 0)])
 def test_clip_to_tensors_that_lie_otherwise(from_, to, src, dst):
