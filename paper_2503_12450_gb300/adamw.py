@@ -24,7 +24,7 @@ class AdamW:
         self.p, self.grads = dict(params), dict(grads)
         self.m = {k: torch.zeros_like(v) for k, v in params.items()}
         self.v = {k: torch.zeros_like(v) for k, v in params.items()}
-        self.ema = {k: v.clone() for k, v in params.items()} if ema_decay is not None else None
+        self.ema = {k: v.detach().clone() for k, v in params.items()} if ema_decay is not None else None
         copies = copies or {}
         # norm and factor (fp32), steps taken and skipped (int32)
         self.state = torch.zeros(4, device=next(iter(params.values())).device)

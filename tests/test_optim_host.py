@@ -48,3 +48,25 @@ def test_a_state_of_another_type_or_size_is_refused(calls):
             f(s)
     assert len(calls) == 15
     lm.lazymar_adamw(Handle, None, 1e-3, steps=1)
+
+
+# --------------------------------------------------------------------------
+# AdamW
+# --------------------------------------------------------------------------
+def _adamw(calls, shapes=dict(w=(4, 3), b=(3,)), **kw):
+    from paper_2503_12450_gb300.adamw import AdamW
+    g = torch.Generator().manual_seed(1)
+    p = {k: torch.randn(s, generator=g) for k, s in shapes.items()}
+    return AdamW(p, {k: torch.zeros_like(v) for k, v in p.items()}, 1e-3, **kw)
+
+
+def test_averages_of_parameters_that_ask_for_gradients_have_no_graph(calls):
+    import copy
+
+    from paper_2503_12450_gb300.adamw import AdamW
+    p = {"w": torch.nn.Parameter(torch.ones(4, 3))}
+    opt = AdamW(p, {"w": torch.zeros(4, 3)}, 1e-3, ema_decay=0.9)
+    assert not opt.ema["w"].requires_grad and opt.ema["w"].is_leaf
+    d = copy.deepcopy(opt.state_dict())
+    opt.load_state_dict(d)
+    assert torch.equal(opt.ema["w"], torch.ones(4, 3)) and not opt.ema["w"].requires_grad
