@@ -55,9 +55,14 @@ class AdamW:
         return dict(d, ema={k: v.clone() for k, v in self.ema.items()}) if self.ema else d
 
     def load_state_dict(self, d):
-        if self.ema and "ema" not in d:
-            raise lm.LazymarError(1, "the state has no averaged weights")
+        """What state_dict() gave for the same tensors; nothing is changed where it does not fit."""
+        mine = dict(m=self.m, v=self.v, **({"ema": self.ema} if self.ema else {}))
+        if "state" not in d or d["state"].shape != self.state.shape or d["state"].dtype != self.state.dtype:
+            raise lm.LazymarError(1, "state: four fp32 elements required")
+        for name, tensors in mine.items():
+            if set(d.get(name, ())) != set(tensors) or any(d[name][k].shape != t.shape for k, t in tensors.items()):
+                raise lm.LazymarError(1, "the state's %s: tensors of these names and shapes required" % name)
         self.state.copy_(d["state"])
-        for name in ("m", "v") + (("ema",) if self.ema else ()):
-            for k, t in getattr(self, name).items():
+        for name, tensors in mine.items():
+            for k, t in tensors.items():
                 t.copy_(d[name][k])

@@ -70,3 +70,29 @@ def test_averages_of_parameters_that_ask_for_gradients_have_no_graph(calls):
     d = copy.deepcopy(opt.state_dict())
     opt.load_state_dict(d)
     assert torch.equal(opt.ema["w"], torch.ones(4, 3)) and not opt.ema["w"].requires_grad
+
+
+def test_a_state_that_does_not_fit_is_refused_and_changes_nothing(calls):
+    """Not spread over the tensors, and not loaded in part."""
+    opt = _adamw(calls, ema_decay=0.9)
+    good = opt.state_dict()
+    for k in ("m", "v", "ema"):
+        for t in good[k].values():
+            t.fill_(2.0)
+    good["state"].fill_(3.0)
+    before = {k: [t.clone() for t in ([v] if k == "state" else v.values())] for k, v in opt.state_dict().items()}
+    bad = [dict(good, state=torch.zeros(1)), dict(good, state=torch.zeros(4, dtype=torch.float64)),
+           {k: v for k, v in good.items() if k != "ema"}, {k: v for k, v in good.items() if k != "m"}]
+    for k in ("m", "v", "ema"):
+        bad += [dict(good, **{k: dict(good[k], w=torch.zeros(3))}), dict(good, **{k: dict(good[k], w=torch.zeros(3, 4))}),
+                dict(good, **{k: {"w": good[k]["w"]}}), dict(good, **{k: dict(good[k], other=torch.zeros(1))})]
+    for d in bad:
+        with pytest.raises(lm.LazymarError, match="state"):
+            opt.load_state_dict(d)
+        now = opt.state_dict()
+        assert all(torch.equal(a, b) for k, w in before.items() for a, b in zip([now[k]] if k == "state" else now[k].values(), w))
+    opt.load_state_dict(good)
+    assert all((t == 2.0).all() for k in ("m", "v", "ema") for t in getattr(opt, k).values()) and (opt.state == 3.0).all()
+    plain = _adamw(calls)
+    plain.load_state_dict(good)  # averages that it does not keep are not looked at
+    assert (plain.m["w"] == 2.0).all()
