@@ -20,12 +20,14 @@ class AdamW:
                  copies=None, decays=lambda name, tensor: tensor.dim() > 1):
         if set(params) != set(grads) or not params:
             raise lm.LazymarError(1, "params and grads: the same names, one at least")
+        copies = copies or {}
+        if not set(copies) <= set(params):
+            raise lm.LazymarError(1, "copies: names of params required")
         self.lr, self.betas, self.eps, self.max_norm, self.ema_decay = lr, betas, eps, max_norm, ema_decay
         self.p, self.grads = dict(params), dict(grads)
         self.m = {k: torch.zeros_like(v) for k, v in params.items()}
         self.v = {k: torch.zeros_like(v) for k, v in params.items()}
         self.ema = {k: v.detach().clone() for k, v in params.items()} if ema_decay is not None else None
-        copies = copies or {}
         # norm and factor (fp32), steps taken and skipped (int32)
         self.state = torch.zeros(4, device=next(iter(params.values())).device)
         self.list = lm.lazymar_params_create([dict(

@@ -96,3 +96,10 @@ def test_a_state_that_does_not_fit_is_refused_and_changes_nothing(calls):
     plain = _adamw(calls)
     plain.load_state_dict(good)  # averages that it does not keep are not looked at
     assert (plain.m["w"] == 2.0).all()
+
+
+def test_copies_of_weights_that_are_not_there_are_refused(calls):
+    with pytest.raises(lm.LazymarError, match="copies"):
+        _adamw(calls, copies={"w": torch.zeros((4, 3), dtype=torch.bfloat16), "weight": torch.zeros(3, dtype=torch.bfloat16)})
+    assert not calls
+    _adamw(calls, copies={"w": torch.zeros((4, 3), dtype=torch.bfloat16)})
