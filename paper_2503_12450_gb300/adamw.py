@@ -61,6 +61,8 @@ class AdamW:
         mine = dict(m=self.m, v=self.v, **({"ema": self.ema} if self.ema else {}))
         if "state" not in d or d["state"].shape != self.state.shape or d["state"].dtype != self.state.dtype:
             raise lm.LazymarError(1, "state: four fp32 elements required")
+        if self.ema and "ema" not in d:
+            raise lm.LazymarError(1, "the state has no averaged weights")
         for name, tensors in mine.items():
             if set(d.get(name, ())) != set(tensors) or any(d[name][k].shape != t.shape for k, t in tensors.items()):
                 raise lm.LazymarError(1, "the state's %s: tensors of these names and shapes required" % name)

@@ -91,6 +91,8 @@ def test_a_state_that_does_not_fit_is_refused_and_changes_nothing(calls):
             opt.load_state_dict(d)
         now = opt.state_dict()
         assert all(torch.equal(a, b) for k, w in before.items() for a, b in zip([now[k]] if k == "state" else now[k].values(), w))
+    with pytest.raises(lm.LazymarError, match="no averaged weights"):
+        opt.load_state_dict(_adamw(calls).state_dict())
     opt.load_state_dict(good)
     assert all((t == 2.0).all() for k in ("m", "v", "ema") for t in getattr(opt, k).values()) and (opt.state == 3.0).all()
     plain = _adamw(calls)
