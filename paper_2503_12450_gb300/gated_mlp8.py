@@ -17,14 +17,22 @@ LAYER = lm.LAZYMAR_NORM_LAYER
 
 
 class GatedMlpStack8:
-    """blocks: a list of dicts of fp32 tensors w1 [H, D], b1 [H], w2 [D, H], b2 [D], used where they are if they are contiguous.
+    """blocks: a list of dicts of fp32 tensors w1 [H, D], b1 [H], w2 [D, H], b2 [D], the same
+    H and D in all, used where they are if they are contiguous.
     `p` and `grads` hold them all under names "0.w1" and so on. One workspace, one stream at a time."""
 
     def __init__(self, blocks, eps=1e-6):
+        if not blocks or blocks[0]["w1"].dim() != 2:
+            raise lm.LazymarError(1, "blocks: one at least, w1 [H, D]")
+        H, D = blocks[0]["w1"].shape
+        for i, b in enumerate(blocks):
+            for k, shape in (("w1", (H, D)), ("b1", (H,)), ("w2", (D, H)), ("b2", (D,))):
+                if tuple(b[k].shape) != shape:
+                    raise lm.LazymarError(1, "blocks: %d.%s %s required, as the first block's w1 says" % (i, k, list(shape)))
         self.p = {"%d.%s" % (i, k): b[k].detach().float().contiguous() for i, b in enumerate(blocks) for k in ("w1", "b1", "w2", "b2")}
         self.grads = {k: torch.zeros_like(v) for k, v in self.p.items()}
         self.depth, self.eps = len(blocks), eps
-        self.H, self.D = self.p["0.w1"].shape
+        self.H, self.D = H, D
         dev = self.p["0.w1"].device
         self.w8 = [dict(w1=Tensor8(self.H, self.D, dev, True), w1t=Tensor8(self.D, self.H, dev, True),
                         w2=Tensor8(self.D, self.H, dev, True), w2t=Tensor8(self.H, self.D, dev, True)) for _ in blocks]
