@@ -11,6 +11,7 @@ branch's output behind it, and GELU's input and output; and the norm's output in
 import torch
 
 from . import lazymar as lm
+from . import mlp_block8
 from .mlp_block8 import BF16, F32, Tensor8, _row_stride
 
 LAYER = lm.LAZYMAR_NORM_LAYER
@@ -19,7 +20,8 @@ LAYER = lm.LAZYMAR_NORM_LAYER
 class GatedMlpStack8:
     """blocks: a list of dicts of fp32 tensors w1 [H, D], b1 [H], w2 [D, H], b2 [D], the same
     H and D in all, used where they are if they are contiguous.
-    `p` and `grads` hold them all under names "0.w1" and so on. One workspace, one stream at a time."""
+    `p` and `grads` hold them all under names "0.w1" and so on. One stream at a time. Buffers are those of one number of
+    rows; another number replaces them, except for those that a captured pass has used, which the object keeps."""
 
     def __init__(self, blocks, eps=1e-6):
         if not blocks or blocks[0]["w1"].dim() != 2:
@@ -38,6 +40,7 @@ class GatedMlpStack8:
                         w2=Tensor8(self.D, self.H, dev, True), w2t=Tensor8(self.H, self.D, dev, True)) for _ in blocks]
         self.kept = None  # rows, group and modulation of the forward pass that backward() belongs to
         self.rows = self.serving_rows = None
+        self.captured = []  # buffers that graphs write to
         self.pack()
 
     def pack(self):
@@ -67,6 +70,11 @@ class GatedMlpStack8:
         if M != self.serving_rows:
             self.hs, self.a_s = Tensor8(M, self.D, dev), Tensor8(M, self.H, dev)
             self.serving_rows = M
+
+    def _hold(self, x, train):
+        """Keeps the buffers of a captured pass."""
+        if mlp_block8.capturing(x):
+            self.captured.append((self.x8, self.k, self.dy8, self.du8) if train else (self.hs, self.a_s))
 
     def forward(self, x, mod, group=0, train=True):
         """x [M, D] fp32; mod [ceil(M / group), 3 D depth] (group 0: one row for all), each block's shift, scale and gate in
@@ -108,6 +116,7 @@ class GatedMlpStack8:
                                      None, M, D, H)
         if train:
             self.kept = (M, group, mod)
+        self._hold(x, train)
         return z
 
     def backward(self, dz, accumulate=False):
@@ -119,6 +128,7 @@ class GatedMlpStack8:
         if tuple(dz.shape) != (M, self.D):
             raise lm.LazymarError(1, "dz: [%d, %d], as the forward pass's rows" % (M, self.D))
         _row_stride(dz, self.D, "dz")
+        self._hold(dz, True)
         D, H, dev, g = self.D, self.H, dz.device, self.grads
         parts, dmod = self._modulation(mod, M, group), torch.empty_like(mod, memory_format=torch.contiguous_format)
         dparts = self._modulation(dmod, M, group)

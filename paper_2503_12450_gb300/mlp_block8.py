@@ -27,6 +27,11 @@ class Tensor8:
         return self.q.numel() + self.scale.numel()
 
 
+def capturing(x):
+    """Whether a pass over x is being captured into a graph."""
+    return x.is_cuda and torch.cuda.is_current_stream_capturing()
+
+
 def _row_stride(t, cols, name):
     """The stride of fp32 rows of `cols` consecutive elements; refuses anything else."""
     if t.dim() != 2 or t.shape[1] != cols or t.dtype != torch.float32 or (cols > 1 and t.stride(1) != 1):
@@ -37,7 +42,8 @@ def _row_stride(t, cols, name):
 class MlpBlock8:
     """Parameters and gradients: dicts of fp32 tensors ln_g, ln_b [D], w1 [H, D], b1 [H], w2 [D, H], b2 [D]. Contiguous
     fp32 parameters are used where they are, not copied: an optimizer over them, or over `p`, updates both. An object
-    has one workspace and belongs to one stream at a time."""
+    has one workspace and belongs to one stream at a time. Buffers are those of one number of rows; another number
+    replaces them, except for those that a captured pass has used, which the object keeps."""
 
     def __init__(self, params, eps=1e-6):
         self.p = {k: v.detach().float().contiguous() for k, v in params.items()}
@@ -48,6 +54,7 @@ class MlpBlock8:
         self.w1, self.w1t = Tensor8(self.H, self.D, dev, True), Tensor8(self.D, self.H, dev, True)
         self.w2, self.w2t = Tensor8(self.D, self.H, dev, True), Tensor8(self.H, self.D, dev, True)
         self.rows = self.serving_rows = None  # of the buffers for training, for serving
+        self.captured = []  # buffers that graphs write to
         self.kept = False  # whether a forward pass has left what backward() reads
         self.pack()
 
@@ -75,6 +82,12 @@ class MlpBlock8:
         self.ws = torch.empty(size, dtype=torch.uint8, device=dev)
         self.rows = M
 
+    def _hold(self, x, train):
+        """Keeps the buffers of a captured pass."""
+        if capturing(x):
+            self.captured.append((self.x8, self.h8, self.dy8, self.u8, self.a8, self.du8, self.mean, self.rstd, self.ws) if train
+                                 else (self.h8s, self.a8s))
+
     def saved_bytes(self):
         return sum(t.bytes() for t in (self.x8, self.h8, self.u8, self.a8))
 
@@ -99,6 +112,7 @@ class MlpBlock8:
         lm.lazymar_block8_linear(lm.LAZYMAR_EPI_RESIDUAL, a8.d, self.w2.d, p["b2"], x, ldx, F32, y, D, None, None, M,
                                  D, H)
         self.kept = self.kept or train
+        self._hold(x, train)
         return y
 
     def backward(self, dy, accumulate=False):
@@ -109,6 +123,7 @@ class MlpBlock8:
         if tuple(dy.shape) != (self.rows, self.D):
             raise lm.LazymarError(1, "dy: [%d, %d], as the forward pass's rows" % (self.rows, self.D))
         lddy = _row_stride(dy, self.D, "dy")
+        self._hold(dy, True)
         M, D, H = dy.shape[0], self.D, self.H
         g, ws, n, dev = self.grads, self.ws, self.ws.numel(), dy.device
         dyb = torch.empty((M, -(-D // 8) * 8), dtype=torch.bfloat16, device=dev)
