@@ -604,7 +604,8 @@ typedef struct lazymar_join_args {
   lazymar_rows y;    /* [M, D] fp32, bf16 or E4M3: the branch's output; absent: post, gate, post_g, post_b are too */
   lazymar_rows gate, scale, shift;             /* fp32 or bf16; scale and shift need pre */
   const float *post_g, *post_b, *pre_g, *pre_b; /* [D]; pre_g and pre_b need pre */
-  /* No two outputs in one place; z, h, h8, z8 and y8 may each be x or y itself, with its type and stride, and no other input. */
+  /* No two outputs in one place; z, h, h8, z8 and y8 may each be x or y itself, with its type and stride, and no other input.
+   * An 8-bit tensor's scales count like its bytes, and only with these may they be y's. */
   lazymar_rows z;    /* [M, D] fp32 or bf16 */
   lazymar_rows h;    /* [M, D] fp32 or bf16 */
   lazymar_rows h8, z8, y8; /* E4M3: h as the operand of lazymar_block8_linear, z and y as checkpoints */
@@ -638,7 +639,7 @@ typedef struct lazymar_join_grad_args {
   const float *post_g, *post_b, *pre_g, *pre_b;
   const float *y_mean, *y_rstd, *z_mean, *z_rstd;  /* of the norms that there are; means not with LAZYMAR_NORM_RMS */
   /* Any of these may be absent, dx, dy and dy8 each dz, dh, z or y itself with its type and stride, and no other input;
-   * no two in one place. */
+   * no two in one place (scales as above). */
   lazymar_rows dx;   /* [M, D] fp32 or bf16 */
   lazymar_rows dy;   /* [M, D] fp32 or bf16 */
   lazymar_rows dy8;  /* [M, D] E4M3: dy as the operand of the input gradient's product */

@@ -345,10 +345,11 @@ lazymar_block8 eight_of(const lazymar_rows& r) { return lazymar_block8{r.p, r.sc
 
 // An output in place of an input: rows are worked on side by side, so in another layout they
 // would overwrite rows that are still to be read.
+// (An 8-bit tensor's scales go with it: in place of those of another one they would leave its bytes without theirs.)
+const uint8_t* scale_of(const lazymar_rows& r) { return r.p && r.dtype == LAZYMAR_E4M3 ? r.scale : nullptr; }
 bool displaced(const lazymar_rows& out, const lazymar_rows& in, int M) {
-  return out.p && out.p == in.p &&
-         (out.dtype != in.dtype || (M > 1 && out.ld != in.ld) ||
-          (out.dtype == LAZYMAR_E4M3 && out.scale == in.scale && out.lds != in.lds));
+  if (scale_of(out) && scale_of(out) == scale_of(in) && (out.p != in.p || out.lds != in.lds)) return true;
+  return out.p && out.p == in.p && (out.dtype != in.dtype || (M > 1 && out.ld != in.ld));
 }
 // An output in place of an input that several rows, or several kernels, read.
 bool shared(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
@@ -392,14 +393,16 @@ extern "C" lazymar_status lazymar_join(const lazymar_join_args* a, void* stream)
   if (!a->pre && (a->h.p || a->h8.p || a->scale.p || a->shift.p || a->pre_g || a->pre_b || a->z_mean || a->z_rstd))
     return bad("h, h8, scale, shift, pre_g, pre_b and z's statistics need pre");
   if (!a->x.p) return bad("x: fp32 or bf16 device tensor, ld >= D required");
-  if (twice({a->z.p, a->h.p, a->h8.p, a->z8.p, a->y8.p, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd}))
+  const uint8_t *const h8s = scale_of(a->h8), *const z8s = scale_of(a->z8), *const y8s = scale_of(a->y8);
+  if (twice({a->z.p, a->h.p, a->h8.p, a->z8.p, a->y8.p, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd, h8s, z8s, y8s}))
     return bad("two outputs in one place");
   for (const lazymar_rows* out : {&a->z, &a->h, &a->h8, &a->z8, &a->y8})
     for (const lazymar_rows* in : {&a->x, &a->y})
       if (displaced(*out, *in, a->M)) return bad("an output in place of x or y: the same type and stride required");
-  if (shared({a->z.p, a->h.p, a->h8.p, a->z8.p, a->y8.p, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd},
+  if (shared({a->z.p, a->h.p, a->h8.p, a->z8.p, a->y8.p, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd, h8s, z8s, y8s},
              {a->gate.p, a->scale.p, a->shift.p, a->post_g, a->post_b, a->pre_g, a->pre_b}) ||
-      shared({a->y_mean, a->y_rstd, a->z_mean, a->z_rstd}, {a->x.p, a->y.p}))
+      shared({a->y_mean, a->y_rstd, a->z_mean, a->z_rstd, h8s, z8s, y8s}, {a->x.p, a->y.p}) ||
+      shared({a->z.p, a->h.p, a->h8.p, a->z8.p, a->y8.p, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd}, {scale_of(a->y)}))
     return bad("an output in place of an input other than x or y");
   const int mods = mod_rows(a->M, a->group);
   CHECK_ROWS(x, ROWS_FLOAT, a->M);
@@ -469,15 +472,18 @@ extern "C" lazymar_status lazymar_join_grad(const lazymar_join_grad_args* a, voi
       return bad("pre needs z and its statistics");
     if ((a->post || a->dgate.p || a->dpost_g) && !a->y.p) return bad("post, dgate and dpost_g need y");
     if (a->post && (!a->y_rstd || (a->post == LAZYMAR_NORM_LAYER && !a->y_mean))) return bad("post needs y's statistics");
-    if (twice({a->dx.p, a->dy.p, a->dy8.p, a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b}))
+    const uint8_t* const dy8s = scale_of(a->dy8);
+    if (twice({a->dx.p, a->dy.p, a->dy8.p, dy8s, a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b}))
       return bad("two outputs in one place");
     for (const lazymar_rows* out : {&a->dx, &a->dy, &a->dy8})
       for (const lazymar_rows* in : {&a->dh, &a->dz, &a->z, &a->y})
         if (displaced(*out, *in, a->M)) return bad("dx, dy or dy8 in place of an input: the same type and stride required");
-    if (shared({a->dx.p, a->dy.p, a->dy8.p, a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b},
+    if (shared({a->dx.p, a->dy.p, a->dy8.p, dy8s, a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b},
                {a->gate.p, a->scale.p, a->post_g, a->post_b, a->pre_g, a->pre_b, a->y_mean, a->y_rstd, a->z_mean, a->z_rstd}) ||
-        shared({a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b},
-               {a->dh.p, a->dz.p, a->z.p, a->y.p}))
+        shared({dy8s, a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b},
+               {a->dh.p, a->dz.p, a->z.p, a->y.p}) ||
+        shared({a->dx.p, a->dy.p, a->dy8.p, a->dgate.p, a->dscale.p, a->dshift.p, a->dpost_g, a->dpost_b, a->dpre_g, a->dpre_b},
+               {scale_of(a->z), scale_of(a->y)}))
       return bad("an output in place of an input, other than dx, dy and dy8 of dz, dh, z and y");
     CHECK_ROWS(dh, ROWS_FLOAT, a->M);
     CHECK_ROWS(dz, ROWS_FLOAT, a->M);
