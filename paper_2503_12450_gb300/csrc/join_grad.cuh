@@ -473,6 +473,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, grad_sm_warps(WPR, PLAIN, ROWWI
     }
     if (!ROWWISE && p.group > 0) flush(start, stop);
   }
+  if (dead) drain_ring(plan, bars);
   if (!ROWWISE && p.group > 0) return;
   // One group, or none: the teams' sums in turn, through shared memory, to the CTA's place.
   const unsigned of = ROWWISE ? need.params : need.mods | need.params;

@@ -232,6 +232,7 @@ __global__ void __launch_bounds__(cta_warps(WPR, join_sm_warps(WPR, PLAIN, STREA
     if (p.h.p) store_row<WHOLE>(p.h, row, cols, v);
     if (p.h8.q) store_row8<WHOLE>(p.h8, row, cols, v);
   }
+  if (dead) drain_ring(plan, bars);
 }
 
 template <int WPR, bool PLAIN, bool STREAMED>

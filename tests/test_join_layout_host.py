@@ -85,3 +85,20 @@ int main() {
     source = open(os.path.join(ROOT, "paper_2503_12450_gb300", "csrc", "join_rows.cuh")).read()
     assert "piece_reaches_out(p, bytes, lowest, tensor_end)" in source
     assert "tensor_end = rows_end(lowest, stream_row(magic, shift, M - 1), pitch, D, t.e)" in source
+
+
+def test_rings_wait_for_their_copies_before_a_kernel_leaves_them():
+    """A warp whose wait has run out leaves the loop over its rows with copies under way; each kernel with a ring waits for
+    them, with a limit, before it returns or uses the rings' memory for sums. (What follows a wait that ran out is
+    not run on a GPU: nothing makes one run out without a fault.)"""
+    csrc = os.path.join(ROOT, "paper_2503_12450_gb300", "csrc")
+    for name, after in (("join_ring.cuh", "template <int WPR, bool PLAIN, bool STREAMED>\ncudaError_t join_ring_run"),
+                        ("join_grad.cuh", "float* const mem = reinterpret_cast<float*>(rings);")):
+        source = open(os.path.join(csrc, name)).read()
+        assert source.count("ring.wait(") == 1
+        at = source.index("if (dead) drain_ring(plan, bars);")
+        assert source.index("ring.wait(") < at < source.index(after)
+        loop = source[source.index("ring.wait("):at]
+        assert "return;" not in loop and "break;" not in loop
+    rows = open(os.path.join(csrc, "join_rows.cuh")).read()
+    assert "for (int i = 0; i < 500 && !mbar_try_wait(&bars[s], now); ++i) {}" in rows
